@@ -136,6 +136,9 @@ def prepare(case, seed):
         Tk = sum(lens_k)
         st.update(lens_k=lens_k, cu_k=_offsets(lens_k), causal=case["causal"],
                   q=randn(T, H, d).to(dt), k=randn(Tk, Hk, d).to(dt), v=randn(Tk, Hk, d).to(dt))
+        if own:
+            from paper_2606_27748_gb300 import flexattn
+            st["ws"] = flexattn.softattn_workspace(st["q"], st["k"], st["cu"])
         return st
     common = randn(1, Hk, d)
     A = torch.rand(1, H, device="cuda", generator=gen) * 15.0 + 1.0
@@ -151,9 +154,7 @@ def prepare(case, seed):
         st["dout"] = randn(T, H, d).to(dt)
     if own:
         from paper_2606_27748_gb300 import flexattn
-        if case["call"] == "attn":
-            st["ws"] = flexattn.softattn_workspace(st["q"], st["k"], st["cu"])
-        elif case["call"] != "delta_token":
+        if case["call"] != "delta_token":
             st["ws"] = flexattn.delta_workspace(st["q"], st["v"], st["cu"],
                                                 backward=case["call"] == "delta_train")
     return st
