@@ -211,6 +211,96 @@ int flex_awd_loss_bwd(const flex_shape* shape, const void* q, const void* k, con
                       float* loss, float* dW1, float* dW2, float* dtau, void* ws,
                       size_t ws_bytes, void* stream);
 
+/* ---- packed batches -------------------------------------------------------------------
+ * The entry points below take sequences of different lengths in one call, one after the
+ * other in [T][heads][d] tensors (token-major, as a projection leaves them), instead of
+ * [B][H][N][d].  Offsets are int32 device arrays of n + 1 entries, cu[0] = 0, not
+ * decreasing, cu[n] <= T: sequence i is rows cu[i] .. cu[i + 1] - 1, and may be empty.  Rows
+ * behind the last sequence are neither read into a result nor written.  Offsets outside
+ * [0, T] are clamped to it, so no call reads or writes out of range; what a call computes
+ * from decreasing offsets is not specified.
+ *
+ * q, k and v may be slices of one wider tensor: a row is `*_stride` elements behind the one
+ * before it (at least heads * d, whole 16-byte units); heads and their d elements are
+ * contiguous.  Outputs, gates and gradients are contiguous.  H heads share Hk key heads
+ * (H % Hk == 0): head h uses key head h / (H / Hk). */
+typedef struct {
+    int n;         /* sequences, >= 1 */
+    int T;         /* rows of q and of the output, >= 1 */
+    int Tk;        /* rows of k and v, >= 1 (the delta rule: Tk == T) */
+    int H;         /* heads */
+    int Hk;        /* key heads: of q and k (delta rule), of k and v (softmax attention) */
+    int d;         /* head size of q, k and v: 64 or 128 */
+    int dtype;     /* flex_dtype of every activation */
+    int q_stride;  /* elements from one row of q to the next */
+    int k_stride;
+    int v_stride;
+} flex_packed;
+
+/* Workspace bytes of flex_delta_fwd (backward = 0) or of both flex_delta_fwd and
+ * flex_delta_bwd (backward = 1); 0 if the shape is invalid or unsupported. */
+size_t flex_delta_workspace_bytes(const flex_packed* shape, int backward);
+
+/* Bytes of the buffer that flex_delta_fwd leaves for flex_delta_bwd (its content is the
+ * library's own); 0 if the shape is invalid or unsupported. */
+size_t flex_delta_save_bytes(const flex_packed* shape);
+
+/* Gated delta rule over whole sequences: linear attention whose state is corrected by what
+ * it already holds under a key, instead of only added to.  Per sequence and head, from S = 0
+ * or S0 and with a_t = exp(g_t):
+ *   e_t = v_t - a_t S_{t-1}^T k_t,   S_t = a_t S_{t-1} + beta_t k_t e_t^T,
+ *   out_t = scale S_t^T q_t.
+ * q, k: [T][Hk][d]; v, out: [T][H][d]; g (log decay, <= 0; -inf forgets everything), beta:
+ * [T][H]; all in shape->dtype.  Keys are used as given: with |k|^2 beta <= 2 the state stays
+ * bounded, which unit keys and beta in [0, 1] (or [0, 2]) ensure.  cu: offsets.
+ * S0: NULL or [n][H][d][d] fp32 (key dimension first, as flex_linattn_decode's S); S1: NULL
+ * or the same, receives each sequence's last state (an empty sequence's is its first); S1
+ * may be S0.  save: NULL, or flex_delta_save_bytes() bytes, 256-byte aligned, filled for
+ * flex_delta_bwd; training starts from the zero state, so S0 must then be NULL.
+ * States and sums are fp32; with bf16 storage and long sequences the products run on the
+ * tensor cores with the state and the corrections as bf16 high and low parts.
+ * Errors: FLEX_EINVAL, FLEX_EUNSUPPORTED (d, or more than 65535 sequences), FLEX_EWORKSPACE. */
+int flex_delta_fwd(const flex_packed* shape, const void* q, const void* k, const void* v,
+                   const void* g, const void* beta, const int* cu, float scale,
+                   const float* S0, float* S1, void* out, void* save, void* ws,
+                   size_t ws_bytes, void* stream);
+
+/* Gradients of L = sum(dout * out) of flex_delta_fwd from the zero state, with respect to
+ * all five inputs, each in its input's shape (contiguous) and in shape->dtype; dq and dk are
+ * summed over the heads that share a key head.  save: what flex_delta_fwd left for the same
+ * shape, inputs, offsets and scale.  With D_t the gradient of S_t (later rows included):
+ *   D_t += scale q_t dout_t^T;  dq_t = scale S_t dout_t;  dv_t = beta_t D_t^T k_t;
+ *   dbeta_t = e_t . D_t^T k_t;  dk_t = beta_t D_t e_t - a_t S_{t-1} dv_t;
+ *   dg_t = a_t <S_{t-1}, D_t - k_t dv_t^T>;  D_{t-1} = a_t (D_t - k_t dv_t^T).
+ * Every sum has a fixed order: results repeat bit for bit. */
+int flex_delta_bwd(const flex_packed* shape, const void* q, const void* k, const void* v,
+                   const void* g, const void* beta, const int* cu, float scale,
+                   const void* dout, const void* save, void* dq, void* dk, void* dv, void* dg,
+                   void* dbeta, void* ws, size_t ws_bytes, void* stream);
+
+/* One token of every sequence: the recurrence above for row i of each tensor (T == n; no
+ * offsets, no workspace), on the caller's S [n][H][d][d] fp32, updated in place.  One kernel. */
+int flex_delta_decode(const flex_packed* shape, const void* q, const void* k, const void* v,
+                      const void* g, const void* beta, float scale, float* S, void* out,
+                      void* stream);
+
+/* Workspace bytes needed by flex_softattn_fwd; 0 if the shape is invalid or unsupported. */
+size_t flex_softattn_workspace_bytes(const flex_packed* shape);
+
+/* Softmax attention over packed sequences (the teacher of the distillation loss above, on its
+ * own): out_i = sum_j exp(scale q_i . k_j - lse_i) v_j, lse_i = log sum_j exp(scale q_i . k_j),
+ * j over the keys of i's sequence, or, when causal, those up to i + (Lk - Lq): the last query
+ * sees every key, so the queries may be the next piece of a prompt, or one token, against all
+ * keys so far.  A row that sees no key (Lq > Lk, or no keys) gives out 0 and lse -inf.
+ * q, out: [T][H][d] with offsets cu_q; k, v: [Tk][Hk][d] with offsets cu_k; lse: NULL or
+ * [T][H] fp32.  H / Hk <= 64.  What lies outside a sequence (NaN included) does not reach its
+ * rows; inside it every v must be finite, also where the mask hides it.
+ * Scores, softmax sums and the output's sums are fp32; with bf16 storage the weights enter
+ * the second product as bf16.  1 kernel, or 2 where the keys are split. */
+int flex_softattn_fwd(const flex_packed* shape, const void* q, const void* k, const void* v,
+                      const int* cu_q, const int* cu_k, float scale, int causal, void* out,
+                      float* lse, void* ws, size_t ws_bytes, void* stream);
+
 /* Cumulative number of kernels this library has enqueued in this process (all entry
  * points, all devices).  Lets a caller count the launches inside a timed region. */
 unsigned long long flex_kernel_launches(void);

@@ -120,4 +120,26 @@ cudaError_t launch_tc_awd_bwd(const Problem& p, const void* q, const void* k, co
                               float4* rowstat, float* slots, float* dtau_part, float* dW1,
                               float* dW2, float* dtau, int* status, cudaStream_t s);
 
+// ---- packed batches: gated delta rule and softmax attention ---------------------------
+struct Packed;    // packed.cuh
+struct AttnArgs;  // softattn.cuh
+
+// Token by token in fp32 (any storage type).  e: NULL, or [T][H][d] fp32 for the backward.
+size_t delta_scan_save_floats(const Packed& p);
+size_t delta_scan_ws_floats(const Packed& p);
+cudaError_t launch_delta_scan_fwd(const Packed& p, const void* q, const void* k, const void* v,
+                                  const void* g, const void* beta, const int* cu, float scale,
+                                  const float* S0, float* S1, void* out, float* e, cudaStream_t s);
+cudaError_t launch_delta_scan_bwd(const Packed& p, const void* q, const void* k, const void* g,
+                                  const void* beta, const int* cu, float scale, const void* dout,
+                                  const float* e, void* dq, void* dk, void* dv, void* dg,
+                                  void* dbeta, float* scratch, cudaStream_t s);
+cudaError_t launch_delta_decode(const Packed& p, const void* q, const void* k, const void* v,
+                                const void* g, const void* beta, float scale, float* S, void* out,
+                                cudaStream_t s);
+
+int softattn_splits(const Packed& p);  // ranges of keys per tile of rows (1-32)
+cudaError_t launch_softattn_simt(const AttnArgs& x, cudaStream_t s);
+cudaError_t launch_softattn_join(const AttnArgs& x, cudaStream_t s);
+
 }  // namespace flex

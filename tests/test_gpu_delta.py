@@ -1,0 +1,236 @@
+"""Gated delta rule over packed sequences (flex_delta_fwd / _bwd / _decode) against its
+definition in 64 bits, token by token."""
+import pytest
+import torch
+
+from paper_2606_27748_gb300 import flexattn
+from packed_ref import check, delta_grads, delta_inputs, delta_ref, offsets, rel, tol
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+NAMES = ("q", "k", "v", "g", "beta")
+LENS = [(1,), (2, 0, 3), (63, 64, 65), (0, 130, 1, 0), (200, 17, 128, 5)]
+HEADS = [(1, 1), (4, 2), (3, 1)]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def library():
+    assert torch.cuda.is_available(), "GPU tests need CUDA"
+    from paper_2606_27748_gb300 import build
+    build.build()
+    flexattn.load()
+
+
+def _fwd(x, cu, **kw):
+    return flexattn.delta_fwd(*(x[n] for n in NAMES), cu, **kw)
+
+
+def _bwd(x, cu, **kw):
+    save = flexattn.delta_save(x["q"], x["v"], cu)
+    _fwd(x, cu, save=save, want_state=False, **kw)
+    return flexattn.delta_bwd(*(x[n] for n in NAMES), cu, x["dout"], save, **kw)
+
+
+@pytest.mark.parametrize("lens", LENS, ids=str)
+@pytest.mark.parametrize("H,Hk", HEADS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_forward(lens, H, Hk, d, dtype):
+    x = delta_inputs(lens, H, Hk, d, dtype)
+    out, last = _fwd(x, offsets(lens))
+    ro, rs = delta_ref(x, lens, d ** -0.5)
+    check(out, ro, "out")
+    check(last, rs, "last state", F32)
+
+
+@pytest.mark.parametrize("lens", LENS, ids=str)
+@pytest.mark.parametrize("H,Hk", HEADS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_backward(lens, H, Hk, d, dtype):
+    x = delta_inputs(lens, H, Hk, d, dtype, seed=1)
+    got = _bwd(x, offsets(lens))
+    for name, y, r in zip(NAMES, got, delta_grads(x, lens, d ** -0.5)):
+        if sum(lens) == 1 and name == "g":  # the only row decays a zero state: exactly 0, which
+            assert float(y.abs().max()) <= 1e-5  # two equal sums leave to fp32 rounding
+            continue
+        check(y, r, "d" + name)
+
+
+def test_backward_against_differences():
+    """Central differences of the kernel's own fp32 forward along a direction of each input, a
+    step of h = 2% of the input's norm: the cubic term is h^2 / 6 = 7e-5 of the slope times a
+    curvature of order 10, the outputs' rounding 1e-6 / h = 5e-5: 5e-3 allows both."""
+    lens, H, Hk, d = (70, 33), 2, 1, 64
+    cu = offsets(lens)
+    x = delta_inputs(lens, H, Hk, d, F32, seed=2)
+    got = _bwd(x, cu)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    for name, y in zip(NAMES, got):
+        step = torch.randn(x[name].shape, device="cuda", generator=gen)
+        step = step * (step * y > 0)  # a direction along which the slope does not cancel
+        slope = float((step.double() * y.double()).sum())
+        h = 2e-2 * float(x[name].norm() / step.norm())
+        L = [float((_fwd({**x, name: x[name] + s * h * step}, cu)[0].double()
+                    * x["dout"].double()).sum()) for s in (1, -1)]
+        assert abs((L[0] - L[1]) / (2 * h) - slope) <= 5e-3 * abs(slope), name
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_first_state_and_in_place(d, dtype):
+    lens, H, Hk = (0, 70, 1, 129), 4, 2
+    x, cu = delta_inputs(lens, H, Hk, d, dtype, seed=4), offsets(lens)
+    S0 = torch.randn(len(lens), H, d, d, device="cuda") / d ** 0.5
+    ro, rs = delta_ref(x, lens, 0.3, S0)
+    out, last = _fwd(x, cu, scale=0.3, state=S0)
+    check(out, ro, "out")
+    check(last, rs, "last state", F32)
+    assert torch.equal(last[0], S0[0])  # an empty sequence keeps its state
+    S = S0.clone()
+    out2, last2 = _fwd(x, cu, scale=0.3, state=S, last_state=S)
+    assert last2 is S and torch.equal(S, last) and torch.equal(out2, out)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_pieces_and_single_tokens_continue_a_prompt(d, dtype):
+    """A prompt in two pieces, then token by token, gives what one call gives."""
+    H, Hk, n, lens = 4, 2, 3, (150, 150, 150)
+    x = delta_inputs(lens, H, Hk, d, dtype, seed=5)
+    ro, rs = delta_ref(x, lens, d ** -0.5)
+    by_seq = {m: t.view(n, 150, *t.shape[1:]) for m, t in x.items()}
+    piece = lambda a, b: {m: t[:, a:b].reshape(-1, *t.shape[2:]).contiguous() for m, t in by_seq.items()}  # noqa: E731
+    o1, S = _fwd(piece(0, 67), offsets((67,) * n))
+    o2, S = _fwd(piece(67, 140), offsets((73,) * n), state=S)
+    o3 = []
+    for t in range(140, 150):
+        tok = piece(t, t + 1)
+        o3.append(flexattn.delta_decode(*(tok[m] for m in NAMES), S))
+    got = torch.cat([o1.view(n, 67, H, d), o2.view(n, 73, H, d), torch.stack(o3, 1)], 1)
+    check(got.reshape(-1, H, d), ro, "out")
+    check(S, rs, "state", F32)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n,H,Hk,d", [(1, 1, 1, 64), (5, 4, 2, 128), (33, 6, 3, 64)])
+def test_decode(n, H, Hk, d, dtype):
+    lens = (1,) * n
+    x = delta_inputs(lens, H, Hk, d, dtype, seed=6)
+    S0 = torch.randn(n, H, d, d, device="cuda") / d ** 0.5
+    ro, rs = delta_ref(x, lens, 0.7, S0)
+    S = S0.clone()
+    out = flexattn.delta_decode(*(x[m] for m in NAMES), S, scale=0.7)
+    check(out, ro, "out")
+    check(S, rs, "state", F32)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_slices_of_one_projection_and_rows_behind(dtype):
+    """q, k, v as slices of one wide tensor; rows behind the last sequence hold NaN, are not read
+    into a result and keep what the outputs held."""
+    lens, H, Hk, d = (40, 90), 4, 2, 64
+    T = sum(lens) + 9
+    x, cu = delta_inputs(lens, H, Hk, d, dtype, seed=7, rows_behind=9), offsets(lens)
+    for t in x.values():
+        t[sum(lens):] = float("nan")
+    wide = torch.cat([x[m].reshape(T, -1) for m in ("q", "k", "v")], 1)
+    a = Hk * d
+    y = dict(x, q=wide[:, :a].view(T, Hk, d), k=wide[:, a:2 * a].view(T, Hk, d),
+             v=wide[:, 2 * a:].view(T, H, d))
+    fill = lambda s: torch.full(s, 7.0, dtype=dtype, device="cuda")  # noqa: E731
+    out = fill((T, H, d))
+    save = flexattn.delta_save(y["q"], y["v"], cu)
+    _, last = _fwd(y, cu, out=out, save=save)
+    grads = {"d" + m: fill(x[m].shape) for m in NAMES}
+    flexattn.delta_bwd(*(y[m] for m in NAMES), cu, x["dout"], save, **grads)
+    inner = {m: t[:sum(lens)].contiguous() for m, t in x.items()}
+    ro, rs = delta_ref(inner, lens, d ** -0.5)
+    check(out[:sum(lens)], ro, "out")
+    check(last, rs, "last state", F32)
+    for m, r in zip(NAMES, delta_grads(inner, lens, d ** -0.5)):
+        check(grads["d" + m][:sum(lens)], r, "d" + m)
+    for t in (out, *grads.values()):
+        assert (t[sum(lens):] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("case", ["reset", "no_decay", "beta_0", "beta_1_same_keys", "fast_decay"])
+def test_gates_at_their_ends(case, dtype):
+    """-inf forgets everything, 0 keeps everything, beta 0 writes nothing; equal keys with beta 1
+    overwrite each other; gates that underflow within a few tokens."""
+    lens, H, Hk, d = (140, 65), 2, 1, 64
+    x, cu = delta_inputs(lens, H, Hk, d, dtype, seed=8), offsets(lens)
+    if case == "reset":
+        x["g"][::29] = float("-inf")
+    elif case == "no_decay":
+        x["g"].zero_()
+    elif case == "beta_0":
+        x["beta"][::2] = 0
+    elif case == "beta_1_same_keys":
+        x["beta"].fill_(1)
+        x["k"][:] = x["k"][:1]
+    else:
+        x["g"].fill_(-60.0)
+    out, last = _fwd(x, cu)
+    ro, rs = delta_ref(x, lens, d ** -0.5)
+    check(out, ro, "out")
+    check(last, rs, "last state", F32)
+    got, ref = _bwd(x, cu), delta_grads(x, lens, d ** -0.5)
+    for name, y, r in zip(NAMES, got, ref):
+        # dg is the difference of sums of terms of up to 10, each held to 2e-5, of which nothing
+        # is left: e^-60 of them; or, with one unit key k and beta 1, S_{t-1} = k w^T while
+        # D_t - k dv_t^T = (I - k k^T) D_t is orthogonal to k, so their product is 0.
+        if name == "g" and case in ("fast_decay", "beta_1_same_keys"):
+            assert float(y.abs().max()) <= 2e-4
+            continue
+        check(y, r, "d" + name)
+
+
+def test_repeats_bit_for_bit_on_another_stream_and_in_a_graph():
+    lens, H, Hk, d = (300, 77), 4, 2, 64
+    x, cu = delta_inputs(lens, H, Hk, d, BF16, seed=9), offsets(lens)
+    save = flexattn.delta_save(x["q"], x["v"], cu)
+    ws = flexattn.delta_workspace(x["q"], x["v"], cu, backward=True)
+
+    def both():
+        out, last = _fwd(x, cu, save=save, ws=ws)
+        return (out, last, *flexattn.delta_bwd(*(x[m] for m in NAMES), cu, x["dout"], save, ws=ws))
+
+    first = [t.clone() for t in both()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        again = both()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(first, again))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = both()
+    for n in NAMES:
+        x[n].copy_(x[n].flip(0))
+    graph.replay()
+    flipped = [t.clone() for t in held]
+    assert all(torch.equal(a, b) for a, b in zip(flipped, both()))
+    assert not torch.equal(flipped[0], first[0])
+    flexattn.check_status(ws)
+
+
+def test_rows_of_one_sequence_do_not_depend_on_the_batch():
+    """A sequence alone and inside a batch: within the rounding of the storage."""
+    lens, H, Hk, d = (100, 260, 31), 2, 2, 128
+    x, cu = delta_inputs(lens, H, Hk, d, BF16, seed=10), offsets(lens)
+    out, last = _fwd(x, cu)
+    one = {m: t[100:360].contiguous() for m, t in x.items()}
+    o1, s1 = _fwd(one, offsets((260,)))
+    assert rel(out[100:360], o1) <= tol(BF16) and rel(last[1], s1[0]) <= tol(F32)
+
+
+def test_offsets_out_of_range_stay_inside():
+    """Offsets beyond the tensors are clamped: the call touches no row that is not there."""
+    lens, H, Hk, d = (50, 30), 2, 1, 64
+    x = delta_inputs(lens, H, Hk, d, F32, seed=11)
+    out, _ = _fwd(x, torch.tensor([0, 50, 900], dtype=torch.int32, device="cuda"))
+    ref, _ = _fwd(x, offsets(lens))
+    assert torch.equal(out, ref)

@@ -1,0 +1,187 @@
+"""Softmax attention over packed sequences (flex_softattn_fwd) against its definition in 64
+bits, and beside the operators it is used with."""
+import pytest
+import torch
+
+from paper_2606_27748_gb300 import flexattn
+from packed_ref import check, delta_inputs, offsets, softattn_ref
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module", autouse=True)
+def library():
+    assert torch.cuda.is_available(), "GPU tests need CUDA"
+    from paper_2606_27748_gb300 import build
+    build.build()
+    flexattn.load()
+
+
+def _inputs(lens_q, lens_k, H, Hk, d, dtype, seed=0, behind=0):
+    gen = torch.Generator().manual_seed(seed)
+    r = lambda *s: torch.randn(*s, generator=gen).to(dtype).cuda()  # noqa: E731
+    return (r(sum(lens_q) + behind, H, d), r(sum(lens_k) + behind, Hk, d),
+            r(sum(lens_k) + behind, Hk, d))
+
+
+def _check(q, k, v, lens_q, lens_k, causal, scale=None, **kw):
+    out, lse = flexattn.softattn_fwd(q, k, v, offsets(lens_q), offsets(lens_k), causal=causal,
+                                     scale=scale, **kw)
+    ro, rz = softattn_ref(q, k, v, lens_q, lens_k, scale or q.shape[2] ** -0.5, causal)
+    n = sum(lens_q)
+    empty = torch.isinf(rz)
+    assert (lse[:n][empty] == float("-inf")).all() and (out[:n][empty] == 0).all()
+    check(out[:n], ro, "out")
+    check(lse[:n][~empty], rz[~empty], "lse")
+    return out, lse
+
+
+SAME = [(1,), (2, 0, 3), (127, 128, 129), (0, 300, 1, 0), (513, 64, 90)]
+
+
+@pytest.mark.parametrize("lens", SAME, ids=str)
+@pytest.mark.parametrize("H,Hk", [(1, 1), (4, 2), (3, 1), (7, 1), (16, 2)])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("causal", [True, False])
+def test_prompts(lens, H, Hk, d, dtype, causal):
+    _check(*_inputs(lens, lens, H, Hk, d, dtype), lens, lens, causal)
+
+
+@pytest.mark.parametrize("lens_q,lens_k", [
+    ((1, 1, 1), (1, 700, 64)),          # one token each
+    ((1,), (5000,)),                    # one token against a long prompt: the keys are split
+    ((70, 3, 130), (200, 3, 1000)),     # the next pieces of prompts
+    ((100, 5, 64), (30, 0, 64)),        # rows that see no key
+    ((64, 64), (0, 64)),                # a sequence without keys
+], ids=str)
+@pytest.mark.parametrize("H,Hk,d", [(4, 4, 64), (8, 1, 128), (6, 2, 128), (64, 1, 64)])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("causal", [True, False])
+def test_fewer_or_more_queries_than_keys(lens_q, lens_k, H, Hk, d, dtype, causal):
+    _check(*_inputs(lens_q, lens_k, H, Hk, d, dtype, seed=1), lens_q, lens_k, causal)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_slices_and_what_lies_outside(dtype):
+    """q, k, v as slices of one projection; NaN in the rows behind the last sequence."""
+    lens, H, Hk, d = (100, 75), 4, 2, 64
+    q, k, v = _inputs(lens, lens, H, Hk, d, dtype, seed=2, behind=60)
+    for t in (q, k, v):
+        t[175:] = float("nan")
+    T = q.shape[0]
+    wide = torch.cat([t.reshape(T, -1) for t in (q, k, v)], 1)
+    a, b = H * d, (H + Hk) * d
+    q, k, v = wide[:, :a].view(T, H, d), wide[:, a:b].view(T, Hk, d), wide[:, b:].view(T, Hk, d)
+    out = torch.full((T, H, d), 7.0, dtype=dtype, device="cuda")
+    lse = torch.full((T, H), 7.0, device="cuda")
+    _check(q, k, v, lens, lens, True, out=out, lse=lse)
+    assert (out[175:] == 7.0).all() and (lse[175:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("split", [False, True])
+def test_nan_of_the_next_sequence_stays_there(dtype, split):
+    """A sequence's last tile of keys reaches into the next sequence's rows."""
+    lens_q, lens_k = ((1, 1), (1000, 40)) if split else ((90, 40), (90, 40))
+    q, k, v = _inputs(lens_q, lens_k, 2, 2, 64, dtype, seed=3)
+    k[lens_k[0]:] = float("nan")
+    v[lens_k[0]:] = float("inf")
+    out, lse = flexattn.softattn_fwd(q, k, v, offsets(lens_q), offsets(lens_k))
+    n = lens_q[0]
+    ro, rz = softattn_ref(q, k, v, lens_q[:1], lens_k[:1], 64 ** -0.5, True)
+    check(out[:n], ro, "out")
+    check(lse[:n], rz, "lse")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("scale", [0.0, 30.0, -1.0])
+def test_score_sizes(dtype, scale):
+    """Equal scores, scores of several thousands (all but one weight underflow), negative scale."""
+    lens = (150, 200)
+    q, k, v = _inputs(lens, lens, 2, 1, 64, dtype, seed=4)
+    out, lse = flexattn.softattn_fwd(q, k, v, offsets(lens), scale=scale)
+    ro, rz = softattn_ref(q, k, v, lens, lens, scale, True)
+    # a score of size s carries s 2^-24 sqrt(d) of fp32 rounding, which the weight takes over
+    extra = 2000.0 * 2.0 ** -24 * 8 if scale == 30.0 else 0.0
+    from packed_ref import rel, tol
+    assert rel(out, ro) <= tol(dtype) + extra and rel(lse, rz) <= tol(F32)
+
+
+def test_largest_weight_first_and_last():
+    """The running maximum rises at the first or at the last block of keys by hundreds."""
+    lens = (600,)
+    for at in (0, 599):
+        q, k, v = _inputs(lens, lens, 2, 2, 64, BF16, seed=5)
+        k[at] = 12 * q[599, :].float().mean(0, keepdim=True).to(BF16)
+        k[at] += 8 * k[at].sign()
+        _check(q, k, v, lens, lens, False)
+
+
+def test_other_stream_graph_and_repeat():
+    lens, lens_k = (200, 1, 64), (200, 900, 64)
+    cu, cu_k = offsets(lens), offsets(lens_k)
+    q, k, v = _inputs(lens, lens_k, 8, 2, 128, BF16, seed=6)
+    ws = flexattn.softattn_workspace(q, k, cu)
+    run = lambda: flexattn.softattn_fwd(q, k, v, cu, cu_k, ws=ws)  # noqa: E731
+    first = [t.clone() for t in run()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        again = run()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(first, again))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = run()
+    q.copy_(q.flip(0))
+    graph.replay()
+    flipped = [t.clone() for t in held]
+    assert all(torch.equal(a, b) for a, b in zip(flipped, run()))
+    assert not torch.equal(flipped[0], first[0])
+    flexattn.check_status(ws)
+
+
+def test_teacher_of_the_distillation_loss():
+    """lse is the normaliser that the distillation's teacher uses: with the frequencies at zero
+    the kernel's weights are uniform and the loss is log N for any teacher, and a packed call of
+    equal lengths gives the [B, H, N, d] softmax."""
+    B, H, N, d = 2, 4, 130, 64
+    gen = torch.Generator().manual_seed(7)
+    q, k, v = (torch.randn(B, H, N, d, generator=gen).to(BF16).cuda() for _ in range(3))
+    W = torch.zeros(H, 64, d, device="cuda")
+    loss = flexattn.awd_loss(q, k, W, causal=False)
+    assert (loss - torch.log(torch.tensor(float(N)))).abs().max() < 1e-2
+    rows = lambda t: t.transpose(1, 2).reshape(B * N, H, d).contiguous()  # noqa: E731
+    out, lse = flexattn.softattn_fwd(rows(q), rows(k), rows(v), offsets((N,) * B), causal=False)
+    s = torch.einsum("bhid,bhjd->bhij", q.double(), k.double()) / d ** 0.5
+    want = torch.softmax(s, -1) @ v.double()
+    check(out, rows(want), "out", BF16)
+    check(lse, torch.logsumexp(s, -1).transpose(1, 2).reshape(B * N, H), "lse", F32)
+
+
+def test_a_mixed_stack_on_one_packed_batch():
+    """A delta-rule layer, then a full-attention layer, on one packed batch; then one token more
+    through both, from the state and from the keys so far."""
+    from packed_ref import delta_ref
+    lens, H, Hk, d = (90, 33, 128), 4, 2, 64
+    cu = offsets(lens)
+    x = delta_inputs(lens, H, Hk, d, BF16, seed=8)
+    args = [x[n] for n in ("q", "k", "v", "g", "beta")]
+    mid, S = flexattn.delta_fwd(*args, cu)
+    out, _ = flexattn.softattn_fwd(mid, mid[:, :Hk], mid[:, Hk:], cu)
+    rm, rs = delta_ref(x, lens, d ** -0.5)
+    check(mid, rm, "first layer")
+    ro, _ = softattn_ref(mid, mid[:, :Hk], mid[:, Hk:], lens, lens, d ** -0.5, True)
+    check(out, ro, "second layer")
+    new = delta_inputs((1,) * 3, H, Hk, d, BF16, seed=9)
+    tok = flexattn.delta_decode(*(new[n] for n in ("q", "k", "v", "g", "beta")), S)
+    rt, _ = delta_ref(new, (1,) * 3, d ** -0.5, rs)
+    check(tok, rt, "token, first layer")
+    lens_k = tuple(n + 1 for n in lens)
+    rows = torch.cat([torch.cat([a, b]) for a, b in zip(mid.split(lens), tok.split(1))])
+    o, _ = flexattn.softattn_fwd(tok, rows[:, :Hk], rows[:, Hk:], offsets((1,) * 3), offsets(lens_k))
+    r, _ = softattn_ref(tok, rows[:, :Hk], rows[:, Hk:], (1,) * 3, lens_k, d ** -0.5, True)
+    check(o, r, "token, second layer")
