@@ -138,8 +138,18 @@ cudaError_t launch_delta_decode(const Packed& p, const void* q, const void* k, c
                                 const void* g, const void* beta, float scale, float* S, void* out,
                                 cudaStream_t s);
 
+// On the tensor cores in chunks of 64 tokens: bf16 storage, sequences long enough.
+bool tc_delta_supported(const Packed& p);
+size_t tc_delta_rec_bytes(const Packed& p);  // what the chunks' products leave for the walk
+cudaError_t launch_tc_delta_fwd(const Packed& p, const void* q, const void* k, const void* v,
+                                const void* g, const void* beta, const int* cu, float scale,
+                                const float* S0, float* S1, void* out, void* rec, int* status,
+                                cudaStream_t s);
+
 int softattn_splits(const Packed& p);  // ranges of keys per tile of rows (1-32)
 cudaError_t launch_softattn_simt(const AttnArgs& x, cudaStream_t s);
+bool tc_softattn_supported(const Packed& p);  // tensor cores: bf16 storage
+cudaError_t launch_tc_softattn(const AttnArgs& x, cudaStream_t s);
 cudaError_t launch_softattn_join(const AttnArgs& x, cudaStream_t s);
 
 }  // namespace flex

@@ -59,7 +59,9 @@ constexpr size_t kHeader = sizeof(flex::WsHeader);
 
 size_t delta_ws_bytes(const Packed& p, bool backward)
 {
-    return kHeader + (backward ? flex::align_up(flex::delta_scan_ws_floats(p) * 4, 256) : 0);
+    size_t n = backward ? flex::align_up(flex::delta_scan_ws_floats(p) * 4, 256) : 0;
+    if (flex::tc_delta_supported(p) && flex::tc_delta_rec_bytes(p) > n) n = flex::tc_delta_rec_bytes(p);
+    return kHeader + n;
 }
 size_t delta_save(const Packed& p) { return flex::align_up(flex::delta_scan_save_floats(p) * 4, 256); }
 
@@ -105,6 +107,11 @@ int flex_delta_fwd(const flex_packed* shape, const void* q, const void* k, const
         return FLEX_EINVAL;
     if (save && S0) return FLEX_EINVAL;
     if ((rc = check_ws(ws, ws_bytes, delta_ws_bytes(p, false)))) return rc;
+    if (flex::tc_delta_supported(p) && !save)
+        return counted(2, flex::launch_tc_delta_fwd(p, q, k, v, g, beta, cu, scale, S0, S1, out,
+                                                    (char*)ws + kHeader,
+                                                    &((flex::WsHeader*)ws)->status,
+                                                    (cudaStream_t)stream));
     return counted(1, flex::launch_delta_scan_fwd(p, q, k, v, g, beta, cu, scale, S0, S1, out,
                                                   (float*)save, (cudaStream_t)stream));
 }
@@ -167,7 +174,9 @@ int flex_softattn_fwd(const flex_packed* shape, const void* q, const void* k, co
     x.part_lse = (float*)((char*)x.part + flex::align_up((size_t)x.splits * p.T * p.H * p.d * 4, 256));
     x.status = &((flex::WsHeader*)ws)->status;
     cudaStream_t s = (cudaStream_t)stream;
-    if ((rc = counted(1, flex::launch_softattn_simt(x, s)))) return rc;
+    rc = counted(1, flex::tc_softattn_supported(p) ? flex::launch_tc_softattn(x, s)
+                                                   : flex::launch_softattn_simt(x, s));
+    if (rc) return rc;
     return x.splits > 1 ? counted(1, flex::launch_softattn_join(x, s)) : FLEX_OK;
 }
 

@@ -1,0 +1,393 @@
+// Softmax attention over packed sequences on the tensor cores (bf16 storage, d 64 or 128):
+// out_i = sum_j softmax_j(scale q_i . k_j) v_j, one pass over the keys with the running maximum
+// and sum of every row.
+//
+// A CTA takes two tiles of 128 rows of one sequence and key head.  The G = H / Hk heads that
+// share the key head are rows of a tile (row = token * G + head, 128 / G tokens), so K and V
+// are read once for all of them, and one TMA box (64 elements, G heads, 128 / G tokens) brings
+// a tile in that order.  While one tile's scores are turned into weights, the tensor core works
+// on the other tile:
+//   warps 0-3, 4-7  softmax of tile A, B: a thread per row
+//   warp 8          issues S = Q K^T (tcgen05, both operands in shared memory) and
+//                   O += P V (P as bf16 in tensor memory, over its scores)
+//   warp 9          TMA: Q once, then K and V tiles of 128 keys through a ring of buffers
+// Tensor memory (512 columns): S/P of A and B, O of A and B.
+//
+// The maximum that a row's weights refer to only has to keep them in range: it is raised (and
+// O and the sum rescaled) when the true one exceeds it by more than 2^8, so after the first
+// blocks O is hardly ever touched; the sum and O are exact for any reference.
+#include <cuda.h>
+
+#include "flex_internal.h"
+#include "softattn.cuh"
+#include "tc_util.cuh"
+
+namespace flex {
+namespace {
+
+using namespace tc;
+
+constexpr int kThreads = 320, kKeys = 128;
+constexpr int kWarpMma = 8, kWarpTma = 9;
+constexpr float kSlack = 8.f;  // in powers of two
+
+template <int D>
+struct Lay {
+    static constexpr uint32_t TILE = 128 * D * 2;  // one tile of 128 rows
+    static constexpr int NB = D == 128 ? 5 : 8;    // K and V tiles in flight
+    static constexpr uint32_t Q = 0, KV = 2 * TILE;
+    static constexpr uint32_t SMEM = KV + NB * TILE + 1024;  // + alignment
+    static constexpr int T_S = 0, T_O = 256;
+};
+
+struct Bars {
+    uint64_t q_full[2], full[8], empty[8], s_full[2], p_ready[2], o_full[2];
+};
+
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// 32 lanes x 32 consecutive columns.
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* v)
+{
+    uint32_t r[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,"
+        "%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+          "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+          "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
+          "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]),
+          "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+    tc_softattn_kernel(const __grid_constant__ CUtensorMap tmap_q,
+                       const __grid_constant__ CUtensorMap tmap_k,
+                       const __grid_constant__ CUtensorMap tmap_v, AttnArgs x)
+{
+    using L = Lay<D>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* sm = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    const uint32_t sb = smem_u32(sm);
+    __shared__ Bars bars;
+    __shared__ uint32_t tmem_base_sh;
+    __shared__ volatile int abort_flag;
+
+    const Packed& pk = x.p;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int G = pk.H / pk.Hk, tpt = 128 / G;  // tokens of a tile
+    const int hk = blockIdx.y % pk.Hk, split = blockIdx.y / pk.Hk;
+    int s, block, qlo, qhi, klo, khi;
+    // the last slots first: with the causal mask a sequence's later rows have more keys
+    if (!find_block(x.cu_q, pk.n, pk.T, 2 * tpt, (int)(gridDim.x - 1 - blockIdx.x), s, block, qlo, qhi))
+        return;
+    seq_rows(x.cu_k, s, pk.Tk, klo, khi);
+    const int t0 = block * 2 * tpt, rows_left = qhi - qlo - t0;
+    const int lk = khi - klo, shift = lk - (qhi - qlo);
+    // tokens and key blocks [first, last) of each tile; a tile without tokens takes none
+    const int ntA = min(tpt, rows_left), ntB = min(tpt, max(rows_left - tpt, 0));
+    int firstA, lastA, firstB, lastB;
+    key_range(x, kKeys, lk, t0 + ntA - 1 + shift, split, firstA, lastA);
+    key_range(x, kKeys, lk, t0 + tpt + ntB - 1 + shift, split, firstB, lastB);
+    // The CTA walks over both tiles' blocks.  B's tokens are at most 128 behind A's, so B has at
+    // most one block more in all and its range starts at most one block behind A's start: every
+    // block of the walk belongs to A or to B, once an empty range is put at the other's start.
+    if (ntB == 0) firstB = lastB = firstA;
+    if (firstA == lastA) firstA = lastA = firstB;
+    if (firstB == lastB) firstB = lastB = firstA;
+    const int first = min(firstA, firstB), last = max(lastA, lastB);
+
+    if (tid == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&bars.q_full[i], 1);
+            mbar_init(&bars.s_full[i], 1);
+            mbar_init(&bars.p_ready[i], 4);
+            mbar_init(&bars.o_full[i], 1);
+        }
+        for (int i = 0; i < L::NB; ++i) {
+            mbar_init(&bars.full[i], 1);
+            mbar_init(&bars.empty[i], 1);
+        }
+        abort_flag = 0;
+        fence_mbar_init();
+    }
+    if (warp == kWarpMma) {
+        tmem_alloc(&tmem_base_sh, 512);
+        tmem_relinquish();
+    }
+    fence_before_sync();
+    __syncthreads();
+    fence_after_sync();
+    const uint32_t tm = tmem_base_sh;
+
+    if (warp == kWarpTma) {
+        // ---- Q of both tiles, then K and V of every block: tile 2 i is K of block first + i,
+        // tile 2 i + 1 its V; tile n goes to buffer n % NB ----
+        for (int X = 0; X < (ntB > 0 ? 2 : 1); ++X) {
+            if (first == last) break;
+            wmbar_arrive_expect_tx(&bars.q_full[X], (uint32_t)(tpt * G * D * 2));
+            for (int b = 0; b < D / 64; ++b)
+                wtma_load_3d(sb + L::Q + X * L::TILE + b * 16384, &tmap_q, 64 * b, hk * G,
+                             qlo + t0 + X * tpt, &bars.q_full[X]);
+        }
+        uint32_t ph = 0;  // parity of `empty` per buffer
+        for (int n = 0; n < 2 * (last - first); ++n) {
+            const int buf = n % L::NB;
+            if (n >= L::NB) {
+                if (!bar_wait_w(&bars.empty[buf], (ph >> buf) & 1, &abort_flag, x.status)) break;
+                ph ^= 1u << buf;
+            }
+            const int row = klo + (first + n / 2) * kKeys;
+            wmbar_arrive_expect_tx(&bars.full[buf], L::TILE);
+            for (int b = 0; b < D / 64; ++b)
+                wtma_load_3d(sb + L::KV + buf * L::TILE + b * 16384, n & 1 ? &tmap_v : &tmap_k,
+                             64 * b, hk, row, &bars.full[buf]);
+        }
+    } else if (warp == kWarpMma) {
+        constexpr uint32_t I_S = idesc_bf16(128, kKeys, 0, 0), I_O = idesc_bf16(128, D, 0, 1);
+        auto adv = [](uint64_t d, uint32_t bytes) { return d + (bytes >> 4); };
+        bool ok = true;
+        uint32_t ph_full = 0, ph_p[2] = {0, 0};
+        auto wait_tile = [&](int n) {  // tile n has landed (each tile is waited for once)
+            const int buf = n % L::NB;
+            if (ok) ok = bar_wait_w(&bars.full[buf], (ph_full >> buf) & 1, &abort_flag, x.status);
+            ph_full ^= 1u << buf;
+        };
+        const int f[2] = {firstA, firstB}, l[2] = {lastA, lastB};
+        auto scores = [&](int X, int j) {  // S_X = Q_X K_j^T
+            const uint64_t dq = sdesc(sb + L::Q + X * L::TILE, 16, 1024);
+            const uint64_t dk = sdesc(sb + L::KV + (uint32_t)((2 * (j - first)) % L::NB) * L::TILE, 16, 1024);
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks)
+                wmma_bf16(tm + L::T_S + 128 * X, adv(dq, (ks >> 2) * 16384 + (ks & 3) * 32),
+                          adv(dk, (ks >> 2) * 16384 + (ks & 3) * 32), I_S, ks > 0);
+            wmma_commit(&bars.s_full[X]);
+        };
+        for (int X = 0; X < 2; ++X)
+            if (f[X] < l[X] && ok) ok = bar_wait_w(&bars.q_full[X], 0, &abort_flag, x.status);
+        for (int j = first - 1; j < last && ok; ++j) {
+            const int n = 2 * (j - first);
+            bool have_v = false, have_k = false;
+            for (int X = 0; X < 2; ++X) {
+                if (j >= f[X] && j < l[X]) {
+                    if (!have_v) {
+                        wait_tile(n + 1);
+                        have_v = true;
+                        if (!ok) break;
+                        // rows behind the sequence's end are another's, and 0 * NaN is NaN
+                        if ((j + 1) * kKeys > lk) {
+                            const uint32_t v = sb + L::KV + (uint32_t)((n + 1) % L::NB) * L::TILE;
+                            for (int e = (lk - j * kKeys) * 8 + lane; e < kKeys * 8; e += 32)
+                                for (int b = 0; b < D / 64; ++b)
+                                    st_shared_v4(v + b * 16384 + e * 16, 0, 0, 0, 0);
+                            fence_proxy_async();
+                            __syncwarp();
+                        }
+                    }
+                    ok = bar_wait_w(&bars.p_ready[X], ph_p[X], &abort_flag, x.status);
+                    ph_p[X] ^= 1;
+                    if (!ok) break;
+                    fence_after_sync();
+                    const uint64_t dv = sdesc(sb + L::KV + (uint32_t)((n + 1) % L::NB) * L::TILE, 16384, 1024);
+#pragma unroll
+                    for (int ks = 0; ks < kKeys / 16; ++ks)
+                        wmma_bf16_tmem_a(tm + L::T_O + D * X, tm + L::T_S + 128 * X + 8 * ks,
+                                         adv(dv, ks * 2048), I_O, (j > f[X]) || ks > 0);
+                    if (j + 1 == l[X]) wmma_commit(&bars.o_full[X]);
+                }
+                if (j + 1 >= f[X] && j + 1 < l[X]) {
+                    if (!have_k) {
+                        wait_tile(n + 2);
+                        have_k = true;
+                        if (!ok) break;
+                    }
+                    scores(X, j + 1);
+                }
+            }
+            if (!ok) break;
+            // buffers whose last reader has been issued (each block has a reader among A and B)
+            if (j >= first) wmma_commit(&bars.empty[(n + 1) % L::NB]);
+            if (j + 1 < last) wmma_commit(&bars.empty[(n + 2) % L::NB]);
+        }
+    } else {
+        // ---- softmax: one row per thread ----
+        const int X = warp >> 2, r = tid & 127, fX = X ? firstB : firstA, lX = X ? lastB : lastA;
+        const int nt = X ? ntB : ntA, tok = t0 + X * tpt + r / G;
+        const bool mine = r < nt * G;
+        // keys this row sees; a row of no token takes them all (its result goes nowhere)
+        const int see = !mine || !x.causal ? lk : min(lk, tok + shift + 1);
+        const int see_all = __reduce_min_sync(0xffffffffu, see);
+        const float sign = x.scale < 0.f ? -1.f : 1.f;
+        // a zero scale becomes one that leaves every score at 0 but a masked one at -inf
+        const float c = fmaxf(fabsf(x.scale) * 1.4426950408889634f, 1e-37f);
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21;
+        const uint32_t ts = tm + lanes + L::T_S + 128 * X, to = tm + lanes + L::T_O + D * X;
+        float m = -INFINITY, l = 0.f;  // reference (powers of two) and sum
+        bool ok = true;
+        for (int j = fX; j < lX; ++j) {
+            if (!(ok = bar_wait_w(&bars.s_full[X], (uint32_t)(j - fX) & 1, &abort_flag, x.status))) break;
+            fence_after_sync();
+            float v[kKeys];
+#pragma unroll
+            for (int i = 0; i < kKeys / 32; ++i) tmem_ld32(ts + 32 * i, v + 32 * i);
+            tmem_wait_ld();
+            if (sign < 0.f) {
+#pragma unroll
+                for (int i = 0; i < kKeys; ++i) v[i] = -v[i];
+            }
+            if ((j + 1) * kKeys > see_all) {
+                const int n = see - j * kKeys;
+#pragma unroll
+                for (int i = 0; i < kKeys; ++i) v[i] = i < n ? v[i] : -INFINITY;
+            }
+            float top[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+            for (int i = 4; i < kKeys; ++i) top[i & 3] = fmaxf(top[i & 3], v[i]);
+            const float now = c * fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+            const bool raise = now > m + kSlack;  // (from -inf on the first key seen)
+            if (__any_sync(0xffffffffu, raise)) {
+                const float keep = raise ? ex2(m - now) : 1.f;  // 0 from -inf
+                if (raise) m = now;
+                l *= keep;
+                if (j > fX) {  // S_j was issued after P_{j-1} V_{j-1}: O is complete
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i) {
+                        float o[32];
+                        tmem_ld32(to + 32 * i, o);
+                        tmem_wait_ld();
+                        uint32_t w[16];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(o[16 * h + e] * keep);
+                            tmem_st16(to + 32 * i + 16 * h, w);
+                        }
+                    }
+                }
+            }
+            const float base = m == -INFINITY ? 0.f : -m;
+            float sum[4] = {};
+#pragma unroll
+            for (int i = 0; i < kKeys / 32; ++i) {
+                uint32_t w[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float p0 = ex2(fmaf(v[32 * i + 2 * e], c, base));
+                    const float p1 = ex2(fmaf(v[32 * i + 2 * e + 1], c, base));
+                    sum[e & 1] += p0;
+                    sum[2 + (e & 1)] += p1;
+                    w[e] = pack_bf16(p0, p1);
+                }
+                tmem_st16(ts + 16 * i, w);
+            }
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            tmem_wait_st();
+            fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars.p_ready[X]);
+        }
+        if (ok && fX < lX) ok = bar_wait_w(&bars.o_full[X], 0, &abort_flag, x.status);
+        fence_after_sync();
+        const size_t rows = (size_t)pk.T * pk.H;
+        const size_t row = (size_t)(qlo + tok) * pk.H + hk * G + r % G;
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        if (ok && mine) {
+            const float z = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+            if (x.splits > 1)
+                x.part_lse[split * rows + row] = z;
+            else if (x.lse)
+                x.lse[row] = z;
+        }
+        if (ok) {  // (the loads from tensor memory are the whole warp's)
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+                float o[32] = {};
+                if (fX < lX) {
+                    tmem_ld32(to + 32 * i, o);
+                    tmem_wait_ld();
+                }
+#pragma unroll
+                for (int e = 0; e < 32; ++e) o[e] = l > 0.f ? o[e] * inv : 0.f;
+                if (!mine) continue;
+                if (x.splits > 1) {
+                    float4* dst = (float4*)(x.part + (split * rows + row) * D + 32 * i);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        dst[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                } else {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) w[e] = pack_bf16(o[2 * e], o[2 * e + 1]);
+                    char* dst = (char*)((__nv_bfloat16*)x.out + row * D + 32 * i);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        store_32b(dst + 32 * e, make_uint4(w[8 * e], w[8 * e + 1], w[8 * e + 2], w[8 * e + 3]),
+                                  make_uint4(w[8 * e + 4], w[8 * e + 5], w[8 * e + 6], w[8 * e + 7]));
+                }
+            }
+        }
+        fence_before_sync();
+    }
+    __syncthreads();
+    drain_after_abort(abort_flag);
+    if (warp == kWarpMma) {
+        fence_after_sync();
+        tmem_dealloc(tm, 512);
+    }
+}
+
+// [rows][heads][d] bf16 with a row stride (elements), as boxes of 64 elements, `bh` heads and
+// `bt` rows, 128-byte swizzle: in shared memory row (t, h) of the box is 128 bytes at
+// (t * bh + h) * 128.  Rows outside read as zero.
+bool make_rows_map(CUtensorMap* m, const void* base, int T, int heads, int d, long long stride, int bh,
+                   int bt)
+{
+    EncodeTiledFn enc = encode_fn();
+    if (!enc) return false;
+    cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)heads, (cuuint64_t)T};
+    cuuint64_t strides[2] = {(cuuint64_t)d * 2, (cuuint64_t)stride * 2};
+    cuuint32_t box[3] = {64, (cuuint32_t)bh, (cuuint32_t)bt};
+    cuuint32_t es[3] = {1, 1, 1};
+    return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box,
+               es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D>
+cudaError_t launch(const AttnArgs& x, cudaStream_t s)
+{
+    const Packed& p = x.p;
+    const int G = p.H / p.Hk, tpt = 128 / G;
+    CUtensorMap mq, mk, mv;
+    if (!make_rows_map(&mq, x.q, p.T, p.H, D, p.qs, G, tpt) ||
+        !make_rows_map(&mk, x.k, p.Tk, p.Hk, D, p.ks, 1, kKeys) ||
+        !make_rows_map(&mv, x.v, p.Tk, p.Hk, D, p.vs, 1, kKeys))
+        return cudaErrorInvalidValue;
+    const int smem = (int)Lay<D>::SMEM;
+    cudaError_t e = cudaFuncSetAttribute(tc_softattn_kernel<D>,
+                                         cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    const dim3 grid((unsigned)block_slots(p.T, p.n, 2 * tpt), (unsigned)(p.Hk * x.splits));
+    return launch_after(tc_softattn_kernel<D>, grid, kThreads, smem, 0, false, s, mq, mk, mv, x);
+}
+
+}  // namespace
+
+bool tc_softattn_supported(const Packed& p) { return p.bf16 && (p.d == 64 || p.d == 128); }
+
+cudaError_t launch_tc_softattn(const AttnArgs& x, cudaStream_t s)
+{
+    return x.p.d == 64 ? launch<64>(x, s) : launch<128>(x, s);
+}
+
+}  // namespace flex

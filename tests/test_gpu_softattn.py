@@ -56,6 +56,8 @@ def test_prompts(lens, H, Hk, d, dtype, causal):
     ((70, 3, 130), (200, 3, 1000)),     # the next pieces of prompts
     ((100, 5, 64), (30, 0, 64)),        # rows that see no key
     ((64, 64), (0, 64)),                # a sequence without keys
+    ((300, 2), (2000, 3000)),           # ranges of keys that end at different rows
+    ((5, 6, 7), (20000, 130, 1)),       # a sequence far longer than the average
 ], ids=str)
 @pytest.mark.parametrize("H,Hk,d", [(4, 4, 64), (8, 1, 128), (6, 2, 128), (64, 1, 64)])
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
@@ -79,6 +81,21 @@ def test_slices_and_what_lies_outside(dtype):
     lse = torch.full((T, H), 7.0, device="cuda")
     _check(q, k, v, lens, lens, True, out=out, lse=lse)
     assert (out[175:] == 7.0).all() and (lse[175:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_row_strides_off_the_head_size(dtype):
+    """Rows padded by 16 bytes: no multiple of a head's bytes."""
+    lens, H, Hk, d = (130, 70), 4, 2, 128
+    q, k, v = _inputs(lens, lens, H, Hk, d, dtype, seed=10)
+    pad = 16 // q.element_size()
+
+    def padded(t):
+        w = torch.full((t.shape[0], t.shape[1] * d + pad), float("nan"), dtype=dtype, device="cuda")
+        w[:, :-pad] = t.reshape(t.shape[0], -1)
+        return w[:, :-pad].view(*t.shape)
+
+    _check(padded(q), padded(k), padded(v), lens, lens, True)
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
