@@ -52,24 +52,62 @@ __device__ __forceinline__ float ex2(float x)
     return y;
 }
 
-// (a, b) as bf16 pairs hi + lo.
+// (a, b) as bf16 pairs hi + lo, from a packed pair.
+__device__ __forceinline__ void split2(uint64_t ab, uint32_t& hi, uint32_t& lo)
+{
+    float a, b;
+    f2_unpack(ab, a, b);
+    hi = pack_bf16(a, b);
+    const uint64_t h = f2_pack(__uint_as_float(hi << 16), __uint_as_float(hi & 0xffff0000u));
+    f2_unpack(f2_fma(h, f2_pack(-1.f, -1.f), ab), a, b);
+    lo = pack_bf16(a, b);
+}
 __device__ __forceinline__ void split(float a, float b, uint32_t& hi, uint32_t& lo)
 {
-    hi = pack_bf16(a, b);
-    lo = pack_bf16(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xffff0000u));
+    split2(f2_pack(a, b), hi, lo);
 }
 
-__device__ __forceinline__ uint64_t adv(uint64_t d, uint32_t bytes) { return d + (bytes >> 4); }
+// Matrix descriptors as their varying low words (address and leading offset); the high word is
+// the same for all (1024 bytes between groups of 8 rows, 128-byte swizzle), so that an issuing
+// warp keeps one register for each.
+__device__ __forceinline__ uint32_t dlow(uint32_t addr, uint32_t lbo) { return (addr >> 4) | (lbo >> 4) << 16; }
+__device__ __forceinline__ uint64_t desc(uint32_t low, uint32_t bytes)
+{
+    constexpr uint32_t kHigh = (1024u >> 4) | 1u << 14 | 2u << 29;
+    return (uint64_t)kHigh << 32 | (low + (bytes >> 4));
+}
 
 // ---- M, P and the gates' factors of every chunk ------------------------------------------
 // One CTA of 128 threads per (chunk, head).  [K; Q] K^T is one tcgen05 product of 128 rows: rows
-// 0-63 (threads 0-63) K K^T, rows 64-127 Q K^T.  The system is solved in fp32: the two diagonal
-// blocks of 32 by forward substitution, a thread per column with the column in registers; then
-// the block below, M21 = X - M22 (beta X) with X = L21 - L21 (beta M11), by all threads.
+// 0-63 (threads 0-63) K K^T, rows 64-127 Q K^T.  The system is solved in fp32: the four diagonal
+// blocks of 16 by forward substitution, a thread per column with the column in registers; then
+// the blocks of 16, and the block of 32, below, M21 = X - M22 (beta X) with X = L21 - L21 (beta M11).
 struct PrepSmem {
     float L[64][68];  // over the operand tiles, once the product is done
-    float M[64][68];  // columns 32-63 of rows 0-31 hold X
+    float M[64][68];  // X stands where M's upper triangle would
 };
+
+// x[r] -= sum_k a[r][k] beta[k] m[k][0..3], k < K, R rows (pitch 68).
+template <int K, int R>
+__device__ __forceinline__ void minus_product(float4* x, const float* a, const float* m, const float* beta)
+{
+#pragma unroll 2
+    for (int k = 0; k < K; k += 4) {
+        float4 l[R], y[4];
+        const float4 bt = *(const float4*)(beta + k);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = *(const float4*)(m + (k + e) * 68);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            l[r] = *(const float4*)(a + r * 68 + k);
+            l[r].x *= -bt.x; l[r].y *= -bt.y; l[r].z *= -bt.z; l[r].w *= -bt.w;
+            x[r].x = fmaf(l[r].w, y[3].x, fmaf(l[r].z, y[2].x, fmaf(l[r].y, y[1].x, fmaf(l[r].x, y[0].x, x[r].x))));
+            x[r].y = fmaf(l[r].w, y[3].y, fmaf(l[r].z, y[2].y, fmaf(l[r].y, y[1].y, fmaf(l[r].x, y[0].y, x[r].y))));
+            x[r].z = fmaf(l[r].w, y[3].z, fmaf(l[r].z, y[2].z, fmaf(l[r].y, y[1].z, fmaf(l[r].x, y[0].z, x[r].z))));
+            x[r].w = fmaf(l[r].w, y[3].w, fmaf(l[r].z, y[2].w, fmaf(l[r].y, y[1].w, fmaf(l[r].x, y[0].w, x[r].w))));
+        }
+    }
+}
 
 template <int D>
 __global__ void __launch_bounds__(128)
@@ -137,11 +175,11 @@ __global__ void __launch_bounds__(128)
         ok = bar_wait_w(&bar_load, 0, &abort_flag, status);
         if (ok) {
             constexpr uint32_t I = idesc_bf16(128, kC, 0, 0);
-            const uint64_t d = sdesc(sb, 16, 1024);
+            const uint32_t d = dlow(sb, 16);
 #pragma unroll
             for (int ks = 0; ks < D / 16; ++ks) {
                 const uint32_t o = (ks >> 2) * 16384 + (ks & 3) * 32;
-                wmma_bf16(tm, adv(d, o), adv(d, o), I, ks > 0);
+                wmma_bf16(tm, desc(d, o), desc(d, o), I, ks > 0);
             }
             wmma_commit(&bar_mma);
         }
@@ -168,41 +206,50 @@ __global__ void __launch_bounds__(128)
         }
         tmem_wait_ld();
         const float G = Gs[row];
+        const int cols = 32 + 32 * (warp & 1);  // columns up to the diagonal of this warp's rows
+        const bool in = row < n;
         if (tid < 64) {  // L, rows behind the end zero (and with them columns: beta is 0 there)
 #pragma unroll
             for (int j = 0; j < 64; j += 4) {
+                if (j >= cols) break;
+                const float4 gj = *(const float4*)&Gs[j];
+                const float y[4] = {gj.x, gj.y, gj.z, gj.w};
                 float4 x;
-                float* y = &x.x;
+                float* z = &x.x;
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    y[e] = j + e < row && row < n ? v[j + e] * ex2(G - Gs[j + e]) : 0.f;
+                for (int e = 0; e < 4; ++e) z[e] = j + e < row && in ? v[j + e] * ex2(G - y[e]) : 0.f;
                 *(float4*)&w.L[row][j] = x;
             }
         } else {
 #pragma unroll
             for (int j = 0; j < 64; j += 8) {
-                float p[8];
+                uint4 out = make_uint4(0, 0, 0, 0);
+                if (j < cols) {
+                    const float4 g0 = *(const float4*)&Gs[j], g1 = *(const float4*)&Gs[j + 4];
+                    const float y[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
+                    float p[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    p[e] = j + e <= row && row < n ? scale * v[j + e] * ex2(G - Gs[j + e]) : 0.f;
-                *(uint4*)(rec + Rec::P + swz128(row, j)) =
-                    make_uint4(pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]),
-                               pack_bf16(p[6], p[7]));
+                    for (int e = 0; e < 8; ++e)
+                        p[e] = j + e <= row && in ? scale * v[j + e] * ex2(G - y[e]) : 0.f;
+                    out = make_uint4(pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]),
+                                     pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7]));
+                }
+                *(uint4*)(rec + Rec::P + swz128(row, j)) = out;
             }
             const float last = Gs[63];
             float* aux = (float*)rec;
             aux[Rec::GAMMA / 4 + row] = ex2(G);
-            aux[Rec::KAPPA / 4 + row] = row < n ? ex2(last - G) : 0.f;
+            aux[Rec::KAPPA / 4 + row] = in ? ex2(last - G) : 0.f;
             aux[Rec::BETA / 4 + row] = Bs[row];
             if (row == 0) aux[Rec::LAST / 4] = ex2(last);
         }
     }
     __syncthreads();
-    if (tid < 64) {  // column `lane` of diagonal block `warp`: x_i = L_ic - sum_k L_ik beta_k x_k
-        const int b = 32 * warp;
-        float y[32];
+    if (lane < 16) {  // column `lane` of diagonal block `warp`: x_i = L_ic - sum_k L_ik beta_k x_k
+        const int b = 16 * warp;
+        float y[16];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
+        for (int i = 0; i < 16; ++i) {
             float a[4] = {};
 #pragma unroll
             for (int k = 0; k < i; k += 4) {
@@ -218,44 +265,30 @@ __global__ void __launch_bounds__(128)
         }
     }
     __syncthreads();
-    const int i0 = 2 * (tid >> 3), j0 = 4 * (tid & 7);  // 2 rows x 4 columns of the block below
-    auto below = [&](const float (*a)[68], int acol, const float (*x)[68], int xcol, int brow,
-                     float4 (&out)[2]) {  // out = sum_k a[i0 + r][acol + k] beta[brow + k] x[k][xcol + j0 ..]
-        out[0] = out[1] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-        for (int k = 0; k < 32; k += 4) {
-            float4 l[2], m[4];
-            const float4 bt = *(const float4*)&Bs[brow + k];
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                l[r] = *(const float4*)&a[i0 + r][acol + k];
-                l[r].x *= bt.x; l[r].y *= bt.y; l[r].z *= bt.z; l[r].w *= bt.w;
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) m[e] = *(const float4*)&x[k + e][xcol + j0];
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                out[r].x = fmaf(l[r].w, m[3].x, fmaf(l[r].z, m[2].x, fmaf(l[r].y, m[1].x, fmaf(l[r].x, m[0].x, out[r].x))));
-                out[r].y = fmaf(l[r].w, m[3].y, fmaf(l[r].z, m[2].y, fmaf(l[r].y, m[1].y, fmaf(l[r].x, m[0].y, out[r].y))));
-                out[r].z = fmaf(l[r].w, m[3].z, fmaf(l[r].z, m[2].z, fmaf(l[r].y, m[1].z, fmaf(l[r].x, m[0].z, out[r].z))));
-                out[r].w = fmaf(l[r].w, m[3].w, fmaf(l[r].z, m[2].w, fmaf(l[r].y, m[1].w, fmaf(l[r].x, m[0].w, out[r].w))));
-            }
-        }
-    };
-    float4 acc[2], X[2];
-    below(w.L + 32, 0, w.M, 0, 0, acc);
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        const float4 l = *(const float4*)&w.L[32 + i0 + r][j0];
-        X[r] = make_float4(l.x - acc[r].x, l.y - acc[r].y, l.z - acc[r].z, l.w - acc[r].w);
-        *(float4*)&w.M[i0 + r][32 + j0] = X[r];
+    {  // two blocks of 16 below the diagonal, one row x 4 columns a thread
+        const int b = 32 * (tid >> 6), i = (tid & 63) >> 2, j = 4 * (tid & 3);
+        float4 x = *(const float4*)&w.L[b + 16 + i][b + j];
+        minus_product<16, 1>(&x, &w.L[b + 16 + i][b], &w.M[b][b + j], &Bs[b]);
+        *(float4*)&w.M[b + i][b + 16 + j] = x;
+        __syncthreads();
+        minus_product<16, 1>(&x, &w.M[b + 16 + i][b + 16], &w.M[b][b + 16 + j], &Bs[b + 16]);
+        *(float4*)&w.M[b + 16 + i][b + j] = x;
+        __syncthreads();
+        // (X is dead: its place belongs to M's upper triangle, which the products below read as 0)
+        *(float4*)&w.M[b + i][b + 16 + j] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
     __syncthreads();
-    below(w.M + 32, 32, w.M, 32, 32, acc);
-#pragma unroll
-    for (int r = 0; r < 2; ++r)
-        *(float4*)&w.M[32 + i0 + r][j0] = make_float4(X[r].x - acc[r].x, X[r].y - acc[r].y,
-                                                      X[r].z - acc[r].z, X[r].w - acc[r].w);
+    {  // the block of 32 below, two rows x 4 columns a thread
+        const int i = 2 * (tid >> 3), j = 4 * (tid & 7);
+        float4 x[2] = {*(const float4*)&w.L[32 + i][j], *(const float4*)&w.L[33 + i][j]};
+        minus_product<32, 2>(x, &w.L[32 + i][0], &w.M[0][j], &Bs[0]);
+        *(float4*)&w.M[i][32 + j] = x[0];
+        *(float4*)&w.M[i + 1][32 + j] = x[1];
+        __syncthreads();
+        minus_product<32, 2>(x, &w.M[32 + i][32], &w.M[0][32 + j], &Bs[32]);
+        *(float4*)&w.M[32 + i][j] = x[0];
+        *(float4*)&w.M[33 + i][j] = x[1];
+    }
     __syncthreads();
     for (int e = tid; e < 64 * 8; e += 128) {
         const int i = e >> 3, j = (e & 7) * 8;
@@ -263,7 +296,8 @@ __global__ void __launch_bounds__(128)
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             const int a = j + 2 * c;
-            split(a < i ? w.M[i][a] : 0.f, a + 1 < i ? w.M[i][a + 1] : 0.f, mh[c], ml[c]);
+            const float2 m = *(const float2*)&w.M[i][a];
+            split(a < i ? m.x : 0.f, a + 1 < i ? m.y : 0.f, mh[c], ml[c]);
         }
         *(uint4*)(rec + Rec::M_HI + swz128(i, j)) = make_uint4(mh[0], mh[1], mh[2], mh[3]);
         *(uint4*)(rec + Rec::M_LO + swz128(i, j)) = make_uint4(ml[0], ml[1], ml[2], ml[3]);
@@ -275,21 +309,21 @@ __global__ void __launch_bounds__(128)
 
 template <int D>
 struct Walk {
-    static constexpr int THREADS = 448;
-    static constexpr int WARPS = D == 128 ? 8 : 4;  // computing warps (lanes of tensor memory in use)
-    static constexpr int EPI = D == 128 ? 4 : 2;    // output warps
+    static constexpr int QUADS = D / 32;            // quadrants of tensor memory's lanes in use
+    static constexpr int WARPS = 2 * QUADS;         // state warps, and as many token warps
+    static constexpr int PIECES = D / 64;           // of the state: 64 key dimensions each
     static constexpr uint32_t TILE = kC * D * 2;    // 64 rows of K, Q or V
     static constexpr uint32_t K = 0, Q = TILE, V = 2 * TILE, REC = 3 * TILE;
     static constexpr uint32_t STAGE = (REC + Rec::BYTES + 1023) / 1024 * 1024;
     static constexpr int ST = D == 128 ? 3 : 4;
     static constexpr uint32_t SMEM = ST * STAGE + 1024;
     // tensor memory columns: S high, low; the chunk's product (K S, then M (beta R), then P U);
-    // beta R, then kappa U, high and low; U; the state's increment; Q S
-    static constexpr int T_SH = 0, T_SL = D / 2, T_X = D, T_AH = D + 64, T_AL = D + 96, T_U = D + 128,
-                         T_D = D + 160, T_Q = 2 * D + 160;
-    static_assert(2 * D + 224 <= 512, "tensor memory");
+    // beta R, then kappa U, high and low; U high and low; the state's increment; Q S
+    static constexpr int T_SH = 0, T_SL = D / 2, T_X = D, T_AH = D + 64, T_AL = D + 96, T_UH = D + 128,
+                         T_UL = D + 160, T_D = D + 192, T_Q = 2 * D + 192;
+    static_assert(2 * D + 256 <= 512, "tensor memory");
 };
-constexpr int kWalkMma = 12, kWalkTma = 13;
+constexpr int kWalkThreads = 640, kWalkMma = 16, kWalkTma = 17;
 
 struct WalkArgs {
     Packed p;
@@ -303,18 +337,21 @@ struct WalkArgs {
     int* status;
 };
 
-// Warps 0-7 (d = 64: 0, 1, 4, 5) compute: quadrant w % 4 of the lanes, half w / 4 of the tokens
-// (R, U) or of the state's columns, whose fp32 master they hold in registers.  Warps 8-11 (8, 9)
-// write the output, 12 issues the products, 13 loads.  A chunk:
-//   compute  S += last chunk's increment; S high, low -> tensor memory            (s_ready)
-//   issue    X = K S                                                              (x_full)
-//   compute  R = V - e^G X; beta R high, low                                      (r_ready)
-//   issue    X = M (beta R)                                                       (e_full)
-//   compute  E = R - X, U = beta E; e^{G_C - G} U high, low; U                    (u_ready)
-//   issue    increment = (e^{G_C - G} U) K (s_full), then X = P U                 (o_full)
-//   output   scale e^G (Q S) + P U                                                (o_free)
+// State warps (0-7; d = 64: 0, 1, 4, 5) hold the state's fp32 master in registers: quadrant w % 4
+// of the lanes, half w / 4 % 2 of each piece of 64 key dimensions.  Token warps (8-15) work on the
+// chunk's tokens, half of them each, and write the output while the state warps are busy.  Warp
+// 16 issues the products, 17 loads.  A chunk:
+//   state   S += last chunk's increment; S high, low -> tensor memory, by pieces   (s_ready)
+//   issue   X = K S                                                                (x_full)
+//   tokens  R = V - e^G X; beta R high, low                                        (r_ready)
+//   issue   X = M (beta R)                                                         (e_full)
+//   tokens  E = R - X, U = beta E; e^{G_C - G} U and U high, low                   (u_ready)
+//   issue   increment = (e^{G_C - G} U) K, by pieces (s_full), then X = P U        (o_full)
+//   tokens  out = scale e^G (Q S) + P U                                    (x_free, q_free)
+// The pieces let the products of one piece run beside the arithmetic of the other.  (One set of
+// warps for state and tokens needs 168 registers a thread and spills what it holds on the way.)
 template <int D>
-__global__ void __launch_bounds__(Walk<D>::THREADS, 1)
+__global__ void __launch_bounds__(kWalkThreads, 1)
     delta_walk_kernel(const __grid_constant__ CUtensorMap tmap_q,
                       const __grid_constant__ CUtensorMap tmap_k,
                       const __grid_constant__ CUtensorMap tmap_v, WalkArgs x)
@@ -323,8 +360,8 @@ __global__ void __launch_bounds__(Walk<D>::THREADS, 1)
     extern __shared__ uint8_t smem_raw[];
     uint8_t* sm = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     const uint32_t sb = smem_u32(sm);
-    __shared__ uint64_t full[W::ST], empty[W::ST], s_ready, x_full, r_ready, e_full, u_ready, s_full,
-        o_full, o_free;
+    __shared__ uint64_t full[W::ST], empty[W::ST], s_ready[2], s_full[2], x_full, r_ready, e_full,
+        u_ready, o_full, x_free, q_free;
     __shared__ uint32_t tmem_base_sh;
     __shared__ volatile int abort_flag;
 
@@ -339,15 +376,18 @@ __global__ void __launch_bounds__(Walk<D>::THREADS, 1)
     if (tid == 0) {
         for (int i = 0; i < W::ST; ++i) {
             mbar_init(&full[i], 1);
-            mbar_init(&empty[i], W::WARPS + W::EPI + 1);
+            mbar_init(&empty[i], 2 * W::WARPS + 1);
         }
-        mbar_init(&s_ready, W::WARPS);
+        for (int i = 0; i < W::PIECES; ++i) {
+            mbar_init(&s_ready[i], W::WARPS);
+            mbar_init(&s_full[i], 1);
+        }
         mbar_init(&r_ready, W::WARPS);
         mbar_init(&u_ready, W::WARPS);
-        mbar_init(&o_free, W::EPI);
+        mbar_init(&x_free, W::WARPS);
+        mbar_init(&q_free, W::WARPS);
         mbar_init(&x_full, 1);
         mbar_init(&e_full, 1);
-        mbar_init(&s_full, 1);
         mbar_init(&o_full, 1);
         abort_flag = 0;
         fence_mbar_init();
@@ -365,237 +405,278 @@ __global__ void __launch_bounds__(Walk<D>::THREADS, 1)
         return bar_wait_w(&full[c % W::ST], (uint32_t)(c / W::ST) & 1, &abort_flag, x.status);
     };
 
-    if (warp == kWalkTma) {
-        grid_dep_wait();  // the records
-        for (int c = 0; c < chunks; ++c) {
-            uint64_t* bar = &full[c % W::ST];
-            if (c >= W::ST &&
-                !bar_wait_w(&empty[c % W::ST], (uint32_t)(c / W::ST - 1) & 1, &abort_flag, x.status))
-                break;
-            const uint32_t st = sb + stage(c);
-            const int t = lo + c * kC;
-            wmbar_arrive_expect_tx(bar, 3 * W::TILE + Rec::BYTES);
-            for (int b = 0; b < D / 64; ++b) {
-                wtma_load_3d(st + W::K + 8192 * b, &tmap_k, 64 * b, hk, t, bar);
-                wtma_load_3d(st + W::V + 8192 * b, &tmap_v, 64 * b, h, t, bar);
-                wtma_load_3d(st + W::Q + 8192 * b, &tmap_q, 64 * b, hk, t, bar);
+    // registers: launched with 96 a thread; 2 x 104 + 2 x 104 + 64 = 480 = 5 x 96
+    if (warp >= 16) {
+        setmaxnreg_dec<64>();
+        if (warp == kWalkTma) {
+            grid_dep_wait();  // the records
+            for (int c = 0; c < chunks; ++c) {
+                uint64_t* bar = &full[c % W::ST];
+                if (c >= W::ST &&
+                    !bar_wait_w(&empty[c % W::ST], (uint32_t)(c / W::ST - 1) & 1, &abort_flag, x.status))
+                    break;
+                const uint32_t st = sb + stage(c);
+                const int t = lo + c * kC;
+                wmbar_arrive_expect_tx(bar, 3 * W::TILE + Rec::BYTES);
+                for (int b = 0; b < D / 64; ++b) {
+                    wtma_load_3d(st + W::K + 8192 * b, &tmap_k, 64 * b, hk, t, bar);
+                    wtma_load_3d(st + W::V + 8192 * b, &tmap_v, 64 * b, h, t, bar);
+                    wtma_load_3d(st + W::Q + 8192 * b, &tmap_q, 64 * b, hk, t, bar);
+                }
+                if (elect_one())
+                    bulk_load(st + W::REC, x.rec + (rec0 + (size_t)c * pk.H) * Rec::BYTES, Rec::BYTES, bar);
             }
-            if (elect_one())
-                bulk_load(st + W::REC, x.rec + (rec0 + (size_t)c * pk.H) * Rec::BYTES, Rec::BYTES, bar);
-        }
-    } else if (warp == kWalkMma) {
-        constexpr uint32_t I_C = idesc_bf16(128, kC, 0, 0), I_D = idesc_bf16(128, D, 0, 1);
-        bool ok = true;
-        auto wait = [&](uint64_t* bar, int phase) {
-            if (ok) ok = bar_wait_w(bar, (uint32_t)phase & 1, &abort_flag, x.status);
-            fence_after_sync();
-        };
-        for (int c = 0; c < chunks && ok; ++c) {
-            const uint32_t st = sb + stage(c);
-            const int n = hi - lo - c * kC;
-            ok = landed(c);
-            if (!ok) break;
-            if (n < kC) {  // K behind the sequence's end is another's, and 0 * NaN is NaN
-                for (int e = n * 8 + lane; e < kC * 8; e += 32)
-                    for (int b = 0; b < D / 64; ++b)
-                        st_shared_v4(st + W::K + 8192 * b + e * 16, 0, 0, 0, 0);
-                fence_proxy_async();
-                __syncwarp();
-            }
-            const uint64_t dk = sdesc(st + W::K, 16, 1024), dq = sdesc(st + W::Q, 16, 1024);
-            const uint64_t dkn = sdesc(st + W::K, 8192, 1024);
-            const uint64_t dmh = sdesc(st + W::REC + Rec::M_HI, 16, 1024);
-            const uint64_t dml = sdesc(st + W::REC + Rec::M_LO, 16, 1024);
-            const uint64_t dp = sdesc(st + W::REC + Rec::P, 16, 1024);
-            if (c > 0) wait(&o_free, c - 1);  // X and Q S of the last chunk have been read
-            wait(&s_ready, c);
-            if (!ok) break;
+        } else if (warp == kWalkMma) {
+            constexpr uint32_t I_C = idesc_bf16(128, kC, 0, 0), I_D = idesc_bf16(128, 64, 0, 1);
+            bool ok = true;
+            auto wait = [&](uint64_t* bar, int phase) {
+                if (ok) ok = bar_wait_w(bar, (uint32_t)phase & 1, &abort_flag, x.status);
+                fence_after_sync();
+            };
+            for (int c = 0; c < chunks && ok; ++c) {
+                const uint32_t st = sb + stage(c);
+                const int n = hi - lo - c * kC;
+                ok = landed(c);
+                if (!ok) break;
+                if (n < kC) {  // K behind the sequence's end is another's, and 0 * NaN is NaN
+                    for (int e = n * 8 + lane; e < kC * 8; e += 32)
+                        for (int b = 0; b < D / 64; ++b)
+                            st_shared_v4(st + W::K + 8192 * b + e * 16, 0, 0, 0, 0);
+                    fence_proxy_async();
+                    __syncwarp();
+                }
+                const uint32_t dk = dlow(st + W::K, 16), dq = dlow(st + W::Q, 16);
+                const uint32_t dkn = dlow(st + W::K, 8192);
+                const uint32_t dmh = dlow(st + W::REC + Rec::M_HI, 16);
+                const uint32_t dml = dlow(st + W::REC + Rec::M_LO, 16);
+                const uint32_t dp = dlow(st + W::REC + Rec::P, 16);
+                if (c > 0) wait(&x_free, c - 1);  // P U of the last chunk has been read from X
 #pragma unroll
-            for (int ks = 0; ks < D / 8; ++ks) {
-                const int k = ks % (D / 16);
-                wmma_bf16_tmem_a(tm + W::T_X, tm + (ks < D / 16 ? W::T_SH : W::T_SL) + 8 * k,
-                                 adv(dk, (k >> 2) * 8192 + (k & 3) * 32), I_C, ks > 0);
-            }
-            wmma_commit(&x_full);
+                for (int p = 0; p < W::PIECES; ++p) {
+                    wait(&s_ready[p], c);
+                    if (!ok) break;
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k)
-                wmma_bf16_tmem_a(tm + W::T_Q, tm + W::T_SH + 8 * k,
-                                 adv(dq, (k >> 2) * 8192 + (k & 3) * 32), I_C, k > 0);
-            wait(&r_ready, c);
-            if (!ok) break;
+                    for (int ks = 0; ks < 8; ++ks)
+                        wmma_bf16_tmem_a(tm + W::T_X, tm + (ks < 4 ? W::T_SH : W::T_SL) + 32 * p + 8 * (ks & 3),
+                                         desc(dk, 8192 * p + (ks & 3) * 32), I_C, p > 0 || ks > 0);
+                }
+                if (!ok) break;
+                wmma_commit(&x_full);
+                if (c > 0) wait(&q_free, c - 1);
+                if (!ok) break;
 #pragma unroll
-            for (int ks = 0; ks < 12; ++ks) {  // high high, low high, high low
-                const int k = ks & 3;
-                wmma_bf16_tmem_a(tm + W::T_X, tm + (ks >> 2 == 1 ? W::T_AL : W::T_AH) + 8 * k,
-                                 adv(ks >> 2 == 2 ? dml : dmh, k * 32), I_C, ks > 0);
-            }
-            wmma_commit(&e_full);
-            wait(&u_ready, c);
-            if (!ok) break;
+                for (int ks = 0; ks < D / 8; ++ks) {
+                    const int k = ks % (D / 16);
+                    wmma_bf16_tmem_a(tm + W::T_Q, tm + (ks < D / 16 ? W::T_SH : W::T_SL) + 8 * k,
+                                     desc(dq, (k >> 2) * 8192 + (k & 3) * 32), I_C, ks > 0);
+                }
+                wait(&r_ready, c);
+                if (!ok) break;
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks)
-                wmma_bf16_tmem_a(tm + W::T_D, tm + (ks < 4 ? W::T_AH : W::T_AL) + 8 * (ks & 3),
-                                 adv(dkn, (ks & 3) * 2048), I_D, ks > 0);
-            wmma_commit(&s_full);
+                for (int ks = 0; ks < 12; ++ks) {  // high high, low high, high low
+                    const int k = ks & 3;
+                    wmma_bf16_tmem_a(tm + W::T_X, tm + (ks >> 2 == 1 ? W::T_AL : W::T_AH) + 8 * k,
+                                     desc(ks >> 2 == 2 ? dml : dmh, k * 32), I_C, ks > 0);
+                }
+                wmma_commit(&e_full);
+                wait(&u_ready, c);
+                if (!ok) break;
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                wmma_bf16_tmem_a(tm + W::T_X, tm + W::T_U + 8 * k, adv(dp, k * 32), I_C, k > 0);
-            wmma_commit(&o_full);
-            wmma_commit(&empty[c % W::ST]);
-        }
-    } else if (warp >= 8 && (warp & 3) < W::EPI) {
-        // ---- output rows ----
-        const uint32_t lanes = (uint32_t)(warp & 3) << 21;
-        const int v = 32 * (warp & 3) + lane;
-        const size_t os = (size_t)pk.H * D;
-        __nv_bfloat16* out = x.out + (size_t)(lo + (lane & 1)) * os + h * D + (v & ~1);
-        for (int c = 0; c < chunks; ++c) {
-            const float* gamma = (const float*)(sm + stage(c) + W::REC + Rec::GAMMA);
-            if (!landed(c)) break;
-            if (!bar_wait_w(&o_full, (uint32_t)c & 1, &abort_flag, x.status)) break;
-            fence_after_sync();
-            const int n = min(kC, hi - lo - c * kC);
-            float o[kC];
+                for (int p = 0; p < W::PIECES; ++p) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float a[16], b[16];
-                tmem_ld16(tm + lanes + W::T_Q + 16 * i, a);
-                tmem_ld16(tm + lanes + W::T_X + 16 * i, b);
-                tmem_wait_ld();
+                    for (int ks = 0; ks < 8; ++ks)
+                        wmma_bf16_tmem_a(tm + W::T_D + 64 * p, tm + (ks < 4 ? W::T_AH : W::T_AL) + 8 * (ks & 3),
+                                         desc(dkn, 8192 * p + (ks & 3) * 2048), I_D, ks > 0);
+                    wmma_commit(&s_full[p]);
+                }
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o[16 * i + e] = fmaf(x.scale * gamma[16 * i + e], a[e], b[e]);
-            }
-            fence_before_sync();
-            __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(&o_free);
-                mbar_arrive(&empty[c % W::ST]);
-            }
-            // neighbouring lanes exchange halves of two rows: each writes two elements of one row
-#pragma unroll
-            for (int i = 0; i < kC; i += 2) {
-                const float other = __shfl_xor_sync(0xffffffffu, lane & 1 ? o[i] : o[i + 1], 1);
-                const uint32_t w = lane & 1 ? pack_bf16(other, o[i + 1]) : pack_bf16(o[i], other);
-                if (i + (lane & 1) < n) *(uint32_t*)(out + (size_t)(c * kC + i) * os) = w;
+                for (int ks = 0; ks < 8; ++ks)
+                    wmma_bf16_tmem_a(tm + W::T_X, tm + (ks < 4 ? W::T_UH : W::T_UL) + 8 * (ks & 3),
+                                     desc(dp, (ks & 3) * 32), I_C, ks > 0);
+                wmma_commit(&o_full);
+                wmma_commit(&empty[c % W::ST]);
             }
         }
-    } else if (warp < 8 && (warp & 3) < W::EPI) {
-        // ---- the state ----
-        const int half = warp >> 2, v = 32 * (warp & 3) + lane;
-        const uint32_t lanes = (uint32_t)(warp & 3) << 21;
-        const uint32_t vcol = (uint32_t)(v >> 6) * 8192;
-        constexpr int N = D / 2;  // columns of the state a thread holds
-        float S[N];
-        const size_t at = ((size_t)s * pk.H + h) * D * D + (size_t)half * N * D + v;
-#pragma unroll
-        for (int i = 0; i < N; ++i) S[i] = x.S0 ? x.S0[at + (size_t)i * D] : 0.f;
-        float decay = 1.f;
-        bool ok = true;
-        auto increment = [&](int c) {  // S = decay S + the increment of chunk c
-            ok = bar_wait_w(&s_full, (uint32_t)c & 1, &abort_flag, x.status);
-            fence_after_sync();
-#pragma unroll
-            for (int i = 0; i < N / 16; ++i) {
-                float d[16];
-                tmem_ld16(tm + lanes + W::T_D + half * N + 16 * i, d);
-                tmem_wait_ld();
-#pragma unroll
-                for (int e = 0; e < 16; ++e) S[16 * i + e] = fmaf(decay, S[16 * i + e], d[e]);
-            }
-        };
+    } else {
+        setmaxnreg_inc<104>();
+        const int half = (warp >> 2) & 1, v = 32 * (warp & 3) + lane;
+        const uint32_t lanes = tm + ((uint32_t)(warp & 3) << 21);
         auto ready = [&](uint64_t* bar) {
             tmem_wait_st();
             fence_before_sync();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar);
         };
-        for (int c = 0; c < chunks; ++c) {
-            if (c > 0) increment(c - 1);
-            if (!ok) break;
-#pragma unroll
-            for (int i = 0; i < N / 32; ++i) {
-                uint32_t wh[16], wl[16];
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    split(S[32 * i + 2 * e], S[32 * i + 2 * e + 1], wh[e], wl[e]);
-                tmem_st16(tm + lanes + W::T_SH + half * (N / 2) + 16 * i, wh);
-                tmem_st16(tm + lanes + W::T_SL + half * (N / 2) + 16 * i, wl);
-                if (x.s_save) {
-                    uint4* dst = (uint4*)(x.s_save + ((rec0 + (size_t)c * pk.H) * D + v) * D + half * N + 32 * i);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        dst[e] = make_uint4(wh[4 * e], wh[4 * e + 1], wh[4 * e + 2], wh[4 * e + 3]);
-                }
-            }
-            ready(&s_ready);
-            if (!(ok = landed(c))) break;
-            const uint8_t* st = sm + stage(c);
-            const float* aux = (const float*)(st + W::REC) + 32 * half;
-            const int n = hi - lo - c * kC - 32 * half;
-            float R[32];
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                const uint32_t r = 32 * half + i;
-                R[i] = __uint_as_float((uint32_t) * (const uint16_t*)(st + W::V + vcol + swz128(r, v & 63)) << 16);
-            }
-            if (!(ok = bar_wait_w(&x_full, (uint32_t)c & 1, &abort_flag, x.status))) break;
+        bool ok = true;
+        auto wait = [&](uint64_t* bar, int phase) {
+            ok = bar_wait_w(bar, (uint32_t)phase & 1, &abort_flag, x.status);
             fence_after_sync();
+            return ok;
+        };
+        if ((warp & 3) >= W::QUADS) {
+            // (no lane of this quadrant holds a value dimension)
+        } else if (warp < 8) {
+            // ---- the state ----
+            float S[W::PIECES][32];  // key dimensions 64 p + 32 half + 0 .. 31
+            const size_t at = ((size_t)s * pk.H + h) * D * D + (size_t)half * 32 * D + v;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                float d[16];
-                uint32_t wh[8], wl[8];
-                tmem_ld16(tm + lanes + W::T_X + 32 * half + 16 * i, d);
+            for (int p = 0; p < W::PIECES; ++p)
+#pragma unroll
+                for (int i = 0; i < 32; ++i) S[p][i] = x.S0 ? x.S0[at + (size_t)(64 * p + i) * D] : 0.f;
+            float decay = 1.f;
+            for (int c = 0; c <= chunks; ++c) {
+#pragma unroll
+                for (int p = 0; p < W::PIECES; ++p) {
+                    if (c > 0 && !wait(&s_full[p], c - 1)) break;
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        if (c > 0) {  // S = decay S + the increment of the last chunk
+                            float a[16];
+                            tmem_ld16(lanes + W::T_D + 64 * p + 32 * half + 16 * j, a);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) S[p][16 * j + e] = fmaf(decay, S[p][16 * j + e], a[e]);
+                        }
+                        if (c < chunks) {
+                            uint32_t wh[8], wl[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                split(S[p][16 * j + 2 * e], S[p][16 * j + 2 * e + 1], wh[e], wl[e]);
+                            tmem_st8(lanes + W::T_SH + 32 * p + 16 * half + 8 * j, wh);
+                            tmem_st8(lanes + W::T_SL + 32 * p + 16 * half + 8 * j, wl);
+                            if (x.s_save) {
+                                uint4* dst = (uint4*)(x.s_save + ((rec0 + (size_t)c * pk.H) * D + v) * D +
+                                                      64 * p + 32 * half + 16 * j);
+                                dst[0] = make_uint4(wh[0], wh[1], wh[2], wh[3]);
+                                dst[1] = make_uint4(wh[4], wh[5], wh[6], wh[7]);
+                            }
+                        }
+                    }
+                    if (c < chunks) ready(&s_ready[p]);
+                }
+                if (!ok || c == chunks || !(ok = landed(c))) break;
+                decay = *(const float*)(sm + stage(c) + W::REC + Rec::LAST);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&empty[c % W::ST]);
+            }
+            if (ok && x.S1) {
+#pragma unroll
+                for (int p = 0; p < W::PIECES; ++p)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) x.S1[at + (size_t)(64 * p + i) * D] = S[p][i];
+            }
+        } else {
+            // ---- the tokens ----
+            const size_t os = (size_t)pk.H * D;
+            __nv_bfloat16* out = x.out + (size_t)(lo + 32 * half + (lane & 1)) * os + h * D + (v & ~1);
+            for (int c = 0; c < chunks; ++c) {
+                if (!(ok = landed(c))) break;
+                const uint8_t* st = sm + stage(c);
+                const float* aux = (const float*)(st + W::REC) + 32 * half;
+                const int n = hi - lo - c * kC - 32 * half;
+                float R[32];
+                {
+                    const uint8_t* col = st + W::V + (uint32_t)(v >> 6) * 8192 + half * 4096;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        R[i] = __uint_as_float((uint32_t) * (const uint16_t*)(col + swz128(i, v & 63)) << 16);
+                }
+                if (n < 32) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) R[i] = i < n ? R[i] : 0.f;
+                }
+                if (!wait(&x_full, c)) break;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    float d[16];
+                    tmem_ld16(lanes + W::T_X + 32 * half + 16 * j, d);
+                    tmem_wait_ld();
+                    uint32_t wh[8], wl[8];
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {  // (X is 0 behind the end: K is)
+                        const float4 gm = *(const float4*)(aux + Rec::GAMMA / 4 + 16 * j + i);
+                        const float4 bt = *(const float4*)(aux + Rec::BETA / 4 + 16 * j + i);
+                        float* r = R + 16 * j + i;
+                        r[0] = fmaf(-gm.x, d[i], r[0]);
+                        r[1] = fmaf(-gm.y, d[i + 1], r[1]);
+                        r[2] = fmaf(-gm.z, d[i + 2], r[2]);
+                        r[3] = fmaf(-gm.w, d[i + 3], r[3]);
+                        split2(f2_mul(f2_pack(bt.x, bt.y), f2_pack(r[0], r[1])), wh[i / 2], wl[i / 2]);
+                        split2(f2_mul(f2_pack(bt.z, bt.w), f2_pack(r[2], r[3])), wh[i / 2 + 1], wl[i / 2 + 1]);
+                    }
+                    tmem_st8(lanes + W::T_AH + 16 * half + 8 * j, wh);
+                    tmem_st8(lanes + W::T_AL + 16 * half + 8 * j, wl);
+                }
+                ready(&r_ready);
+                if (!wait(&e_full, c)) break;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    float d[16];
+                    tmem_ld16(lanes + W::T_X + 32 * half + 16 * j, d);
+                    tmem_wait_ld();
+                    uint32_t wh[8], wl[8], uh[8], ul[8];
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        const float4 bt = *(const float4*)(aux + Rec::BETA / 4 + 16 * j + i);
+                        const float4 kp = *(const float4*)(aux + Rec::KAPPA / 4 + 16 * j + i);
+                        float* r = R + 16 * j + i;
+                        r[0] -= d[i];
+                        r[1] -= d[i + 1];
+                        r[2] -= d[i + 2];
+                        r[3] -= d[i + 3];
+                        const uint64_t u0 = f2_mul(f2_pack(bt.x, bt.y), f2_pack(r[0], r[1]));
+                        const uint64_t u1 = f2_mul(f2_pack(bt.z, bt.w), f2_pack(r[2], r[3]));
+                        split2(f2_mul(f2_pack(kp.x, kp.y), u0), wh[i / 2], wl[i / 2]);
+                        split2(f2_mul(f2_pack(kp.z, kp.w), u1), wh[i / 2 + 1], wl[i / 2 + 1]);
+                        split2(u0, uh[i / 2], ul[i / 2]);
+                        split2(u1, uh[i / 2 + 1], ul[i / 2 + 1]);
+                    }
+                    tmem_st8(lanes + W::T_AH + 16 * half + 8 * j, wh);
+                    tmem_st8(lanes + W::T_AL + 16 * half + 8 * j, wl);
+                    tmem_st8(lanes + W::T_UH + 16 * half + 8 * j, uh);
+                    tmem_st8(lanes + W::T_UL + 16 * half + 8 * j, ul);
+                }
+                ready(&u_ready);
+                if (x.e_save) {
+                    uint4* dst = (uint4*)(x.e_save + ((rec0 + (size_t)c * pk.H) * D + v) * kC + 32 * half);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        dst[i] = make_uint4(pack_bf16(R[8 * i], R[8 * i + 1]), pack_bf16(R[8 * i + 2], R[8 * i + 3]),
+                                            pack_bf16(R[8 * i + 4], R[8 * i + 5]), pack_bf16(R[8 * i + 6], R[8 * i + 7]));
+                }
+                if (!wait(&o_full, c)) break;
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    tmem_ld16(lanes + W::T_X + 32 * half + 16 * j, *(float(*)[16])(R + 16 * j));
                 tmem_wait_ld();
+                fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&x_free);
+                // neighbouring lanes exchange halves of two rows: each writes two elements of one
+                __nv_bfloat16* dst = out + (size_t)(c * kC) * os;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int t = 16 * i + e;
-                    R[t] = t < n ? fmaf(-aux[Rec::GAMMA / 4 + t], d[e], R[t]) : 0.f;
+                for (int j = 0; j < 2; ++j) {
+                    float d[16];
+                    tmem_ld16(lanes + W::T_Q + 32 * half + 16 * j, d);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 16; e += 2) {
+                        const float2 gm = *(const float2*)(aux + Rec::GAMMA / 4 + 16 * j + e);
+                        const float o0 = fmaf(x.scale * gm.x, d[e], R[16 * j + e]);
+                        const float o1 = fmaf(x.scale * gm.y, d[e + 1], R[16 * j + e + 1]);
+                        const float other = __shfl_xor_sync(0xffffffffu, lane & 1 ? o0 : o1, 1);
+                        const uint32_t w = lane & 1 ? pack_bf16(other, o1) : pack_bf16(o0, other);
+                        if (16 * j + e + (lane & 1) < n) *(uint32_t*)dst = w;
+                        dst += 2 * os;
+                    }
                 }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int t = 16 * i + 2 * e;
-                    split(aux[Rec::BETA / 4 + t] * R[t], aux[Rec::BETA / 4 + t + 1] * R[t + 1], wh[e], wl[e]);
+                fence_before_sync();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(&q_free);
+                    mbar_arrive(&empty[c % W::ST]);
                 }
-                tmem_st8(tm + lanes + W::T_AH + 16 * half + 8 * i, wh);
-                tmem_st8(tm + lanes + W::T_AL + 16 * half + 8 * i, wl);
             }
-            ready(&r_ready);
-            if (!(ok = bar_wait_w(&e_full, (uint32_t)c & 1, &abort_flag, x.status))) break;
-            fence_after_sync();
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                float d[16];
-                uint32_t wh[8], wl[8], wu[8];
-                tmem_ld16(tm + lanes + W::T_X + 32 * half + 16 * i, d);
-                tmem_wait_ld();
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int t = 16 * i + 2 * e;
-                    R[t] -= d[2 * e];
-                    R[t + 1] -= d[2 * e + 1];
-                    const float u0 = aux[Rec::BETA / 4 + t] * R[t], u1 = aux[Rec::BETA / 4 + t + 1] * R[t + 1];
-                    wu[e] = pack_bf16(u0, u1);
-                    split(aux[Rec::KAPPA / 4 + t] * u0, aux[Rec::KAPPA / 4 + t + 1] * u1, wh[e], wl[e]);
-                }
-                tmem_st8(tm + lanes + W::T_AH + 16 * half + 8 * i, wh);
-                tmem_st8(tm + lanes + W::T_AL + 16 * half + 8 * i, wl);
-                tmem_st8(tm + lanes + W::T_U + 16 * half + 8 * i, wu);
-            }
-            decay = *(const float*)(st + W::REC + Rec::LAST);
-            ready(&u_ready);
-            if (lane == 0) mbar_arrive(&empty[c % W::ST]);
-            if (x.e_save) {
-                uint4* dst = (uint4*)(x.e_save + ((rec0 + (size_t)c * pk.H) * D + v) * kC + 32 * half);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    dst[i] = make_uint4(pack_bf16(R[8 * i], R[8 * i + 1]), pack_bf16(R[8 * i + 2], R[8 * i + 3]),
-                                        pack_bf16(R[8 * i + 4], R[8 * i + 5]), pack_bf16(R[8 * i + 6], R[8 * i + 7]));
-            }
-        }
-        if (ok && chunks > 0) increment(chunks - 1);
-        if (ok && x.S1) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) x.S1[at + (size_t)i * D] = S[i];
         }
         fence_before_sync();
     }
@@ -642,7 +723,7 @@ cudaError_t fwd(const Packed& p, const void* q, const void* k, const void* v, co
                          s, mq, mk, p, (const __nv_bfloat16*)g, (const __nv_bfloat16*)beta, x.cu,
                          x.scale, rec, x.status);
     if (e == cudaSuccess)
-        e = launch_after(delta_walk_kernel<D>, dim3((unsigned)(p.n * p.H)), Walk<D>::THREADS, walk, 0,
+        e = launch_after(delta_walk_kernel<D>, dim3((unsigned)(p.n * p.H)), kWalkThreads, walk, 0,
                          true, s, mq, mk, mv, x);
     return e;
 }
