@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(128)
                       const int* __restrict__ cu, float scale, uint8_t* rec, int* status)
 {
     extern __shared__ uint8_t smem_raw[];
-    uint8_t* sm = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    uint8_t* sm = smem_raw + ((0u - smem_u32(smem_raw)) & 1023u);  // (stays a shared-memory pointer)
     const uint32_t sb = smem_u32(sm);
     PrepSmem& w = *reinterpret_cast<PrepSmem*>(sm);
     __shared__ uint64_t bar_load, bar_mma;
@@ -358,7 +358,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
 {
     using W = Walk<D>;
     extern __shared__ uint8_t smem_raw[];
-    uint8_t* sm = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    uint8_t* sm = smem_raw + ((0u - smem_u32(smem_raw)) & 1023u);  // (stays a shared-memory pointer)
     const uint32_t sb = smem_u32(sm);
     __shared__ uint64_t full[W::ST], empty[W::ST], s_ready[2], s_full[2], x_full, r_ready, e_full,
         u_ready, o_full, x_free, q_free;

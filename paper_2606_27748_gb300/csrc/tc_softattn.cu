@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 {
     using L = Lay<D>;
     extern __shared__ uint8_t smem_raw[];
-    uint8_t* sm = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    uint8_t* sm = smem_raw + ((0u - smem_u32(smem_raw)) & 1023u);  // (stays a shared-memory pointer)
     const uint32_t sb = smem_u32(sm);
     __shared__ Bars bars;
     __shared__ uint32_t tmem_base_sh;
