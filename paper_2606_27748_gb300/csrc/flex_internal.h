@@ -140,10 +140,19 @@ cudaError_t launch_delta_decode(const Packed& p, const void* q, const void* k, c
 
 // On the tensor cores in chunks of 64 tokens: bf16 storage, sequences long enough.
 bool tc_delta_supported(const Packed& p);
-size_t tc_delta_rec_bytes(const Packed& p);  // what the chunks' products leave for the walk
+// What a forward leaves for its walk (workspace) or for the backward (save), and the backward's
+// scratch.
+size_t tc_delta_rec_bytes(const Packed& p);
+size_t tc_delta_save_bytes(const Packed& p);
+size_t tc_delta_bwd_bytes(const Packed& p);
+// rec: tc_delta_rec_bytes of workspace, or a save buffer (saving)
 cudaError_t launch_tc_delta_fwd(const Packed& p, const void* q, const void* k, const void* v,
                                 const void* g, const void* beta, const int* cu, float scale,
-                                const float* S0, float* S1, void* out, void* rec, int* status,
+                                const float* S0, float* S1, void* out, void* rec, bool saving,
+                                int* status, cudaStream_t s);
+cudaError_t launch_tc_delta_bwd(const Packed& p, const void* q, const void* k, const int* cu,
+                                float scale, const void* dout, const void* save, void* dq, void* dk,
+                                void* dv, void* dg, void* dbeta, void* scratch, int* status,
                                 cudaStream_t s);
 
 int softattn_splits(const Packed& p);  // ranges of keys per tile of rows (1-32)

@@ -57,13 +57,20 @@ bool gates(const Packed& p, std::initializer_list<const void*> ps)
 
 constexpr size_t kHeader = sizeof(flex::WsHeader);
 
+// The fp32 scans' scratch of the backward, or the tensor-core kernels': the chunks' records
+// (forward without a save buffer), the states' gradients (backward).
 size_t delta_ws_bytes(const Packed& p, bool backward)
 {
-    size_t n = backward ? flex::align_up(flex::delta_scan_ws_floats(p) * 4, 256) : 0;
-    if (flex::tc_delta_supported(p) && flex::tc_delta_rec_bytes(p) > n) n = flex::tc_delta_rec_bytes(p);
-    return kHeader + n;
+    if (!flex::tc_delta_supported(p))
+        return kHeader + (backward ? flex::align_up(flex::delta_scan_ws_floats(p) * 4, 256) : 0);
+    const size_t f = flex::tc_delta_rec_bytes(p), b = backward ? flex::tc_delta_bwd_bytes(p) : 0;
+    return kHeader + flex::align_up(f > b ? f : b, 256);
 }
-size_t delta_save(const Packed& p) { return flex::align_up(flex::delta_scan_save_floats(p) * 4, 256); }
+size_t delta_save(const Packed& p)
+{
+    return flex::align_up(flex::tc_delta_supported(p) ? flex::tc_delta_save_bytes(p)
+                                                      : flex::delta_scan_save_floats(p) * 4, 256);
+}
 
 // Partial outputs, then partial log sums, when the keys are split.
 size_t attn_ws_bytes(const Packed& p)
@@ -107,9 +114,9 @@ int flex_delta_fwd(const flex_packed* shape, const void* q, const void* k, const
         return FLEX_EINVAL;
     if (save && S0) return FLEX_EINVAL;
     if ((rc = check_ws(ws, ws_bytes, delta_ws_bytes(p, false)))) return rc;
-    if (flex::tc_delta_supported(p) && !save)
+    if (flex::tc_delta_supported(p))
         return counted(2, flex::launch_tc_delta_fwd(p, q, k, v, g, beta, cu, scale, S0, S1, out,
-                                                    (char*)ws + kHeader,
+                                                    save ? save : (char*)ws + kHeader, save != nullptr,
                                                     &((flex::WsHeader*)ws)->status,
                                                     (cudaStream_t)stream));
     return counted(1, flex::launch_delta_scan_fwd(p, q, k, v, g, beta, cu, scale, S0, S1, out,
@@ -129,6 +136,11 @@ int flex_delta_bwd(const flex_packed* shape, const void* q, const void* k, const
         return FLEX_EINVAL;
     if (!save || !aligned(save, 256)) return FLEX_EINVAL;
     if ((rc = check_ws(ws, ws_bytes, delta_ws_bytes(p, true)))) return rc;
+    if (flex::tc_delta_supported(p))
+        return counted(2, flex::launch_tc_delta_bwd(p, q, k, cu, scale, dout, save, dq, dk, dv, dg,
+                                                    dbeta, (char*)ws + kHeader,
+                                                    &((flex::WsHeader*)ws)->status,
+                                                    (cudaStream_t)stream));
     return counted(4, flex::launch_delta_scan_bwd(p, q, k, g, beta, cu, scale, dout,
                                                   (const float*)save, dq, dk, dv, dg, dbeta,
                                                   (float*)((char*)ws + kHeader),

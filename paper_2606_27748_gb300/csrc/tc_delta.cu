@@ -37,12 +37,12 @@ constexpr float kLog2e = 1.4426950408889634f;
 // the differences of the sums G have to be finite.
 constexpr float kLeastGate = -88.f;
 
-// What the walk needs of a chunk, as it is copied to shared memory: M's high and low parts and P
-// (64 x 64 bf16, 128-byte rows, swizzled), then e^G, e^{G_C - G}, beta (64 floats each; 0 behind
-// the sequence's end) and e^{G_C}.
+// What the walk needs of a chunk, as it is copied to shared memory: M's low and high parts and P
+// (64 x 64 bf16, 128-byte rows, swizzled), then -e^G, e^{G_C - G}, beta (0 behind the
+// sequence's end), G in powers of two (64 floats each) and e^{G_C}.
 struct Rec {
-    static constexpr uint32_t M_HI = 0, M_LO = 8192, P = 16384, AUX = 24576, BYTES = 25600;
-    static constexpr uint32_t GAMMA = AUX, KAPPA = AUX + 256, BETA = AUX + 512, LAST = AUX + 768;
+    static constexpr uint32_t M_LO = 0, M_HI = 8192, P = 16384, AUX = 24576, BYTES = 25856;
+    static constexpr uint32_t GAMMA = AUX, KAPPA = AUX + 256, BETA = AUX + 512, G = AUX + 768, LAST = AUX + 1024;
 };
 
 __device__ __forceinline__ float ex2(float x)
@@ -75,6 +75,16 @@ __device__ __forceinline__ uint64_t desc(uint32_t low, uint32_t bytes)
 {
     constexpr uint32_t kHigh = (1024u >> 4) | 1u << 14 | 2u << 29;
     return (uint64_t)kHigh << 32 | (low + (bytes >> 4));
+}
+
+// Four products of 16 along K with A in tensor memory (8 columns a step) and B in shared memory
+// (`bstep` bytes a step), into one accumulator.
+__device__ __forceinline__ void mma4(uint32_t d, uint32_t a, uint32_t b_low, uint32_t bstep, uint32_t idesc,
+                                     uint32_t accumulate)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        wmma_bf16_tmem_a(d, a + 8 * i, desc(b_low, bstep * i), idesc, i > 0 ? 1u : accumulate);
 }
 
 // ---- M, P and the gates' factors of every chunk ------------------------------------------
@@ -238,9 +248,10 @@ __global__ void __launch_bounds__(128)
             }
             const float last = Gs[63];
             float* aux = (float*)rec;
-            aux[Rec::GAMMA / 4 + row] = ex2(G);
+            aux[Rec::GAMMA / 4 + row] = -ex2(G);
             aux[Rec::KAPPA / 4 + row] = in ? ex2(last - G) : 0.f;
             aux[Rec::BETA / 4 + row] = Bs[row];
+            aux[Rec::G / 4 + row] = G;
             if (row == 0) aux[Rec::LAST / 4] = ex2(last);
         }
     }
@@ -345,7 +356,7 @@ struct WalkArgs {
 //   issue   X = K S                                                                (x_full)
 //   tokens  R = V - e^G X; beta R high, low                                        (r_ready)
 //   issue   X = M (beta R)                                                         (e_full)
-//   tokens  E = R - X, U = beta E; e^{G_C - G} U and U high, low                   (u_ready)
+//   tokens  E = R - X, U = beta E; e^{G_C - G} U, then U, high, low        (u_ready, p_ready)
 //   issue   increment = (e^{G_C - G} U) K, by pieces (s_full), then X = P U        (o_full)
 //   tokens  out = scale e^G (Q S) + P U                                    (x_free, q_free)
 // The pieces let the products of one piece run beside the arithmetic of the other.  (One set of
@@ -361,7 +372,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
     uint8_t* sm = smem_raw + ((0u - smem_u32(smem_raw)) & 1023u);  // (stays a shared-memory pointer)
     const uint32_t sb = smem_u32(sm);
     __shared__ uint64_t full[W::ST], empty[W::ST], s_ready[2], s_full[2], x_full, r_ready, e_full,
-        u_ready, o_full, x_free, q_free;
+        u_ready, p_ready, o_full, x_free, q_free;
     __shared__ uint32_t tmem_base_sh;
     __shared__ volatile int abort_flag;
 
@@ -384,6 +395,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
         }
         mbar_init(&r_ready, W::WARPS);
         mbar_init(&u_ready, W::WARPS);
+        mbar_init(&p_ready, W::WARPS);
         mbar_init(&x_free, W::WARPS);
         mbar_init(&q_free, W::WARPS);
         mbar_init(&x_full, 1);
@@ -400,6 +412,10 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
     __syncthreads();
     fence_after_sync();
     const uint32_t tm = tmem_base_sh;
+    if (tm != 0 && tid == 0) {  // (cannot be; nothing is issued then)
+        abort_flag = 1;
+        if (x.status) atomicExch(x.status, (int)FLEX_ECUDA);
+    }
     auto stage = [&](int c) { return (uint32_t)(c % W::ST) * W::STAGE; };
     auto landed = [&](int c) {
         return bar_wait_w(&full[c % W::ST], (uint32_t)(c / W::ST) & 1, &abort_flag, x.status);
@@ -426,7 +442,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                 if (elect_one())
                     bulk_load(st + W::REC, x.rec + (rec0 + (size_t)c * pk.H) * Rec::BYTES, Rec::BYTES, bar);
             }
-        } else if (warp == kWalkMma) {
+        } else if (warp == kWalkMma && tm == 0) {  // all of tensor memory starts at its address 0
             constexpr uint32_t I_C = idesc_bf16(128, kC, 0, 0), I_D = idesc_bf16(128, 64, 0, 1);
             bool ok = true;
             auto wait = [&](uint64_t* bar, int phase) {
@@ -455,44 +471,36 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                 for (int p = 0; p < W::PIECES; ++p) {
                     wait(&s_ready[p], c);
                     if (!ok) break;
-#pragma unroll
-                    for (int ks = 0; ks < 8; ++ks)
-                        wmma_bf16_tmem_a(tm + W::T_X, tm + (ks < 4 ? W::T_SH : W::T_SL) + 32 * p + 8 * (ks & 3),
-                                         desc(dk, 8192 * p + (ks & 3) * 32), I_C, p > 0 || ks > 0);
+                    mma4(W::T_X, W::T_SH + 32 * p, dk + 512 * p, 32, I_C, p > 0);
+                    mma4(W::T_X, W::T_SL + 32 * p, dk + 512 * p, 32, I_C, 1);
                 }
                 if (!ok) break;
                 wmma_commit(&x_full);
                 if (c > 0) wait(&q_free, c - 1);
                 if (!ok) break;
 #pragma unroll
-                for (int ks = 0; ks < D / 8; ++ks) {
-                    const int k = ks % (D / 16);
-                    wmma_bf16_tmem_a(tm + W::T_Q, tm + (ks < D / 16 ? W::T_SH : W::T_SL) + 8 * k,
-                                     desc(dq, (k >> 2) * 8192 + (k & 3) * 32), I_C, ks > 0);
+                for (int p = 0; p < W::PIECES; ++p) {
+                    mma4(W::T_Q, W::T_SH + 32 * p, dq + 512 * p, 32, I_C, p > 0);
+                    mma4(W::T_Q, W::T_SL + 32 * p, dq + 512 * p, 32, I_C, 1);
                 }
                 wait(&r_ready, c);
                 if (!ok) break;
-#pragma unroll
-                for (int ks = 0; ks < 12; ++ks) {  // high high, low high, high low
-                    const int k = ks & 3;
-                    wmma_bf16_tmem_a(tm + W::T_X, tm + (ks >> 2 == 1 ? W::T_AL : W::T_AH) + 8 * k,
-                                     desc(ks >> 2 == 2 ? dml : dmh, k * 32), I_C, ks > 0);
-                }
+                mma4(W::T_X, W::T_AH, dmh, 32, I_C, 0);
+                mma4(W::T_X, W::T_AL, dmh, 32, I_C, 1);
+                mma4(W::T_X, W::T_AH, dml, 32, I_C, 1);
                 wmma_commit(&e_full);
                 wait(&u_ready, c);
                 if (!ok) break;
 #pragma unroll
                 for (int p = 0; p < W::PIECES; ++p) {
-#pragma unroll
-                    for (int ks = 0; ks < 8; ++ks)
-                        wmma_bf16_tmem_a(tm + W::T_D + 64 * p, tm + (ks < 4 ? W::T_AH : W::T_AL) + 8 * (ks & 3),
-                                         desc(dkn, 8192 * p + (ks & 3) * 2048), I_D, ks > 0);
+                    mma4(W::T_D + 64 * p, W::T_AH, dkn + 512 * p, 2048, I_D, 0);
+                    mma4(W::T_D + 64 * p, W::T_AL, dkn + 512 * p, 2048, I_D, 1);
                     wmma_commit(&s_full[p]);
                 }
-#pragma unroll
-                for (int ks = 0; ks < 8; ++ks)
-                    wmma_bf16_tmem_a(tm + W::T_X, tm + (ks < 4 ? W::T_UH : W::T_UL) + 8 * (ks & 3),
-                                     desc(dp, (ks & 3) * 32), I_C, ks > 0);
+                wait(&p_ready, c);
+                if (!ok) break;
+                mma4(W::T_X, W::T_UH, dp, 32, I_C, 0);
+                mma4(W::T_X, W::T_UL, dp, 32, I_C, 1);
                 wmma_commit(&o_full);
                 wmma_commit(&empty[c % W::ST]);
             }
@@ -517,13 +525,16 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
             // (no lane of this quadrant holds a value dimension)
         } else if (warp < 8) {
             // ---- the state ----
-            float S[W::PIECES][32];  // key dimensions 64 p + 32 half + 0 .. 31
+            uint64_t S[W::PIECES][16];  // pairs of key dimensions 64 p + 32 half + 0 .. 31
             const size_t at = ((size_t)s * pk.H + h) * D * D + (size_t)half * 32 * D + v;
 #pragma unroll
             for (int p = 0; p < W::PIECES; ++p)
 #pragma unroll
-                for (int i = 0; i < 32; ++i) S[p][i] = x.S0 ? x.S0[at + (size_t)(64 * p + i) * D] : 0.f;
-            float decay = 1.f;
+                for (int i = 0; i < 16; ++i) {
+                    const float* y = x.S0 + at + (size_t)(64 * p + 2 * i) * D;
+                    S[p][i] = x.S0 ? f2_pack(y[0], y[D]) : f2_pack(0.f, 0.f);
+                }
+            uint64_t decay = f2_pack(1.f, 1.f);
             for (int c = 0; c <= chunks; ++c) {
 #pragma unroll
                 for (int p = 0; p < W::PIECES; ++p) {
@@ -535,13 +546,13 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                             tmem_ld16(lanes + W::T_D + 64 * p + 32 * half + 16 * j, a);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) S[p][16 * j + e] = fmaf(decay, S[p][16 * j + e], a[e]);
+                            for (int e = 0; e < 8; ++e)
+                                S[p][8 * j + e] = f2_fma(decay, S[p][8 * j + e], f2_pack(a[2 * e], a[2 * e + 1]));
                         }
                         if (c < chunks) {
                             uint32_t wh[8], wl[8];
 #pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                split(S[p][16 * j + 2 * e], S[p][16 * j + 2 * e + 1], wh[e], wl[e]);
+                            for (int e = 0; e < 8; ++e) split2(S[p][8 * j + e], wh[e], wl[e]);
                             tmem_st8(lanes + W::T_SH + 32 * p + 16 * half + 8 * j, wh);
                             tmem_st8(lanes + W::T_SL + 32 * p + 16 * half + 8 * j, wl);
                             if (x.s_save) {
@@ -555,7 +566,8 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                     if (c < chunks) ready(&s_ready[p]);
                 }
                 if (!ok || c == chunks || !(ok = landed(c))) break;
-                decay = *(const float*)(sm + stage(c) + W::REC + Rec::LAST);
+                const float last = *(const float*)(sm + stage(c) + W::REC + Rec::LAST);
+                decay = f2_pack(last, last);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&empty[c % W::ST]);
             }
@@ -563,7 +575,13 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
 #pragma unroll
                 for (int p = 0; p < W::PIECES; ++p)
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) x.S1[at + (size_t)(64 * p + i) * D] = S[p][i];
+                    for (int i = 0; i < 16; ++i) {
+                        float* y = x.S1 + at + (size_t)(64 * p + 2 * i) * D;
+                        float a, b;
+                        f2_unpack(S[p][i], a, b);
+                        y[0] = a;
+                        y[D] = b;
+                    }
             }
         } else {
             // ---- the tokens ----
@@ -574,16 +592,23 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                 const uint8_t* st = sm + stage(c);
                 const float* aux = (const float*)(st + W::REC) + 32 * half;
                 const int n = hi - lo - c * kC - 32 * half;
-                float R[32];
+                uint64_t R[16];  // pairs of tokens
                 {
                     const uint8_t* col = st + W::V + (uint32_t)(v >> 6) * 8192 + half * 4096;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        R[i] = __uint_as_float((uint32_t) * (const uint16_t*)(col + swz128(i, v & 63)) << 16);
+                    for (int i = 0; i < 16; ++i) {
+                        const uint32_t a = *(const uint16_t*)(col + swz128(2 * i, v & 63));
+                        const uint32_t b = *(const uint16_t*)(col + swz128(2 * i + 1, v & 63));
+                        R[i] = f2_pack(__uint_as_float(a << 16), __uint_as_float(b << 16));
+                    }
                 }
                 if (n < 32) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) R[i] = i < n ? R[i] : 0.f;
+                    for (int i = 0; i < 16; ++i) {
+                        float a, b;
+                        f2_unpack(R[i], a, b);
+                        R[i] = f2_pack(2 * i < n ? a : 0.f, 2 * i + 1 < n ? b : 0.f);
+                    }
                 }
                 if (!wait(&x_full, c)) break;
 #pragma unroll
@@ -593,80 +618,98 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                     tmem_wait_ld();
                     uint32_t wh[8], wl[8];
 #pragma unroll
-                    for (int i = 0; i < 16; i += 4) {  // (X is 0 behind the end: K is)
-                        const float4 gm = *(const float4*)(aux + Rec::GAMMA / 4 + 16 * j + i);
-                        const float4 bt = *(const float4*)(aux + Rec::BETA / 4 + 16 * j + i);
-                        float* r = R + 16 * j + i;
-                        r[0] = fmaf(-gm.x, d[i], r[0]);
-                        r[1] = fmaf(-gm.y, d[i + 1], r[1]);
-                        r[2] = fmaf(-gm.z, d[i + 2], r[2]);
-                        r[3] = fmaf(-gm.w, d[i + 3], r[3]);
-                        split2(f2_mul(f2_pack(bt.x, bt.y), f2_pack(r[0], r[1])), wh[i / 2], wl[i / 2]);
-                        split2(f2_mul(f2_pack(bt.z, bt.w), f2_pack(r[2], r[3])), wh[i / 2 + 1], wl[i / 2 + 1]);
+                    for (int i = 0; i < 8; i += 2) {  // (X is 0 behind the end: K is)
+                        const ulonglong2 gm = *(const ulonglong2*)(aux + Rec::GAMMA / 4 + 16 * j + 2 * i);
+                        const ulonglong2 bt = *(const ulonglong2*)(aux + Rec::BETA / 4 + 16 * j + 2 * i);
+                        uint64_t* r = R + 8 * j + i;
+                        // (e^G holds its negative in the record: R = V - e^G X)
+                        r[0] = f2_fma(gm.x, f2_pack(d[2 * i], d[2 * i + 1]), r[0]);
+                        r[1] = f2_fma(gm.y, f2_pack(d[2 * i + 2], d[2 * i + 3]), r[1]);
+                        split2(f2_mul(bt.x, r[0]), wh[i], wl[i]);
+                        split2(f2_mul(bt.y, r[1]), wh[i + 1], wl[i + 1]);
                     }
                     tmem_st8(lanes + W::T_AH + 16 * half + 8 * j, wh);
                     tmem_st8(lanes + W::T_AL + 16 * half + 8 * j, wl);
                 }
                 ready(&r_ready);
                 if (!wait(&e_full, c)) break;
+                const uint64_t minus = f2_pack(-1.f, -1.f);
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     float d[16];
                     tmem_ld16(lanes + W::T_X + 32 * half + 16 * j, d);
                     tmem_wait_ld();
-                    uint32_t wh[8], wl[8], uh[8], ul[8];
+                    uint32_t wh[8], wl[8];
 #pragma unroll
-                    for (int i = 0; i < 16; i += 4) {
-                        const float4 bt = *(const float4*)(aux + Rec::BETA / 4 + 16 * j + i);
-                        const float4 kp = *(const float4*)(aux + Rec::KAPPA / 4 + 16 * j + i);
-                        float* r = R + 16 * j + i;
-                        r[0] -= d[i];
-                        r[1] -= d[i + 1];
-                        r[2] -= d[i + 2];
-                        r[3] -= d[i + 3];
-                        const uint64_t u0 = f2_mul(f2_pack(bt.x, bt.y), f2_pack(r[0], r[1]));
-                        const uint64_t u1 = f2_mul(f2_pack(bt.z, bt.w), f2_pack(r[2], r[3]));
-                        split2(f2_mul(f2_pack(kp.x, kp.y), u0), wh[i / 2], wl[i / 2]);
-                        split2(f2_mul(f2_pack(kp.z, kp.w), u1), wh[i / 2 + 1], wl[i / 2 + 1]);
-                        split2(u0, uh[i / 2], ul[i / 2]);
-                        split2(u1, uh[i / 2 + 1], ul[i / 2 + 1]);
+                    for (int i = 0; i < 8; i += 2) {
+                        const ulonglong2 bt = *(const ulonglong2*)(aux + Rec::BETA / 4 + 16 * j + 2 * i);
+                        const ulonglong2 kp = *(const ulonglong2*)(aux + Rec::KAPPA / 4 + 16 * j + 2 * i);
+                        uint64_t* r = R + 8 * j + i;
+                        r[0] = f2_fma(f2_pack(d[2 * i], d[2 * i + 1]), minus, r[0]);
+                        r[1] = f2_fma(f2_pack(d[2 * i + 2], d[2 * i + 3]), minus, r[1]);
+                        split2(f2_mul(f2_mul(kp.x, bt.x), r[0]), wh[i], wl[i]);
+                        split2(f2_mul(f2_mul(kp.y, bt.y), r[1]), wh[i + 1], wl[i + 1]);
                     }
                     tmem_st8(lanes + W::T_AH + 16 * half + 8 * j, wh);
                     tmem_st8(lanes + W::T_AL + 16 * half + 8 * j, wl);
+                }
+                ready(&u_ready);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {  // (the output waits for nothing but the next chunk's X)
+                    uint32_t uh[8], ul[8];
+#pragma unroll
+                    for (int i = 0; i < 8; i += 2) {
+                        const ulonglong2 bt = *(const ulonglong2*)(aux + Rec::BETA / 4 + 16 * j + 2 * i);
+                        split2(f2_mul(bt.x, R[8 * j + i]), uh[i], ul[i]);
+                        split2(f2_mul(bt.y, R[8 * j + i + 1]), uh[i + 1], ul[i + 1]);
+                    }
                     tmem_st8(lanes + W::T_UH + 16 * half + 8 * j, uh);
                     tmem_st8(lanes + W::T_UL + 16 * half + 8 * j, ul);
                 }
-                ready(&u_ready);
+                ready(&p_ready);
                 if (x.e_save) {
                     uint4* dst = (uint4*)(x.e_save + ((rec0 + (size_t)c * pk.H) * D + v) * kC + 32 * half);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        dst[i] = make_uint4(pack_bf16(R[8 * i], R[8 * i + 1]), pack_bf16(R[8 * i + 2], R[8 * i + 3]),
-                                            pack_bf16(R[8 * i + 4], R[8 * i + 5]), pack_bf16(R[8 * i + 6], R[8 * i + 7]));
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            float a, b;
+                            f2_unpack(R[4 * i + e], a, b);
+                            w[e] = pack_bf16(a, b);
+                        }
+                        dst[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
                 }
                 if (!wait(&o_full, c)) break;
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    tmem_ld16(lanes + W::T_X + 32 * half + 16 * j, *(float(*)[16])(R + 16 * j));
-                tmem_wait_ld();
+                for (int j = 0; j < 2; ++j) {
+                    float d[16];
+                    tmem_ld16(lanes + W::T_X + 32 * half + 16 * j, d);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) R[8 * j + e] = f2_pack(d[2 * e], d[2 * e + 1]);
+                }
                 fence_before_sync();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&x_free);
                 // neighbouring lanes exchange halves of two rows: each writes two elements of one
                 __nv_bfloat16* dst = out + (size_t)(c * kC) * os;
+                const uint32_t pick = lane & 1 ? 0x3276u : 0x5410u;
+                const uint64_t factor = f2_pack(-x.scale, -x.scale);
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     float d[16];
                     tmem_ld16(lanes + W::T_Q + 32 * half + 16 * j, d);
                     tmem_wait_ld();
 #pragma unroll
-                    for (int e = 0; e < 16; e += 2) {
-                        const float2 gm = *(const float2*)(aux + Rec::GAMMA / 4 + 16 * j + e);
-                        const float o0 = fmaf(x.scale * gm.x, d[e], R[16 * j + e]);
-                        const float o1 = fmaf(x.scale * gm.y, d[e + 1], R[16 * j + e + 1]);
-                        const float other = __shfl_xor_sync(0xffffffffu, lane & 1 ? o0 : o1, 1);
-                        const uint32_t w = lane & 1 ? pack_bf16(other, o1) : pack_bf16(o0, other);
-                        if (16 * j + e + (lane & 1) < n) *(uint32_t*)dst = w;
+                    for (int e = 0; e < 8; ++e) {
+                        const uint64_t gm = *(const uint64_t*)(aux + Rec::GAMMA / 4 + 16 * j + 2 * e);
+                        float o0, o1;
+                        f2_unpack(f2_fma(f2_mul(factor, gm), f2_pack(d[2 * e], d[2 * e + 1]), R[8 * j + e]), o0, o1);
+                        const uint32_t w = pack_bf16(o0, o1);
+                        const uint32_t y = __byte_perm(w, __shfl_xor_sync(0xffffffffu, w, 1), pick);
+                        if (16 * j + 2 * e + (lane & 1) < n) *(uint32_t*)dst = y;
                         dst += 2 * os;
                     }
                 }
@@ -685,6 +728,697 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
     if (warp == kWalkMma) {
         fence_after_sync();
         tmem_dealloc(tm, 512);
+    }
+}
+
+// ---- backward, the walk in reverse -------------------------------------------------------
+// With D the gradient of the state behind a chunk (the scale folded into P),
+//   dU = P^T dO + e^{G_C - G} K D,  Y = dU - M^T (beta dU),  dV = beta Y,  dbeta = E . Y,
+//   D <- e^{G_C} D + Q^T (scale e^G dO) - K^T (e^G dV).
+// Held transposed like the forward's walk, with the same roles and steps.  All results are bf16,
+// so every operand is bf16 without a low part; D itself stays fp32 in registers.  D of every
+// chunk, dV and the products E . Y (summed over a quadrant's 32 value dimensions) go to memory.
+template <int D>
+struct Back {
+    static constexpr uint32_t TILE = kC * D * 2;
+    static constexpr uint32_t REC_BYTES = Rec::BYTES - Rec::M_HI;  // M's high part, P, factors
+    static constexpr uint32_t K = 0, Q = TILE, DO = 2 * TILE, REC = 3 * TILE;
+    static constexpr uint32_t STAGE = (REC + REC_BYTES + 1023) / 1024 * 1024;
+    static constexpr int ST = D == 128 ? 3 : 4;
+    static constexpr uint32_t SMEM = ST * STAGE + 1024;
+    static constexpr uint32_t M = REC, P = REC + Rec::P - Rec::M_HI, AUX = REC + Rec::AUX - Rec::M_HI;
+    // tensor memory: D; K D, then M^T (beta dU); P^T dO; beta dU; -e^G dV; scale e^G dO; increment
+    static constexpr int T_S = 0, T_X = D / 2, T_P = T_X + 64, T_A = T_P + 64, T_R = T_A + 32,
+                         T_O = T_R + 32, T_D = T_O + 32;
+    static_assert(T_D + D <= 512, "tensor memory");
+};
+
+struct BackArgs {
+    Packed p;
+    const int* cu;
+    float scale;
+    const uint8_t* rec;
+    const __nv_bfloat16* e;  // E^T [slot][H][d][64]
+    __nv_bfloat16* ds;       // D^T [slot][H][d][d]
+    float* db;               // [slot][H][4][64]
+    __nv_bfloat16* dv;
+    int* status;
+};
+
+// sum_lane x[i] for 32 values i: lane i returns the sum of value i.  Every step halves the values.
+__device__ __forceinline__ float transpose_sum(float (&x)[32])
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int m = 16; m >= 1; m >>= 1) {
+        const bool up = lane & m;
+#pragma unroll
+        for (int i = 0; i < m; ++i) {
+            const float give = up ? x[i] : x[i + m], keep = up ? x[i + m] : x[i];
+            x[i] = keep + __shfl_xor_sync(0xffffffffu, give, m);
+        }
+    }
+    return x[0];
+}
+
+template <int D>
+__global__ void __launch_bounds__(kWalkThreads, 1)
+    delta_back_kernel(const __grid_constant__ CUtensorMap tmap_q,
+                      const __grid_constant__ CUtensorMap tmap_k,
+                      const __grid_constant__ CUtensorMap tmap_do, BackArgs x)
+{
+    using W = Walk<D>;
+    using B = Back<D>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* sm = smem_raw + ((0u - smem_u32(smem_raw)) & 1023u);  // (stays a shared-memory pointer)
+    const uint32_t sb = smem_u32(sm);
+    __shared__ uint64_t full[B::ST], empty[B::ST], s_ready[2], s_full[2], x_full, r_ready, e_full, u_ready;
+    __shared__ uint32_t tmem_base_sh;
+    __shared__ volatile int abort_flag;
+
+    const Packed& pk = x.p;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int h = blockIdx.x % pk.H, s = blockIdx.x / pk.H, hk = h / (pk.H / pk.Hk);
+    int lo, hi;
+    seq_rows(x.cu, s, pk.T, lo, hi);
+    const int chunks = (hi - lo + kC - 1) / kC;
+    const size_t rec0 = ((size_t)(lo / kC + s)) * pk.H + h;
+
+    if (tid == 0) {
+        for (int i = 0; i < B::ST; ++i) {
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], 2 * W::WARPS + 1);
+        }
+        for (int i = 0; i < W::PIECES; ++i) {
+            mbar_init(&s_ready[i], W::WARPS);
+            mbar_init(&s_full[i], 1);
+        }
+        mbar_init(&r_ready, W::WARPS);
+        mbar_init(&u_ready, W::WARPS);
+        mbar_init(&x_full, 1);
+        mbar_init(&e_full, 1);
+        abort_flag = 0;
+        fence_mbar_init();
+    }
+    if (warp == kWalkMma) {
+        tmem_alloc(&tmem_base_sh, 512);
+        tmem_relinquish();
+    }
+    fence_before_sync();
+    __syncthreads();
+    fence_after_sync();
+    const uint32_t tm = tmem_base_sh;
+    if (tm != 0 && tid == 0) {  // (cannot be; nothing is issued then)
+        abort_flag = 1;
+        if (x.status) atomicExch(x.status, (int)FLEX_ECUDA);
+    }
+    // step r works on chunk chunks - 1 - r
+    auto stage = [&](int r) { return (uint32_t)(r % B::ST) * B::STAGE; };
+    auto landed = [&](int r) {
+        return bar_wait_w(&full[r % B::ST], (uint32_t)(r / B::ST) & 1, &abort_flag, x.status);
+    };
+
+    // registers: launched with 96 a thread; 4 x 104 + 64 = 480 = 5 x 96
+    if (warp >= 16) {
+        setmaxnreg_dec<64>();
+        if (warp == kWalkTma) {
+            for (int r = 0; r < chunks; ++r) {
+                uint64_t* bar = &full[r % B::ST];
+                if (r >= B::ST &&
+                    !bar_wait_w(&empty[r % B::ST], (uint32_t)(r / B::ST - 1) & 1, &abort_flag, x.status))
+                    break;
+                const uint32_t st = sb + stage(r);
+                const int c = chunks - 1 - r, t = lo + c * kC;
+                wmbar_arrive_expect_tx(bar, 3 * B::TILE + B::REC_BYTES);
+                for (int b = 0; b < D / 64; ++b) {
+                    wtma_load_3d(st + B::DO + 8192 * b, &tmap_do, 64 * b, h, t, bar);
+                    wtma_load_3d(st + B::K + 8192 * b, &tmap_k, 64 * b, hk, t, bar);
+                    wtma_load_3d(st + B::Q + 8192 * b, &tmap_q, 64 * b, hk, t, bar);
+                }
+                if (elect_one())
+                    bulk_load(st + B::REC, x.rec + (rec0 + (size_t)c * pk.H) * Rec::BYTES + Rec::M_HI,
+                              B::REC_BYTES, bar);
+            }
+        } else if (warp == kWalkMma && tm == 0) {
+            constexpr uint32_t I_C = idesc_bf16(128, kC, 0, 0), I_CM = idesc_bf16(128, kC, 0, 1);
+            constexpr uint32_t I_P = idesc_bf16(128, kC, 1, 1), I_D = idesc_bf16(128, 64, 0, 1);
+            bool ok = true;
+            auto wait = [&](uint64_t* bar, int phase) {
+                if (ok) ok = bar_wait_w(bar, (uint32_t)phase & 1, &abort_flag, x.status);
+                fence_after_sync();
+            };
+            for (int r = 0; r < chunks && ok; ++r) {
+                const uint32_t st = sb + stage(r);
+                const int n = hi - lo - (chunks - 1 - r) * kC;
+                ok = landed(r);
+                if (!ok) break;
+                if (n < kC) {  // rows behind the sequence's end are another's, and 0 * NaN is NaN
+                    for (int e = n * 8 + lane; e < kC * 8; e += 32)
+                        for (int b = 0; b < 3 * D / 64; ++b)  // K, Q, dO
+                            st_shared_v4(st + 8192 * b + e * 16, 0, 0, 0, 0);
+                    fence_proxy_async();
+                    __syncwarp();
+                }
+                const uint32_t dk = dlow(st + B::K, 16), dkn = dlow(st + B::K, 8192);
+                const uint32_t dqn = dlow(st + B::Q, 8192), dod = dlow(st + B::DO, 8192);
+                const uint32_t dm = dlow(st + B::M, 16), dp = dlow(st + B::P, 16);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)  // P^T dO, A across the rows of dO
+                    wmma_bf16(B::T_P, desc(dod, 2048 * k), desc(dp, 2048 * k), I_P, k > 0);
+#pragma unroll
+                for (int p = 0; p < W::PIECES; ++p) {
+                    wait(&s_ready[p], r);
+                    if (!ok) break;
+                    mma4(B::T_X, B::T_S + 32 * p, dk + 512 * p, 32, I_C, p > 0);
+                }
+                if (!ok) break;
+                wmma_commit(&x_full);
+                wait(&r_ready, r);
+                if (!ok) break;
+                mma4(B::T_X, B::T_A, dm, 2048, I_CM, 0);
+                wmma_commit(&e_full);
+#pragma unroll
+                for (int p = 0; p < W::PIECES; ++p) mma4(B::T_D + 64 * p, B::T_O, dqn + 512 * p, 2048, I_D, 0);
+                wait(&u_ready, r);
+                if (!ok) break;
+#pragma unroll
+                for (int p = 0; p < W::PIECES; ++p) {
+                    mma4(B::T_D + 64 * p, B::T_R, dkn + 512 * p, 2048, I_D, 1);
+                    wmma_commit(&s_full[p]);
+                }
+                wmma_commit(&empty[r % B::ST]);
+            }
+        }
+    } else {
+        setmaxnreg_inc<104>();
+        const int half = (warp >> 2) & 1, v = 32 * (warp & 3) + lane;
+        const uint32_t lanes = tm + ((uint32_t)(warp & 3) << 21);
+        auto ready = [&](uint64_t* bar) {
+            tmem_wait_st();
+            fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar);
+        };
+        bool ok = true;
+        auto wait = [&](uint64_t* bar, int phase) {
+            ok = bar_wait_w(bar, (uint32_t)phase & 1, &abort_flag, x.status);
+            fence_after_sync();
+            return ok;
+        };
+        if ((warp & 3) >= W::QUADS) {
+            // (no lane of this quadrant holds a value dimension)
+        } else if (warp < 8) {
+            // ---- the state's gradient ----
+            uint64_t S[W::PIECES][16];  // pairs of key dimensions 64 p + 32 half + 0 .. 31
+#pragma unroll
+            for (int p = 0; p < W::PIECES; ++p)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) S[p][i] = f2_pack(0.f, 0.f);
+            uint64_t decay = f2_pack(1.f, 1.f);
+            for (int r = 0; r < chunks; ++r) {
+                __nv_bfloat16* ds = x.ds + ((rec0 + (size_t)(chunks - 1 - r) * pk.H) * D + v) * D + 32 * half;
+#pragma unroll
+                for (int p = 0; p < W::PIECES; ++p) {
+                    if (r > 0 && !wait(&s_full[p], r - 1)) break;
+                    uint32_t w[16];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        if (r > 0) {  // S = decay S + the increment of the chunk behind
+                            float a[16];
+                            tmem_ld16(lanes + B::T_D + 64 * p + 32 * half + 16 * j, a);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                S[p][8 * j + e] = f2_fma(decay, S[p][8 * j + e], f2_pack(a[2 * e], a[2 * e + 1]));
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            float a, b;
+                            f2_unpack(S[p][8 * j + e], a, b);
+                            w[8 * j + e] = pack_bf16(a, b);
+                        }
+                    }
+                    tmem_st16(lanes + B::T_S + 32 * p + 16 * half, w);
+                    ready(&s_ready[p]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        ((uint4*)(ds + 64 * p))[e] = make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
+                }
+                if (!ok || !(ok = landed(r))) break;
+                const float last = *(const float*)(sm + stage(r) + B::AUX + Rec::LAST - Rec::AUX);
+                decay = f2_pack(last, last);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&empty[r % B::ST]);
+            }
+        } else {
+            // ---- the tokens ----
+            const size_t os = (size_t)pk.H * D;
+            __nv_bfloat16* dv = x.dv + (size_t)(lo + 32 * half + (lane & 1)) * os + h * D + (v & ~1);
+            const uint32_t pick = lane & 1 ? 0x3276u : 0x5410u;
+            const uint64_t minus = f2_pack(-1.f, -1.f), factor = f2_pack(-x.scale, -x.scale);
+            for (int r = 0; r < chunks; ++r) {
+                const int c = chunks - 1 - r, n = hi - lo - c * kC - 32 * half;
+                const size_t slot = rec0 + (size_t)c * pk.H;
+                uint4 ev[4];  // E of this lane's value dimension, 32 tokens
+                {
+                    const uint4* src = (const uint4*)(x.e + (slot * D + v) * kC + 32 * half);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) ev[i] = src[i];
+                }
+                if (!(ok = landed(r))) break;
+                const uint8_t* st = sm + stage(r);
+                const float* aux = (const float*)(st + B::AUX) + 32 * half;
+                constexpr int kG = 0, kK = (Rec::KAPPA - Rec::AUX) / 4, kB = (Rec::BETA - Rec::AUX) / 4;
+                // the products of the last step have read scale e^G dO
+                if (r > 0 && !wait(&s_full[W::PIECES - 1], r - 1)) break;
+                {
+                    const uint8_t* col = st + B::DO + (uint32_t)(v >> 6) * 8192 + half * 4096;
+                    uint32_t w[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const uint32_t a = *(const uint16_t*)(col + swz128(2 * i, v & 63));
+                        const uint32_t b = *(const uint16_t*)(col + swz128(2 * i + 1, v & 63));
+                        const uint64_t gm = *(const uint64_t*)(aux + kG + 2 * i);
+                        float y, z;
+                        f2_unpack(f2_mul(f2_mul(factor, gm), f2_pack(__uint_as_float(a << 16), __uint_as_float(b << 16))), y, z);
+                        w[i] = pack_bf16(2 * i < n ? y : 0.f, 2 * i + 1 < n ? z : 0.f);
+                    }
+                    tmem_st16(lanes + B::T_O + 16 * half, w);
+                }
+                if (!wait(&x_full, r)) break;
+                uint64_t U[16];  // dU, then Y: pairs of tokens
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    float d[16], y[16];
+                    tmem_ld16(lanes + B::T_X + 32 * half + 16 * j, d);
+                    tmem_ld16(lanes + B::T_P + 32 * half + 16 * j, y);
+                    tmem_wait_ld();
+                    uint32_t w[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const uint64_t kp = *(const uint64_t*)(aux + kK + 16 * j + 2 * i);
+                        const uint64_t bt = *(const uint64_t*)(aux + kB + 16 * j + 2 * i);
+                        U[8 * j + i] = f2_fma(kp, f2_pack(d[2 * i], d[2 * i + 1]), f2_pack(y[2 * i], y[2 * i + 1]));
+                        float a, b;
+                        f2_unpack(f2_mul(bt, U[8 * j + i]), a, b);
+                        w[i] = pack_bf16(a, b);
+                    }
+                    tmem_st8(lanes + B::T_A + 16 * half + 8 * j, w);
+                }
+                ready(&r_ready);
+                if (!wait(&e_full, r)) break;
+                uint32_t wv[16];  // dV
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    float d[16];
+                    tmem_ld16(lanes + B::T_X + 32 * half + 16 * j, d);
+                    tmem_wait_ld();
+                    uint32_t w[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const uint64_t gm = *(const uint64_t*)(aux + kG + 16 * j + 2 * i);  // -e^G
+                        const uint64_t bt = *(const uint64_t*)(aux + kB + 16 * j + 2 * i);
+                        U[8 * j + i] = f2_fma(f2_pack(d[2 * i], d[2 * i + 1]), minus, U[8 * j + i]);
+                        const uint64_t y = f2_mul(bt, U[8 * j + i]);
+                        float a, b;
+                        f2_unpack(y, a, b);
+                        wv[8 * j + i] = pack_bf16(a, b);
+                        f2_unpack(f2_mul(gm, y), a, b);
+                        w[i] = pack_bf16(a, b);
+                    }
+                    tmem_st8(lanes + B::T_R + 16 * half + 8 * j, w);
+                }
+                ready(&u_ready);
+                if (lane == 0) mbar_arrive(&empty[r % B::ST]);
+                __nv_bfloat16* dst = dv + (size_t)(c * kC) * os;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const uint32_t y = __byte_perm(wv[i], __shfl_xor_sync(0xffffffffu, wv[i], 1), pick);
+                    if (2 * i + (lane & 1) < n) *(uint32_t*)dst = y;
+                    dst += 2 * os;
+                }
+                float prod[32];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const uint32_t e = (&ev[i / 4].x)[i % 4];
+                    float a, b;
+                    f2_unpack(U[i], a, b);
+                    prod[2 * i] = a * __uint_as_float(e << 16);
+                    prod[2 * i + 1] = b * __uint_as_float(e & 0xffff0000u);
+                }
+                x.db[(slot * 4 + (warp & 3)) * 64 + 32 * half + lane] = transpose_sum(prod);
+            }
+        }
+        fence_before_sync();
+    }
+    __syncthreads();
+    drain_after_abort(abort_flag);
+    if (warp == kWalkMma) {
+        fence_after_sync();
+        tmem_dealloc(tm, 512);
+    }
+}
+
+// ---- backward, the gradients of every chunk ----------------------------------------------
+// With S the state ahead of the chunk, D the gradient of the one behind, and the walk's dV:
+//   Zq = scale tril(Y o dO U^T),  Zk = -tril(Y o dV U^T, -1)       (U = beta E)
+//   dQ = scale e^G (dO S^T) + Zq K
+//   dK = Zq^T Q + (Zk + Zk^T) K + e^{G_C - G} (U D^T) - e^G (dV S^T)
+//   dg_t = sum_{i >= t > j} (Zq o Q K^T + Zk o K K^T)_ij + sum_{i >= t} a_i + sum_{j < t} b_j + e^{G_C} <S, D>,
+//   a_i = scale e^G q_i.(S dO_i) - e^G k_i.(S dV_i),  b_j = e^{G_C - G_j} beta_j k_j.(D E_j)
+// (dg without differences of long sums, which would lose what bf16 operands leave.)  One CTA of
+// 8 warps per (chunk, key head) runs over the heads that share it; dQ^T and dK^T are products of
+// key dimension x token, summed over the heads in registers: a lane holds one key dimension
+// (quadrant w % 4) and a warp half of the tokens (w / 4).  256 columns of tensor memory, taken
+// twice: [C1 | C2 | S dO | S dV], then [Zq K | Z Q, Z K | D E].  For d = 64 products have rows
+// 64-127 that read whatever lies behind a tile (within shared memory) and are not looked at.
+template <int D>
+struct Grad {
+    static constexpr uint32_t TILE = kC * D * 2, BLOCK = D * 128;  // 64 tokens; D rows of 64 elements
+    // [Q; K] and [dO; dV]: per 64 elements, 64 rows of the one and 64 of the other
+    static constexpr uint32_t QK = 0, OV = 2 * TILE, E = 4 * TILE, S = E + BLOCK, DS = S + BLOCK * (D / 64),
+                              ZQ = DS + BLOCK * (D / 64), ZK = ZQ + 8192, END = ZK + 8192;
+    static constexpr uint32_t SMEM = END + 1024;
+};
+
+struct GradArgs {
+    Packed p;
+    const int* cu;
+    float scale;
+    const uint8_t* rec;
+    const float* db;
+    __nv_bfloat16 *dq, *dk, *dg, *dbeta;
+    int* status;
+};
+
+template <int D>
+__global__ void __launch_bounds__(256, D == 64 ? 2 : 1)
+    delta_grad_kernel(const __grid_constant__ CUtensorMap tmap_q,
+                      const __grid_constant__ CUtensorMap tmap_k,
+                      const __grid_constant__ CUtensorMap tmap_do,
+                      const __grid_constant__ CUtensorMap tmap_dv,
+                      const __grid_constant__ CUtensorMap tmap_e,
+                      const __grid_constant__ CUtensorMap tmap_s,
+                      const __grid_constant__ CUtensorMap tmap_ds, GradArgs x)
+{
+    using L = Grad<D>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* sm = smem_raw + ((0u - smem_u32(smem_raw)) & 1023u);  // (stays a shared-memory pointer)
+    const uint32_t sb = smem_u32(sm);
+    __shared__ uint64_t bar_load, bar_mma;
+    __shared__ uint32_t tmem_base_sh;
+    __shared__ volatile int abort_flag;
+    __shared__ __align__(16) float aux[256];  // -e^G, e^{G_C - G}, beta, G (in powers of two)
+    __shared__ float pairs[4][64], cross[4][32], sums_a[4][64], sums_b[4][64], ab[2][64], dots[8], last_sh;
+
+    const Packed& pk = x.p;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, hk = blockIdx.y, G = pk.H / pk.Hk;
+    int s, chunk, lo, hi;
+    if (!find_block(x.cu, pk.n, pk.T, kC, (int)blockIdx.x, s, chunk, lo, hi)) return;
+    const int t0 = lo + chunk * kC, n = min(kC, hi - t0);
+    if (tid == 0) {
+        mbar_init(&bar_load, 1);
+        mbar_init(&bar_mma, 1);
+        abort_flag = 0;
+        fence_mbar_init();
+    }
+    if (warp == 0) {
+        tmem_alloc(&tmem_base_sh, 256);
+        tmem_relinquish();
+    }
+    fence_before_sync();
+    __syncthreads();
+    fence_after_sync();
+    const uint32_t tm = tmem_base_sh;
+    const int quad = warp & 3, half = warp >> 2, kd = 32 * quad + lane;
+    const bool mine = kd < D;  // this lane holds a key dimension (whole warps)
+    const uint32_t lanes = tm + ((uint32_t)quad << 21);
+    uint64_t dq[16], dk[16];  // pairs of tokens 32 half + 0 .. 31
+#pragma unroll
+    for (int i = 0; i < 16; ++i) dq[i] = dk[i] = f2_pack(0.f, 0.f);
+    grid_dep_wait();  // dV, D and the products E . Y
+    bool ok = true;
+    uint32_t ph = 0, ph_mma = 0;
+    auto products_done = [&] {  // every thread; false when a wait gave up
+        ok = bar_wait_w(&bar_mma, ph_mma, &abort_flag, x.status);
+        ph_mma ^= 1;
+        fence_after_sync();
+        return ok;
+    };
+    for (int h = hk * G; h < (hk + 1) * G; ++h) {
+        const size_t slot = (size_t)blockIdx.x * pk.H + h;
+        if (warp == 0) {
+            wmbar_arrive_expect_tx(&bar_load, 2 * L::TILE + L::BLOCK * (1 + 2 * (D / 64)) +
+                                                  (h == hk * G ? 2 * L::TILE : 0));
+            for (int b = 0; b < D / 64; ++b) {
+                if (h == hk * G) {
+                    wtma_load_3d(sb + L::QK + 16384 * b, &tmap_q, 64 * b, hk, t0, &bar_load);
+                    wtma_load_3d(sb + L::QK + 16384 * b + 8192, &tmap_k, 64 * b, hk, t0, &bar_load);
+                }
+                wtma_load_3d(sb + L::OV + 16384 * b, &tmap_do, 64 * b, h, t0, &bar_load);
+                wtma_load_3d(sb + L::OV + 16384 * b + 8192, &tmap_dv, 64 * b, h, t0, &bar_load);
+                wtma_load_3d(sb + L::S + L::BLOCK * b, &tmap_s, 64 * b, 0, (int)slot, &bar_load);
+                wtma_load_3d(sb + L::DS + L::BLOCK * b, &tmap_ds, 64 * b, 0, (int)slot, &bar_load);
+            }
+            wtma_load_3d(sb + L::E, &tmap_e, 0, 0, (int)slot, &bar_load);
+        }
+        const float* rec = (const float*)(x.rec + slot * Rec::BYTES + Rec::AUX);
+        aux[tid] = rec[tid];
+        if (tid == 0) last_sh = rec[256];
+        ok = bar_wait_w(&bar_load, ph, &abort_flag, x.status);
+        ph ^= 1;
+        if (h == hk * G && n < kC && ok) {  // rows behind the end are another's, and 0 * NaN is NaN
+            for (int e = n * 8 + tid; e < kC * 8; e += 256)
+                for (int b = 0; b < 2 * (D / 64); ++b)
+                    st_shared_v4(sb + L::QK + 8192 * b + e * 16, 0, 0, 0, 0);
+            fence_proxy_async();
+        }
+        if (!__syncthreads_and(ok)) {
+            ok = false;
+            break;
+        }
+        const uint32_t qk = dlow(sb + L::QK, 16), ov = dlow(sb + L::OV, 16), de = dlow(sb + L::E, 8192);
+        if (warp == 0) {
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+                const uint32_t o = (k >> 2) * 16384 + (k & 3) * 32;
+                wmma_bf16(tm, desc(ov, o), desc(de, 2048 * k), idesc_bf16(128, kC, 0, 1), k > 0);
+            }
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+                const uint32_t o = (k >> 2) * 16384 + (k & 3) * 32;
+                wmma_bf16(tm + 64, desc(qk, o), desc(qk, o + 8192), idesc_bf16(128, kC, 0, 0), k > 0);
+            }
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k)
+                    wmma_bf16(tm + 128 + 64 * y, desc(dlow(sb + L::S, L::BLOCK), 2048 * k),
+                              desc(ov, 8192 * y + (k >> 2) * 16384 + (k & 3) * 32),
+                              idesc_bf16(128, kC, 1, 0), k > 0);
+            wmma_commit(&bar_mma);
+        }
+        {  // <S, D> while the products run
+            float dot = 0.f;
+            for (int e = tid; e < D * D / 8; e += 256) {
+                const uint4 a = *(const uint4*)(sm + L::S + 16 * e), b = *(const uint4*)(sm + L::DS + 16 * e);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t u = (&a.x)[i], w = (&b.x)[i];
+                    dot = fmaf(__uint_as_float(u << 16), __uint_as_float(w << 16), dot);
+                    dot = fmaf(__uint_as_float(u & 0xffff0000u), __uint_as_float(w & 0xffff0000u), dot);
+                }
+            }
+#pragma unroll
+            for (int m = 1; m < 32; m *= 2) dot += __shfl_xor_sync(0xffffffffu, dot, m);
+            if (lane == 0) dots[warp] = dot;
+        }
+        ok = products_done();
+        if (ok) {
+            // Z: row i = kd % 64 of Zq (quadrants 0, 1) or Zk, columns 32 half + 0 .. 31
+            const int i = kd & 63;
+            const bool key = quad >= 2;
+            const float Gi = aux[192 + i], f = key ? -1.f : x.scale;
+            const int jmax = (i < n ? (key ? i : i + 1) : 0) - 32 * half;  // columns below it count
+            float pre[32], run = 0.f;
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                float c1[16], c2[16];
+                tmem_ld16(lanes + 32 * half + 16 * y, c1);
+                tmem_ld16(lanes + 64 + 32 * half + 16 * y, c2);
+                tmem_wait_ld();
+                uint32_t w[8];
+#pragma unroll
+                for (int j = 0; j < 16; j += 2) {
+                    float z[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int jj = 16 * y + j + e, col = 32 * half + jj;
+                        z[e] = jj < jmax ? f * aux[128 + col] * ex2(Gi - aux[192 + col]) * c1[j + e] : 0.f;
+                        pre[jj] = run;  // the sum over the columns before this one
+                        run += jj < jmax ? z[e] * c2[j + e] : 0.f;
+                    }
+                    w[j / 2] = pack_bf16(z[0], z[1]);
+                }
+                const uint32_t dst = sb + (key ? L::ZK : L::ZQ);
+                st_shared_v4(dst + swz128(i, 32 * half + 16 * y), w[0], w[1], w[2], w[3]);
+                st_shared_v4(dst + swz128(i, 32 * half + 16 * y + 8), w[4], w[5], w[6], w[7]);
+            }
+            // sum over rows i >= t of the columns j < t: within this half of the columns ...
+            const int base = (quad & 1) * 32 - 32 * half;  // row - column offset of this warp's lane 0
+#pragma unroll
+            for (int t = 0; t < 32; ++t) pre[t] = base + lane >= t ? pre[t] : 0.f;
+            pairs[quad][32 * half + lane] = transpose_sum(pre);
+            // ... and, for t in the second half, all of the first half's columns
+            if (half == 0) {
+                float suffix = run;
+#pragma unroll
+                for (int m = 1; m < 32; m *= 2) {
+                    const float o = __shfl_down_sync(0xffffffffu, suffix, m);
+                    if (lane + m < 32) suffix += o;
+                }
+                cross[quad][lane] = quad & 1 ? suffix : 0.f;
+            }
+        }
+        const uint8_t* qcol = sm + L::QK + (kd >> 6) * 16384 + half * 4096;
+        if (ok && mine) {
+            float dot[32];
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                float a[16], b[16];
+                tmem_ld16(lanes + 128 + 32 * half + 16 * y, a);
+                tmem_ld16(lanes + 192 + 32 * half + 16 * y, b);
+                tmem_wait_ld();
+#pragma unroll
+                for (int j = 0; j < 16; j += 2) {
+                    float u[2], w[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int jj = 16 * y + j + e;
+                        const bool in = 32 * half + jj < n;
+                        const float gm = aux[32 * half + jj];  // -e^G
+                        u[e] = in ? -x.scale * gm * a[j + e] : 0.f;
+                        w[e] = in ? gm * b[j + e] : 0.f;
+                        const uint32_t qv = *(const uint16_t*)(qcol + swz128(jj, kd & 63));
+                        const uint32_t kv = *(const uint16_t*)(qcol + 8192 + swz128(jj, kd & 63));
+                        dot[jj] = u[e] * __uint_as_float(qv << 16) + w[e] * __uint_as_float(kv << 16);
+                    }
+                    dq[8 * y + j / 2] = f2_fma(f2_pack(u[0], u[1]), f2_pack(1.f, 1.f), dq[8 * y + j / 2]);
+                    dk[8 * y + j / 2] = f2_fma(f2_pack(w[0], w[1]), f2_pack(1.f, 1.f), dk[8 * y + j / 2]);
+                }
+            }
+            sums_a[quad][32 * half + lane] = transpose_sum(dot);
+        }
+        fence_proxy_async();  // Z
+        fence_before_sync();
+        if (!__syncthreads_and(ok)) {
+            ok = false;
+            break;
+        }
+        fence_after_sync();
+        if (warp == 0) {
+            const uint32_t zq = dlow(sb + L::ZQ, 16), zk = dlow(sb + L::ZK, 16);
+            const uint32_t zqn = dlow(sb + L::ZQ, 8192), zkn = dlow(sb + L::ZK, 8192);
+            const uint32_t qn = dlow(sb + L::QK, 16384), kn = dlow(sb + L::QK + 8192, 16384);
+            constexpr uint32_t I_KM = idesc_bf16(128, kC, 1, 0), I_MM = idesc_bf16(128, kC, 1, 1);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) wmma_bf16(tm, desc(kn, 2048 * k), desc(zq, 32 * k), I_KM, k > 0);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) wmma_bf16(tm + 64, desc(qn, 2048 * k), desc(zqn, 2048 * k), I_MM, k > 0);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) wmma_bf16(tm + 64, desc(kn, 2048 * k), desc(zkn, 2048 * k), I_MM, 1);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) wmma_bf16(tm + 64, desc(kn, 2048 * k), desc(zk, 32 * k), I_KM, 1);
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+                wmma_bf16(tm + 128, desc(dlow(sb + L::DS, L::BLOCK), 2048 * k), desc(de, 2048 * k), I_MM, k > 0);
+            wmma_commit(&bar_mma);
+        }
+        ok = products_done();
+        if (ok && mine) {
+            float dot[32];
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                float a[16], b[16], e2[16];
+                tmem_ld16(lanes + 32 * half + 16 * y, a);
+                tmem_ld16(lanes + 64 + 32 * half + 16 * y, b);
+                tmem_ld16(lanes + 128 + 32 * half + 16 * y, e2);
+                tmem_wait_ld();
+#pragma unroll
+                for (int j = 0; j < 16; j += 2) {
+                    float w[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int jj = 16 * y + j + e, col = 32 * half + jj;
+                        const uint32_t kv = *(const uint16_t*)(qcol + 8192 + swz128(jj, kd & 63));
+                        w[e] = aux[64 + col] * aux[128 + col] * e2[j + e];
+                        dot[jj] = w[e] * __uint_as_float(kv << 16);
+                        w[e] += b[j + e];
+                    }
+                    dq[8 * y + j / 2] = f2_fma(f2_pack(a[j], a[j + 1]), f2_pack(1.f, 1.f), dq[8 * y + j / 2]);
+                    dk[8 * y + j / 2] = f2_fma(f2_pack(w[0], w[1]), f2_pack(1.f, 1.f), dk[8 * y + j / 2]);
+                }
+            }
+            sums_b[quad][32 * half + lane] = transpose_sum(dot);
+        }
+        fence_before_sync();
+        if (!__syncthreads_and(ok)) {  // (also: tensor memory and the tiles are free for the next head)
+            ok = false;
+            break;
+        }
+        if (tid < 64) {
+            float A = 0.f, B = 0.f;
+#pragma unroll
+            for (int y = 0; y < D / 32; ++y) {
+                A += sums_a[y][tid];
+                B += sums_b[y][tid];
+            }
+            ab[0][tid] = A;
+            ab[1][tid] = B;
+        }
+        __syncthreads();
+        if (tid < n) {
+            float g = 0.f, db = 0.f;
+#pragma unroll
+            for (int y = 0; y < 8; ++y) g += dots[y];
+            g *= last_sh;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) g += pairs[y][tid];
+            if (tid >= 32) g += cross[1][tid - 32] + cross[3][tid - 32];
+            for (int j = 0; j < 64; ++j) g += j >= tid ? ab[0][j] : ab[1][j];
+            const float* part = x.db + slot * 256 + tid;
+#pragma unroll
+            for (int y = 0; y < D / 32; ++y) db += part[64 * y];
+            const size_t at = (size_t)(t0 + tid) * pk.H + h;
+            x.dg[at] = __float2bfloat16_rn(g);
+            x.dbeta[at] = __float2bfloat16_rn(db);
+        }
+        __syncthreads();
+    }
+    if (ok && mine) {  // neighbouring lanes exchange halves of two rows: each writes two elements of one
+        const uint32_t pick = lane & 1 ? 0x3276u : 0x5410u;
+        const size_t os = (size_t)pk.Hk * D;
+        const size_t at = (size_t)(t0 + 32 * half + (lane & 1)) * os + hk * D + (kd & ~1);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float a, b;
+            f2_unpack(dq[i], a, b);
+            const uint32_t w = pack_bf16(a, b);
+            f2_unpack(dk[i], a, b);
+            const uint32_t y = pack_bf16(a, b);
+            const uint32_t w2 = __byte_perm(w, __shfl_xor_sync(0xffffffffu, w, 1), pick);
+            const uint32_t y2 = __byte_perm(y, __shfl_xor_sync(0xffffffffu, y, 1), pick);
+            if (32 * half + 2 * i + (lane & 1) < n) {
+                *(uint32_t*)(x.dq + at + 2 * i * os) = w2;
+                *(uint32_t*)(x.dk + at + 2 * i * os) = y2;
+            }
+        }
+    }
+    __syncthreads();
+    drain_after_abort(abort_flag);
+    if (warp == 0) {
+        fence_after_sync();
+        tmem_dealloc(tm, 256);
     }
 }
 
@@ -728,6 +1462,47 @@ cudaError_t fwd(const Packed& p, const void* q, const void* k, const void* v, co
     return e;
 }
 
+template <int D>
+cudaError_t back(const Packed& p, const void* q, const void* k, const void* dout, const void* e,
+                 const void* st, BackArgs& x, GradArgs& g, cudaStream_t s)
+{
+    CUtensorMap mq, mk, mo, mv, me, ms, md;
+    const int slots = block_slots(p.T, p.n, kC) * p.H;
+    if (!make_chunk_map(&mq, q, p.T, p.Hk, D, p.qs) || !make_chunk_map(&mk, k, p.T, p.Hk, D, p.ks) ||
+        !make_chunk_map(&mo, dout, p.T, p.H, D, (long long)p.H * D) ||
+        !make_chunk_map(&mv, x.dv, p.T, p.H, D, (long long)p.H * D) ||
+        !make_feat_map(&me, e, slots, D, kC, D) || !make_feat_map(&ms, st, slots, D, D, D) ||
+        !make_feat_map(&md, x.ds, slots, D, D, D))
+        return cudaErrorInvalidValue;
+    const int walk = (int)Back<D>::SMEM, grad = (int)Grad<D>::SMEM;
+    cudaError_t r = cudaFuncSetAttribute(delta_back_kernel<D>,
+                                         cudaFuncAttributeMaxDynamicSharedMemorySize, walk);
+    if (r == cudaSuccess)
+        r = cudaFuncSetAttribute(delta_grad_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, grad);
+    if (r == cudaSuccess)
+        r = launch_after(delta_back_kernel<D>, dim3((unsigned)(p.n * p.H)), kWalkThreads, walk, 0,
+                         false, s, mq, mk, mo, x);
+    if (r == cudaSuccess)
+        r = launch_after(delta_grad_kernel<D>,
+                         dim3((unsigned)block_slots(p.T, p.n, kC), (unsigned)p.Hk), 256, grad, 0, true,
+                         s, mq, mk, mo, mv, me, ms, md, g);
+    return r;
+}
+
+// The parts of a save buffer: records, E^T, S^T.
+struct SaveParts {
+    size_t e, s, total;
+};
+SaveParts save_parts(const Packed& p)
+{
+    const size_t slots = (size_t)block_slots(p.T, p.n, kC) * p.H;
+    SaveParts x;
+    x.e = align_up(slots * Rec::BYTES, 256);
+    x.s = x.e + slots * p.d * kC * 2;
+    x.total = x.s + slots * p.d * p.d * 2;
+    return x;
+}
+
 }  // namespace
 
 bool tc_delta_supported(const Packed& p) { return p.bf16 && p.T >= 32 * (long long)p.n; }
@@ -736,18 +1511,51 @@ size_t tc_delta_rec_bytes(const Packed& p)
 {
     return (size_t)block_slots(p.T, p.n, kC) * p.H * Rec::BYTES;
 }
+size_t tc_delta_save_bytes(const Packed& p) { return save_parts(p).total; }
+size_t tc_delta_bwd_bytes(const Packed& p)  // D^T, then the products E . Y
+{
+    return (size_t)block_slots(p.T, p.n, kC) * p.H * ((size_t)p.d * p.d * 2 + 4 * 64 * 4);
+}
 
 cudaError_t launch_tc_delta_fwd(const Packed& p, const void* q, const void* k, const void* v,
                                 const void* g, const void* beta, const int* cu, float scale,
-                                const float* S0, float* S1, void* out, void* rec, int* status,
-                                cudaStream_t s)
+                                const float* S0, float* S1, void* out, void* rec, bool saving,
+                                int* status, cudaStream_t s)
 {
     WalkArgs x = {};
     x.p = p;
     x.cu = cu; x.scale = scale; x.S0 = S0; x.S1 = S1;
     x.out = (__nv_bfloat16*)out; x.rec = (const uint8_t*)rec; x.status = status;
+    if (saving) {
+        const SaveParts at = save_parts(p);
+        x.e_save = (__nv_bfloat16*)((char*)rec + at.e);
+        x.s_save = (__nv_bfloat16*)((char*)rec + at.s);
+    }
     return p.d == 64 ? fwd<64>(p, q, k, v, g, beta, x, (uint8_t*)rec, s)
                      : fwd<128>(p, q, k, v, g, beta, x, (uint8_t*)rec, s);
+}
+
+cudaError_t launch_tc_delta_bwd(const Packed& p, const void* q, const void* k, const int* cu,
+                                float scale, const void* dout, const void* save, void* dq, void* dk,
+                                void* dv, void* dg, void* dbeta, void* scratch, int* status,
+                                cudaStream_t s)
+{
+    const SaveParts at = save_parts(p);
+    const char* base = (const char*)save;
+    BackArgs x = {};
+    x.p = p;
+    x.cu = cu; x.scale = scale; x.rec = (const uint8_t*)save;
+    x.e = (const __nv_bfloat16*)(base + at.e);
+    x.ds = (__nv_bfloat16*)scratch;
+    x.db = (float*)((char*)scratch + (size_t)block_slots(p.T, p.n, kC) * p.H * p.d * p.d * 2);
+    x.dv = (__nv_bfloat16*)dv; x.status = status;
+    GradArgs y = {};
+    y.p = p;
+    y.cu = cu; y.scale = scale; y.rec = (const uint8_t*)save; y.db = x.db;
+    y.dq = (__nv_bfloat16*)dq; y.dk = (__nv_bfloat16*)dk; y.dg = (__nv_bfloat16*)dg;
+    y.dbeta = (__nv_bfloat16*)dbeta; y.status = status;
+    return p.d == 64 ? back<64>(p, q, k, dout, base + at.e, base + at.s, x, y, s)
+                     : back<128>(p, q, k, dout, base + at.e, base + at.s, x, y, s);
 }
 
 }  // namespace flex

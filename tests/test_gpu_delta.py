@@ -179,11 +179,13 @@ def test_gates_at_their_ends(case, dtype):
     check(last, rs, "last state", F32)
     got, ref = _bwd(x, cu), delta_grads(x, lens, d ** -0.5)
     for name, y, r in zip(NAMES, got, ref):
-        # dg is the difference of sums of terms of up to 10, each held to 2e-5, of which nothing
-        # is left: e^-60 of them; or, with one unit key k and beta 1, S_{t-1} = k w^T while
-        # D_t - k dv_t^T = (I - k k^T) D_t is orthogonal to k, so their product is 0.
+        # dg is made of terms of up to 10, each held to the tolerance of the type, of which next
+        # to nothing is left: e^-60 of them; or, with one unit key k and beta 1, S_{t-1} = k w^T
+        # while D_t - k dv_t^T = (I - k k^T) D_t is orthogonal to k, so their product is 0 (up to
+        # |k|^2 - 1).  So its error is at most 10 times the tolerance: 2e-4 in fp32, whose sums
+        # keep 2e-5 of each term, 8e-2 in bf16, whose products keep 2 * 2^-8 of each.
         if name == "g" and case in ("fast_decay", "beta_1_same_keys"):
-            assert float(y.abs().max()) <= 2e-4
+            assert float((y.double() - r).abs().max()) <= 10 * tol(dtype)
             continue
         check(y, r, "d" + name)
 
