@@ -1,13 +1,19 @@
-// Gated delta rule token by token, in fp32: whole sequences forward and backward, and the
-// single-token step.  Per sequence and head, with a_t = exp(g_t),
+// Gated delta rule in fp32: whole sequences forward and backward, and the single-token step.  Per
+// sequence and head, with a_t = exp(g_t),
 //   e_t = v_t - a_t S^T k_t,  S <- a_t S + beta_t k_t e_t^T,  out_t = scale S^T q_t.
 //
 // Every column S[:, j] of the state depends on no other column (e_t[j] needs only column j), and
 // once e is known every row S[i, :] depends on no other row.  So a state is cut into lines
-// (columns, or rows) of which a few lanes each hold 16 entries in registers, and no block waits
-// for another.  The backward runs three such scans: columns in reverse for D^T k (D: the gradient
-// of the state), then rows forward (dq, and S_{t-1} dv) and rows in reverse (D u), the two halves
-// of one grid.  Sums over a line are a few shuffles; sums over lines never occur.
+// (columns, or rows) of which 8 or 16 lanes each hold 8 entries in registers, and no block waits
+// for another.  The backward runs three such scans: columns in reverse for Y = D^T k (D: the
+// gradient of the state), then rows forward (dq, and S_{t-1} dv) and rows in reverse (D u), the
+// two halves of one grid.  Sums over a line are a few shuffles; sums over lines never occur.
+//
+// A column's next step needs the sum of its last one, so what bounds a scan is one warp's chain of
+// product, shuffles and update, and how many warps share a scheduler and the shared memory
+// meanwhile.  Measured for a prompt of 1000 (training 4 x 1000), H4 d64: 8 lanes to a line 188 us
+// (578); 4 lanes 173 (614); 8 tokens at once with their mutual products (a triangular system), 4
+// lanes 222 us (890 instructions a warp for 8 tokens), 16 lanes 255 (bound by shared-memory reads).
 #include "flex_internal.h"
 #include "packed.cuh"
 #include "tc_util.cuh"
@@ -15,15 +21,13 @@
 namespace flex {
 namespace {
 
-constexpr int kThreads = 128;
+constexpr int kLines = 32;  // lines of a block
 
-// One line per P lanes, 16 entries each: entry 4 i + e of lane p is element 4 (p + P i) + e, so a
-// warp's 16-byte reads of a staged vector touch P consecutive pieces.
 template <int D>
-struct Lines {
-    static constexpr int P = D / 16;
-    static constexpr int N = kThreads / P;   // lines of a block
-    static constexpr int TT = 1024 / D;      // tokens staged at a time
+struct Cfg {
+    static constexpr int P = D / 8;           // lanes of a line
+    static constexpr int THREADS = kLines * P;
+    static constexpr int COL = 16, ROW = 1024 / D;  // tokens staged at a time
 };
 
 template <int P>
@@ -33,159 +37,161 @@ __device__ __forceinline__ float line_sum(float x)
     for (int m = 1; m < P; m *= 2) x += __shfl_xor_sync(0xffffffffu, x, m);
     return x;
 }
-
-__device__ __forceinline__ float dot16(const float (&s)[16], const float4 (&x)[4])
-{
-    float a = 0.f, b = 0.f, c = 0.f, d = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        a = fmaf(s[4 * i], x[i].x, a);
-        b = fmaf(s[4 * i + 1], x[i].y, b);
-        c = fmaf(s[4 * i + 2], x[i].z, c);
-        d = fmaf(s[4 * i + 3], x[i].w, d);
-    }
-    return (a + b) + (c + d);
-}
-// s = a s + w x
-__device__ __forceinline__ void axpy16(float (&s)[16], float a, float w, const float4 (&x)[4])
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        s[4 * i] = fmaf(w, x[i].x, a * s[4 * i]);
-        s[4 * i + 1] = fmaf(w, x[i].y, a * s[4 * i + 1]);
-        s[4 * i + 2] = fmaf(w, x[i].z, a * s[4 * i + 2]);
-        s[4 * i + 3] = fmaf(w, x[i].w, a * s[4 * i + 3]);
-    }
-}
+// Two sums over a line at once: their shuffles run side by side.
 template <int P>
-__device__ __forceinline__ void read16(float4 (&x)[4], const float* vec, int p)
+__device__ __forceinline__ void line_sum2(float& x, float& y)
 {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = *(const float4*)(vec + 4 * (p + P * i));
+    for (int m = 1; m < P; m *= 2) {
+        const float a = __shfl_xor_sync(0xffffffffu, x, m), b = __shfl_xor_sync(0xffffffffu, y, m);
+        x += a;
+        y += b;
+    }
 }
 
-// A tile of tokens in shared memory: up to three vectors of D elements and two values per line
-// for every token, and the token's a and beta.
+// Sums of 8 values over a line's lanes, each of which returns the one of value p / (P / 8): every
+// step halves the values that a lane still adds up, 7 or 8 shuffles instead of 24 or 32.
+template <int P>
+__device__ __forceinline__ float line_sums8(float (&x)[8], int p)
+{
+#pragma unroll
+    for (int m = P / 2, n = 4; n >= 1; m /= 2, n /= 2) {
+        const bool up = p & m;
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const float give = up ? x[i] : x[i + n], keep = up ? x[i + n] : x[i];
+            x[i] = keep + __shfl_xor_sync(0xffffffffu, give, m);
+        }
+    }
+    return P == 16 ? x[0] + __shfl_xor_sync(0xffffffffu, x[0], 1) : x[0];
+}
+
+// A lane's 8 entries of a line (elements 4 p + 0 .. 3, and D / 2 further) as packed pairs.
 template <int D>
-struct Tile {
-    float vec[3][Lines<D>::TT][D];
-    float line[2][Lines<D>::TT][Lines<D>::N];
-    float a[Lines<D>::TT], beta[Lines<D>::TT];
-};
+struct Vec {
+    uint64_t x[4];
 
-// A vector operand: rows of D elements at base + t * stride, times `mul`, times beta_t if asked.
-struct Rows {
-    const void* base;
-    long long stride;
-    float mul;
-    bool f32, by_beta;
-};
-
-// The loads of one tile, held in registers while the tile before it is worked on.
-template <typename T, int D, int NV, int NL>
-struct Fetch {
-    static constexpr int TT = Lines<D>::TT, LN = Lines<D>::N;
-    static constexpr int LP = (TT * LN + kThreads - 1) / kThreads;
-    float4 v[NV][2];
-    float l[NL][LP];
-    float a, beta;
-    float vb[2];
-
-    // Tokens t0 .. t0 + TT - 1 of which those in [lo, hi) exist; the others read as zero (and
-    // are not worked on).
-    __device__ __forceinline__ void load(const Rows (&rows)[NV], const Rows (&line)[NL], int line0,
-                                         const T* g, const T* beta_p, int H, int h, int t0, int lo,
-                                         int hi, int tid)
+    __device__ __forceinline__ void read(const float* vec, int p)
     {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const int e = 4 * (tid + kThreads * i), t = t0 + e / D, c = e % D;
-            const bool in = t >= lo && t < hi;
-            vb[i] = 0.f;
-            if (in) vb[i] = to_f32(beta_p[(size_t)t * H + h]);
+            const ulonglong2 y = *(const ulonglong2*)(vec + D / 2 * i + 4 * p);
+            x[2 * i] = y.x;
+            x[2 * i + 1] = y.y;
+        }
+    }
+    __device__ __forceinline__ float dot(const Vec& y) const
+    {
+        const uint64_t a = tc::f2_fma(x[2], y.x[2], tc::f2_mul(x[0], y.x[0]));
+        const uint64_t b = tc::f2_fma(x[3], y.x[3], tc::f2_mul(x[1], y.x[1]));
+        float c, d, e, f;
+        tc::f2_unpack(a, c, d);
+        tc::f2_unpack(b, e, f);
+        return (c + d) + (e + f);
+    }
+    __device__ __forceinline__ void add(float w, const Vec& y)  // += w y
+    {
+        const uint64_t ww = tc::f2_pack(w, w);
 #pragma unroll
-            for (int n = 0; n < NV; ++n) {
-                v[n][i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (!in) continue;
-                if (rows[n].f32)
-                    v[n][i] = load4((const float*)rows[n].base + t * rows[n].stride + c);
-                else
-                    v[n][i] = load4((const T*)rows[n].base + t * rows[n].stride + c);
-            }
+        for (int i = 0; i < 4; ++i) x[i] = tc::f2_fma(ww, y.x[i], x[i]);
+    }
+    __device__ __forceinline__ void scale(float a)
+    {
+        const uint64_t aa = tc::f2_pack(a, a);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = tc::f2_mul(aa, x[i]);
+    }
+};
+template <int D>
+__device__ __forceinline__ int element(int i, int p) { return D / 2 * (i / 4) + 4 * p + i % 4; }
+
+// The tile of tokens that a column scan works on: k, q and the lines' values (v, or dout).
+template <int D>
+struct ColTile {
+    float k[Cfg<D>::COL][D], q[Cfg<D>::COL][D];
+    float line[Cfg<D>::COL][kLines];
+    float a[Cfg<D>::COL], beta[Cfg<D>::COL];
+};
+
+// Runs `step(tile, j, t)` over the rows [lo, hi) of a sequence, forward or in reverse; the next
+// tile's loads are in flight behind the current one's work.  Steps are unrolled, and leave for the
+// next one the sums that nothing waits for.
+template <typename T, int D, bool REV, typename Step>
+__device__ __forceinline__ void col_scan(ColTile<D>* tiles, const T* k, long long ks, const T* q,
+                                         long long qs, const T* line, long long ls, const T* g,
+                                         const T* beta, int H, int lo, int hi, Step step)
+{
+    constexpr int TT = Cfg<D>::COL, NT = Cfg<D>::THREADS, LP = TT * kLines / NT;
+    static_assert(TT * D == 4 * NT, "four elements of a vector to a thread");
+    const int tid = threadIdx.x, nt = (hi - lo + TT - 1) / TT;
+    float4 kr, qr;
+    float lr[LP], ar = 0.f, br = 0.f;
+    auto start = [&](int i) { return REV ? hi - (i + 1) * TT : lo + i * TT; };
+    auto load = [&](int t0) {
+        {
+            const int e = 4 * tid, t = t0 + e / D, c = e % D;
+            const bool in = t >= lo && t < hi;
+            kr = in ? load4(k + t * ks + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+            qr = in ? load4(q + t * qs + c) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
 #pragma unroll
         for (int i = 0; i < LP; ++i) {
-            const int e = tid + kThreads * i, t = t0 + e / LN, c = line0 + e % LN;
-            const bool in = e < TT * LN && t >= lo && t < hi;
-#pragma unroll
-            for (int n = 0; n < NL; ++n)
-                l[n][i] = in ? to_f32(((const T*)line[n].base)[t * line[n].stride + c]) : 0.f;
+            const int e = tid + NT * i, t = t0 + e / kLines;
+            lr[i] = t >= lo && t < hi ? to_f32(line[t * ls + e % kLines]) : 0.f;
         }
         if (tid < TT) {
             const int t = t0 + tid;
             const bool in = t >= lo && t < hi;
-            a = in ? expf(to_f32(g[(size_t)t * H + h])) : 0.f;
-            beta = in ? to_f32(beta_p[(size_t)t * H + h]) : 0.f;
+            ar = in ? expf(to_f32(g[(size_t)t * H])) : 0.f;
+            br = in ? to_f32(beta[(size_t)t * H]) : 0.f;
         }
-    }
-    __device__ __forceinline__ void put(Tile<D>& s, const Rows (&rows)[NV], const Rows (&line)[NL],
-                                        int tid) const
-    {
+    };
+    auto put = [&](ColTile<D>& s) {
+        *(float4*)(&s.k[0][0] + 4 * tid) = kr;
+        *(float4*)(&s.q[0][0] + 4 * tid) = qr;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int e = 4 * (tid + kThreads * i);
-#pragma unroll
-            for (int n = 0; n < NV; ++n) {
-                const float m = rows[n].by_beta ? rows[n].mul * vb[i] : rows[n].mul;
-                float4 x = v[n][i];
-                x.x *= m; x.y *= m; x.z *= m; x.w *= m;
-                *(float4*)(&s.vec[n][0][0] + e) = x;
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < LP; ++i) {
-            const int e = tid + kThreads * i;
-            if (e < TT * LN) {
-#pragma unroll
-                for (int n = 0; n < NL; ++n) (&s.line[n][0][0])[e] = l[n][i] * line[n].mul;
-            }
-        }
+        for (int i = 0; i < LP; ++i) (&s.line[0][0])[tid + NT * i] = lr[i];
         if (tid < TT) {
-            s.a[tid] = a;
-            s.beta[tid] = beta;
+            s.a[tid] = ar;
+            s.beta[tid] = br;
         }
-    }
-};
-
-// Runs `step(tile, j, t)` over the rows [lo, hi) of a sequence, forward or in reverse, the next
-// tile's loads in flight behind the current one's work.
-template <typename T, int D, int NV, int NL, bool REV, typename Step>
-__device__ __forceinline__ void scan(Tile<D>* tiles, const Rows (&rows)[NV], const Rows (&line)[NL],
-                                     int line0, const T* g, const T* beta, int H, int h, int lo,
-                                     int hi, Step step)
-{
-    constexpr int TT = Lines<D>::TT;
-    const int tid = threadIdx.x, nt = (hi - lo + TT - 1) / TT;
-    Fetch<T, D, NV, NL> f;
-    auto start = [&](int i) { return REV ? hi - (i + 1) * TT : lo + i * TT; };
+    };
     if (nt > 0) {
-        f.load(rows, line, line0, g, beta, H, h, start(0), lo, hi, tid);
-        f.put(tiles[0], rows, line, tid);
+        load(start(0));
+        put(tiles[0]);
     }
     __syncthreads();
     for (int i = 0; i < nt; ++i) {
         const int t0 = start(i);
-        if (i + 1 < nt) f.load(rows, line, line0, g, beta, H, h, start(i + 1), lo, hi, tid);
-        const Tile<D>& s = tiles[i & 1];
+        if (i + 1 < nt) load(start(i + 1));
+        const ColTile<D>& s = tiles[i & 1];
         if (REV) {
-            for (int j = TT - 1; j >= 0 && t0 + j >= lo; --j) step(s, j, t0 + j);
+            if (t0 >= lo) {
+#pragma unroll 4
+                for (int j = TT - 1; j >= 0; --j) step(s, j, t0 + j);
+            } else {
+                for (int j = TT - 1; t0 + j >= lo; --j) step(s, j, t0 + j);
+            }
         } else {
-            for (int j = 0; j < TT && t0 + j < hi; ++j) step(s, j, t0 + j);
+            if (t0 + TT <= hi) {
+#pragma unroll 4
+                for (int j = 0; j < TT; ++j) step(s, j, t0 + j);
+            } else {
+                for (int j = 0; t0 + j < hi; ++j) step(s, j, t0 + j);
+            }
         }
-        if (i + 1 < nt) f.put(tiles[(i + 1) & 1], rows, line, tid);
+        if (i + 1 < nt) put(tiles[(i + 1) & 1]);
         __syncthreads();
     }
 }
+
+// The tile of tokens that a row scan works on: u = beta e, dv = beta du, scale dout; k and q.
+template <int D>
+struct RowTile {
+    float vec[3][Cfg<D>::ROW][D];
+    float k[Cfg<D>::ROW][kLines], q[Cfg<D>::ROW][kLines];
+    float a[Cfg<D>::ROW];
+};
 
 struct ScanArgs {
     Packed p;
@@ -202,141 +208,214 @@ struct ScanArgs {
 template <int D>
 __device__ __forceinline__ void place(const Packed& p, int b, int& line0, int& h, int& s)
 {
-    constexpr int LB = D / Lines<D>::N;
-    line0 = (b % LB) * Lines<D>::N;
+    constexpr int LB = D / kLines;
+    line0 = (b % LB) * kLines;
     h = (b / LB) % p.H;
     s = b / LB / p.H;
 }
 
-// Forward, one column per P lanes.  e (NULL or [T][H][d] fp32) receives v - a S^T k.
+// Forward by columns.  e (NULL or [T][H][d] fp32) receives v - a S^T k.
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) delta_fwd_kernel(ScanArgs x)
+__global__ void __launch_bounds__(Cfg<D>::THREADS) delta_fwd_kernel(ScanArgs x)
 {
-    using L = Lines<D>;
-    __shared__ Tile<D> tiles[2];
+    constexpr int P = Cfg<D>::P;
+    __shared__ ColTile<D> tiles[2];
     const Packed& pk = x.p;
     int col0, h, s, lo, hi;
     place<D>(pk, blockIdx.x, col0, h, s);
     seq_rows(x.cu, s, pk.T, lo, hi);
-    const int tid = threadIdx.x, p = tid % L::P, cl = tid / L::P, col = col0 + cl;
+    const int tid = threadIdx.x, p = tid % P, cl = tid / P, col = col0 + cl;
     const int H = pk.H, hk = h / (H / pk.Hk);
-    float S[16];
-    const size_t at = ((size_t)s * H + h) * D * D;
+    Vec<D> S;
+    const size_t at = ((size_t)s * H + h) * D * D + col;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int r = 4 * (p + L::P * (i / 4)) + i % 4;
-        S[i] = x.S0 ? x.S0[at + (size_t)r * D + col] : 0.f;
-    }
-    const Rows rows[2] = {{(const T*)x.k + hk * D, pk.ks, 1.f, false, false},
-                          {(const T*)x.q + hk * D, pk.qs, x.scale, false, false}};
-    const Rows line[1] = {{(const T*)x.v + h * D, pk.vs, 1.f, false, false}};
-    T* out = (T*)x.out + h * D + col;
-    float* e_out = x.e ? x.e + h * D + col : nullptr;
+    for (int i = 0; i < 4; ++i)
+        S.x[i] = x.S0 ? tc::f2_pack(x.S0[at + (size_t)element<D>(2 * i, p) * D],
+                                    x.S0[at + (size_t)element<D>(2 * i + 1, p) * D])
+                      : tc::f2_pack(0.f, 0.f);
     const long long os = (long long)H * D;
-    scan<T, D, 2, 1, false>(tiles, rows, line, col0, (const T*)x.g, (const T*)x.beta, H, h, lo, hi,
-                            [&](const Tile<D>& tile, int j, int t) {
-        float4 k[4], q[4];
-        read16<L::P>(k, tile.vec[0][j], p);
-        read16<L::P>(q, tile.vec[1][j], p);
-        const float a = tile.a[j];
-        const float e = tile.line[0][j][cl] - a * line_sum<L::P>(dot16(S, k));
-        axpy16(S, a, tile.beta[j] * e, k);
-        const float o = line_sum<L::P>(dot16(S, q));
+    T* out = (T*)x.out + (long long)lo * os + h * D + col;  // of the token that `o` belongs to
+    float* e_out = x.e ? x.e + h * D + col : nullptr;
+    float o = 0.f;
+    bool any = false;
+    col_scan<T, D, false>(tiles, (const T*)x.k + hk * D, pk.ks, (const T*)x.q + hk * D, pk.qs,
+                          (const T*)x.v + h * D + col0, pk.vs, (const T*)x.g + h, (const T*)x.beta + h,
+                          H, lo, hi, [&](const ColTile<D>& w, int j, int t) {
+        Vec<D> k, q;
+        k.read(w.k[j], p);
+        q.read(w.q[j], p);
+        const float a = w.a[j], beta = w.beta[j];
+        float sk = S.dot(k);
+        line_sum2<P>(sk, o);
+        const float e = fmaf(-a, sk, w.line[j][cl]);
+        S.scale(a);
+        S.add(beta * e, k);
         if (p == 0) {
-            from_f32(out[t * os], o);
+            if (any) from_f32(*out, x.scale * o);
             if (e_out) e_out[t * os] = e;
         }
+        if (any) out += os;
+        any = true;
+        o = S.dot(q);
     });
+    o = line_sum<P>(o);
+    if (any && p == 0) from_f32(*out, x.scale * o);
     if (x.S1) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int r = 4 * (p + L::P * (i / 4)) + i % 4;
-            x.S1[at + (size_t)r * D + col] = S[i];
+        for (int i = 0; i < 4; ++i) {
+            float a, b;
+            tc::f2_unpack(S.x[i], a, b);
+            x.S1[at + (size_t)element<D>(2 * i, p) * D] = a;
+            x.S1[at + (size_t)element<D>(2 * i + 1, p) * D] = b;
         }
     }
 }
 
 // Backward, first scan: columns of D in reverse; du_t = D_t^T k_t, D <- a (D - k dv^T).
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) delta_bwd_cols_kernel(ScanArgs x)
+__global__ void __launch_bounds__(Cfg<D>::THREADS) delta_bwd_cols_kernel(ScanArgs x)
 {
-    using L = Lines<D>;
-    __shared__ Tile<D> tiles[2];
+    constexpr int P = Cfg<D>::P;
+    __shared__ ColTile<D> tiles[2];
     const Packed& pk = x.p;
     int col0, h, s, lo, hi;
     place<D>(pk, blockIdx.x, col0, h, s);
     seq_rows(x.cu, s, pk.T, lo, hi);
-    const int tid = threadIdx.x, p = tid % L::P, cl = tid / L::P;
+    const int tid = threadIdx.x, p = tid % P, cl = tid / P;
     const int H = pk.H, hk = h / (H / pk.Hk);
     const long long os = (long long)H * D;
-    float S[16] = {};
-    const Rows rows[2] = {{(const T*)x.k + hk * D, pk.ks, 1.f, false, false},
-                          {(const T*)x.q + hk * D, pk.qs, x.scale, false, false}};
-    const Rows line[1] = {{(const T*)x.dout + h * D, os, 1.f, false, false}};
+    Vec<D> S = {};
     float* du_out = x.du + h * D + col0 + cl;
-    scan<T, D, 2, 1, true>(tiles, rows, line, col0, (const T*)x.g, (const T*)x.beta, H, h, lo, hi,
-                           [&](const Tile<D>& tile, int j, int t) {
-        float4 k[4], q[4];
-        read16<L::P>(k, tile.vec[0][j], p);
-        read16<L::P>(q, tile.vec[1][j], p);
-        axpy16(S, 1.f, tile.line[0][j][cl], q);
-        const float du = line_sum<L::P>(dot16(S, k)), a = tile.a[j];
-        axpy16(S, a, -a * tile.beta[j] * du, k);
+    col_scan<T, D, true>(tiles, (const T*)x.k + hk * D, pk.ks, (const T*)x.q + hk * D, pk.qs,
+                         (const T*)x.dout + h * D + col0, os, (const T*)x.g + h, (const T*)x.beta + h,
+                         H, lo, hi, [&](const ColTile<D>& w, int j, int t) {
+        Vec<D> k, q;
+        k.read(w.k[j], p);
+        q.read(w.q[j], p);
+        const float a = w.a[j], beta = w.beta[j];
+        S.add(x.scale * w.line[j][cl], q);
+        const float du = line_sum<P>(S.dot(k));
+        S.add(-beta * du, k);
+        S.scale(a);
         if (p == 0) du_out[t * os] = du;
     });
 }
 
 // Backward, the row scans: even blocks rows of S forward (dq = scale S dout, r = a S_{t-1} dv),
-// odd blocks rows of D in reverse (w = D u, u = beta e).
+// odd blocks rows of D in reverse (w = D u, u = beta e).  By tokens; sums of 8 tokens at once.
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) delta_bwd_rows_kernel(ScanArgs x)
+__global__ void __launch_bounds__(Cfg<D>::THREADS) delta_bwd_rows_kernel(ScanArgs x)
 {
-    using L = Lines<D>;
-    __shared__ Tile<D> tiles[2];
+    constexpr int TT = Cfg<D>::ROW, NT = Cfg<D>::THREADS, P = Cfg<D>::P;
+    constexpr int SLOTS = TT * D / 4;                            // 16-byte pieces of a vector: 256
+    constexpr int LV = (3 * SLOTS + NT - 1) / NT, LL = TT * kLines / NT ? TT * kLines / NT : 1;
+    __shared__ RowTile<D> tiles[2];
     tc::grid_dep_wait();  // du
     const Packed& pk = x.p;
+    const bool rev = blockIdx.x & 1;
     int row0, h, s, lo, hi;
     place<D>(pk, blockIdx.x / 2, row0, h, s);
     seq_rows(x.cu, s, pk.T, lo, hi);
-    const int tid = threadIdx.x, p = tid % L::P, rl = tid / L::P;
+    const int tid = threadIdx.x, p = tid % P, rl = tid / P, nt = (hi - lo + TT - 1) / TT;
     const int H = pk.H, hk = h / (H / pk.Hk);
     const long long os = (long long)H * D;
-    float S[16] = {};
-    const Rows rows[3] = {{x.e + h * D, os, 1.f, true, true},
-                          {x.du + h * D, os, 1.f, true, true},
-                          {(const T*)x.dout + h * D, os, x.scale, false, false}};
-    const Rows line[2] = {{(const T*)x.k + hk * D, pk.ks, 1.f, false, false},
-                          {(const T*)x.q + hk * D, pk.qs, 1.f, false, false}};
-    const size_t out0 = h * D + row0 + rl;
-    if (blockIdx.x % 2 == 0) {
-        scan<T, D, 3, 2, false>(tiles, rows, line, row0, (const T*)x.g, (const T*)x.beta, H, h, lo,
-                                hi, [&](const Tile<D>& tile, int j, int t) {
-            float4 u[4], dv[4], dO[4];
-            read16<L::P>(u, tile.vec[0][j], p);
-            read16<L::P>(dv, tile.vec[1][j], p);
-            read16<L::P>(dO, tile.vec[2][j], p);
-            const float a = tile.a[j];
-            const float r = a * line_sum<L::P>(dot16(S, dv));
-            axpy16(S, a, tile.line[0][j][rl], u);
-            const float dq = line_sum<L::P>(dot16(S, dO));
-            if (p == 0) {
-                x.rh[out0 + t * os] = r;
-                x.dqh[out0 + t * os] = dq;
+    const T *g = (const T*)x.g + h, *beta = (const T*)x.beta + h;
+    const T *k = (const T*)x.k + hk * D + row0, *q = (const T*)x.q + hk * D + row0;
+    Vec<D> S = {};
+
+    float4 v[LV];  // this thread's pieces of the three vectors
+    float kr[LL], qr[LL], ar = 0.f;
+    auto start = [&](int i) { return rev ? hi - (i + 1) * TT : lo + i * TT; };
+    auto load = [&](int t0) {
+#pragma unroll
+        for (int i = 0; i < LV; ++i) {
+            const int slot = tid + NT * i, n = slot / SLOTS, e = slot % SLOTS * 4, t = t0 + e / D, c = e % D;
+            v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (n >= 3 || t < lo || t >= hi) continue;
+            const size_t at = (size_t)t * os + h * D + c;
+            float m = x.scale;
+            if (n < 2) {
+                v[i] = load4((n ? x.du : x.e) + at);
+                m = to_f32(beta[(size_t)t * H]);
+            } else {
+                v[i] = load4((const T*)x.dout + at);
             }
-        });
-    } else {
-        scan<T, D, 3, 2, true>(tiles, rows, line, row0, (const T*)x.g, (const T*)x.beta, H, h, lo,
-                               hi, [&](const Tile<D>& tile, int j, int t) {
-            float4 u[4], dv[4], dO[4];
-            read16<L::P>(u, tile.vec[0][j], p);
-            read16<L::P>(dv, tile.vec[1][j], p);
-            read16<L::P>(dO, tile.vec[2][j], p);
-            const float a = tile.a[j];
-            axpy16(S, 1.f, tile.line[1][j][rl], dO);
-            const float w = line_sum<L::P>(dot16(S, u));
-            axpy16(S, a, -a * tile.line[0][j][rl], dv);
-            if (p == 0) x.wh[out0 + t * os] = w;
-        });
+            v[i].x *= m; v[i].y *= m; v[i].z *= m; v[i].w *= m;
+        }
+#pragma unroll
+        for (int i = 0; i < LL; ++i) {
+            const int e = tid + NT * i, t = t0 + e / kLines;
+            const bool in = e < TT * kLines && t >= lo && t < hi;
+            kr[i] = in ? to_f32(k[t * pk.ks + e % kLines]) : 0.f;
+            qr[i] = in ? to_f32(q[t * pk.qs + e % kLines]) : 0.f;
+        }
+        if (tid < TT) ar = t0 + tid >= lo && t0 + tid < hi ? expf(to_f32(g[(size_t)(t0 + tid) * H])) : 1.f;
+    };
+    auto put = [&](RowTile<D>& w) {
+#pragma unroll
+        for (int i = 0; i < LV; ++i) {
+            const int slot = tid + NT * i;
+            if (slot < 3 * SLOTS) *(float4*)(&w.vec[0][0][0] + 4 * slot) = v[i];
+        }
+#pragma unroll
+        for (int i = 0; i < LL; ++i) {
+            const int e = tid + NT * i;
+            if (e < TT * kLines) {
+                (&w.k[0][0])[e] = kr[i];
+                (&w.q[0][0])[e] = qr[i];
+            }
+        }
+        if (tid < TT) w.a[tid] = ar;
+    };
+    if (nt > 0) {
+        load(start(0));
+        put(tiles[0]);
+    }
+    __syncthreads();
+    const size_t out = (size_t)h * D + row0 + rl;
+    for (int i = 0; i < nt; ++i) {
+        const RowTile<D>& w = tiles[i & 1];
+        if (i + 1 < nt) load(start(i + 1));
+#pragma unroll 1
+        for (int jj = 0; jj < TT; jj += 8) {
+            const int j = rev ? TT - 8 - jj : jj, t = start(i) + j + p / (P / 8);  // the token whose sums this lane gets
+            const bool store = (P == 8 || !(p & 1)) && t >= lo && t < hi;
+            float a[8], b[8];
+            if (!rev) {
+#pragma unroll
+                for (int y = 0; y < 8; ++y) {
+                    Vec<D> u, dv, dO;
+                    u.read(w.vec[0][j + y], p);
+                    dv.read(w.vec[1][j + y], p);
+                    dO.read(w.vec[2][j + y], p);
+                    S.scale(w.a[j + y]);
+                    a[y] = S.dot(dv);
+                    S.add(w.k[j + y][rl], u);
+                    b[y] = S.dot(dO);
+                }
+                const float r = line_sums8<P>(a, p), dq = line_sums8<P>(b, p);
+                if (store) {
+                    x.rh[out + t * os] = r;
+                    x.dqh[out + t * os] = dq;
+                }
+            } else {
+#pragma unroll
+                for (int y = 7; y >= 0; --y) {
+                    Vec<D> u, dv, dO;
+                    u.read(w.vec[0][j + y], p);
+                    dv.read(w.vec[1][j + y], p);
+                    dO.read(w.vec[2][j + y], p);
+                    S.add(w.q[j + y][rl], dO);
+                    a[y] = S.dot(u);
+                    S.add(-w.k[j + y][rl], dv);
+                    S.scale(w.a[j + y]);
+                }
+                const float z = line_sums8<P>(a, p);
+                if (store) x.wh[out + t * os] = z;
+            }
+        }
+        if (i + 1 < nt) put(tiles[(i + 1) & 1]);
+        __syncthreads();
     }
 }
 
@@ -493,12 +572,12 @@ __global__ void __launch_bounds__(NT) delta_decode_kernel(ScanArgs x)
 }
 
 template <int D>
-long long scan_blocks(const Packed& p) { return (long long)p.n * p.H * (D / Lines<D>::N); }
+long long scan_blocks(const Packed& p) { return (long long)p.n * p.H * (D / kLines); }
 
 template <typename T, int D>
 cudaError_t fwd(const ScanArgs& x, cudaStream_t s)
 {
-    return tc::launch_after(delta_fwd_kernel<T, D>, dim3((unsigned)scan_blocks<D>(x.p)), kThreads, 0,
+    return tc::launch_after(delta_fwd_kernel<T, D>, dim3((unsigned)scan_blocks<D>(x.p)), Cfg<D>::THREADS, 0,
                             0, false, s, x);
 }
 
@@ -507,10 +586,10 @@ cudaError_t bwd(const ScanArgs& x, const FinishArgs& f, cudaStream_t s)
 {
     const Packed& p = x.p;
     const unsigned blocks = (unsigned)scan_blocks<D>(p);
-    cudaError_t e = tc::launch_after(delta_bwd_cols_kernel<T, D>, dim3(blocks), kThreads, 0, 0,
+    cudaError_t e = tc::launch_after(delta_bwd_cols_kernel<T, D>, dim3(blocks), Cfg<D>::THREADS, 0, 0,
                                      false, s, x);
     if (e == cudaSuccess)
-        e = tc::launch_after(delta_bwd_rows_kernel<T, D>, dim3(2 * blocks), kThreads, 0, 0, true, s, x);
+        e = tc::launch_after(delta_bwd_rows_kernel<T, D>, dim3(2 * blocks), Cfg<D>::THREADS, 0, 0, true, s, x);
     const long long items = (long long)p.T * p.Hk;
     if (e == cudaSuccess)
         e = tc::launch_after(delta_bwd_finish_kernel<T, D>, dim3((unsigned)((items + 3) / 4)), 128, 0,

@@ -67,6 +67,17 @@ __device__ __forceinline__ void split(float a, float b, uint32_t& hi, uint32_t& 
     split2(f2_pack(a, b), hi, lo);
 }
 
+// Eight packed pairs rounded to bf16.
+__device__ __forceinline__ void pack8(const uint64_t* x, uint32_t (&w)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float a, b;
+        f2_unpack(x[i], a, b);
+        w[i] = pack_bf16(a, b);
+    }
+}
+
 // Matrix descriptors as their varying low words (address and leading offset); the high word is
 // the same for all (1024 bytes between groups of 8 rows, 128-byte swizzle), so that an issuing
 // warp keeps one register for each.
@@ -555,15 +566,21 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                             for (int e = 0; e < 8; ++e) split2(S[p][8 * j + e], wh[e], wl[e]);
                             tmem_st8(lanes + W::T_SH + 32 * p + 16 * half + 8 * j, wh);
                             tmem_st8(lanes + W::T_SL + 32 * p + 16 * half + 8 * j, wl);
-                            if (x.s_save) {
-                                uint4* dst = (uint4*)(x.s_save + ((rec0 + (size_t)c * pk.H) * D + v) * D +
-                                                      64 * p + 32 * half + 16 * j);
-                                dst[0] = make_uint4(wh[0], wh[1], wh[2], wh[3]);
-                                dst[1] = make_uint4(wh[4], wh[5], wh[6], wh[7]);
-                            }
                         }
                     }
                     if (c < chunks) ready(&s_ready[p]);
+                }
+                if (x.s_save && ok && c < chunks) {  // (rounded again: the walk waits for the pieces)
+#pragma unroll
+                    for (int p = 0; p < W::PIECES; ++p) {
+                        __nv_bfloat16* dst = x.s_save + ((rec0 + (size_t)c * pk.H) * D + v) * D + 64 * p + 32 * half;
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            uint32_t w[8];
+                            pack8(S[p] + 8 * j, w);
+                            store_32b(dst + 16 * j, make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7]));
+                        }
+                    }
                 }
                 if (!ok || c == chunks || !(ok = landed(c))) break;
                 const float last = *(const float*)(sm + stage(c) + W::REC + Rec::LAST);
@@ -940,7 +957,6 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
 #pragma unroll
                 for (int p = 0; p < W::PIECES; ++p) {
                     if (r > 0 && !wait(&s_full[p], r - 1)) break;
-                    uint32_t w[16];
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         if (r > 0) {  // S = decay S + the increment of the chunk behind
@@ -951,18 +967,22 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                             for (int e = 0; e < 8; ++e)
                                 S[p][8 * j + e] = f2_fma(decay, S[p][8 * j + e], f2_pack(a[2 * e], a[2 * e + 1]));
                         }
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            float a, b;
-                            f2_unpack(S[p][8 * j + e], a, b);
-                            w[8 * j + e] = pack_bf16(a, b);
-                        }
+                        uint32_t w[8];
+                        pack8(S[p] + 8 * j, w);
+                        tmem_st8(lanes + B::T_S + 32 * p + 16 * half + 8 * j, w);
                     }
-                    tmem_st16(lanes + B::T_S + 32 * p + 16 * half, w);
                     ready(&s_ready[p]);
+                }
+                if (ok) {  // (rounded again: the walk waits for the pieces)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        ((uint4*)(ds + 64 * p))[e] = make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
+                    for (int p = 0; p < W::PIECES; ++p)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            uint32_t w[8];
+                            pack8(S[p] + 8 * j, w);
+                            store_32b(ds + 64 * p + 16 * j, make_uint4(w[0], w[1], w[2], w[3]),
+                                      make_uint4(w[4], w[5], w[6], w[7]));
+                        }
                 }
                 if (!ok || !(ok = landed(r))) break;
                 const float last = *(const float*)(sm + stage(r) + B::AUX + Rec::LAST - Rec::AUX);

@@ -307,58 +307,61 @@ def awd_loss_bwd(q, k, W1, W2=None, causal=False, tau=None, dloss=None, loss=Non
 
 # ---- packed batches: sequences of different lengths, rows [T][heads][d] ------------------
 
-def _rows(t, what, heads=None, d=None, T=None):
-    """The row stride of a [T, heads, d] tensor whose heads and elements are contiguous (a slice
-    of wider rows is fine)."""
-    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1) or (
-            t.shape[1] > 1 and t.stride(1) != t.shape[2]):
-        raise ValueError(f"{what}: rows [T, heads, d] with contiguous heads")
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+def _rows(t, what, shape, dtype, dev):
+    """The row stride of a tensor [T, heads, d] of this shape and type on device `dev` whose heads
+    and elements are contiguous (a slice of wider rows is fine)."""
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError(f"{what}: {tuple(t.shape)} {t.dtype}, not {tuple(shape)} {dtype}")
+    if t.get_device() != dev:
         raise ValueError(f"{what}: not on the current CUDA device")
-    for got, want in ((t.shape[0], T), (t.shape[1], heads), (t.shape[2], d)):
-        if want is not None and got != want:
-            raise ValueError(f"{what}: shape {tuple(t.shape)} does not fit the other tensors")
-    stride = t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
-    if stride >= 2 ** 31:
-        raise ValueError(f"{what}: row stride {stride}")
-    return stride
+    row, head, one = t.stride()
+    T, heads, d = shape
+    if (one != 1 and d > 1) or (head != d and heads > 1):
+        raise ValueError(f"{what}: rows [T, heads, d] with contiguous heads")
+    if T <= 1:
+        return heads * d
+    if row >= 2 ** 31:
+        raise ValueError(f"{what}: row stride {row}")
+    return row
 
 
-def _plain(t, what, shape, dtype):
-    """A contiguous tensor of this shape and type on the current device, as a pointer."""
+def _plain(t, what, shape, dtype, dev):
+    """A contiguous tensor of this shape and type on device `dev` (or None), as a pointer."""
     if t is None:
         return None
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
-        raise ValueError(f"{what}: {tuple(t.shape)} {t.dtype}, not {tuple(shape)} {dtype}")
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{what}: {tuple(t.shape)} {t.dtype}, not contiguous {tuple(shape)} {dtype}")
+    if t.get_device() != dev:
         raise ValueError(f"{what}: not on the current CUDA device")
-    return _ptr(t)
+    return t.data_ptr()
 
 
-def _offsets(cu, what="cu"):
+def _offsets(cu, what, dev):
     if cu.dim() != 1 or cu.numel() < 2 or cu.dtype != torch.int32:
         raise ValueError(f"{what}: int32 offsets of at least one sequence")
-    return _plain(cu, what, cu.shape, torch.int32)
+    return _plain(cu, what, cu.shape, torch.int32, dev)
 
 
-def _packed_delta(q, k, v, n):
-    T, H, d = v.shape
-    qs = _rows(q, "q", None, d, T)
-    ks = _rows(k, "k", q.shape[1], d, T)
-    vs = _rows(v, "v")
-    if not q.dtype == k.dtype == v.dtype:
-        raise ValueError("q, k and v are of one type")
-    return FlexPacked(n, T, T, H, q.shape[1], d, _dtype_code(q), qs, ks, vs)
+def _rank3(t, what):
+    if t.dim() != 3:
+        raise ValueError(f"{what}: rows [T, heads, d]")
+    return t.shape
 
 
-def _packed_attn(q, k, v, n):
-    T, H, d = q.shape
-    qs = _rows(q, "q")
-    ks = _rows(k, "k", None, d)
-    vs = _rows(v, "v", k.shape[1], d, k.shape[0])
-    if not q.dtype == k.dtype == v.dtype:
-        raise ValueError("q, k and v are of one type")
-    return FlexPacked(n, T, k.shape[0], H, k.shape[1], d, _dtype_code(q), qs, ks, vs)
+def _packed_delta(q, k, v, n, dev):
+    T, H, d = _rank3(v, "v")
+    Hk, dt = _rank3(q, "q")[1], q.dtype
+    rows = (T, Hk, d)
+    return FlexPacked(n, T, T, H, Hk, d, _dtype_code(q), _rows(q, "q", rows, dt, dev),
+                      _rows(k, "k", rows, dt, dev), _rows(v, "v", (T, H, d), dt, dev))
+
+
+def _packed_attn(q, k, v, n, dev):
+    T, H, d = _rank3(q, "q")
+    Tk, Hk, dt = *_rank3(k, "k")[:2], q.dtype
+    rows = (Tk, Hk, d)
+    return FlexPacked(n, T, Tk, H, Hk, d, _dtype_code(q), _rows(q, "q", (T, H, d), dt, dev),
+                      _rows(k, "k", rows, dt, dev), _rows(v, "v", rows, dt, dev))
 
 
 def _zeros(n, what, device):
@@ -369,18 +372,25 @@ def _zeros(n, what, device):
 
 def delta_workspace(q, v, cu, backward=False) -> torch.Tensor:
     """A caller-owned workspace for delta_fwd (backward: for delta_bwd too) on such tensors."""
-    shape = _packed_delta(q, q, v, cu.numel() - 1)
+    shape = _packed_delta(q, q, v, cu.numel() - 1, torch.cuda.current_device())
     return _zeros(int(load().flex_delta_workspace_bytes(ctypes.byref(shape), int(bool(backward)))),
                   "flex_delta_workspace_bytes", q.device)
 
 
 def delta_save(q, v, cu) -> torch.Tensor:
     """The buffer in which delta_fwd leaves what delta_bwd needs (not initialised)."""
-    shape = _packed_delta(q, q, v, cu.numel() - 1)
+    shape = _packed_delta(q, q, v, cu.numel() - 1, torch.cuda.current_device())
     n = int(load().flex_delta_save_bytes(ctypes.byref(shape)))
     if n == 0:
         raise FlexError(FLEX_EUNSUPPORTED, "flex_delta_save_bytes")
     return torch.empty(n, dtype=torch.uint8, device=q.device)
+
+
+def _saved(save, shape, dev):
+    """A save buffer for this shape, as a pointer."""
+    if save.numel() < load().flex_delta_save_bytes(ctypes.byref(shape)):
+        raise FlexError(FLEX_EWORKSPACE, "save")
+    return _plain(save, "save", save.shape, torch.uint8, dev)
 
 
 def delta_fwd(q, k, v, g, beta, cu, scale=None, state=None, out=None, want_state=True,
@@ -389,69 +399,74 @@ def delta_fwd(q, k, v, g, beta, cu, scale=None, state=None, out=None, want_state
     None).  q, k [T, Hk, d]; v [T, H, d]; g (log decay), beta [T, H]; cu int32 [n + 1].  state:
     the sequences' first state (default zero; last_state may be the same tensor).  save: a
     delta_save() buffer for delta_bwd (then without `state`).  scale: default 1 / sqrt(d)."""
+    dev = torch.cuda.current_device()
+    cu_ptr, n = _offsets(cu, "cu", dev), cu.numel() - 1
+    shape = _packed_delta(q, k, v, n, dev)
     T, H, d = v.shape
-    n = cu.numel() - 1
-    shape = _packed_delta(q, k, v, n)
-    gp, bp = (_plain(x, w, (T, H), q.dtype) for x, w in ((g, "g"), (beta, "beta")))
+    gates, dt, st = (T, H), q.dtype, (n, H, d, d)
     if out is None:
-        out = torch.empty(T, H, d, dtype=q.dtype, device=q.device)
+        out = torch.empty(T, H, d, dtype=dt, device=q.device)
     if last_state is None and want_state:
-        last_state = torch.empty(n, H, d, d, dtype=torch.float32, device=q.device)
+        last_state = torch.empty(st, dtype=torch.float32, device=q.device)
     if ws is None:
         ws = delta_workspace(q, v, cu)
-    if save is not None and save.numel() < load().flex_delta_save_bytes(ctypes.byref(shape)):
-        raise FlexError(FLEX_EWORKSPACE, "save")
-    st = (n, H, d, d)
     _check(load().flex_delta_fwd(
-        ctypes.byref(shape), q.data_ptr(), k.data_ptr(), v.data_ptr(), gp, bp, _offsets(cu),
-        d ** -0.5 if scale is None else scale, _plain(state, "state", st, torch.float32),
-        _plain(last_state, "last_state", st, torch.float32),
-        _plain(out, "out", (T, H, d), q.dtype), _ptr(save), _ptr(ws), ws.numel(),
-        _stream(stream)), "flex_delta_fwd")
+        ctypes.byref(shape), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+        _plain(g, "g", gates, dt, dev), _plain(beta, "beta", gates, dt, dev), cu_ptr,
+        d ** -0.5 if scale is None else scale, _plain(state, "state", st, torch.float32, dev),
+        _plain(last_state, "last_state", st, torch.float32, dev),
+        _plain(out, "out", (T, H, d), dt, dev), None if save is None else _saved(save, shape, dev),
+        _plain(ws, "ws", ws.shape, torch.uint8, dev), ws.numel(), _stream(stream)),
+        "flex_delta_fwd")
     return out, last_state
 
 
 def delta_bwd(q, k, v, g, beta, cu, dout, save, scale=None, dq=None, dk=None, dv=None, dg=None,
               dbeta=None, ws=None, stream=None):
     """(dq, dk, dv, dg, dbeta) of L = sum(dout * out) of delta_fwd, which filled `save`."""
-    T, H, d = v.shape
-    shape = _packed_delta(q, k, v, cu.numel() - 1)
-    dt, dev = q.dtype, q.device
-    gp, bp = (_plain(x, w, (T, H), dt) for x, w in ((g, "g"), (beta, "beta")))
-    shapes = (q.shape, k.shape, v.shape, g.shape, beta.shape)
-    names = ("dq", "dk", "dv", "dg", "dbeta")
-    grads = [torch.empty(s, dtype=dt, device=dev) if x is None else x
+    dev = torch.cuda.current_device()
+    cu_ptr = _offsets(cu, "cu", dev)
+    shape = _packed_delta(q, k, v, cu.numel() - 1, dev)
+    dt, T, H = q.dtype, v.shape[0], v.shape[1]
+    gates = (T, H)
+    names, shapes = ("dq", "dk", "dv", "dg", "dbeta"), (q.shape, k.shape, v.shape, gates, gates)
+    grads = [torch.empty(s, dtype=dt, device=q.device) if x is None else x
              for x, s in zip((dq, dk, dv, dg, dbeta), shapes)]
     if ws is None:
         ws = delta_workspace(q, v, cu, backward=True)
-    if save.numel() < load().flex_delta_save_bytes(ctypes.byref(shape)):
-        raise FlexError(FLEX_EWORKSPACE, "save")
     _check(load().flex_delta_bwd(
-        ctypes.byref(shape), q.data_ptr(), k.data_ptr(), v.data_ptr(), gp, bp, _offsets(cu),
-        d ** -0.5 if scale is None else scale, _plain(dout, "dout", (T, H, d), dt), _ptr(save),
-        *(_plain(x, w, s, dt) for x, w, s in zip(grads, names, shapes)), _ptr(ws), ws.numel(),
-        _stream(stream)), "flex_delta_bwd")
+        ctypes.byref(shape), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+        _plain(g, "g", gates, dt, dev), _plain(beta, "beta", gates, dt, dev), cu_ptr,
+        v.shape[2] ** -0.5 if scale is None else scale, _plain(dout, "dout", v.shape, dt, dev),
+        _saved(save, shape, dev),
+        *(_plain(x, w, s, dt, dev) for x, w, s in zip(grads, names, shapes)),
+        _plain(ws, "ws", ws.shape, torch.uint8, dev), ws.numel(), _stream(stream)),
+        "flex_delta_bwd")
     return tuple(grads)
 
 
 def delta_decode(q, k, v, g, beta, S, scale=None, out=None, stream=None):
     """One token of each sequence: q, k [n, Hk, d]; v [n, H, d]; g, beta [n, H]; the state S
     [n, H, d, d] fp32 is updated in place.  Returns out [n, H, d]."""
+    dev = torch.cuda.current_device()
+    shape = _packed_delta(q, k, v, v.shape[0], dev)
     n, H, d = v.shape
-    shape = _packed_delta(q, k, v, n)
-    gp, bp = (_plain(x, w, (n, H), q.dtype) for x, w in ((g, "g"), (beta, "beta")))
+    gates, dt = (n, H), q.dtype
     if out is None:
-        out = torch.empty(n, H, d, dtype=q.dtype, device=q.device)
-    _check(load().flex_delta_decode(
-        ctypes.byref(shape), q.data_ptr(), k.data_ptr(), v.data_ptr(), gp, bp,
-        d ** -0.5 if scale is None else scale, _plain(S, "S", (n, H, d, d), torch.float32),
-        _plain(out, "out", (n, H, d), q.dtype), _stream(stream)), "flex_delta_decode")
+        out = torch.empty((n, H, d), dtype=dt, device=q.device)
+    rc = load().flex_delta_decode(
+        ctypes.byref(shape), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+        _plain(g, "g", gates, dt, dev), _plain(beta, "beta", gates, dt, dev),
+        d ** -0.5 if scale is None else scale, _plain(S, "S", (n, H, d, d), torch.float32, dev),
+        _plain(out, "out", (n, H, d), dt, dev), _stream(stream))
+    if rc:
+        raise FlexError(rc, "flex_delta_decode")
     return out
 
 
 def softattn_workspace(q, k, cu_q) -> torch.Tensor:
     """A caller-owned workspace for softattn_fwd on such tensors."""
-    shape = _packed_attn(q, k, k, cu_q.numel() - 1)
+    shape = _packed_attn(q, k, k, cu_q.numel() - 1, torch.cuda.current_device())
     return _zeros(int(load().flex_softattn_workspace_bytes(ctypes.byref(shape))),
                   "flex_softattn_workspace_bytes", q.device)
 
@@ -461,11 +476,12 @@ def softattn_fwd(q, k, v, cu_q, cu_k=None, causal=True, scale=None, out=None, ls
     """Softmax attention over packed sequences: (out [T, H, d], lse [T, H] fp32 or None).
     q [T, H, d] with offsets cu_q; k, v [Tk, Hk, d] with offsets cu_k (default cu_q).  causal:
     the last query of a sequence sees all its keys.  scale: default 1 / sqrt(d)."""
-    T, H, d = q.shape
+    dev = torch.cuda.current_device()
     cu_k = cu_q if cu_k is None else cu_k
     if cu_k.shape != cu_q.shape:
         raise ValueError("cu_q and cu_k are of one length")
-    shape = _packed_attn(q, k, v, cu_q.numel() - 1)
+    shape = _packed_attn(q, k, v, cu_q.numel() - 1, dev)
+    T, H, d = q.shape
     if out is None:
         out = torch.empty(T, H, d, dtype=q.dtype, device=q.device)
     if lse is None and want_lse:
@@ -473,10 +489,13 @@ def softattn_fwd(q, k, v, cu_q, cu_k=None, causal=True, scale=None, out=None, ls
     if ws is None:
         ws = softattn_workspace(q, k, cu_q)
     _check(load().flex_softattn_fwd(
-        ctypes.byref(shape), q.data_ptr(), k.data_ptr(), v.data_ptr(), _offsets(cu_q, "cu_q"),
-        _offsets(cu_k, "cu_k"), d ** -0.5 if scale is None else scale, int(bool(causal)),
-        _plain(out, "out", (T, H, d), q.dtype), _plain(lse, "lse", (T, H), torch.float32),
-        _ptr(ws), ws.numel(), _stream(stream)), "flex_softattn_fwd")
+        ctypes.byref(shape), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+        _offsets(cu_q, "cu_q", dev), _offsets(cu_k, "cu_k", dev),
+        d ** -0.5 if scale is None else scale, int(bool(causal)),
+        _plain(out, "out", (T, H, d), q.dtype, dev),
+        _plain(lse, "lse", (T, H), torch.float32, dev),
+        _plain(ws, "ws", ws.shape, torch.uint8, dev), ws.numel(), _stream(stream)),
+        "flex_softattn_fwd")
     return out, lse
 
 

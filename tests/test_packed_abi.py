@@ -123,9 +123,27 @@ def test_binding_refuses_what_is_not_on_the_gpu_or_does_not_fit():
         flexattn.delta_fwd(q, q, v, g, g, cu)
     with pytest.raises((ValueError, RuntimeError, AssertionError)):
         flexattn.softattn_fwd(v, q, q, cu)
+    cpu, f32 = q.get_device(), torch.float32
+    rows = torch.zeros(10, 64, 4).transpose(1, 2)
+    with pytest.raises(ValueError):  # heads not contiguous
+        flexattn._rows(rows, "q", rows.shape, f32, cpu)
+    with pytest.raises(ValueError):  # another shape, another type, another device
+        flexattn._rows(q, "q", (10, 3, 64), f32, cpu)
     with pytest.raises(ValueError):
-        flexattn._rows(torch.zeros(10, 64, 4).transpose(1, 2), "q")
+        flexattn._rows(q, "q", q.shape, torch.bfloat16, cpu)
     with pytest.raises(ValueError):
-        flexattn._offsets(torch.zeros(3, dtype=torch.int64))
+        flexattn._rows(q, "q", q.shape, f32, 0)
+    wide = torch.zeros(10, 3 * 128)
+    assert flexattn._rows(wide[:, 128:256].view(10, 2, 64), "q", (10, 2, 64), f32, cpu) == 384
+    for bad in (torch.zeros(3, dtype=torch.int64), torch.zeros(1, dtype=torch.int32),
+                torch.zeros(2, 2, dtype=torch.int32)):
+        with pytest.raises(ValueError):
+            flexattn._offsets(bad, "cu", cpu)
     with pytest.raises(ValueError):
-        flexattn._plain(torch.zeros(3, 4), "g", (3, 5), torch.float32)
+        flexattn._plain(torch.zeros(3, 4), "g", (3, 5), f32, cpu)
+    with pytest.raises(ValueError):
+        flexattn._plain(torch.zeros(4, 3).t(), "g", (3, 4), f32, cpu)
+    with pytest.raises(ValueError):
+        flexattn._rank3(torch.zeros(3, 4), "q")
+    with pytest.raises(TypeError):
+        flexattn._dtype_code(torch.zeros(3, dtype=torch.float16))
