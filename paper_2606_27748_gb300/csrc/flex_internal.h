@@ -158,6 +158,7 @@ cudaError_t launch_tc_delta_bwd(const Packed& p, const void* q, const void* k, c
 int softattn_splits(const Packed& p);  // ranges of keys per tile of rows (1-32)
 cudaError_t launch_softattn_simt(const AttnArgs& x, cudaStream_t s);
 bool tc_softattn_supported(const Packed& p);  // tensor cores: bf16 storage
+int tc_softattn_rows(const Packed& p);        // rows of a block: 32, 128 or 256
 cudaError_t launch_tc_softattn(const AttnArgs& x, cudaStream_t s);
 cudaError_t launch_softattn_join(const AttnArgs& x, cudaStream_t s);
 

@@ -215,16 +215,17 @@ cudaError_t launch_simt(const AttnArgs& x, cudaStream_t s)
 int softattn_splits(const Packed& p)
 {
     // Ranges of keys per tile.  Rows that fill their tiles are cut only as far as it takes to
-    // give every SM a block: each range costs 4 (d + 1) bytes a row, written and read.  Rows that
-    // do not (single tokens) cost next to nothing to join, and four blocks an SM even out the
-    // sequences' different lengths.  A range is 256 keys of an average sequence or more; 32
-    // ranges (the join's lanes) at most.
+    // give every SM a block: each range costs 4 (d + 1) bytes a row, written and read.  A few rows
+    // (single tokens) cost next to nothing to join, and eight blocks an SM even out the sequences'
+    // different lengths.  A range is 256 keys of an average sequence or more; 32 ranges (the
+    // join's lanes) at most.
     const int G = p.H / p.Hk;
     const bool tc = tc_softattn_supported(p);
-    const int tokens = tc ? 2 * (128 / G) : kRows / G;  // of a block
-    const long long slots = block_slots(p.T, p.n, tokens), blocks = slots * p.Hk;
-    const bool few = (long long)p.T * 8 <= slots * tokens;
-    const long long want = ((few ? 4 : tc ? 1 : 2) * 152 + blocks - 1) / blocks;
+    const int rows = tc ? tc_softattn_rows(p) : kRows;
+    const int tokens = rows == 256 ? 2 * (128 / G) : rows / G;  // of a block
+    const long long blocks = (long long)block_slots(p.T, p.n, tokens) * p.Hk;
+    const bool few = (long long)p.T * G <= 32LL * p.n;
+    const long long want = ((few ? 8 : tc ? 1 : 2) * 152 + blocks - 1) / blocks;
     const long long most = (long long)p.Tk / p.n / 256;
     const long long n = want < most ? want : most;
     return n < 1 ? 1 : n > 32 ? 32 : (int)n;

@@ -2,16 +2,20 @@
 // out_i = sum_j softmax_j(scale q_i . k_j) v_j, one pass over the keys with the running maximum
 // and sum of every row.
 //
-// A CTA takes two tiles of 128 rows of one sequence and key head.  The G = H / Hk heads that
+// A CTA takes two tiles (short sequences: one) of 128 rows of one sequence and key head.  The G = H / Hk heads that
 // share the key head are rows of a tile (row = token * G + head, 128 / G tokens), so K and V
 // are read once for all of them, and one TMA box (64 elements, G heads, 128 / G tokens) brings
 // a tile in that order.  While one tile's scores are turned into weights, the tensor core works
 // on the other tile:
 //   warps 0-3, 4-7  softmax of tile A, B: a thread per row
-//   warp 8          issues S = Q K^T (tcgen05, both operands in shared memory) and
+//   the next warp   issues S = Q K^T (tcgen05, both operands in shared memory) and
 //                   O += P V (P as bf16 in tensor memory, over its scores)
-//   warp 9          TMA: Q once, then K and V tiles of 128 keys through a ring of buffers
-// Tensor memory (512 columns): S/P of A and B, O of A and B.
+//   the last warp   TMA: Q once, then K and V tiles of 128 keys through a ring of buffers
+// Tensor memory (512 columns; one tile 256): S/P of A and B, O of A and B.
+// Sequences of at most 128 rows would leave tile B empty; with one tile a CTA takes half the
+// tensor memory and shared memory, and the two CTAs of an SM hide each other's start and end.  Of
+// at most 32 rows (single tokens above all) one softmax warp is enough, and only 32 rows of Q are
+// kept: the product's other 96 rows read whatever lies behind them and are not looked at.
 //
 // The maximum that a row's weights refer to only has to keep them in range: it is raised (and
 // O and the sum rescaled) when the true one exceeds it by more than 2^8, so after the first
@@ -27,17 +31,24 @@ namespace {
 
 using namespace tc;
 
-constexpr int kThreads = 320, kKeys = 128;
-constexpr int kWarpMma = 8, kWarpTma = 9;
+constexpr int kKeys = 128;
 constexpr float kSlack = 8.f;  // in powers of two
 
-template <int D>
+// ROWS: of a CTA, 256 (two tiles), 128 or 32.
+template <int D, int ROWS>
 struct Lay {
-    static constexpr uint32_t TILE = 128 * D * 2;  // one tile of 128 rows
-    static constexpr int NB = D == 128 ? 5 : 8;    // K and V tiles in flight
-    static constexpr uint32_t Q = 0, KV = 2 * TILE;
+    static constexpr int TILES = ROWS == 256 ? 2 : 1, R = ROWS / TILES;  // rows in use of a tile
+    static constexpr int SW = R / 32, MMA = SW * TILES, TMA = MMA + 1;
+    // whole warpgroups, so that the softmax warps can take registers that the others give back:
+    // 384 x 168 = 256 x 216 + 128 x 72; 256 x 128 = 128 x 184 + 128 x 72
+    static constexpr int THREADS = ROWS == 32 ? 96 : 128 * (TILES + 1);
+    static constexpr int MORE = ROWS == 256 ? 216 : 184, LESS = 72;
+    static constexpr uint32_t TILE = 128 * D * 2;  // one K or V tile
+    static constexpr uint32_t QB = R * 128, QT = QB * (D / 64);  // 64 elements of a Q tile, a Q tile
+    static constexpr int NB = ROWS == 256 ? (D == 128 ? 5 : 8) : ROWS == 128 ? (D == 128 ? 2 : 5) : (D == 128 ? 3 : 6);
+    static constexpr uint32_t Q = 0, KV = TILES * QT;
     static constexpr uint32_t SMEM = KV + NB * TILE + 1024;  // + alignment
-    static constexpr int T_S = 0, T_O = 256;
+    static constexpr int T_S = 0, T_O = 128 * TILES, COLS = 256 * TILES;
 };
 
 struct Bars {
@@ -69,13 +80,14 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* v)
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 
-template <int D>
-__global__ void __launch_bounds__(kThreads, 1)
+template <int D, int ROWS>
+__global__ void __launch_bounds__(Lay<D, ROWS>::THREADS, ROWS == 256 ? 1 : 2)
     tc_softattn_kernel(const __grid_constant__ CUtensorMap tmap_q,
                        const __grid_constant__ CUtensorMap tmap_k,
                        const __grid_constant__ CUtensorMap tmap_v, AttnArgs x)
 {
-    using L = Lay<D>;
+    using L = Lay<D, ROWS>;
+    constexpr int TILES = L::TILES;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* sm = smem_raw + ((0u - smem_u32(smem_raw)) & 1023u);  // (stays a shared-memory pointer)
     const uint32_t sb = smem_u32(sm);
@@ -85,17 +97,15 @@ __global__ void __launch_bounds__(kThreads, 1)
 
     const Packed& pk = x.p;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int G = pk.H / pk.Hk, tpt = 128 / G;  // tokens of a tile
-    const int hk = blockIdx.y % pk.Hk, split = blockIdx.y / pk.Hk;
+    const int G = pk.H / pk.Hk, tpt = L::R / G;  // tokens of a tile
+    const int hk = blockIdx.x % pk.Hk, split = blockIdx.x / pk.Hk;
     int s, block, qlo, qhi, klo, khi;
-    // the last slots first: with the causal mask a sequence's later rows have more keys
-    if (!find_block(x.cu_q, pk.n, pk.T, 2 * tpt, (int)(gridDim.x - 1 - blockIdx.x), s, block, qlo, qhi))
-        return;
+    if (!find_tile(x, TILES * tpt, (int)(blockIdx.z * gridDim.y + blockIdx.y), s, block, qlo, qhi)) return;
     seq_rows(x.cu_k, s, pk.Tk, klo, khi);
-    const int t0 = block * 2 * tpt, rows_left = qhi - qlo - t0;
+    const int t0 = block * TILES * tpt, rows_left = qhi - qlo - t0;
     const int lk = khi - klo, shift = lk - (qhi - qlo);
     // tokens and key blocks [first, last) of each tile; a tile without tokens takes none
-    const int ntA = min(tpt, rows_left), ntB = min(tpt, max(rows_left - tpt, 0));
+    const int ntA = min(tpt, rows_left), ntB = TILES == 2 ? min(tpt, max(rows_left - tpt, 0)) : 0;
     int firstA, lastA, firstB, lastB;
     key_range(x, kKeys, lk, t0 + ntA - 1 + shift, split, firstA, lastA);
     key_range(x, kKeys, lk, t0 + tpt + ntB - 1 + shift, split, firstB, lastB);
@@ -111,7 +121,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int i = 0; i < 2; ++i) {
             mbar_init(&bars.q_full[i], 1);
             mbar_init(&bars.s_full[i], 1);
-            mbar_init(&bars.p_ready[i], 4);
+            mbar_init(&bars.p_ready[i], L::SW);
             mbar_init(&bars.o_full[i], 1);
         }
         for (int i = 0; i < L::NB; ++i) {
@@ -121,8 +131,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         abort_flag = 0;
         fence_mbar_init();
     }
-    if (warp == kWarpMma) {
-        tmem_alloc(&tmem_base_sh, 512);
+    if (warp == L::MMA) {
+        tmem_alloc(&tmem_base_sh, L::COLS);
         tmem_relinquish();
     }
     fence_before_sync();
@@ -130,14 +140,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     fence_after_sync();
     const uint32_t tm = tmem_base_sh;
 
-    if (warp == kWarpTma) {
+    if (warp >= L::MMA) {
+    if (ROWS != 32) setmaxnreg_dec<L::LESS>();
+    if (warp == L::TMA) {
         // ---- Q of both tiles, then K and V of every block: tile 2 i is K of block first + i,
         // tile 2 i + 1 its V; tile n goes to buffer n % NB ----
         for (int X = 0; X < (ntB > 0 ? 2 : 1); ++X) {
             if (first == last) break;
             wmbar_arrive_expect_tx(&bars.q_full[X], (uint32_t)(tpt * G * D * 2));
             for (int b = 0; b < D / 64; ++b)
-                wtma_load_3d(sb + L::Q + X * L::TILE + b * 16384, &tmap_q, 64 * b, hk * G,
+                wtma_load_3d(sb + L::Q + X * L::QT + b * L::QB, &tmap_q, 64 * b, hk * G,
                              qlo + t0 + X * tpt, &bars.q_full[X]);
         }
         uint32_t ph = 0;  // parity of `empty` per buffer
@@ -153,7 +165,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 wtma_load_3d(sb + L::KV + buf * L::TILE + b * 16384, n & 1 ? &tmap_v : &tmap_k,
                              64 * b, hk, row, &bars.full[buf]);
         }
-    } else if (warp == kWarpMma) {
+    } else if (warp == L::MMA) {
         constexpr uint32_t I_S = idesc_bf16(128, kKeys, 0, 0), I_O = idesc_bf16(128, D, 0, 1);
         auto adv = [](uint64_t d, uint32_t bytes) { return d + (bytes >> 4); };
         bool ok = true;
@@ -165,20 +177,20 @@ __global__ void __launch_bounds__(kThreads, 1)
         };
         const int f[2] = {firstA, firstB}, l[2] = {lastA, lastB};
         auto scores = [&](int X, int j) {  // S_X = Q_X K_j^T
-            const uint64_t dq = sdesc(sb + L::Q + X * L::TILE, 16, 1024);
+            const uint64_t dq = sdesc(sb + L::Q + X * L::QT, 16, 1024);
             const uint64_t dk = sdesc(sb + L::KV + (uint32_t)((2 * (j - first)) % L::NB) * L::TILE, 16, 1024);
 #pragma unroll
             for (int ks = 0; ks < D / 16; ++ks)
-                wmma_bf16(tm + L::T_S + 128 * X, adv(dq, (ks >> 2) * 16384 + (ks & 3) * 32),
+                wmma_bf16(tm + L::T_S + 128 * X, adv(dq, (ks >> 2) * L::QB + (ks & 3) * 32),
                           adv(dk, (ks >> 2) * 16384 + (ks & 3) * 32), I_S, ks > 0);
             wmma_commit(&bars.s_full[X]);
         };
-        for (int X = 0; X < 2; ++X)
+        for (int X = 0; X < TILES; ++X)
             if (f[X] < l[X] && ok) ok = bar_wait_w(&bars.q_full[X], 0, &abort_flag, x.status);
         for (int j = first - 1; j < last && ok; ++j) {
             const int n = 2 * (j - first);
             bool have_v = false, have_k = false;
-            for (int X = 0; X < 2; ++X) {
+            for (int X = 0; X < TILES; ++X) {
                 if (j >= f[X] && j < l[X]) {
                     if (!have_v) {
                         wait_tile(n + 1);
@@ -219,9 +231,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (j >= first) wmma_commit(&bars.empty[(n + 1) % L::NB]);
             if (j + 1 < last) wmma_commit(&bars.empty[(n + 2) % L::NB]);
         }
+    }
     } else {
+        if (ROWS != 32) setmaxnreg_inc<L::MORE>();
         // ---- softmax: one row per thread ----
-        const int X = warp >> 2, r = tid & 127, fX = X ? firstB : firstA, lX = X ? lastB : lastA;
+        const int X = warp / L::SW, r = 32 * (warp % L::SW) + lane, fX = X ? firstB : firstA, lX = X ? lastB : lastA;
         const int nt = X ? ntB : ntA, tok = t0 + X * tpt + r / G;
         const bool mine = r < nt * G;
         // keys this row sees; a row of no token takes them all (its result goes nowhere)
@@ -252,7 +266,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             float top[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-            for (int i = 4; i < kKeys; ++i) top[i & 3] = fmaxf(top[i & 3], v[i]);
+            for (int i = 4; i < kKeys; i += 8) {  // (pairs: a maximum of three takes one instruction)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (i + e + 4 < kKeys) top[e] = fmaxf(top[e], fmaxf(v[i + e], v[i + e + 4]));
+                    else top[e] = fmaxf(top[e], v[i + e]);
+            }
             const float now = c * fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
             const bool raise = now > m + kSlack;  // (from -inf on the first key seen)
             if (__any_sync(0xffffffffu, raise)) {
@@ -276,21 +295,28 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             }
             const float base = m == -INFINITY ? 0.f : -m;
-            float sum[4] = {};
+            const uint64_t cc = f2_pack(c, c), bb = f2_pack(base, base), one = f2_pack(1.f, 1.f);
+            uint64_t sum[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
 #pragma unroll
             for (int i = 0; i < kKeys / 32; ++i) {
                 uint32_t w[16];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const float p0 = ex2(fmaf(v[32 * i + 2 * e], c, base));
-                    const float p1 = ex2(fmaf(v[32 * i + 2 * e + 1], c, base));
-                    sum[e & 1] += p0;
-                    sum[2 + (e & 1)] += p1;
+                    float p0, p1;
+                    f2_unpack(f2_fma(f2_pack(v[32 * i + 2 * e], v[32 * i + 2 * e + 1]), cc, bb), p0, p1);
+                    p0 = ex2(p0);
+                    p1 = ex2(p1);
+                    sum[e & 1] = f2_fma(f2_pack(p0, p1), one, sum[e & 1]);
                     w[e] = pack_bf16(p0, p1);
                 }
                 tmem_st16(ts + 16 * i, w);
             }
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            {
+                float a, b, d, e;
+                f2_unpack(sum[0], a, b);
+                f2_unpack(sum[1], d, e);
+                l += (a + b) + (d + e);
+            }
             tmem_wait_st();
             fence_before_sync();
             __syncwarp();
@@ -340,9 +366,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     __syncthreads();
     drain_after_abort(abort_flag);
-    if (warp == kWarpMma) {
+    if (warp == L::MMA) {
         fence_after_sync();
-        tmem_dealloc(tm, 512);
+        tmem_dealloc(tm, L::COLS);
     }
 }
 
@@ -363,27 +389,45 @@ bool make_rows_map(CUtensorMap* m, const void* base, int T, int heads, int d, lo
                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D>
+template <int D, int ROWS>
 cudaError_t launch(const AttnArgs& x, cudaStream_t s)
 {
+    using L = Lay<D, ROWS>;
     const Packed& p = x.p;
-    const int G = p.H / p.Hk, tpt = 128 / G;
+    const int G = p.H / p.Hk, tpt = L::R / G;
     CUtensorMap mq, mk, mv;
     if (!make_rows_map(&mq, x.q, p.T, p.H, D, p.qs, G, tpt) ||
         !make_rows_map(&mk, x.k, p.Tk, p.Hk, D, p.ks, 1, kKeys) ||
         !make_rows_map(&mv, x.v, p.Tk, p.Hk, D, p.vs, 1, kKeys))
         return cudaErrorInvalidValue;
-    const int smem = (int)Lay<D>::SMEM;
-    cudaError_t e = cudaFuncSetAttribute(tc_softattn_kernel<D>,
-                                         cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    cudaError_t e = cudaFuncSetAttribute(tc_softattn_kernel<D, ROWS>,
+                                         cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L::SMEM);
     if (e != cudaSuccess) return e;
-    const dim3 grid((unsigned)block_slots(p.T, p.n, 2 * tpt), (unsigned)(p.Hk * x.splits));
-    return launch_after(tc_softattn_kernel<D>, grid, kThreads, smem, 0, false, s, mq, mk, mv, x);
+    // key heads and ranges of a tile side by side, then the tiles, longest first
+    const int slots = block_slots(p.T, p.n, L::TILES * tpt), y = slots < 65535 ? slots : 65535;
+    const dim3 grid((unsigned)(p.Hk * x.splits), (unsigned)y, (unsigned)((slots + y - 1) / y));
+    return launch_after(tc_softattn_kernel<D, ROWS>, grid, L::THREADS, (int)L::SMEM, 0, false, s, mq, mk,
+                        mv, x);
+}
+
+template <int D>
+cudaError_t launch(const AttnArgs& x, cudaStream_t s)
+{
+    const int rows = tc_softattn_rows(x.p);
+    return rows == 32 ? launch<D, 32>(x, s) : rows == 128 ? launch<D, 128>(x, s) : launch<D, 256>(x, s);
 }
 
 }  // namespace
 
 bool tc_softattn_supported(const Packed& p) { return p.bf16 && (p.d == 64 || p.d == 128); }
+
+// What holds an average sequence's rows.
+int tc_softattn_rows(const Packed& p)
+{
+    const int G = p.H / p.Hk;
+    const long long rows = (long long)p.T * G;
+    return G <= 32 && rows <= 32LL * p.n ? 32 : rows <= 128LL * p.n ? 128 : 256;
+}
 
 cudaError_t launch_tc_softattn(const AttnArgs& x, cudaStream_t s)
 {
