@@ -186,13 +186,13 @@ __global__ void __launch_bounds__(128) softattn_join_kernel(AttnArgs x)
     const float inv = total > 0.f ? 1.f / total : 0.f;
     const int c = 4 * lane;
     float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s = 0; s < x.splits; ++s) {
+    const float* part = x.part + row * pk.d + min(c, pk.d - 4);
+#pragma unroll 8
+    for (int s = 0; s < x.splits; ++s) {  // (every range has written its rows: 0 if it saw no key)
         const float w = __shfl_sync(0xffffffffu, weight, s) * inv;
-        if (w != 0.f && c < pk.d) {
-            const float4 v = load4(x.part + (s * rows + row) * pk.d + c);
-            y.x = fmaf(w, v.x, y.x); y.y = fmaf(w, v.y, y.y);
-            y.z = fmaf(w, v.z, y.z); y.w = fmaf(w, v.w, y.w);
-        }
+        const float4 v = load4(part + s * rows * pk.d);
+        y.x = fmaf(w, v.x, y.x); y.y = fmaf(w, v.y, y.y);
+        y.z = fmaf(w, v.z, y.z); y.w = fmaf(w, v.w, y.w);
     }
     if (c < pk.d) store4((T*)x.out + row * pk.d + c, y);
     if (lane == 0 && x.lse) x.lse[row] = top == -INFINITY ? -INFINITY : top + logf(total);

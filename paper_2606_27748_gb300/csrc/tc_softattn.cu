@@ -8,10 +8,17 @@
 // a tile in that order.  While one tile's scores are turned into weights, the tensor core works
 // on the other tile:
 //   warps 0-3, 4-7  softmax of tile A, B: a thread per row
-//   the next warp   issues S = Q K^T (tcgen05, both operands in shared memory) and
-//                   O += P V (P as bf16 in tensor memory, over its scores)
+//   then            S = Q K^T (tcgen05, both operands in shared memory) and O += P V (P as bf16 in
+//                   tensor memory) issued by one warp that takes the tiles in turn; for d = 64 by a
+//                   warp for each
 //   the last warp   TMA: Q once, then K and V tiles of 128 keys through a ring of buffers
-// Tensor memory (512 columns; one tile 256): S/P of A and B, O of A and B.
+// Tensor memory (512 columns; one tile 256): S of A and B, O of A and B.  For d = 128 that is all of
+// it, P takes the place of its scores, and the products (2050 cycles for a block of 128 keys and both
+// tiles) bound the kernel; a warp for each tile's products made it slower (16384 keys, H16 Hk4: 699 ->
+// 907 us).  For d = 64 the softmax does (maxima, exponentials and sums in turn, 1350 cycles a tile):
+// P has columns of its own, so that the next scores are there when the softmax wants them, and each
+// tile's products are issued when that tile is ready (packed prompts 4000, 1531, .., H12: 53 -> 47 us).
+// Two threads to a row, 16 softmax warps, were slower for both (764 us, 54 us).
 // Sequences of at most 128 rows would leave tile B empty; with one tile a CTA takes half the
 // tensor memory and shared memory, and the two CTAs of an SM hide each other's start and end.  Of
 // at most 32 rows (single tokens above all) one softmax warp is enough, and only 32 rows of Q are
@@ -38,7 +45,9 @@ constexpr float kSlack = 8.f;  // in powers of two
 template <int D, int ROWS>
 struct Lay {
     static constexpr int TILES = ROWS == 256 ? 2 : 1, R = ROWS / TILES;  // rows in use of a tile
-    static constexpr int SW = R / 32, MMA = SW * TILES, TMA = MMA + 1;
+    static constexpr bool OWN_P = D == 64;             // see above
+    static constexpr int ISSUERS = OWN_P ? TILES : 1;  // warps that issue products
+    static constexpr int SW = R / 32, MMA = SW * TILES, TMA = MMA + ISSUERS;
     // whole warpgroups, so that the softmax warps can take registers that the others give back:
     // 384 x 168 = 256 x 216 + 128 x 72; 256 x 128 = 128 x 184 + 128 x 72
     static constexpr int THREADS = ROWS == 32 ? 96 : 128 * (TILES + 1);
@@ -49,10 +58,11 @@ struct Lay {
     static constexpr uint32_t Q = 0, KV = TILES * QT;
     static constexpr uint32_t SMEM = KV + NB * TILE + 1024;  // + alignment
     static constexpr int T_S = 0, T_O = 128 * TILES, COLS = 256 * TILES;
+    static constexpr int T_P = OWN_P ? T_O + D * TILES : T_S, P_STEP = OWN_P ? 64 : 128;  // of a tile
 };
 
 struct Bars {
-    uint64_t q_full[2], full[8], empty[8], s_full[2], p_ready[2], o_full[2];
+    uint64_t q_full[2], full[8], empty[8], s_full[2], s_loaded[2], p_ready[2], pv_done[2];
 };
 
 __device__ __forceinline__ float ex2(float x)
@@ -122,11 +132,12 @@ __global__ void __launch_bounds__(Lay<D, ROWS>::THREADS, ROWS == 256 ? 1 : 2)
             mbar_init(&bars.q_full[i], 1);
             mbar_init(&bars.s_full[i], 1);
             mbar_init(&bars.p_ready[i], L::SW);
-            mbar_init(&bars.o_full[i], 1);
+            mbar_init(&bars.s_loaded[i], L::SW);
+            mbar_init(&bars.pv_done[i], 1);
         }
         for (int i = 0; i < L::NB; ++i) {
             mbar_init(&bars.full[i], 1);
-            mbar_init(&bars.empty[i], 1);
+            mbar_init(&bars.empty[i], L::ISSUERS);
         }
         abort_flag = 0;
         fence_mbar_init();
@@ -138,11 +149,18 @@ __global__ void __launch_bounds__(Lay<D, ROWS>::THREADS, ROWS == 256 ? 1 : 2)
     fence_before_sync();
     __syncthreads();
     fence_after_sync();
-    const uint32_t tm = tmem_base_sh;
+    // All of tensor memory starts at its address 0; as a constant it spares the issuing warps moves
+    // to uniform registers.
+    const uint32_t tm = L::COLS == 512 && L::OWN_P ? 0u : tmem_base_sh;
+    if (tmem_base_sh != tm && tid == 0) {  // (cannot be; nothing is issued then)
+        abort_flag = 1;
+        if (x.status) atomicExch(x.status, (int)FLEX_ECUDA);
+    }
 
     if (warp >= L::MMA) {
     if (ROWS != 32) setmaxnreg_dec<L::LESS>();
-    if (warp == L::TMA) {
+    if (tmem_base_sh != tm) {
+    } else if (warp == L::TMA) {
         // ---- Q of both tiles, then K and V of every block: tile 2 i is K of block first + i,
         // tile 2 i + 1 its V; tile n goes to buffer n % NB ----
         for (int X = 0; X < (ntB > 0 ? 2 : 1); ++X) {
@@ -165,71 +183,94 @@ __global__ void __launch_bounds__(Lay<D, ROWS>::THREADS, ROWS == 256 ? 1 : 2)
                 wtma_load_3d(sb + L::KV + buf * L::TILE + b * 16384, n & 1 ? &tmap_v : &tmap_k,
                              64 * b, hk, row, &bars.full[buf]);
         }
-    } else if (warp == L::MMA) {
+    } else if (warp < L::TMA) {
         constexpr uint32_t I_S = idesc_bf16(128, kKeys, 0, 0), I_O = idesc_bf16(128, D, 0, 1);
         auto adv = [](uint64_t d, uint32_t bytes) { return d + (bytes >> 4); };
-        bool ok = true;
-        uint32_t ph_full = 0, ph_p[2] = {0, 0};
-        auto wait_tile = [&](int n) {  // tile n has landed (each tile is waited for once)
-            const int buf = n % L::NB;
-            if (ok) ok = bar_wait_w(&bars.full[buf], (ph_full >> buf) & 1, &abort_flag, x.status);
-            ph_full ^= 1u << buf;
-        };
         const int f[2] = {firstA, firstB}, l[2] = {lastA, lastB};
-        auto scores = [&](int X, int j) {  // S_X = Q_X K_j^T
-            const uint64_t dq = sdesc(sb + L::Q + X * L::QT, 16, 1024);
-            const uint64_t dk = sdesc(sb + L::KV + (uint32_t)((2 * (j - first)) % L::NB) * L::TILE, 16, 1024);
+        bool ok = true;
+        auto wait = [&](uint64_t* bar, int phase) {
+            if (ok) ok = bar_wait_w(bar, (uint32_t)phase & 1, &abort_flag, x.status);
+            fence_after_sync();
+            return ok;
+        };
+        // K of block j is tile 2 (j - first), its V the next
+        auto buffer = [&](int n) { return sb + L::KV + (uint32_t)(n % L::NB) * L::TILE; };
+        auto landed = [&](int n) { return wait(&bars.full[n % L::NB], n / L::NB); };
+        auto release = [&](int n) { wmma_commit(&bars.empty[n % L::NB]); };
+        auto scores = [&](int X, int j) {  // S = Q K_j^T
+            const int n = 2 * (j - first);
+            if (L::OWN_P && (!landed(n) || (j > f[X] && !wait(&bars.s_loaded[X], j - 1 - f[X])))) return;
+            const uint64_t dq = sdesc(sb + L::Q + X * L::QT, 16, 1024), dk = sdesc(buffer(n), 16, 1024);
 #pragma unroll
             for (int ks = 0; ks < D / 16; ++ks)
                 wmma_bf16(tm + L::T_S + 128 * X, adv(dq, (ks >> 2) * L::QB + (ks & 3) * 32),
                           adv(dk, (ks >> 2) * 16384 + (ks & 3) * 32), I_S, ks > 0);
             wmma_commit(&bars.s_full[X]);
         };
-        for (int X = 0; X < TILES; ++X)
-            if (f[X] < l[X] && ok) ok = bar_wait_w(&bars.q_full[X], 0, &abort_flag, x.status);
-        for (int j = first - 1; j < last && ok; ++j) {
-            const int n = 2 * (j - first);
-            bool have_v = false, have_k = false;
-            for (int X = 0; X < TILES; ++X) {
-                if (j >= f[X] && j < l[X]) {
-                    if (!have_v) {
-                        wait_tile(n + 1);
-                        have_v = true;
-                        if (!ok) break;
-                        // rows behind the sequence's end are another's, and 0 * NaN is NaN
-                        if ((j + 1) * kKeys > lk) {
-                            const uint32_t v = sb + L::KV + (uint32_t)((n + 1) % L::NB) * L::TILE;
-                            for (int e = (lk - j * kKeys) * 8 + lane; e < kKeys * 8; e += 32)
-                                for (int b = 0; b < D / 64; ++b)
-                                    st_shared_v4(v + b * 16384 + e * 16, 0, 0, 0, 0);
-                            fence_proxy_async();
-                            __syncwarp();
-                        }
-                    }
-                    ok = bar_wait_w(&bars.p_ready[X], ph_p[X], &abort_flag, x.status);
-                    ph_p[X] ^= 1;
-                    if (!ok) break;
-                    fence_after_sync();
-                    const uint64_t dv = sdesc(sb + L::KV + (uint32_t)((n + 1) % L::NB) * L::TILE, 16384, 1024);
-#pragma unroll
-                    for (int ks = 0; ks < kKeys / 16; ++ks)
-                        wmma_bf16_tmem_a(tm + L::T_O + D * X, tm + L::T_S + 128 * X + 8 * ks,
-                                         adv(dv, ks * 2048), I_O, (j > f[X]) || ks > 0);
-                    if (j + 1 == l[X]) wmma_commit(&bars.o_full[X]);
-                }
-                if (j + 1 >= f[X] && j + 1 < l[X]) {
-                    if (!have_k) {
-                        wait_tile(n + 2);
-                        have_k = true;
-                        if (!ok) break;
-                    }
-                    scores(X, j + 1);
-                }
+        auto have_v = [&](int j) {
+            const int n = 2 * (j - first) + 1;
+            // rows behind the sequence's end are another's, and 0 * NaN is NaN (every issuing warp
+            // clears them: what it then reads is cleared)
+            if (landed(n) && (j + 1) * kKeys > lk) {
+                for (int e = (lk - j * kKeys) * 8 + lane; e < kKeys * 8; e += 32)
+                    for (int b = 0; b < D / 64; ++b) st_shared_v4(buffer(n) + b * 16384 + e * 16, 0, 0, 0, 0);
+                fence_proxy_async();
+                __syncwarp();
             }
-            if (!ok) break;
-            // buffers whose last reader has been issued (each block has a reader among A and B)
-            if (j >= first) wmma_commit(&bars.empty[(n + 1) % L::NB]);
-            if (j + 1 < last) wmma_commit(&bars.empty[(n + 2) % L::NB]);
+        };
+        auto weighted = [&](int X, int j) {  // O += P V_j
+            const int n = 2 * (j - first) + 1;
+            if (L::OWN_P) have_v(j);
+            if (!wait(&bars.p_ready[X], j - f[X])) return;
+            const uint64_t dv = sdesc(buffer(n), 16384, 1024);
+#pragma unroll
+            for (int ks = 0; ks < kKeys / 16; ++ks)
+                wmma_bf16_tmem_a(tm + L::T_O + D * X, tm + L::T_P + L::P_STEP * X + 8 * ks,
+                                 adv(dv, ks * 2048), I_O, (j > f[X]) || ks > 0);
+            if (L::OWN_P || j + 1 == l[X]) wmma_commit(&bars.pv_done[X]);
+        };
+        if (L::OWN_P) {
+            const int X = warp - L::MMA;
+            auto pass = [&](int j) {  // a block of the other tile's only
+                for (int n = 2 * (j - first); n < 2 * (j - first) + 2; ++n)
+                    if (landed(n) && lane == 0) mbar_arrive(&bars.empty[n % L::NB]);
+            };
+            auto both = [&](int j, bool k, bool v) {  // the scores of block j + 1, then block j's O
+                if (k) {
+                    scores(X, j + 1);
+                    if (ok) release(2 * (j + 1 - first));
+                }
+                if (v && ok) {
+                    weighted(X, j);
+                    if (ok) release(2 * (j - first) + 1);
+                }
+            };
+            const int begin = f[X] < l[X] ? f[X] : last, end = f[X] < l[X] ? l[X] : last;
+            for (int j = first; j < begin && ok; ++j) pass(j);
+            if (begin < end) wait(&bars.q_full[X], 0);
+            for (int j = begin - 1; j < end && begin < end && ok; ++j) both(j, j + 1 < end, j >= begin);
+            for (int j = end; j < last && ok; ++j) pass(j);
+        } else {
+            for (int X = 0; X < TILES; ++X)
+                if (f[X] < l[X]) wait(&bars.q_full[X], 0);
+            for (int j = first - 1; j < last && ok; ++j) {
+                bool k_here = false, v_here = false;
+                for (int X = 0; X < TILES; ++X) {
+                    if (j >= f[X] && j < l[X]) {
+                        if (!v_here) have_v(j);
+                        v_here = true;
+                        if (ok) weighted(X, j);
+                    }
+                    if (j + 1 >= f[X] && j + 1 < l[X]) {
+                        if (!k_here) landed(2 * (j + 1 - first));
+                        k_here = true;
+                        if (ok) scores(X, j + 1);
+                    }
+                }
+                // every block has a reader among A and B; its buffers are free behind the last one's
+                if (ok && j >= first) release(2 * (j - first) + 1);
+                if (ok && j + 1 < last) release(2 * (j + 1 - first));
+            }
         }
     }
     } else {
@@ -246,6 +287,7 @@ __global__ void __launch_bounds__(Lay<D, ROWS>::THREADS, ROWS == 256 ? 1 : 2)
         const float c = fmaxf(fabsf(x.scale) * 1.4426950408889634f, 1e-37f);
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;
         const uint32_t ts = tm + lanes + L::T_S + 128 * X, to = tm + lanes + L::T_O + D * X;
+        const uint32_t tp = tm + lanes + L::T_P + L::P_STEP * X;
         float m = -INFINITY, l = 0.f;  // reference (powers of two) and sum
         bool ok = true;
         for (int j = fX; j < lX; ++j) {
@@ -255,6 +297,11 @@ __global__ void __launch_bounds__(Lay<D, ROWS>::THREADS, ROWS == 256 ? 1 : 2)
 #pragma unroll
             for (int i = 0; i < kKeys / 32; ++i) tmem_ld32(ts + 32 * i, v + 32 * i);
             tmem_wait_ld();
+            if (L::OWN_P) {
+                fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars.s_loaded[X]);
+            }
             if (sign < 0.f) {
 #pragma unroll
                 for (int i = 0; i < kKeys; ++i) v[i] = -v[i];
@@ -273,12 +320,16 @@ __global__ void __launch_bounds__(Lay<D, ROWS>::THREADS, ROWS == 256 ? 1 : 2)
                     else top[e] = fmaxf(top[e], v[i + e]);
             }
             const float now = c * fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+            if (L::OWN_P && j > fX) {  // P and O of the block before are done with
+                if (!(ok = bar_wait_w(&bars.pv_done[X], (uint32_t)(j - 1 - fX) & 1, &abort_flag, x.status))) break;
+                fence_after_sync();
+            }
             const bool raise = now > m + kSlack;  // (from -inf on the first key seen)
             if (__any_sync(0xffffffffu, raise)) {
                 const float keep = raise ? ex2(m - now) : 1.f;  // 0 from -inf
                 if (raise) m = now;
                 l *= keep;
-                if (j > fX) {  // S_j was issued after P_{j-1} V_{j-1}: O is complete
+                if (j > fX) {  // (d = 128: S_j was issued after P_{j-1} V_{j-1}, so O is complete)
 #pragma unroll
                     for (int i = 0; i < D / 32; ++i) {
                         float o[32];
@@ -309,7 +360,7 @@ __global__ void __launch_bounds__(Lay<D, ROWS>::THREADS, ROWS == 256 ? 1 : 2)
                     sum[e & 1] = f2_fma(f2_pack(p0, p1), one, sum[e & 1]);
                     w[e] = pack_bf16(p0, p1);
                 }
-                tmem_st16(ts + 16 * i, w);
+                tmem_st16(tp + 16 * i, w);
             }
             {
                 float a, b, d, e;
@@ -322,7 +373,8 @@ __global__ void __launch_bounds__(Lay<D, ROWS>::THREADS, ROWS == 256 ? 1 : 2)
             __syncwarp();
             if (lane == 0) mbar_arrive(&bars.p_ready[X]);
         }
-        if (ok && fX < lX) ok = bar_wait_w(&bars.o_full[X], 0, &abort_flag, x.status);
+        if (ok && fX < lX)
+            ok = bar_wait_w(&bars.pv_done[X], L::OWN_P ? (uint32_t)(lX - 1 - fX) & 1 : 0u, &abort_flag, x.status);
         fence_after_sync();
         const size_t rows = (size_t)pk.T * pk.H;
         const size_t row = (size_t)(qlo + tok) * pk.H + hk * G + r % G;
@@ -368,7 +420,7 @@ __global__ void __launch_bounds__(Lay<D, ROWS>::THREADS, ROWS == 256 ? 1 : 2)
     drain_after_abort(abort_flag);
     if (warp == L::MMA) {
         fence_after_sync();
-        tmem_dealloc(tm, L::COLS);
+        tmem_dealloc(tmem_base_sh, L::COLS);
     }
 }
 
