@@ -216,16 +216,17 @@ int softattn_splits(const Packed& p)
 {
     // Ranges of keys per tile.  Rows that fill their tiles are cut only as far as it takes to
     // give every SM a block: each range costs 4 (d + 1) bytes a row, written and read.  A few rows
-    // (single tokens) cost next to nothing to join, and eight blocks an SM even out the sequences'
-    // different lengths.  A range is 256 keys of an average sequence or more; 32 ranges (the
-    // join's lanes) at most.
+    // (single tokens) cost next to nothing to join, and two blocks fit an SM; more of them pay their
+    // start and end without filling it better (16 sequences of 8000 and 16 of 1777 keys, H16 Hk4
+    // d128: 66 us for one block an SM, 61 for two, 64 for three, 68 for four, 73 for eight).  A range
+    // is 256 keys of an average sequence or more; 32 ranges (the join's lanes) at most.
     const int G = p.H / p.Hk;
     const bool tc = tc_softattn_supported(p);
     const int rows = tc ? tc_softattn_rows(p) : kRows;
     const int tokens = rows == 256 ? 2 * (128 / G) : rows / G;  // of a block
     const long long blocks = (long long)block_slots(p.T, p.n, tokens) * p.Hk;
     const bool few = (long long)p.T * G <= 32LL * p.n;
-    const long long want = ((few ? 8 : tc ? 1 : 2) * 152 + blocks - 1) / blocks;
+    const long long want = ((few ? 2 : tc ? 1 : 2) * 152 + blocks - 1) / blocks;
     const long long most = (long long)p.Tk / p.n / 256;
     const long long n = want < most ? want : most;
     return n < 1 ? 1 : n > 32 ? 32 : (int)n;

@@ -782,6 +782,35 @@ struct BackArgs {
     int* status;
 };
 
+// 32 lanes x 32 bits, 8 consecutive columns.
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, float (&v)[8])
+{
+    uint32_t r[8];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+                   "=r"(r[7])
+                 : "r"(taddr)
+                 : "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+// sum_lane x[i] for 16 values i: lanes 2 i and 2 i + 1 return the sum of value i.
+__device__ __forceinline__ float transpose_sum16(float (&x)[16])
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int m = 16, n = 8; n >= 1; m >>= 1, n >>= 1) {
+        const bool up = lane & m;
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const float give = up ? x[i] : x[i + n], keep = up ? x[i + n] : x[i];
+            x[i] = keep + __shfl_xor_sync(0xffffffffu, give, m);
+        }
+    }
+    return x[0] + __shfl_xor_sync(0xffffffffu, x[0], 1);
+}
+
 // sum_lane x[i] for 32 values i: lane i returns the sum of value i.  Every step halves the values.
 __device__ __forceinline__ float transpose_sum(float (&x)[32])
 {
@@ -1104,14 +1133,17 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
 //   Zq = scale tril(Y o dO U^T),  Zk = -tril(Y o dV U^T, -1)       (U = beta E)
 //   dQ = scale e^G (dO S^T) + Zq K
 //   dK = Zq^T Q + (Zk + Zk^T) K + e^{G_C - G} (U D^T) - e^G (dV S^T)
-//   dg_t = sum_{i >= t > j} (Zq o Q K^T + Zk o K K^T)_ij + sum_{i >= t} a_i + sum_{j < t} b_j + e^{G_C} <S, D>,
-//   a_i = scale e^G q_i.(S dO_i) - e^G k_i.(S dV_i),  b_j = e^{G_C - G_j} beta_j k_j.(D E_j)
-// (dg without differences of long sums, which would lose what bf16 operands leave.)  One CTA of
-// 8 warps per (chunk, key head) runs over the heads that share it; dQ^T and dK^T are products of
-// key dimension x token, summed over the heads in registers: a lane holds one key dimension
-// (quadrant w % 4) and a warp half of the tokens (w / 4).  256 columns of tensor memory, taken
-// twice: [C1 | C2 | S dO | S dV], then [Zq K | Z Q, Z K | D E].  For d = 64 products have rows
-// 64-127 that read whatever lies behind a tile (within shared memory) and are not looked at.
+//   dg_t = sum_{i >= t} a_i + sum_{j < t} b_j + e^{G_C} <S, D>,
+//   a_i = scale e^G q_i.(S dO_i) - e^G k_i.(S dV_i),
+//   b_j = e^{G_C - G_j} beta_j k_j.(D E_j) + k_j.(Zq^T Q + Zk^T K)_j - q_j.(Zq K)_j - k_j.(Zk K)_j
+// (a pair (i, j) of Zq o Q K^T + Zk o K K^T belongs to the dg_t with i >= t > j: in the sum over
+// b it comes in with its column j and leaves with its row i.  Rows and columns add up the same
+// bf16 values of Z in fp32, so what cancels does so exactly.)  One CTA of 8 warps per (chunk, key
+// head) runs over the heads that share it; dQ^T and dK^T are products of key dimension x token,
+// summed over the heads in registers: a lane holds one key dimension (quadrant w % 4) and a warp
+// half of the tokens (w / 4).  256 columns of tensor memory, taken twice: [dO E, dV E | - | S dO |
+// S dV], then [Zq K | Zq^T Q + Zk^T K | D E | Zk K].  For d = 64 products have rows 64-127 that read
+// whatever lies behind a tile (within shared memory) and are not looked at.
 template <int D>
 struct Grad {
     static constexpr uint32_t TILE = kC * D * 2, BLOCK = D * 128;  // 64 tokens; D rows of 64 elements
@@ -1149,7 +1181,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1)
     __shared__ uint32_t tmem_base_sh;
     __shared__ volatile int abort_flag;
     __shared__ __align__(16) float aux[256];  // -e^G, e^{G_C - G}, beta, G (in powers of two)
-    __shared__ float pairs[4][64], cross[4][32], sums_a[4][64], sums_b[4][64], ab[2][64], dots[8], last_sh;
+    __shared__ __align__(16) float sums_a[4][64], sums_b[4][64], ab[2][64], dots[8], last_sh;
 
     const Packed& pk = x.p;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, hk = blockIdx.y, G = pk.H / pk.Hk;
@@ -1217,17 +1249,12 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1)
             ok = false;
             break;
         }
-        const uint32_t qk = dlow(sb + L::QK, 16), ov = dlow(sb + L::OV, 16), de = dlow(sb + L::E, 8192);
+        const uint32_t ov = dlow(sb + L::OV, 16), de = dlow(sb + L::E, 8192);
         if (warp == 0) {
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
                 const uint32_t o = (k >> 2) * 16384 + (k & 3) * 32;
                 wmma_bf16(tm, desc(ov, o), desc(de, 2048 * k), idesc_bf16(128, kC, 0, 1), k > 0);
-            }
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-                const uint32_t o = (k >> 2) * 16384 + (k & 3) * 32;
-                wmma_bf16(tm + 64, desc(qk, o), desc(qk, o + 8192), idesc_bf16(128, kC, 0, 0), k > 0);
             }
 #pragma unroll
             for (int y = 0; y < 2; ++y)
@@ -1260,74 +1287,69 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1)
             const bool key = quad >= 2;
             const float Gi = aux[192 + i], f = key ? -1.f : x.scale;
             const int jmax = (i < n ? (key ? i : i + 1) : 0) - 32 * half;  // columns below it count
-            float pre[32], run = 0.f;
+            const uint32_t dst = sb + (key ? L::ZK : L::ZQ);
+            const bool none = half == 1 && !(quad & 1);  // all of this warp's lies above the diagonal
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-                float c1[16], c2[16];
-                tmem_ld16(lanes + 32 * half + 16 * y, c1);
-                tmem_ld16(lanes + 64 + 32 * half + 16 * y, c2);
-                tmem_wait_ld();
-                uint32_t w[8];
+                uint32_t w[8] = {};
+                if (!none) {
+                    float c1[16];
+                    tmem_ld16(lanes + 32 * half + 16 * y, c1);
+                    tmem_wait_ld();
 #pragma unroll
-                for (int j = 0; j < 16; j += 2) {
-                    float z[2];
+                    for (int j = 0; j < 16; j += 4) {
+                        const float4 bt = *(const float4*)&aux[128 + 32 * half + 16 * y + j];
+                        const float4 gj = *(const float4*)&aux[192 + 32 * half + 16 * y + j];
+                        const float b4[4] = {bt.x, bt.y, bt.z, bt.w}, g4[4] = {gj.x, gj.y, gj.z, gj.w};
+                        float z[4];
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int jj = 16 * y + j + e, col = 32 * half + jj;
-                        z[e] = jj < jmax ? f * aux[128 + col] * ex2(Gi - aux[192 + col]) * c1[j + e] : 0.f;
-                        pre[jj] = run;  // the sum over the columns before this one
-                        run += jj < jmax ? z[e] * c2[j + e] : 0.f;
+                        for (int e = 0; e < 4; ++e)
+                            z[e] = 16 * y + j + e < jmax ? f * b4[e] * ex2(Gi - g4[e]) * c1[j + e] : 0.f;
+                        w[j / 2] = pack_bf16(z[0], z[1]);
+                        w[j / 2 + 1] = pack_bf16(z[2], z[3]);
                     }
-                    w[j / 2] = pack_bf16(z[0], z[1]);
                 }
-                const uint32_t dst = sb + (key ? L::ZK : L::ZQ);
                 st_shared_v4(dst + swz128(i, 32 * half + 16 * y), w[0], w[1], w[2], w[3]);
                 st_shared_v4(dst + swz128(i, 32 * half + 16 * y + 8), w[4], w[5], w[6], w[7]);
-            }
-            // sum over rows i >= t of the columns j < t: within this half of the columns ...
-            const int base = (quad & 1) * 32 - 32 * half;  // row - column offset of this warp's lane 0
-#pragma unroll
-            for (int t = 0; t < 32; ++t) pre[t] = base + lane >= t ? pre[t] : 0.f;
-            pairs[quad][32 * half + lane] = transpose_sum(pre);
-            // ... and, for t in the second half, all of the first half's columns
-            if (half == 0) {
-                float suffix = run;
-#pragma unroll
-                for (int m = 1; m < 32; m *= 2) {
-                    const float o = __shfl_down_sync(0xffffffffu, suffix, m);
-                    if (lane + m < 32) suffix += o;
-                }
-                cross[quad][lane] = quad & 1 ? suffix : 0.f;
             }
         }
         const uint8_t* qcol = sm + L::QK + (kd >> 6) * 16384 + half * 4096;
         if (ok && mine) {
-            float dot[32];
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-                float a[16], b[16];
-                tmem_ld16(lanes + 128 + 32 * half + 16 * y, a);
-                tmem_ld16(lanes + 192 + 32 * half + 16 * y, b);
-                tmem_wait_ld();
+                float dot[16];
 #pragma unroll
-                for (int j = 0; j < 16; j += 2) {
-                    float u[2], w[2];
+                for (int z = 0; z < 2; ++z) {
+                    const int c0 = 32 * half + 16 * y + 8 * z;
+                    float a[8], b[8];
+                    tmem_ld8(lanes + 128 + c0, a);
+                    tmem_ld8(lanes + 192 + c0, b);
+                    tmem_wait_ld();
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int jj = 16 * y + j + e;
-                        const bool in = 32 * half + jj < n;
-                        const float gm = aux[32 * half + jj];  // -e^G
-                        u[e] = in ? -x.scale * gm * a[j + e] : 0.f;
-                        w[e] = in ? gm * b[j + e] : 0.f;
-                        const uint32_t qv = *(const uint16_t*)(qcol + swz128(jj, kd & 63));
-                        const uint32_t kv = *(const uint16_t*)(qcol + 8192 + swz128(jj, kd & 63));
-                        dot[jj] = u[e] * __uint_as_float(qv << 16) + w[e] * __uint_as_float(kv << 16);
+                    for (int j = 0; j < 8; j += 4) {
+                        const float4 g4 = *(const float4*)&aux[c0 + j];
+                        const float gm[4] = {g4.x, g4.y, g4.z, g4.w};  // -e^G
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int jj = 16 * y + 8 * z + j + e;
+                            const bool in = 32 * half + jj < n;
+                            a[j + e] = in ? -x.scale * gm[e] * a[j + e] : 0.f;
+                            b[j + e] = in ? gm[e] * b[j + e] : 0.f;
+                            const uint32_t qv = *(const uint16_t*)(qcol + swz128(jj, kd & 63));
+                            const uint32_t kv = *(const uint16_t*)(qcol + 8192 + swz128(jj, kd & 63));
+                            dot[8 * z + j + e] = a[j + e] * __uint_as_float(qv << 16) + b[j + e] * __uint_as_float(kv << 16);
+                        }
                     }
-                    dq[8 * y + j / 2] = f2_fma(f2_pack(u[0], u[1]), f2_pack(1.f, 1.f), dq[8 * y + j / 2]);
-                    dk[8 * y + j / 2] = f2_fma(f2_pack(w[0], w[1]), f2_pack(1.f, 1.f), dk[8 * y + j / 2]);
+#pragma unroll
+                    for (int j = 0; j < 8; j += 2) {
+                        const int at = 8 * y + 4 * z + j / 2;
+                        dq[at] = f2_fma(f2_pack(a[j], a[j + 1]), f2_pack(1.f, 1.f), dq[at]);
+                        dk[at] = f2_fma(f2_pack(b[j], b[j + 1]), f2_pack(1.f, 1.f), dk[at]);
+                    }
                 }
+                const float sum = transpose_sum16(dot);
+                if (!(lane & 1)) sums_a[quad][32 * half + 16 * y + lane / 2] = sum;
             }
-            sums_a[quad][32 * half + lane] = transpose_sum(dot);
         }
         fence_proxy_async();  // Z
         fence_before_sync();
@@ -1348,7 +1370,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1)
 #pragma unroll
             for (int k = 0; k < 4; ++k) wmma_bf16(tm + 64, desc(kn, 2048 * k), desc(zkn, 2048 * k), I_MM, 1);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) wmma_bf16(tm + 64, desc(kn, 2048 * k), desc(zk, 32 * k), I_KM, 1);
+            for (int k = 0; k < 4; ++k) wmma_bf16(tm + 192, desc(kn, 2048 * k), desc(zk, 32 * k), I_KM, k > 0);
 #pragma unroll
             for (int k = 0; k < D / 16; ++k)
                 wmma_bf16(tm + 128, desc(dlow(sb + L::DS, L::BLOCK), 2048 * k), desc(de, 2048 * k), I_MM, k > 0);
@@ -1356,30 +1378,43 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1)
         }
         ok = products_done();
         if (ok && mine) {
-            float dot[32];
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-                float a[16], b[16], e2[16];
-                tmem_ld16(lanes + 32 * half + 16 * y, a);
-                tmem_ld16(lanes + 64 + 32 * half + 16 * y, b);
-                tmem_ld16(lanes + 128 + 32 * half + 16 * y, e2);
-                tmem_wait_ld();
+                float dot[16];
 #pragma unroll
-                for (int j = 0; j < 16; j += 2) {
-                    float w[2];
+                for (int z = 0; z < 2; ++z) {
+                    const int c0 = 32 * half + 16 * y + 8 * z;
+                    float a[8], b[8], d[8], e2[8];
+                    tmem_ld8(lanes + c0, a);         // Zq K
+                    tmem_ld8(lanes + 64 + c0, b);    // Zq^T Q + Zk^T K
+                    tmem_ld8(lanes + 128 + c0, e2);  // D E
+                    tmem_ld8(lanes + 192 + c0, d);   // Zk K
+                    tmem_wait_ld();
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int jj = 16 * y + j + e, col = 32 * half + jj;
-                        const uint32_t kv = *(const uint16_t*)(qcol + 8192 + swz128(jj, kd & 63));
-                        w[e] = aux[64 + col] * aux[128 + col] * e2[j + e];
-                        dot[jj] = w[e] * __uint_as_float(kv << 16);
-                        w[e] += b[j + e];
+                    for (int j = 0; j < 8; j += 4) {
+                        const float4 k4 = *(const float4*)&aux[64 + c0 + j], b4 = *(const float4*)&aux[128 + c0 + j];
+                        const float kb[4] = {k4.x * b4.x, k4.y * b4.y, k4.z * b4.z, k4.w * b4.w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int jj = 16 * y + 8 * z + j + e;
+                            const uint32_t qv = *(const uint16_t*)(qcol + swz128(jj, kd & 63));
+                            const uint32_t kv = *(const uint16_t*)(qcol + 8192 + swz128(jj, kd & 63));
+                            const float write = fmaf(kb[e], e2[j + e], b[j + e]);
+                            dot[8 * z + j + e] = fmaf(write - d[j + e], __uint_as_float(kv << 16),
+                                                      -a[j + e] * __uint_as_float(qv << 16));
+                            b[j + e] = write + d[j + e];
+                        }
                     }
-                    dq[8 * y + j / 2] = f2_fma(f2_pack(a[j], a[j + 1]), f2_pack(1.f, 1.f), dq[8 * y + j / 2]);
-                    dk[8 * y + j / 2] = f2_fma(f2_pack(w[0], w[1]), f2_pack(1.f, 1.f), dk[8 * y + j / 2]);
+#pragma unroll
+                    for (int j = 0; j < 8; j += 2) {
+                        const int at = 8 * y + 4 * z + j / 2;
+                        dq[at] = f2_fma(f2_pack(a[j], a[j + 1]), f2_pack(1.f, 1.f), dq[at]);
+                        dk[at] = f2_fma(f2_pack(b[j], b[j + 1]), f2_pack(1.f, 1.f), dk[at]);
+                    }
                 }
+                const float sum = transpose_sum16(dot);
+                if (!(lane & 1)) sums_b[quad][32 * half + 16 * y + lane / 2] = sum;
             }
-            sums_b[quad][32 * half + lane] = transpose_sum(dot);
         }
         fence_before_sync();
         if (!__syncthreads_and(ok)) {  // (also: tensor memory and the tiles are free for the next head)
@@ -1402,10 +1437,14 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1)
 #pragma unroll
             for (int y = 0; y < 8; ++y) g += dots[y];
             g *= last_sh;
+            float behind = 0.f, ahead = 0.f;
 #pragma unroll
-            for (int y = 0; y < 4; ++y) g += pairs[y][tid];
-            if (tid >= 32) g += cross[1][tid - 32] + cross[3][tid - 32];
-            for (int j = 0; j < 64; ++j) g += j >= tid ? ab[0][j] : ab[1][j];
+            for (int j = 0; j < 64; j += 4) {
+                const float4 a4 = *(const float4*)&ab[0][j], b4 = *(const float4*)&ab[1][j];
+                behind += (j >= tid ? a4.x : b4.x) + (j + 1 >= tid ? a4.y : b4.y);
+                ahead += (j + 2 >= tid ? a4.z : b4.z) + (j + 3 >= tid ? a4.w : b4.w);
+            }
+            g += behind + ahead;
             const float* part = x.db + slot * 256 + tid;
 #pragma unroll
             for (int y = 0; y < D / 32; ++y) db += part[64 * y];
