@@ -16,10 +16,10 @@
 // shared memory (read along their rows or across them), and no operand is ever transposed.
 // For d = 64 the lower 64 of the 128 lanes carry the state; the others compute on whatever they hold.
 //
-// Precision: K and Q are exact.  What multiplies them on the way of the state (S, beta R, U, and
-// M) is split into bf16 high and low parts (2^-17), so that the state, held in fp32 registers, is
-// accurate to fp32's order.  The output's own products take S, U and P as bf16: it is rounded to
-// bf16 anyway.
+// Precision: K and Q are exact.  What multiplies them (S, beta R, U, M and P) is split into bf16 high
+// and low parts (2^-17; products of two low parts are left out), so that the state, held in fp32
+// registers, is off by 3e-6 and the output by little more than its own rounding (with P as bf16 by
+// 1.6 times it).  The backward's results are bf16, and of its operands only P is split.
 #include <cuda.h>
 
 #include "flex_internal.h"
@@ -37,11 +37,11 @@ constexpr float kLog2e = 1.4426950408889634f;
 // the differences of the sums G have to be finite.
 constexpr float kLeastGate = -88.f;
 
-// What the walk needs of a chunk, as it is copied to shared memory: M's low and high parts and P
-// (64 x 64 bf16, 128-byte rows, swizzled), then -e^G, e^{G_C - G}, beta (0 behind the
+// What the walk needs of a chunk, as it is copied to shared memory: M's low and high parts and
+// P's high and low ones // (64 x 64 bf16, 128-byte rows, swizzled), then -e^G, e^{G_C - G}, beta (0 behind the
 // sequence's end), G in powers of two (64 floats each) and e^{G_C}.
 struct Rec {
-    static constexpr uint32_t M_LO = 0, M_HI = 8192, P = 16384, AUX = 24576, BYTES = 25856;
+    static constexpr uint32_t M_LO = 0, M_HI = 8192, P = 16384, P_LO = 24576, AUX = 32768, BYTES = 34048;
     static constexpr uint32_t GAMMA = AUX, KAPPA = AUX + 256, BETA = AUX + 512, G = AUX + 768, LAST = AUX + 1024;
 };
 
@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(128)
         } else {
 #pragma unroll
             for (int j = 0; j < 64; j += 8) {
-                uint4 out = make_uint4(0, 0, 0, 0);
+                uint4 out = make_uint4(0, 0, 0, 0), out_lo = out;
                 if (j < cols) {
                     const float4 g0 = *(const float4*)&Gs[j], g1 = *(const float4*)&Gs[j + 4];
                     const float y[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
@@ -252,10 +252,13 @@ __global__ void __launch_bounds__(128)
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
                         p[e] = j + e <= row && in ? scale * v[j + e] * ex2(G - y[e]) : 0.f;
-                    out = make_uint4(pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]),
-                                     pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7]));
+                    split(p[0], p[1], out.x, out_lo.x);
+                    split(p[2], p[3], out.y, out_lo.y);
+                    split(p[4], p[5], out.z, out_lo.z);
+                    split(p[6], p[7], out.w, out_lo.w);
                 }
                 *(uint4*)(rec + Rec::P + swz128(row, j)) = out;
+                *(uint4*)(rec + Rec::P_LO + swz128(row, j)) = out_lo;
             }
             const float last = Gs[63];
             float* aux = (float*)rec;
@@ -337,7 +340,7 @@ struct Walk {
     static constexpr uint32_t TILE = kC * D * 2;    // 64 rows of K, Q or V
     static constexpr uint32_t K = 0, Q = TILE, V = 2 * TILE, REC = 3 * TILE;
     static constexpr uint32_t STAGE = (REC + Rec::BYTES + 1023) / 1024 * 1024;
-    static constexpr int ST = D == 128 ? 3 : 4;
+    static constexpr int ST = D == 128 ? 2 : 3;
     static constexpr uint32_t SMEM = ST * STAGE + 1024;
     // tensor memory columns: S high, low; the chunk's product (K S, then M (beta R), then P U);
     // beta R, then kappa U, high and low; U high and low; the state's increment; Q S
@@ -476,7 +479,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                 const uint32_t dkn = dlow(st + W::K, 8192);
                 const uint32_t dmh = dlow(st + W::REC + Rec::M_HI, 16);
                 const uint32_t dml = dlow(st + W::REC + Rec::M_LO, 16);
-                const uint32_t dp = dlow(st + W::REC + Rec::P, 16);
+                const uint32_t dp = dlow(st + W::REC + Rec::P, 16), dpl = dlow(st + W::REC + Rec::P_LO, 16);
                 if (c > 0) wait(&x_free, c - 1);  // P U of the last chunk has been read from X
 #pragma unroll
                 for (int p = 0; p < W::PIECES; ++p) {
@@ -512,6 +515,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                 if (!ok) break;
                 mma4(W::T_X, W::T_UH, dp, 32, I_C, 0);
                 mma4(W::T_X, W::T_UL, dp, 32, I_C, 1);
+                mma4(W::T_X, W::T_UH, dpl, 32, I_C, 1);
                 wmma_commit(&o_full);
                 wmma_commit(&empty[c % W::ST]);
             }
@@ -758,7 +762,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
 template <int D>
 struct Back {
     static constexpr uint32_t TILE = kC * D * 2;
-    static constexpr uint32_t REC_BYTES = Rec::BYTES - Rec::M_HI;  // M's high part, P, factors
+    static constexpr uint32_t REC_BYTES = Rec::BYTES - Rec::M_HI;  // M's high part, P, the factors
     static constexpr uint32_t K = 0, Q = TILE, DO = 2 * TILE, REC = 3 * TILE;
     static constexpr uint32_t STAGE = (REC + REC_BYTES + 1023) / 1024 * 1024;
     static constexpr int ST = D == 128 ? 3 : 4;
@@ -929,8 +933,8 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                 const uint32_t dqn = dlow(st + B::Q, 8192), dod = dlow(st + B::DO, 8192);
                 const uint32_t dm = dlow(st + B::M, 16), dp = dlow(st + B::P, 16);
 #pragma unroll
-                for (int k = 0; k < 4; ++k)  // P^T dO, A across the rows of dO
-                    wmma_bf16(B::T_P, desc(dod, 2048 * k), desc(dp, 2048 * k), I_P, k > 0);
+                for (int k = 0; k < 8; ++k)  // P^T dO, A across the rows of dO; P_LO follows P
+                    wmma_bf16(B::T_P, desc(dod, 2048 * (k & 3)), desc(dp, 2048 * k), I_P, k > 0);
 #pragma unroll
                 for (int p = 0; p < W::PIECES; ++p) {
                     wait(&s_ready[p], r);
