@@ -1137,17 +1137,16 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
 //   Zq = scale tril(Y o dO U^T),  Zk = -tril(Y o dV U^T, -1)       (U = beta E)
 //   dQ = scale e^G (dO S^T) + Zq K
 //   dK = Zq^T Q + (Zk + Zk^T) K + e^{G_C - G} (U D^T) - e^G (dV S^T)
-//   dg_t = sum_{i >= t} a_i + sum_{j < t} b_j + e^{G_C} <S, D>,
-//   a_i = scale e^G q_i.(S dO_i) - e^G k_i.(S dV_i),
-//   b_j = e^{G_C - G_j} beta_j k_j.(D E_j) + k_j.(Zq^T Q + Zk^T K)_j - q_j.(Zq K)_j - k_j.(Zk K)_j
-// (a pair (i, j) of Zq o Q K^T + Zk o K K^T belongs to the dg_t with i >= t > j: in the sum over
-// b it comes in with its column j and leaves with its row i.  Rows and columns add up the same
-// bf16 values of Z in fp32, so what cancels does so exactly.)  One CTA of 8 warps per (chunk, key
-// head) runs over the heads that share it; dQ^T and dK^T are products of key dimension x token,
-// summed over the heads in registers: a lane holds one key dimension (quadrant w % 4) and a warp
-// half of the tokens (w / 4).  256 columns of tensor memory, taken twice: [dO E, dV E | - | S dO |
-// S dV], then [Zq K | Zq^T Q + Zk^T K | D E | Zk K].  For d = 64 products have rows 64-127 that read
-// whatever lies behind a tile (within shared memory) and are not looked at.
+//   dg_t = sum_{i >= t > j} W_ij + sum_{i >= t} a_i + sum_{j < t} b_j + e^{G_C} <S, D>,
+//   W = Zq o Q K^T + Zk o K K^T,  a_i = scale e^G q_i.(S dO_i) - e^G k_i.(S dV_i),
+//   b_j = e^{G_C - G_j} beta_j k_j.(D E_j)
+// (W as sum_{j < t} of its column j minus its row j: the sums are of the same fp32 values, so what
+// cancels does so exactly.)  One CTA of 8 warps per (chunk, key head) runs over the heads that share
+// it; dQ^T and dK^T are products of key dimension x token, summed over the heads in registers: a
+// lane holds one key dimension (quadrant w % 4) and a warp half of the tokens (w / 4).  256 columns
+// of tensor memory, taken twice: [dO E, dV E | Q K^T, K K^T | S dO | S dV], then [Zq K | Zq^T Q +
+// (Zk + Zk^T) K | D E].  For d = 64 products have rows 64-127 that read whatever lies behind a tile
+// (within shared memory) and are not looked at.
 template <int D>
 struct Grad {
     static constexpr uint32_t TILE = kC * D * 2, BLOCK = D * 128;  // 64 tokens; D rows of 64 elements
@@ -1185,7 +1184,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1)
     __shared__ uint32_t tmem_base_sh;
     __shared__ volatile int abort_flag;
     __shared__ __align__(16) float aux[256];  // -e^G, e^{G_C - G}, beta, G (in powers of two)
-    __shared__ __align__(16) float sums_a[4][64], sums_b[4][64], ab[2][64], dots[8], last_sh;
+    __shared__ __align__(16) float sums_a[4][64], sums_b[4][64], cols[4][64], rows[2][128], ab[2][64], dots[8], last_sh;
 
     const Packed& pk = x.p;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, hk = blockIdx.y, G = pk.H / pk.Hk;
@@ -1253,12 +1252,17 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1)
             ok = false;
             break;
         }
-        const uint32_t ov = dlow(sb + L::OV, 16), de = dlow(sb + L::E, 8192);
+        const uint32_t qk = dlow(sb + L::QK, 16), ov = dlow(sb + L::OV, 16), de = dlow(sb + L::E, 8192);
         if (warp == 0) {
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
                 const uint32_t o = (k >> 2) * 16384 + (k & 3) * 32;
                 wmma_bf16(tm, desc(ov, o), desc(de, 2048 * k), idesc_bf16(128, kC, 0, 1), k > 0);
+            }
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+                const uint32_t o = (k >> 2) * 16384 + (k & 3) * 32;
+                wmma_bf16(tm + 64, desc(qk, o), desc(qk, o + 8192), idesc_bf16(128, kC, 0, 0), k > 0);
             }
 #pragma unroll
             for (int y = 0; y < 2; ++y)
@@ -1293,12 +1297,15 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1)
             const int jmax = (i < n ? (key ? i : i + 1) : 0) - 32 * half;  // columns below it count
             const uint32_t dst = sb + (key ? L::ZK : L::ZQ);
             const bool none = half == 1 && !(quad & 1);  // all of this warp's lies above the diagonal
+            float row = 0.f;
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
                 uint32_t w[8] = {};
+                float col = 0.f;
                 if (!none) {
-                    float c1[16];
+                    float c1[16], W[16];
                     tmem_ld16(lanes + 32 * half + 16 * y, c1);
+                    tmem_ld16(lanes + 64 + 32 * half + 16 * y, W);
                     tmem_wait_ld();
 #pragma unroll
                     for (int j = 0; j < 16; j += 4) {
@@ -1307,15 +1314,22 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1)
                         const float b4[4] = {bt.x, bt.y, bt.z, bt.w}, g4[4] = {gj.x, gj.y, gj.z, gj.w};
                         float z[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            z[e] = 16 * y + j + e < jmax ? f * b4[e] * ex2(Gi - g4[e]) * c1[j + e] : 0.f;
+                        for (int e = 0; e < 4; ++e) {
+                            const bool in = 16 * y + j + e < jmax;
+                            z[e] = in ? f * b4[e] * ex2(Gi - g4[e]) * c1[j + e] : 0.f;
+                            W[j + e] = in ? z[e] * W[j + e] : 0.f;
+                            row += W[j + e];
+                        }
                         w[j / 2] = pack_bf16(z[0], z[1]);
                         w[j / 2 + 1] = pack_bf16(z[2], z[3]);
                     }
+                    col = transpose_sum16(W);
                 }
                 st_shared_v4(dst + swz128(i, 32 * half + 16 * y), w[0], w[1], w[2], w[3]);
                 st_shared_v4(dst + swz128(i, 32 * half + 16 * y + 8), w[4], w[5], w[6], w[7]);
+                if (!(lane & 1)) cols[quad][32 * half + 16 * y + lane / 2] = col;
             }
+            rows[half][kd] = row;
         }
         const uint8_t* qcol = sm + L::QK + (kd >> 6) * 16384 + half * 4096;
         if (ok && mine) {
@@ -1374,7 +1388,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1)
 #pragma unroll
             for (int k = 0; k < 4; ++k) wmma_bf16(tm + 64, desc(kn, 2048 * k), desc(zkn, 2048 * k), I_MM, 1);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) wmma_bf16(tm + 192, desc(kn, 2048 * k), desc(zk, 32 * k), I_KM, k > 0);
+            for (int k = 0; k < 4; ++k) wmma_bf16(tm + 64, desc(kn, 2048 * k), desc(zk, 32 * k), I_KM, 1);
 #pragma unroll
             for (int k = 0; k < D / 16; ++k)
                 wmma_bf16(tm + 128, desc(dlow(sb + L::DS, L::BLOCK), 2048 * k), desc(de, 2048 * k), I_MM, k > 0);
@@ -1388,11 +1402,10 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1)
 #pragma unroll
                 for (int z = 0; z < 2; ++z) {
                     const int c0 = 32 * half + 16 * y + 8 * z;
-                    float a[8], b[8], d[8], e2[8];
+                    float a[8], b[8], e2[8];
                     tmem_ld8(lanes + c0, a);         // Zq K
-                    tmem_ld8(lanes + 64 + c0, b);    // Zq^T Q + Zk^T K
+                    tmem_ld8(lanes + 64 + c0, b);    // Zq^T Q + (Zk + Zk^T) K
                     tmem_ld8(lanes + 128 + c0, e2);  // D E
-                    tmem_ld8(lanes + 192 + c0, d);   // Zk K
                     tmem_wait_ld();
 #pragma unroll
                     for (int j = 0; j < 8; j += 4) {
@@ -1401,12 +1414,10 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const int jj = 16 * y + 8 * z + j + e;
-                            const uint32_t qv = *(const uint16_t*)(qcol + swz128(jj, kd & 63));
                             const uint32_t kv = *(const uint16_t*)(qcol + 8192 + swz128(jj, kd & 63));
-                            const float write = fmaf(kb[e], e2[j + e], b[j + e]);
-                            dot[8 * z + j + e] = fmaf(write - d[j + e], __uint_as_float(kv << 16),
-                                                      -a[j + e] * __uint_as_float(qv << 16));
-                            b[j + e] = write + d[j + e];
+                            const float write = kb[e] * e2[j + e];
+                            dot[8 * z + j + e] = write * __uint_as_float(kv << 16);
+                            b[j + e] += write;
                         }
                     }
 #pragma unroll
@@ -1432,6 +1443,9 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1)
                 A += sums_a[y][tid];
                 B += sums_b[y][tid];
             }
+#pragma unroll
+            for (int y = 0; y < 4; ++y) B += cols[y][tid];
+            B -= (rows[0][tid] + rows[1][tid]) + (rows[0][64 + tid] + rows[1][64 + tid]);
             ab[0][tid] = A;
             ab[1][tid] = B;
         }
