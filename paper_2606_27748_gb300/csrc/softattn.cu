@@ -225,8 +225,7 @@ int softattn_splits(const Packed& p)
     const int rows = tc ? tc_softattn_rows(p) : kRows;
     const int tokens = rows == 256 ? 2 * (128 / G) : rows / G;  // of a block
     const long long blocks = (long long)block_slots(p.T, p.n, tokens) * p.Hk;
-    const bool few = (long long)p.T * G <= 32LL * p.n;
-    const long long want = ((few ? 2 : tc ? 1 : 2) * 152 + blocks - 1) / blocks;
+    const long long want = ((softattn_few(p) || !tc ? 2 : 1) * 152 + blocks - 1) / blocks;
     const long long most = (long long)p.Tk / p.n / 256;
     const long long n = want < most ? want : most;
     return n < 1 ? 1 : n > 32 ? 32 : (int)n;

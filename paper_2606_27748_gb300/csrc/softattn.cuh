@@ -18,6 +18,9 @@ struct AttnArgs {
     int* status;
 };
 
+// One or two tokens a sequence on average: the step of a serving batch.
+inline bool softattn_few(const Packed& p) { return p.T <= 2LL * p.n; }
+
 // Blocks [first, last) of `size` keys that range `split` of a tile takes: those up to the key
 // `newest` that its last row sees (causal), cut evenly.
 __device__ __forceinline__ void key_range(const AttnArgs& x, int size, int lk, int newest, int split,

@@ -67,6 +67,14 @@ __device__ __forceinline__ void split(float a, float b, uint32_t& hi, uint32_t& 
     split2(f2_pack(a, b), hi, lo);
 }
 
+// 32 lanes x 32 columns: both loads in flight together.
+__device__ __forceinline__ void load32(uint32_t taddr, float (&a)[2][16])
+{
+    tmem_ld16(taddr, a[0]);
+    tmem_ld16(taddr + 16, a[1]);
+    tmem_wait_ld();
+}
+
 // Eight packed pairs rounded to bf16.
 __device__ __forceinline__ void pack8(const uint64_t* x, uint32_t (&w)[8])
 {
@@ -554,15 +562,16 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
 #pragma unroll
                 for (int p = 0; p < W::PIECES; ++p) {
                     if (c > 0 && !wait(&s_full[p], c - 1)) break;
+                    // (all of a step's loads ahead of their first use: a round trip to tensor memory
+                    // takes 250 cycles)
+                    float a[2][16];
+                    if (c > 0) load32(lanes + W::T_D + 64 * p + 32 * half, a);
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         if (c > 0) {  // S = decay S + the increment of the last chunk
-                            float a[16];
-                            tmem_ld16(lanes + W::T_D + 64 * p + 32 * half + 16 * j, a);
-                            tmem_wait_ld();
 #pragma unroll
                             for (int e = 0; e < 8; ++e)
-                                S[p][8 * j + e] = f2_fma(decay, S[p][8 * j + e], f2_pack(a[2 * e], a[2 * e + 1]));
+                                S[p][8 * j + e] = f2_fma(decay, S[p][8 * j + e], f2_pack(a[j][2 * e], a[j][2 * e + 1]));
                         }
                         if (c < chunks) {
                             uint32_t wh[8], wl[8];
@@ -632,11 +641,10 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                     }
                 }
                 if (!wait(&x_full, c)) break;
+                float d[2][16];
+                load32(lanes + W::T_X + 32 * half, d);
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    float d[16];
-                    tmem_ld16(lanes + W::T_X + 32 * half + 16 * j, d);
-                    tmem_wait_ld();
                     uint32_t wh[8], wl[8];
 #pragma unroll
                     for (int i = 0; i < 8; i += 2) {  // (X is 0 behind the end: K is)
@@ -644,8 +652,8 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                         const ulonglong2 bt = *(const ulonglong2*)(aux + Rec::BETA / 4 + 16 * j + 2 * i);
                         uint64_t* r = R + 8 * j + i;
                         // (e^G holds its negative in the record: R = V - e^G X)
-                        r[0] = f2_fma(gm.x, f2_pack(d[2 * i], d[2 * i + 1]), r[0]);
-                        r[1] = f2_fma(gm.y, f2_pack(d[2 * i + 2], d[2 * i + 3]), r[1]);
+                        r[0] = f2_fma(gm.x, f2_pack(d[j][2 * i], d[j][2 * i + 1]), r[0]);
+                        r[1] = f2_fma(gm.y, f2_pack(d[j][2 * i + 2], d[j][2 * i + 3]), r[1]);
                         split2(f2_mul(bt.x, r[0]), wh[i], wl[i]);
                         split2(f2_mul(bt.y, r[1]), wh[i + 1], wl[i + 1]);
                     }
@@ -655,19 +663,17 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                 ready(&r_ready);
                 if (!wait(&e_full, c)) break;
                 const uint64_t minus = f2_pack(-1.f, -1.f);
+                load32(lanes + W::T_X + 32 * half, d);
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    float d[16];
-                    tmem_ld16(lanes + W::T_X + 32 * half + 16 * j, d);
-                    tmem_wait_ld();
                     uint32_t wh[8], wl[8];
 #pragma unroll
                     for (int i = 0; i < 8; i += 2) {
                         const ulonglong2 bt = *(const ulonglong2*)(aux + Rec::BETA / 4 + 16 * j + 2 * i);
                         const ulonglong2 kp = *(const ulonglong2*)(aux + Rec::KAPPA / 4 + 16 * j + 2 * i);
                         uint64_t* r = R + 8 * j + i;
-                        r[0] = f2_fma(f2_pack(d[2 * i], d[2 * i + 1]), minus, r[0]);
-                        r[1] = f2_fma(f2_pack(d[2 * i + 2], d[2 * i + 3]), minus, r[1]);
+                        r[0] = f2_fma(f2_pack(d[j][2 * i], d[j][2 * i + 1]), minus, r[0]);
+                        r[1] = f2_fma(f2_pack(d[j][2 * i + 2], d[j][2 * i + 3]), minus, r[1]);
                         split2(f2_mul(f2_mul(kp.x, bt.x), r[0]), wh[i], wl[i]);
                         split2(f2_mul(f2_mul(kp.y, bt.y), r[1]), wh[i + 1], wl[i + 1]);
                     }
@@ -703,14 +709,9 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                     }
                 }
                 if (!wait(&o_full, c)) break;
+                load32(lanes + W::T_X + 32 * half, d);
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    float d[16];
-                    tmem_ld16(lanes + W::T_X + 32 * half + 16 * j, d);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) R[8 * j + e] = f2_pack(d[2 * e], d[2 * e + 1]);
-                }
+                for (int e = 0; e < 16; ++e) R[e] = f2_pack(d[e / 8][2 * (e % 8)], d[e / 8][2 * (e % 8) + 1]);
                 fence_before_sync();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&x_free);
@@ -718,16 +719,14 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                 __nv_bfloat16* dst = out + (size_t)(c * kC) * os;
                 const uint32_t pick = lane & 1 ? 0x3276u : 0x5410u;
                 const uint64_t factor = f2_pack(-x.scale, -x.scale);
+                load32(lanes + W::T_Q + 32 * half, d);
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    float d[16];
-                    tmem_ld16(lanes + W::T_Q + 32 * half + 16 * j, d);
-                    tmem_wait_ld();
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const uint64_t gm = *(const uint64_t*)(aux + Rec::GAMMA / 4 + 16 * j + 2 * e);
                         float o0, o1;
-                        f2_unpack(f2_fma(f2_mul(factor, gm), f2_pack(d[2 * e], d[2 * e + 1]), R[8 * j + e]), o0, o1);
+                        f2_unpack(f2_fma(f2_mul(factor, gm), f2_pack(d[j][2 * e], d[j][2 * e + 1]), R[8 * j + e]), o0, o1);
                         const uint32_t w = pack_bf16(o0, o1);
                         const uint32_t y = __byte_perm(w, __shfl_xor_sync(0xffffffffu, w, 1), pick);
                         if (16 * j + 2 * e + (lane & 1) < n) *(uint32_t*)dst = y;
@@ -990,15 +989,14 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
 #pragma unroll
                 for (int p = 0; p < W::PIECES; ++p) {
                     if (r > 0 && !wait(&s_full[p], r - 1)) break;
+                    float a[2][16];
+                    if (r > 0) load32(lanes + B::T_D + 64 * p + 32 * half, a);
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         if (r > 0) {  // S = decay S + the increment of the chunk behind
-                            float a[16];
-                            tmem_ld16(lanes + B::T_D + 64 * p + 32 * half + 16 * j, a);
-                            tmem_wait_ld();
 #pragma unroll
                             for (int e = 0; e < 8; ++e)
-                                S[p][8 * j + e] = f2_fma(decay, S[p][8 * j + e], f2_pack(a[2 * e], a[2 * e + 1]));
+                                S[p][8 * j + e] = f2_fma(decay, S[p][8 * j + e], f2_pack(a[j][2 * e], a[j][2 * e + 1]));
                         }
                         uint32_t w[8];
                         pack8(S[p] + 8 * j, w);
@@ -1060,18 +1058,18 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                 }
                 if (!wait(&x_full, r)) break;
                 uint64_t U[16];  // dU, then Y: pairs of tokens
+                float d[2][16], y[2][16];
+                tmem_ld16(lanes + B::T_P + 32 * half, y[0]);
+                tmem_ld16(lanes + B::T_P + 32 * half + 16, y[1]);
+                load32(lanes + B::T_X + 32 * half, d);
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    float d[16], y[16];
-                    tmem_ld16(lanes + B::T_X + 32 * half + 16 * j, d);
-                    tmem_ld16(lanes + B::T_P + 32 * half + 16 * j, y);
-                    tmem_wait_ld();
                     uint32_t w[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const uint64_t kp = *(const uint64_t*)(aux + kK + 16 * j + 2 * i);
                         const uint64_t bt = *(const uint64_t*)(aux + kB + 16 * j + 2 * i);
-                        U[8 * j + i] = f2_fma(kp, f2_pack(d[2 * i], d[2 * i + 1]), f2_pack(y[2 * i], y[2 * i + 1]));
+                        U[8 * j + i] = f2_fma(kp, f2_pack(d[j][2 * i], d[j][2 * i + 1]), f2_pack(y[j][2 * i], y[j][2 * i + 1]));
                         float a, b;
                         f2_unpack(f2_mul(bt, U[8 * j + i]), a, b);
                         w[i] = pack_bf16(a, b);
@@ -1081,17 +1079,15 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                 ready(&r_ready);
                 if (!wait(&e_full, r)) break;
                 uint32_t wv[16];  // dV
+                load32(lanes + B::T_X + 32 * half, d);
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    float d[16];
-                    tmem_ld16(lanes + B::T_X + 32 * half + 16 * j, d);
-                    tmem_wait_ld();
                     uint32_t w[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const uint64_t gm = *(const uint64_t*)(aux + kG + 16 * j + 2 * i);  // -e^G
                         const uint64_t bt = *(const uint64_t*)(aux + kB + 16 * j + 2 * i);
-                        U[8 * j + i] = f2_fma(f2_pack(d[2 * i], d[2 * i + 1]), minus, U[8 * j + i]);
+                        U[8 * j + i] = f2_fma(f2_pack(d[j][2 * i], d[j][2 * i + 1]), minus, U[8 * j + i]);
                         const uint64_t y = f2_mul(bt, U[8 * j + i]);
                         float a, b;
                         f2_unpack(y, a, b);
@@ -1582,7 +1578,14 @@ SaveParts save_parts(const Packed& p)
 
 }  // namespace
 
-bool tc_delta_supported(const Packed& p) { return p.bf16 && p.T >= 32 * (long long)p.n; }
+// By the average length (the lengths are on the device).  A walk costs a sequence 10 us and 3 us for
+// each 64 tokens, the scans 0.2 us (d = 128: 0.35) for each token.  Measured, H16, scans / chunks in us:
+//   d = 64:  64 x 16 tokens 35 / 64, 64 x 32 60 / 66, 64 x 64 109 / 68; training 137 / 139, 241 / 146
+//   d = 128: 8 x 16 tokens 27 / 19, 64 x 16 150 / 80, 64 x 64 472 / 86
+//   one prompt of 4000 among 100 single tokens: d = 64 794 / 216, d = 128 1283 / 270
+// so the chunks take over at 16 and 8 tokens: below what uniform short sequences of d = 64 would
+// like, for the sake of prompts among single tokens.
+bool tc_delta_supported(const Packed& p) { return p.bf16 && (long long)p.T * p.d >= 1024LL * p.n; }
 
 size_t tc_delta_rec_bytes(const Packed& p)
 {

@@ -473,12 +473,13 @@ cudaError_t launch(const AttnArgs& x, cudaStream_t s)
 
 bool tc_softattn_supported(const Packed& p) { return p.bf16 && (p.d == 64 || p.d == 128); }
 
-// What holds an average sequence's rows.
+// One or two tokens a sequence: 32 rows; else what holds an average sequence's rows.  (The lengths
+// are on the device: a long prompt among single tokens raises the average and takes large blocks.)
 int tc_softattn_rows(const Packed& p)
 {
     const int G = p.H / p.Hk;
-    const long long rows = (long long)p.T * G;
-    return G <= 32 && rows <= 32LL * p.n ? 32 : rows <= 128LL * p.n ? 128 : 256;
+    if (softattn_few(p) && G <= 32) return 32;
+    return (long long)p.T * G <= 128LL * p.n ? 128 : 256;
 }
 
 cudaError_t launch_tc_softattn(const AttnArgs& x, cudaStream_t s)

@@ -364,6 +364,22 @@ def _packed_attn(q, k, v, n, dev):
                       _rows(k, "k", rows, dt, dev), _rows(v, "v", rows, dt, dev))
 
 
+def _new(stream, shape, dtype, device):
+    """A result's tensor, of the current stream; used on `stream` too."""
+    t = torch.empty(shape, dtype=dtype, device=device)
+    if stream is not None:
+        t.record_stream(stream)
+    return t
+
+
+def _scratch(stream, make, *args, **kw):
+    """A workspace for one call: filled and, once released, reused in the order of `stream`."""
+    if stream is None:
+        return make(*args, **kw)
+    with torch.cuda.stream(stream):
+        return make(*args, **kw)
+
+
 def _zeros(n, what, device):
     if n == 0:
         raise FlexError(FLEX_EUNSUPPORTED, what)
@@ -405,11 +421,11 @@ def delta_fwd(q, k, v, g, beta, cu, scale=None, state=None, out=None, want_state
     T, H, d = v.shape
     gates, dt, st = (T, H), q.dtype, (n, H, d, d)
     if out is None:
-        out = torch.empty(T, H, d, dtype=dt, device=q.device)
+        out = _new(stream, (T, H, d), dt, q.device)
     if last_state is None and want_state:
-        last_state = torch.empty(st, dtype=torch.float32, device=q.device)
+        last_state = _new(stream, st, torch.float32, q.device)
     if ws is None:
-        ws = delta_workspace(q, v, cu)
+        ws = _scratch(stream, delta_workspace, q, v, cu)
     _check(load().flex_delta_fwd(
         ctypes.byref(shape), q.data_ptr(), k.data_ptr(), v.data_ptr(),
         _plain(g, "g", gates, dt, dev), _plain(beta, "beta", gates, dt, dev), cu_ptr,
@@ -430,10 +446,10 @@ def delta_bwd(q, k, v, g, beta, cu, dout, save, scale=None, dq=None, dk=None, dv
     dt, T, H = q.dtype, v.shape[0], v.shape[1]
     gates = (T, H)
     names, shapes = ("dq", "dk", "dv", "dg", "dbeta"), (q.shape, k.shape, v.shape, gates, gates)
-    grads = [torch.empty(s, dtype=dt, device=q.device) if x is None else x
+    grads = [_new(stream, s, dt, q.device) if x is None else x
              for x, s in zip((dq, dk, dv, dg, dbeta), shapes)]
     if ws is None:
-        ws = delta_workspace(q, v, cu, backward=True)
+        ws = _scratch(stream, delta_workspace, q, v, cu, backward=True)
     _check(load().flex_delta_bwd(
         ctypes.byref(shape), q.data_ptr(), k.data_ptr(), v.data_ptr(),
         _plain(g, "g", gates, dt, dev), _plain(beta, "beta", gates, dt, dev), cu_ptr,
@@ -453,7 +469,7 @@ def delta_decode(q, k, v, g, beta, S, scale=None, out=None, stream=None):
     n, H, d = v.shape
     gates, dt = (n, H), q.dtype
     if out is None:
-        out = torch.empty((n, H, d), dtype=dt, device=q.device)
+        out = _new(stream, (n, H, d), dt, q.device)
     rc = load().flex_delta_decode(
         ctypes.byref(shape), q.data_ptr(), k.data_ptr(), v.data_ptr(),
         _plain(g, "g", gates, dt, dev), _plain(beta, "beta", gates, dt, dev),
@@ -483,11 +499,11 @@ def softattn_fwd(q, k, v, cu_q, cu_k=None, causal=True, scale=None, out=None, ls
     shape = _packed_attn(q, k, v, cu_q.numel() - 1, dev)
     T, H, d = q.shape
     if out is None:
-        out = torch.empty(T, H, d, dtype=q.dtype, device=q.device)
+        out = _new(stream, (T, H, d), q.dtype, q.device)
     if lse is None and want_lse:
-        lse = torch.empty(T, H, dtype=torch.float32, device=q.device)
+        lse = _new(stream, (T, H), torch.float32, q.device)
     if ws is None:
-        ws = softattn_workspace(q, k, cu_q)
+        ws = _scratch(stream, softattn_workspace, q, k, cu_q)
     _check(load().flex_softattn_fwd(
         ctypes.byref(shape), q.data_ptr(), k.data_ptr(), v.data_ptr(),
         _offsets(cu_q, "cu_q", dev), _offsets(cu_k, "cu_k", dev),

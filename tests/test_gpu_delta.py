@@ -236,3 +236,67 @@ def test_offsets_out_of_range_stay_inside():
     out, _ = _fwd(x, torch.tensor([0, 50, 900], dtype=torch.int32, device="cuda"))
     ref, _ = _fwd(x, offsets(lens))
     assert torch.equal(out, ref)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_nan_of_the_next_sequence_stays_there(d, dtype):
+    """A chunk's tiles reach into the next sequence, all of whose inputs are NaN."""
+    lens, H, Hk = (70, 90), 2, 2
+    x, cu = delta_inputs(lens, H, Hk, d, dtype, seed=12), offsets(lens)
+    for t in x.values():
+        t[70:] = float("nan")
+    out, last = _fwd(x, cu)
+    grads = _bwd(x, cu)
+    one = {m: t[:70].contiguous() for m, t in x.items()}
+    ro, rs = delta_ref(one, lens[:1], d ** -0.5)
+    check(out[:70], ro, "out")
+    check(last[0], rs[0], "last state", F32)
+    for m, y, r in zip(NAMES, grads, delta_grads(one, lens[:1], d ** -0.5)):
+        check(y[:70], r, "d" + m)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_a_prompt_among_single_tokens(dtype):
+    lens, H, Hk, d = (1, 500) + (1,) * 9 + (0, 33), 2, 1, 64
+    x, cu = delta_inputs(lens, H, Hk, d, dtype, seed=13), offsets(lens)
+    out, last = _fwd(x, cu)
+    ro, rs = delta_ref(x, lens, d ** -0.5)
+    check(out, ro, "out")
+    check(last, rs, "last state", F32)
+    for m, y, r in zip(NAMES, _bwd(x, cu), delta_grads(x, lens, d ** -0.5)):
+        check(y, r, "d" + m)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_rows_far_apart(dtype):
+    """Row strides that put the last rows more than 2^31 elements behind the first."""
+    lens, H, Hk, d = (130, 20), 2, 1, 64
+    T, stride = 150, (1 << 24) + 8
+    x, cu = delta_inputs(lens, H, Hk, d, dtype, seed=14), offsets(lens)
+    # three views of one long buffer, 512 elements apart inside each row
+    long = torch.empty((T - 1) * stride + 2048, dtype=dtype, device="cuda")
+    y = dict(x)
+    for i, m in enumerate(("q", "k", "v")):
+        t = x[m]
+        y[m] = torch.as_strided(long, t.shape, (stride, d, 1), storage_offset=512 * i)
+        y[m].copy_(t)
+    a, b = _fwd(x, cu), _fwd(y, cu)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    assert all(torch.equal(u, w) for u, w in zip(_bwd(x, cu), _bwd(y, cu)))
+
+
+def test_calls_on_a_stream_of_their_own():
+    """`stream=` without a workspace: the call's scratch belongs to that stream."""
+    lens, H, Hk, d = (300, 77), 4, 2, 64
+    x, cu = delta_inputs(lens, H, Hk, d, BF16, seed=15), offsets(lens)
+    want = _fwd(x, cu)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = []
+    for _ in range(4):
+        got.append(_fwd(x, cu, stream=side))
+        torch.zeros(1 << 22, device="cuda")  # would land in scratch released too early
+    torch.cuda.current_stream().wait_stream(side)
+    for out, last in got:
+        assert torch.equal(out, want[0]) and torch.equal(last, want[1])

@@ -161,6 +161,57 @@ def test_other_stream_graph_and_repeat():
     flexattn.check_status(ws)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("H,Hk", [(4, 4), (8, 1)])
+def test_a_prompt_among_single_tokens(H, Hk, dtype):
+    lens_q, lens_k = (1, 400) + (1,) * 20 + (0, 2), (900, 400) + (70,) * 20 + (5, 600)
+    _check(*_inputs(lens_q, lens_k, H, Hk, 64, dtype, seed=11), lens_q, lens_k, True)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("causal", [True, False])
+def test_many_sequences(dtype, causal):
+    """More sequences than are put in order by their work."""
+    lens = tuple((7 * i) % 40 for i in range(150)) + (260,)
+    _check(*_inputs(lens, lens, 2, 1, 64, dtype, seed=12), lens, lens, causal)
+    tok = (1,) * len(lens)
+    lens_k = tuple(n + 1 for n in lens)
+    _check(*_inputs(tok, lens_k, 2, 1, 64, dtype, seed=13), tok, lens_k, causal)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_rows_far_apart(dtype):
+    """Row strides that put the last rows more than 2^31 elements behind the first."""
+    lens, H, Hk, d, stride = (130, 20), 2, 1, 64, (1 << 24) + 8
+    q, k, v = _inputs(lens, lens, H, Hk, d, dtype, seed=14)
+    long = torch.empty(149 * stride + 2048, dtype=dtype, device="cuda")
+
+    def far(t, at):
+        y = torch.as_strided(long, t.shape, (stride, d, 1), storage_offset=at)
+        y.copy_(t)
+        return y
+
+    a = flexattn.softattn_fwd(q, k, v, offsets(lens))
+    b = flexattn.softattn_fwd(far(q, 0), far(k, 512), far(v, 1024), offsets(lens))
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_calls_on_a_stream_of_their_own():
+    """`stream=` without a workspace: the call's scratch belongs to that stream."""
+    lens, lens_k = (1, 2), (3000, 900)
+    q, k, v = _inputs(lens, lens_k, 8, 2, 128, BF16, seed=15)
+    cu, cu_k = offsets(lens), offsets(lens_k)
+    want = flexattn.softattn_fwd(q, k, v, cu, cu_k)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = []
+    for _ in range(4):
+        got.append(flexattn.softattn_fwd(q, k, v, cu, cu_k, stream=side))
+        torch.zeros(1 << 22, device="cuda")  # would land in scratch released too early
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(o, want[0]) and torch.equal(z, want[1]) for o, z in got)
+
+
 def test_teacher_of_the_distillation_loss():
     """lse is the normaliser that the distillation's teacher uses: with the frequencies at zero
     the kernel's weights are uniform and the loss is log N for any teacher, and a packed call of
