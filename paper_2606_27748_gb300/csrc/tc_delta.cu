@@ -67,14 +67,6 @@ __device__ __forceinline__ void split(float a, float b, uint32_t& hi, uint32_t& 
     split2(f2_pack(a, b), hi, lo);
 }
 
-// 32 lanes x 32 columns: both loads in flight together.
-__device__ __forceinline__ void load32(uint32_t taddr, float (&a)[2][16])
-{
-    tmem_ld16(taddr, a[0]);
-    tmem_ld16(taddr + 16, a[1]);
-    tmem_wait_ld();
-}
-
 // Eight packed pairs rounded to bf16.
 __device__ __forceinline__ void pack8(const uint64_t* x, uint32_t (&w)[8])
 {
@@ -345,6 +337,10 @@ struct Walk {
     static constexpr int QUADS = D / 32;            // quadrants of tensor memory's lanes in use
     static constexpr int WARPS = 2 * QUADS;         // state warps, and as many token warps
     static constexpr int PIECES = D / 64;           // of the state: 64 key dimensions each
+    // The issuing and the loading warp: for d = 64, which computes on quadrants 0 and 1 and so on
+    // schedulers 0 and 1, they go to the others (reverse walk, 8 x 2048 H12: 82 -> 72 us; d = 128 is
+    // the slower for it).
+    static constexpr int MMA = D == 64 ? 18 : 16, TMA = D == 64 ? 19 : 17;
     static constexpr uint32_t TILE = kC * D * 2;    // 64 rows of K, Q or V
     static constexpr uint32_t K = 0, Q = TILE, V = 2 * TILE, REC = 3 * TILE;
     static constexpr uint32_t STAGE = (REC + Rec::BYTES + 1023) / 1024 * 1024;
@@ -356,7 +352,7 @@ struct Walk {
                          T_UL = D + 160, T_D = D + 192, T_Q = 2 * D + 192;
     static_assert(2 * D + 256 <= 512, "tensor memory");
 };
-constexpr int kWalkThreads = 640, kWalkMma = 16, kWalkTma = 17;
+constexpr int kWalkThreads = 640;
 
 struct WalkArgs {
     Packed p;
@@ -373,7 +369,7 @@ struct WalkArgs {
 // State warps (0-7; d = 64: 0, 1, 4, 5) hold the state's fp32 master in registers: quadrant w % 4
 // of the lanes, half w / 4 % 2 of each piece of 64 key dimensions.  Token warps (8-15) work on the
 // chunk's tokens, half of them each, and write the output while the state warps are busy.  Warp
-// 16 issues the products, 17 loads.  A chunk:
+// MMA issues the products, warp TMA loads.  A chunk:
 //   state   S += last chunk's increment; S high, low -> tensor memory, by pieces   (s_ready)
 //   issue   X = K S                                                                (x_full)
 //   tokens  R = V - e^G X; beta R high, low                                        (r_ready)
@@ -426,7 +422,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
         abort_flag = 0;
         fence_mbar_init();
     }
-    if (warp == kWalkMma) {
+    if (warp == W::MMA) {
         tmem_alloc(&tmem_base_sh, 512);
         tmem_relinquish();
     }
@@ -446,7 +442,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
     // registers: launched with 96 a thread; 2 x 104 + 2 x 104 + 64 = 480 = 5 x 96
     if (warp >= 16) {
         setmaxnreg_dec<64>();
-        if (warp == kWalkTma) {
+        if (warp == W::TMA) {
             grid_dep_wait();  // the records
             for (int c = 0; c < chunks; ++c) {
                 uint64_t* bar = &full[c % W::ST];
@@ -464,7 +460,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                 if (elect_one())
                     bulk_load(st + W::REC, x.rec + (rec0 + (size_t)c * pk.H) * Rec::BYTES, Rec::BYTES, bar);
             }
-        } else if (warp == kWalkMma && tm == 0) {  // all of tensor memory starts at its address 0
+        } else if (warp == W::MMA && tm == 0) {  // all of tensor memory starts at its address 0
             constexpr uint32_t I_C = idesc_bf16(128, kC, 0, 0), I_D = idesc_bf16(128, 64, 0, 1);
             bool ok = true;
             auto wait = [&](uint64_t* bar, int phase) {
@@ -562,16 +558,15 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
 #pragma unroll
                 for (int p = 0; p < W::PIECES; ++p) {
                     if (c > 0 && !wait(&s_full[p], c - 1)) break;
-                    // (all of a step's loads ahead of their first use: a round trip to tensor memory
-                    // takes 250 cycles)
-                    float a[2][16];
-                    if (c > 0) load32(lanes + W::T_D + 64 * p + 32 * half, a);
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         if (c > 0) {  // S = decay S + the increment of the last chunk
+                            float a[16];
+                            tmem_ld16(lanes + W::T_D + 64 * p + 32 * half + 16 * j, a);
+                            tmem_wait_ld();
 #pragma unroll
                             for (int e = 0; e < 8; ++e)
-                                S[p][8 * j + e] = f2_fma(decay, S[p][8 * j + e], f2_pack(a[j][2 * e], a[j][2 * e + 1]));
+                                S[p][8 * j + e] = f2_fma(decay, S[p][8 * j + e], f2_pack(a[2 * e], a[2 * e + 1]));
                         }
                         if (c < chunks) {
                             uint32_t wh[8], wl[8];
@@ -641,10 +636,11 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                     }
                 }
                 if (!wait(&x_full, c)) break;
-                float d[2][16];
-                load32(lanes + W::T_X + 32 * half, d);
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
+                    float d[16];
+                    tmem_ld16(lanes + W::T_X + 32 * half + 16 * j, d);
+                    tmem_wait_ld();
                     uint32_t wh[8], wl[8];
 #pragma unroll
                     for (int i = 0; i < 8; i += 2) {  // (X is 0 behind the end: K is)
@@ -652,8 +648,8 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                         const ulonglong2 bt = *(const ulonglong2*)(aux + Rec::BETA / 4 + 16 * j + 2 * i);
                         uint64_t* r = R + 8 * j + i;
                         // (e^G holds its negative in the record: R = V - e^G X)
-                        r[0] = f2_fma(gm.x, f2_pack(d[j][2 * i], d[j][2 * i + 1]), r[0]);
-                        r[1] = f2_fma(gm.y, f2_pack(d[j][2 * i + 2], d[j][2 * i + 3]), r[1]);
+                        r[0] = f2_fma(gm.x, f2_pack(d[2 * i], d[2 * i + 1]), r[0]);
+                        r[1] = f2_fma(gm.y, f2_pack(d[2 * i + 2], d[2 * i + 3]), r[1]);
                         split2(f2_mul(bt.x, r[0]), wh[i], wl[i]);
                         split2(f2_mul(bt.y, r[1]), wh[i + 1], wl[i + 1]);
                     }
@@ -663,17 +659,19 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                 ready(&r_ready);
                 if (!wait(&e_full, c)) break;
                 const uint64_t minus = f2_pack(-1.f, -1.f);
-                load32(lanes + W::T_X + 32 * half, d);
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
+                    float d[16];
+                    tmem_ld16(lanes + W::T_X + 32 * half + 16 * j, d);
+                    tmem_wait_ld();
                     uint32_t wh[8], wl[8];
 #pragma unroll
                     for (int i = 0; i < 8; i += 2) {
                         const ulonglong2 bt = *(const ulonglong2*)(aux + Rec::BETA / 4 + 16 * j + 2 * i);
                         const ulonglong2 kp = *(const ulonglong2*)(aux + Rec::KAPPA / 4 + 16 * j + 2 * i);
                         uint64_t* r = R + 8 * j + i;
-                        r[0] = f2_fma(f2_pack(d[j][2 * i], d[j][2 * i + 1]), minus, r[0]);
-                        r[1] = f2_fma(f2_pack(d[j][2 * i + 2], d[j][2 * i + 3]), minus, r[1]);
+                        r[0] = f2_fma(f2_pack(d[2 * i], d[2 * i + 1]), minus, r[0]);
+                        r[1] = f2_fma(f2_pack(d[2 * i + 2], d[2 * i + 3]), minus, r[1]);
                         split2(f2_mul(f2_mul(kp.x, bt.x), r[0]), wh[i], wl[i]);
                         split2(f2_mul(f2_mul(kp.y, bt.y), r[1]), wh[i + 1], wl[i + 1]);
                     }
@@ -709,9 +707,14 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                     }
                 }
                 if (!wait(&o_full, c)) break;
-                load32(lanes + W::T_X + 32 * half, d);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) R[e] = f2_pack(d[e / 8][2 * (e % 8)], d[e / 8][2 * (e % 8) + 1]);
+                for (int j = 0; j < 2; ++j) {
+                    float d[16];
+                    tmem_ld16(lanes + W::T_X + 32 * half + 16 * j, d);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) R[8 * j + e] = f2_pack(d[2 * e], d[2 * e + 1]);
+                }
                 fence_before_sync();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&x_free);
@@ -719,14 +722,16 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                 __nv_bfloat16* dst = out + (size_t)(c * kC) * os;
                 const uint32_t pick = lane & 1 ? 0x3276u : 0x5410u;
                 const uint64_t factor = f2_pack(-x.scale, -x.scale);
-                load32(lanes + W::T_Q + 32 * half, d);
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
+                    float d[16];
+                    tmem_ld16(lanes + W::T_Q + 32 * half + 16 * j, d);
+                    tmem_wait_ld();
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const uint64_t gm = *(const uint64_t*)(aux + Rec::GAMMA / 4 + 16 * j + 2 * e);
                         float o0, o1;
-                        f2_unpack(f2_fma(f2_mul(factor, gm), f2_pack(d[j][2 * e], d[j][2 * e + 1]), R[8 * j + e]), o0, o1);
+                        f2_unpack(f2_fma(f2_mul(factor, gm), f2_pack(d[2 * e], d[2 * e + 1]), R[8 * j + e]), o0, o1);
                         const uint32_t w = pack_bf16(o0, o1);
                         const uint32_t y = __byte_perm(w, __shfl_xor_sync(0xffffffffu, w, 1), pick);
                         if (16 * j + 2 * e + (lane & 1) < n) *(uint32_t*)dst = y;
@@ -745,7 +750,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
     }
     __syncthreads();
     drain_after_abort(abort_flag);
-    if (warp == kWalkMma) {
+    if (warp == W::MMA) {
         fence_after_sync();
         tmem_dealloc(tm, 512);
     }
@@ -869,7 +874,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
         abort_flag = 0;
         fence_mbar_init();
     }
-    if (warp == kWalkMma) {
+    if (warp == W::MMA) {
         tmem_alloc(&tmem_base_sh, 512);
         tmem_relinquish();
     }
@@ -890,7 +895,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
     // registers: launched with 96 a thread; 4 x 104 + 64 = 480 = 5 x 96
     if (warp >= 16) {
         setmaxnreg_dec<64>();
-        if (warp == kWalkTma) {
+        if (warp == W::TMA) {
             for (int r = 0; r < chunks; ++r) {
                 uint64_t* bar = &full[r % B::ST];
                 if (r >= B::ST &&
@@ -908,7 +913,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                     bulk_load(st + B::REC, x.rec + (rec0 + (size_t)c * pk.H) * Rec::BYTES + Rec::M_HI,
                               B::REC_BYTES, bar);
             }
-        } else if (warp == kWalkMma && tm == 0) {
+        } else if (warp == W::MMA && tm == 0) {
             constexpr uint32_t I_C = idesc_bf16(128, kC, 0, 0), I_CM = idesc_bf16(128, kC, 0, 1);
             constexpr uint32_t I_P = idesc_bf16(128, kC, 1, 1), I_D = idesc_bf16(128, 64, 0, 1);
             bool ok = true;
@@ -984,16 +989,25 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) S[p][i] = f2_pack(0.f, 0.f);
             uint64_t decay = f2_pack(1.f, 1.f);
+            // A round trip to tensor memory takes 250 cycles: for d = 64 both loads of a step are in
+            // flight together (78 -> 72 us for 8 x 2048, H12; d = 128 has no registers left for it).
+            constexpr bool ahead = D == 64;
             for (int r = 0; r < chunks; ++r) {
                 __nv_bfloat16* ds = x.ds + ((rec0 + (size_t)(chunks - 1 - r) * pk.H) * D + v) * D + 32 * half;
 #pragma unroll
                 for (int p = 0; p < W::PIECES; ++p) {
                     if (r > 0 && !wait(&s_full[p], r - 1)) break;
+                    const uint32_t inc = lanes + B::T_D + 64 * p + 32 * half;
                     float a[2][16];
-                    if (r > 0) load32(lanes + B::T_D + 64 * p + 32 * half, a);
+                    if (ahead && r > 0) {
+                        tmem_ld16(inc, a[0]);
+                        tmem_ld16(inc + 16, a[1]);
+                    }
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         if (r > 0) {  // S = decay S + the increment of the chunk behind
+                            if (!ahead) tmem_ld16(inc + 16 * j, a[j]);
+                            tmem_wait_ld();
 #pragma unroll
                             for (int e = 0; e < 8; ++e)
                                 S[p][8 * j + e] = f2_fma(decay, S[p][8 * j + e], f2_pack(a[j][2 * e], a[j][2 * e + 1]));
@@ -1058,12 +1072,20 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                 }
                 if (!wait(&x_full, r)) break;
                 uint64_t U[16];  // dU, then Y: pairs of tokens
+                constexpr bool ahead = D == 64;  // (see above)
                 float d[2][16], y[2][16];
-                tmem_ld16(lanes + B::T_P + 32 * half, y[0]);
-                tmem_ld16(lanes + B::T_P + 32 * half + 16, y[1]);
-                load32(lanes + B::T_X + 32 * half, d);
+                auto fetch = [&](int j) {
+                    tmem_ld16(lanes + B::T_X + 32 * half + 16 * j, d[j]);
+                    tmem_ld16(lanes + B::T_P + 32 * half + 16 * j, y[j]);
+                };
+                if (ahead) {
+                    fetch(0);
+                    fetch(1);
+                }
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
+                    if (!ahead) fetch(j);
+                    tmem_wait_ld();
                     uint32_t w[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
@@ -1079,9 +1101,14 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                 ready(&r_ready);
                 if (!wait(&e_full, r)) break;
                 uint32_t wv[16];  // dV
-                load32(lanes + B::T_X + 32 * half, d);
+                if (ahead) {
+                    tmem_ld16(lanes + B::T_X + 32 * half, d[0]);
+                    tmem_ld16(lanes + B::T_X + 32 * half + 16, d[1]);
+                }
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
+                    if (!ahead) tmem_ld16(lanes + B::T_X + 32 * half + 16 * j, d[j]);
+                    tmem_wait_ld();
                     uint32_t w[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
@@ -1122,7 +1149,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
     }
     __syncthreads();
     drain_after_abort(abort_flag);
-    if (warp == kWalkMma) {
+    if (warp == W::MMA) {
         fence_after_sync();
         tmem_dealloc(tm, 512);
     }
