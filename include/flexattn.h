@@ -257,9 +257,11 @@ size_t flex_delta_save_bytes(const flex_packed* shape);
  * or the same, receives each sequence's last state (an empty sequence's is its first); S1
  * may be S0.  save: NULL, or flex_delta_save_bytes() bytes, 256-byte aligned, filled for
  * flex_delta_bwd; training starts from the zero state, so S0 must then be NULL.
- * States and sums are fp32; with bf16 storage and long sequences the products run on the
- * tensor cores with the state and the corrections as bf16 high and low parts.
- * Errors: FLEX_EINVAL, FLEX_EUNSUPPORTED (d, or more than 65535 sequences), FLEX_EWORKSPACE. */
+ * States and sums are fp32.  bf16 storage with 1024 / d tokens a sequence on average runs in
+ * chunks of 64 tokens on the tensor cores, with the state, the corrections and the weights as
+ * bf16 high and low parts (2 kernels; log decays below -88 count as -88); the rest token by token
+ * (1 kernel).  Errors: FLEX_EINVAL, FLEX_EUNSUPPORTED (d, or more than 65535 sequences or 1024
+ * heads), FLEX_EWORKSPACE. */
 int flex_delta_fwd(const flex_packed* shape, const void* q, const void* k, const void* v,
                    const void* g, const void* beta, const int* cu, float scale,
                    const float* S0, float* S1, void* out, void* save, void* ws,
@@ -272,7 +274,7 @@ int flex_delta_fwd(const flex_packed* shape, const void* q, const void* k, const
  *   D_t += scale q_t dout_t^T;  dq_t = scale S_t dout_t;  dv_t = beta_t D_t^T k_t;
  *   dbeta_t = e_t . D_t^T k_t;  dk_t = beta_t D_t e_t - a_t S_{t-1} dv_t;
  *   dg_t = a_t <S_{t-1}, D_t - k_t dv_t^T>;  D_{t-1} = a_t (D_t - k_t dv_t^T).
- * Every sum has a fixed order: results repeat bit for bit. */
+ * Every sum has a fixed order: results repeat bit for bit.  2 kernels (4 token by token). */
 int flex_delta_bwd(const flex_packed* shape, const void* q, const void* k, const void* v,
                    const void* g, const void* beta, const int* cu, float scale,
                    const void* dout, const void* save, void* dq, void* dk, void* dv, void* dg,
@@ -296,7 +298,8 @@ size_t flex_softattn_workspace_bytes(const flex_packed* shape);
  * [T][H] fp32.  H / Hk <= 64.  What lies outside a sequence (NaN included) does not reach its
  * rows; inside it every v must be finite, also where the mask hides it.
  * Scores, softmax sums and the output's sums are fp32; with bf16 storage the weights enter
- * the second product as bf16.  1 kernel, or 2 where the keys are split. */
+ * the second product as bf16 (their sum is taken before that rounding).  Results repeat bit for
+ * bit.  1 kernel, or 2 where the keys are split. */
 int flex_softattn_fwd(const flex_packed* shape, const void* q, const void* k, const void* v,
                       const int* cu_q, const int* cu_k, float scale, int causal, void* out,
                       float* lse, void* ws, size_t ws_bytes, void* stream);
