@@ -300,3 +300,35 @@ def test_calls_on_a_stream_of_their_own():
     torch.cuda.current_stream().wait_stream(side)
     for out, last in got:
         assert torch.equal(out, want[0]) and torch.equal(last, want[1])
+
+
+@pytest.mark.parametrize("dtype,rows", [(F32, 5), (BF16, 5), (BF16, 70)], ids=str)
+def test_sequences_that_are_all_empty(dtype, rows):
+    H, Hk, d = 2, 1, 64
+    x, cu = delta_inputs((0, 0), H, Hk, d, dtype, seed=16, rows_behind=rows), offsets((0, 0))
+    out = torch.full((rows, H, d), 7.0, dtype=dtype, device="cuda")
+    save = flexattn.delta_save(x["q"], x["v"], cu)
+    _, last = _fwd(x, cu, out=out, save=save)
+    grads = {"d" + m: torch.full_like(x[m], 7.0) for m in NAMES}
+    flexattn.delta_bwd(*(x[m] for m in NAMES), cu, x["dout"], save, **grads)
+    assert (last == 0).all()
+    assert all((t == 7.0).all() for t in (out, *grads.values()))
+    S0 = torch.randn(2, H, d, d, device="cuda")
+    assert torch.equal(_fwd(x, cu, state=S0)[1], S0)
+
+
+@pytest.mark.parametrize("dtype,lens,fwd,bwd", [(F32, (100, 30), 1, 4), (BF16, (3, 4), 1, 4),
+                                                (BF16, (100, 30), 2, 2)], ids=str)
+def test_launch_counts(dtype, lens, fwd, bwd):
+    x, cu = delta_inputs(lens, 2, 1, 64, dtype, seed=17), offsets(lens)
+    save = flexattn.delta_save(x["q"], x["v"], cu)
+    n = [flexattn.kernel_launches()]
+    _fwd(x, cu, save=save)
+    n.append(flexattn.kernel_launches())
+    flexattn.delta_bwd(*(x[m] for m in NAMES), cu, x["dout"], save)
+    n.append(flexattn.kernel_launches())
+    k = len(lens)
+    flexattn.delta_decode(*(x[m][:k].contiguous() for m in NAMES),
+                          torch.zeros(k, 2, 64, 64, device="cuda"))
+    n.append(flexattn.kernel_launches())
+    assert [b - a for a, b in zip(n, n[1:])] == [fwd, bwd, 1]

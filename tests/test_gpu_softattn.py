@@ -212,6 +212,15 @@ def test_calls_on_a_stream_of_their_own():
     assert all(torch.equal(o, want[0]) and torch.equal(z, want[1]) for o, z in got)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_sequences_that_are_all_empty(dtype):
+    q, k, v = _inputs((0, 0), (5, 0), 2, 1, 64, dtype, seed=16, behind=40)
+    out = torch.full_like(q, 7.0)
+    lse = torch.full(q.shape[:2], 7.0, device="cuda")
+    flexattn.softattn_fwd(q, k, v, offsets((0, 0)), offsets((5, 0)), out=out, lse=lse)
+    assert (out == 7.0).all() and (lse == 7.0).all()
+
+
 def test_teacher_of_the_distillation_loss():
     """lse is the normaliser that the distillation's teacher uses: with the frequencies at zero
     the kernel's weights are uniform and the loss is log N for any teacher, and a packed call of
