@@ -18,7 +18,8 @@ constexpr int kRows = 64, kKeys = 64, kThreads = 256;
 
 // fp32: tiles of 64 rows x 64 keys, 256 threads.  A thread holds 4 x 4 scores (rows 4 ty ..,
 // keys tx, tx + 16, ..) and 4 x D / 16 outputs; each 16-byte shared read feeds 8 (scores) to
-// 10 (outputs) FMAs.  Row pads of 4 floats keep the reads of 16 keys apart by banks.
+// 10 (outputs) FMAs.  Row pads of 4 floats keep the reads of 16 keys apart by banks.  V's loads are
+// in flight behind the scores, the next K's behind the outputs.
 template <int D>
 struct SimtSmem {
     float q[kRows][D + 4];
@@ -34,9 +35,9 @@ __global__ void __launch_bounds__(kThreads) softattn_simt_kernel(AttnArgs x)
     const Packed& pk = x.p;
     const int G = pk.H / pk.Hk, tpt = kRows / G;  // tokens of a tile
     const int tid = threadIdx.x, tx = tid % 16, ty = tid / 16;
-    const int hk = blockIdx.y % pk.Hk, split = blockIdx.y / pk.Hk;
+    const int hk = blockIdx.x % pk.Hk, split = blockIdx.x / pk.Hk;
     int s, block, qlo, qhi, klo, khi;
-    if (!find_block(x.cu_q, pk.n, pk.T, tpt, (int)blockIdx.x, s, block, qlo, qhi)) return;
+    if (!find_tile(x, tpt, (int)(blockIdx.z * gridDim.y + blockIdx.y), s, block, qlo, qhi)) return;
     seq_rows(x.cu_k, s, pk.Tk, klo, khi);
     const int t0 = block * tpt, nt = min(tpt, qhi - qlo - t0);  // tokens of this tile
     const int lk = khi - klo, shift = lk - (qhi - qlo);
@@ -58,16 +59,29 @@ __global__ void __launch_bounds__(kThreads) softattn_simt_kernel(AttnArgs x)
         const int r = 4 * ty + i;
         see[i] = r >= nt * G ? 0 : x.causal ? min(lk, t0 + r / G + shift + 1) : lk;
     }
+    float4 held[D / 16];  // this thread's part of the tile that comes next
+    auto fetch = [&](const T* base, long long stride, int j0) {
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            const int e = tid + kThreads * i, r = e / (D / 4), c = e % (D / 4) * 4;
+            held[i] = j0 + r < lk ? load4(base + (klo + j0 + r) * stride + hk * D + c)
+                                  : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+    };
+    auto put = [&] {
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            const int e = tid + kThreads * i;
+            *(float4*)&sm.kv[e / (D / 4)][e % (D / 4) * 4] = held[i];
+        }
+    };
+    if (first < last) fetch((const T*)x.k, pk.ks, first * kKeys);
     for (int b = first; b < last; ++b) {
         const int j0 = b * kKeys;
         __syncthreads();
-        for (int e = tid; e < kKeys * D / 4; e += kThreads) {
-            const int r = e / (D / 4), c = e % (D / 4) * 4;
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (j0 + r < lk) v = load4((const T*)x.k + (klo + j0 + r) * pk.ks + hk * D + c);
-            *(float4*)&sm.kv[r][c] = v;
-        }
+        put();
         __syncthreads();
+        fetch((const T*)x.v, pk.vs, j0);
         float sc[4][4] = {};
 #pragma unroll 4
         for (int c = 0; c < D; c += 4) {
@@ -107,13 +121,9 @@ __global__ void __launch_bounds__(kThreads) softattn_simt_kernel(AttnArgs x)
             for (int c = 0; c < D / 16; ++c) o[i][c] *= keep;
         }
         __syncthreads();
-        for (int e = tid; e < kKeys * D / 4; e += kThreads) {
-            const int r = e / (D / 4), c = e % (D / 4) * 4;
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (j0 + r < lk) v = load4((const T*)x.v + (klo + j0 + r) * pk.vs + hk * D + c);
-            *(float4*)&sm.kv[r][c] = v;
-        }
+        put();
         __syncthreads();
+        if (b + 1 < last) fetch((const T*)x.k, pk.ks, j0 + kKeys);
 #pragma unroll 2
         for (int j = 0; j < kKeys; j += 4) {
             float4 p[4];
@@ -206,8 +216,7 @@ cudaError_t launch_simt(const AttnArgs& x, cudaStream_t s)
     cudaError_t e = cudaFuncSetAttribute(softattn_simt_kernel<T, D>,
                                          cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    const dim3 grid((unsigned)block_slots(p.T, p.n, kRows / (p.H / p.Hk)), (unsigned)(p.Hk * x.splits));
-    return tc::launch_after(softattn_simt_kernel<T, D>, grid, kThreads, smem, 0, false, s, x);
+    return tc::launch_after(softattn_simt_kernel<T, D>, softattn_grid(x, kRows / (p.H / p.Hk)), kThreads, smem, 0, false, s, x);
 }
 
 }  // namespace
@@ -219,14 +228,14 @@ int softattn_splits(const Packed& p)
     // (single tokens) cost next to nothing to join, and two blocks fit an SM; more of them pay their
     // start and end without filling it better (16 sequences of 8000 and 16 of 1777 keys, H16 Hk4
     // d128: 66 us for one block an SM, 61 for two, 64 for three, 68 for four, 73 for eight).  A range
-    // is 256 keys of an average sequence or more; 32 ranges (the join's lanes) at most.
+    // is 256 keys (fp32: 128) of an average sequence or more; 32 ranges (the join's lanes) at most.
     const int G = p.H / p.Hk;
     const bool tc = tc_softattn_supported(p);
     const int rows = tc ? tc_softattn_rows(p) : kRows;
     const int tokens = rows == 256 ? 2 * (128 / G) : rows / G;  // of a block
     const long long blocks = (long long)block_slots(p.T, p.n, tokens) * p.Hk;
     const long long want = ((softattn_few(p) || !tc ? 2 : 1) * 152 + blocks - 1) / blocks;
-    const long long most = (long long)p.Tk / p.n / 256;
+    const long long most = (long long)p.Tk / p.n / (tc ? 256 : 128);
     const long long n = want < most ? want : most;
     return n < 1 ? 1 : n > 32 ? 32 : (int)n;
 }

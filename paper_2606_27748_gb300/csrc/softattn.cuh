@@ -18,6 +18,14 @@ struct AttnArgs {
     int* status;
 };
 
+// Key heads and ranges of a tile side by side, then the tiles, longest first (find_tile's rank is
+// blockIdx.z * gridDim.y + blockIdx.y).
+inline dim3 softattn_grid(const AttnArgs& x, int tokens)
+{
+    const int slots = block_slots(x.p.T, x.p.n, tokens), y = slots < 65535 ? slots : 65535;
+    return dim3((unsigned)(x.p.Hk * x.splits), (unsigned)y, (unsigned)((slots + y - 1) / y));
+}
+
 // One or two tokens a sequence on average: the step of a serving batch.
 inline bool softattn_few(const Packed& p) { return p.T <= 2LL * p.n; }
 

@@ -455,10 +455,7 @@ cudaError_t launch(const AttnArgs& x, cudaStream_t s)
     cudaError_t e = cudaFuncSetAttribute(tc_softattn_kernel<D, ROWS>,
                                          cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L::SMEM);
     if (e != cudaSuccess) return e;
-    // key heads and ranges of a tile side by side, then the tiles, longest first
-    const int slots = block_slots(p.T, p.n, L::TILES * tpt), y = slots < 65535 ? slots : 65535;
-    const dim3 grid((unsigned)(p.Hk * x.splits), (unsigned)y, (unsigned)((slots + y - 1) / y));
-    return launch_after(tc_softattn_kernel<D, ROWS>, grid, L::THREADS, (int)L::SMEM, 0, false, s, mq, mk,
+    return launch_after(tc_softattn_kernel<D, ROWS>, softattn_grid(x, L::TILES * tpt), L::THREADS, (int)L::SMEM, 0, false, s, mq, mk,
                         mv, x);
 }
 
