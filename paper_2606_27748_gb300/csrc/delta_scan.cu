@@ -4,16 +4,17 @@
 //
 // Every column S[:, j] of the state depends on no other column (e_t[j] needs only column j), and
 // once e is known every row S[i, :] depends on no other row.  So a state is cut into lines
-// (columns, or rows) of which 8 or 16 lanes each hold 8 entries in registers, and no block waits
+// (columns, or rows) of which a few lanes each hold 8 or 16 entries in registers, and no block waits
 // for another.  The backward runs three such scans: columns in reverse for Y = D^T k (D: the
 // gradient of the state), then rows forward (dq, and S_{t-1} dv) and rows in reverse (D u), the
 // two halves of one grid.  Sums over a line are a few shuffles; sums over lines never occur.
 //
 // A column's next step needs the sum of its last one, so what bounds a scan is one warp's chain of
-// product, shuffles and update, and how many warps share a scheduler and the shared memory
-// meanwhile.  Measured for a prompt of 1000 (training 4 x 1000), H4 d64: 8 lanes to a line 188 us
-// (578); 4 lanes 173 (614); 8 tokens at once with their mutual products (a triangular system), 4
-// lanes 222 us (890 instructions a warp for 8 tokens), 16 lanes 255 (bound by shared-memory reads).
+// product (90 cycles of 360 a token), shuffles (130) and update, and how many warps share a
+// scheduler and the shared memory meanwhile.  Measured, H4 d64: forward, 1000 tokens, with 8 lanes
+// to a line 181 us, with 4 208; reverse, 4 x 1000, with 4 lanes 142, with 8 156; 8 tokens at once with
+// their mutual products (a triangular system), 4 lanes 222 us (890 instructions a warp for 8
+// tokens), 16 lanes 255 (bound by shared-memory reads).
 #include "flex_internal.h"
 #include "packed.cuh"
 #include "tc_util.cuh"
@@ -25,8 +26,8 @@ constexpr int kLines = 32;  // lines of a block
 
 template <int D>
 struct Cfg {
-    static constexpr int P = D / 8;           // lanes of a line
-    static constexpr int THREADS = kLines * P;
+    // lanes of a line: columns forward, columns in reverse, rows
+    static constexpr int PF = D / 8, PB = D / 16, PR = D / 8;
     static constexpr int COL = 16, ROW = 1024 / D;  // tokens staged at a time
 };
 
@@ -66,44 +67,50 @@ __device__ __forceinline__ float line_sums8(float (&x)[8], int p)
     return P == 16 ? x[0] + __shfl_xor_sync(0xffffffffu, x[0], 1) : x[0];
 }
 
-// A lane's 8 entries of a line (elements 4 p + 0 .. 3, and D / 2 further) as packed pairs.
-template <int D>
+// A lane's D / P entries of a line (elements 4 p + 0 .. 3 of every 4 P) as packed pairs.
+template <int D, int P>
 struct Vec {
-    uint64_t x[4];
+    static constexpr int N = D / P / 2;
+    uint64_t x[N];
 
     __device__ __forceinline__ void read(const float* vec, int p)
     {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const ulonglong2 y = *(const ulonglong2*)(vec + D / 2 * i + 4 * p);
+        for (int i = 0; i < N / 2; ++i) {
+            const ulonglong2 y = *(const ulonglong2*)(vec + 4 * (P * i + p));
             x[2 * i] = y.x;
             x[2 * i + 1] = y.y;
         }
     }
     __device__ __forceinline__ float dot(const Vec& y) const
     {
-        const uint64_t a = tc::f2_fma(x[2], y.x[2], tc::f2_mul(x[0], y.x[0]));
-        const uint64_t b = tc::f2_fma(x[3], y.x[3], tc::f2_mul(x[1], y.x[1]));
-        float c, d, e, f;
-        tc::f2_unpack(a, c, d);
-        tc::f2_unpack(b, e, f);
-        return (c + d) + (e + f);
+        uint64_t a[N / 2];
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) a[i] = tc::f2_fma(x[i + N / 2], y.x[i + N / 2], tc::f2_mul(x[i], y.x[i]));
+        float c[N];
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) tc::f2_unpack(a[i], c[2 * i], c[2 * i + 1]);
+#pragma unroll
+        for (int m = 1; m < N; m *= 2)
+#pragma unroll
+            for (int i = 0; i + m < N; i += 2 * m) c[i] += c[i + m];
+        return c[0];
     }
     __device__ __forceinline__ void add(float w, const Vec& y)  // += w y
     {
         const uint64_t ww = tc::f2_pack(w, w);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = tc::f2_fma(ww, y.x[i], x[i]);
+        for (int i = 0; i < N; ++i) x[i] = tc::f2_fma(ww, y.x[i], x[i]);
     }
     __device__ __forceinline__ void scale(float a)
     {
         const uint64_t aa = tc::f2_pack(a, a);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = tc::f2_mul(aa, x[i]);
+        for (int i = 0; i < N; ++i) x[i] = tc::f2_mul(aa, x[i]);
     }
 };
-template <int D>
-__device__ __forceinline__ int element(int i, int p) { return D / 2 * (i / 4) + 4 * p + i % 4; }
+template <int P>
+__device__ __forceinline__ int element(int i, int p) { return 4 * (P * (i / 4) + p) + i % 4; }
 
 // The tile of tokens that a column scan works on: k, q and the lines' values (v, or dout).
 template <int D>
@@ -117,23 +124,23 @@ struct ColTile {
 // tile's loads are in flight behind the current one's work, and nothing is computed from them before
 // that is done (an exponential of the gates ahead of it cost 50 of 480 cycles a token).  Steps are
 // unrolled, and leave for the next one the sums that nothing waits for.
-template <typename T, int D, bool REV, typename Step>
+template <typename T, int D, int P, bool REV, typename Step>
 __device__ __forceinline__ void col_scan(ColTile<D>* tiles, const T* k, long long ks, const T* q,
                                          long long qs, const T* line, long long ls, const T* g,
                                          const T* beta, int H, int lo, int hi, Step step)
 {
-    constexpr int TT = Cfg<D>::COL, NT = Cfg<D>::THREADS, LP = TT * kLines / NT;
-    static_assert(TT * D == 4 * NT, "four elements of a vector to a thread");
+    constexpr int TT = Cfg<D>::COL, NT = kLines * P, LP = TT * kLines / NT, V4 = TT * D / 4 / NT;
     const int tid = threadIdx.x, nt = (hi - lo + TT - 1) / TT;
-    float4 kr, qr;
+    float4 kr[V4], qr[V4];
     float lr[LP], ar = 0.f, br = 0.f;
     auto start = [&](int i) { return REV ? hi - (i + 1) * TT : lo + i * TT; };
     auto load = [&](int t0) {
-        {
-            const int e = 4 * tid, t = t0 + e / D, c = e % D;
+#pragma unroll
+        for (int i = 0; i < V4; ++i) {
+            const int e = 4 * (tid + NT * i), t = t0 + e / D, c = e % D;
             const bool in = t >= lo && t < hi;
-            kr = in ? load4(k + t * ks + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-            qr = in ? load4(q + t * qs + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+            kr[i] = in ? load4(k + t * ks + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+            qr[i] = in ? load4(q + t * qs + c) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
 #pragma unroll
         for (int i = 0; i < LP; ++i) {
@@ -148,8 +155,11 @@ __device__ __forceinline__ void col_scan(ColTile<D>* tiles, const T* k, long lon
         }
     };
     auto put = [&](ColTile<D>& s) {
-        *(float4*)(&s.k[0][0] + 4 * tid) = kr;
-        *(float4*)(&s.q[0][0] + 4 * tid) = qr;
+#pragma unroll
+        for (int i = 0; i < V4; ++i) {
+            *(float4*)(&s.k[0][0] + 4 * (tid + NT * i)) = kr[i];
+            *(float4*)(&s.q[0][0] + 4 * (tid + NT * i)) = qr[i];
+        }
 #pragma unroll
         for (int i = 0; i < LP; ++i) (&s.line[0][0])[tid + NT * i] = lr[i];
         if (tid < TT) {
@@ -217,9 +227,9 @@ __device__ __forceinline__ void place(const Packed& p, int b, int& line0, int& h
 
 // Forward by columns.  e (NULL or [T][H][d] fp32) receives v - a S^T k.
 template <typename T, int D>
-__global__ void __launch_bounds__(Cfg<D>::THREADS) delta_fwd_kernel(ScanArgs x)
+__global__ void __launch_bounds__(kLines * Cfg<D>::PF) delta_fwd_kernel(ScanArgs x)
 {
-    constexpr int P = Cfg<D>::P;
+    constexpr int P = Cfg<D>::PF;
     __shared__ ColTile<D> tiles[2];
     const Packed& pk = x.p;
     int col0, h, s, lo, hi;
@@ -227,22 +237,22 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS) delta_fwd_kernel(ScanArgs x)
     seq_rows(x.cu, s, pk.T, lo, hi);
     const int tid = threadIdx.x, p = tid % P, cl = tid / P, col = col0 + cl;
     const int H = pk.H, hk = h / (H / pk.Hk);
-    Vec<D> S;
+    Vec<D, P> S;
     const size_t at = ((size_t)s * H + h) * D * D + col;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        S.x[i] = x.S0 ? tc::f2_pack(x.S0[at + (size_t)element<D>(2 * i, p) * D],
-                                    x.S0[at + (size_t)element<D>(2 * i + 1, p) * D])
+    for (int i = 0; i < Vec<D, P>::N; ++i)
+        S.x[i] = x.S0 ? tc::f2_pack(x.S0[at + (size_t)element<P>(2 * i, p) * D],
+                                    x.S0[at + (size_t)element<P>(2 * i + 1, p) * D])
                       : tc::f2_pack(0.f, 0.f);
     const long long os = (long long)H * D;
     T* out = (T*)x.out + (long long)lo * os + h * D + col;  // of the token that `o` belongs to
     float* e_out = x.e ? x.e + h * D + col : nullptr;
     float o = 0.f;
     bool any = false;
-    col_scan<T, D, false>(tiles, (const T*)x.k + hk * D, pk.ks, (const T*)x.q + hk * D, pk.qs,
-                          (const T*)x.v + h * D + col0, pk.vs, (const T*)x.g + h, (const T*)x.beta + h,
-                          H, lo, hi, [&](const ColTile<D>& w, int j, int t) {
-        Vec<D> k, q;
+    col_scan<T, D, P, false>(tiles, (const T*)x.k + hk * D, pk.ks, (const T*)x.q + hk * D, pk.qs,
+                             (const T*)x.v + h * D + col0, pk.vs, (const T*)x.g + h,
+                             (const T*)x.beta + h, H, lo, hi, [&](const ColTile<D>& w, int j, int t) {
+        Vec<D, P> k, q;
         k.read(w.k[j], p);
         q.read(w.q[j], p);
         const float a = w.a[j], beta = w.beta[j];
@@ -263,20 +273,20 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS) delta_fwd_kernel(ScanArgs x)
     if (any && p == 0) from_f32(*out, x.scale * o);
     if (x.S1) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < Vec<D, P>::N; ++i) {
             float a, b;
             tc::f2_unpack(S.x[i], a, b);
-            x.S1[at + (size_t)element<D>(2 * i, p) * D] = a;
-            x.S1[at + (size_t)element<D>(2 * i + 1, p) * D] = b;
+            x.S1[at + (size_t)element<P>(2 * i, p) * D] = a;
+            x.S1[at + (size_t)element<P>(2 * i + 1, p) * D] = b;
         }
     }
 }
 
 // Backward, first scan: columns of D in reverse; du_t = D_t^T k_t, D <- a (D - k dv^T).
 template <typename T, int D>
-__global__ void __launch_bounds__(Cfg<D>::THREADS) delta_bwd_cols_kernel(ScanArgs x)
+__global__ void __launch_bounds__(kLines * Cfg<D>::PB) delta_bwd_cols_kernel(ScanArgs x)
 {
-    constexpr int P = Cfg<D>::P;
+    constexpr int P = Cfg<D>::PB;
     __shared__ ColTile<D> tiles[2];
     const Packed& pk = x.p;
     int col0, h, s, lo, hi;
@@ -285,12 +295,12 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS) delta_bwd_cols_kernel(ScanArg
     const int tid = threadIdx.x, p = tid % P, cl = tid / P;
     const int H = pk.H, hk = h / (H / pk.Hk);
     const long long os = (long long)H * D;
-    Vec<D> S = {};
+    Vec<D, P> S = {};
     float* du_out = x.du + h * D + col0 + cl;
-    col_scan<T, D, true>(tiles, (const T*)x.k + hk * D, pk.ks, (const T*)x.q + hk * D, pk.qs,
-                         (const T*)x.dout + h * D + col0, os, (const T*)x.g + h, (const T*)x.beta + h,
-                         H, lo, hi, [&](const ColTile<D>& w, int j, int t) {
-        Vec<D> k, q;
+    col_scan<T, D, P, true>(tiles, (const T*)x.k + hk * D, pk.ks, (const T*)x.q + hk * D, pk.qs,
+                            (const T*)x.dout + h * D + col0, os, (const T*)x.g + h,
+                            (const T*)x.beta + h, H, lo, hi, [&](const ColTile<D>& w, int j, int t) {
+        Vec<D, P> k, q;
         k.read(w.k[j], p);
         q.read(w.q[j], p);
         const float a = w.a[j], beta = w.beta[j];
@@ -305,9 +315,9 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS) delta_bwd_cols_kernel(ScanArg
 // Backward, the row scans: even blocks rows of S forward (dq = scale S dout, r = a S_{t-1} dv),
 // odd blocks rows of D in reverse (w = D u, u = beta e).  By tokens; sums of 8 tokens at once.
 template <typename T, int D>
-__global__ void __launch_bounds__(Cfg<D>::THREADS) delta_bwd_rows_kernel(ScanArgs x)
+__global__ void __launch_bounds__(kLines * Cfg<D>::PR) delta_bwd_rows_kernel(ScanArgs x)
 {
-    constexpr int TT = Cfg<D>::ROW, NT = Cfg<D>::THREADS, P = Cfg<D>::P;
+    constexpr int TT = Cfg<D>::ROW, NT = kLines * Cfg<D>::PR, P = Cfg<D>::PR;
     constexpr int SLOTS = TT * D / 4;                            // 16-byte pieces of a vector: 256
     constexpr int LV = (3 * SLOTS + NT - 1) / NT, LL = TT * kLines / NT ? TT * kLines / NT : 1;
     __shared__ RowTile<D> tiles[2];
@@ -322,7 +332,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS) delta_bwd_rows_kernel(ScanArg
     const long long os = (long long)H * D;
     const T *g = (const T*)x.g + h, *beta = (const T*)x.beta + h;
     const T *k = (const T*)x.k + hk * D + row0, *q = (const T*)x.q + hk * D + row0;
-    Vec<D> S = {};
+    Vec<D, P> S = {};
 
     float4 v[LV];  // this thread's pieces of the three vectors, and what they are multiplied by
     float m[LV], kr[LL], qr[LL], ar = 0.f;
@@ -387,7 +397,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS) delta_bwd_rows_kernel(ScanArg
             if (!rev) {
 #pragma unroll
                 for (int y = 0; y < 8; ++y) {
-                    Vec<D> u, dv, dO;
+                    Vec<D, P> u, dv, dO;
                     u.read(w.vec[0][j + y], p);
                     dv.read(w.vec[1][j + y], p);
                     dO.read(w.vec[2][j + y], p);
@@ -404,7 +414,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS) delta_bwd_rows_kernel(ScanArg
             } else {
 #pragma unroll
                 for (int y = 7; y >= 0; --y) {
-                    Vec<D> u, dv, dO;
+                    Vec<D, P> u, dv, dO;
                     u.read(w.vec[0][j + y], p);
                     dv.read(w.vec[1][j + y], p);
                     dO.read(w.vec[2][j + y], p);
@@ -580,7 +590,7 @@ long long scan_blocks(const Packed& p) { return (long long)p.n * p.H * (D / kLin
 template <typename T, int D>
 cudaError_t fwd(const ScanArgs& x, cudaStream_t s)
 {
-    return tc::launch_after(delta_fwd_kernel<T, D>, dim3((unsigned)scan_blocks<D>(x.p)), Cfg<D>::THREADS, 0,
+    return tc::launch_after(delta_fwd_kernel<T, D>, dim3((unsigned)scan_blocks<D>(x.p)), kLines * Cfg<D>::PF, 0,
                             0, false, s, x);
 }
 
@@ -589,10 +599,10 @@ cudaError_t bwd(const ScanArgs& x, const FinishArgs& f, cudaStream_t s)
 {
     const Packed& p = x.p;
     const unsigned blocks = (unsigned)scan_blocks<D>(p);
-    cudaError_t e = tc::launch_after(delta_bwd_cols_kernel<T, D>, dim3(blocks), Cfg<D>::THREADS, 0, 0,
+    cudaError_t e = tc::launch_after(delta_bwd_cols_kernel<T, D>, dim3(blocks), kLines * Cfg<D>::PB, 0, 0,
                                      false, s, x);
     if (e == cudaSuccess)
-        e = tc::launch_after(delta_bwd_rows_kernel<T, D>, dim3(2 * blocks), Cfg<D>::THREADS, 0, 0, true, s, x);
+        e = tc::launch_after(delta_bwd_rows_kernel<T, D>, dim3(2 * blocks), kLines * Cfg<D>::PR, 0, 0, true, s, x);
     const long long items = (long long)p.T * p.Hk;
     if (e == cudaSuccess)
         e = tc::launch_after(delta_bwd_finish_kernel<T, D>, dim3((unsigned)((items + 3) / 4)), 128, 0,
