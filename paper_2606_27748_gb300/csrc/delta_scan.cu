@@ -23,6 +23,7 @@ namespace flex {
 namespace {
 
 constexpr int kLines = 32;  // lines of a block
+constexpr int kMark = 64;   // tokens between two marks of a sequence (see delta_bwd_gate_kernel)
 
 template <int D>
 struct Cfg {
@@ -213,7 +214,15 @@ struct ScanArgs {
     float* S1;
     void* out;
     float *e, *du, *dqh, *rh, *wh;  // [T][H][d]
+    float *Sm, *Dm;                 // [T / kMark][H][d][d]: S and D at the marks
 };
+
+// A mark's place in Sm and Dm: marks lie kMark tokens apart within a sequence, the first one kMark
+// behind its start, so no two of a batch, whatever its sequences, share a multiple of kMark.
+__device__ __forceinline__ size_t mark(const Packed& p, int t, int h)
+{
+    return ((size_t)(t / kMark - 1) * p.H + h) * p.d * p.d;
+}
 
 // Which line block, head and sequence this block works on (line blocks of a head side by side).
 template <int D>
@@ -336,7 +345,9 @@ __global__ void __launch_bounds__(kLines * Cfg<D>::PR) delta_bwd_rows_kernel(Sca
 
     float4 v[LV];  // this thread's pieces of the three vectors, and what they are multiplied by
     float m[LV], kr[LL], qr[LL], ar = 0.f;
-    auto start = [&](int i) { return rev ? hi - (i + 1) * TT : lo + i * TT; };
+    // In reverse the tiles lie as they do forward: the tokens behind the last one leave D zero.
+    static_assert(kMark % TT == 0, "marks lie between tiles");
+    auto start = [&](int i) { return lo + (rev ? nt - 1 - i : i) * TT; };
     auto load = [&](int t0) {
 #pragma unroll
         for (int i = 0; i < LV; ++i) {
@@ -427,6 +438,13 @@ __global__ void __launch_bounds__(kLines * Cfg<D>::PR) delta_bwd_rows_kernel(Sca
                 if (store) x.wh[out + t * os] = z;
             }
         }
+        const int m0 = start(i) + (rev ? 0 : TT);  // the token that the state now stands before
+        if (m0 > lo && m0 < hi && (m0 - lo) % kMark == 0) {
+            float* to = (rev ? x.Dm : x.Sm) + mark(pk, m0, h) + (size_t)(row0 + rl) * D;
+#pragma unroll
+            for (int y = 0; y < Vec<D, P>::N / 2; ++y)
+                *(ulonglong2*)(to + 4 * (P * y + p)) = make_ulonglong2(S.x[2 * y], S.x[2 * y + 1]);
+        }
         if (i + 1 < nt) put(tiles[(i + 1) & 1]);
         __syncthreads();
     }
@@ -438,6 +456,7 @@ struct FinishArgs {
     const int* cu;
     const float *e, *du, *dqh, *rh, *wh;
     void *dq, *dk, *dv, *dbeta, *dg;
+    const float *Sm, *Dm;
     float* dG;  // [H][T]
 };
 
@@ -490,35 +509,44 @@ __global__ void __launch_bounds__(128) delta_bwd_finish_kernel(FinishArgs x)
     }
 }
 
-// dg_t = the sum of dG from t to the end of t's sequence.  The terms nearly cancel over a long
-// sequence, so they are added up in 64 bits.
+// dg_t = the sum of dG from t to the end of t's sequence = <D, S> between t - 1 and t.  The terms
+// nearly cancel over a long sequence: summed to its end, roundings of the scans made dg 2.1e-6 wrong
+// (2-norm, 1000 tokens, H4 d64) and worse with the length.  So the row scans leave S and D at marks
+// kMark tokens apart (8 MB of 4 x 1000 tokens), <D, S> is taken there, and only the terms up to the
+// next mark are added, in 64 bits.  One block per (kMark tokens, head).
 template <typename T>
 __global__ void __launch_bounds__(256) delta_bwd_gate_kernel(FinishArgs x)
 {
-    tc::grid_dep_wait();
-    __shared__ double part[8];
+    __shared__ double part[8], first;
     const Packed& pk = x.p;
-    const int h = blockIdx.x % pk.H, s = blockIdx.x / pk.H, tid = threadIdx.x, lane = tid & 31;
-    int lo, hi;
-    seq_rows(x.cu, s, pk.T, lo, hi);
-    const float* dG = x.dG + (size_t)h * pk.T;
-    double behind = 0.;
-    for (int end = hi; end > lo; end -= 256) {
-        const int t = end - 1 - tid;
-        double v = t >= lo ? (double)dG[t] : 0.;
-#pragma unroll
-        for (int m = 1; m < 32; m *= 2) {
-            const double o = __shfl_up_sync(0xffffffffu, v, m);
-            if (lane >= m) v += o;
+    const int h = blockIdx.x % pk.H, tid = threadIdx.x, lane = tid & 31;
+    int s, block, lo, hi;
+    if (!find_block(x.cu, pk.n, pk.T, kMark, (int)(blockIdx.x / pk.H), s, block, lo, hi)) return;
+    const int t0 = lo + block * kMark, t1 = min(t0 + kMark, hi), t = t1 - 1 - tid;
+    tc::grid_dep_wait();
+    double v = t >= t0 ? (double)x.dG[(size_t)h * pk.T + t] : 0.;
+    double dot = 0.;
+    if (t1 < hi) {
+        const float *S = x.Sm + mark(pk, t1, h), *D = x.Dm + mark(pk, t1, h);
+        for (int i = 4 * tid; i < pk.d * pk.d; i += 4 * 256) {
+            const float4 a = load4(S + i), b = load4(D + i);
+            dot += (double)(a.x * b.x + a.y * b.y + (a.z * b.z + a.w * b.w));
         }
-        if (lane == 31) part[tid >> 5] = v;
-        __syncthreads();
-        double before = behind;
-        for (int w = 0; w < (tid >> 5); ++w) before += part[w];
-        for (int w = 0; w < 8; ++w) behind += part[w];
-        if (t >= lo) from_f32(((T*)x.dg)[(size_t)t * pk.H + h], (float)(before + v));
-        __syncthreads();
     }
+#pragma unroll
+    for (int m = 16; m; m /= 2) dot += __shfl_xor_sync(0xffffffffu, dot, m);
+#pragma unroll
+    for (int m = 1; m < 32; m *= 2) {
+        const double o = __shfl_up_sync(0xffffffffu, v, m);
+        if (lane >= m) v += o;
+    }
+    if (lane == 0) part[tid >> 5] = dot;
+    if (tid == 31) first = v;
+    __syncthreads();
+    if (t < t0) return;
+    dot = tid >= 32 ? first : 0.;
+    for (int w = 0; w < 8; ++w) dot += part[w];
+    from_f32(((T*)x.dg)[(size_t)t * pk.H + h], (float)(dot + v));
 }
 
 // One token of a sequence: block (i, h) holds the state S [D][D] in registers, a float4 of
@@ -608,8 +636,9 @@ cudaError_t bwd(const ScanArgs& x, const FinishArgs& f, cudaStream_t s)
         e = tc::launch_after(delta_bwd_finish_kernel<T, D>, dim3((unsigned)((items + 3) / 4)), 128, 0,
                              0, true, s, f);
     if (e == cudaSuccess)
-        e = tc::launch_after(delta_bwd_gate_kernel<T>, dim3((unsigned)(p.n * p.H)), 256, 0, 0, true,
-                             s, f);
+        e = tc::launch_after(delta_bwd_gate_kernel<T>,
+                             dim3((unsigned)((long long)block_slots(p.T, p.n, kMark) * p.H)), 256, 0, 0,
+                             true, s, f);
     return e;
 }
 
@@ -625,8 +654,12 @@ cudaError_t decode(const ScanArgs& x, cudaStream_t s)
 }  // namespace
 
 size_t delta_scan_save_floats(const Packed& p) { return (size_t)p.T * p.H * p.d; }
-// du, dq, r, w per head, and dG
-size_t delta_scan_ws_floats(const Packed& p) { return 4 * delta_scan_save_floats(p) + (size_t)p.T * p.H; }
+static size_t mark_floats(const Packed& p) { return (size_t)(p.T / kMark) * p.H * p.d * p.d; }
+// du, dq, r, w per head, S and D at the marks, and dG
+size_t delta_scan_ws_floats(const Packed& p)
+{
+    return 4 * delta_scan_save_floats(p) + 2 * mark_floats(p) + (size_t)p.T * p.H;
+}
 
 cudaError_t launch_delta_scan_fwd(const Packed& p, const void* q, const void* k, const void* v,
                                   const void* g, const void* beta, const int* cu, float scale,
@@ -651,12 +684,14 @@ cudaError_t launch_delta_scan_bwd(const Packed& p, const void* q, const void* k,
     x.q = q; x.k = k; x.g = g; x.beta = beta; x.dout = dout;
     x.cu = cu; x.scale = scale; x.e = const_cast<float*>(e);
     x.du = scratch; x.dqh = scratch + n; x.rh = scratch + 2 * n; x.wh = scratch + 3 * n;
+    x.Sm = scratch + 4 * n; x.Dm = x.Sm + mark_floats(p);
     FinishArgs f = {};
     f.p = p;
     f.q = q; f.k = k; f.beta = beta; f.cu = cu;
     f.e = e; f.du = x.du; f.dqh = x.dqh; f.rh = x.rh; f.wh = x.wh;
     f.dq = dq; f.dk = dk; f.dv = dv; f.dbeta = dbeta; f.dg = dg;
-    f.dG = scratch + 4 * n;
+    f.Sm = x.Sm; f.Dm = x.Dm;
+    f.dG = x.Dm + mark_floats(p);
     if (p.bf16) return p.d == 64 ? bwd<__nv_bfloat16, 64>(x, f, s) : bwd<__nv_bfloat16, 128>(x, f, s);
     return p.d == 64 ? bwd<float, 64>(x, f, s) : bwd<float, 128>(x, f, s);
 }

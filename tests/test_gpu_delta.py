@@ -332,3 +332,15 @@ def test_launch_counts(dtype, lens, fwd, bwd):
                           torch.zeros(k, 2, 64, 64, device="cuda"))
     n.append(flexattn.kernel_launches())
     assert [b - a for a, b in zip(n, n[1:])] == [fwd, bwd, 1]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_gate_gradients_of_long_sequences_stay_exact(d):
+    """dg is a sum over the tokens that follow, whose terms nearly cancel.  At most 64 of them are
+    added to an exact <D, S>, each three products with a rounding each: sqrt(64) * 3 * 2^-24 =
+    1.5e-6 of the terms, which are of dg's own size, whatever the length."""
+    lens, H, Hk = (1500, 64, 65, 600), 2, 1
+    x = delta_inputs(lens, H, Hk, d, F32, seed=21)
+    got = _bwd(x, offsets(lens))[3].double()
+    ref = delta_grads(x, lens, d ** -0.5)[3]
+    assert float((got - ref).norm() / ref.norm()) <= 1.5e-6
