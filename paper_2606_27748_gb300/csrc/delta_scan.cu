@@ -10,11 +10,12 @@
 // two halves of one grid.  Sums over a line are a few shuffles; sums over lines never occur.
 //
 // A column's next step needs the sum of its last one, so what bounds a scan is one warp's chain of
-// product (90 cycles of 360 a token), shuffles (130) and update, and how many warps share a
+// product (90 cycles a token), shuffles (130) and update, and how many warps share a
 // scheduler and the shared memory meanwhile.  Measured, H4 d64: forward, 1000 tokens, with 8 lanes
-// to a line 181 us, with 4 208; reverse, 4 x 1000, with 4 lanes 142, with 8 156; 8 tokens at once with
-// their mutual products (a triangular system), 4 lanes 222 us (890 instructions a warp for 8
-// tokens), 16 lanes 255 (bound by shared-memory reads).
+// to a line 181 us, with 4 208 (blocks of 32 lines; 137 in blocks of 16, see narrow()); reverse,
+// 4 x 1000, with 4 lanes 142, with 8 156; 8 tokens at once with their mutual products (a triangular
+// system), 4 lanes 222 us (890 instructions a warp for 8 tokens), 16 lanes 255 (bound by
+// shared-memory reads).
 #include "flex_internal.h"
 #include "packed.cuh"
 #include "tc_util.cuh"
@@ -22,7 +23,7 @@
 namespace flex {
 namespace {
 
-constexpr int kLines = 32;  // lines of a block
+constexpr int kNarrow = 16, kWide = 32;  // lines of a block (see narrow())
 constexpr int kMark = 64;   // tokens between two marks of a sequence (see delta_bwd_gate_kernel)
 
 template <int D>
@@ -114,10 +115,10 @@ template <int P>
 __device__ __forceinline__ int element(int i, int p) { return 4 * (P * (i / 4) + p) + i % 4; }
 
 // The tile of tokens that a column scan works on: k, q and the lines' values (v, or dout).
-template <int D>
+template <int D, int L>
 struct ColTile {
     float k[Cfg<D>::COL][D], q[Cfg<D>::COL][D];
-    float line[Cfg<D>::COL][kLines];
+    float line[Cfg<D>::COL][L];
     float a[Cfg<D>::COL], beta[Cfg<D>::COL];
 };
 
@@ -125,12 +126,12 @@ struct ColTile {
 // tile's loads are in flight behind the current one's work, and nothing is computed from them before
 // that is done (an exponential of the gates ahead of it cost 50 of 480 cycles a token).  Steps are
 // unrolled, and leave for the next one the sums that nothing waits for.
-template <typename T, int D, int P, bool REV, typename Step>
-__device__ __forceinline__ void col_scan(ColTile<D>* tiles, const T* k, long long ks, const T* q,
+template <typename T, int D, int L, int P, bool REV, typename Step>
+__device__ __forceinline__ void col_scan(ColTile<D, L>* tiles, const T* k, long long ks, const T* q,
                                          long long qs, const T* line, long long ls, const T* g,
                                          const T* beta, int H, int lo, int hi, Step step)
 {
-    constexpr int TT = Cfg<D>::COL, NT = kLines * P, LP = TT * kLines / NT, V4 = TT * D / 4 / NT;
+    constexpr int TT = Cfg<D>::COL, NT = L * P, LP = TT * L / NT, V4 = TT * D / 4 / NT;
     const int tid = threadIdx.x, nt = (hi - lo + TT - 1) / TT;
     float4 kr[V4], qr[V4];
     float lr[LP], ar = 0.f, br = 0.f;
@@ -145,8 +146,8 @@ __device__ __forceinline__ void col_scan(ColTile<D>* tiles, const T* k, long lon
         }
 #pragma unroll
         for (int i = 0; i < LP; ++i) {
-            const int e = tid + NT * i, t = t0 + e / kLines;
-            lr[i] = t >= lo && t < hi ? to_f32(line[t * ls + e % kLines]) : 0.f;
+            const int e = tid + NT * i, t = t0 + e / L;
+            lr[i] = t >= lo && t < hi ? to_f32(line[t * ls + e % L]) : 0.f;
         }
         if (tid < TT) {
             const int t = t0 + tid;
@@ -155,7 +156,7 @@ __device__ __forceinline__ void col_scan(ColTile<D>* tiles, const T* k, long lon
             br = in ? to_f32(beta[(size_t)t * H]) : 0.f;
         }
     };
-    auto put = [&](ColTile<D>& s) {
+    auto put = [&](ColTile<D, L>& s) {
 #pragma unroll
         for (int i = 0; i < V4; ++i) {
             *(float4*)(&s.k[0][0] + 4 * (tid + NT * i)) = kr[i];
@@ -176,7 +177,7 @@ __device__ __forceinline__ void col_scan(ColTile<D>* tiles, const T* k, long lon
     for (int i = 0; i < nt; ++i) {
         const int t0 = start(i);
         if (i + 1 < nt) load(start(i + 1));
-        const ColTile<D>& s = tiles[i & 1];
+        const ColTile<D, L>& s = tiles[i & 1];
         if (REV) {
             if (t0 >= lo) {
 #pragma unroll 4
@@ -198,10 +199,10 @@ __device__ __forceinline__ void col_scan(ColTile<D>* tiles, const T* k, long lon
 }
 
 // The tile of tokens that a row scan works on: u = beta e, dv = beta du, scale dout; k and q.
-template <int D>
+template <int D, int L>
 struct RowTile {
     float vec[3][Cfg<D>::ROW][D];
-    float k[Cfg<D>::ROW][kLines], q[Cfg<D>::ROW][kLines];
+    float k[Cfg<D>::ROW][L], q[Cfg<D>::ROW][L];
     float a[Cfg<D>::ROW];
 };
 
@@ -225,24 +226,24 @@ __device__ __forceinline__ size_t mark(const Packed& p, int t, int h)
 }
 
 // Which line block, head and sequence this block works on (line blocks of a head side by side).
-template <int D>
+template <int D, int L>
 __device__ __forceinline__ void place(const Packed& p, int b, int& line0, int& h, int& s)
 {
-    constexpr int LB = D / kLines;
-    line0 = (b % LB) * kLines;
+    constexpr int LB = D / L;
+    line0 = (b % LB) * L;
     h = (b / LB) % p.H;
     s = b / LB / p.H;
 }
 
 // Forward by columns.  e (NULL or [T][H][d] fp32) receives v - a S^T k.
-template <typename T, int D>
-__global__ void __launch_bounds__(kLines * Cfg<D>::PF) delta_fwd_kernel(ScanArgs x)
+template <typename T, int D, int L>
+__global__ void __launch_bounds__(L * Cfg<D>::PF, L == kNarrow) delta_fwd_kernel(ScanArgs x)
 {
     constexpr int P = Cfg<D>::PF;
-    __shared__ ColTile<D> tiles[2];
+    __shared__ ColTile<D, L> tiles[2];
     const Packed& pk = x.p;
     int col0, h, s, lo, hi;
-    place<D>(pk, blockIdx.x, col0, h, s);
+    place<D, L>(pk, blockIdx.x, col0, h, s);
     seq_rows(x.cu, s, pk.T, lo, hi);
     const int tid = threadIdx.x, p = tid % P, cl = tid / P, col = col0 + cl;
     const int H = pk.H, hk = h / (H / pk.Hk);
@@ -258,9 +259,9 @@ __global__ void __launch_bounds__(kLines * Cfg<D>::PF) delta_fwd_kernel(ScanArgs
     float* e_out = x.e ? x.e + h * D + col : nullptr;
     float o = 0.f;
     bool any = false;
-    col_scan<T, D, P, false>(tiles, (const T*)x.k + hk * D, pk.ks, (const T*)x.q + hk * D, pk.qs,
+    col_scan<T, D, L, P, false>(tiles, (const T*)x.k + hk * D, pk.ks, (const T*)x.q + hk * D, pk.qs,
                              (const T*)x.v + h * D + col0, pk.vs, (const T*)x.g + h,
-                             (const T*)x.beta + h, H, lo, hi, [&](const ColTile<D>& w, int j, int t) {
+                             (const T*)x.beta + h, H, lo, hi, [&](const ColTile<D, L>& w, int j, int t) {
         Vec<D, P> k, q;
         k.read(w.k[j], p);
         q.read(w.q[j], p);
@@ -292,23 +293,23 @@ __global__ void __launch_bounds__(kLines * Cfg<D>::PF) delta_fwd_kernel(ScanArgs
 }
 
 // Backward, first scan: columns of D in reverse; du_t = D_t^T k_t, D <- a (D - k dv^T).
-template <typename T, int D>
-__global__ void __launch_bounds__(kLines * Cfg<D>::PB) delta_bwd_cols_kernel(ScanArgs x)
+template <typename T, int D, int L>
+__global__ void __launch_bounds__(L * Cfg<D>::PB, L == kNarrow) delta_bwd_cols_kernel(ScanArgs x)
 {
     constexpr int P = Cfg<D>::PB;
-    __shared__ ColTile<D> tiles[2];
+    __shared__ ColTile<D, L> tiles[2];
     const Packed& pk = x.p;
     int col0, h, s, lo, hi;
-    place<D>(pk, blockIdx.x, col0, h, s);
+    place<D, L>(pk, blockIdx.x, col0, h, s);
     seq_rows(x.cu, s, pk.T, lo, hi);
     const int tid = threadIdx.x, p = tid % P, cl = tid / P;
     const int H = pk.H, hk = h / (H / pk.Hk);
     const long long os = (long long)H * D;
     Vec<D, P> S = {};
     float* du_out = x.du + h * D + col0 + cl;
-    col_scan<T, D, P, true>(tiles, (const T*)x.k + hk * D, pk.ks, (const T*)x.q + hk * D, pk.qs,
+    col_scan<T, D, L, P, true>(tiles, (const T*)x.k + hk * D, pk.ks, (const T*)x.q + hk * D, pk.qs,
                             (const T*)x.dout + h * D + col0, os, (const T*)x.g + h,
-                            (const T*)x.beta + h, H, lo, hi, [&](const ColTile<D>& w, int j, int t) {
+                            (const T*)x.beta + h, H, lo, hi, [&](const ColTile<D, L>& w, int j, int t) {
         Vec<D, P> k, q;
         k.read(w.k[j], p);
         q.read(w.q[j], p);
@@ -323,18 +324,18 @@ __global__ void __launch_bounds__(kLines * Cfg<D>::PB) delta_bwd_cols_kernel(Sca
 
 // Backward, the row scans: even blocks rows of S forward (dq = scale S dout, r = a S_{t-1} dv),
 // odd blocks rows of D in reverse (w = D u, u = beta e).  By tokens; sums of 8 tokens at once.
-template <typename T, int D>
-__global__ void __launch_bounds__(kLines * Cfg<D>::PR) delta_bwd_rows_kernel(ScanArgs x)
+template <typename T, int D, int L>
+__global__ void __launch_bounds__(L * Cfg<D>::PR, L == kNarrow) delta_bwd_rows_kernel(ScanArgs x)
 {
-    constexpr int TT = Cfg<D>::ROW, NT = kLines * Cfg<D>::PR, P = Cfg<D>::PR;
+    constexpr int TT = Cfg<D>::ROW, NT = L * Cfg<D>::PR, P = Cfg<D>::PR;
     constexpr int SLOTS = TT * D / 4;                            // 16-byte pieces of a vector: 256
-    constexpr int LV = (3 * SLOTS + NT - 1) / NT, LL = TT * kLines / NT ? TT * kLines / NT : 1;
-    __shared__ RowTile<D> tiles[2];
+    constexpr int LV = (3 * SLOTS + NT - 1) / NT, LL = TT * L / NT ? TT * L / NT : 1;
+    __shared__ RowTile<D, L> tiles[2];
     tc::grid_dep_wait();  // du
     const Packed& pk = x.p;
     const bool rev = blockIdx.x & 1;
     int row0, h, s, lo, hi;
-    place<D>(pk, blockIdx.x / 2, row0, h, s);
+    place<D, L>(pk, blockIdx.x / 2, row0, h, s);
     seq_rows(x.cu, s, pk.T, lo, hi);
     const int tid = threadIdx.x, p = tid % P, rl = tid / P, nt = (hi - lo + TT - 1) / TT;
     const int H = pk.H, hk = h / (H / pk.Hk);
@@ -366,14 +367,14 @@ __global__ void __launch_bounds__(kLines * Cfg<D>::PR) delta_bwd_rows_kernel(Sca
         }
 #pragma unroll
         for (int i = 0; i < LL; ++i) {
-            const int e = tid + NT * i, t = t0 + e / kLines;
-            const bool in = e < TT * kLines && t >= lo && t < hi;
-            kr[i] = in ? to_f32(k[t * pk.ks + e % kLines]) : 0.f;
-            qr[i] = in ? to_f32(q[t * pk.qs + e % kLines]) : 0.f;
+            const int e = tid + NT * i, t = t0 + e / L;
+            const bool in = e < TT * L && t >= lo && t < hi;
+            kr[i] = in ? to_f32(k[t * pk.ks + e % L]) : 0.f;
+            qr[i] = in ? to_f32(q[t * pk.qs + e % L]) : 0.f;
         }
         if (tid < TT) ar = t0 + tid >= lo && t0 + tid < hi ? to_f32(g[(size_t)(t0 + tid) * H]) : 0.f;
     };
-    auto put = [&](RowTile<D>& w) {
+    auto put = [&](RowTile<D, L>& w) {
 #pragma unroll
         for (int i = 0; i < LV; ++i) {
             const int slot = tid + NT * i;
@@ -384,7 +385,7 @@ __global__ void __launch_bounds__(kLines * Cfg<D>::PR) delta_bwd_rows_kernel(Sca
 #pragma unroll
         for (int i = 0; i < LL; ++i) {
             const int e = tid + NT * i;
-            if (e < TT * kLines) {
+            if (e < TT * L) {
                 (&w.k[0][0])[e] = kr[i];
                 (&w.q[0][0])[e] = qr[i];
             }
@@ -398,7 +399,7 @@ __global__ void __launch_bounds__(kLines * Cfg<D>::PR) delta_bwd_rows_kernel(Sca
     __syncthreads();
     const size_t out = (size_t)h * D + row0 + rl;
     for (int i = 0; i < nt; ++i) {
-        const RowTile<D>& w = tiles[i & 1];
+        const RowTile<D, L>& w = tiles[i & 1];
         if (i + 1 < nt) load(start(i + 1));
 #pragma unroll 1
         for (int jj = 0; jj < TT; jj += 8) {
@@ -612,25 +613,44 @@ __global__ void __launch_bounds__(NT) delta_decode_kernel(ScanArgs x)
                            x.scale * fmaf(kq, u.z, a * sq.z), x.scale * fmaf(kq, u.w, a * sq.w)));
 }
 
+// Blocks of L lines.  16 of them where even so every block has an SM to itself (fewer warps there
+// to share its schedulers and shared memory, and registers for as many loads as a thread then has
+// in flight), else 32 (half the staging).  Measured, 16 against 32 lines, sequences of 500 tokens, us:
+// d64 forward 78 and 103 (128 blocks of 16 lines), 144 and 140 (512), 447 and 427 (2048); columns and
+// rows backward 127 and 161 (64, 128), 479 and 425 (512, 1024); d128 forward 103 and 162 (128), backward
+// 183 and 272 (32, 64), 423 and 398 (256, 512).
 template <int D>
-long long scan_blocks(const Packed& p) { return (long long)p.n * p.H * (D / kLines); }
+bool narrow(const Packed& p, int sides)
+{
+    return (long long)p.n * p.H * (D / kNarrow) * sides <= tc::sm_count();
+}
+
+template <int D, int L, typename Kernel>
+cudaError_t scan(Kernel kernel, int P, int sides, bool after, const ScanArgs& x, cudaStream_t s)
+{
+    const long long blocks = (long long)x.p.n * x.p.H * (D / L) * sides;
+    return tc::launch_after(kernel, dim3((unsigned)blocks), L * P, 0, 0, after, s, x);
+}
 
 template <typename T, int D>
 cudaError_t fwd(const ScanArgs& x, cudaStream_t s)
 {
-    return tc::launch_after(delta_fwd_kernel<T, D>, dim3((unsigned)scan_blocks<D>(x.p)), kLines * Cfg<D>::PF, 0,
-                            0, false, s, x);
+    using C = Cfg<D>;
+    return narrow<D>(x.p, 1) ? scan<D, kNarrow>(delta_fwd_kernel<T, D, kNarrow>, C::PF, 1, false, x, s)
+                             : scan<D, kWide>(delta_fwd_kernel<T, D, kWide>, C::PF, 1, false, x, s);
 }
 
 template <typename T, int D>
 cudaError_t bwd(const ScanArgs& x, const FinishArgs& f, cudaStream_t s)
 {
+    using C = Cfg<D>;
     const Packed& p = x.p;
-    const unsigned blocks = (unsigned)scan_blocks<D>(p);
-    cudaError_t e = tc::launch_after(delta_bwd_cols_kernel<T, D>, dim3(blocks), kLines * Cfg<D>::PB, 0, 0,
-                                     false, s, x);
+    cudaError_t e = narrow<D>(p, 1)
+        ? scan<D, kNarrow>(delta_bwd_cols_kernel<T, D, kNarrow>, C::PB, 1, false, x, s)
+        : scan<D, kWide>(delta_bwd_cols_kernel<T, D, kWide>, C::PB, 1, false, x, s);
     if (e == cudaSuccess)
-        e = tc::launch_after(delta_bwd_rows_kernel<T, D>, dim3(2 * blocks), kLines * Cfg<D>::PR, 0, 0, true, s, x);
+        e = narrow<D>(p, 2) ? scan<D, kNarrow>(delta_bwd_rows_kernel<T, D, kNarrow>, C::PR, 2, true, x, s)
+                            : scan<D, kWide>(delta_bwd_rows_kernel<T, D, kWide>, C::PR, 2, true, x, s);
     const long long items = (long long)p.T * p.Hk;
     if (e == cudaSuccess)
         e = tc::launch_after(delta_bwd_finish_kernel<T, D>, dim3((unsigned)((items + 3) / 4)), 128, 0,

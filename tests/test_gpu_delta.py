@@ -344,3 +344,20 @@ def test_gate_gradients_of_long_sequences_stay_exact(d):
     got = _bwd(x, offsets(lens))[3].double()
     ref = delta_grads(x, lens, d ** -0.5)[3]
     assert float((got - ref).norm() / ref.norm()) <= 1.5e-6
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_scans_of_few_and_of_many_sequences_agree(d):
+    """Blocks are narrower where few sequences leave SMs idle; no sum depends on it."""
+    lens, H, Hk = (70,) * 20, 4, 2
+    x, cu = delta_inputs(lens, H, Hk, d, F32, seed=22), offsets(lens)
+    out, last = _fwd(x, cu)
+    ro, rs = delta_ref(x, lens, d ** -0.5)
+    check(out, ro, "out")
+    check(last, rs, "last state", F32)
+    got = _bwd(x, cu)
+    for name, y, r in zip(NAMES, got, delta_grads(x, lens, d ** -0.5)):
+        check(y, r, "d" + name)
+    one = {n: t[:70] for n, t in x.items()}
+    for a, b in zip((*_fwd(one, cu[:2]), *_bwd(one, cu[:2])), (out, last, *got)):
+        assert torch.equal(a, b[:len(a)])
