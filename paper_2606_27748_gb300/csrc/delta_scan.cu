@@ -453,7 +453,7 @@ __global__ void __launch_bounds__(L * Cfg<D>::PR, L == kNarrow) delta_bwd_rows_k
 
 struct FinishArgs {
     Packed p;
-    const void *q, *k, *beta;
+    const void *q, *k, *g, *beta;
     const int* cu;
     const float *e, *du, *dqh, *rh, *wh;
     void *dq, *dk, *dv, *dbeta, *dg;
@@ -462,8 +462,8 @@ struct FinishArgs {
 };
 
 // Row by row: dq and dk summed over the heads of a key head, dv = beta du, dbeta = e . du, and
-// the gradient of the summed log decay, dG = q.dq - k.r - k.w (q_t and the reading k_t come with
-// exp(+G_t), the writing k_t with exp(-G_t)).  One warp per (row, key head), D / 32 elements a lane.
+// dG = q.dq - k.r - k.w, by which dg falls from a token to the next (q_t and the reading k_t come
+// with exp(+G_t), the writing k_t with exp(-G_t), G_t the sum of the log decays).  One warp per (row, key head), D / 32 elements a lane.
 template <typename T, int D>
 __global__ void __launch_bounds__(128) delta_bwd_finish_kernel(FinishArgs x)
 {
@@ -510,25 +510,27 @@ __global__ void __launch_bounds__(128) delta_bwd_finish_kernel(FinishArgs x)
     }
 }
 
-// dg_t = the sum of dG from t to the end of t's sequence = <D, S> between t - 1 and t.  The terms
-// nearly cancel over a long sequence: summed to its end, roundings of the scans made dg 2.1e-6 wrong
-// (2-norm, 1000 tokens, H4 d64) and worse with the length.  So the row scans leave S and D at marks
-// kMark tokens apart (8 MB of 4 x 1000 tokens), <D, S> is taken there, and only the terms up to the
-// next mark are added, in 64 bits.  One block per (kMark tokens, head).
+// dg_t = a_t <S_{t-1}, D_t - k_t dv_t^T> falls by dG_t from t to t + 1.  As a sum of dG over a whole
+// sequence its terms nearly cancel (1000 tokens, H4 d64: dg 2.1e-6 wrong in the 2-norm, and worse
+// with the length).  So the row scans leave S and D at marks kMark tokens apart (8 MB of 4 x 1000
+// tokens), dg at a mark is <D, S>, and only the terms since then are subtracted, in 64 bits.  At a
+// sequence's first token the state ahead is 0, and at a token with a_t = 0 nothing of it is left:
+// dg is 0 there, not what two equal sums leave to rounding, and the terms are counted from there.
+// One block per (kMark tokens, head).
 template <typename T>
 __global__ void __launch_bounds__(256) delta_bwd_gate_kernel(FinishArgs x)
 {
-    __shared__ double part[8], first;
+    __shared__ double part[8], before[kMark], half;  // before: the terms from the mark up to a token
+    __shared__ int half_from;
     const Packed& pk = x.p;
     const int h = blockIdx.x % pk.H, tid = threadIdx.x, lane = tid & 31;
     int s, block, lo, hi;
     if (!find_block(x.cu, pk.n, pk.T, kMark, (int)(blockIdx.x / pk.H), s, block, lo, hi)) return;
-    const int t0 = lo + block * kMark, t1 = min(t0 + kMark, hi), t = t1 - 1 - tid;
+    const int t0 = lo + block * kMark, n = min(kMark, hi - t0), t = t0 + tid;
     tc::grid_dep_wait();
-    double v = t >= t0 ? (double)x.dG[(size_t)h * pk.T + t] : 0.;
     double dot = 0.;
-    if (t1 < hi) {
-        const float *S = x.Sm + mark(pk, t1, h), *D = x.Dm + mark(pk, t1, h);
+    if (t0 > lo) {
+        const float *S = x.Sm + mark(pk, t0, h), *D = x.Dm + mark(pk, t0, h);
         for (int i = 4 * tid; i < pk.d * pk.d; i += 4 * 256) {
             const float4 a = load4(S + i), b = load4(D + i);
             dot += (double)(a.x * b.x + a.y * b.y + (a.z * b.z + a.w * b.w));
@@ -536,18 +538,33 @@ __global__ void __launch_bounds__(256) delta_bwd_gate_kernel(FinishArgs x)
     }
 #pragma unroll
     for (int m = 16; m; m /= 2) dot += __shfl_xor_sync(0xffffffffu, dot, m);
+    // sums of the terms up to t, and the last token up to t whose gate is 0 (-1: none since the mark)
+    double sum = tid < n ? (double)x.dG[(size_t)h * pk.T + t] : 0.;
+    int from = tid < n && expf(to_f32(((const T*)x.g)[(size_t)t * pk.H + h])) == 0.f ? tid : -1;
 #pragma unroll
     for (int m = 1; m < 32; m *= 2) {
-        const double o = __shfl_up_sync(0xffffffffu, v, m);
-        if (lane >= m) v += o;
+        const double o = __shfl_up_sync(0xffffffffu, sum, m);
+        const int f = __shfl_up_sync(0xffffffffu, from, m);
+        if (lane >= m) {
+            sum += o;
+            from = max(from, f);
+        }
     }
     if (lane == 0) part[tid >> 5] = dot;
-    if (tid == 31) first = v;
+    if (tid == 31) {
+        half = sum;
+        half_from = from;
+    }
+    const double up = __shfl_up_sync(0xffffffffu, sum, 1);
     __syncthreads();
-    if (t < t0) return;
-    dot = tid >= 32 ? first : 0.;
+    if (tid < kMark) before[tid] = (lane ? up : 0.) + (tid >= 32 ? half : 0.);
+    __syncthreads();
+    if (tid >= n) return;
+    if (tid >= 32) from = max(from, half_from);
+    dot = 0.;
     for (int w = 0; w < 8; ++w) dot += part[w];
-    from_f32(((T*)x.dg)[(size_t)t * pk.H + h], (float)(dot + v));
+    const double first = from >= 0 ? before[from] : dot;
+    from_f32(((T*)x.dg)[(size_t)t * pk.H + h], (float)(first - before[tid]));
 }
 
 // One token of a sequence: block (i, h) holds the state S [D][D] in registers, a float4 of
@@ -707,7 +724,7 @@ cudaError_t launch_delta_scan_bwd(const Packed& p, const void* q, const void* k,
     x.Sm = scratch + 4 * n; x.Dm = x.Sm + mark_floats(p);
     FinishArgs f = {};
     f.p = p;
-    f.q = q; f.k = k; f.beta = beta; f.cu = cu;
+    f.q = q; f.k = k; f.g = g; f.beta = beta; f.cu = cu;
     f.e = e; f.du = x.du; f.dqh = x.dqh; f.rh = x.rh; f.wh = x.wh;
     f.dq = dq; f.dk = dk; f.dv = dv; f.dbeta = dbeta; f.dg = dg;
     f.Sm = x.Sm; f.Dm = x.Dm;

@@ -361,3 +361,31 @@ def test_scans_of_few_and_of_many_sequences_agree(d):
     one = {n: t[:70] for n, t in x.items()}
     for a, b in zip((*_fwd(one, cu[:2]), *_bwd(one, cu[:2])), (out, last, *got)):
         assert torch.equal(a, b[:len(a)])
+
+
+@pytest.mark.parametrize("dtype,lens", [(F32, (1,)), (F32, (1, 1, 0, 1, 1)), (F32, (1, 130, 2, 64, 65)),
+                                        (BF16, (1,)), (BF16, (1, 1, 0, 1, 1)), (BF16, (1, 2, 4, 1))], ids=str)
+@pytest.mark.parametrize("d", [64, 128])
+def test_the_gate_of_a_first_token_has_no_gradient(d, dtype, lens):
+    """dg_t = a_t <S_{t-1}, ..>: ahead of a sequence's first token the state is 0, so dg is 0."""
+    x = delta_inputs(lens, 3, 1, d, dtype, seed=23)
+    dg = _bwd(x, offsets(lens))[3]
+    at = torch.tensor([0, *torch.tensor(lens).cumsum(0).tolist()])[:-1][torch.tensor(lens) > 0]
+    assert (dg[at.cuda()] == 0).all()
+    if sum(lens) > len(lens):
+        check(dg, delta_grads(x, lens, d ** -0.5)[3], "dg")
+
+
+@pytest.mark.parametrize("dtype,lens", [(F32, (200, 5, 64)), (BF16, (6, 4, 3))], ids=str)
+@pytest.mark.parametrize("every", [1, 3, 70])
+@pytest.mark.parametrize("d", [64, 128])
+def test_the_gate_of_a_reset_has_no_gradient(d, every, dtype, lens):
+    """A gate of -inf: a_t = 0, and with it dg_t.  The others' dg: in fp32 the bound of
+    test_gate_gradients_of_long_sequences_stay_exact, in bf16 its storage's."""
+    x = delta_inputs(lens, 2, 1, d, dtype, seed=24)
+    x["g"][::every] = float("-inf")
+    dg = _bwd(x, offsets(lens))[3]
+    assert (dg[::every] == 0).all()
+    if every > 1:
+        ref = delta_grads(x, lens, d ** -0.5)[3]
+        assert rel(dg, ref) <= (1.5e-6 if dtype == F32 else tol(BF16))
