@@ -951,6 +951,9 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                 if (!ok) break;
                 mma4(B::T_X, B::T_A, dm, 2048, I_CM, 0);
                 wmma_commit(&e_full);
+                // The first chunk's increment is used by nobody, and nobody would wait for it: the
+                // block would free its tensor memory with products on their way into it.
+                if (r + 1 == chunks) break;
 #pragma unroll
                 for (int p = 0; p < W::PIECES; ++p) mma4(B::T_D + 64 * p, B::T_O, dqn + 512 * p, 2048, I_D, 0);
                 wait(&u_ready, r);

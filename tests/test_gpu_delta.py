@@ -389,3 +389,20 @@ def test_the_gate_of_a_reset_has_no_gradient(d, every, dtype, lens):
     if every > 1:
         ref = delta_grads(x, lens, d ** -0.5)[3]
         assert rel(dg, ref) <= (1.5e-6 if dtype == F32 else tol(BF16))
+
+
+@pytest.mark.parametrize("d,n", [(64, 17), (64, 70), (128, 9), (128, 65)])
+def test_blocks_that_follow_each_other_on_an_sm(d, n):
+    """Many times as many walks as SMs, each of one or two chunks, whose blocks take over shared
+    and tensor memory from one another: every copy of a sequence has the same results."""
+    H, copies = 4, 150
+    x = delta_inputs((n,) * 4, H, 2, d, BF16, seed=25)
+    many = {m: t.repeat(copies, *([1] * (t.dim() - 1))) for m, t in x.items()}
+    cu = offsets((n,) * (4 * copies))
+    got = (*_fwd(many, cu), *_bwd(many, cu))
+    for y in got:
+        y = y.view(copies, -1)
+        assert torch.equal(y, y[:1].expand_as(y))
+    ro, rs = delta_ref(x, (n,) * 4, d ** -0.5)
+    for y, r in zip(got, (ro, rs, *delta_grads(x, (n,) * 4, d ** -0.5))):
+        check(y[:len(r)], r, "first copy", F32 if y is got[1] else BF16)
