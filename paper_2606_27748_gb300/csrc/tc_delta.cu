@@ -1278,6 +1278,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1)
             ok = false;
             break;
         }
+        fence_after_sync();  // the other warps' loads of the head before, whose columns are overwritten
         const uint32_t qk = dlow(sb + L::QK, 16), ov = dlow(sb + L::OV, 16), de = dlow(sb + L::E, 8192);
         if (warp == 0) {
 #pragma unroll

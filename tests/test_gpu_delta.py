@@ -406,3 +406,17 @@ def test_blocks_that_follow_each_other_on_an_sm(d, n):
     ro, rs = delta_ref(x, (n,) * 4, d ** -0.5)
     for y, r in zip(got, (ro, rs, *delta_grads(x, (n,) * 4, d ** -0.5))):
         check(y[:len(r)], r, "first copy", F32 if y is got[1] else BF16)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_gradients_of_many_heads_to_a_key_head(d):
+    """A block takes the heads of a key head one after the other through the same columns of tensor
+    memory: the gates' and values' gradients do not depend on which head came before."""
+    H, lens = 8, (70, 200, 5)
+    x = delta_inputs(lens, H, 1, d, BF16, seed=26)
+    cu = offsets(lens)
+    got, turned = _bwd(x, cu), _bwd({m: t.flip(1) if m not in ("q", "k") else t for m, t in x.items()}, cu)
+    for y, z in zip(got[2:], turned[2:]):
+        assert torch.equal(y, z.flip(1))
+    for name, y, r in zip(NAMES, got, delta_grads(x, lens, d ** -0.5)):
+        check(y, r, "d" + name)
