@@ -161,10 +161,11 @@ __global__ void __launch_bounds__(Lay<D, ROWS>::THREADS, ROWS == 256 ? 1 : 2)
     if (ROWS != 32) setmaxnreg_dec<L::LESS>();
     if (tmem_base_sh != tm) {
     } else if (warp == L::TMA) {
-        // ---- Q of both tiles, then K and V of every block: tile 2 i is K of block first + i,
+        // ---- Q of the tiles at work, then K and V of every block: tile 2 i is K of block first + i,
         // tile 2 i + 1 its V; tile n goes to buffer n % NB ----
-        for (int X = 0; X < (ntB > 0 ? 2 : 1); ++X) {
-            if (first == last) break;
+        for (int X = 0; X < TILES; ++X) {
+            // (an empty range's tile is waited for by nobody, and the CTA may end ahead of its copy)
+            if (X ? firstB == lastB : firstA == lastA) continue;
             wmbar_arrive_expect_tx(&bars.q_full[X], (uint32_t)(tpt * G * D * 2));
             for (int b = 0; b < D / 64; ++b)
                 wtma_load_3d(sb + L::Q + X * L::QT + b * L::QB, &tmap_q, 64 * b, hk * G,

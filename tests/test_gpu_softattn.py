@@ -262,3 +262,21 @@ def test_a_mixed_stack_on_one_packed_batch():
     o, _ = flexattn.softattn_fwd(tok, rows[:, :Hk], rows[:, Hk:], offsets((1,) * 3), offsets(lens_k))
     r, _ = softattn_ref(tok, rows[:, :Hk], rows[:, Hk:], (1,) * 3, lens_k, d ** -0.5, True)
     check(o, r, "token, second layer")
+
+
+@pytest.mark.parametrize("lens_q,lens_k", [
+    ((512, 512), (512, 512)),           # two ranges; the first one of rows 0-127 has no block
+    ((300,), (300,)), ((700, 40), (700, 900)),
+    ((256,), (1100,)), ((130, 130), (1300, 1290)),
+], ids=str)
+@pytest.mark.parametrize("H,Hk,d", [(2, 2, 64), (2, 2, 128), (4, 1, 128), (4, 1, 64)])
+def test_ranges_without_keys_beside_others(lens_q, lens_k, H, Hk, d):
+    """Causal, keys split: of a block's two tiles one may have no key in a range.  Many calls one
+    behind the other, whose blocks take over shared memory from one another, agree."""
+    q, k, v = _inputs(lens_q, lens_k, H, Hk, d, BF16, seed=17)
+    ws = flexattn.softattn_workspace(q, k, offsets(lens_q))
+    out, lse = _check(q, k, v, lens_q, lens_k, True, ws=ws)
+    cu, cu_k = offsets(lens_q), offsets(lens_k)
+    for o, z in [flexattn.softattn_fwd(q, k, v, cu, cu_k, ws=ws) for _ in range(20)]:
+        assert torch.equal(o, out) and torch.equal(z, lse)
+    flexattn.check_status(ws)
