@@ -521,7 +521,8 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                 mma4(W::T_X, W::T_UL, dp, 32, I_C, 1);
                 mma4(W::T_X, W::T_UH, dpl, 32, I_C, 1);
                 wmma_commit(&o_full);
-                wmma_commit(&empty[c % W::ST]);
+                // (only where a later load waits for it: no arrival may be on its way when the block ends)
+                if (c + W::ST < chunks) wmma_commit(&empty[c % W::ST]);
             }
         }
     } else {
@@ -963,7 +964,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                     mma4(B::T_D + 64 * p, B::T_R, dkn + 512 * p, 2048, I_D, 1);
                     wmma_commit(&s_full[p]);
                 }
-                wmma_commit(&empty[r % B::ST]);
+                if (r + B::ST < chunks) wmma_commit(&empty[r % B::ST]);  // (see the forward's)
             }
         }
     } else {

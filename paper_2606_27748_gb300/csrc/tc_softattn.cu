@@ -197,7 +197,11 @@ __global__ void __launch_bounds__(Lay<D, ROWS>::THREADS, ROWS == 256 ? 1 : 2)
         // K of block j is tile 2 (j - first), its V the next
         auto buffer = [&](int n) { return sb + L::KV + (uint32_t)(n % L::NB) * L::TILE; };
         auto landed = [&](int n) { return wait(&bars.full[n % L::NB], n / L::NB); };
-        auto release = [&](int n) { wmma_commit(&bars.empty[n % L::NB]); };
+        // (only where a later load waits for it: no arrival may be on its way when the CTA ends)
+        auto again = [&](int n) { return n + L::NB < 2 * (last - first); };
+        auto release = [&](int n) {
+            if (again(n)) wmma_commit(&bars.empty[n % L::NB]);
+        };
         auto scores = [&](int X, int j) {  // S = Q K_j^T
             const int n = 2 * (j - first);
             if (L::OWN_P && (!landed(n) || (j > f[X] && !wait(&bars.s_loaded[X], j - 1 - f[X])))) return;
@@ -234,7 +238,7 @@ __global__ void __launch_bounds__(Lay<D, ROWS>::THREADS, ROWS == 256 ? 1 : 2)
             const int X = warp - L::MMA;
             auto pass = [&](int j) {  // a block of the other tile's only
                 for (int n = 2 * (j - first); n < 2 * (j - first) + 2; ++n)
-                    if (landed(n) && lane == 0) mbar_arrive(&bars.empty[n % L::NB]);
+                    if (landed(n) && again(n) && lane == 0) mbar_arrive(&bars.empty[n % L::NB]);
             };
             auto both = [&](int j, bool k, bool v) {  // the scores of block j + 1, then block j's O
                 if (k) {
