@@ -365,10 +365,14 @@ def _packed_attn(q, k, v, n, dev):
 
 
 def _new(stream, shape, dtype, device):
-    """A result's tensor, of the current stream; used on `stream` too."""
-    t = torch.empty(shape, dtype=dtype, device=device)
-    if stream is not None:
-        t.record_stream(stream)
+    """A result's tensor.  With `stream` it is of that stream's memory, since what the current
+    stream's pool hands out may still be at work there, and is held until the current stream,
+    which is to use it, is done with it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream())
     return t
 
 

@@ -420,3 +420,36 @@ def test_gradients_of_many_heads_to_a_key_head(d):
         assert torch.equal(y, z.flip(1))
     for name, y, r in zip(NAMES, got, delta_grads(x, lens, d ** -0.5)):
         check(y, r, "d" + name)
+
+
+def _held_busy(shapes):
+    """Blocks of these shapes that the allocator hands out again at once, which the current stream
+    only comes to overwrite after some 20 ms of products."""
+    a = torch.randn(8192, 8192, device="cuda")
+    blocks = [torch.empty(s, dtype=t, device="cuda") for s, t in shapes for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(2):
+        a = a @ a
+    for t in blocks:
+        t.fill_(float("nan"))
+
+
+def test_results_on_a_stream_of_their_own_share_no_block_with_pending_work():
+    lens, H, Hk, d = (300, 77), 4, 2, 64
+    x, cu = delta_inputs(lens, H, Hk, d, BF16, seed=27), offsets(lens)
+    T, side = sum(lens), torch.cuda.Stream()
+    out, last = _fwd(x, cu)
+    grads = _bwd(x, cu)
+    save = flexattn.delta_save(x["q"], x["v"], cu)
+    S = torch.zeros(2, H, d, d, device="cuda")
+    tok = [x[n][:2].contiguous() for n in NAMES]
+    one = flexattn.delta_decode(*tok, S.clone())
+    torch.cuda.synchronize()
+    _held_busy([((T, H, d), BF16), ((T, Hk, d), BF16), ((T, H), BF16), ((2, H, d), BF16),
+                ((2, H, d, d), F32)])
+    got = [*_fwd(x, cu, save=save, stream=side)]
+    got += flexattn.delta_bwd(*(x[n] for n in NAMES), cu, x["dout"], save, stream=side)
+    got.append(flexattn.delta_decode(*tok, S, stream=side))
+    torch.cuda.current_stream().wait_stream(side)
+    for y, want in zip(got, (out, last, *grads, one)):
+        assert torch.equal(y, want)

@@ -280,3 +280,22 @@ def test_ranges_without_keys_beside_others(lens_q, lens_k, H, Hk, d):
     for o, z in [flexattn.softattn_fwd(q, k, v, cu, cu_k, ws=ws) for _ in range(20)]:
         assert torch.equal(o, out) and torch.equal(z, lse)
     flexattn.check_status(ws)
+
+
+def test_results_on_a_stream_of_their_own_share_no_block_with_pending_work():
+    """Blocks of the results' sizes are free again, but the current stream has yet to write them."""
+    lens, H, Hk, d = (300, 77), 4, 2, 64
+    q, k, v = _inputs(lens, lens, H, Hk, d, BF16, seed=18)
+    cu, side = offsets(lens), torch.cuda.Stream()
+    want = flexattn.softattn_fwd(q, k, v, cu)
+    a = torch.randn(8192, 8192, device="cuda")
+    blocks = [torch.empty_like(t) for t in want for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(2):
+        a = a @ a
+    for t in blocks:
+        t.fill_(float("nan"))
+    del blocks, t
+    got = flexattn.softattn_fwd(q, k, v, cu, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])

@@ -147,3 +147,31 @@ def test_binding_refuses_what_is_not_on_the_gpu_or_does_not_fit():
         flexattn._rank3(torch.zeros(3, 4), "q")
     with pytest.raises(TypeError):
         flexattn._dtype_code(torch.zeros(3, dtype=torch.float16))
+
+
+def test_results_on_another_stream_come_from_its_own_memory(monkeypatch):
+    """With `stream=`, a result's block comes from that stream's pool (another's block may still be
+    at work there) and is marked as used on the caller's stream."""
+    import contextlib
+    inside, marked = [], []
+
+    class Tensor:
+        def __init__(self):
+            self.of = inside[-1] if inside else "current"
+
+        def record_stream(self, s):
+            marked.append(s)
+
+    @contextlib.contextmanager
+    def stream(s):
+        inside.append(s)
+        yield
+        inside.pop()
+
+    monkeypatch.setattr(torch.cuda, "stream", stream)
+    monkeypatch.setattr(torch.cuda, "current_stream",
+                        lambda device=None: inside[-1] if inside else "current")
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: Tensor())
+    t = flexattn._new("side", (3,), torch.float32, "cuda")
+    assert t.of == "side" and marked == ["current"]
+    assert flexattn._new(None, (3,), torch.float32, "cuda").of == "current" and len(marked) == 1
