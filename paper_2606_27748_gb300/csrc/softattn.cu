@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(kThreads) softattn_simt_kernel(AttnArgs x)
         for (int w = 1; w < 16; w *= 2) l[i] += __shfl_xor_sync(0xffffffffu, l[i], w);
         const int r = 4 * ty + i;
         if (r >= nt * G) continue;
-        const float inv = l[i] > 0.f ? 1.f / l[i] : 0.f;
+        const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];  // (no key seen; a NaN sum goes on)
         const size_t row = (size_t)(qlo + t0 + r / G) * pk.H + hk * G + r % G;
         if (tx == 0) {
             const float z = m[i] + logf(l[i]);
@@ -172,8 +172,9 @@ __global__ void __launch_bounds__(kThreads) softattn_simt_kernel(AttnArgs x)
 }
 
 // Joins the ranges of every row: out = sum_s exp(lse_s - lse) out_s, lse = log sum_s exp(lse_s),
-// ranges in order.  A warp per row; a range that saw no key (lse -inf) has weight 0.  Bound by
-// the partial results' bytes (in L2: splitting is for few rows).
+// ranges in order.  A warp per row; a range that saw no key (lse -inf) has weight 0, one that met a
+// NaN (lse NaN) makes the sum NaN.  Bound by the partial results' bytes (in L2: splitting is for few
+// rows).
 template <typename T>
 __global__ void __launch_bounds__(128) softattn_join_kernel(AttnArgs x)
 {
@@ -193,7 +194,7 @@ __global__ void __launch_bounds__(128) softattn_join_kernel(AttnArgs x)
     float total = weight;
 #pragma unroll
     for (int w = 1; w < 32; w *= 2) total += __shfl_xor_sync(0xffffffffu, total, w);
-    const float inv = total > 0.f ? 1.f / total : 0.f;
+    const float inv = total == 0.f ? 0.f : 1.f / total;
     const int c = 4 * lane;
     float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
     const float* part = x.part + row * pk.d + min(c, pk.d - 4);
@@ -205,7 +206,7 @@ __global__ void __launch_bounds__(128) softattn_join_kernel(AttnArgs x)
         y.z = fmaf(w, v.z, y.z); y.w = fmaf(w, v.w, y.w);
     }
     if (c < pk.d) store4((T*)x.out + row * pk.d + c, y);
-    if (lane == 0 && x.lse) x.lse[row] = top == -INFINITY ? -INFINITY : top + logf(total);
+    if (lane == 0 && x.lse) x.lse[row] = total == 0.f ? -INFINITY : top + logf(total);
 }
 
 template <typename T, int D>

@@ -383,9 +383,10 @@ __global__ void __launch_bounds__(Lay<D, ROWS>::THREADS, ROWS == 256 ? 1 : 2)
         fence_after_sync();
         const size_t rows = (size_t)pk.T * pk.H;
         const size_t row = (size_t)(qlo + tok) * pk.H + hk * G + r % G;
-        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const bool none = l == 0.f;  // no key seen (a NaN or infinite score leaves a sum of NaN, and goes on)
+        const float inv = 1.f / l;
         if (ok && mine) {
-            const float z = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+            const float z = none ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
             if (x.splits > 1)
                 x.part_lse[split * rows + row] = z;
             else if (x.lse)
@@ -400,7 +401,7 @@ __global__ void __launch_bounds__(Lay<D, ROWS>::THREADS, ROWS == 256 ? 1 : 2)
                     tmem_wait_ld();
                 }
 #pragma unroll
-                for (int e = 0; e < 32; ++e) o[e] = l > 0.f ? o[e] * inv : 0.f;
+                for (int e = 0; e < 32; ++e) o[e] = none ? 0.f : o[e] * inv;
                 if (!mine) continue;
                 if (x.splits > 1) {
                     float4* dst = (float4*)(x.part + (split * rows + row) * D + 32 * i);

@@ -299,3 +299,35 @@ def test_results_on_a_stream_of_their_own_share_no_block_with_pending_work():
     got = flexattn.softattn_fwd(q, k, v, cu, stream=side)
     torch.cuda.current_stream().wait_stream(side)
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("lens_q,lens_k", [((150, 300), (150, 300)),   # one range of keys
+                                           ((700,), (700,)),           # two, on the tensor cores
+                                           ((1, 1), (3000, 200))],     # single tokens, many
+                         ids=str)
+@pytest.mark.parametrize("what", ["q", "k", "inf"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_nan_and_infinite_scores_reach_the_rows_that_see_them(lens_q, lens_k, what, d, dtype):
+    """A NaN in a row of q makes that row NaN, one in a key (or a score of +inf) every row that sees
+    the key; all other rows are what they are without it."""
+    H, Hk, G = 4, 2, 2
+    q, k, v = _inputs(lens_q, lens_k, H, Hk, d, dtype, seed=19)
+    q[:, :, 0] = q[:, :, 0].abs() + 0.5
+    clean, rz = softattn_ref(q, k, v, lens_q, lens_k, d ** -0.5, True)
+    cu, cu_k = offsets(lens_q), offsets(lens_k)
+    nq, nk = lens_q[0], lens_k[0]
+    for at in (0, nk // 2, nk - 1):
+        hit = torch.zeros(sum(lens_q), H, dtype=torch.bool, device="cuda")
+        x, y = q.clone(), k.clone()
+        if what == "q":
+            x[at % nq, 1, 5] = float("nan")
+            hit[at % nq, 1] = True
+        else:
+            y[at, 1, 0] = float("nan") if what == "k" else float("inf")
+            sees = torch.arange(nq, device="cuda") + nk - nq >= at
+            hit[:nq, G:] = sees[:, None]
+        out, lse = flexattn.softattn_fwd(x, y, v, cu, cu_k)
+        assert torch.isnan(out[hit]).all() and torch.isnan(lse[hit]).all()
+        check(out[~hit], clean[~hit], "out")
+        check(lse[~hit], rz[~hit], "lse")
