@@ -178,7 +178,8 @@ __global__ void __launch_bounds__(128)
         for (int i = 0; i < 2; ++i) {
             const int j = 2 * lane + i;
             const size_t at = (size_t)(t0 + j) * pk.H + h;
-            a[i] = j < n ? fmaxf(__bfloat162float(g[at]), kLeastGate) * kLog2e : 0.f;
+            const float gate = j < n ? __bfloat162float(g[at]) : 0.f;
+            a[i] = (gate < kLeastGate ? kLeastGate : gate) * kLog2e;  // (NaN stays)
             Bs[j] = j < n ? __bfloat162float(beta[at]) : 0.f;
         }
         float sum = a[0] + a[1];

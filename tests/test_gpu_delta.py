@@ -453,3 +453,37 @@ def test_results_on_a_stream_of_their_own_share_no_block_with_pending_work():
     torch.cuda.current_stream().wait_stream(side)
     for y, want in zip(got, (out, last, *grads, one)):
         assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("what", ["g", "beta", "k", "v"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_nan_inside_a_sequence_goes_on_to_its_end_and_nowhere_else(d, what, dtype):
+    """A NaN of one head (of one key head: k) at one token: that sequence's rows from there on are
+    NaN, the chunks of 64 tokens before it, the other heads and the other sequences what they were."""
+    lens, H, Hk, at = (300, 70), 4, 2, 150
+    x, cu = delta_inputs(lens, H, Hk, d, dtype, seed=28), offsets(lens)
+    ro, rs = delta_ref(x, lens, d ** -0.5)
+    ref = delta_grads(x, lens, d ** -0.5)
+    if what in ("g", "beta"):
+        x[what][at, 3] = float("nan")
+    else:
+        x[what][at, 1 if what == "k" else 3] = float("nan")
+    out, last = _fwd(x, cu)
+    grads = _bwd(x, cu)
+    heads = [2, 3] if what == "k" else [3]
+    clean = [h for h in range(H) if h not in heads]
+    assert torch.isnan(out[at:300, heads]).all() and torch.isnan(last[0, heads]).all()
+    before = at if dtype == F32 else at // 64 * 64
+    check(out[:before], ro[:before], "out ahead")
+    check(out[300:], ro[300:], "next sequence")
+    check(out[:, clean], ro[:, clean], "other heads")
+    check(last[1], rs[1], "next state", F32)
+    check(last[:, clean], rs[:, clean], "other states", F32)
+    for name, y, r in zip(NAMES, grads, ref):
+        check(y[300:], r[300:], "d" + name)
+        same = [0] if name in ("q", "k") else clean
+        check(y[:, same], r[:, same], "d" + name)
+    assert torch.isnan(grads[0][at + 1:300, 1]).all()  # dq_t = scale S_t dout_t
+    if what != "v":  # dv_t = beta_t D_t^T k_t, and D depends on everything but v
+        assert torch.isnan(grads[2][:at, heads]).all()
