@@ -276,6 +276,9 @@ int flex_delta_fwd(const flex_packed* shape, const void* q, const void* k, const
  *   D_t += scale q_t dout_t^T;  dq_t = scale S_t dout_t;  dv_t = beta_t D_t^T k_t;
  *   dbeta_t = e_t . D_t^T k_t;  dk_t = beta_t D_t e_t - a_t S_{t-1} dv_t;
  *   dg_t = a_t <S_{t-1}, D_t - k_t dv_t^T>;  D_{t-1} = a_t (D_t - k_t dv_t^T).
+ * dg_t is exactly 0 where a_t S_{t-1} is: at first tokens and at resets (a gate below -103, in
+ * chunks of -88 or less).  Elsewhere its error is one of the terms q.dq and k.dk that it is summed
+ * from, of which a strong decay leaves little.
  * Every sum has a fixed order: results repeat bit for bit.  2 kernels (4 token by token). */
 int flex_delta_bwd(const flex_packed* shape, const void* q, const void* k, const void* v,
                    const void* g, const void* beta, const int* cu, float scale,

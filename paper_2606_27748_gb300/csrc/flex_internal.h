@@ -150,10 +150,10 @@ cudaError_t launch_tc_delta_fwd(const Packed& p, const void* q, const void* k, c
                                 const void* g, const void* beta, const int* cu, float scale,
                                 const float* S0, float* S1, void* out, void* rec, bool saving,
                                 int* status, cudaStream_t s);
-cudaError_t launch_tc_delta_bwd(const Packed& p, const void* q, const void* k, const int* cu,
-                                float scale, const void* dout, const void* save, void* dq, void* dk,
-                                void* dv, void* dg, void* dbeta, void* scratch, int* status,
-                                cudaStream_t s);
+cudaError_t launch_tc_delta_bwd(const Packed& p, const void* q, const void* k, const void* g,
+                                const int* cu, float scale, const void* dout, const void* save,
+                                void* dq, void* dk, void* dv, void* dg, void* dbeta, void* scratch,
+                                int* status, cudaStream_t s);
 
 int softattn_splits(const Packed& p);  // ranges of keys per tile of rows (1-32)
 cudaError_t launch_softattn_simt(const AttnArgs& x, cudaStream_t s);

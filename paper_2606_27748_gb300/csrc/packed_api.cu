@@ -137,7 +137,7 @@ int flex_delta_bwd(const flex_packed* shape, const void* q, const void* k, const
     if (!save || !aligned(save, 256)) return FLEX_EINVAL;
     if ((rc = check_ws(ws, ws_bytes, delta_ws_bytes(p, true)))) return rc;
     if (flex::tc_delta_supported(p))
-        return counted(2, flex::launch_tc_delta_bwd(p, q, k, cu, scale, dout, save, dq, dk, dv, dg,
+        return counted(2, flex::launch_tc_delta_bwd(p, q, k, g, cu, scale, dout, save, dq, dk, dv, dg,
                                                     dbeta, (char*)ws + kHeader,
                                                     &((flex::WsHeader*)ws)->status,
                                                     (cudaStream_t)stream));

@@ -1190,6 +1190,7 @@ struct GradArgs {
     float scale;
     const uint8_t* rec;
     const float* db;
+    const __nv_bfloat16* g;
     __nv_bfloat16 *dq, *dk, *dg, *dbeta;
     int* status;
 };
@@ -1496,7 +1497,8 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1)
 #pragma unroll
             for (int y = 0; y < D / 32; ++y) db += part[64 * y];
             const size_t at = (size_t)(t0 + tid) * pk.H + h;
-            x.dg[at] = __float2bfloat16_rn(g);
+            // (a reset, a_t = 0: the sums leave their rounding where dg is 0)
+            x.dg[at] = __float2bfloat16_rn(__bfloat162float(x.g[at]) <= kLeastGate ? 0.f : g);
             x.dbeta[at] = __float2bfloat16_rn(db);
         }
         __syncthreads();
@@ -1648,10 +1650,10 @@ cudaError_t launch_tc_delta_fwd(const Packed& p, const void* q, const void* k, c
                      : fwd<128>(p, q, k, v, g, beta, x, (uint8_t*)rec, s);
 }
 
-cudaError_t launch_tc_delta_bwd(const Packed& p, const void* q, const void* k, const int* cu,
-                                float scale, const void* dout, const void* save, void* dq, void* dk,
-                                void* dv, void* dg, void* dbeta, void* scratch, int* status,
-                                cudaStream_t s)
+cudaError_t launch_tc_delta_bwd(const Packed& p, const void* q, const void* k, const void* g,
+                                const int* cu, float scale, const void* dout, const void* save,
+                                void* dq, void* dk, void* dv, void* dg, void* dbeta, void* scratch,
+                                int* status, cudaStream_t s)
 {
     const SaveParts at = save_parts(p);
     const char* base = (const char*)save;
@@ -1665,6 +1667,7 @@ cudaError_t launch_tc_delta_bwd(const Packed& p, const void* q, const void* k, c
     GradArgs y = {};
     y.p = p;
     y.cu = cu; y.scale = scale; y.rec = (const uint8_t*)save; y.db = x.db;
+    y.g = (const __nv_bfloat16*)g;
     y.dq = (__nv_bfloat16*)dq; y.dk = (__nv_bfloat16*)dk; y.dg = (__nv_bfloat16*)dg;
     y.dbeta = (__nv_bfloat16*)dbeta; y.status = status;
     return p.d == 64 ? back<64>(p, q, k, dout, base + at.e, base + at.s, x, y, s)

@@ -376,7 +376,7 @@ def test_the_gate_of_a_first_token_has_no_gradient(d, dtype, lens):
         check(dg, delta_grads(x, lens, d ** -0.5)[3], "dg")
 
 
-@pytest.mark.parametrize("dtype,lens", [(F32, (200, 5, 64)), (BF16, (6, 4, 3))], ids=str)
+@pytest.mark.parametrize("dtype,lens", [(F32, (200, 5, 64)), (BF16, (6, 4, 3)), (BF16, (200, 65))], ids=str)
 @pytest.mark.parametrize("every", [1, 3, 70])
 @pytest.mark.parametrize("d", [64, 128])
 def test_the_gate_of_a_reset_has_no_gradient(d, every, dtype, lens):
