@@ -32,14 +32,17 @@ namespace {
 using namespace tc;
 
 constexpr int kC = 64;             // tokens of a chunk
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr double kLog2e = 1.4426950408889634;
 // A log decay of -88 is exp(-88) = 6e-39, no factor in fp32 sums; -inf is taken as that, since
-// the differences of the sums G have to be finite.
+// the differences of the sums G have to be finite.  A chunk's G may so reach -8000 (powers of two),
+// where fp32 knows a difference to 2^-12 only and with it the decay between two tokens behind a few
+// resets: 32 of them, then slow decays, made the last state 1e-4 wrong.  So G is summed in 64 bits
+// and kept as a high and a low float.
 constexpr float kLeastGate = -88.f;
 
 // What the walk needs of a chunk, as it is copied to shared memory: M's low and high parts and
-// P's high and low ones // (64 x 64 bf16, 128-byte rows, swizzled), then -e^G, e^{G_C - G}, beta (0 behind the
-// sequence's end), G in powers of two (64 floats each) and e^{G_C}.
+// P's high and low ones (64 x 64 bf16, 128-byte rows, swizzled), then -e^G, e^{G_C - G}, beta (0
+// behind the sequence's end), G's high part in powers of two (64 floats each) and e^{G_C}.
 struct Rec {
     static constexpr uint32_t M_LO = 0, M_HI = 8192, P = 16384, P_LO = 24576, AUX = 32768, BYTES = 34048;
     static constexpr uint32_t GAMMA = AUX, KAPPA = AUX + 256, BETA = AUX + 512, G = AUX + 768, LAST = AUX + 1024;
@@ -144,7 +147,7 @@ __global__ void __launch_bounds__(128)
     __shared__ uint64_t bar_load, bar_mma;
     __shared__ uint32_t tmem_base_sh;
     __shared__ volatile int abort_flag;
-    __shared__ __align__(16) float Gs[64], Bs[64];
+    __shared__ __align__(16) float Gs[64], Gl[64], Bs[64];  // G, high and low; beta
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, h = blockIdx.y;
     int s, chunk, lo, hi;
@@ -173,25 +176,29 @@ __global__ void __launch_bounds__(128)
         }
     }
     if (warp == 1) {  // sums of the gates, two tokens a lane
-        float a[2];
+        double a[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int j = 2 * lane + i;
             const size_t at = (size_t)(t0 + j) * pk.H + h;
             const float gate = j < n ? __bfloat162float(g[at]) : 0.f;
-            a[i] = (gate < kLeastGate ? kLeastGate : gate) * kLog2e;  // (NaN stays)
+            a[i] = (double)(gate < kLeastGate ? kLeastGate : gate) * kLog2e;  // (NaN stays)
             Bs[j] = j < n ? __bfloat162float(beta[at]) : 0.f;
         }
-        float sum = a[0] + a[1];
+        double sum = a[0] + a[1];
 #pragma unroll
         for (int m = 1; m < 32; m *= 2) {
-            const float o = __shfl_up_sync(0xffffffffu, sum, m);
+            const double o = __shfl_up_sync(0xffffffffu, sum, m);
             if (lane >= m) sum += o;
         }
-        float before = __shfl_up_sync(0xffffffffu, sum, 1);
-        if (lane == 0) before = 0.f;
-        Gs[2 * lane] = before + a[0];
-        Gs[2 * lane + 1] = sum;
+        double before = __shfl_up_sync(0xffffffffu, sum, 1);
+        if (lane == 0) before = 0.;
+        const double G[2] = {before + a[0], sum};
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            Gs[2 * lane + i] = (float)G[i];
+            Gl[2 * lane + i] = (float)(G[i] - (double)(float)G[i]);
+        }
     }
     if (warp == 0) {
         ok = bar_wait_w(&bar_load, 0, &abort_flag, status);
@@ -228,18 +235,35 @@ __global__ void __launch_bounds__(128)
         }
         tmem_wait_ld();
         const float G = Gs[row];
+        const uint64_t G2 = f2_pack(G, G), Gl2 = f2_pack(Gl[row], Gl[row]), one = f2_pack(1.f, 1.f);
+        const uint64_t minus = f2_pack(-1.f, -1.f);
+        // (G down to -32 is known to 2^-20, and the low part would change a decay by 1e-6 at most)
+        const bool far = !(Gs[63] >= -32.f);
+        auto decays = [&](int j, float (&y)[4]) {  // of this row against columns j .. j + 3
+            const ulonglong2 h = *(const ulonglong2*)&Gs[j];
+            uint64_t a = f2_fma(h.x, minus, G2), b = f2_fma(h.y, minus, G2);
+            if (far) {
+                const ulonglong2 l = *(const ulonglong2*)&Gl[j];
+                a = f2_fma(f2_fma(l.x, minus, Gl2), one, a);
+                b = f2_fma(f2_fma(l.y, minus, Gl2), one, b);
+            }
+            f2_unpack(a, y[0], y[1]);
+            f2_unpack(b, y[2], y[3]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = ex2(y[e]);
+        };
         const int cols = 32 + 32 * (warp & 1);  // columns up to the diagonal of this warp's rows
         const bool in = row < n;
         if (tid < 64) {  // L, rows behind the end zero (and with them columns: beta is 0 there)
 #pragma unroll
             for (int j = 0; j < 64; j += 4) {
                 if (j >= cols) break;
-                const float4 gj = *(const float4*)&Gs[j];
-                const float y[4] = {gj.x, gj.y, gj.z, gj.w};
+                float y[4];
+                decays(j, y);
                 float4 x;
                 float* z = &x.x;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) z[e] = j + e < row && in ? v[j + e] * ex2(G - y[e]) : 0.f;
+                for (int e = 0; e < 4; ++e) z[e] = j + e < row && in ? v[j + e] * y[e] : 0.f;
                 *(float4*)&w.L[row][j] = x;
             }
         } else {
@@ -247,12 +271,12 @@ __global__ void __launch_bounds__(128)
             for (int j = 0; j < 64; j += 8) {
                 uint4 out = make_uint4(0, 0, 0, 0), out_lo = out;
                 if (j < cols) {
-                    const float4 g0 = *(const float4*)&Gs[j], g1 = *(const float4*)&Gs[j + 4];
-                    const float y[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
-                    float p[8];
+                    float y[2][4], p[8];
+                    decays(j, y[0]);
+                    decays(j + 4, y[1]);
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        p[e] = j + e <= row && in ? scale * v[j + e] * ex2(G - y[e]) : 0.f;
+                        p[e] = j + e <= row && in ? scale * v[j + e] * y[e / 4][e % 4] : 0.f;
                     split(p[0], p[1], out.x, out_lo.x);
                     split(p[2], p[3], out.y, out_lo.y);
                     split(p[4], p[5], out.z, out_lo.z);
@@ -264,7 +288,7 @@ __global__ void __launch_bounds__(128)
             const float last = Gs[63];
             float* aux = (float*)rec;
             aux[Rec::GAMMA / 4 + row] = -ex2(G);
-            aux[Rec::KAPPA / 4 + row] = in ? ex2(last - G) : 0.f;
+            aux[Rec::KAPPA / 4 + row] = in ? ex2((last - G) + (Gl[63] - Gl[row])) : 0.f;
             aux[Rec::BETA / 4 + row] = Bs[row];
             aux[Rec::G / 4 + row] = G;
             if (row == 0) aux[Rec::LAST / 4] = ex2(last);
@@ -1323,6 +1347,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1)
             // Z: row i = kd % 64 of Zq (quadrants 0, 1) or Zk, columns 32 half + 0 .. 31
             const int i = kd & 63;
             const bool key = quad >= 2;
+            // (G without its low part leaves a decay off by 3.4e-4 at most; Z is rounded by up to 2^-8)
             const float Gi = aux[192 + i], f = key ? -1.f : x.scale;
             const int jmax = (i < n ? (key ? i : i + 1) : 0) - 32 * half;  // columns below it count
             const uint32_t dst = sb + (key ? L::ZK : L::ZQ);

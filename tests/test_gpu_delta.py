@@ -487,3 +487,23 @@ def test_a_nan_inside_a_sequence_goes_on_to_its_end_and_nowhere_else(d, what, dt
     assert torch.isnan(grads[0][at + 1:300, 1]).all()  # dq_t = scale S_t dout_t
     if what != "v":  # dv_t = beta_t D_t^T k_t, and D depends on everything but v
         assert torch.isnan(grads[2][:at, heads]).all()
+
+
+@pytest.mark.parametrize("gate,many", [(float("-inf"), 1), (float("-inf"), 8), (float("-inf"), 32),
+                                       (float("-inf"), 56), (-20.0, 40), (-3.0, 40)], ids=str)
+@pytest.mark.parametrize("d", [64, 128])
+def test_tokens_behind_resets_are_as_accurate_as_others(d, gate, many):
+    """Resets or strong decays at a chunk's start, then slow decays: what follows them is held to
+    the bounds of any other sequence, forward and backward."""
+    lens, H, Hk = (64, 130), 4, 2
+    x, cu = delta_inputs(lens, H, Hk, d, BF16, seed=29), offsets(lens)
+    at = torch.arange(194, device="cuda")
+    at = torch.where(at < 64, at, at - 64) % 64
+    x["g"] = torch.where((at < many)[:, None], gate, x["g"].clamp(-0.1, -0.01)).to(BF16)
+    out, last = _fwd(x, cu)
+    ro, rs = delta_ref(x, lens, d ** -0.5)
+    for i, (a, b) in enumerate(((0, 64), (64, 194))):
+        check(out[a:b], ro[a:b], "out")
+        check(last[i], rs[i], "last state", F32)
+    for name, y, r in zip(NAMES, _bwd(x, cu), delta_grads(x, lens, d ** -0.5)):
+        check(y, r, "d" + name)
