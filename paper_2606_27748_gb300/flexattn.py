@@ -19,6 +19,7 @@ LIBRARY = os.path.join(_PKG, "libflexattn.so")
 FLEX_F32, FLEX_BF16 = 0, 1
 FLEX_OK, FLEX_EINVAL, FLEX_EUNSUPPORTED, FLEX_EWORKSPACE, FLEX_ECUDA, FLEX_ETIMEOUT = (
     0, -1, -2, -3, -4, -5)
+WS_HEADER = 256  # bytes of a workspace's control words
 
 EXPORTS = ("flex_strerror", "flex_workspace_bytes", "flex_featmap", "flex_linattn_fwd",
            "flex_linattn_bwd", "flex_decode_workspace_bytes", "flex_linattn_decode",
@@ -384,17 +385,21 @@ def _scratch(stream, make, *args, **kw):
         return make(*args, **kw)
 
 
-def _zeros(n, what, device):
+def _workspace(n, what, device):
+    """n bytes of workspace for the packed calls, which start from its header alone."""
     if n == 0:
         raise FlexError(FLEX_EUNSUPPORTED, what)
-    return torch.zeros(n, dtype=torch.uint8, device=device)
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    ws[:WS_HEADER].zero_()
+    return ws
 
 
 def delta_workspace(q, v, cu, backward=False) -> torch.Tensor:
     """A caller-owned workspace for delta_fwd (backward: for delta_bwd too) on such tensors."""
     shape = _packed_delta(q, q, v, cu.numel() - 1, torch.cuda.current_device())
-    return _zeros(int(load().flex_delta_workspace_bytes(ctypes.byref(shape), int(bool(backward)))),
-                  "flex_delta_workspace_bytes", q.device)
+    return _workspace(
+        int(load().flex_delta_workspace_bytes(ctypes.byref(shape), int(bool(backward)))),
+        "flex_delta_workspace_bytes", q.device)
 
 
 def delta_save(q, v, cu) -> torch.Tensor:
@@ -487,8 +492,8 @@ def delta_decode(q, k, v, g, beta, S, scale=None, out=None, stream=None):
 def softattn_workspace(q, k, cu_q) -> torch.Tensor:
     """A caller-owned workspace for softattn_fwd on such tensors."""
     shape = _packed_attn(q, k, k, cu_q.numel() - 1, torch.cuda.current_device())
-    return _zeros(int(load().flex_softattn_workspace_bytes(ctypes.byref(shape))),
-                  "flex_softattn_workspace_bytes", q.device)
+    return _workspace(int(load().flex_softattn_workspace_bytes(ctypes.byref(shape))),
+                      "flex_softattn_workspace_bytes", q.device)
 
 
 def softattn_fwd(q, k, v, cu_q, cu_k=None, causal=True, scale=None, out=None, lse=None,

@@ -507,3 +507,18 @@ def test_tokens_behind_resets_are_as_accurate_as_others(d, gate, many):
         check(last[i], rs[i], "last state", F32)
     for name, y, r in zip(NAMES, _bwd(x, cu), delta_grads(x, lens, d ** -0.5)):
         check(y, r, "d" + name)
+
+
+@pytest.mark.parametrize("dtype,lens", [(F32, (130, 70)), (BF16, (130, 70)), (BF16, (3, 2))], ids=str)
+def test_workspaces_start_from_their_header_alone(dtype, lens):
+    """Whatever else a workspace holds (NaN here) reaches no result."""
+    H, Hk, d = 4, 2, 64
+    x, cu = delta_inputs(lens, H, Hk, d, dtype, seed=30), offsets(lens)
+    want = (*_fwd(x, cu), *_bwd(x, cu))
+    ws = flexattn.delta_workspace(x["q"], x["v"], cu, backward=True)
+    got = []
+    for call in (lambda: _fwd(x, cu, ws=ws), lambda: _bwd(x, cu, ws=ws)):
+        ws[256:] = 0xff
+        got += call()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    flexattn.check_status(ws)

@@ -331,3 +331,18 @@ def test_nan_and_infinite_scores_reach_the_rows_that_see_them(lens_q, lens_k, wh
         assert torch.isnan(out[hit]).all() and torch.isnan(lse[hit]).all()
         check(out[~hit], clean[~hit], "out")
         check(lse[~hit], rz[~hit], "lse")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_workspaces_start_from_their_header_alone(dtype):
+    """Whatever else a workspace holds (NaN here) reaches no result of split keys."""
+    lens, lens_k = (1, 2), (3000, 900)
+    q, k, v = _inputs(lens, lens_k, 8, 2, 128, dtype, seed=20)
+    cu, cu_k = offsets(lens), offsets(lens_k)
+    want = flexattn.softattn_fwd(q, k, v, cu, cu_k)
+    ws = flexattn.softattn_workspace(q, k, cu)
+    assert ws.numel() > 256
+    ws[256:] = 0xff
+    got = flexattn.softattn_fwd(q, k, v, cu, cu_k, ws=ws)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    flexattn.check_status(ws)

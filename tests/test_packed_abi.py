@@ -175,3 +175,13 @@ def test_results_on_another_stream_come_from_its_own_memory(monkeypatch):
     t = flexattn._new("side", (3,), torch.float32, "cuda")
     assert t.of == "side" and marked == ["current"]
     assert flexattn._new(None, (3,), torch.float32, "cuda").of == "current" and len(marked) == 1
+
+
+def test_workspaces(lib, monkeypatch):
+    """Only the header is cleared."""
+    empty = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: empty(*a, **k).fill_(7))
+    ws = flexattn._workspace(1000, "", "cpu")
+    assert (ws[:256] == 0).all() and (ws[256:] == 7).all()
+    with pytest.raises(flexattn.FlexError):
+        flexattn._workspace(0, "", "cpu")
