@@ -239,7 +239,8 @@ typedef struct {
 
 /* Workspace bytes of flex_delta_fwd (backward = 0) or of both flex_delta_fwd and
  * flex_delta_bwd (backward = 1); 0 if the shape is invalid or unsupported.  Of the packed calls'
- * workspaces the first 256 bytes alone have to be zero before the first use. */
+ * workspaces the first 256 bytes alone have to be zero before the first use; flex_delta_fwd with
+ * `save` needs no more than those. */
 size_t flex_delta_workspace_bytes(const flex_packed* shape, int backward);
 
 /* Bytes of the buffer that flex_delta_fwd leaves for flex_delta_bwd (its content is the

@@ -113,7 +113,8 @@ int flex_delta_fwd(const flex_packed* shape, const void* q, const void* k, const
     if ((S0 && !aligned(S0, 16)) || (S1 && !aligned(S1, 16)) || (save && !aligned(save, 256)))
         return FLEX_EINVAL;
     if (save && S0) return FLEX_EINVAL;
-    if ((rc = check_ws(ws, ws_bytes, delta_ws_bytes(p, false)))) return rc;
+    // (with save the chunks' records go there)
+    if ((rc = check_ws(ws, ws_bytes, save ? kHeader : delta_ws_bytes(p, false)))) return rc;
     if (flex::tc_delta_supported(p))
         return counted(2, flex::launch_tc_delta_fwd(p, q, k, v, g, beta, cu, scale, S0, S1, out,
                                                     save ? save : (char*)ws + kHeader, save != nullptr,

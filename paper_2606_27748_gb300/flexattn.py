@@ -433,8 +433,10 @@ def delta_fwd(q, k, v, g, beta, cu, scale=None, state=None, out=None, want_state
         out = _new(stream, (T, H, d), dt, q.device)
     if last_state is None and want_state:
         last_state = _new(stream, st, torch.float32, q.device)
-    if ws is None:
+    if ws is None and save is None:
         ws = _scratch(stream, delta_workspace, q, v, cu)
+    elif ws is None:  # (what the kernels leave for each other goes to `save`)
+        ws = _scratch(stream, _workspace, WS_HEADER, "flex_delta_fwd", q.device)
     _check(load().flex_delta_fwd(
         ctypes.byref(shape), q.data_ptr(), k.data_ptr(), v.data_ptr(),
         _plain(g, "g", gates, dt, dev), _plain(beta, "beta", gates, dt, dev), cu_ptr,

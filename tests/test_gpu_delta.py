@@ -511,7 +511,8 @@ def test_tokens_behind_resets_are_as_accurate_as_others(d, gate, many):
 
 @pytest.mark.parametrize("dtype,lens", [(F32, (130, 70)), (BF16, (130, 70)), (BF16, (3, 2))], ids=str)
 def test_workspaces_start_from_their_header_alone(dtype, lens):
-    """Whatever else a workspace holds (NaN here) reaches no result."""
+    """Whatever else a workspace holds (NaN here) reaches no result; a forward that saves takes one of
+    256 bytes and allocates no more."""
     H, Hk, d = 4, 2, 64
     x, cu = delta_inputs(lens, H, Hk, d, dtype, seed=30), offsets(lens)
     want = (*_fwd(x, cu), *_bwd(x, cu))
@@ -522,3 +523,13 @@ def test_workspaces_start_from_their_header_alone(dtype, lens):
         got += call()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     flexattn.check_status(ws)
+    save = flexattn.delta_save(x["q"], x["v"], cu)
+    out = torch.empty_like(x["v"])
+    small = torch.zeros(256, dtype=torch.uint8, device="cuda")
+    _fwd(x, cu, save=save, out=out, want_state=False, ws=small)
+    assert torch.equal(out, want[0])
+    torch.cuda.reset_peak_memory_stats()
+    held = torch.cuda.memory_allocated()
+    _fwd(x, cu, save=save, out=out, want_state=False)
+    most = torch.cuda.max_memory_allocated()  # (the comparison allocates)
+    assert most - held <= 512 and torch.equal(out, want[0])

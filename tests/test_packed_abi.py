@@ -178,7 +178,9 @@ def test_results_on_another_stream_come_from_its_own_memory(monkeypatch):
 
 
 def test_workspaces(lib, monkeypatch):
-    """Only the header is cleared."""
+    """A forward that saves asks for the header alone; only the header is cleared."""
+    s = _shape()
+    assert _fwd(lib, s, save=P, n=255) == FLEX_EWORKSPACE
     empty = torch.empty
     monkeypatch.setattr(torch, "empty", lambda *a, **k: empty(*a, **k).fill_(7))
     ws = flexattn._workspace(1000, "", "cpu")
