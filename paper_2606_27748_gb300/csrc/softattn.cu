@@ -27,7 +27,7 @@ struct SimtSmem {
     float p[kRows][kKeys + 4];
 };
 
-template <typename T, int D>
+template <int D>
 __global__ void __launch_bounds__(kThreads) softattn_simt_kernel(AttnArgs x)
 {
     extern __shared__ __align__(16) char raw[];
@@ -48,7 +48,7 @@ __global__ void __launch_bounds__(kThreads) softattn_simt_kernel(AttnArgs x)
         const int r = e / (D / 4), c = e % (D / 4) * 4;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         if (r < nt * G)
-            v = load4((const T*)x.q + (qlo + t0 + r / G) * pk.qs + (hk * G + r % G) * D + c);
+            v = load4((const float*)x.q + (qlo + t0 + r / G) * pk.qs + (hk * G + r % G) * D + c);
         *(float4*)&sm.q[r][c] = v;
     }
     float o[4][D / 16] = {}, m[4], l[4] = {};
@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(kThreads) softattn_simt_kernel(AttnArgs x)
         see[i] = r >= nt * G ? 0 : x.causal ? min(lk, t0 + r / G + shift + 1) : lk;
     }
     float4 held[D / 16];  // this thread's part of the tile that comes next
-    auto fetch = [&](const T* base, long long stride, int j0) {
+    auto fetch = [&](const float* base, long long stride, int j0) {
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
             const int e = tid + kThreads * i, r = e / (D / 4), c = e % (D / 4) * 4;
@@ -75,13 +75,13 @@ __global__ void __launch_bounds__(kThreads) softattn_simt_kernel(AttnArgs x)
             *(float4*)&sm.kv[e / (D / 4)][e % (D / 4) * 4] = held[i];
         }
     };
-    if (first < last) fetch((const T*)x.k, pk.ks, first * kKeys);
+    if (first < last) fetch((const float*)x.k, pk.ks, first * kKeys);
     for (int b = first; b < last; ++b) {
         const int j0 = b * kKeys;
         __syncthreads();
         put();
         __syncthreads();
-        fetch((const T*)x.v, pk.vs, j0);
+        fetch((const float*)x.v, pk.vs, j0);
         float sc[4][4] = {};
 #pragma unroll 4
         for (int c = 0; c < D; c += 4) {
@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(kThreads) softattn_simt_kernel(AttnArgs x)
         __syncthreads();
         put();
         __syncthreads();
-        if (b + 1 < last) fetch((const T*)x.k, pk.ks, j0 + kKeys);
+        if (b + 1 < last) fetch((const float*)x.k, pk.ks, j0 + kKeys);
 #pragma unroll 2
         for (int j = 0; j < kKeys; j += 4) {
             float4 p[4];
@@ -166,7 +166,7 @@ __global__ void __launch_bounds__(kThreads) softattn_simt_kernel(AttnArgs x)
             if (x.splits > 1)
                 store4(x.part + ((size_t)split * pk.T * pk.H + row) * D + col, y);
             else
-                store4((T*)x.out + row * D + col, y);
+                store4((float*)x.out + row * D + col, y);
         }
     }
 }
@@ -209,15 +209,15 @@ __global__ void __launch_bounds__(128) softattn_join_kernel(AttnArgs x)
     if (lane == 0 && x.lse) x.lse[row] = total == 0.f ? -INFINITY : top + logf(total);
 }
 
-template <typename T, int D>
+template <int D>
 cudaError_t launch_simt(const AttnArgs& x, cudaStream_t s)
 {
     const Packed& p = x.p;
     const int smem = (int)sizeof(SimtSmem<D>);
-    cudaError_t e = cudaFuncSetAttribute(softattn_simt_kernel<T, D>,
+    cudaError_t e = cudaFuncSetAttribute(softattn_simt_kernel<D>,
                                          cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    return tc::launch_after(softattn_simt_kernel<T, D>, softattn_grid(x, kRows / (p.H / p.Hk)), kThreads, smem, 0, false, s, x);
+    return tc::launch_after(softattn_simt_kernel<D>, softattn_grid(x, kRows / (p.H / p.Hk)), kThreads, smem, 0, false, s, x);
 }
 
 }  // namespace
@@ -243,10 +243,7 @@ int softattn_splits(const Packed& p)
 
 cudaError_t launch_softattn_simt(const AttnArgs& x, cudaStream_t s)
 {
-    const Packed& p = x.p;
-    if (p.bf16)
-        return p.d == 64 ? launch_simt<__nv_bfloat16, 64>(x, s) : launch_simt<__nv_bfloat16, 128>(x, s);
-    return p.d == 64 ? launch_simt<float, 64>(x, s) : launch_simt<float, 128>(x, s);
+    return x.p.d == 64 ? launch_simt<64>(x, s) : launch_simt<128>(x, s);
 }
 
 cudaError_t launch_softattn_join(const AttnArgs& x, cudaStream_t s)

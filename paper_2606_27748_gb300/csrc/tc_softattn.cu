@@ -474,7 +474,7 @@ cudaError_t launch(const AttnArgs& x, cudaStream_t s)
 
 }  // namespace
 
-bool tc_softattn_supported(const Packed& p) { return p.bf16 && (p.d == 64 || p.d == 128); }
+bool tc_softattn_supported(const Packed& p) { return p.bf16; }
 
 // One or two tokens a sequence: 32 rows; else what holds an average sequence's rows.  (The lengths
 // are on the device: a long prompt among single tokens raises the average and takes large blocks.)
