@@ -102,3 +102,38 @@ def softattn_ref(q, k, v, lens_q, lens_k, scale, causal):
         lses.append(z.transpose(0, 1))
         a, b = a + nq, b + nk
     return torch.cat(outs), torch.cat(lses)
+
+
+# Bounds for one sequence by itself, whose rows would drown in a batch's norm.  Derived before the
+# first run, with roundings of random sign (2-norms over hundreds of values):
+# - ROUNDED: a result's rounding to bf16 is uniform in +- 2^-8 of its power of two, 2^-8 / sqrt(3) of
+#   its value at most;
+# - WEIGHTED: the weights of softmax attention are rounded so too, and with random v their errors add
+#   up as the output itself does: sqrt(2) of it;
+# - GRADIENT: as many roundings as a bf16 gradient's longest chain of rounded operands has (the state or
+#   its gradient, E twice, dV, Z) and its own, sqrt(6) of it, at the 1 / sqrt(2) that uniform
+#   significands leave of the bound above;
+# - SPLIT: bf16 high and low parts leave 2^-17 / sqrt(3) of an operand; three operands on the way to
+#   the state (S, beta R, U);
+# - PLAIN: fp32 sums of 128 products carry sqrt(128) 2^-24 of a typical sum; a state or an output
+#   takes 5 such errors over (see the tolerances above).
+ROUNDED = 2.0 ** -8 / 3 ** 0.5
+WEIGHTED = 2 ** 0.5 * ROUNDED
+GRADIENT = (6 / 2) ** 0.5 * ROUNDED
+SPLIT = 3 ** 0.5 * 2.0 ** -17 / 3 ** 0.5
+PLAIN = 5 * 128 ** 0.5 * 2.0 ** -24
+
+
+def check_each(x, ref, lens, bound, what):
+    """Every sequence's rows by themselves.  The bounds are for the root of a mean square; that of N
+    errors strays by 1 / sqrt(2 N) of it (the squares of a normal variable have a variance of twice
+    their mean's square, those of a rounding less), three times which is allowed: 7% for 1000 values,
+    but half for the 20 gates of 5 rows of 4 heads."""
+    assert torch.isfinite(x[:sum(lens)]).all(), f"{what}: not finite"
+    at = 0
+    for i, n in enumerate(lens):
+        if n:
+            r = rel(x[at:at + n], ref[at:at + n])
+            most = bound * (1 + 3 / (2 * ref[at:at + n].numel()) ** 0.5)
+            assert r <= most, f"{what} of sequence {i} ({n} rows): relative L2 {r:.3e} > {most:.3e}"
+        at += n

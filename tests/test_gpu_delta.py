@@ -533,3 +533,18 @@ def test_workspaces_start_from_their_header_alone(dtype, lens):
     _fwd(x, cu, save=save, out=out, want_state=False)
     most = torch.cuda.max_memory_allocated()  # (the comparison allocates)
     assert most - held <= 512 and torch.equal(out, want[0])
+
+
+@pytest.mark.parametrize("lens", [(200, 17, 128, 5), (64, 400, 63, 30)], ids=str)
+@pytest.mark.parametrize("H,Hk", [(4, 4), (8, 4)])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_every_sequence_by_itself(lens, H, Hk, d, dtype):
+    from packed_ref import GRADIENT, PLAIN, ROUNDED, SPLIT, check_each
+    x, cu = delta_inputs(lens, H, Hk, d, dtype, seed=31), offsets(lens)
+    out, last = _fwd(x, cu)
+    ro, rs = delta_ref(x, lens, d ** -0.5)
+    check_each(out, ro, lens, PLAIN if dtype == F32 else ROUNDED, "out")
+    check_each(last, rs, (1,) * len(lens), PLAIN if dtype == F32 else SPLIT, "last state")
+    for name, y, r in zip(NAMES, _bwd(x, cu), delta_grads(x, lens, d ** -0.5)):
+        check_each(y, r, lens, PLAIN if dtype == F32 else GRADIENT, "d" + name)

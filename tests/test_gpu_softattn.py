@@ -346,3 +346,21 @@ def test_workspaces_start_from_their_header_alone(dtype):
     got = flexattn.softattn_fwd(q, k, v, cu, cu_k, ws=ws)
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
     flexattn.check_status(ws)
+
+
+@pytest.mark.parametrize("lens_q,lens_k,causal", [
+    ((200, 17, 128, 5), (200, 17, 128, 5), True), ((300, 1, 64), (300, 1000, 64), True),
+    ((5, 6, 7), (20000, 130, 1), False),     # a sequence far longer than the average
+    ((1,) * 6, (4000, 3, 700, 128, 129, 1), True), ((700, 300), (3000, 900), False),
+], ids=str)
+@pytest.mark.parametrize("H,Hk", [(8, 8), (8, 2)])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_every_sequence_by_itself(lens_q, lens_k, causal, H, Hk, d, dtype):
+    from packed_ref import PLAIN, WEIGHTED, check_each
+    q, k, v = _inputs(lens_q, lens_k, H, Hk, d, dtype, seed=21)
+    out, lse = flexattn.softattn_fwd(q, k, v, offsets(lens_q), offsets(lens_k), causal=causal)
+    ro, rz = softattn_ref(q, k, v, lens_q, lens_k, d ** -0.5, causal)
+    check_each(out, ro, lens_q, PLAIN if dtype == F32 else WEIGHTED, "out")
+    # (a row of one key has lse = its score, which may be next to 0)
+    assert float((lse - rz).abs().max()) <= PLAIN * (1 + float(rz.abs().max()))
