@@ -548,3 +548,37 @@ def test_every_sequence_by_itself(lens, H, Hk, d, dtype):
     check_each(last, rs, (1,) * len(lens), PLAIN if dtype == F32 else SPLIT, "last state")
     for name, y, r in zip(NAMES, _bwd(x, cu), delta_grads(x, lens, d ** -0.5)):
         check_each(y, r, lens, PLAIN if dtype == F32 else GRADIENT, "d" + name)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_as_many_sequences_as_a_call_takes(dtype):
+    """65535 single tokens from the zero state: out = scale (q.k) beta v, the state k (beta v)^T."""
+    n, d = 65535, 64
+    x = delta_inputs((1,) * n, 2, 1, d, dtype, seed=33)
+    cu = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    out, last = _fwd(x, cu)
+    q, k, v, beta = (x[m].double() for m in ("q", "k", "v", "beta"))
+    u = beta[..., None] * v
+    check(out, d ** -0.5 * (q * k).sum(-1, keepdim=True) * u, "out")
+    for i in (0, 1, 31999, n - 1):
+        check(last[i], k[i, 0][None, :, None] * u[i][:, None, :], "state", F32)
+    dq, dk, dv, dg, db = _bwd(x, cu)
+    du = d ** -0.5 * (q * k).sum(-1, keepdim=True) * x["dout"].double()
+    check(dv, beta[..., None] * du, "dv")
+    check(db, (v * du).sum(-1), "dbeta")
+    w = d ** -0.5 * (u * x["dout"].double()).sum((1, 2))[:, None, None]
+    check(dq, w * k, "dq")
+    check(dk, w * q, "dk")
+    assert (dg == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_as_many_heads_as_a_call_takes(dtype):
+    lens, H, Hk, d = (70, 3), 1024, 16, 64
+    x, cu = delta_inputs(lens, H, Hk, d, dtype, seed=34), offsets(lens)
+    out, last = _fwd(x, cu)
+    ro, rs = delta_ref(x, lens, d ** -0.5)
+    check(out, ro, "out")
+    check(last, rs, "last state", F32)
+    for name, y, r in zip(NAMES, _bwd(x, cu), delta_grads(x, lens, d ** -0.5)):
+        check(y, r, "d" + name)

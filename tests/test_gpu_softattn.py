@@ -364,3 +364,65 @@ def test_every_sequence_by_itself(lens_q, lens_k, causal, H, Hk, d, dtype):
     check_each(out, ro, lens_q, PLAIN if dtype == F32 else WEIGHTED, "out")
     # (a row of one key has lse = its score, which may be next to 0)
     assert float((lse - rz).abs().max()) <= PLAIN * (1 + float(rz.abs().max()))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_as_many_sequences_as_a_call_takes(dtype):
+    """65535 single tokens that see one key each: its value, and its score as the log sum."""
+    n, H, Hk, d = 65535, 2, 1, 64
+    one = (1,) * n
+    q, k, v = _inputs(one, one, H, Hk, d, dtype, seed=22)
+    out, lse = flexattn.softattn_fwd(q, k, v, torch.arange(n + 1, dtype=torch.int32, device="cuda"))
+    assert torch.equal(out, v.expand(n, H, d))
+    check(lse, d ** -0.5 * (q.double() * k.double()).sum(-1), "lse")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("lens_q,lens_k", [((70, 3), (70, 300)), ((1, 1), (700, 40))], ids=str)
+def test_as_many_heads_as_a_call_takes(lens_q, lens_k, dtype):
+    _check(*_inputs(lens_q, lens_k, 1024, 16, 64, dtype, seed=23), lens_q, lens_k, True)
+
+
+def test_calls_of_both_operators_on_two_streams_at_once():
+    """Their blocks share SMs, and with them shared and tensor memory; each call's results are what
+    they are alone, also from two graphs replayed at once."""
+    lens, H, Hk, d = (300, 64, 513, 90) * 4, 4, 2, 64
+    cu = offsets(lens)
+    x = delta_inputs(lens, H, Hk, d, BF16, seed=24)
+    args = [x[n] for n in ("q", "k", "v", "g", "beta")]
+    q, k, v = _inputs(lens, lens, H, Hk, d, BF16, seed=25)
+    tok = tuple(1 for _ in lens)
+    cu1 = offsets(tok)
+    q1 = q[:len(lens)].contiguous()
+    save = flexattn.delta_save(x["q"], x["v"], cu)
+
+    def delta():
+        out, last = flexattn.delta_fwd(*args, cu, save=save)
+        return (out, last, *flexattn.delta_bwd(*args, cu, x["dout"], save))
+
+    def attention():
+        return (*flexattn.softattn_fwd(q, k, v, cu), *flexattn.softattn_fwd(q1, k, v, cu1, cu))
+
+    want = delta(), attention()
+    graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    held = []
+    torch.cuda.synchronize()
+    for g, f in zip(graphs, (delta, attention)):
+        with torch.cuda.graph(g):
+            held.append(f())
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = ([], [])
+    for _ in range(10):
+        for i, f in enumerate((delta, attention)):
+            with torch.cuda.stream(sides[i]):
+                got[i].append(f())
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for s, g in zip(sides, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    for i in range(2):
+        for y in (*got[i], held[i]):
+            assert all(torch.equal(a, b) for a, b in zip(y, want[i]))
