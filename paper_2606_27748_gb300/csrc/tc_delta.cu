@@ -19,7 +19,10 @@
 // Precision: K and Q are exact.  What multiplies them (S, beta R, U, M and P) is split into bf16 high
 // and low parts (2^-17; products of two low parts are left out), so that the state, held in fp32
 // registers, is off by 3e-6 and the output by little more than its own rounding (with P as bf16 by
-// 1.6 times it).  The backward's results are bf16, and of its operands only P is split.
+// 1.6 times it).  The backward's results are bf16 and held to 1.2 times their own rounding: of its
+// operands P, E and Zq (below) are split, which left 1.8 times it as bf16 (E and Zq 1.7e-3 each of
+// dq's 3.0e-3, dk's and dg's 3.1e-3; splitting them took 331 us to 355, 8 x 2048 H12 d64); the state
+// and its gradient of a chunk, dV and the walk's own operands, bf16 too, leave 0.6e-3 or less each.
 #include <cuda.h>
 
 #include "flex_internal.h"
@@ -387,7 +390,8 @@ struct WalkArgs {
     float* S1;
     __nv_bfloat16* out;
     const uint8_t* rec;
-    __nv_bfloat16 *e_save, *s_save;  // NULL, or E^T [slot][H][d][64] and S^T [slot][H][d][d] of each chunk
+    // NULL, or E^T [slot][H][high, low][d][64] and S^T [slot][H][d][d] of each chunk
+    __nv_bfloat16 *e_save, *s_save;
     int* status;
 };
 
@@ -719,17 +723,15 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                 }
                 ready(&p_ready);
                 if (x.e_save) {
-                    uint4* dst = (uint4*)(x.e_save + ((rec0 + (size_t)c * pk.H) * D + v) * kC + 32 * half);
+                    __nv_bfloat16* dst = x.e_save + ((rec0 + (size_t)c * pk.H) * 2 * D + v) * kC + 32 * half;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint32_t w[4];
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t w[8], y[8];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            float a, b;
-                            f2_unpack(R[4 * i + e], a, b);
-                            w[e] = pack_bf16(a, b);
-                        }
-                        dst[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                        for (int e = 0; e < 8; ++e) split2(R[8 * i + e], w[e], y[e]);
+                        store_32b(dst + 16 * i, make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7]));
+                        store_32b(dst + D * kC + 16 * i, make_uint4(y[0], y[1], y[2], y[3]),
+                                  make_uint4(y[4], y[5], y[6], y[7]));
                     }
                 }
                 if (!wait(&o_full, c)) break;
@@ -787,15 +789,17 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
 //   dU = P^T dO + e^{G_C - G} K D,  Y = dU - M^T (beta dU),  dV = beta Y,  dbeta = E . Y,
 //   D <- e^{G_C} D + Q^T (scale e^G dO) - K^T (e^G dV).
 // Held transposed like the forward's walk, with the same roles and steps.  All results are bf16,
-// so every operand is bf16 without a low part; D itself stays fp32 in registers.  D of every
-// chunk, dV and the products E . Y (summed over a quadrant's 32 value dimensions) go to memory.
+// so the products' operands but P are bf16 without a low part (see the top); D itself stays fp32 in
+// registers.  D of every chunk, dV and the products E . Y (in fp32, summed over a quadrant's 32 value
+// dimensions) go to memory.
 template <int D>
 struct Back {
     static constexpr uint32_t TILE = kC * D * 2;
     static constexpr uint32_t REC_BYTES = Rec::BYTES - Rec::M_HI;  // M's high part, P, the factors
-    static constexpr uint32_t K = 0, Q = TILE, DO = 2 * TILE, REC = 3 * TILE;
+    // (E: a value dimension a row, high parts, then low ones)
+    static constexpr uint32_t K = 0, Q = TILE, DO = 2 * TILE, E = 3 * TILE, REC = 5 * TILE;
     static constexpr uint32_t STAGE = (REC + REC_BYTES + 1023) / 1024 * 1024;
-    static constexpr int ST = D == 128 ? 3 : 4;
+    static constexpr int ST = D == 128 ? 2 : 3;
     static constexpr uint32_t SMEM = ST * STAGE + 1024;
     static constexpr uint32_t M = REC, P = REC + Rec::P - Rec::M_HI, AUX = REC + Rec::AUX - Rec::M_HI;
     // tensor memory: D; K D, then M^T (beta dU); P^T dO; beta dU; -e^G dV; scale e^G dO; increment
@@ -809,7 +813,6 @@ struct BackArgs {
     const int* cu;
     float scale;
     const uint8_t* rec;
-    const __nv_bfloat16* e;  // E^T [slot][H][d][64]
     __nv_bfloat16* ds;       // D^T [slot][H][d][d]
     float* db;               // [slot][H][4][64]
     __nv_bfloat16* dv;
@@ -865,7 +868,8 @@ template <int D>
 __global__ void __launch_bounds__(kWalkThreads, 1)
     delta_back_kernel(const __grid_constant__ CUtensorMap tmap_q,
                       const __grid_constant__ CUtensorMap tmap_k,
-                      const __grid_constant__ CUtensorMap tmap_do, BackArgs x)
+                      const __grid_constant__ CUtensorMap tmap_do,
+                      const __grid_constant__ CUtensorMap tmap_e, BackArgs x)
 {
     using W = Walk<D>;
     using B = Back<D>;
@@ -929,12 +933,13 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                     break;
                 const uint32_t st = sb + stage(r);
                 const int c = chunks - 1 - r, t = lo + c * kC;
-                wmbar_arrive_expect_tx(bar, 3 * B::TILE + B::REC_BYTES);
+                wmbar_arrive_expect_tx(bar, 5 * B::TILE + B::REC_BYTES);
                 for (int b = 0; b < D / 64; ++b) {
                     wtma_load_3d(st + B::DO + 8192 * b, &tmap_do, 64 * b, h, t, bar);
                     wtma_load_3d(st + B::K + 8192 * b, &tmap_k, 64 * b, hk, t, bar);
                     wtma_load_3d(st + B::Q + 8192 * b, &tmap_q, 64 * b, hk, t, bar);
                 }
+                wtma_load_3d(st + B::E, &tmap_e, 0, 0, (int)(rec0 + (size_t)c * pk.H), bar);
                 if (elect_one())
                     bulk_load(st + B::REC, x.rec + (rec0 + (size_t)c * pk.H) * Rec::BYTES + Rec::M_HI,
                               B::REC_BYTES, bar);
@@ -1073,12 +1078,6 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
             for (int r = 0; r < chunks; ++r) {
                 const int c = chunks - 1 - r, n = hi - lo - c * kC - 32 * half;
                 const size_t slot = rec0 + (size_t)c * pk.H;
-                uint4 ev[4];  // E of this lane's value dimension, 32 tokens
-                {
-                    const uint4* src = (const uint4*)(x.e + (slot * D + v) * kC + 32 * half);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) ev[i] = src[i];
-                }
                 if (!(ok = landed(r))) break;
                 const uint8_t* st = sm + stage(r);
                 const float* aux = (const float*)(st + B::AUX) + 32 * half;
@@ -1154,7 +1153,6 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                     tmem_st8(lanes + B::T_R + 16 * half + 8 * j, w);
                 }
                 ready(&u_ready);
-                if (lane == 0) mbar_arrive(&empty[r % B::ST]);
                 __nv_bfloat16* dst = dv + (size_t)(c * kC) * os;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
@@ -1162,15 +1160,22 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                     if (2 * i + (lane & 1) < n) *(uint32_t*)dst = y;
                     dst += 2 * os;
                 }
-                float prod[32];
+                float prod[32];  // E . Y of this lane's value dimension
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const uint32_t e = (&ev[i / 4].x)[i % 4];
-                    float a, b;
-                    f2_unpack(U[i], a, b);
-                    prod[2 * i] = a * __uint_as_float(e << 16);
-                    prod[2 * i + 1] = b * __uint_as_float(e & 0xffff0000u);
+                for (int i = 0; i < 4; ++i) {
+                    const uint4 eh = *(const uint4*)(st + B::E + swz128(v, 32 * half + 8 * i));
+                    const uint4 el = *(const uint4*)(st + B::E + D * 128 + swz128(v, 32 * half + 8 * i));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t y = (&eh.x)[e], z = (&el.x)[e];
+                        float a, b;
+                        f2_unpack(U[4 * i + e], a, b);
+                        prod[8 * i + 2 * e] = a * (__uint_as_float(y << 16) + __uint_as_float(z << 16));
+                        prod[8 * i + 2 * e + 1] = b * (__uint_as_float(y & 0xffff0000u) + __uint_as_float(z & 0xffff0000u));
+                    }
                 }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&empty[r % B::ST]);
                 x.db[(slot * 4 + (warp & 3)) * 64 + 32 * half + lane] = transpose_sum(prod);
             }
         }
@@ -1197,14 +1202,15 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
 // it; dQ^T and dK^T are products of key dimension x token, summed over the heads in registers: a
 // lane holds one key dimension (quadrant w % 4) and a warp half of the tokens (w / 4).  256 columns
 // of tensor memory, taken twice: [dO E, dV E | Q K^T, K K^T | S dO | S dV], then [Zq K | Zq^T Q +
-// (Zk + Zk^T) K | D E].  For d = 64 products have rows 64-127 that read whatever lies behind a tile
+// (Zk + Zk^T) K | D E], E and Zq as high and low parts.  For d = 64 products have rows 64-127 that read whatever lies behind a tile
 // (within shared memory) and are not looked at.
 template <int D>
 struct Grad {
     static constexpr uint32_t TILE = kC * D * 2, BLOCK = D * 128;  // 64 tokens; D rows of 64 elements
     // [Q; K] and [dO; dV]: per 64 elements, 64 rows of the one and 64 of the other
-    static constexpr uint32_t QK = 0, OV = 2 * TILE, E = 4 * TILE, S = E + BLOCK, DS = S + BLOCK * (D / 64),
-                              ZQ = DS + BLOCK * (D / 64), ZK = ZQ + 8192, END = ZK + 8192;
+    // (E and Zq: high parts, then low ones)
+    static constexpr uint32_t QK = 0, OV = 2 * TILE, E = 4 * TILE, S = E + 2 * BLOCK, DS = S + BLOCK * (D / 64),
+                              ZQ = DS + BLOCK * (D / 64), ZK = ZQ + 16384, END = ZK + 8192;
     static constexpr uint32_t SMEM = END + 1024;
 };
 
@@ -1276,7 +1282,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1)
     for (int h = hk * G; h < (hk + 1) * G; ++h) {
         const size_t slot = (size_t)blockIdx.x * pk.H + h;
         if (warp == 0) {
-            wmbar_arrive_expect_tx(&bar_load, 2 * L::TILE + L::BLOCK * (1 + 2 * (D / 64)) +
+            wmbar_arrive_expect_tx(&bar_load, 2 * L::TILE + L::BLOCK * (2 + 2 * (D / 64)) +
                                                   (h == hk * G ? 2 * L::TILE : 0));
             for (int b = 0; b < D / 64; ++b) {
                 if (h == hk * G) {
@@ -1309,8 +1315,8 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1)
         const uint32_t qk = dlow(sb + L::QK, 16), ov = dlow(sb + L::OV, 16), de = dlow(sb + L::E, 8192);
         if (warp == 0) {
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-                const uint32_t o = (k >> 2) * 16384 + (k & 3) * 32;
+            for (int k = 0; k < D / 8; ++k) {  // (E low follows E)
+                const uint32_t o = (k % (D / 16) >> 2) * 16384 + (k & 3) * 32;
                 wmma_bf16(tm, desc(ov, o), desc(de, 2048 * k), idesc_bf16(128, kC, 0, 1), k > 0);
             }
 #pragma unroll
@@ -1355,7 +1361,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1)
             float row = 0.f;
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-                uint32_t w[8] = {};
+                uint32_t w[8] = {}, wl[8] = {};
                 float col = 0.f;
                 if (!none) {
                     float c1[16], W[16];
@@ -1375,13 +1381,17 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1)
                             W[j + e] = in ? z[e] * W[j + e] : 0.f;
                             row += W[j + e];
                         }
-                        w[j / 2] = pack_bf16(z[0], z[1]);
-                        w[j / 2 + 1] = pack_bf16(z[2], z[3]);
+                        split(z[0], z[1], w[j / 2], wl[j / 2]);
+                        split(z[2], z[3], w[j / 2 + 1], wl[j / 2 + 1]);
                     }
                     col = transpose_sum16(W);
                 }
                 st_shared_v4(dst + swz128(i, 32 * half + 16 * y), w[0], w[1], w[2], w[3]);
                 st_shared_v4(dst + swz128(i, 32 * half + 16 * y + 8), w[4], w[5], w[6], w[7]);
+                if (!key) {
+                    st_shared_v4(dst + 8192 + swz128(i, 32 * half + 16 * y), wl[0], wl[1], wl[2], wl[3]);
+                    st_shared_v4(dst + 8192 + swz128(i, 32 * half + 16 * y + 8), wl[4], wl[5], wl[6], wl[7]);
+                }
                 if (!(lane & 1)) cols[quad][32 * half + 16 * y + lane / 2] = col;
             }
             rows[half][kd] = row;
@@ -1437,16 +1447,18 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1)
             const uint32_t qn = dlow(sb + L::QK, 16384), kn = dlow(sb + L::QK + 8192, 16384);
             constexpr uint32_t I_KM = idesc_bf16(128, kC, 1, 0), I_MM = idesc_bf16(128, kC, 1, 1);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) wmma_bf16(tm, desc(kn, 2048 * k), desc(zq, 32 * k), I_KM, k > 0);
+            for (int k = 0; k < 8; ++k)  // (high, then low parts of Zq)
+                wmma_bf16(tm, desc(kn, 2048 * (k & 3)), desc(zq, (k >> 2) * 8192 + 32 * (k & 3)), I_KM, k > 0);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) wmma_bf16(tm + 64, desc(qn, 2048 * k), desc(zqn, 2048 * k), I_MM, k > 0);
+            for (int k = 0; k < 8; ++k)
+                wmma_bf16(tm + 64, desc(qn, 2048 * (k & 3)), desc(zqn, 2048 * k), I_MM, k > 0);
 #pragma unroll
             for (int k = 0; k < 4; ++k) wmma_bf16(tm + 64, desc(kn, 2048 * k), desc(zkn, 2048 * k), I_MM, 1);
 #pragma unroll
             for (int k = 0; k < 4; ++k) wmma_bf16(tm + 64, desc(kn, 2048 * k), desc(zk, 32 * k), I_KM, 1);
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k)
-                wmma_bf16(tm + 128, desc(dlow(sb + L::DS, L::BLOCK), 2048 * k), desc(de, 2048 * k), I_MM, k > 0);
+            for (int k = 0; k < D / 8; ++k)
+                wmma_bf16(tm + 128, desc(dlow(sb + L::DS, L::BLOCK), 2048 * (k % (D / 16))), desc(de, 2048 * k), I_MM, k > 0);
             wmma_commit(&bar_mma);
         }
         ok = products_done();
@@ -1604,7 +1616,7 @@ cudaError_t back(const Packed& p, const void* q, const void* k, const void* dout
     if (!make_chunk_map(&mq, q, p.T, p.Hk, D, p.qs) || !make_chunk_map(&mk, k, p.T, p.Hk, D, p.ks) ||
         !make_chunk_map(&mo, dout, p.T, p.H, D, (long long)p.H * D) ||
         !make_chunk_map(&mv, x.dv, p.T, p.H, D, (long long)p.H * D) ||
-        !make_feat_map(&me, e, slots, D, kC, D) || !make_feat_map(&ms, st, slots, D, D, D) ||
+        !make_feat_map(&me, e, slots, 2 * D, kC, 2 * D) || !make_feat_map(&ms, st, slots, D, D, D) ||
         !make_feat_map(&md, x.ds, slots, D, D, D))
         return cudaErrorInvalidValue;
     const int walk = (int)Back<D>::SMEM, grad = (int)Grad<D>::SMEM;
@@ -1614,7 +1626,7 @@ cudaError_t back(const Packed& p, const void* q, const void* k, const void* dout
         r = cudaFuncSetAttribute(delta_grad_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, grad);
     if (r == cudaSuccess)
         r = launch_after(delta_back_kernel<D>, dim3((unsigned)(p.n * p.H)), kWalkThreads, walk, 0,
-                         false, s, mq, mk, mo, x);
+                         false, s, mq, mk, mo, me, x);
     if (r == cudaSuccess)
         r = launch_after(delta_grad_kernel<D>,
                          dim3((unsigned)block_slots(p.T, p.n, kC), (unsigned)p.Hk), 256, grad, 0, true,
@@ -1622,7 +1634,7 @@ cudaError_t back(const Packed& p, const void* q, const void* k, const void* dout
     return r;
 }
 
-// The parts of a save buffer: records, E^T, S^T.
+// The parts of a save buffer: records, E^T (high and low parts), S^T.
 struct SaveParts {
     size_t e, s, total;
 };
@@ -1631,7 +1643,7 @@ SaveParts save_parts(const Packed& p)
     const size_t slots = (size_t)block_slots(p.T, p.n, kC) * p.H;
     SaveParts x;
     x.e = align_up(slots * Rec::BYTES, 256);
-    x.s = x.e + slots * p.d * kC * 2;
+    x.s = x.e + slots * 2 * p.d * kC * 2;
     x.total = x.s + slots * p.d * p.d * 2;
     return x;
 }
@@ -1685,7 +1697,6 @@ cudaError_t launch_tc_delta_bwd(const Packed& p, const void* q, const void* k, c
     BackArgs x = {};
     x.p = p;
     x.cu = cu; x.scale = scale; x.rec = (const uint8_t*)save;
-    x.e = (const __nv_bfloat16*)(base + at.e);
     x.ds = (__nv_bfloat16*)scratch;
     x.db = (float*)((char*)scratch + (size_t)block_slots(p.T, p.n, kC) * p.H * p.d * p.d * 2);
     x.dv = (__nv_bfloat16*)dv; x.status = status;

@@ -582,3 +582,16 @@ def test_as_many_heads_as_a_call_takes(dtype):
     check(last, rs, "last state", F32)
     for name, y, r in zip(NAMES, _bwd(x, cu), delta_grads(x, lens, d ** -0.5)):
         check(y, r, "d" + name)
+
+
+@pytest.mark.parametrize("H,Hk,d", [(4, 4, 64), (8, 4, 64), (4, 2, 128)])
+def test_bf16_gradients_are_near_their_own_rounding(H, Hk, d):
+    """E and the pairs' weights Z enter the gradients' products as bf16 high and low parts.  What is
+    rounded on the way (the state, its gradient, dV, and what the walk multiplies) leaves no more
+    than two roundings' worth beside a result's own: sqrt(3) of one, at the 1 / sqrt(2) that uniform
+    significands leave of the largest."""
+    from packed_ref import ROUNDED, check_each
+    lens = (512, 200, 333)
+    x, cu = delta_inputs(lens, H, Hk, d, BF16, seed=32), offsets(lens)
+    for name, y, r in zip(NAMES, _bwd(x, cu), delta_grads(x, lens, d ** -0.5)):
+        check_each(y, r, lens, (3 / 2) ** 0.5 * ROUNDED, "d" + name)
