@@ -261,7 +261,9 @@ size_t flex_delta_save_bytes(const flex_packed* shape);
  * flex_delta_bwd; training starts from the zero state, so S0 must then be NULL.
  * States and sums are fp32.  bf16 storage with 1024 / d tokens a sequence on average runs in
  * chunks of 64 tokens on the tensor cores, with the state, the corrections and the weights as
- * bf16 high and low parts (2 kernels; log decays below -88 count as -88); the rest token by token
+ * bf16 high and low parts (2 kernels; log decays below -88 count as -88).  What is added to the
+ * state comes in three such parts, or with `save` in two: the last state is off by 7e-7, or 3e-6
+ * (2-norm), and the two forms' outputs may differ in their last bit.  The rest runs token by token
  * (1 kernel).  A NaN in a row goes on to every later row of its sequence and head and to its last
  * state; in chunks also to the rows of its own chunk ahead of it.  Other sequences and heads
  * never see it.  Errors: FLEX_EINVAL, FLEX_EUNSUPPORTED (d, or more than 65535 sequences or 1024

@@ -17,12 +17,16 @@
 // For d = 64 the lower 64 of the 128 lanes carry the state; the others compute on whatever they hold.
 //
 // Precision: K and Q are exact.  What multiplies them (S, beta R, U, M and P) is split into bf16 high
-// and low parts (2^-17; products of two low parts are left out), so that the state, held in fp32
-// registers, is off by 3e-6 and the output by little more than its own rounding (with P as bf16 by
-// 1.6 times it).  The backward's results are bf16 and held to 1.2 times their own rounding: of its
-// operands P, E and Zq (below) are split, which left 1.8 times it as bf16 (E and Zq 1.7e-3 each of
-// dq's 3.0e-3, dk's and dg's 3.1e-3; splitting them took 331 us to 355, 8 x 2048 H12 d64); the state
-// and its gradient of a chunk, dV and the walk's own operands, bf16 too, leave 0.6e-3 or less each.
+// and low parts (2^-17), so that the output is off by little more than its own rounding (with P as
+// bf16 by 1.6 times it).  The state, held in fp32 registers, would be off by 2.8e-6 so, nearly all of
+// it from e^{G_C - G} U, what a chunk adds.  A prompt's walk takes that and beta R in three parts and
+// multiplies M's and beta R's low parts too: 6e-7 to 7e-7 (8 x 4096, H16 d128: 371 -> 394 us; S and M
+// need no third part: emulated, 5e-8 and 5e-7).  The walk that saves for the backward, whose results
+// are bf16, does without (third parts for both: 371 us instead of 355 for 8 x 2048 H12 d64).
+// The backward's results are bf16 and held to 1.2 times their own rounding: of its operands P, E and
+// Zq (below) are split, which left 1.8 times it as bf16 (E and Zq 1.7e-3 each of dq's 3.0e-3, dk's and
+// dg's 3.1e-3; splitting them took 331 us to 355, 8 x 2048 H12 d64); the state and its gradient of a
+// chunk, dV and the walk's own operands, bf16 too, leave 0.6e-3 or less each.
 #include <cuda.h>
 
 #include "flex_internal.h"
@@ -71,6 +75,19 @@ __device__ __forceinline__ void split2(uint64_t ab, uint32_t& hi, uint32_t& lo)
 __device__ __forceinline__ void split(float a, float b, uint32_t& hi, uint32_t& lo)
 {
     split2(f2_pack(a, b), hi, lo);
+}
+
+// ... and, if `third`, what those leave.
+__device__ __forceinline__ void split23(uint64_t ab, bool third, uint32_t& hi, uint32_t& lo, uint32_t& rest)
+{
+    split2(ab, hi, lo);
+    if (!third) return;
+    const uint64_t minus = f2_pack(-1.f, -1.f);
+    ab = f2_fma(f2_pack(__uint_as_float(hi << 16), __uint_as_float(hi & 0xffff0000u)), minus, ab);
+    ab = f2_fma(f2_pack(__uint_as_float(lo << 16), __uint_as_float(lo & 0xffff0000u)), minus, ab);
+    float a, b;
+    f2_unpack(ab, a, b);
+    rest = pack_bf16(a, b);
 }
 
 // Eight packed pairs rounded to bf16.
@@ -378,6 +395,9 @@ struct Walk {
     // beta R, then kappa U, high and low; U high and low; the state's increment; Q S
     static constexpr int T_SH = 0, T_SL = D / 2, T_X = D, T_AH = D + 64, T_AL = D + 96, T_UH = D + 128,
                          T_UL = D + 160, T_D = D + 192, T_Q = 2 * D + 192;
+    // The third parts: of beta R where U comes once the product with M is done, of kappa U where the
+    // state's last piece stands, which that product's completion frees and s_full of that piece hands on.
+    static constexpr int T_RM = T_UH, T_KM = T_SH + 32 * (PIECES - 1);
     static_assert(2 * D + 256 <= 512, "tensor memory");
 };
 constexpr int kWalkThreads = 640;
@@ -390,7 +410,7 @@ struct WalkArgs {
     float* S1;
     __nv_bfloat16* out;
     const uint8_t* rec;
-    // NULL, or E^T [slot][H][high, low][d][64] and S^T [slot][H][d][d] of each chunk
+    // (saving) E^T [slot][H][high, low][d][64] and S^T [slot][H][d][d] of each chunk
     __nv_bfloat16 *e_save, *s_save;
     int* status;
 };
@@ -407,8 +427,9 @@ struct WalkArgs {
 //   issue   increment = (e^{G_C - G} U) K, by pieces (s_full), then X = P U        (o_full)
 //   tokens  out = scale e^G (Q S) + P U                                    (x_free, q_free)
 // The pieces let the products of one piece run beside the arithmetic of the other.  (One set of
-// warps for state and tokens needs 168 registers a thread and spills what it holds on the way.)
-template <int D>
+// warps for state and tokens would need 168 registers a thread, of 96.)  SAVE: leave E and S for the
+// backward, without third parts (see the top).
+template <int D, bool SAVE>
 __global__ void __launch_bounds__(kWalkThreads, 1)
     delta_walk_kernel(const __grid_constant__ CUtensorMap tmap_q,
                       const __grid_constant__ CUtensorMap tmap_k,
@@ -535,6 +556,10 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                 mma4(W::T_X, W::T_AH, dmh, 32, I_C, 0);
                 mma4(W::T_X, W::T_AL, dmh, 32, I_C, 1);
                 mma4(W::T_X, W::T_AH, dml, 32, I_C, 1);
+                if (!SAVE) {
+                    mma4(W::T_X, W::T_RM, dmh, 32, I_C, 1);
+                    mma4(W::T_X, W::T_AL, dml, 32, I_C, 1);
+                }
                 wmma_commit(&e_full);
                 wait(&u_ready, c);
                 if (!ok) break;
@@ -542,6 +567,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                 for (int p = 0; p < W::PIECES; ++p) {
                     mma4(W::T_D + 64 * p, W::T_AH, dkn + 512 * p, 2048, I_D, 0);
                     mma4(W::T_D + 64 * p, W::T_AL, dkn + 512 * p, 2048, I_D, 1);
+                    if (!SAVE) mma4(W::T_D + 64 * p, W::T_KM, dkn + 512 * p, 2048, I_D, 1);
                     wmma_commit(&s_full[p]);
                 }
                 wait(&p_ready, c);
@@ -608,7 +634,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                     }
                     if (c < chunks) ready(&s_ready[p]);
                 }
-                if (x.s_save && ok && c < chunks) {  // (rounded again: the walk waits for the pieces)
+                if (SAVE && ok && c < chunks) {  // (rounded again: the walk waits for the pieces)
 #pragma unroll
                     for (int p = 0; p < W::PIECES; ++p) {
                         __nv_bfloat16* dst = x.s_save + ((rec0 + (size_t)c * pk.H) * D + v) * D + 64 * p + 32 * half;
@@ -671,7 +697,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                     float d[16];
                     tmem_ld16(lanes + W::T_X + 32 * half + 16 * j, d);
                     tmem_wait_ld();
-                    uint32_t wh[8], wl[8];
+                    uint32_t wh[8], wl[8], wm[8];
 #pragma unroll
                     for (int i = 0; i < 8; i += 2) {  // (X is 0 behind the end: K is)
                         const ulonglong2 gm = *(const ulonglong2*)(aux + Rec::GAMMA / 4 + 16 * j + 2 * i);
@@ -680,11 +706,12 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                         // (e^G holds its negative in the record: R = V - e^G X)
                         r[0] = f2_fma(gm.x, f2_pack(d[2 * i], d[2 * i + 1]), r[0]);
                         r[1] = f2_fma(gm.y, f2_pack(d[2 * i + 2], d[2 * i + 3]), r[1]);
-                        split2(f2_mul(bt.x, r[0]), wh[i], wl[i]);
-                        split2(f2_mul(bt.y, r[1]), wh[i + 1], wl[i + 1]);
+                        split23(f2_mul(bt.x, r[0]), !SAVE, wh[i], wl[i], wm[i]);
+                        split23(f2_mul(bt.y, r[1]), !SAVE, wh[i + 1], wl[i + 1], wm[i + 1]);
                     }
                     tmem_st8(lanes + W::T_AH + 16 * half + 8 * j, wh);
                     tmem_st8(lanes + W::T_AL + 16 * half + 8 * j, wl);
+                    if (!SAVE) tmem_st8(lanes + W::T_RM + 16 * half + 8 * j, wm);
                 }
                 ready(&r_ready);
                 if (!wait(&e_full, c)) break;
@@ -694,7 +721,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                     float d[16];
                     tmem_ld16(lanes + W::T_X + 32 * half + 16 * j, d);
                     tmem_wait_ld();
-                    uint32_t wh[8], wl[8];
+                    uint32_t wh[8], wl[8], wm[8];
 #pragma unroll
                     for (int i = 0; i < 8; i += 2) {
                         const ulonglong2 bt = *(const ulonglong2*)(aux + Rec::BETA / 4 + 16 * j + 2 * i);
@@ -702,11 +729,12 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                         uint64_t* r = R + 8 * j + i;
                         r[0] = f2_fma(f2_pack(d[2 * i], d[2 * i + 1]), minus, r[0]);
                         r[1] = f2_fma(f2_pack(d[2 * i + 2], d[2 * i + 3]), minus, r[1]);
-                        split2(f2_mul(f2_mul(kp.x, bt.x), r[0]), wh[i], wl[i]);
-                        split2(f2_mul(f2_mul(kp.y, bt.y), r[1]), wh[i + 1], wl[i + 1]);
+                        split23(f2_mul(f2_mul(kp.x, bt.x), r[0]), !SAVE, wh[i], wl[i], wm[i]);
+                        split23(f2_mul(f2_mul(kp.y, bt.y), r[1]), !SAVE, wh[i + 1], wl[i + 1], wm[i + 1]);
                     }
                     tmem_st8(lanes + W::T_AH + 16 * half + 8 * j, wh);
                     tmem_st8(lanes + W::T_AL + 16 * half + 8 * j, wl);
+                    if (!SAVE) tmem_st8(lanes + W::T_KM + 16 * half + 8 * j, wm);
                 }
                 ready(&u_ready);
 #pragma unroll
@@ -722,7 +750,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                     tmem_st8(lanes + W::T_UL + 16 * half + 8 * j, ul);
                 }
                 ready(&p_ready);
-                if (x.e_save) {
+                if (SAVE) {
                     __nv_bfloat16* dst = x.e_save + ((rec0 + (size_t)c * pk.H) * 2 * D + v) * kC + 32 * half;
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
@@ -1592,17 +1620,18 @@ cudaError_t fwd(const Packed& p, const void* q, const void* k, const void* v, co
         return cudaErrorInvalidValue;
     const int prep = (D * 256 > (int)sizeof(PrepSmem) ? D * 256 : (int)sizeof(PrepSmem)) + 1024;
     const int walk = (int)Walk<D>::SMEM;
+    const auto kernel = x.e_save ? delta_walk_kernel<D, true> : delta_walk_kernel<D, false>;
     cudaError_t e = cudaFuncSetAttribute(delta_prep_kernel<D>,
                                          cudaFuncAttributeMaxDynamicSharedMemorySize, prep);
     if (e == cudaSuccess)
-        e = cudaFuncSetAttribute(delta_walk_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, walk);
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, walk);
     if (e == cudaSuccess)
         e = launch_after(delta_prep_kernel<D>,
                          dim3((unsigned)block_slots(p.T, p.n, kC), (unsigned)p.H), 128, prep, 0, false,
                          s, mq, mk, p, (const __nv_bfloat16*)g, (const __nv_bfloat16*)beta, x.cu,
                          x.scale, rec, x.status);
     if (e == cudaSuccess)
-        e = launch_after(delta_walk_kernel<D>, dim3((unsigned)(p.n * p.H)), kWalkThreads, walk, 0,
+        e = launch_after(kernel, dim3((unsigned)(p.n * p.H)), kWalkThreads, walk, 0,
                          true, s, mq, mk, mv, x);
     return e;
 }
