@@ -383,8 +383,8 @@ struct Walk {
     static constexpr int WARPS = 2 * QUADS;         // state warps, and as many token warps
     static constexpr int PIECES = D / 64;           // of the state: 64 key dimensions each
     // The issuing and the loading warp: for d = 64, which computes on quadrants 0 and 1 and so on
-    // schedulers 0 and 1, they go to the others (reverse walk, 8 x 2048 H12: 82 -> 72 us; d = 128 is
-    // the slower for it).
+    // schedulers 0 and 1, they go to the others (training, 8 x 2048 H12: 356 -> 350 us; d = 128 is the
+    // slower for it).
     static constexpr int MMA = D == 64 ? 18 : 16, TMA = D == 64 ? 19 : 17;
     static constexpr uint32_t TILE = kC * D * 2;    // 64 rows of K, Q or V
     static constexpr uint32_t K = 0, Q = TILE, V = 2 * TILE, REC = 3 * TILE;
@@ -1051,28 +1051,21 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) S[p][i] = f2_pack(0.f, 0.f);
             uint64_t decay = f2_pack(1.f, 1.f);
-            // A round trip to tensor memory takes 250 cycles: for d = 64 both loads of a step are in
-            // flight together (78 -> 72 us for 8 x 2048, H12; d = 128 has no registers left for it).
-            constexpr bool ahead = D == 64;
             for (int r = 0; r < chunks; ++r) {
                 __nv_bfloat16* ds = x.ds + ((rec0 + (size_t)(chunks - 1 - r) * pk.H) * D + v) * D + 32 * half;
 #pragma unroll
                 for (int p = 0; p < W::PIECES; ++p) {
                     if (r > 0 && !wait(&s_full[p], r - 1)) break;
                     const uint32_t inc = lanes + B::T_D + 64 * p + 32 * half;
-                    float a[2][16];
-                    if (ahead && r > 0) {
-                        tmem_ld16(inc, a[0]);
-                        tmem_ld16(inc + 16, a[1]);
-                    }
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         if (r > 0) {  // S = decay S + the increment of the chunk behind
-                            if (!ahead) tmem_ld16(inc + 16 * j, a[j]);
+                            float a[16];
+                            tmem_ld16(inc + 16 * j, a);
                             tmem_wait_ld();
 #pragma unroll
                             for (int e = 0; e < 8; ++e)
-                                S[p][8 * j + e] = f2_fma(decay, S[p][8 * j + e], f2_pack(a[j][2 * e], a[j][2 * e + 1]));
+                                S[p][8 * j + e] = f2_fma(decay, S[p][8 * j + e], f2_pack(a[2 * e], a[2 * e + 1]));
                         }
                         uint32_t w[8];
                         pack8(S[p] + 8 * j, w);
@@ -1128,26 +1121,18 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                 }
                 if (!wait(&x_full, r)) break;
                 uint64_t U[16];  // dU, then Y: pairs of tokens
-                constexpr bool ahead = D == 64;  // (see above)
-                float d[2][16], y[2][16];
-                auto fetch = [&](int j) {
-                    tmem_ld16(lanes + B::T_X + 32 * half + 16 * j, d[j]);
-                    tmem_ld16(lanes + B::T_P + 32 * half + 16 * j, y[j]);
-                };
-                if (ahead) {
-                    fetch(0);
-                    fetch(1);
-                }
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    if (!ahead) fetch(j);
+                    float d[16], y[16];
+                    tmem_ld16(lanes + B::T_X + 32 * half + 16 * j, d);
+                    tmem_ld16(lanes + B::T_P + 32 * half + 16 * j, y);
                     tmem_wait_ld();
                     uint32_t w[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const uint64_t kp = *(const uint64_t*)(aux + kK + 16 * j + 2 * i);
                         const uint64_t bt = *(const uint64_t*)(aux + kB + 16 * j + 2 * i);
-                        U[8 * j + i] = f2_fma(kp, f2_pack(d[j][2 * i], d[j][2 * i + 1]), f2_pack(y[j][2 * i], y[j][2 * i + 1]));
+                        U[8 * j + i] = f2_fma(kp, f2_pack(d[2 * i], d[2 * i + 1]), f2_pack(y[2 * i], y[2 * i + 1]));
                         float a, b;
                         f2_unpack(f2_mul(bt, U[8 * j + i]), a, b);
                         w[i] = pack_bf16(a, b);
@@ -1157,20 +1142,17 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
                 ready(&r_ready);
                 if (!wait(&e_full, r)) break;
                 uint32_t wv[16];  // dV
-                if (ahead) {
-                    tmem_ld16(lanes + B::T_X + 32 * half, d[0]);
-                    tmem_ld16(lanes + B::T_X + 32 * half + 16, d[1]);
-                }
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    if (!ahead) tmem_ld16(lanes + B::T_X + 32 * half + 16 * j, d[j]);
+                    float d[16];
+                    tmem_ld16(lanes + B::T_X + 32 * half + 16 * j, d);
                     tmem_wait_ld();
                     uint32_t w[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const uint64_t gm = *(const uint64_t*)(aux + kG + 16 * j + 2 * i);  // -e^G
                         const uint64_t bt = *(const uint64_t*)(aux + kB + 16 * j + 2 * i);
-                        U[8 * j + i] = f2_fma(f2_pack(d[j][2 * i], d[j][2 * i + 1]), minus, U[8 * j + i]);
+                        U[8 * j + i] = f2_fma(f2_pack(d[2 * i], d[2 * i + 1]), minus, U[8 * j + i]);
                         const uint64_t y = f2_mul(bt, U[8 * j + i]);
                         float a, b;
                         f2_unpack(y, a, b);
@@ -1679,13 +1661,16 @@ SaveParts save_parts(const Packed& p)
 
 }  // namespace
 
-// By the average length (the lengths are on the device).  A walk costs a sequence 10 us and 3 us for
-// each 64 tokens, the scans 0.2 us (d = 128: 0.35) for each token.  Measured, H16, scans / chunks in us:
-//   d = 64:  64 x 16 tokens 35 / 64, 64 x 32 60 / 66, 64 x 64 109 / 68; training 137 / 139, 241 / 146
-//   d = 128: 8 x 16 tokens 27 / 19, 64 x 16 150 / 80, 64 x 64 472 / 86
-//   one prompt of 4000 among 100 single tokens: d = 64 794 / 216, d = 128 1283 / 270
+// By the average length (the lengths are on the device).  A walk costs a sequence 10 us and 3.6 us (d =
+// 128: 4.4) for each 64 tokens, the scans 0.2 us (0.32) for each token.  Measured, H16, scans / chunks
+// in us:
+//   d = 64:  64 x 16 tokens 33 / 65, 64 x 32 57 / 66, 64 x 64 107 / 69; training, 64 x 16 128 / 144,
+//            64 x 32 233 / 149
+//   d = 128: 8 x 16 tokens 24 / 17, 64 x 16 146 / 79, 64 x 64 468 / 85
+//   one prompt of 4000 among 100 single tokens: d = 64 797 / 241, d = 128 1280 / 292
 // so the chunks take over at 16 and 8 tokens: below what uniform short sequences of d = 64 would
-// like, for the sake of prompts among single tokens.
+// like, for the sake of prompts among single tokens (too many of which, 266 beside 4000 tokens for
+// d = 64, still bring the scans).
 bool tc_delta_supported(const Packed& p) { return p.bf16 && (long long)p.T * p.d >= 1024LL * p.n; }
 
 size_t tc_delta_rec_bytes(const Packed& p)
