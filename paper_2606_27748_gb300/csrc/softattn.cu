@@ -230,6 +230,8 @@ int softattn_splits(const Packed& p)
     // start and end without filling it better (16 sequences of 8000 and 16 of 1777 keys, H16 Hk4
     // d128: 66 us for one block an SM, 61 for two, 64 for three, 68 for four, 73 for eight).  A range
     // is 256 keys (fp32: 128) of an average sequence or more; 32 ranges (the join's lanes) at most.
+    // (152 SMs as a constant: the workspace's size must not go by the device that is current when it
+    // is asked for, and the order of a row's sums not by where it runs.)
     const int G = p.H / p.Hk;
     const bool tc = tc_softattn_supported(p);
     const int rows = tc ? tc_softattn_rows(p) : kRows;
