@@ -1212,8 +1212,8 @@ __global__ void __launch_bounds__(kWalkThreads, 1)
 // it; dQ^T and dK^T are products of key dimension x token, summed over the heads in registers: a
 // lane holds one key dimension (quadrant w % 4) and a warp half of the tokens (w / 4).  256 columns
 // of tensor memory, taken twice: [dO E, dV E | Q K^T, K K^T | S dO | S dV], then [Zq K | Zq^T Q +
-// (Zk + Zk^T) K | D E], E and Zq as high and low parts.  For d = 64 products have rows 64-127 that read whatever lies behind a tile
-// (within shared memory) and are not looked at.
+// (Zk + Zk^T) K | D E], E and Zq as high and low parts.  For d = 64 products have rows 64-127 that read
+// whatever lies behind a tile (within shared memory) and are not looked at.
 template <int D>
 struct Grad {
     static constexpr uint32_t TILE = kC * D * 2, BLOCK = D * 128;  // 64 tokens; D rows of 64 elements

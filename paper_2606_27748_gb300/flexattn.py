@@ -307,6 +307,9 @@ def awd_loss_bwd(q, k, W1, W2=None, causal=False, tau=None, dloss=None, loss=Non
 
 
 # ---- packed batches: sequences of different lengths, rows [T][heads][d] ------------------
+#
+# `stream`: the call runs there, and its results are of that stream's memory; the inputs have to be
+# ready on it, and to be kept until it is done with them.
 
 def _rows(t, what, shape, dtype, dev):
     """The row stride of a tensor [T, heads, d] of this shape and type on device `dev` whose heads
