@@ -313,6 +313,67 @@ int flex_softattn_fwd(const flex_packed* shape, const void* q, const void* k, co
                       const int* cu_q, const int* cu_k, float scale, int causal, void* out,
                       float* lse, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- around the recurrence ------------------------------------------------------------
+ * What a recurrent layer on packed batches has besides the calls above.  Rows are [T][channels],
+ * found by the same offsets; rows behind the last sequence are neither read into a result nor
+ * written.  Activations may be slices of wider rows (`*_stride` elements from one to the next, at
+ * least a row, whole 16-byte units; 16-byte aligned); outputs, gradients and parameters are
+ * contiguous.  Parameters and their gradients are fp32. */
+typedef struct {
+    int n;         /* sequences, >= 1 */
+    int T;         /* rows, >= 1 */
+    int D;         /* channels, whole 16-byte units */
+    int G;         /* groups of channels that share B and C: D % G == 0, whole fours */
+    int N;         /* states of a channel: 8, 16 or 32 */
+    int dtype;     /* flex_dtype of every activation */
+    int softplus;  /* 1: the step is softplus(dt + dt_bias), 0: dt + dt_bias */
+    int x_stride;
+    int dt_stride;
+    int b_stride;
+    int c_stride;
+    int z_stride;  /* (where z is given) */
+} flex_ssm;
+
+/* Workspace bytes of flex_ssm_fwd (backward = 0) or of both flex_ssm_fwd and flex_ssm_bwd
+ * (backward = 1), and of the buffer that flex_ssm_fwd leaves for flex_ssm_bwd; 0 if the shape is
+ * invalid or unsupported. */
+size_t flex_ssm_workspace_bytes(const flex_ssm* shape, int backward);
+size_t flex_ssm_save_bytes(const flex_ssm* shape);
+
+/* Selective state space scan over whole sequences.  Per sequence and channel c of group g, from
+ * h = 0 or S0, with the step D_t = softplus(dt_t[c] + dt_bias[c]) (or without softplus):
+ *   h_t[i] = exp(D_t A[c][i]) h_{t-1}[i] + D_t x_t[c] B_t[g][i],
+ *   out_t[c] = (sum_i C_t[g][i] h_t[i] + D[c] x_t[c]) silu(z_t[c]).
+ * x, dt, z, out: [T][D]; B, C: [T][G][N]; all in shape->dtype.  A: [D][N], D, dt_bias: [D], fp32,
+ * finite.  D, z (no gate) and dt_bias may be NULL.
+ * S0: NULL or [n][D][N] fp32; S1: NULL or the same, receives each sequence's last state (an empty
+ * sequence's is its first); S1 may be S0.  save: NULL, or flex_ssm_save_bytes() bytes, 256-byte
+ * aligned, filled for flex_ssm_bwd; S0 must then be NULL.
+ * States and sums are fp32.  A NaN in a row goes on to later rows of its sequence (of x, dt or z: of
+ * its channel; of B or C: of its group) and never to other sequences.  Results repeat bit for bit.
+ * 1 kernel, or 2 where sequences are cut.  Errors: FLEX_EINVAL, FLEX_EUNSUPPORTED (N, D, or more than
+ * 65535 sequences, 65536 channels or 1024 groups), FLEX_EWORKSPACE. */
+int flex_ssm_fwd(const flex_ssm* shape, const void* x, const void* dt, const float* A, const void* B,
+                 const void* C, const float* D, const void* z, const float* dt_bias, const int* cu,
+                 const float* S0, float* S1, void* out, void* save, void* ws, size_t ws_bytes,
+                 void* stream);
+
+/* Gradients of L = sum(dout * out) of flex_ssm_fwd from the zero state, with respect to all its
+ * inputs, each in its input's shape (contiguous); dD, dz and ddt_bias are given exactly when D, z and
+ * dt_bias are.  save: what flex_ssm_fwd left for the same shape, inputs and offsets.  Every sum has a
+ * fixed order: results repeat bit for bit.  2 kernels, or 3 where sequences are cut. */
+int flex_ssm_bwd(const flex_ssm* shape, const void* x, const void* dt, const float* A, const void* B,
+                 const void* C, const float* D, const void* z, const float* dt_bias, const int* cu,
+                 const void* dout, const void* save, void* dx, void* ddt, float* dA, void* dB,
+                 void* dC, float* dD, void* dz, float* ddt_bias, void* ws, size_t ws_bytes,
+                 void* stream);
+
+/* One token of every sequence: the recurrence above for row i of each tensor (T == n; no offsets, no
+ * workspace), on the caller's S [n][D][N] fp32, updated in place.  One kernel. */
+int flex_ssm_decode(const flex_ssm* shape, const void* x, const void* dt, const float* A,
+                    const void* B, const void* C, const float* D, const void* z,
+                    const float* dt_bias, float* S, void* out, void* stream);
+
 /* Cumulative number of kernels this library has enqueued in this process (all entry
  * points, all devices).  Lets a caller count the launches inside a timed region. */
 unsigned long long flex_kernel_launches(void);

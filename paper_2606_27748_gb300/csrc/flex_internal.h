@@ -162,4 +162,13 @@ int tc_softattn_rows(const Packed& p);        // rows of a block: 32, 128 or 256
 cudaError_t launch_tc_softattn(const AttnArgs& x, cudaStream_t s);
 cudaError_t launch_softattn_join(const AttnArgs& x, cudaStream_t s);
 
+// ---- packed batches: selective state space scan ----------------------------------------
+struct SsmArgs;  // ssm.cuh
+// Tokens of a block (a multiple of 64), or T + 1 where sequences stay whole.
+int ssm_rows(const SsmArgs& a, bool backward);
+cudaError_t launch_ssm_fwd(const SsmArgs& a, cudaStream_t s);        // 1 kernel, cut: 2
+cudaError_t launch_ssm_back_ends(const SsmArgs& a, cudaStream_t s);  // 1
+cudaError_t launch_ssm_bwd(const SsmArgs& a, cudaStream_t s);        // 2 kernels, cut: 3
+cudaError_t launch_ssm_decode(const SsmArgs& a, cudaStream_t s);
+
 }  // namespace flex

@@ -1,0 +1,172 @@
+// Host side of the entry points around the recurrence (include/flexattn.h): argument checks,
+// workspace layout and dispatch.  Nothing here allocates device memory or synchronises.
+#include "flex_internal.h"
+#include "ssm.cuh"
+
+#include <initializer_list>
+
+namespace {
+
+constexpr size_t kHeader = sizeof(flex::WsHeader);
+
+bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
+// All given and on 16-byte boundaries.
+bool all16(std::initializer_list<const void*> ps)
+{
+    for (const void* p : ps)
+        if (!p || !aligned(p, 16)) return false;
+    return true;
+}
+// On 16-byte boundaries where given.
+bool opt16(std::initializer_list<const void*> ps)
+{
+    for (const void* p : ps)
+        if (!aligned(p, 16)) return false;
+    return true;
+}
+bool offsets(const int* cu) { return cu && aligned(cu, 4); }
+int check_ws(const void* ws, size_t ws_bytes, size_t need)
+{
+    if (!ws || !aligned(ws, 256)) return FLEX_EINVAL;
+    return ws_bytes < need ? FLEX_EWORKSPACE : FLEX_OK;
+}
+int counted(int n, cudaError_t e)
+{
+    if (e != cudaSuccess) return FLEX_ECUDA;
+    flex::add_launches(n);
+    return FLEX_OK;
+}
+int unit(int dtype) { return dtype == FLEX_BF16 ? 8 : 4; }  // elements of 16 bytes
+bool strides(int dtype, std::initializer_list<int> stride, int least)
+{
+    for (int s : stride)
+        if (s % unit(dtype) || s < least) return false;
+    return true;
+}
+
+int make_ssm(const flex_ssm* s, bool z, flex::SsmArgs* a)
+{
+    if (!s || s->n < 1 || s->T < 1 || s->D < 1 || s->G < 1 || s->N < 1) return FLEX_EINVAL;
+    if (s->dtype != FLEX_F32 && s->dtype != FLEX_BF16) return FLEX_EINVAL;
+    if (s->D % s->G) return FLEX_EINVAL;
+    if (s->N != 8 && s->N != 16 && s->N != 32) return FLEX_EUNSUPPORTED;
+    if (s->D % unit(s->dtype) || s->D / s->G % 4) return FLEX_EUNSUPPORTED;
+    if (s->n > 65535 || s->T > (1 << 30) || s->D > 65536 || s->G > 1024) return FLEX_EUNSUPPORTED;
+    if (!strides(s->dtype, {s->x_stride, s->dt_stride}, s->D)) return FLEX_EINVAL;
+    if (!strides(s->dtype, {s->b_stride, s->c_stride}, s->G * s->N)) return FLEX_EINVAL;
+    if (z && !strides(s->dtype, {s->z_stride}, s->D)) return FLEX_EINVAL;
+    *a = {};
+    a->n = s->n; a->T = s->T; a->D = s->D; a->G = s->G; a->N = s->N;
+    a->bf16 = s->dtype == FLEX_BF16; a->softplus = s->softplus != 0;
+    a->xs = s->x_stride; a->ds = s->dt_stride; a->bs = s->b_stride; a->cs = s->c_stride;
+    a->zs = s->z_stride;
+    return FLEX_OK;
+}
+
+size_t floats(size_t n) { return flex::align_up(n * 4, 256); }
+
+// Blocks' ends and sums of steps where sequences are cut; backward: sums over blocks' channels and
+// tokens too.  With ws the pointers into it are set.
+size_t ssm_layout(flex::SsmArgs* a, bool backward, char* ws)
+{
+    size_t at = kHeader;
+    auto take = [&](size_t n) {
+        float* p = (float*)(ws + at);
+        at += floats(n);
+        return ws ? p : nullptr;
+    };
+    a->rows = flex::ssm_rows(*a, backward);
+    const size_t slots = flex::block_slots(a->T, a->n, a->rows), DN = (size_t)a->D * a->N;
+    if (a->rows <= a->T) {
+        a->ends = take(slots * DN);
+        a->sums = take(slots * a->D);
+    }
+    if (backward) {
+        a->part_bc = take((size_t)flex::ssm::group_tiles(*a) * a->T * a->G * 2 * a->N);
+        a->part_a = take(slots * DN);
+        a->part_d = take(slots * 2 * a->D);
+    }
+    return at;
+}
+size_t ssm_ws_bytes(const flex::SsmArgs& a, bool backward)
+{
+    flex::SsmArgs x = a;
+    const size_t f = ssm_layout(&x, false, nullptr), b = backward ? ssm_layout(&x, true, nullptr) : 0;
+    return f > b ? f : b;
+}
+size_t ssm_save_bytes(const flex::SsmArgs& a)
+{
+    return floats((size_t)flex::block_slots(a.T, a.n, flex::ssm::kTile) * a.D * a.N);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t flex_ssm_workspace_bytes(const flex_ssm* shape, int backward)
+{
+    flex::SsmArgs a;
+    return make_ssm(shape, false, &a) == FLEX_OK ? ssm_ws_bytes(a, backward != 0) : 0;
+}
+
+size_t flex_ssm_save_bytes(const flex_ssm* shape)
+{
+    flex::SsmArgs a;
+    return make_ssm(shape, false, &a) == FLEX_OK ? ssm_save_bytes(a) : 0;
+}
+
+int flex_ssm_fwd(const flex_ssm* shape, const void* x, const void* dt, const float* A, const void* B,
+                 const void* C, const float* D, const void* z, const float* dt_bias, const int* cu,
+                 const float* S0, float* S1, void* out, void* save, void* ws, size_t ws_bytes,
+                 void* stream)
+{
+    flex::SsmArgs a;
+    int rc = make_ssm(shape, z != nullptr, &a);
+    if (rc) return rc;
+    if (!all16({x, dt, A, B, C, out}) || !opt16({D, z, dt_bias, S0, S1}) || !offsets(cu)) return FLEX_EINVAL;
+    if (save && (S0 || !aligned(save, 256))) return FLEX_EINVAL;
+    const size_t need = ssm_layout(&a, false, nullptr);
+    if ((rc = check_ws(ws, ws_bytes, need))) return rc;
+    ssm_layout(&a, false, (char*)ws);
+    a.x = x; a.dt = dt; a.A = A; a.B = B; a.C = C; a.Ds = D; a.z = z; a.bias = dt_bias; a.cu = cu;
+    a.h0 = S0; a.h1 = S1; a.out = out; a.marks = (float*)save;
+    return counted(a.rows <= a.T ? 2 : 1, flex::launch_ssm_fwd(a, (cudaStream_t)stream));
+}
+
+int flex_ssm_bwd(const flex_ssm* shape, const void* x, const void* dt, const float* A, const void* B,
+                 const void* C, const float* D, const void* z, const float* dt_bias, const int* cu,
+                 const void* dout, const void* save, void* dx, void* ddt, float* dA, void* dB,
+                 void* dC, float* dD, void* dz, float* ddt_bias, void* ws, size_t ws_bytes,
+                 void* stream)
+{
+    flex::SsmArgs a;
+    int rc = make_ssm(shape, z != nullptr, &a);
+    if (rc) return rc;
+    if (!all16({x, dt, A, B, C, dout, dx, ddt, dA, dB, dC}) || !opt16({D, z, dt_bias, dD, dz, ddt_bias}))
+        return FLEX_EINVAL;
+    if (!offsets(cu) || !save || !aligned(save, 256)) return FLEX_EINVAL;
+    if (!D != !dD || !z != !dz || !dt_bias != !ddt_bias) return FLEX_EINVAL;
+    const size_t need = ssm_layout(&a, true, nullptr);
+    if ((rc = check_ws(ws, ws_bytes, need))) return rc;
+    ssm_layout(&a, true, (char*)ws);
+    a.x = x; a.dt = dt; a.A = A; a.B = B; a.C = C; a.Ds = D; a.z = z; a.bias = dt_bias; a.cu = cu;
+    a.marks = (float*)save; a.dout = dout;
+    a.dx = dx; a.ddt = ddt; a.dA = dA; a.dB = dB; a.dC = dC; a.dDs = dD; a.dz = dz; a.dbias = ddt_bias;
+    return counted(a.rows <= a.T ? 3 : 2, flex::launch_ssm_bwd(a, (cudaStream_t)stream));
+}
+
+int flex_ssm_decode(const flex_ssm* shape, const void* x, const void* dt, const float* A,
+                    const void* B, const void* C, const float* D, const void* z,
+                    const float* dt_bias, float* S, void* out, void* stream)
+{
+    flex::SsmArgs a;
+    const int rc = make_ssm(shape, z != nullptr, &a);
+    if (rc) return rc;
+    if (a.T != a.n) return FLEX_EINVAL;
+    if (!all16({x, dt, A, B, C, S, out}) || !opt16({D, z, dt_bias})) return FLEX_EINVAL;
+    a.x = x; a.dt = dt; a.A = A; a.B = B; a.C = C; a.Ds = D; a.z = z; a.bias = dt_bias;
+    a.h1 = S; a.out = out;
+    return counted(1, flex::launch_ssm_decode(a, (cudaStream_t)stream));
+}
+
+}  // extern "C"

@@ -26,8 +26,9 @@ EXPORTS = ("flex_strerror", "flex_workspace_bytes", "flex_featmap", "flex_linatt
            "flex_awd_workspace_bytes", "flex_awd_loss", "flex_awd_bwd_workspace_bytes",
            "flex_awd_loss_bwd", "flex_delta_workspace_bytes", "flex_delta_save_bytes",
            "flex_delta_fwd", "flex_delta_bwd", "flex_delta_decode",
-           "flex_softattn_workspace_bytes", "flex_softattn_fwd", "flex_kernel_launches", "flex_check_status",
-           "flex_debug_stall")
+           "flex_softattn_workspace_bytes", "flex_softattn_fwd", "flex_ssm_workspace_bytes",
+           "flex_ssm_save_bytes", "flex_ssm_fwd", "flex_ssm_bwd", "flex_ssm_decode",
+           "flex_kernel_launches", "flex_check_status", "flex_debug_stall")
 
 
 class FlexShape(ctypes.Structure):
@@ -38,6 +39,12 @@ class FlexShape(ctypes.Structure):
 class FlexPacked(ctypes.Structure):
     _fields_ = [(name, ctypes.c_int) for name in (
         "n", "T", "Tk", "H", "Hk", "d", "dtype", "q_stride", "k_stride", "v_stride")]
+
+
+class FlexSsm(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int) for name in (
+        "n", "T", "D", "G", "N", "dtype", "softplus", "x_stride", "dt_stride", "b_stride",
+        "c_stride", "z_stride")]
 
 
 class FlexError(RuntimeError):
@@ -95,6 +102,14 @@ def load(path: str = LIBRARY) -> ctypes.CDLL:
         lib.flex_softattn_workspace_bytes.argtypes = [pkd]
         lib.flex_softattn_workspace_bytes.restype = sz
         lib.flex_softattn_fwd.argtypes = [pkd, vp, vp, vp, vp, vp, fl, ip, vp, vp, vp, sz, vp]
+        ssm = ctypes.POINTER(FlexSsm)
+        lib.flex_ssm_workspace_bytes.argtypes = [ssm, ip]
+        lib.flex_ssm_workspace_bytes.restype = sz
+        lib.flex_ssm_save_bytes.argtypes = [ssm]
+        lib.flex_ssm_save_bytes.restype = sz
+        lib.flex_ssm_fwd.argtypes = [ssm] + [vp] * 14 + [sz, vp]
+        lib.flex_ssm_bwd.argtypes = [ssm] + [vp] * 20 + [sz, vp]
+        lib.flex_ssm_decode.argtypes = [ssm] + [vp] * 11
         lib.flex_check_status.argtypes = [vp, vp]
         lib.flex_debug_stall.argtypes = [vp, sz, ip, vp]
         lib.flex_kernel_launches.argtypes = []
@@ -102,7 +117,8 @@ def load(path: str = LIBRARY) -> ctypes.CDLL:
         for fn in (lib.flex_featmap, lib.flex_linattn_fwd, lib.flex_linattn_bwd,
                    lib.flex_linattn_decode, lib.flex_awd_loss, lib.flex_awd_loss_bwd,
                    lib.flex_delta_fwd, lib.flex_delta_bwd, lib.flex_delta_decode,
-                   lib.flex_softattn_fwd, lib.flex_check_status, lib.flex_debug_stall):
+                   lib.flex_softattn_fwd, lib.flex_ssm_fwd, lib.flex_ssm_bwd, lib.flex_ssm_decode,
+                   lib.flex_check_status, lib.flex_debug_stall):
             fn.restype = ip
         _lib = lib
         return lib
@@ -527,6 +543,138 @@ def softattn_fwd(q, k, v, cu_q, cu_k=None, causal=True, scale=None, out=None, ls
         _plain(ws, "ws", ws.shape, torch.uint8, dev), ws.numel(), _stream(stream)),
         "flex_softattn_fwd")
     return out, lse
+
+
+# ---- around the recurrence: rows [T, channels] of packed sequences ----------------------
+#
+# Activations may be slices of wider rows; parameters are fp32 and contiguous.
+
+def _row_stride(t, what, shape, dtype, dev):
+    """The row stride of a tensor of this shape and type on device `dev` whose rows are contiguous
+    (a slice of wider rows is fine)."""
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError(f"{what}: {tuple(t.shape)} {t.dtype}, not {tuple(shape)} {dtype}")
+    if t.get_device() != dev:
+        raise ValueError(f"{what}: not on the current CUDA device")
+    if t.is_contiguous():
+        return t[0].numel()
+    if not t[0].is_contiguous():
+        raise ValueError(f"{what}: rows of contiguous elements")
+    row = t.stride(0)
+    if row >= 2 ** 31:
+        raise ValueError(f"{what}: row stride {row}")
+    return row if t.shape[0] > 1 else t[0].numel()
+
+
+def _packed_ssm(x, dt, B, C, z, n, softplus, dev):
+    if x.dim() != 2 or B.dim() != 3:
+        raise ValueError("x: rows [T, D]; B: rows [T, G, N]")
+    (T, D), (_, G, N), ty = x.shape, B.shape, x.dtype
+    if T == 0:
+        raise ValueError("x: no rows")
+    bc = (T, G, N)
+    return FlexSsm(n, T, D, G, N, _dtype_code(x), int(bool(softplus)),
+                   _row_stride(x, "x", (T, D), ty, dev), _row_stride(dt, "dt", (T, D), ty, dev),
+                   _row_stride(B, "B", bc, ty, dev), _row_stride(C, "C", bc, ty, dev),
+                   0 if z is None else _row_stride(z, "z", (T, D), ty, dev))
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+def ssm_workspace(x, B, cu, backward=False) -> torch.Tensor:
+    """A caller-owned workspace for ssm_fwd (backward: for ssm_bwd too) on such tensors."""
+    shape = _packed_ssm(x, x, B, B, None, cu.numel() - 1, True, torch.cuda.current_device())
+    return _workspace(int(load().flex_ssm_workspace_bytes(ctypes.byref(shape), int(bool(backward)))),
+                      "flex_ssm_workspace_bytes", x.device)
+
+
+def ssm_save(x, B, cu) -> torch.Tensor:
+    """The buffer in which ssm_fwd leaves what ssm_bwd needs (not initialised)."""
+    shape = _packed_ssm(x, x, B, B, None, cu.numel() - 1, True, torch.cuda.current_device())
+    n = int(load().flex_ssm_save_bytes(ctypes.byref(shape)))
+    if n == 0:
+        raise FlexError(FLEX_EUNSUPPORTED, "flex_ssm_save_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=x.device)
+
+
+def _ssm_saved(save, shape, dev):
+    if save.numel() < load().flex_ssm_save_bytes(ctypes.byref(shape)):
+        raise FlexError(FLEX_EWORKSPACE, "save")
+    return _plain(save, "save", save.shape, torch.uint8, dev)
+
+
+def ssm_fwd(x, dt, A, B, C, cu, D=None, z=None, dt_bias=None, softplus=True, state=None, out=None,
+            last_state=None, want_state=True, save=None, ws=None, stream=None):
+    """Selective state space scan over packed sequences: (out [T, D], last state [n, D, N] fp32 or
+    None).  x, dt, z (gate) [T, D]; B, C [T, G, N]; A [D, N], D (skip), dt_bias [D] fp32; cu int32
+    [n + 1].  state: the sequences' first state (default zero; last_state may be the same tensor).
+    save: an ssm_save() buffer for ssm_bwd (then without `state`)."""
+    dev, f32 = torch.cuda.current_device(), torch.float32
+    cu_ptr, n = _offsets(cu, "cu", dev), cu.numel() - 1
+    shape = _packed_ssm(x, dt, B, C, z, n, softplus, dev)
+    st = (n, shape.D, shape.N)
+    if out is None:
+        out = _new(stream, x.shape, x.dtype, x.device)
+    if last_state is None and want_state:
+        last_state = _new(stream, st, f32, x.device)
+    if ws is None:
+        ws = _scratch(stream, ssm_workspace, x, B, cu)
+    _check(load().flex_ssm_fwd(
+        ctypes.byref(shape), x.data_ptr(), dt.data_ptr(), _plain(A, "A", st[1:], f32, dev),
+        B.data_ptr(), C.data_ptr(), _plain(D, "D", st[1:2], f32, dev), _at(z),
+        _plain(dt_bias, "dt_bias", st[1:2], f32, dev), cu_ptr, _plain(state, "state", st, f32, dev),
+        _plain(last_state, "last_state", st, f32, dev), _plain(out, "out", x.shape, x.dtype, dev),
+        None if save is None else _ssm_saved(save, shape, dev),
+        _plain(ws, "ws", ws.shape, torch.uint8, dev), ws.numel(), _stream(stream)), "flex_ssm_fwd")
+    return out, last_state
+
+
+def ssm_bwd(x, dt, A, B, C, cu, dout, save, D=None, z=None, dt_bias=None, softplus=True, dx=None,
+            ddt=None, dA=None, dB=None, dC=None, dD=None, dz=None, ddt_bias=None, ws=None,
+            stream=None):
+    """(dx, ddt, dA, dB, dC, dD, dz, ddt_bias) of L = sum(dout * out) of ssm_fwd, which filled
+    `save`; dD, dz and ddt_bias are None where D, z and dt_bias are."""
+    dev, f32, ty = torch.cuda.current_device(), torch.float32, x.dtype
+    cu_ptr = _offsets(cu, "cu", dev)
+    shape = _packed_ssm(x, dt, B, C, z, cu.numel() - 1, softplus, dev)
+    T, d = x.shape
+    inputs = (x, dt, A, B, C, D, z, dt_bias)
+    names = ("dx", "ddt", "dA", "dB", "dC", "dD", "dz", "ddt_bias")
+    shapes = ((T, d), (T, d), (d, shape.N), B.shape, B.shape, (d,), (T, d), (d,))
+    types = (ty, ty, f32, ty, ty, f32, ty, f32)
+    grads = [_new(stream, s, t, x.device) if g is None and i is not None else g for g, i, s, t in zip(
+        (dx, ddt, dA, dB, dC, dD, dz, ddt_bias), inputs, shapes, types)]
+    if ws is None:
+        ws = _scratch(stream, ssm_workspace, x, B, cu, backward=True)
+    _check(load().flex_ssm_bwd(
+        ctypes.byref(shape), x.data_ptr(), dt.data_ptr(), _plain(A, "A", (d, shape.N), f32, dev),
+        B.data_ptr(), C.data_ptr(), _plain(D, "D", (d,), f32, dev), _at(z),
+        _plain(dt_bias, "dt_bias", (d,), f32, dev), cu_ptr, _plain(dout, "dout", (T, d), ty, dev),
+        _ssm_saved(save, shape, dev),
+        *(_plain(g, w, s, t, dev) for g, w, s, t in zip(grads, names, shapes, types)),
+        _plain(ws, "ws", ws.shape, torch.uint8, dev), ws.numel(), _stream(stream)), "flex_ssm_bwd")
+    return tuple(grads)
+
+
+def ssm_decode(x, dt, A, B, C, S, D=None, z=None, dt_bias=None, softplus=True, out=None,
+               stream=None):
+    """One token of each sequence: x, dt, z [n, D]; B, C [n, G, N]; the state S [n, D, N] fp32 is
+    updated in place.  Returns out [n, D]."""
+    dev, f32 = torch.cuda.current_device(), torch.float32
+    shape = _packed_ssm(x, dt, B, C, z, x.shape[0], softplus, dev)
+    st = (x.shape[0], shape.D, shape.N)
+    if out is None:
+        out = _new(stream, x.shape, x.dtype, x.device)
+    rc = load().flex_ssm_decode(
+        ctypes.byref(shape), x.data_ptr(), dt.data_ptr(), _plain(A, "A", st[1:], f32, dev),
+        B.data_ptr(), C.data_ptr(), _plain(D, "D", st[1:2], f32, dev), _at(z),
+        _plain(dt_bias, "dt_bias", st[1:2], f32, dev), _plain(S, "S", st, f32, dev),
+        _plain(out, "out", x.shape, x.dtype, dev), _stream(stream))
+    if rc:
+        raise FlexError(rc, "flex_ssm_decode")
+    return out
 
 
 def check_status(ws, stream=None):
