@@ -36,10 +36,10 @@ def _ssm(**kw):
     return FlexSsm(*(x[name] for name, _ in FlexSsm._fields_))
 
 
-def _call(f, names, s, n=BIG, ws=True, **kw):
+def _call(f, names, s, n=BIG, scratch=True, **kw):
     given = {"S0": None, "save": P if "dout" in names else None}
     args = [kw.get(name, given.get(name, P)) for name in names]
-    return f(ctypes.byref(s) if s else None, *args, *([n, None] if ws else [None]))
+    return f(ctypes.byref(s) if s else None, *args, *([n, None] if scratch else [None]))
 
 
 def _fwd(lib, s, **kw):
@@ -51,7 +51,7 @@ def _bwd(lib, s, **kw):
 
 
 def _token(lib, s, **kw):
-    return _call(lib.flex_ssm_decode, TOKEN, s, ws=False, **kw)
+    return _call(lib.flex_ssm_decode, TOKEN, s, scratch=False, **kw)
 
 
 @pytest.mark.parametrize("kw", [dict(n=0), dict(T=0), dict(D=0), dict(G=0), dict(N=0), dict(G=3),
