@@ -34,6 +34,7 @@ struct SsmArgs {  // (declared in flex_internal.h)
 namespace ssm {
 
 constexpr int kTile = 16;  // tokens staged at a time, and between two marks
+constexpr int kSMs = 152;  // of a GB300: a workspace's size is to depend on the shape alone
 
 // A thread holds 4 states of one channel; L = N / 4 lanes hold a channel.  Blocks of 64 channels,
 // or 32 where a channel takes 8 lanes and more.

@@ -333,7 +333,7 @@ cudaError_t decode_n(const SsmArgs& a, cudaStream_t s)
 // that as many blocks as that are there.
 int ssm_rows(const SsmArgs& a, bool backward)
 {
-    const long long tiles = (long long)group_tiles(a) * a.G, want = 2LL * tc::sm_count();
+    const long long tiles = (long long)group_tiles(a) * a.G, want = 2LL * kSMs;
     if (!backward && a.n * tiles >= want) return a.T + 1;
     long long rows = (a.T * tiles + want - 1) / want;
     rows = (rows + 4 * kTile - 1) / (4 * kTile) * (4 * kTile);
