@@ -228,7 +228,7 @@ def _run_own(st):
         if call == "norm_fwd":
             return outs
         dx, dres, dz, dw, dscale = flexattn.norm_bwd(
-            st["x"], st["w"], rstd, st["dout"], z=st["z"], total=total, scale=st["scale"],
+            st["x"], st["w"], rstd, st["dout"], z=st["z"], res=st["res"], scale=st["scale"],
             dtotal=st.get("dsum"))
         return (*outs, *(g for g in (dx, dres, dz, dw, dscale) if g is not None))
     x = [st[n] for n in ("x", "delta", "A", "B", "C")]
