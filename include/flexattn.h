@@ -374,6 +374,74 @@ int flex_ssm_decode(const flex_ssm* shape, const void* x, const void* dt, const 
                     const void* B, const void* C, const float* D, const void* z,
                     const float* dt_bias, float* S, void* out, void* stream);
 
+typedef struct {
+    int n;         /* sequences, >= 1 */
+    int T;         /* rows, >= 1 */
+    int D;         /* channels, whole 16-byte units */
+    int W;         /* taps: 2, 3 or 4 */
+    int dtype;     /* flex_dtype of every activation */
+    int silu;      /* 1: out = silu(pre), 0: out = pre */
+    int x_stride;
+} flex_conv;
+
+/* Short causal convolution, channel by channel, over whole sequences:
+ *   pre_t[c] = bias[c] + sum_j w[c][j] x_{t - (W - 1) + j}[c],  out_t = silu(pre_t) or pre_t.
+ * x, out: [T][D]; w: [D][W], bias: NULL or [D], fp32; cu: offsets.  The rows ahead of a sequence's
+ * first are those of S0 (NULL: zeros), [n][W - 1][D] in shape->dtype, oldest first; S1: NULL or the
+ * same, receives each sequence's last W - 1 rows (with what S0 holds where it has fewer), and is
+ * another buffer than S0.  One kernel.  Errors: FLEX_EINVAL, FLEX_EUNSUPPORTED (W, D, or more than
+ * 65535 sequences or 65536 channels). */
+int flex_conv_fwd(const flex_conv* shape, const void* x, const float* w, const float* bias,
+                  const int* cu, const void* S0, void* S1, void* out, void* stream);
+
+/* Gradients of L = sum(dout * out) of flex_conv_fwd without S0: dx [T][D], dw [D][W], dbias [D] (given
+ * exactly when bias is).  ws: flex_conv_workspace_bytes() bytes (0 if the shape is invalid or
+ * unsupported).  Sums have a fixed order: results repeat bit for bit.  2 kernels. */
+size_t flex_conv_workspace_bytes(const flex_conv* shape);
+int flex_conv_bwd(const flex_conv* shape, const void* x, const float* w, const float* bias,
+                  const int* cu, const void* dout, void* dx, float* dw, float* dbias, void* ws,
+                  size_t ws_bytes, void* stream);
+
+/* One token of every sequence: row i of x and out (T == n; no offsets), on the caller's state S
+ * [n][W - 1][D], which moves on by that row.  One kernel. */
+int flex_conv_decode(const flex_conv* shape, const void* x, const float* w, const float* bias,
+                     void* S, void* out, void* stream);
+
+typedef struct {
+    int T;          /* rows, >= 1 */
+    int H;          /* heads */
+    int d;          /* elements that a norm is taken over: whole 16-byte units, at most 8192 */
+    int dtype;      /* flex_dtype of every activation */
+    int heads;      /* of the parameters: H, or 1 that all heads share */
+    int x_stride;
+    int z_stride;   /* (where z is given) */
+    int res_stride; /* (where res is given) */
+    float eps;
+} flex_norm;
+
+/* Root-mean-square norm of every row and head, behind a block with its gate, or ahead of the next
+ * one with the residual sum:
+ *   r = x, or res + scale * x;  out = r (mean(r^2) + eps)^(-1/2) w, times silu(z) where z is given.
+ * x, z, res, out: [T][H][d]; w, scale: [heads][d] fp32; z, res and scale (only with res) may be NULL.
+ * total: [T][H][d], receives r (given exactly when res is; may be res itself, not a slice of it), of
+ * which out is computed before it is rounded.  rstd: NULL or [T][H] fp32, for flex_norm_bwd.
+ * end: NULL, or a device int (cu + n, say): only rows ahead of it are read and written.  One kernel.
+ * Errors: FLEX_EINVAL, FLEX_EUNSUPPORTED (d, more than 1024 heads, or 2^31 rows of heads). */
+int flex_norm_fwd(const flex_norm* shape, const void* x, const float* w, const void* z,
+                  const void* res, const float* scale, const int* end, void* out, void* total,
+                  float* rstd, void* stream);
+
+/* Gradients of L = sum(dout * out) + sum(dtotal * total): dx, dres, dz [T][H][d], dw, dscale [heads][d].
+ * rstd: of flex_norm_fwd with the same inputs.  dtotal: NULL (zeros) or [T][H][d].  dres, dz and
+ * dscale are given exactly when res, z and scale are; dx always but with res and no scale, when dres
+ * is it.  ws: flex_norm_workspace_bytes() bytes (0 if the shape is invalid or unsupported).  Sums have
+ * a fixed order: results repeat bit for bit.  2 kernels. */
+size_t flex_norm_workspace_bytes(const flex_norm* shape);
+int flex_norm_bwd(const flex_norm* shape, const void* x, const float* w, const void* z,
+                  const void* res, const float* scale, const int* end, const float* rstd,
+                  const void* dout, const void* dtotal, void* dx, void* dres, void* dz, float* dw,
+                  float* dscale, void* ws, size_t ws_bytes, void* stream);
+
 /* Cumulative number of kernels this library has enqueued in this process (all entry
  * points, all devices).  Lets a caller count the launches inside a timed region. */
 unsigned long long flex_kernel_launches(void);

@@ -1,0 +1,384 @@
+// Short causal convolution over packed sequences, channel by channel:
+//   pre_t = b + sum_j w_j x_{t - (W - 1) + j},  out_t = silu(pre_t) or pre_t,
+// rows ahead of a sequence's first being its state's (the last W - 1 rows of what came before) or 0.
+//
+// A thread walks a run of rows of 16 bytes of channels (backward: 4 channels) with the last rows in
+// registers, so every row is read once but for the W - 1 ahead of each run; runs are cut from all
+// rows alike, whatever the sequences.  Bound by DRAM: x read once and out written once.
+#include "flex_internal.h"
+#include "layer.cuh"
+
+namespace flex {
+namespace {
+
+// The sequence that row t lies in (t < cu[n]): the last that starts at or before it.
+__device__ __forceinline__ int find_row(const int* cu, int n, int t)
+{
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (__ldg(cu + mid) <= t) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+__device__ __forceinline__ int rows_end(const int* cu, int n, int T) { return min(max(__ldg(cu + n), 0), T); }
+
+constexpr int kAhead = 4;  // rows whose loads are in flight together
+
+template <typename T, int W>
+__global__ void __launch_bounds__(128) conv_fwd_kernel(ConvArgs a, long long runs, long long run_blocks)
+{
+    constexpr int V = Pack<T>::N;
+    const int CV = a.D / V;
+    const T* x = (const T*)a.x;
+    if (blockIdx.x >= run_blocks) {  // the sequences' last rows
+        const long long i = (blockIdx.x - run_blocks) * 128 + threadIdx.x;
+        const long long row = i / CV;
+        const int c = (int)(i % CV) * V, s = (int)(row / (W - 1)), j = (int)(row % (W - 1));
+        if (s >= a.n) return;
+        int lo, hi;
+        seq_rows(a.cu, s, a.T, lo, hi);
+        const int t = hi - (W - 1) + j;
+        Pack<T> v;
+        v.zero();
+        if (t >= lo) v.load(x + (long long)t * a.xs + c);
+        else if (a.S0) v.load((const T*)a.S0 + ((long long)s * (W - 1) + (t - lo + W - 1)) * a.D + c);
+        v.store((T*)a.S1 + row * a.D + c);
+        return;
+    }
+    const long long i = blockIdx.x * 128LL + threadIdx.x;
+    const int c = (int)(i % CV) * V;
+    const int end = rows_end(a.cu, a.n, a.T);
+    const long long first = i / CV * a.run;
+    if (first >= end) return;
+    const int t0 = (int)first, t1 = min(end, t0 + a.run);
+    int s = find_row(a.cu, a.n, t0), lo, hi;
+    seq_rows(a.cu, s, a.T, lo, hi);
+    float w[W][V], b[V], win[W - 1][V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        b[k] = a.bias ? a.bias[c + k] : 0.f;
+#pragma unroll
+        for (int j = 0; j < W; ++j) w[j][k] = a.w[(size_t)(c + k) * W + j];
+    }
+    // the rows ahead of row t of sequence s
+    auto before = [&](int t) {
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) {
+            const int u = t - (W - 1) + j;
+            Pack<T> v;
+            v.zero();
+            if (u >= lo) v.load(x + (long long)u * a.xs + c);
+            else if (a.S0) v.load((const T*)a.S0 + ((long long)s * (W - 1) + (u - lo + W - 1)) * a.D + c);
+            v.get(win[j]);
+        }
+    };
+    Pack<T> next[kAhead];
+    auto load = [&](int t) {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (t + k < t1) next[k].load(x + (long long)(t + k) * a.xs + c);
+    };
+    load(t0);
+    before(t0);
+    for (int t = t0; t < t1; t += kAhead) {
+        Pack<T> now[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) now[k] = next[k];
+        if (t + kAhead < t1) load(t + kAhead);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (t + k >= t1) break;
+            if (t + k >= hi && s + 1 < a.n) {  // the next sequence that has rows
+                do {
+                    ++s;
+                    seq_rows(a.cu, s, a.T, lo, hi);
+                } while (t + k >= hi && s + 1 < a.n);
+                before(t + k);
+            }
+            float v[V], y[V];
+            now[k].get(v);
+#pragma unroll
+            for (int q = 0; q < V; ++q) {
+                float p = b[q];
+#pragma unroll
+                for (int j = 0; j < W - 1; ++j) p = fmaf(w[j][q], win[j][q], p);
+                p = fmaf(w[W - 1][q], v[q], p);
+                y[q] = a.silu ? p * logistic(p) : p;
+#pragma unroll
+                for (int j = 0; j + 1 < W - 1; ++j) win[j][q] = win[j + 1][q];
+                win[W - 2][q] = v[q];
+            }
+            Pack<T> o;
+            o.set(y);
+            o.store((T*)a.out + (long long)(t + k) * a.D + c);
+        }
+    }
+}
+
+// Gradients: dpre_t = dout_t silu'(pre_t), dx_t = sum_j w_j dpre_{t + (W - 1) - j} within the
+// sequence, dw_j = sum_t dpre_t x_{t - (W - 1) + j}, db = sum_t dpre_t.  A thread walks its run and the
+// W - 1 rows behind it, whose dpre its last rows' dx wants; dw and db are summed over a block's 8 runs
+// in their order, and over blocks by a kernel of their own.
+template <typename T, int W>
+__global__ void __launch_bounds__(256) conv_bwd_kernel(ConvArgs a)
+{
+    __shared__ float4 sums[8][W + 1][32];
+    const int c = (blockIdx.x * 32 + threadIdx.x) * 4;
+    const bool mine = c < a.D;
+    const int end = rows_end(a.cu, a.n, a.T);
+    const long long first = ((long long)blockIdx.y * 8 + threadIdx.y) * a.run;
+    const T *x = (const T*)a.x, *dout = (const T*)a.dout;
+    float dw[W][4] = {}, db[4] = {};
+    if (mine && first < end) {
+        const int t0 = (int)first, t1 = min(end, t0 + a.run), t2 = min(end, t1 + W - 1);
+        int s = find_row(a.cu, a.n, t0), lo, hi;
+        seq_rows(a.cu, s, a.T, lo, hi);
+        float w[W][4], b[4], win[W - 1][4], acc[W][4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            b[k] = a.bias ? a.bias[c + k] : 0.f;
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                w[j][k] = a.w[(size_t)(c + k) * W + j];
+                acc[j][k] = 0.f;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) {
+            const int u = t0 - (W - 1) + j;
+            const float4 v = u >= lo ? load4(x + (long long)u * a.xs + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+            win[j][0] = v.x; win[j][1] = v.y; win[j][2] = v.z; win[j][3] = v.w;
+        }
+        float4 nx[kAhead], nd[kAhead];
+        auto load = [&](int t) {
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                nx[k] = nd[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (t + k < t2) {
+                    nx[k] = load4(x + (long long)(t + k) * a.xs + c);
+                    nd[k] = load4(dout + (long long)(t + k) * a.D + c);
+                }
+            }
+        };
+        load(t0);
+        for (int t = t0; t < t1 + W - 1; t += kAhead) {
+            float4 px[kAhead], pd[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) { px[k] = nx[k]; pd[k] = nd[k]; }
+            if (t + kAhead < t2) load(t + kAhead);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const int u = t + k;
+                if (u >= t1 + W - 1) break;
+                if (u < t2) {
+                    if (u >= hi && s + 1 < a.n) {
+                        do {
+                            ++s;
+                            seq_rows(a.cu, s, a.T, lo, hi);
+                        } while (u >= hi && s + 1 < a.n);
+#pragma unroll
+                        for (int j = 0; j < W - 1; ++j) win[j][0] = win[j][1] = win[j][2] = win[j][3] = 0.f;
+                    }
+                    const float v[4] = {px[k].x, px[k].y, px[k].z, px[k].w};
+                    const float g[4] = {pd[k].x, pd[k].y, pd[k].z, pd[k].w};
+                    const bool own = u < t1;
+                    const int at = u - lo;  // rows of the sequence ahead of this one
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        float p = b[q];
+#pragma unroll
+                        for (int j = 0; j < W - 1; ++j) p = fmaf(w[j][q], win[j][q], p);
+                        p = fmaf(w[W - 1][q], v[q], p);
+                        float dp = g[q];
+                        if (a.silu) {
+                            const float l = logistic(p);
+                            dp *= l * fmaf(p, 1.f - l, 1.f);
+                        }
+                        if (own) {
+                            db[q] += dp;
+#pragma unroll
+                            for (int j = 0; j < W - 1; ++j) dw[j][q] = fmaf(dp, win[j][q], dw[j][q]);
+                            dw[W - 1][q] = fmaf(dp, v[q], dw[W - 1][q]);
+                        }
+#pragma unroll
+                        for (int j = 0; j < W; ++j)
+                            if (W - 1 - j <= at) acc[j][q] = fmaf(w[j][q], dp, acc[j][q]);
+#pragma unroll
+                        for (int j = 0; j + 1 < W - 1; ++j) win[j][q] = win[j + 1][q];
+                        win[W - 2][q] = v[q];
+                    }
+                }
+                const int done = u - (W - 1);  // nothing more is added to this row's dx
+                if (done >= t0)
+                    store4((T*)a.dx + (long long)done * a.D + c,
+                           make_float4(acc[0][0], acc[0][1], acc[0][2], acc[0][3]));
+#pragma unroll
+                for (int j = 0; j + 1 < W; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) acc[j][q] = acc[j + 1][q];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) acc[W - 1][q] = 0.f;
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < W; ++j)
+        sums[threadIdx.y][j][threadIdx.x] = make_float4(dw[j][0], dw[j][1], dw[j][2], dw[j][3]);
+    sums[threadIdx.y][W][threadIdx.x] = make_float4(db[0], db[1], db[2], db[3]);
+    __syncthreads();
+    if (threadIdx.y <= W && mine) {
+        float4 v = sums[0][threadIdx.y][threadIdx.x];
+#pragma unroll
+        for (int k = 1; k < 8; ++k) {
+            const float4 u = sums[k][threadIdx.y][threadIdx.x];
+            v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+        }
+        // dw as [D][W], then db: columns of a matrix of one row a block
+        float* to = a.part + (size_t)blockIdx.y * (W + 1) * a.D;
+        const float f[4] = {v.x, v.y, v.z, v.w};
+        const int j = threadIdx.y;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if (j < W) to[(size_t)(c + q) * W + j] = f[q];
+            else to[(size_t)a.D * W + c + q] = f[q];
+        }
+    }
+}
+
+// One row of every sequence, the state moved on by it.
+template <typename T, int W>
+__global__ void __launch_bounds__(128) conv_decode_kernel(ConvArgs a)
+{
+    constexpr int V = Pack<T>::N;
+    const int CV = a.D / V;
+    const long long i = blockIdx.x * 128LL + threadIdx.x;
+    const long long s = i / CV;
+    const int c = (int)(i % CV) * V;
+    if (s >= a.n) return;
+    T* state = (T*)a.S1 + s * (W - 1) * a.D + c;
+    Pack<T> rows[W];
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) rows[j].load(state + (long long)j * a.D);
+    rows[W - 1].load((const T*)a.x + s * a.xs + c);
+    float p[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) p[k] = a.bias ? a.bias[c + k] : 0.f;
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+        float v[V];
+        rows[j].get(v);
+#pragma unroll
+        for (int k = 0; k < V; ++k) p[k] = fmaf(a.w[(size_t)(c + k) * W + j], v[k], p[k]);
+    }
+    if (a.silu)
+#pragma unroll
+        for (int k = 0; k < V; ++k) p[k] *= logistic(p[k]);
+    Pack<T> o;
+    o.set(p);
+    o.store((T*)a.out + s * a.D + c);
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) rows[j + 1].store(state + (long long)j * a.D);
+}
+
+constexpr int kSlices = 16;
+__global__ void __launch_bounds__(32 * kSlices) column_sums_kernel(const float* from, int cols, int split,
+                                                                   int step, int count, float* to0, float* to1)
+{
+    __shared__ float4 sums[kSlices][32];
+    tc::grid_dep_wait();
+    const int c = (blockIdx.x * 32 + threadIdx.x) * 4;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (c < cols) {
+#pragma unroll 4
+        for (int k = threadIdx.y; k < count; k += kSlices) {
+            const float4 u = *(const float4*)(from + (size_t)(blockIdx.y + (size_t)k * step) * cols + c);
+            v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+        }
+    }
+    sums[threadIdx.y][threadIdx.x] = v;
+    __syncthreads();
+    if (threadIdx.y || c >= cols) return;
+#pragma unroll
+    for (int k = 1; k < kSlices; ++k) {
+        const float4 u = sums[k][threadIdx.x];
+        v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+    }
+    if (c < split) *(float4*)(to0 + (size_t)blockIdx.y * split + c) = v;
+    else if (to1) *(float4*)(to1 + (size_t)blockIdx.y * (cols - split) + c - split) = v;
+}
+
+template <typename T, int W>
+cudaError_t fwd(const ConvArgs& a, cudaStream_t s)
+{
+    const int CV = a.D / Pack<T>::N;
+    const long long runs = (a.T + a.run - 1) / a.run, blocks = (runs * CV + 127) / 128;
+    const long long more = a.S1 ? ((long long)a.n * (W - 1) * CV + 127) / 128 : 0;
+    return tc::launch_after(conv_fwd_kernel<T, W>, dim3((unsigned)(blocks + more)), 128, 0, 0, false, s, a,
+                            runs, blocks);
+}
+template <typename T, int W>
+cudaError_t bwd(const ConvArgs& a, cudaStream_t s)
+{
+    const int rows = conv_bwd_blocks(a);
+    conv_bwd_kernel<T, W><<<dim3((a.D + 127) / 128, rows), dim3(32, 8), 0, s>>>(a);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    return launch_column_sums(a.part, (W + 1) * a.D, W * a.D, 1, 1, rows, a.dw, a.dbias, s);
+}
+template <typename T, int W>
+cudaError_t decode(const ConvArgs& a, cudaStream_t s)
+{
+    const long long items = (long long)a.n * (a.D / Pack<T>::N);
+    return tc::launch_after(conv_decode_kernel<T, W>, dim3((unsigned)((items + 127) / 128)), 128, 0, 0, false,
+                            s, a);
+}
+
+enum What { kFwd, kBwd, kDecode };
+template <typename T, int W>
+cudaError_t call(const ConvArgs& a, What what, cudaStream_t s)
+{
+    return what == kFwd ? fwd<T, W>(a, s) : what == kBwd ? bwd<T, W>(a, s) : decode<T, W>(a, s);
+}
+template <typename T>
+cudaError_t call_w(const ConvArgs& a, What what, cudaStream_t s)
+{
+    return a.W == 2 ? call<T, 2>(a, what, s) : a.W == 3 ? call<T, 3>(a, what, s) : call<T, 4>(a, what, s);
+}
+cudaError_t call_t(const ConvArgs& a, What what, cudaStream_t s)
+{
+    return a.bf16 ? call_w<__nv_bfloat16>(a, what, s) : call_w<float>(a, what, s);
+}
+
+}  // namespace
+
+cudaError_t launch_column_sums(const float* from, int cols, int split, int sums, int step, int count,
+                               float* to0, float* to1, cudaStream_t s)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((cols + 127) / 128), (unsigned)sums);
+    cfg.blockDim = dim3(32, kSlices);
+    cfg.stream = s;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, column_sums_kernel, from, cols, split, step, count, to0, to1);
+}
+
+// Rows of a thread's run: long ones read fewer rows twice, short ones fill the SMs.
+int conv_run(const ConvArgs& a, bool backward)
+{
+    const long long lanes = backward ? a.D / 4 : a.D / (a.bf16 ? 8 : 4), want = 152LL * 1024;
+    int run = 32;
+    while (run > 4 && (a.T + run - 1) / run * lanes < want) run /= 2;
+    return run;
+}
+int conv_bwd_blocks(const ConvArgs& a) { return (a.T + 8 * a.run - 1) / (8 * a.run); }
+
+cudaError_t launch_conv_fwd(const ConvArgs& a, cudaStream_t s) { return call_t(a, kFwd, s); }
+cudaError_t launch_conv_bwd(const ConvArgs& a, cudaStream_t s) { return call_t(a, kBwd, s); }
+cudaError_t launch_conv_decode(const ConvArgs& a, cudaStream_t s) { return call_t(a, kDecode, s); }
+
+}  // namespace flex

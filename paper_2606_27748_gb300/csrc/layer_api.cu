@@ -1,6 +1,7 @@
 // Host side of the entry points around the recurrence (include/flexattn.h): argument checks,
 // workspace layout and dispatch.  Nothing here allocates device memory or synchronises.
 #include "flex_internal.h"
+#include "layer.cuh"
 #include "ssm.cuh"
 
 #include <initializer_list>
@@ -82,7 +83,7 @@ size_t ssm_layout(flex::SsmArgs* a, bool backward, char* ws)
         a->sums = take(slots * a->D);
     }
     if (backward) {
-        a->part_bc = take((size_t)flex::ssm::group_tiles(*a) * a->T * a->G * 2 * a->N);
+        a->part_bc = take((size_t)flex::ssm_bwd_tiles(*a) * a->T * a->G * 2 * a->N);
         a->part_a = take(slots * DN);
         a->part_d = take(slots * 2 * a->D);
     }
@@ -97,6 +98,42 @@ size_t ssm_ws_bytes(const flex::SsmArgs& a, bool backward)
 size_t ssm_save_bytes(const flex::SsmArgs& a)
 {
     return floats((size_t)flex::block_slots(a.T, a.n, flex::ssm::kTile) * a.D * a.N);
+}
+
+int make_conv(const flex_conv* s, flex::ConvArgs* a)
+{
+    if (!s || s->n < 1 || s->T < 1 || s->D < 1 || s->W < 1) return FLEX_EINVAL;
+    if (s->dtype != FLEX_F32 && s->dtype != FLEX_BF16) return FLEX_EINVAL;
+    if (s->W < 2 || s->W > 4 || s->D % unit(s->dtype)) return FLEX_EUNSUPPORTED;
+    if (s->n > 65535 || s->T > (1 << 30) || s->D > 65536) return FLEX_EUNSUPPORTED;
+    if (!strides(s->dtype, {s->x_stride}, s->D)) return FLEX_EINVAL;
+    *a = {};
+    a->n = s->n; a->T = s->T; a->D = s->D; a->W = s->W;
+    a->bf16 = s->dtype == FLEX_BF16; a->silu = s->silu != 0; a->xs = s->x_stride;
+    return FLEX_OK;
+}
+size_t conv_ws_bytes(flex::ConvArgs* a)
+{
+    a->run = flex::conv_run(*a, true);
+    return kHeader + floats((size_t)flex::conv_bwd_blocks(*a) * (a->W + 1) * a->D);
+}
+
+int make_norm(const flex_norm* s, bool z, bool res, flex::NormArgs* a)
+{
+    if (!s || s->T < 1 || s->H < 1 || s->d < 1 || !(s->eps >= 0.f)) return FLEX_EINVAL;
+    if (s->dtype != FLEX_F32 && s->dtype != FLEX_BF16) return FLEX_EINVAL;
+    if (s->heads != 1 && s->heads != s->H) return FLEX_EINVAL;
+    if (s->d % unit(s->dtype) || s->d > 8192) return FLEX_EUNSUPPORTED;
+    if (s->T > (1 << 30) || s->H > 1024 || (long long)s->T * s->H >= 1LL << 31) return FLEX_EUNSUPPORTED;
+    const int row = s->H * s->d;
+    if (!strides(s->dtype, {s->x_stride}, row)) return FLEX_EINVAL;
+    if (z && !strides(s->dtype, {s->z_stride}, row)) return FLEX_EINVAL;
+    if (res && !strides(s->dtype, {s->res_stride}, row)) return FLEX_EINVAL;
+    *a = {};
+    a->T = s->T; a->H = s->H; a->d = s->d; a->heads = s->heads; a->eps = s->eps;
+    a->bf16 = s->dtype == FLEX_BF16;
+    a->xs = s->x_stride; a->zs = s->z_stride; a->rs = s->res_stride;
+    return FLEX_OK;
 }
 
 }  // namespace
@@ -167,6 +204,94 @@ int flex_ssm_decode(const flex_ssm* shape, const void* x, const void* dt, const 
     a.x = x; a.dt = dt; a.A = A; a.B = B; a.C = C; a.Ds = D; a.z = z; a.bias = dt_bias;
     a.h1 = S; a.out = out;
     return counted(1, flex::launch_ssm_decode(a, (cudaStream_t)stream));
+}
+
+size_t flex_conv_workspace_bytes(const flex_conv* shape)
+{
+    flex::ConvArgs a;
+    return make_conv(shape, &a) == FLEX_OK ? conv_ws_bytes(&a) : 0;
+}
+
+int flex_conv_fwd(const flex_conv* shape, const void* x, const float* w, const float* bias,
+                  const int* cu, const void* S0, void* S1, void* out, void* stream)
+{
+    flex::ConvArgs a;
+    const int rc = make_conv(shape, &a);
+    if (rc) return rc;
+    if (!all16({x, w, out}) || !opt16({bias, S0, S1}) || !offsets(cu)) return FLEX_EINVAL;
+    if (S0 && S0 == S1) return FLEX_EINVAL;
+    a.x = x; a.w = w; a.bias = bias; a.cu = cu; a.S0 = S0; a.S1 = S1; a.out = out;
+    a.run = flex::conv_run(a, false);
+    return counted(1, flex::launch_conv_fwd(a, (cudaStream_t)stream));
+}
+
+int flex_conv_bwd(const flex_conv* shape, const void* x, const float* w, const float* bias,
+                  const int* cu, const void* dout, void* dx, float* dw, float* dbias, void* ws,
+                  size_t ws_bytes, void* stream)
+{
+    flex::ConvArgs a;
+    int rc = make_conv(shape, &a);
+    if (rc) return rc;
+    if (!all16({x, w, dout, dx, dw}) || !opt16({bias, dbias}) || !offsets(cu)) return FLEX_EINVAL;
+    if (!bias != !dbias) return FLEX_EINVAL;
+    const size_t need = conv_ws_bytes(&a);
+    if ((rc = check_ws(ws, ws_bytes, need))) return rc;
+    a.x = x; a.w = w; a.bias = bias; a.cu = cu; a.dout = dout; a.dx = dx; a.dw = dw; a.dbias = dbias;
+    a.part = (float*)((char*)ws + kHeader);
+    return counted(2, flex::launch_conv_bwd(a, (cudaStream_t)stream));
+}
+
+int flex_conv_decode(const flex_conv* shape, const void* x, const float* w, const float* bias,
+                     void* S, void* out, void* stream)
+{
+    flex::ConvArgs a;
+    const int rc = make_conv(shape, &a);
+    if (rc) return rc;
+    if (a.T != a.n) return FLEX_EINVAL;
+    if (!all16({x, w, S, out}) || !opt16({bias})) return FLEX_EINVAL;
+    a.x = x; a.w = w; a.bias = bias; a.S1 = S; a.out = out;
+    return counted(1, flex::launch_conv_decode(a, (cudaStream_t)stream));
+}
+
+size_t flex_norm_workspace_bytes(const flex_norm* shape)
+{
+    flex::NormArgs a;
+    return make_norm(shape, false, false, &a) == FLEX_OK ? kHeader + floats(flex::norm_part_floats(a)) : 0;
+}
+
+int flex_norm_fwd(const flex_norm* shape, const void* x, const float* w, const void* z,
+                  const void* res, const float* scale, const int* end, void* out, void* total,
+                  float* rstd, void* stream)
+{
+    flex::NormArgs a;
+    const int rc = make_norm(shape, z != nullptr, res != nullptr, &a);
+    if (rc) return rc;
+    if (!all16({x, w, out}) || !opt16({z, res, scale, total}) || !aligned(end, 4) || !aligned(rstd, 4))
+        return FLEX_EINVAL;
+    if (!res != !total || (scale && !res)) return FLEX_EINVAL;
+    a.x = x; a.w = w; a.z = z; a.res = res; a.scale = scale; a.end = end;
+    a.out = out; a.total = total; a.rstd = rstd;
+    return counted(1, flex::launch_norm_fwd(a, (cudaStream_t)stream));
+}
+
+int flex_norm_bwd(const flex_norm* shape, const void* x, const float* w, const void* z,
+                  const void* res, const float* scale, const int* end, const float* rstd,
+                  const void* dout, const void* dtotal, void* dx, void* dres, void* dz, float* dw,
+                  float* dscale, void* ws, size_t ws_bytes, void* stream)
+{
+    flex::NormArgs a;
+    int rc = make_norm(shape, z != nullptr, res != nullptr, &a);
+    if (rc) return rc;
+    if (!all16({x, w, dout, dw}) || !opt16({z, res, scale, dtotal, dx, dres, dz, dscale})) return FLEX_EINVAL;
+    if (!rstd || !aligned(rstd, 4) || !aligned(end, 4)) return FLEX_EINVAL;
+    if (!res != !dres || !z != !dz || !scale != !dscale || (scale && !res) || (dtotal && !res))
+        return FLEX_EINVAL;
+    if (!dx != (res && !scale)) return FLEX_EINVAL;  // (without a scale dres is dx too)
+    if ((rc = check_ws(ws, ws_bytes, kHeader + floats(flex::norm_part_floats(a))))) return rc;
+    a.x = x; a.w = w; a.z = z; a.res = res; a.scale = scale; a.end = end; a.rstd = const_cast<float*>(rstd);
+    a.dout = dout; a.dtotal = dtotal; a.dx = dx; a.dres = dres; a.dz = dz; a.dw = dw; a.dscale = dscale;
+    a.part = (float*)((char*)ws + kHeader);
+    return counted(2, flex::launch_norm_bwd(a, (cudaStream_t)stream));
 }
 
 }  // extern "C"

@@ -1,0 +1,292 @@
+// Norms around a block: r = x, or res + scale x (the residual stream, which is written too); out =
+// r rstd w, rstd = (mean r^2 + eps)^-1/2 over the d elements of a head, times silu(z) where a gate is
+// given; and the gradients.
+//
+// A group of threads, a power of two of them, takes a (row, head), 16 bytes at a time, and holds all of
+// it in registers between the sum and what it is for.  Bound by DRAM: every tensor is read or written
+// once.  The backward's groups stay with their head and walk rows, keeping sums for dw and dscale.
+#include "flex_internal.h"
+#include "layer.cuh"
+
+namespace flex {
+namespace {
+
+constexpr int kThreads = 256;
+
+// Sum over a group of `tpr` threads; past a warp through shared memory, two slots in turn.
+__device__ __forceinline__ float group_sum(float v, int tpr, float* slots)
+{
+#pragma unroll
+    for (int m = 16; m >= 1; m /= 2)
+        if (m < tpr) v += __shfl_xor_sync(0xffffffffu, v, m);
+    if (tpr <= 32) return v;
+    const int warp = threadIdx.x / 32, per = tpr / 32, first = warp / per * per;
+    if (threadIdx.x % 32 == 0) slots[warp] = v;
+    __syncthreads();
+    v = 0.f;
+    for (int k = 0; k < per; ++k) v += slots[first + k];
+    return v;
+}
+
+__device__ __forceinline__ long long row_count(const NormArgs& a)
+{
+    return a.end ? min(max(__ldg(a.end), 0), a.T) : a.T;
+}
+
+template <typename T, int K>
+__global__ void __launch_bounds__(kThreads) norm_fwd_kernel(NormArgs a, int tpr)
+{
+    constexpr int V = Pack<T>::N;
+    __shared__ float slots[kThreads / 32];
+    const long long item = (long long)blockIdx.x * (kThreads / tpr) + threadIdx.x / tpr;
+    const int lane = threadIdx.x % tpr;
+    const long long t = item / a.H;
+    const int h = (int)(item % a.H);
+    const bool in = t < row_count(a);
+    Pack<T> xr[K], zr[K], rr[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int e = (lane + k * tpr) * V;
+        xr[k].zero(); zr[k].zero(); rr[k].zero();
+        if (!in || e >= a.d) continue;
+        xr[k].load((const T*)a.x + t * a.xs + (long long)h * a.d + e);
+        if (a.res) rr[k].load((const T*)a.res + t * a.rs + (long long)h * a.d + e);
+        if (a.z) zr[k].load((const T*)a.z + t * a.zs + (long long)h * a.d + e);
+    }
+    const int p = a.heads > 1 ? h * a.d : 0;
+    float r[K][V], sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int e = (lane + k * tpr) * V;
+        xr[k].get(r[k]);
+        if (a.res) {
+            float y[V], s[V];
+            rr[k].get(y);
+            if (a.scale && e < a.d) load_params<V>(s, a.scale + p + e);
+#pragma unroll
+            for (int q = 0; q < V; ++q) r[k][q] = a.scale ? fmaf(e < a.d ? s[q] : 0.f, r[k][q], y[q]) : r[k][q] + y[q];
+            if (in && e < a.d) {
+                rr[k].set(r[k]);
+                rr[k].store((T*)a.total + item * a.d + e);
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < V; ++q) sum = fmaf(r[k][q], r[k][q], sum);
+    }
+    sum = group_sum(sum, tpr, slots);
+    const float rstd = rsqrtf(sum / (float)a.d + a.eps);
+    if (!in) return;
+    if (a.rstd && lane == 0) a.rstd[item] = rstd;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int e = (lane + k * tpr) * V;
+        if (e >= a.d) continue;
+        float w[V], g[V];
+        load_params<V>(w, a.w + p + e);
+        zr[k].get(g);
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+            r[k][q] *= rstd * w[q];
+            if (a.z) r[k][q] *= g[q] * logistic(g[q]);
+        }
+        xr[k].set(r[k]);
+        xr[k].store((T*)a.out + item * a.d + e);
+    }
+}
+
+// With n = r rstd and g = dout silu(z): dn = g w, dr = rstd (dn - n mean(dn n)) + dtotal;
+// dres = dr, dx = scale dr, dscale += dr x, dw += g n, dz = dout silu'(z) n w.  r is found again from
+// x and res, since a rounded sum would leave its rounding in the parameters' gradients.
+template <typename T, int K, bool RES, bool GATE>
+__global__ void __launch_bounds__(kThreads) norm_bwd_kernel(NormArgs a, int tpr)
+{
+    constexpr int V = Pack<T>::N;
+    __shared__ float slots[2][kThreads / 32];
+    const int per = kThreads / tpr, lane = threadIdx.x % tpr;
+    const long long group = (long long)blockIdx.x * per + threadIdx.x / tpr, groups = (long long)gridDim.x * per;
+    const long long items = row_count(a) * a.H;
+    // groups % H == 0 where the parameters are a head's own: a group's head is always the same
+    const int p = a.heads > 1 ? (int)(group % a.H) * a.d : 0;
+    float dw[K][V] = {}, ds[RES ? K : 1][V] = {};
+    Pack<T> xr[K], rr[K], zr[K], gr[K], tr[K];
+    auto load = [&](long long item) {
+        const long long t = item / a.H, at = item % a.H * a.d;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int e = (lane + k * tpr) * V;
+            xr[k].zero(); gr[k].zero();
+            if (RES) { rr[k].zero(); tr[k].zero(); }
+            if (GATE) zr[k].zero();
+            if (item >= items || e >= a.d) continue;
+            xr[k].load((const T*)a.x + t * a.xs + at + e);
+            gr[k].load((const T*)a.dout + item * a.d + e);
+            if (RES) rr[k].load((const T*)a.res + t * a.rs + at + e);
+            if (RES && a.dtotal) tr[k].load((const T*)a.dtotal + item * a.d + e);
+            if (GATE) zr[k].load((const T*)a.z + t * a.zs + at + e);
+        }
+    };
+    int turn = 0;
+    load(group);
+    // (every group of a block makes the same number of rounds: the sums may have block barriers)
+    for (long long base = group - threadIdx.x / tpr; base < items; base += groups, turn ^= 1) {
+        const long long item = base + threadIdx.x / tpr;
+        const bool in = item < items;
+        const float rstd = in ? a.rstd[item] : 0.f;
+        float n[K][V], dn[K][V], sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int e = (lane + k * tpr) * V;
+            float w[V], g[V], x[V];
+#pragma unroll
+            for (int q = 0; q < V; ++q) w[q] = 0.f;
+            if (e < a.d) load_params<V>(w, a.w + p + e);
+            xr[k].get(n[k]);
+            if (RES) {
+                float y[V], s[V];
+                rr[k].get(y);
+                if (a.scale && e < a.d) load_params<V>(s, a.scale + p + e);
+#pragma unroll
+                for (int q = 0; q < V; ++q)
+                    n[k][q] = a.scale ? fmaf(e < a.d ? s[q] : 0.f, n[k][q], y[q]) : n[k][q] + y[q];
+            }
+            gr[k].get(g);
+            if (GATE) zr[k].get(x);
+            float dz[V];
+#pragma unroll
+            for (int q = 0; q < V; ++q) {
+                n[k][q] *= rstd;
+                if (GATE) {
+                    const float l = logistic(x[q]);
+                    dz[q] = g[q] * l * fmaf(x[q], 1.f - l, 1.f) * n[k][q] * w[q];
+                    g[q] *= x[q] * l;
+                }
+                dw[k][q] = fmaf(g[q], n[k][q], dw[k][q]);
+                dn[k][q] = g[q] * w[q];
+                sum = fmaf(dn[k][q], n[k][q], sum);
+            }
+            if (GATE && in && e < a.d) {
+                zr[k].set(dz);
+                zr[k].store((T*)a.dz + item * a.d + e);
+            }
+        }
+        sum = group_sum(sum, tpr, slots[turn]) / (float)a.d;
+        Pack<T> xo[K], to[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            xo[k] = xr[k];
+            if (RES) to[k] = tr[k];
+        }
+        load(item + groups);
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int e = (lane + k * tpr) * V;
+            if (!in || e >= a.d) continue;
+            float dr[V];
+#pragma unroll
+            for (int q = 0; q < V; ++q) dr[q] = rstd * fmaf(-n[k][q], sum, dn[k][q]);
+            Pack<T> o;
+            if (RES) {
+                float y[V], x[V];
+                to[k].get(y);
+                xo[k].get(x);
+#pragma unroll
+                for (int q = 0; q < V; ++q) {
+                    dr[q] += y[q];
+                    ds[k][q] = fmaf(dr[q], x[q], ds[k][q]);
+                }
+                o.set(dr);
+                o.store((T*)a.dres + item * a.d + e);
+                if (!a.scale) continue;
+                float s[V];
+                load_params<V>(s, a.scale + p + e);
+#pragma unroll
+                for (int q = 0; q < V; ++q) dr[q] *= s[q];
+            }
+            o.set(dr);
+            o.store((T*)a.dx + item * a.d + e);
+        }
+    }
+    const int cols = RES && a.scale ? 2 * a.d : a.d;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int e = (lane + k * tpr) * V;
+        if (e >= a.d) continue;
+        float* to = a.part + (size_t)group * cols + e;
+#pragma unroll
+        for (int q = 0; q < V; q += 4) {
+            *(float4*)(to + q) = make_float4(dw[k][q], dw[k][q + 1], dw[k][q + 2], dw[k][q + 3]);
+            if (RES && a.scale)
+                *(float4*)(to + a.d + q) = make_float4(ds[k][q], ds[k][q + 1], ds[k][q + 2], ds[k][q + 3]);
+        }
+    }
+}
+
+struct Plan { int tpr, K; };
+// Threads of a group and 16-byte units of each: 2, or more where a row has more than 512 units.
+Plan plan(const NormArgs& a)
+{
+    const int units = a.d / (a.bf16 ? 8 : 4);
+    int tpr = 1;
+    while (tpr < kThreads && 2 * tpr < units) tpr *= 2;
+    const int need = (units + tpr - 1) / tpr;
+    return {tpr, need <= 2 ? need : need <= 4 ? 4 : 8};
+}
+
+template <typename T>
+cudaError_t fwd(const NormArgs& a, cudaStream_t s)
+{
+    const Plan p = plan(a);
+    const int per = kThreads / p.tpr;
+    const dim3 grid((unsigned)(((long long)a.T * a.H + per - 1) / per));
+    constexpr int most = 32 / Pack<T>::N;  // (rows of 8192 elements)
+    auto kernel = p.K == 1 ? norm_fwd_kernel<T, 1> : p.K == 2 ? norm_fwd_kernel<T, 2>
+                : p.K == 4 ? norm_fwd_kernel<T, 4> : norm_fwd_kernel<T, most>;
+    return tc::launch_after(kernel, grid, kThreads, 0, 0, false, s, a, p.tpr);
+}
+template <typename T, int K>
+cudaError_t bwd_k(const NormArgs& a, const Plan& p, cudaStream_t s)
+{
+    auto kernel = a.res ? (a.z ? norm_bwd_kernel<T, K, true, true> : norm_bwd_kernel<T, K, true, false>)
+                        : (a.z ? norm_bwd_kernel<T, K, false, true> : norm_bwd_kernel<T, K, false, false>);
+    const int blocks = norm_bwd_blocks(a), groups = blocks * (kThreads / p.tpr);
+    const cudaError_t e = tc::launch_after(kernel, dim3((unsigned)blocks), kThreads, 0, 0, false, s, a, p.tpr);
+    if (e != cudaSuccess) return e;
+    const bool two = a.res && a.scale;
+    return launch_column_sums(a.part, two ? 2 * a.d : a.d, a.d, a.heads, a.heads, groups / a.heads, a.dw,
+                              two ? a.dscale : nullptr, s);
+}
+template <typename T>
+cudaError_t bwd(const NormArgs& a, cudaStream_t s)
+{
+    const Plan p = plan(a);
+    return p.K == 1 ? bwd_k<T, 1>(a, p, s) : p.K == 2 ? bwd_k<T, 2>(a, p, s)
+         : p.K == 4 ? bwd_k<T, 4>(a, p, s) : bwd_k<T, 32 / Pack<T>::N>(a, p, s);
+}
+
+}  // namespace
+
+// Blocks of the backward, 2 an SM at most; whole groups for every head that has its own parameters.
+int norm_bwd_blocks(const NormArgs& a)
+{
+    const int per = kThreads / plan(a).tpr;
+    const long long all = ((long long)a.T * a.H + per - 1) / per;
+    int unit = a.heads;  // blocks whose groups are a multiple of the heads
+    while (unit % 2 == 0 && unit / 2 * per % a.heads == 0) unit /= 2;
+    const long long blocks = all < 304 ? all : 304;
+    return (int)((blocks + unit - 1) / unit * unit);
+}
+size_t norm_part_floats(const NormArgs& a)
+{
+    return (size_t)norm_bwd_blocks(a) * (kThreads / plan(a).tpr) * 2 * a.d;
+}
+
+cudaError_t launch_norm_fwd(const NormArgs& a, cudaStream_t s)
+{
+    return a.bf16 ? fwd<__nv_bfloat16>(a, s) : fwd<float>(a, s);
+}
+cudaError_t launch_norm_bwd(const NormArgs& a, cudaStream_t s)
+{
+    return a.bf16 ? bwd<__nv_bfloat16>(a, s) : bwd<float>(a, s);
+}
+
+}  // namespace flex

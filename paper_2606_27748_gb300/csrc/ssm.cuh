@@ -36,21 +36,18 @@ namespace ssm {
 constexpr int kTile = 16;  // tokens staged at a time, and between two marks
 constexpr int kSMs = 152;  // of a GB300: a workspace's size is to depend on the shape alone
 
-// A thread holds 4 states of one channel; L = N / 4 lanes hold a channel.  Blocks of 64 channels,
-// or 32 where a channel takes 8 lanes and more.
-template <int L>
+// A thread holds 4 states of one channel; L = N / 4 lanes hold a channel; a block takes CT channels.
+template <int L, int CT_>
 struct Cfg {
-    static constexpr int N = 4 * L, CT = L <= 4 ? 64 : 32, THREADS = CT * L;
+    static constexpr int N = 4 * L, CT = CT_, THREADS = CT * L;
     static constexpr int QUADS = kTile * CT / 4;  // groups of 4 channels of a token in a tile
     static constexpr int PT = QUADS > THREADS ? QUADS / THREADS : 1;  // of them a thread stages
     static constexpr int BC = kTile * N / 2;      // groups of 4 values of B and C in a tile
     static constexpr int PBC = BC > THREADS ? BC / THREADS : 1;
 };
-inline int tile_channels(int N) { return N <= 16 ? 64 : 32; }
-inline int group_tiles(const SsmArgs& a)
+inline int group_tiles(const SsmArgs& a, int channels)
 {
-    const int c = tile_channels(a.N);
-    return (a.D / a.G + c - 1) / c;
+    return (a.D / a.G + channels - 1) / channels;
 }
 
 // Sums of L values over L lanes (lane p of them): lane p returns the one of value slot(p).  Every
@@ -82,42 +79,53 @@ __device__ __forceinline__ float rcp(float x)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kLog2eLow = 1.925963033500e-08f;  // log2(e) - float(log2(e))
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 
-// exp(x) for x <= 0 and above -80: 2^hi with the product's own rounding made good
+__device__ __forceinline__ float max_nan(float x, float y)  // a NaN stays one
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
+    return r;
+}
+// exp(-|x|), 0 from 111 on; off by 3e-7 at 7, where steps near 0.001 lie (the product's rounding)
 __device__ __forceinline__ float exp_neg(float x)
 {
-    const float hi = x * kLog2e;
-    const float lo = fmaf(x, kLog2eLow, fmaf(x, kLog2e, -hi));
-    const float y = ex2(hi);
-    return fmaf(y, lo * 0.693147180559945f, y);
+    return ex2(max_nan(-fabsf(x), -111.f) * kLog2e);
 }
 
-// softplus(x) = max(x, 0) + log1p(t), t = exp(-|x|), with log1p(t) = 2 atanh(s), s = t / (2 + t)
-// <= 1/3, by its series in s^2 up to s^15 (the next term is 7e-10 of the sum); t is exact to its
-// last bits however small, as a step near 0.001 needs it.
+// softplus(x) = max(x, 0) + log1p(t), t = exp(-|x|) in [0, 1], of 4 values.  log1p(t) / t is a
+// polynomial of degree 8 (least relative error, 3e-8, found by exchange), so that small steps keep
+// their relative accuracy.  0 for -inf, exactly.
+__device__ __forceinline__ void softplus4(float (&x)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+        float a = max_nan(-fabsf(x[i]), -111.f), b = max_nan(-fabsf(x[i + 1]), -111.f);
+        tc::f2_unpack(tc::f2_mul(tc::f2_pack(a, b), tc::f2_pack(kLog2e, kLog2e)), a, b);
+        const uint64_t t = tc::f2_pack(ex2(a), ex2(b));
+        constexpr float c[9] = {9.9999996988e-01f, -4.9999493140e-01f, 3.3319096808e-01f,
+                                -2.4842982216e-01f, 1.9106006770e-01f, -1.3663245815e-01f,
+                                7.8225952120e-02f, -2.9505238928e-02f, 5.2326943023e-03f};
+        uint64_t p = tc::f2_pack(c[8], c[8]);
+#pragma unroll
+        for (int k = 7; k >= 0; --k) p = tc::f2_fma(p, t, tc::f2_pack(c[k], c[k]));
+        p = tc::f2_fma(p, t, tc::f2_pack(fmaxf(x[i], 0.f), fmaxf(x[i + 1], 0.f)));
+        tc::f2_unpack(p, x[i], x[i + 1]);
+    }
+}
 __device__ __forceinline__ float softplus(float x)
 {
-    const float t = exp_neg(fmaxf(-fabsf(x), -80.f));
-    const float s = t * rcp(2.f + t), y = s * s;
-    float p = fmaf(y, 1.f / 15, 1.f / 13);
-    p = fmaf(p, y, 1.f / 11);
-    p = fmaf(p, y, 1.f / 9);
-    p = fmaf(p, y, 1.f / 7);
-    p = fmaf(p, y, 1.f / 5);
-    p = fmaf(p, y, 1.f / 3);
-    p = fmaf(p, y, 1.f);
-    const float top = x > 0.f ? x : (x == x ? 0.f : x);  // (a NaN stays one)
-    return fmaf(2.f * s, p, top);
+    float v[4] = {x, x, x, x};
+    softplus4(v);
+    return v[0];
 }
 // its derivative
 __device__ __forceinline__ float sigmoid(float x)
 {
-    const float t = exp_neg(fmaxf(-fabsf(x), -80.f)), r = rcp(1.f + t);
-    const float y = x > 0.f ? r : t * r;
-    return x == x ? y : x;
+    const float t = exp_neg(x), r = rcp(1.f + t);
+    return x < 0.f ? t * r : r;
 }
+__device__ __forceinline__ float silu(float x) { return __fdividef(x, 1.f + __expf(-x)); }
 
 // Four elements as they lie in memory.
 template <typename T>
@@ -127,6 +135,7 @@ struct Quad<float> {
     float4 r;
     __device__ __forceinline__ void load(const float* p) { r = *(const float4*)p; }
     __device__ __forceinline__ void zero() { r = make_float4(0.f, 0.f, 0.f, 0.f); }
+    __device__ __forceinline__ void low() { r.x = r.y = r.z = r.w = __uint_as_float(0xff800000u); }
     __device__ __forceinline__ float4 get() const { return r; }
 };
 template <>
@@ -134,6 +143,7 @@ struct Quad<__nv_bfloat16> {
     uint2 r;
     __device__ __forceinline__ void load(const __nv_bfloat16* p) { r = *(const uint2*)p; }
     __device__ __forceinline__ void zero() { r = make_uint2(0u, 0u); }
+    __device__ __forceinline__ void low() { r = make_uint2(0xff80ff80u, 0xff80ff80u); }  // -inf
     __device__ __forceinline__ float4 get() const
     {
         return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u),
@@ -162,12 +172,15 @@ struct alignas(16) F2x2 {  // a thread's 4 states as packed pairs
         return lo + hi;
     }
 };
-// exp(d A) for A2 = A log2(e)
+// exp(d A) for A2 = A log2(e).  ex2.approx comes out 0 to 5e-8 low on average (by up to 2.7e-8 where
+// a state lasts for tens of tokens), which adds up over the tokens a state lasts; kUp in the
+// exponent makes half of that good, at no cost.
+constexpr float kUp = 2e-8f;
 __device__ __forceinline__ F2x2 decay(const F2x2& A2, uint64_t dd)
 {
     F2x2 e;
-    e.x = tc::f2_mul(A2.x, dd);
-    e.y = tc::f2_mul(A2.y, dd);
+    e.x = tc::f2_fma(A2.x, dd, tc::f2_pack(kUp, kUp));
+    e.y = tc::f2_fma(A2.y, dd, tc::f2_pack(kUp, kUp));
     const float4 v = e.get();
     e.from(make_float4(ex2(v.x), ex2(v.y), ex2(v.z), ex2(v.w)));
     return e;
@@ -179,16 +192,16 @@ struct Place {
     int g, c0, nc, tile;                      // group, first channel, channels, tile of the group
 };
 // false where the slot has no rows (an empty sequence has one such slot, block 0, to itself)
-template <int L>
+template <int CT>
 __device__ __forceinline__ bool find_place(const SsmArgs& a, int index, Place& p)
 {
-    const int Dg = a.D / a.G, tiles = (Dg + Cfg<L>::CT - 1) / Cfg<L>::CT, all = tiles * a.G;
+    const int Dg = a.D / a.G, tiles = (Dg + CT - 1) / CT, all = tiles * a.G;
     p.slot = index / all;
     const int t = index % all;
     p.g = t / tiles;
     p.tile = t % tiles;
-    p.c0 = p.g * Dg + p.tile * Cfg<L>::CT;
-    p.nc = min(Cfg<L>::CT, Dg - p.tile * Cfg<L>::CT);
+    p.c0 = p.g * Dg + p.tile * CT;
+    p.nc = min(CT, Dg - p.tile * CT);
     const bool found = find_block(a.cu, a.n, a.T, a.rows, p.slot, p.s, p.block, p.lo, p.hi);
     p.first = found ? p.lo + p.block * a.rows : p.lo;
     p.last = min((long long)p.hi, (long long)p.first + a.rows);

@@ -17,9 +17,12 @@ namespace {
 
 using namespace ssm;
 
+// Channels of a block.
+constexpr int channels(int L) { return L <= 4 ? 64 : 32; }
+
 template <int L>
 struct Smem {
-    using C = Cfg<L>;
+    using C = Cfg<L, channels(L)>;
     static constexpr int WARPS = C::THREADS / 32, SPLIT = 8 / L, PARTS = WARPS * SPLIT;
     struct Tile {
         float2 td[kTile][C::CT];       // D_t, D_t x_t
@@ -32,10 +35,10 @@ struct Smem {
 };
 
 template <typename T, int L>
-__global__ void __launch_bounds__(Cfg<L>::THREADS, 2 * 256 / Cfg<L>::THREADS)
+__global__ void __launch_bounds__(channels(L) * L, 512 / (channels(L) * L))
 ssm_bwd_kernel(SsmArgs a)
 {
-    using C = Cfg<L>;
+    using C = Cfg<L, channels(L)>;
     using S = Smem<L>;
     constexpr int N = C::N, CT = C::CT, NT = C::THREADS, PT = C::PT, PBC = C::PBC;
     constexpr int YB = L < 4 ? 4 : L;
@@ -43,7 +46,7 @@ ssm_bwd_kernel(SsmArgs a)
     S& sm = *(S*)raw;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     Place p;
-    const bool found = find_place<L>(a, blockIdx.x, p);
+    const bool found = find_place<channels(L)>(a, blockIdx.x, p);
     const int ch = tid / L, sub = tid % L;
     const bool mine = ch < p.nc;
     const size_t DN = (size_t)a.D * N, state = (size_t)(p.c0 + ch) * N + 4 * sub;
@@ -84,7 +87,6 @@ ssm_bwd_kernel(SsmArgs a)
         if (a.Ds) Ds = *(const float4*)(a.Ds + p.c0 + q4);
     }
     const int nt = (p.last - p.first + kTile - 1) / kTile;
-    auto silu = [](float v) { return __fdividef(v, 1.f + __expf(-v)); };
 
     struct Raw { Quad<T> x[PT], d[PT], z[PT], o[PT], bc[PBC]; } r;
     auto load = [&](int i) {
@@ -92,7 +94,8 @@ ssm_bwd_kernel(SsmArgs a)
 #pragma unroll
         for (int k = 0; k < PT; ++k) {
             const long long t = t0 + tq + k * (NT / CQ);
-            r.x[k].zero(); r.d[k].zero(); r.z[k].zero(); r.o[k].zero();
+            r.x[k].zero(); r.z[k].zero(); r.o[k].zero();
+            if (a.softplus) r.d[k].low(); else r.d[k].zero();  // a step of 0
             if (stages && t < p.last) {
                 r.x[k].load(x + t * a.xs + p.c0 + q4);
                 r.d[k].load(dt + t * a.ds + p.c0 + q4);
@@ -112,12 +115,11 @@ ssm_bwd_kernel(SsmArgs a)
             }
         }
     };
-    auto put = [&](int i, typename S::Tile& s) {
+    auto put = [&](typename S::Tile& s) {
 #pragma unroll
         for (int k = 0; k < PT; ++k) {
             const int tt = tq + k * (NT / CQ);
             if (tid >= C::QUADS) break;
-            const bool in = stages && p.first + i * kTile + tt < p.last;
             const float4 dv = r.d[k].get(), xv = r.x[k].get();
             float4 o = r.o[k].get();
             if (z) {
@@ -125,8 +127,7 @@ ssm_bwd_kernel(SsmArgs a)
                 o.x *= silu(g.x); o.y *= silu(g.y); o.z *= silu(g.z); o.w *= silu(g.w);
             }
             float d[4] = {dv.x + bias.x, dv.y + bias.y, dv.z + bias.z, dv.w + bias.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) d[j] = in ? (a.softplus ? softplus(d[j]) : d[j]) : 0.f;
+            if (a.softplus) softplus4(d);
             float4* to = (float4*)&s.td[tt][q4];
             to[0] = make_float4(d[0], d[0] * xv.x, d[1], d[1] * xv.y);
             to[1] = make_float4(d[2], d[2] * xv.z, d[3], d[3] * xv.w);
@@ -141,12 +142,14 @@ ssm_bwd_kernel(SsmArgs a)
 
     const float* marks = a.marks + ((size_t)(p.lo / kTile + p.s) + (p.first - p.lo) / kTile) * DN + state;
     load(nt - 1);
+    F2x2 dAt;  // a tile's part, so that long sums are sums of sums
     for (int i = nt - 1; i >= 0; --i) {
         typename S::Tile& s = sm.tiles[i & 1];
-        put(i, s);
+        put(s);
         F2x2 h0;
         h0.from(mine ? *(const float4*)(marks + i * DN) : make_float4(0.f, 0.f, 0.f, 0.f));
         __syncthreads();
+        dAt.x = dAt.y = 0;
         // the states again, and y
         F2x2 hh[kTile];
 #pragma unroll
@@ -204,8 +207,8 @@ ssm_bwd_kernel(SsmArgs a)
                     v.x = tc::f2_mul(e.x, h.x);
                     v.y = tc::f2_mul(e.y, h.y);
                     s2[j] = v.dot(A2);
-                    dA.x = tc::f2_fma(dd, v.x, dA.x);
-                    dA.y = tc::f2_fma(dd, v.y, dA.y);
+                    dAt.x = tc::f2_fma(dd, v.x, dAt.x);
+                    dAt.y = tc::f2_fma(dd, v.y, dAt.y);
                 }
                 // Sums over the warp's channels for two tokens: 4 L groups of 4 values, of which a
                 // lane adds those of 4 channels.  They are read in turn, since two groups' rows
@@ -235,6 +238,8 @@ ssm_bwd_kernel(SsmArgs a)
             }
         }
         __syncthreads();
+        dA.x = tc::f2_fma(dAt.x, tc::f2_pack(1.f, 1.f), dA.x);
+        dA.y = tc::f2_fma(dAt.y, tc::f2_pack(1.f, 1.f), dA.y);
         // the tile's gradients
 #pragma unroll
         for (int k = 0; k < PT; ++k) {
@@ -249,7 +254,7 @@ ssm_bwd_kernel(SsmArgs a)
             float gx[4], gd[4], gz[4], gD[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float s1 = sm.sums[0][tt][q4 + j], s2 = sm.sums[1][tt][q4 + j] * 0.693147180559945f;
+                const float s1 = sm.sums[0][tt][q4 + j], s2 = sm.sums[1][tt][q4 + j] * kLn2;
                 const float dy = s.dy[tt][q4 + j], d = s.td[tt][q4 + j].x;
                 gx[j] = fmaf(s1, d, Dv[j] * dy);
                 gd[j] = fmaf(s1, xv[j], s2);
@@ -347,12 +352,12 @@ __global__ void __launch_bounds__(256) ssm_bwd_sum_kernel(SsmArgs a, int tiles, 
 template <typename T, int L>
 cudaError_t bwd(const SsmArgs& a, bool after, cudaStream_t s)
 {
-    const int slots = block_slots(a.T, a.n, a.rows), tiles = group_tiles(a);
+    const int slots = block_slots(a.T, a.n, a.rows), tiles = group_tiles(a, channels(L));
     auto kernel = ssm_bwd_kernel<T, L>;
     static_assert(sizeof(Smem<L>) <= 113 * 1024, "two blocks an SM");
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Smem<L>));
     if (e != cudaSuccess) return e;
-    e = tc::launch_after(kernel, dim3((unsigned)((long long)slots * tiles * a.G)), Cfg<L>::THREADS,
+    e = tc::launch_after(kernel, dim3((unsigned)((long long)slots * tiles * a.G)), channels(L) * L,
                          sizeof(Smem<L>), 0, after, s, a);
     if (e != cudaSuccess) return e;
     const long long bc = ((long long)a.T * a.G * 2 * a.N / 4 + 255) / 256;
@@ -371,6 +376,8 @@ cudaError_t bwd_n(const SsmArgs& a, bool after, cudaStream_t s)
 }
 
 }  // namespace
+
+int ssm_bwd_tiles(const SsmArgs& a) { return group_tiles(a, channels(a.N / 4)); }
 
 cudaError_t launch_ssm_bwd(const SsmArgs& a, cudaStream_t s)
 {

@@ -19,226 +19,323 @@ using namespace ssm;
 
 enum Mode { kOut, kEnds, kBack };
 
-// One tile of tokens in shared memory.
-template <int L, int MODE>
-struct Tile {
-    float2 td[kTile][Cfg<L>::CT];     // D_t, and D_t x_t (kBack: dy_t)
-    float bc[kTile][2][Cfg<L>::N];    // B and C (kEnds: B, kBack: C)
+// How a block's threads divide a tile of tokens.  A thread holds SP states of each of CH channels.
+template <typename T, int N_, int CH, int SP, int CT_>
+struct Layout {
+    static constexpr int N = N_, CT = CT_, L = N / SP, NT = CT / CH * L;
+    static constexpr int QUADS = kTile * CT / 4, PT = QUADS / NT;  // groups of 4 channels of a token
+    static constexpr int BC = kTile * N / 2, PBC = (BC + NT - 1) / NT;  // of 4 values of B and C
+    static constexpr int RING = 4;
+    struct Raw {  // a tile as it lies in memory
+        T x[kTile][CT], dt[kTile][CT], z[kTile][CT], bc[kTile][2][N];
+    };
+    struct Smem {
+        Raw raw[RING];
+        float2 td[2][kTile][CT];       // D_t, and D_t x_t (kBack: dy_t)
+        float bc[2][kTile][2][N];      // B and C
+        float y[2][kTile][CT + 8];
+    };
 };
+
+__device__ __forceinline__ void copy_quad(float* to, const float* from, bool in)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
+                 "l"(from), "r"(in ? 16 : 0));
+}
+__device__ __forceinline__ void copy_quad(__nv_bfloat16* to, const __nv_bfloat16* from, bool in)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
+                 "l"(from), "r"(in ? 8 : 0));
+}
+
+// SP states as packed pairs.
+template <int SP>
+struct States {
+    uint64_t v[SP / 2];
+    __device__ __forceinline__ void read(const float* p)
+    {
+#pragma unroll
+        for (int i = 0; i < SP / 4; ++i) {
+            const ulonglong2 u = *(const ulonglong2*)(p + 4 * i);
+            v[2 * i] = u.x;
+            v[2 * i + 1] = u.y;
+        }
+    }
+    __device__ __forceinline__ void write(float* p) const
+    {
+#pragma unroll
+        for (int i = 0; i < SP / 4; ++i) *(ulonglong2*)(p + 4 * i) = make_ulonglong2(v[2 * i], v[2 * i + 1]);
+    }
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < SP / 2; ++i) v[i] = 0;
+    }
+};
+__device__ __forceinline__ uint64_t ex2_pair(uint64_t x)
+{
+    float a, b;
+    tc::f2_unpack(x, a, b);
+    return tc::f2_pack(ex2(a), ex2(b));
+}
+__device__ __forceinline__ uint64_t twice(float x) { return tc::f2_pack(x, x); }
 
 // kOut: outputs, last states and marks.  kEnds: what a block leaves behind, without outputs.  kBack:
 // the same of the gradient of the state, from the block's last token to its first:
 // e_{t-1} = exp(D_t A) (e_t + dy_t C_t).
-template <typename T, int L, int MODE>
-__global__ void __launch_bounds__(Cfg<L>::THREADS) ssm_scan_kernel(SsmArgs a)
+//
+// Tiles of 16 tokens are copied to shared memory two ahead, their steps and inputs computed one
+// ahead, once for all states; a tile's outputs are finished after the next block barrier, of which
+// there is one a tile.
+template <typename T, int N, int CH, int SP, int CT, int MODE>
+__global__ void __launch_bounds__(CT / CH * (N / SP)) ssm_scan_kernel(SsmArgs a)
 {
-    using C = Cfg<L>;
-    constexpr int N = C::N, CT = C::CT, NT = C::THREADS, PT = C::PT, PBC = C::PBC;
-    constexpr int YB = L < 4 ? 4 / L * L : L;  // tokens whose y's are added up together
-    __shared__ alignas(16) Tile<L, MODE> tiles[2];
-    __shared__ alignas(16) float sy[MODE == kOut ? 2 : 1][MODE == kOut ? kTile : 1][CT + 8];
+    using Y = Layout<T, N, CH, SP, CT>;
+    constexpr int L = Y::L, NT = Y::NT, PT = Y::PT, PBC = Y::PBC, CQ = CT / 4;
+    extern __shared__ __align__(16) unsigned char smem[];
+    typename Y::Smem& sm = *(typename Y::Smem*)smem;
     const int tid = threadIdx.x;
     Place p;
-    const bool found = find_place<L>(a, blockIdx.x, p);
-    const int ch = tid / L, sub = tid % L;
-    const bool mine = ch < p.nc;
-    const size_t state = (size_t)(p.c0 + ch) * N + 4 * sub;  // within [D][N]
+    const bool found = find_place<CT>(a, blockIdx.x, p);
+    const int ch = tid / L * CH, sub = tid % L;
+    const bool mine = ch < p.nc;  // (channels come in fours)
+    const size_t state = (size_t)(p.c0 + ch) * N + SP * sub;  // within [D][N]; the next channel's + N
     const size_t DN = (size_t)a.D * N;
     // the kernel ahead left ends and sums; nothing is read of them before this
     tc::grid_dep_wait();
     if (!found) {
-        if (MODE == kOut && a.h1 && p.block == 0 && p.lo == p.hi && mine)
-            *(float4*)(a.h1 + p.s * DN + state) =
-                a.h0 ? *(const float4*)(a.h0 + p.s * DN + state) : make_float4(0.f, 0.f, 0.f, 0.f);
+        if (MODE == kOut && a.h1 && p.block == 0 && p.lo == p.hi && mine) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                States<SP> v;
+                v.zero();
+                if (a.h0) v.read(a.h0 + p.s * DN + state + c * N);
+                v.write(a.h1 + p.s * DN + state + c * N);
+            }
+        }
         return;
     }
     const int blocks = (p.hi - p.lo + a.rows - 1) / a.rows;
     if (MODE == kEnds && p.block == blocks - 1) return;  // nothing comes after it
     if (MODE == kBack && p.block == 0) return;
 
-    F2x2 A2, h;
-    {
-        float4 v = mine ? *(const float4*)(a.A + state) : make_float4(0.f, 0.f, 0.f, 0.f);
-        A2.from(make_float4(v.x * kLog2e, v.y * kLog2e, v.z * kLog2e, v.w * kLog2e));
-        v = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (MODE != kBack && p.block == 0 && a.h0 && mine) {
+    States<SP> A2[CH], h[CH];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        A2[c].zero();
+        h[c].zero();
+        if (!mine) continue;
+        A2[c].read(a.A + state + c * N);
+#pragma unroll
+        for (int i = 0; i < SP / 2; ++i) A2[c].v[i] = tc::f2_mul(A2[c].v[i], twice(kLog2e));
+        if (MODE != kBack && p.block == 0 && a.h0) {
             // h1 may be h0: of a sequence in several blocks the first kernel keeps a copy, in the
             // place of the last block's end, which nothing else takes
-            float* copy = a.ends + (size_t)(p.slot + blocks - 1) * DN + state;
-            v = *(const float4*)(MODE == kOut && blocks > 1 ? copy : a.h0 + p.s * DN + state);
-            if (MODE == kEnds) *(float4*)copy = v;
+            float* copy = a.ends + (size_t)(p.slot + blocks - 1) * DN + state + c * N;
+            h[c].read(MODE == kOut && blocks > 1 ? copy : a.h0 + p.s * DN + state + c * N);
+            if (MODE == kEnds) h[c].write(copy);
         }
-        h.from(v);
-    }
-    if (MODE == kOut && p.block > 0 && mine) {
-        for (int j = p.slot - p.block; j < p.slot; ++j) {
-            const float sum = a.sums[(size_t)j * a.D + p.c0 + ch];
-            const F2x2 w = decay(A2, tc::f2_pack(sum, sum));
-            F2x2 e;
-            e.from(*(const float4*)(a.ends + j * DN + state));
-            h.x = tc::f2_fma(w.x, h.x, e.x);
-            h.y = tc::f2_fma(w.y, h.y, e.y);
-        }
+        if (MODE == kOut && p.block > 0)
+            for (int j = p.slot - p.block; j < p.slot; ++j) {
+                const uint64_t sum = twice(a.sums[(size_t)j * a.D + p.c0 + ch + c]);
+                States<SP> e;
+                e.read(a.ends + j * DN + state + c * N);
+#pragma unroll
+                for (int i = 0; i < SP / 2; ++i)
+                    h[c].v[i] = tc::f2_fma(ex2_pair(tc::f2_mul(A2[c].v[i], sum)), h[c].v[i], e.v[i]);
+            }
     }
 
-    const T *x = (const T*)a.x, *dt = (const T*)a.dt, *z = (const T*)a.z, *dout = (const T*)a.dout;
-    Quad<T> xr[2][PT], zr[2][PT], dr[PT], bcr[PBC];
-    // a thread's groups of 4 channels: tokens tid / (CT / 4) + ..., channels 4 (tid % (CT / 4)) + ...
-    constexpr int CQ = CT / 4;
-    const int q4 = 4 * (tid % CQ), tq = tid / CQ;
-    const bool stages = tid < C::QUADS && q4 < p.nc;
+    const int q4 = 4 * (tid % CQ), tq = tid / CQ;  // a thread's groups of channels: tokens tq + k NT / CQ
+    const bool stages = q4 < p.nc;
     float4 bias = make_float4(0.f, 0.f, 0.f, 0.f), Ds = bias;
     if (stages) {
         if (a.bias) bias = *(const float4*)(a.bias + p.c0 + q4);
         if (MODE == kOut && a.Ds) Ds = *(const float4*)(a.Ds + p.c0 + q4);
     }
+    const bool gate = MODE != kEnds && a.z;
     const int nt = (p.last - p.first + kTile - 1) / kTile;
     auto start = [&](int i) { return MODE == kBack ? p.first + (nt - 1 - i) * kTile : p.first + i * kTile; };
-    auto load = [&](int i, Quad<T>(&xq)[PT], Quad<T>(&zq)[PT]) {
+    auto fetch = [&](int i) {
+        typename Y::Raw& r = sm.raw[i % Y::RING];
         const int t0 = start(i);
+        const size_t c = p.c0 + q4;
 #pragma unroll
         for (int k = 0; k < PT; ++k) {
-            const long long t = t0 + tq + k * (NT / CQ);
-            xq[k].zero(); zq[k].zero(); dr[k].zero();
-            if (stages && t < p.last) {
-                dr[k].load(dt + t * a.ds + p.c0 + q4);
-                if (MODE == kBack) xq[k].load(dout + t * a.D + p.c0 + q4);
-                else xq[k].load(x + t * a.xs + p.c0 + q4);
-                if (MODE != kEnds && z) zq[k].load(z + t * a.zs + p.c0 + q4);
-            }
+            const int tt = tq + k * (NT / CQ);
+            const long long t = t0 + tt;
+            const bool in = stages && t < p.last;
+            const size_t row = in ? t : p.first;  // (what is not read has a valid address too)
+            const size_t at = in ? c : p.c0;
+            copy_quad(&r.dt[tt][q4], (const T*)a.dt + row * a.ds + at, in);
+            if (MODE == kBack) copy_quad(&r.x[tt][q4], (const T*)a.dout + row * a.D + at, in);
+            else copy_quad(&r.x[tt][q4], (const T*)a.x + row * a.xs + at, in);
+            if (gate) copy_quad(&r.z[tt][q4], (const T*)a.z + row * a.zs + at, in);
         }
 #pragma unroll
         for (int k = 0; k < PBC; ++k) {
-            const int e = tid + k * NT, which = e / (C::BC / 2), i4 = e % (C::BC / 2);
-            const long long t = t0 + i4 / L;
-            bcr[k].zero();
-            if (e < C::BC && t < p.last) {
-                const int at = p.g * N + 4 * (i4 % L);
-                if (which == 0 && MODE != kBack) bcr[k].load((const T*)a.B + t * a.bs + at);
-                if (which == 1 && MODE != kEnds) bcr[k].load((const T*)a.C + t * a.cs + at);
-            }
+            const int e = tid + k * NT;
+            if (Y::BC % NT && e >= Y::BC) break;
+            const int which = e / (Y::BC / 2), i4 = e % (Y::BC / 2), tt = i4 / (N / 4), m = 4 * (i4 % (N / 4));
+            const bool in = t0 + tt < p.last;
+            const size_t row = in ? t0 + tt : p.first;
+            if (which == 0 && MODE != kBack) copy_quad(&r.bc[tt][0][m], (const T*)a.B + row * a.bs + p.g * N + m, in);
+            if (which == 1 && MODE != kEnds) copy_quad(&r.bc[tt][1][m], (const T*)a.C + row * a.cs + p.g * N + m, in);
         }
     };
-    auto silu = [](float v) { return __fdividef(v, 1.f + __expf(-v)); };
-    auto put = [&](int i, Tile<L, MODE>& s, const Quad<T>(&xq)[PT], const Quad<T>(&zq)[PT]) {
+    auto convert = [&](int i) {
+        const typename Y::Raw& r = sm.raw[i % Y::RING];
         const int t0 = start(i);
 #pragma unroll
         for (int k = 0; k < PT; ++k) {
             const int tt = tq + k * (NT / CQ);
-            if (tid >= C::QUADS) break;
+            Quad<T> dr, xr, zr;
+            dr.load(&r.dt[tt][q4]);
+            xr.load(&r.x[tt][q4]);
             // a token that does not exist takes a step of 0: it changes nothing
-            const bool in = stages && t0 + tt < p.last;
-            const float4 r = dr[k].get();
-            float4 v = xq[k].get();
-            if (MODE == kBack && z) {
-                const float4 g = zq[k].get();
+            if (a.softplus && !(stages && t0 + tt < p.last)) dr.low();
+            float4 v = xr.get();
+            const float4 w = dr.get();
+            if (MODE == kBack && gate) {
+                zr.load(&r.z[tt][q4]);
+                const float4 g = zr.get();
                 v.x *= silu(g.x); v.y *= silu(g.y); v.z *= silu(g.z); v.w *= silu(g.w);
             }
-            float d[4] = {r.x + bias.x, r.y + bias.y, r.z + bias.z, r.w + bias.w};
-            float u[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                d[j] = in ? (a.softplus ? softplus(d[j]) : d[j]) : 0.f;
-                if (MODE != kBack) u[j] *= d[j];
-                if (!in) u[j] = 0.f;
-            }
-            float4* to = (float4*)&s.td[tt][q4];
-            to[0] = make_float4(d[0], u[0], d[1], u[1]);
-            to[1] = make_float4(d[2], u[2], d[3], u[3]);
+            float d[4] = {w.x + bias.x, w.y + bias.y, w.z + bias.z, w.w + bias.w};
+            if (a.softplus) softplus4(d);
+            else if (!(stages && t0 + tt < p.last)) d[0] = d[1] = d[2] = d[3] = 0.f;
+            if (MODE != kBack) { v.x *= d[0]; v.y *= d[1]; v.z *= d[2]; v.w *= d[3]; }
+            float4* to = (float4*)&sm.td[i & 1][tt][q4];
+            to[0] = make_float4(d[0], v.x, d[1], v.y);
+            to[1] = make_float4(d[2], v.z, d[3], v.w);
         }
 #pragma unroll
         for (int k = 0; k < PBC; ++k) {
-            const int e = tid + k * NT, which = e / (C::BC / 2), i4 = e % (C::BC / 2);
-            if (e < C::BC) *(float4*)&s.bc[i4 / L][which][4 * (i4 % L)] = bcr[k].get();
+            const int e = tid + k * NT;
+            if (Y::BC % NT && e >= Y::BC) break;
+            const int which = e / (Y::BC / 2), i4 = e % (Y::BC / 2), tt = i4 / (N / 4), m = 4 * (i4 % (N / 4));
+            if (which != (MODE == kBack ? 0 : MODE == kEnds ? 1 : 2)) {
+                Quad<T> v;
+                v.load(&r.bc[tt][which][m]);
+                *(float4*)&sm.bc[i & 1][tt][which][m] = v.get();
+            }
         }
     };
-    auto finish = [&](int i, const Quad<T>(&xq)[PT], const Quad<T>(&zq)[PT]) {
+    auto finish = [&](int i) {
+        const typename Y::Raw& r = sm.raw[i % Y::RING];
 #pragma unroll
         for (int k = 0; k < PT; ++k) {
             const int tt = tq + k * (NT / CQ);
             const long long t = start(i) + tt;
             if (!stages || t >= p.last) continue;
-            float4 y = *(const float4*)&sy[i & 1][MODE == kOut ? tt : 0][q4];
-            const float4 v = xq[k].get();
+            float4 y = *(const float4*)&sm.y[i & 1][tt][q4];
+            Quad<T> xr, zr;
+            xr.load(&r.x[tt][q4]);
+            const float4 v = xr.get();
             y.x = fmaf(Ds.x, v.x, y.x); y.y = fmaf(Ds.y, v.y, y.y);
             y.z = fmaf(Ds.z, v.z, y.z); y.w = fmaf(Ds.w, v.w, y.w);
-            if (z) {
-                const float4 g = zq[k].get();
+            if (gate) {
+                zr.load(&r.z[tt][q4]);
+                const float4 g = zr.get();
                 y.x *= silu(g.x); y.y *= silu(g.y); y.z *= silu(g.z); y.w *= silu(g.w);
             }
             store4((T*)a.out + t * a.D + p.c0 + q4, y);
         }
     };
 
-    float sum = 0.f;
+    float sum[CH] = {};
     float* marks = MODE == kOut && a.marks && mine
         ? a.marks + ((size_t)(p.lo / kTile + p.s) + (p.first - p.lo) / kTile) * DN + state : nullptr;
-    load(0, xr[0], zr[0]);
-    put(0, tiles[0], xr[0], zr[0]);
+    fetch(0);
+    asm volatile("cp.async.commit_group;");
+    if (nt > 1) fetch(1);
+    asm volatile("cp.async.commit_group;");
+    asm volatile("cp.async.wait_group 1;");
     __syncthreads();
-    auto body = [&](int i, auto par) {
-        constexpr int P = decltype(par)::value;
-        if (i + 1 < nt) load(i + 1, xr[P ^ 1], zr[P ^ 1]);
+    convert(0);
+    for (int i = 0; i < nt; ++i) {
+        asm volatile("cp.async.wait_group 0;");
+        __syncthreads();
+        if (i + 2 < nt) fetch(i + 2);
+        asm volatile("cp.async.commit_group;");
+        if (MODE == kOut && i > 0) finish(i - 1);
+        if (i + 1 < nt) convert(i + 1);
         if (marks) {
-            *(float4*)marks = h.get();
+#pragma unroll
+            for (int c = 0; c < CH; ++c) h[c].write(marks + c * N);
             marks += DN;
         }
-        const Tile<L, MODE>& s = tiles[P];
-        if (MODE == kOut) {
+        const float2(*td)[CT] = sm.td[i & 1];
+        const float(*bc)[2][N] = sm.bc[i & 1];
+        constexpr int YB = MODE == kOut && L > 2 ? L : 2;
+#pragma unroll 2
+        for (int b = 0; b < kTile; b += YB) {
+            float y[CH][YB];
 #pragma unroll
-            for (int b = 0; b < kTile; b += YB) {
-                float y[YB];
+            for (int jj = 0; jj < YB; ++jj) {
+                const int j = MODE == kBack ? kTile - 1 - b - jj : b + jj;
+                States<SP> B, C;
+                if (MODE != kBack) B.read(&bc[j][0][SP * sub]);
+                if (MODE != kEnds) C.read(&bc[j][1][SP * sub]);
+                float2 du[CH];
 #pragma unroll
-                for (int j = 0; j < YB; ++j) {
-                    const float2 td = s.td[b + j][ch];
-                    const F2x2 B = *(const F2x2*)&s.bc[b + j][0][4 * sub];
-                    const F2x2 Cv = *(const F2x2*)&s.bc[b + j][1][4 * sub];
-                    const F2x2 w = decay(A2, tc::f2_pack(td.x, td.x));
-                    const uint64_t dx = tc::f2_pack(td.y, td.y);
-                    h.x = tc::f2_fma(w.x, h.x, tc::f2_mul(dx, B.x));
-                    h.y = tc::f2_fma(w.y, h.y, tc::f2_mul(dx, B.y));
-                    y[j] = h.dot(Cv);
+                for (int c = 0; c < CH; c += 2) {
+                    const float4 v = *(const float4*)&td[j][ch + c];
+                    du[c] = make_float2(v.x, v.y);
+                    du[c + 1] = make_float2(v.z, v.w);
                 }
+#pragma unroll
+                for (int c = 0; c < CH; ++c) {
+                    const uint64_t d = twice(du[c].x), u = twice(du[c].y);
+                    uint64_t acc = 0;
+#pragma unroll
+                    for (int i2 = 0; i2 < SP / 2; ++i2) {
+                        const uint64_t w = ex2_pair(tc::f2_fma(A2[c].v[i2], d, twice(kUp)));
+                        uint64_t& s = h[c].v[i2];
+                        if (MODE == kBack) s = tc::f2_mul(w, tc::f2_fma(u, C.v[i2], s));
+                        else s = tc::f2_fma(w, s, tc::f2_mul(u, B.v[i2]));
+                        if (MODE == kOut) acc = i2 ? tc::f2_fma(s, C.v[i2], acc) : tc::f2_mul(s, C.v[i2]);
+                    }
+                    if (MODE == kOut) {
+                        float lo, hi;
+                        tc::f2_unpack(acc, lo, hi);
+                        y[c][jj] = lo + hi;
+                    } else {
+                        sum[c] += du[c].x;
+                    }
+                }
+            }
+            if (MODE == kOut) {
 #pragma unroll
                 for (int j = 0; j < YB; j += L) {
-                    float v[L];
+                    float v[CH];
 #pragma unroll
-                    for (int k = 0; k < L; ++k) v[k] = y[j + k];
-                    sy[P][b + j + sub][ch] = lane_sums<L>(v, sub);
+                    for (int c = 0; c < CH; ++c) {
+                        float x[L];
+#pragma unroll
+                        for (int k = 0; k < L; ++k) x[k] = y[c][j + k];
+                        v[c] = lane_sums<L>(x, sub);
+                    }
+                    float* to = &sm.y[i & 1][b + j + sub][ch];
+#pragma unroll
+                    for (int c = 0; c < CH; c += 2) *(float2*)(to + c) = make_float2(v[c], v[c + 1]);
                 }
-            }
-        } else {
-#pragma unroll 8
-            for (int k = 0; k < kTile; ++k) {
-                const int j = MODE == kBack ? kTile - 1 - k : k;
-                const float2 td = s.td[j][ch];
-                const F2x2 v = *(const F2x2*)&s.bc[j][MODE == kBack][4 * sub];
-                const F2x2 w = decay(A2, tc::f2_pack(td.x, td.x));
-                const uint64_t u = tc::f2_pack(td.y, td.y);
-                if (MODE == kEnds) {
-                    h.x = tc::f2_fma(w.x, h.x, tc::f2_mul(u, v.x));
-                    h.y = tc::f2_fma(w.y, h.y, tc::f2_mul(u, v.y));
-                } else {
-                    h.x = tc::f2_mul(w.x, tc::f2_fma(u, v.x, h.x));
-                    h.y = tc::f2_mul(w.y, tc::f2_fma(u, v.y, h.y));
-                }
-                sum += td.x;
             }
         }
-        if (i + 1 < nt) put(i + 1, tiles[P ^ 1], xr[P ^ 1], zr[P ^ 1]);
+    }
+    if (MODE == kOut) {
         __syncthreads();
-        if (MODE == kOut) finish(i, xr[P], zr[P]);
-    };
-    for (int i = 0; i < nt; i += 2) {
-        body(i, std::integral_constant<int, 0>());
-        if (i + 1 < nt) body(i + 1, std::integral_constant<int, 1>());
+        finish(nt - 1);
     }
     if (!mine) return;
-    if (MODE == kOut) {
-        if (a.h1 && p.last == p.hi) *(float4*)(a.h1 + p.s * DN + state) = h.get();
-    } else {
-        *(float4*)(a.ends + p.slot * DN + state) = h.get();
-        if (sub == 0) a.sums[(size_t)p.slot * a.D + p.c0 + ch] = sum;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        if (MODE == kOut) {
+            if (a.h1 && p.last == p.hi) h[c].write(a.h1 + p.s * DN + state + c * N);
+        } else {
+            h[c].write(a.ends + p.slot * DN + state + c * N);
+            if (sub == 0) a.sums[(size_t)p.slot * a.D + p.c0 + ch + c] = sum[c];
+        }
     }
 }
 
@@ -293,13 +390,27 @@ __global__ void __launch_bounds__(256) ssm_decode_kernel(SsmArgs a)
     }
 }
 
-template <typename T, int L>
+template <typename T, int N, int CH, int SP, int CT>
 cudaError_t scan(const SsmArgs& a, int mode, bool after, cudaStream_t s)
 {
-    const long long blocks = (long long)block_slots(a.T, a.n, a.rows) * group_tiles(a) * a.G;
-    auto kernel = mode == kOut ? ssm_scan_kernel<T, L, kOut>
-                : mode == kEnds ? ssm_scan_kernel<T, L, kEnds> : ssm_scan_kernel<T, L, kBack>;
-    return tc::launch_after(kernel, dim3((unsigned)blocks), Cfg<L>::THREADS, 0, 0, after, s, a);
+    using Y = Layout<T, N, CH, SP, CT>;
+    const long long blocks = (long long)block_slots(a.T, a.n, a.rows) * group_tiles(a, CT) * a.G;
+    auto kernel = mode == kOut ? ssm_scan_kernel<T, N, CH, SP, CT, kOut>
+                : mode == kEnds ? ssm_scan_kernel<T, N, CH, SP, CT, kEnds>
+                                : ssm_scan_kernel<T, N, CH, SP, CT, kBack>;
+    constexpr int bytes = sizeof(typename Y::Smem);
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != cudaSuccess) return e;
+    return tc::launch_after(kernel, dim3((unsigned)blocks), Y::NT, bytes, 0, after, s, a);
+}
+template <typename T>
+cudaError_t scan_n(const SsmArgs& a, int mode, bool after, cudaStream_t s)
+{
+    switch (a.N) {
+    case 8: return scan<T, 8, 2, 4, 64>(a, mode, after, s);
+    case 16: return scan<T, 16, 2, 4, 64>(a, mode, after, s);
+    default: return scan<T, 32, 2, 4, 64>(a, mode, after, s);
+    }
 }
 template <typename T, int L>
 cudaError_t decode(const SsmArgs& a, cudaStream_t s)
@@ -308,15 +419,6 @@ cudaError_t decode(const SsmArgs& a, cudaStream_t s)
     return tc::launch_after(ssm_decode_kernel<T, L>, grid, 256, 0, 0, false, s, a);
 }
 
-template <typename T>
-cudaError_t scan_n(const SsmArgs& a, int mode, bool after, cudaStream_t s)
-{
-    switch (a.N) {
-    case 8: return scan<T, 2>(a, mode, after, s);
-    case 16: return scan<T, 4>(a, mode, after, s);
-    default: return scan<T, 8>(a, mode, after, s);
-    }
-}
 template <typename T>
 cudaError_t decode_n(const SsmArgs& a, cudaStream_t s)
 {
@@ -329,12 +431,13 @@ cudaError_t decode_n(const SsmArgs& a, cudaStream_t s)
 
 }  // namespace
 
-// Sequences stay whole where their channels fill the SMs at 2 blocks each; else they are cut, so
-// that as many blocks as that are there.
+// Sequences stay whole where their blocks fill the SMs (8 x 4096, D 2048: 489 us whole, 666 cut);
+// else they are cut, so that there are 8 blocks an SM (8192, D 1280: 2 134 us, 4 151, 8 124).  The
+// backward's are cut in any case, into 2 blocks an SM, as many as run at a time.
 int ssm_rows(const SsmArgs& a, bool backward)
 {
-    const long long tiles = (long long)group_tiles(a) * a.G, want = 2LL * kSMs;
-    if (!backward && a.n * tiles >= want) return a.T + 1;
+    const long long tiles = (long long)group_tiles(a, 64) * a.G, want = (backward ? 2 : 8) * kSMs;
+    if (!backward && a.n * tiles >= kSMs) return a.T + 1;
     long long rows = (a.T * tiles + want - 1) / want;
     rows = (rows + 4 * kTile - 1) / (4 * kTile) * (4 * kTile);
     return rows > a.T ? a.T + 1 : (int)rows;

@@ -28,6 +28,8 @@ EXPORTS = ("flex_strerror", "flex_workspace_bytes", "flex_featmap", "flex_linatt
            "flex_delta_fwd", "flex_delta_bwd", "flex_delta_decode",
            "flex_softattn_workspace_bytes", "flex_softattn_fwd", "flex_ssm_workspace_bytes",
            "flex_ssm_save_bytes", "flex_ssm_fwd", "flex_ssm_bwd", "flex_ssm_decode",
+           "flex_conv_workspace_bytes", "flex_conv_fwd", "flex_conv_bwd", "flex_conv_decode",
+           "flex_norm_workspace_bytes", "flex_norm_fwd", "flex_norm_bwd",
            "flex_kernel_launches", "flex_check_status", "flex_debug_stall")
 
 
@@ -45,6 +47,16 @@ class FlexSsm(ctypes.Structure):
     _fields_ = [(name, ctypes.c_int) for name in (
         "n", "T", "D", "G", "N", "dtype", "softplus", "x_stride", "dt_stride", "b_stride",
         "c_stride", "z_stride")]
+
+
+class FlexConv(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int) for name in ("n", "T", "D", "W", "dtype", "silu", "x_stride")]
+
+
+class FlexNorm(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int) for name in (
+        "T", "H", "d", "dtype", "heads", "x_stride", "z_stride", "res_stride")] + [
+        ("eps", ctypes.c_float)]
 
 
 class FlexError(RuntimeError):
@@ -110,6 +122,16 @@ def load(path: str = LIBRARY) -> ctypes.CDLL:
         lib.flex_ssm_fwd.argtypes = [ssm] + [vp] * 14 + [sz, vp]
         lib.flex_ssm_bwd.argtypes = [ssm] + [vp] * 20 + [sz, vp]
         lib.flex_ssm_decode.argtypes = [ssm] + [vp] * 11
+        conv, norm = ctypes.POINTER(FlexConv), ctypes.POINTER(FlexNorm)
+        lib.flex_conv_workspace_bytes.argtypes = [conv]
+        lib.flex_conv_workspace_bytes.restype = sz
+        lib.flex_conv_fwd.argtypes = [conv] + [vp] * 8
+        lib.flex_conv_bwd.argtypes = [conv] + [vp] * 9 + [sz, vp]
+        lib.flex_conv_decode.argtypes = [conv] + [vp] * 6
+        lib.flex_norm_workspace_bytes.argtypes = [norm]
+        lib.flex_norm_workspace_bytes.restype = sz
+        lib.flex_norm_fwd.argtypes = [norm] + [vp] * 10
+        lib.flex_norm_bwd.argtypes = [norm] + [vp] * 15 + [sz, vp]
         lib.flex_check_status.argtypes = [vp, vp]
         lib.flex_debug_stall.argtypes = [vp, sz, ip, vp]
         lib.flex_kernel_launches.argtypes = []
@@ -118,7 +140,8 @@ def load(path: str = LIBRARY) -> ctypes.CDLL:
                    lib.flex_linattn_decode, lib.flex_awd_loss, lib.flex_awd_loss_bwd,
                    lib.flex_delta_fwd, lib.flex_delta_bwd, lib.flex_delta_decode,
                    lib.flex_softattn_fwd, lib.flex_ssm_fwd, lib.flex_ssm_bwd, lib.flex_ssm_decode,
-                   lib.flex_check_status, lib.flex_debug_stall):
+                   lib.flex_conv_fwd, lib.flex_conv_bwd, lib.flex_conv_decode, lib.flex_norm_fwd,
+                   lib.flex_norm_bwd, lib.flex_check_status, lib.flex_debug_stall):
             fn.restype = ip
         _lib = lib
         return lib
@@ -675,6 +698,169 @@ def ssm_decode(x, dt, A, B, C, S, D=None, z=None, dt_bias=None, softplus=True, o
     if rc:
         raise FlexError(rc, "flex_ssm_decode")
     return out
+
+
+def _packed_conv(x, w, n, silu, dev):
+    """The call's shape; x [T, D] or [T, heads, d] rows, of D channels together."""
+    if x.dim() < 2 or w.dim() != 2:
+        raise ValueError("x: rows [T, D]; w: taps [D, W]")
+    T = x.shape[0]
+    if T == 0:
+        raise ValueError("x: no rows")
+    D = x.numel() // T
+    return FlexConv(n, T, D, w.shape[1], _dtype_code(x), int(bool(silu)),
+                    _row_stride(x, "x", x.shape, x.dtype, dev))
+
+
+def conv_workspace(x, w, cu) -> torch.Tensor:
+    """A caller-owned workspace for conv_bwd on such tensors."""
+    shape = _packed_conv(x, w, cu.numel() - 1, True, torch.cuda.current_device())
+    return _workspace(int(load().flex_conv_workspace_bytes(ctypes.byref(shape))),
+                      "flex_conv_workspace_bytes", x.device)
+
+
+def conv_fwd(x, w, cu, bias=None, silu=True, state=None, out=None, last_state=None,
+             want_state=False, stream=None):
+    """Short causal convolution of every channel over packed sequences: (out like x, last state
+    [n, W - 1, D] or None).  x [T, D] or [T, heads, d]; w [D, W], bias [D] fp32; cu int32 [n + 1];
+    state: the W - 1 rows ahead of every sequence, oldest first (default zeros; last_state is
+    another tensor)."""
+    dev, f32 = torch.cuda.current_device(), torch.float32
+    cu_ptr, n = _offsets(cu, "cu", dev), cu.numel() - 1
+    shape = _packed_conv(x, w, n, silu, dev)
+    D, W, ty = shape.D, shape.W, x.dtype
+    st = (n, W - 1, D)
+    if out is None:
+        out = _new(stream, x.shape, ty, x.device)
+    if last_state is None and want_state:
+        last_state = _new(stream, st, ty, x.device)
+    _check(load().flex_conv_fwd(
+        ctypes.byref(shape), x.data_ptr(), _plain(w, "w", (D, W), f32, dev),
+        _plain(bias, "bias", (D,), f32, dev), cu_ptr, _plain(state, "state", st, ty, dev),
+        _plain(last_state, "last_state", st, ty, dev), _plain(out, "out", x.shape, ty, dev),
+        _stream(stream)), "flex_conv_fwd")
+    return out, last_state
+
+
+def conv_bwd(x, w, cu, dout, bias=None, silu=True, dx=None, dw=None, dbias=None, ws=None,
+             stream=None):
+    """(dx, dw, dbias) of L = sum(dout * out) of conv_fwd without `state`; dbias is None where bias
+    is."""
+    dev, f32, ty = torch.cuda.current_device(), torch.float32, x.dtype
+    cu_ptr = _offsets(cu, "cu", dev)
+    shape = _packed_conv(x, w, cu.numel() - 1, silu, dev)
+    D, W = shape.D, shape.W
+    if dx is None:
+        dx = _new(stream, x.shape, ty, x.device)
+    if dw is None:
+        dw = _new(stream, (D, W), f32, x.device)
+    if dbias is None and bias is not None:
+        dbias = _new(stream, (D,), f32, x.device)
+    if ws is None:
+        ws = _scratch(stream, conv_workspace, x, w, cu)
+    _check(load().flex_conv_bwd(
+        ctypes.byref(shape), x.data_ptr(), _plain(w, "w", (D, W), f32, dev),
+        _plain(bias, "bias", (D,), f32, dev), cu_ptr, _plain(dout, "dout", x.shape, ty, dev),
+        _plain(dx, "dx", x.shape, ty, dev), _plain(dw, "dw", (D, W), f32, dev),
+        _plain(dbias, "dbias", (D,), f32, dev), _plain(ws, "ws", ws.shape, torch.uint8, dev),
+        ws.numel(), _stream(stream)), "flex_conv_bwd")
+    return dx, dw, dbias
+
+
+def conv_decode(x, w, state, bias=None, silu=True, out=None, stream=None):
+    """One token of each sequence: x [n, D] or [n, heads, d]; state [n, W - 1, D] moves on by it, in
+    place.  Returns out like x."""
+    dev, f32 = torch.cuda.current_device(), torch.float32
+    shape = _packed_conv(x, w, x.shape[0], silu, dev)
+    D, W, ty = shape.D, shape.W, x.dtype
+    if out is None:
+        out = _new(stream, x.shape, ty, x.device)
+    _check(load().flex_conv_decode(
+        ctypes.byref(shape), x.data_ptr(), _plain(w, "w", (D, W), f32, dev),
+        _plain(bias, "bias", (D,), f32, dev), _plain(state, "state", (shape.n, W - 1, D), ty, dev),
+        _plain(out, "out", x.shape, ty, dev), _stream(stream)), "flex_conv_decode")
+    return out
+
+
+def _packed_norm(x, w, z, res, eps, dev):
+    if x.dim() != 3 or w.dim() not in (1, 2):
+        raise ValueError("x: rows [T, heads, d]; w: [d] or [heads, d]")
+    (T, H, d), ty = x.shape, x.dtype
+    if T == 0:
+        raise ValueError("x: no rows")
+    return FlexNorm(T, H, d, _dtype_code(x), 1 if w.dim() == 1 else w.shape[0],
+                    _row_stride(x, "x", x.shape, ty, dev),
+                    0 if z is None else _row_stride(z, "z", x.shape, ty, dev),
+                    0 if res is None else _row_stride(res, "res", x.shape, ty, dev), eps)
+
+
+def _params(w, shape):
+    """The shape of a norm's parameters."""
+    return (shape.d,) if w.dim() == 1 else (shape.heads, shape.d)
+
+
+def _rows_end(cu, dev):
+    """The device int that says where the last sequence ends, or None."""
+    return None if cu is None else _offsets(cu, "cu", dev) + 4 * (cu.numel() - 1)
+
+
+def norm_workspace(x, w) -> torch.Tensor:
+    """A caller-owned workspace for norm_bwd on such tensors."""
+    shape = _packed_norm(x, w, None, None, 0.0, torch.cuda.current_device())
+    return _workspace(int(load().flex_norm_workspace_bytes(ctypes.byref(shape))),
+                      "flex_norm_workspace_bytes", x.device)
+
+
+def norm_fwd(x, w, z=None, res=None, scale=None, eps=1e-6, cu=None, out=None, total=None, rstd=None,
+             want_rstd=False, stream=None):
+    """Root-mean-square norm of rows [T, heads, d] over d: (out, total, rstd).  Of x, or of the
+    residual sum total = res + scale * x, which is given back too (None without res; may be res
+    itself); times silu(z).  w, scale: [d], or [heads, d], fp32.  cu: only the rows of these
+    sequences.  rstd [T, heads] fp32 is what norm_bwd needs."""
+    dev, f32, ty = torch.cuda.current_device(), torch.float32, x.dtype
+    shape = _packed_norm(x, w, z, res, eps, dev)
+    if out is None:
+        out = _new(stream, x.shape, ty, x.device)
+    if total is None and res is not None:
+        total = _new(stream, x.shape, ty, x.device)
+    if rstd is None and want_rstd:
+        rstd = _new(stream, x.shape[:2], f32, x.device)
+    _check(load().flex_norm_fwd(
+        ctypes.byref(shape), x.data_ptr(), _plain(w, "w", _params(w, shape), f32, dev), _at(z),
+        _at(res), _plain(scale, "scale", _params(w, shape), f32, dev), _rows_end(cu, dev),
+        _plain(out, "out", x.shape, ty, dev), _plain(total, "total", x.shape, ty, dev),
+        _plain(rstd, "rstd", x.shape[:2], f32, dev), _stream(stream)), "flex_norm_fwd")
+    return out, total, rstd
+
+
+def norm_bwd(x, w, rstd, dout, z=None, res=None, scale=None, eps=1e-6, cu=None, dtotal=None, dx=None,
+             dres=None, dz=None, dw=None, dscale=None, ws=None, stream=None):
+    """(dx, dres, dz, dw, dscale) of L = sum(dout * out) + sum(dtotal * total) of norm_fwd, which gave
+    `rstd`; None where the input is.  With res and without scale dx and dres are one tensor."""
+    dev, f32, ty = torch.cuda.current_device(), torch.float32, x.dtype
+    shape = _packed_norm(x, w, z, res, eps, dev)
+    par, one = _params(w, shape), res is not None and scale is None
+    if dres is None and res is not None:
+        dres = _new(stream, x.shape, ty, x.device)
+    if dx is None and not one:
+        dx = _new(stream, x.shape, ty, x.device)
+    if dz is None and z is not None:
+        dz = _new(stream, x.shape, ty, x.device)
+    if dw is None:
+        dw = _new(stream, par, f32, x.device)
+    if dscale is None and scale is not None:
+        dscale = _new(stream, par, f32, x.device)
+    if ws is None:
+        ws = _scratch(stream, norm_workspace, x, w)
+    _check(load().flex_norm_bwd(
+        ctypes.byref(shape), x.data_ptr(), _plain(w, "w", par, f32, dev), _at(z), _at(res),
+        _plain(scale, "scale", par, f32, dev), _rows_end(cu, dev),
+        _plain(rstd, "rstd", x.shape[:2], f32, dev), _plain(dout, "dout", x.shape, ty, dev),
+        _plain(dtotal, "dtotal", x.shape, ty, dev), _plain(dx, "dx", x.shape, ty, dev),
+        _plain(dres, "dres", x.shape, ty, dev), _plain(dz, "dz", x.shape, ty, dev),
+        _plain(dw, "dw", par, f32, dev), _plain(dscale, "dscale", par, f32, dev),
+        _plain(ws, "ws", ws.shape, torch.uint8, dev), ws.numel(), _stream(stream)), "flex_norm_bwd")
+    return (dres if one else dx), dres, dz, dw, dscale
 
 
 def check_status(ws, stream=None):

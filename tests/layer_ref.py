@@ -115,3 +115,72 @@ def gradients(f, x, names, sent):
     given = [n for n in names if x[n] is not None]
     got = dict(zip(given, torch.autograd.grad(loss, [leaves[n] for n in given])))
     return [got.get(n) for n in names]
+
+
+# ---- short convolution -----------------------------------------------------------------------
+
+CONV = ("x", "w", "bias")
+
+
+def conv_inputs(lens, D, W, dtype, seed=0, bias=True, rows_behind=0, pad=0, device="cuda"):
+    gen = torch.Generator().manual_seed(seed)
+    T = sum(lens) + rows_behind
+    r = lambda *s: torch.randn(*s, generator=gen, dtype=torch.float64)  # noqa: E731
+    x = {"x": r(T, D).to(dtype), "w": r(D, W).to(F32), "bias": r(D).to(F32) if bias else None,
+         "dout": r(T, D).to(dtype)}
+    x = {n: t if t is None else t.to(device) for n, t in x.items()}
+    x["x"] = sliced(x["x"], pad)
+    return x
+
+
+def conv_ref(x, lens, state=None, act=True):
+    """(out, last rows) in float64, for the rows of the sequences.  Differentiable."""
+    v, w = x["x"].double(), x["w"].double()
+    D, W = w.shape
+    outs, lasts, at = [], [], 0
+    for i, n in enumerate(lens):
+        ahead = (torch.zeros(W - 1, D, dtype=torch.float64, device=v.device) if state is None
+                 else state[i].double())
+        rows = torch.cat([ahead, v[at:at + n]])
+        for t in range(n):
+            p = (rows[t:t + W] * w.t()).sum(0)
+            if x["bias"] is not None:
+                p = p + x["bias"].double()
+            outs.append(silu(p) if act else p)
+        lasts.append(rows[n:])
+        at += n
+    out = torch.stack(outs) if outs else v[:0]
+    return out, torch.stack(lasts)
+
+
+# ---- norms -------------------------------------------------------------------------------------
+
+NORM = ("x", "res", "z", "w", "scale")
+
+
+def norm_inputs(T, H, d, dtype, heads=None, gate=False, res=False, scale=False, seed=0, pad=0,
+                device="cuda"):
+    gen = torch.Generator().manual_seed(seed)
+    r = lambda *s: torch.randn(*s, generator=gen, dtype=torch.float64)  # noqa: E731
+    par = (d,) if heads is None else (heads, d)
+    x = {"x": r(T, H, d).to(dtype), "res": (2 * r(T, H, d)).to(dtype) if res else None,
+         "z": r(T, H, d).to(dtype) if gate else None, "w": (1 + 0.3 * r(*par)).to(F32),
+         "scale": (0.5 + 0.2 * r(*par)).to(F32) if scale else None, "dout": r(T, H, d).to(dtype),
+         "dtotal": r(T, H, d).to(dtype) if res else None}
+    x = {n: t if t is None else t.to(device) for n, t in x.items()}
+    for n in ("x", "res", "z"):
+        if x[n] is not None:
+            x[n] = sliced(x[n], pad)
+    return x
+
+
+def norm_ref(x, eps):
+    """(out, total or None) in float64.  Differentiable."""
+    r, w = x["x"].double(), x["w"].double()
+    if x["res"] is not None:
+        s = 1.0 if x["scale"] is None else x["scale"].double()
+        r = x["res"].double() + s * r
+    out = r / torch.sqrt((r * r).mean(-1, keepdim=True) + eps) * w
+    if x["z"] is not None:
+        out = out * silu(x["z"].double())
+    return out, (r if x["res"] is not None else None)

@@ -7,7 +7,7 @@ import torch
 
 from paper_2606_27748_gb300 import flexattn
 from paper_2606_27748_gb300.flexattn import (FLEX_EINVAL, FLEX_EUNSUPPORTED, FLEX_EWORKSPACE,
-                                             FlexSsm)
+                                             FlexConv, FlexNorm, FlexSsm)
 
 P = ctypes.c_void_p(1 << 20)  # never dereferenced: validation fails first
 OFF = ctypes.c_void_p((1 << 20) + 2)
@@ -125,3 +125,124 @@ def test_ssm_binding_refuses():
             flexattn._packed_ssm(*args.values(), 1, True, cpu)
     with pytest.raises(TypeError):
         flexattn._packed_ssm(*(t.half() for t in (x, x, B, B)), None, 1, True, cpu)
+
+
+# ---- short convolution -------------------------------------------------------------------------
+
+CONV_FWD = ("x", "w", "bias", "cu", "S0", "S1", "out")
+CONV_BWD = ("x", "w", "bias", "cu", "dout", "dx", "dw", "dbias", "ws")
+CONV_TOKEN = ("x", "w", "bias", "S", "out")
+
+
+def _conv(**kw):
+    x = dict(n=3, T=100, D=64, W=4, dtype=1, silu=1, x_stride=64)
+    x.update(kw)
+    return FlexConv(*(x[name] for name, _ in FlexConv._fields_))
+
+
+def _plain_call(f, names, s, *more, **kw):
+    return f(ctypes.byref(s) if s else None, *(kw.get(n, None if n == "S0" else P) for n in names), *more, None)
+
+
+def _conv_calls(lib, s, n=BIG, **kw):
+    return [_plain_call(lib.flex_conv_fwd, CONV_FWD, s, **kw),
+            _plain_call(lib.flex_conv_bwd, CONV_BWD, s, n, **kw),
+            _plain_call(lib.flex_conv_decode, CONV_TOKEN, s, **kw)]
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(n=0), FLEX_EINVAL), (dict(T=0), FLEX_EINVAL), (dict(D=0), FLEX_EINVAL), (dict(W=0), FLEX_EINVAL),
+    (dict(dtype=3), FLEX_EINVAL), (dict(x_stride=56), FLEX_EINVAL), (dict(x_stride=66), FLEX_EINVAL),
+    (dict(W=1), FLEX_EUNSUPPORTED), (dict(W=5), FLEX_EUNSUPPORTED), (dict(D=60), FLEX_EUNSUPPORTED),
+    (dict(n=65536), FLEX_EUNSUPPORTED), (dict(D=65544), FLEX_EUNSUPPORTED)], ids=str)
+def test_conv_shapes(lib, kw, status):
+    s = _conv(**kw)
+    assert _conv_calls(lib, s) == [status] * 3
+    assert lib.flex_conv_workspace_bytes(ctypes.byref(s)) == 0
+
+
+def test_conv_pointers_and_workspace(lib):
+    s, one = _conv(), _conv(T=3)
+    assert _conv_calls(lib, None) == [FLEX_EINVAL] * 3
+    for f, names, shape, more in ((lib.flex_conv_fwd, CONV_FWD, s, ()),
+                                  (lib.flex_conv_bwd, CONV_BWD, s, (BIG,)),
+                                  (lib.flex_conv_decode, CONV_TOKEN, one, ())):
+        for name in names:
+            off = ctypes.c_void_p((1 << 20) + 1)
+            assert _plain_call(f, names, shape, *more, **{name: off}) == FLEX_EINVAL, name
+            if name not in ("S0", "S1", "bias") or (name == "bias" and "dbias" in names):
+                assert _plain_call(f, names, shape, *more, **{name: None}) == FLEX_EINVAL, name
+    assert _plain_call(lib.flex_conv_decode, CONV_TOKEN, s) == FLEX_EINVAL  # T != n
+    assert _plain_call(lib.flex_conv_fwd, CONV_FWD, s, S0=P, S1=P) == FLEX_EINVAL  # one buffer
+    need = lib.flex_conv_workspace_bytes(ctypes.byref(s))
+    assert need > 256
+    assert _plain_call(lib.flex_conv_bwd, CONV_BWD, s, need - 1) == FLEX_EWORKSPACE
+
+
+# ---- norms -------------------------------------------------------------------------------------
+
+NORM_FWD = ("x", "w", "z", "res", "scale", "end", "out", "total", "rstd")
+NORM_BWD = ("x", "w", "z", "res", "scale", "end", "rstd", "dout", "dtotal", "dx", "dres", "dz", "dw",
+            "dscale", "ws")
+
+
+def _norm(**kw):
+    x = dict(T=100, H=4, d=64, dtype=1, heads=1, x_stride=256, z_stride=256, res_stride=256, eps=1e-6)
+    x.update(kw)
+    return FlexNorm(*(x[name] for name, _ in FlexNorm._fields_))
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(T=0), FLEX_EINVAL), (dict(H=0), FLEX_EINVAL), (dict(d=0), FLEX_EINVAL), (dict(heads=2), FLEX_EINVAL),
+    (dict(dtype=-1), FLEX_EINVAL), (dict(eps=-1.0), FLEX_EINVAL), (dict(eps=float("nan")), FLEX_EINVAL),
+    (dict(x_stride=248), FLEX_EINVAL), (dict(z_stride=260), FLEX_EINVAL), (dict(res_stride=0), FLEX_EINVAL),
+    (dict(d=60), FLEX_EUNSUPPORTED), (dict(H=1, d=8200, x_stride=8200), FLEX_EUNSUPPORTED),
+    (dict(H=1025), FLEX_EUNSUPPORTED), (dict(T=1 << 30, H=2), FLEX_EUNSUPPORTED)], ids=str)
+def test_norm_shapes(lib, kw, status):
+    s = _norm(**kw)
+    assert _plain_call(lib.flex_norm_fwd, NORM_FWD, s) == status
+    assert _plain_call(lib.flex_norm_bwd, NORM_BWD, s, BIG) == status
+    if "z_stride" not in kw and "res_stride" not in kw:  # (strides of what the size does not know)
+        assert lib.flex_norm_workspace_bytes(ctypes.byref(s)) == 0
+
+
+def test_norm_pointers_and_workspace(lib):
+    s = _norm()
+    fwd = lambda **kw: _plain_call(lib.flex_norm_fwd, NORM_FWD, s, **kw)  # noqa: E731
+    bwd = lambda n=BIG, **kw: _plain_call(lib.flex_norm_bwd, NORM_BWD, s, n, **kw)  # noqa: E731
+    assert _plain_call(lib.flex_norm_fwd, NORM_FWD, None) == FLEX_EINVAL
+    off = ctypes.c_void_p((1 << 20) + 2)
+    for name in NORM_FWD:
+        assert fwd(**{name: off}) == FLEX_EINVAL, name
+    for name in ("x", "w", "out", "total", "res"):  # (total goes with res, scale wants it)
+        assert fwd(**{name: None}) == FLEX_EINVAL, name
+    for name in NORM_BWD:
+        assert bwd(**{name: off}) == FLEX_EINVAL, name
+    for name in ("x", "w", "rstd", "dout", "dx", "dres", "dz", "dw", "dscale", "ws", "z", "res", "scale"):
+        assert bwd(**{name: None}) == FLEX_EINVAL, name
+    assert bwd(scale=None, dscale=None) == FLEX_EINVAL  # dres is dx, which is not given then
+    need = lib.flex_norm_workspace_bytes(ctypes.byref(s))
+    assert bwd(need - 1) == FLEX_EWORKSPACE
+    assert bwd(need - 1, scale=None, dscale=None, dx=None) == FLEX_EWORKSPACE
+
+
+def test_conv_and_norm_bindings_refuse():
+    x, w, cu = torch.zeros(10, 64), torch.zeros(64, 4), torch.tensor([0, 10], dtype=torch.int32)
+    with pytest.raises((ValueError, RuntimeError, AssertionError)):
+        flexattn.conv_fwd(x, w, cu)  # not on the GPU
+    cpu = x.get_device()
+    s = flexattn._packed_conv(torch.zeros(10, 96)[:, :64].view(10, 4, 16), w, 1, True, cpu)
+    assert (s.T, s.D, s.W, s.x_stride) == (10, 64, 4, 96)
+    for bad in (x[:0], x[0], torch.zeros(64, 10).t()):
+        with pytest.raises(ValueError):
+            flexattn._packed_conv(bad, w, 1, True, cpu)
+    y, p = torch.zeros(10, 4, 64), torch.zeros(64)
+    s = flexattn._packed_norm(y, p, None, y, 1e-6, cpu)
+    assert (s.T, s.H, s.d, s.heads, s.res_stride) == (10, 4, 64, 1, 256)
+    assert flexattn._packed_norm(y, torch.zeros(4, 64), None, None, 1e-6, cpu).heads == 4
+    for args in ((x, p, None, None), (y, torch.zeros(1, 4, 64), None, None), (y, p, y[:9], None),
+                 (y, p, None, y.double()), (y[:0], p, None, None)):
+        with pytest.raises(ValueError):
+            flexattn._packed_norm(*args, 1e-6, cpu)
+    with pytest.raises(ValueError):
+        flexattn._plain(torch.zeros(65), "w", flexattn._params(p, s), torch.float32, cpu)
