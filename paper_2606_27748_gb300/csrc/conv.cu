@@ -2,8 +2,7 @@
 //   pre_t = b + sum_j w_j x_{t - (W - 1) + j},  out_t = silu(pre_t) or pre_t,
 // rows ahead of a sequence's first being its state's (the last W - 1 rows of what came before) or 0.
 //
-// A thread walks a run of rows of 16 bytes of channels (backward: 4 channels) with the last rows in
-// registers, so every row is read once but for the W - 1 ahead of each run; runs are cut from all
+// A thread walks a run of rows of 4 channels with the last rows in registers, so every row is read once but for the W - 1 ahead of each run; runs are cut from all
 // rows alike, whatever the sequences.  Bound by DRAM: x read once and out written once.
 #include "flex_internal.h"
 #include "layer.cuh"
@@ -23,23 +22,38 @@ __device__ __forceinline__ int find_row(const int* cu, int n, int t)
 }
 __device__ __forceinline__ int rows_end(const int* cu, int n, int T) { return min(max(__ldg(cu + n), 0), T); }
 
-constexpr int kAhead = 4;  // rows whose loads are in flight together
+constexpr int kAhead = 8;  // rows whose loads are in flight together
+
+// 4 channels' parameters: w [D][W], fp32.
+template <int W>
+__device__ __forceinline__ void load_taps(float (&w)[W][4], float (&b)[4], const ConvArgs& a, int c)
+{
+    float v[4 * W];
+    load_params<4 * W>(v, a.w + (size_t)c * W);
+    if (a.bias) load_params<4>(b, a.bias + c);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        if (!a.bias) b[q] = 0.f;
+#pragma unroll
+        for (int j = 0; j < W; ++j) w[j][q] = v[q * W + j];
+    }
+}
+__device__ __forceinline__ void spread(float (&v)[4], float4 u) { v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w; }
 
 template <typename T, int W>
-__global__ void __launch_bounds__(128) conv_fwd_kernel(ConvArgs a, long long runs, long long run_blocks)
+__global__ void __launch_bounds__(128) conv_fwd_kernel(ConvArgs a, long long run_blocks)
 {
-    constexpr int V = Pack<T>::N;
-    const int CV = a.D / V;
+    const int CQ = a.D / 4;
     const T* x = (const T*)a.x;
     if (blockIdx.x >= run_blocks) {  // the sequences' last rows
         const long long i = (blockIdx.x - run_blocks) * 128 + threadIdx.x;
-        const long long row = i / CV;
-        const int c = (int)(i % CV) * V, s = (int)(row / (W - 1)), j = (int)(row % (W - 1));
+        const long long row = i / CQ;
+        const int c = (int)(i % CQ) * 4, s = (int)(row / (W - 1)), j = (int)(row % (W - 1));
         if (s >= a.n) return;
         int lo, hi;
         seq_rows(a.cu, s, a.T, lo, hi);
         const int t = hi - (W - 1) + j;
-        Pack<T> v;
+        Quad<T> v;
         v.zero();
         if (t >= lo) v.load(x + (long long)t * a.xs + c);
         else if (a.S0) v.load((const T*)a.S0 + ((long long)s * (W - 1) + (t - lo + W - 1)) * a.D + c);
@@ -47,45 +61,33 @@ __global__ void __launch_bounds__(128) conv_fwd_kernel(ConvArgs a, long long run
         return;
     }
     const long long i = blockIdx.x * 128LL + threadIdx.x;
-    const int c = (int)(i % CV) * V;
+    const int c = (int)(i % CQ) * 4;
     const int end = rows_end(a.cu, a.n, a.T);
-    const long long first = i / CV * a.run;
+    const long long first = i / CQ * a.run;
     if (first >= end) return;
     const int t0 = (int)first, t1 = min(end, t0 + a.run);
     int s = find_row(a.cu, a.n, t0), lo, hi;
     seq_rows(a.cu, s, a.T, lo, hi);
-    float w[W][V], b[V], win[W - 1][V];
-#pragma unroll
-    for (int k = 0; k < V; ++k) {
-        b[k] = a.bias ? a.bias[c + k] : 0.f;
-#pragma unroll
-        for (int j = 0; j < W; ++j) w[j][k] = a.w[(size_t)(c + k) * W + j];
-    }
+    float w[W][4], b[4], win[W - 1][4];
+    load_taps<W>(w, b, a, c);
     // the rows ahead of row t of sequence s
     auto before = [&](int t) {
 #pragma unroll
         for (int j = 0; j < W - 1; ++j) {
             const int u = t - (W - 1) + j;
-            Pack<T> v;
+            Quad<T> v;
             v.zero();
             if (u >= lo) v.load(x + (long long)u * a.xs + c);
             else if (a.S0) v.load((const T*)a.S0 + ((long long)s * (W - 1) + (u - lo + W - 1)) * a.D + c);
-            v.get(win[j]);
+            spread(win[j], v.get());
         }
     };
-    Pack<T> next[kAhead];
-    auto load = [&](int t) {
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k)
-            if (t + k < t1) next[k].load(x + (long long)(t + k) * a.xs + c);
-    };
-    load(t0);
     before(t0);
     for (int t = t0; t < t1; t += kAhead) {
-        Pack<T> now[kAhead];
+        Quad<T> rows[kAhead];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) now[k] = next[k];
-        if (t + kAhead < t1) load(t + kAhead);
+        for (int k = 0; k < kAhead; ++k)
+            if (t + k < t1) rows[k].load(x + (long long)(t + k) * a.xs + c);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             if (t + k >= t1) break;
@@ -96,10 +98,10 @@ __global__ void __launch_bounds__(128) conv_fwd_kernel(ConvArgs a, long long run
                 } while (t + k >= hi && s + 1 < a.n);
                 before(t + k);
             }
-            float v[V], y[V];
-            now[k].get(v);
+            float v[4], y[4];
+            spread(v, rows[k].get());
 #pragma unroll
-            for (int q = 0; q < V; ++q) {
+            for (int q = 0; q < 4; ++q) {
                 float p = b[q];
 #pragma unroll
                 for (int j = 0; j < W - 1; ++j) p = fmaf(w[j][q], win[j][q], p);
@@ -109,9 +111,7 @@ __global__ void __launch_bounds__(128) conv_fwd_kernel(ConvArgs a, long long run
                 for (int j = 0; j + 1 < W - 1; ++j) win[j][q] = win[j + 1][q];
                 win[W - 2][q] = v[q];
             }
-            Pack<T> o;
-            o.set(y);
-            o.store((T*)a.out + (long long)(t + k) * a.D + c);
+            store4((T*)a.out + (long long)(t + k) * a.D + c, make_float4(y[0], y[1], y[2], y[3]));
         }
     }
 }
@@ -120,8 +120,9 @@ __global__ void __launch_bounds__(128) conv_fwd_kernel(ConvArgs a, long long run
 // sequence, dw_j = sum_t dpre_t x_{t - (W - 1) + j}, db = sum_t dpre_t.  A thread walks its run and the
 // W - 1 rows behind it, whose dpre its last rows' dx wants; dw and db are summed over a block's 8 runs
 // in their order, and over blocks by a kernel of their own.
+constexpr int kBack = 4;
 template <typename T, int W>
-__global__ void __launch_bounds__(256) conv_bwd_kernel(ConvArgs a)
+__global__ void __launch_bounds__(256, 2) conv_bwd_kernel(ConvArgs a)
 {
     __shared__ float4 sums[8][W + 1][32];
     const int c = (blockIdx.x * 32 + threadIdx.x) * 4;
@@ -135,40 +136,27 @@ __global__ void __launch_bounds__(256) conv_bwd_kernel(ConvArgs a)
         int s = find_row(a.cu, a.n, t0), lo, hi;
         seq_rows(a.cu, s, a.T, lo, hi);
         float w[W][4], b[4], win[W - 1][4], acc[W][4];
+        load_taps<W>(w, b, a, c);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            b[k] = a.bias ? a.bias[c + k] : 0.f;
-#pragma unroll
-            for (int j = 0; j < W; ++j) {
-                w[j][k] = a.w[(size_t)(c + k) * W + j];
-                acc[j][k] = 0.f;
-            }
-        }
+        for (int j = 0; j < W; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
 #pragma unroll
         for (int j = 0; j < W - 1; ++j) {
             const int u = t0 - (W - 1) + j;
             const float4 v = u >= lo ? load4(x + (long long)u * a.xs + c) : make_float4(0.f, 0.f, 0.f, 0.f);
             win[j][0] = v.x; win[j][1] = v.y; win[j][2] = v.z; win[j][3] = v.w;
         }
-        float4 nx[kAhead], nd[kAhead];
-        auto load = [&](int t) {
+        for (int t = t0; t < t1 + W - 1; t += kBack) {
+            Quad<T> px[kBack], pd[kBack];
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-                nx[k] = nd[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int k = 0; k < kBack; ++k) {
+                px[k].zero(); pd[k].zero();
                 if (t + k < t2) {
-                    nx[k] = load4(x + (long long)(t + k) * a.xs + c);
-                    nd[k] = load4(dout + (long long)(t + k) * a.D + c);
+                    px[k].load(x + (long long)(t + k) * a.xs + c);
+                    pd[k].load(dout + (long long)(t + k) * a.D + c);
                 }
             }
-        };
-        load(t0);
-        for (int t = t0; t < t1 + W - 1; t += kAhead) {
-            float4 px[kAhead], pd[kAhead];
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) { px[k] = nx[k]; pd[k] = nd[k]; }
-            if (t + kAhead < t2) load(t + kAhead);
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
+            for (int k = 0; k < kBack; ++k) {
                 const int u = t + k;
                 if (u >= t1 + W - 1) break;
                 if (u < t2) {
@@ -180,8 +168,9 @@ __global__ void __launch_bounds__(256) conv_bwd_kernel(ConvArgs a)
 #pragma unroll
                         for (int j = 0; j < W - 1; ++j) win[j][0] = win[j][1] = win[j][2] = win[j][3] = 0.f;
                     }
-                    const float v[4] = {px[k].x, px[k].y, px[k].z, px[k].w};
-                    const float g[4] = {pd[k].x, pd[k].y, pd[k].z, pd[k].w};
+                    float v[4], g[4];
+                    spread(v, px[k].get());
+                    spread(g, pd[k].get());
                     const bool own = u < t1;
                     const int at = u - lo;  // rows of the sequence ahead of this one
 #pragma unroll
@@ -281,16 +270,17 @@ __global__ void __launch_bounds__(128) conv_decode_kernel(ConvArgs a)
     for (int j = 0; j < W - 1; ++j) rows[j + 1].store(state + (long long)j * a.D);
 }
 
-constexpr int kSlices = 16;
-__global__ void __launch_bounds__(32 * kSlices) column_sums_kernel(const float* from, int cols, int split,
-                                                                   int step, int count, float* to0, float* to1)
+// Blocks of 32 columns: few rows are summed (some hundred), so what costs is their loads' latency.
+constexpr int kSlices = 32;
+__global__ void __launch_bounds__(8 * kSlices) column_sums_kernel(const float* from, int cols, int split,
+                                                                  int step, int count, float* to0, float* to1)
 {
-    __shared__ float4 sums[kSlices][32];
+    __shared__ float4 sums[kSlices][8];
     tc::grid_dep_wait();
-    const int c = (blockIdx.x * 32 + threadIdx.x) * 4;
+    const int c = (blockIdx.x * 8 + threadIdx.x) * 4;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (c < cols) {
-#pragma unroll 4
+#pragma unroll 8
         for (int k = threadIdx.y; k < count; k += kSlices) {
             const float4 u = *(const float4*)(from + (size_t)(blockIdx.y + (size_t)k * step) * cols + c);
             v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
@@ -311,11 +301,11 @@ __global__ void __launch_bounds__(32 * kSlices) column_sums_kernel(const float* 
 template <typename T, int W>
 cudaError_t fwd(const ConvArgs& a, cudaStream_t s)
 {
-    const int CV = a.D / Pack<T>::N;
-    const long long runs = (a.T + a.run - 1) / a.run, blocks = (runs * CV + 127) / 128;
-    const long long more = a.S1 ? ((long long)a.n * (W - 1) * CV + 127) / 128 : 0;
+    const int CQ = a.D / 4;
+    const long long blocks = ((long long)(a.T + a.run - 1) / a.run * CQ + 127) / 128;
+    const long long more = a.S1 ? ((long long)a.n * (W - 1) * CQ + 127) / 128 : 0;
     return tc::launch_after(conv_fwd_kernel<T, W>, dim3((unsigned)(blocks + more)), 128, 0, 0, false, s, a,
-                            runs, blocks);
+                            blocks);
 }
 template <typename T, int W>
 cudaError_t bwd(const ConvArgs& a, cudaStream_t s)
@@ -356,8 +346,8 @@ cudaError_t launch_column_sums(const float* from, int cols, int split, int sums,
                                float* to0, float* to1, cudaStream_t s)
 {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((cols + 127) / 128), (unsigned)sums);
-    cfg.blockDim = dim3(32, kSlices);
+    cfg.gridDim = dim3((unsigned)((cols + 31) / 32), (unsigned)sums);
+    cfg.blockDim = dim3(8, kSlices);
     cfg.stream = s;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -368,9 +358,9 @@ cudaError_t launch_column_sums(const float* from, int cols, int split, int sums,
 }
 
 // Rows of a thread's run: long ones read fewer rows twice, short ones fill the SMs.
-int conv_run(const ConvArgs& a, bool backward)
+int conv_run(const ConvArgs& a)
 {
-    const long long lanes = backward ? a.D / 4 : a.D / (a.bf16 ? 8 : 4), want = 152LL * 1024;
+    const long long lanes = a.D / 4, want = 152LL * 1024;
     int run = 32;
     while (run > 4 && (a.T + run - 1) / run * lanes < want) run /= 2;
     return run;

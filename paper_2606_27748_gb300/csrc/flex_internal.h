@@ -175,7 +175,7 @@ cudaError_t launch_ssm_decode(const SsmArgs& a, cudaStream_t s);
 // ---- packed batches: short convolution and norms around the recurrence -------------------
 struct ConvArgs;  // layer.cuh
 struct NormArgs;
-int conv_run(const ConvArgs& a, bool backward);  // rows of a thread (ConvArgs::run)
+int conv_run(const ConvArgs& a);                 // rows of a thread (ConvArgs::run)
 int conv_bwd_blocks(const ConvArgs& a);          // blocks of rows, of which each leaves sums
 cudaError_t launch_conv_fwd(const ConvArgs& a, cudaStream_t s);     // 1 kernel
 cudaError_t launch_conv_bwd(const ConvArgs& a, cudaStream_t s);     // 2

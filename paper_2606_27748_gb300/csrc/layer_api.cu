@@ -114,7 +114,7 @@ int make_conv(const flex_conv* s, flex::ConvArgs* a)
 }
 size_t conv_ws_bytes(flex::ConvArgs* a)
 {
-    a->run = flex::conv_run(*a, true);
+    a->run = flex::conv_run(*a);
     return kHeader + floats((size_t)flex::conv_bwd_blocks(*a) * (a->W + 1) * a->D);
 }
 
@@ -221,7 +221,7 @@ int flex_conv_fwd(const flex_conv* shape, const void* x, const float* w, const f
     if (!all16({x, w, out}) || !opt16({bias, S0, S1}) || !offsets(cu)) return FLEX_EINVAL;
     if (S0 && S0 == S1) return FLEX_EINVAL;
     a.x = x; a.w = w; a.bias = bias; a.cu = cu; a.S0 = S0; a.S1 = S1; a.out = out;
-    a.run = flex::conv_run(a, false);
+    a.run = flex::conv_run(a);
     return counted(1, flex::launch_conv_fwd(a, (cudaStream_t)stream));
 }
 

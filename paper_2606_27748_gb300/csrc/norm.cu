@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(kThreads) norm_fwd_kernel(NormArgs a, int tpr)
 // dres = dr, dx = scale dr, dscale += dr x, dw += g n, dz = dout silu'(z) n w.  r is found again from
 // x and res, since a rounded sum would leave its rounding in the parameters' gradients.
 template <typename T, int K, bool RES, bool GATE>
-__global__ void __launch_bounds__(kThreads) norm_bwd_kernel(NormArgs a, int tpr)
+__global__ void __launch_bounds__(kThreads, K == 1 ? 2 : 1) norm_bwd_kernel(NormArgs a, int tpr)
 {
     constexpr int V = Pack<T>::N;
     __shared__ float slots[2][kThreads / 32];
@@ -222,12 +222,13 @@ __global__ void __launch_bounds__(kThreads) norm_bwd_kernel(NormArgs a, int tpr)
 }
 
 struct Plan { int tpr, K; };
-// Threads of a group and 16-byte units of each: 2, or more where a row has more than 512 units.
-Plan plan(const NormArgs& a)
+// Threads of a group and 16-byte units of each: at most 2 forward and 1 backward, which holds more of
+// each in registers; more where a row has more than 512 or 256 units.
+Plan plan(const NormArgs& a, bool backward)
 {
     const int units = a.d / (a.bf16 ? 8 : 4);
     int tpr = 1;
-    while (tpr < kThreads && 2 * tpr < units) tpr *= 2;
+    while (tpr < kThreads && (backward ? 1 : 2) * tpr < units) tpr *= 2;
     const int need = (units + tpr - 1) / tpr;
     return {tpr, need <= 2 ? need : need <= 4 ? 4 : 8};
 }
@@ -235,7 +236,7 @@ Plan plan(const NormArgs& a)
 template <typename T>
 cudaError_t fwd(const NormArgs& a, cudaStream_t s)
 {
-    const Plan p = plan(a);
+    const Plan p = plan(a, false);
     const int per = kThreads / p.tpr;
     const dim3 grid((unsigned)(((long long)a.T * a.H + per - 1) / per));
     constexpr int most = 32 / Pack<T>::N;  // (rows of 8192 elements)
@@ -258,7 +259,7 @@ cudaError_t bwd_k(const NormArgs& a, const Plan& p, cudaStream_t s)
 template <typename T>
 cudaError_t bwd(const NormArgs& a, cudaStream_t s)
 {
-    const Plan p = plan(a);
+    const Plan p = plan(a, true);
     return p.K == 1 ? bwd_k<T, 1>(a, p, s) : p.K == 2 ? bwd_k<T, 2>(a, p, s)
          : p.K == 4 ? bwd_k<T, 4>(a, p, s) : bwd_k<T, 32 / Pack<T>::N>(a, p, s);
 }
@@ -268,7 +269,7 @@ cudaError_t bwd(const NormArgs& a, cudaStream_t s)
 // Blocks of the backward, 2 an SM at most; whole groups for every head that has its own parameters.
 int norm_bwd_blocks(const NormArgs& a)
 {
-    const int per = kThreads / plan(a).tpr;
+    const int per = kThreads / plan(a, true).tpr;
     const long long all = ((long long)a.T * a.H + per - 1) / per;
     int unit = a.heads;  // blocks whose groups are a multiple of the heads
     while (unit % 2 == 0 && unit / 2 * per % a.heads == 0) unit /= 2;
@@ -277,7 +278,7 @@ int norm_bwd_blocks(const NormArgs& a)
 }
 size_t norm_part_floats(const NormArgs& a)
 {
-    return (size_t)norm_bwd_blocks(a) * (kThreads / plan(a).tpr) * 2 * a.d;
+    return (size_t)norm_bwd_blocks(a) * (kThreads / plan(a, true).tpr) * 2 * a.d;
 }
 
 cudaError_t launch_norm_fwd(const NormArgs& a, cudaStream_t s)

@@ -72,4 +72,30 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v)
     *(uint2*)p = make_uint2(*(uint32_t*)&a, *(uint32_t*)&b);
 }
 
+// Four elements as they lie in memory.
+template <typename T>
+struct Quad;
+template <>
+struct Quad<float> {
+    float4 r;
+    __device__ __forceinline__ void load(const float* p) { r = *(const float4*)p; }
+    __device__ __forceinline__ void store(float* p) const { *(float4*)p = r; }
+    __device__ __forceinline__ void zero() { r = make_float4(0.f, 0.f, 0.f, 0.f); }
+    __device__ __forceinline__ void low() { r.x = r.y = r.z = r.w = __uint_as_float(0xff800000u); }
+    __device__ __forceinline__ float4 get() const { return r; }
+};
+template <>
+struct Quad<__nv_bfloat16> {
+    uint2 r;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) { r = *(const uint2*)p; }
+    __device__ __forceinline__ void store(__nv_bfloat16* p) const { *(uint2*)p = r; }
+    __device__ __forceinline__ void zero() { r = make_uint2(0u, 0u); }
+    __device__ __forceinline__ void low() { r = make_uint2(0xff80ff80u, 0xff80ff80u); }  // -inf
+    __device__ __forceinline__ float4 get() const
+    {
+        return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u),
+                           __uint_as_float(r.y << 16), __uint_as_float(r.y & 0xffff0000u));
+    }
+};
+
 }  // namespace flex

@@ -127,30 +127,6 @@ __device__ __forceinline__ float sigmoid(float x)
 }
 __device__ __forceinline__ float silu(float x) { return __fdividef(x, 1.f + __expf(-x)); }
 
-// Four elements as they lie in memory.
-template <typename T>
-struct Quad;
-template <>
-struct Quad<float> {
-    float4 r;
-    __device__ __forceinline__ void load(const float* p) { r = *(const float4*)p; }
-    __device__ __forceinline__ void zero() { r = make_float4(0.f, 0.f, 0.f, 0.f); }
-    __device__ __forceinline__ void low() { r.x = r.y = r.z = r.w = __uint_as_float(0xff800000u); }
-    __device__ __forceinline__ float4 get() const { return r; }
-};
-template <>
-struct Quad<__nv_bfloat16> {
-    uint2 r;
-    __device__ __forceinline__ void load(const __nv_bfloat16* p) { r = *(const uint2*)p; }
-    __device__ __forceinline__ void zero() { r = make_uint2(0u, 0u); }
-    __device__ __forceinline__ void low() { r = make_uint2(0xff80ff80u, 0xff80ff80u); }  // -inf
-    __device__ __forceinline__ float4 get() const
-    {
-        return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u),
-                           __uint_as_float(r.y << 16), __uint_as_float(r.y & 0xffff0000u));
-    }
-};
-
 struct alignas(16) F2x2 {  // a thread's 4 states as packed pairs
     uint64_t x, y;
     __device__ __forceinline__ void from(float4 v)

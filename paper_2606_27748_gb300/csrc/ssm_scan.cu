@@ -352,39 +352,44 @@ __global__ void __launch_bounds__(256) ssm_decode_kernel(SsmArgs a)
     const bool mine = c < a.D;
     const size_t DN = (size_t)a.D * N, state = (size_t)c * N + 4 * sub;
     const int g = mine ? c / (a.D / a.G) : 0;
-    float4 h[kSeqs];
-#pragma unroll
-    for (int k = 0; k < kSeqs; ++k)
-        if (mine && s0 + k < a.n) h[k] = *(const float4*)(a.h1 + (s0 + k) * DN + state);
     const unsigned lanes = __ballot_sync(0xffffffffu, mine);
     if (!mine) return;  // (the lanes of a channel go together)
+    float4 h[kSeqs];
+    Quad<T> B[kSeqs], C[kSeqs];
+    T x[kSeqs], d[kSeqs], z[kSeqs];
+#pragma unroll
+    for (int k = 0; k < kSeqs; ++k) {
+        const long long t = min(s0 + k, a.n - 1);
+        h[k] = *(const float4*)(a.h1 + t * DN + state);
+        B[k].load((const T*)a.B + t * a.bs + g * N + 4 * sub);
+        C[k].load((const T*)a.C + t * a.cs + g * N + 4 * sub);
+        x[k] = ((const T*)a.x)[t * a.xs + c];
+        d[k] = ((const T*)a.dt)[t * a.ds + c];
+        if (a.z) z[k] = ((const T*)a.z)[t * a.zs + c];
+    }
     const float4 A = *(const float4*)(a.A + state);
     const float bias = a.bias ? a.bias[c] : 0.f, Ds = a.Ds ? a.Ds[c] : 0.f;
 #pragma unroll
     for (int k = 0; k < kSeqs; ++k) {
         const long long t = s0 + k;
         if (t >= a.n) break;
-        const float x = to_f32(((const T*)a.x)[t * a.xs + c]);
-        float d = to_f32(((const T*)a.dt)[t * a.ds + c]) + bias;
-        if (a.softplus) d = softplus(d);
-        const float4 B = load4((const T*)a.B + t * a.bs + g * N + 4 * sub);
-        const float4 C = load4((const T*)a.C + t * a.cs + g * N + 4 * sub);
-        const float dx = d * x;
+        const float xv = to_f32(x[k]);
+        float dv = to_f32(d[k]) + bias;
+        if (a.softplus) dv = softplus(dv);
+        const float4 Bv = B[k].get(), Cv = C[k].get();
+        const float dx = dv * xv;
         float4 v = h[k];
-        v.x = fmaf(expf(d * A.x), v.x, dx * B.x);
-        v.y = fmaf(expf(d * A.y), v.y, dx * B.y);
-        v.z = fmaf(expf(d * A.z), v.z, dx * B.z);
-        v.w = fmaf(expf(d * A.w), v.w, dx * B.w);
+        v.x = fmaf(expf(dv * A.x), v.x, dx * Bv.x);
+        v.y = fmaf(expf(dv * A.y), v.y, dx * Bv.y);
+        v.z = fmaf(expf(dv * A.z), v.z, dx * Bv.z);
+        v.w = fmaf(expf(dv * A.w), v.w, dx * Bv.w);
         *(float4*)(a.h1 + t * DN + state) = v;
-        float y = fmaf(v.x, C.x, v.y * C.y) + fmaf(v.z, C.z, v.w * C.w);
+        float y = fmaf(v.x, Cv.x, v.y * Cv.y) + fmaf(v.z, Cv.z, v.w * Cv.w);
 #pragma unroll
         for (int m = 1; m < L; m *= 2) y += __shfl_xor_sync(lanes, y, m);
         if (sub == 0) {
-            y = fmaf(Ds, x, y);
-            if (a.z) {
-                const float z = to_f32(((const T*)a.z)[t * a.zs + c]);
-                y *= z / (1.f + expf(-z));
-            }
+            y = fmaf(Ds, xv, y);
+            if (a.z) y *= silu(to_f32(z[k]));
             from_f32(((T*)a.out)[t * a.D + c], y);
         }
     }

@@ -579,14 +579,15 @@ def _row_stride(t, what, shape, dtype, dev):
         raise ValueError(f"{what}: {tuple(t.shape)} {t.dtype}, not {tuple(shape)} {dtype}")
     if t.get_device() != dev:
         raise ValueError(f"{what}: not on the current CUDA device")
-    if t.is_contiguous():
-        return t[0].numel()
-    if not t[0].is_contiguous():
-        raise ValueError(f"{what}: rows of contiguous elements")
-    row = t.stride(0)
+    sizes, strides, n = t.shape, t.stride(), 1
+    for i in range(len(sizes) - 1, 0, -1):
+        if strides[i] != n and sizes[i] != 1:
+            raise ValueError(f"{what}: rows of contiguous elements")
+        n *= sizes[i]
+    row = strides[0] if sizes[0] > 1 else n
     if row >= 2 ** 31:
         raise ValueError(f"{what}: row stride {row}")
-    return row if t.shape[0] > 1 else t[0].numel()
+    return row
 
 
 def _packed_ssm(x, dt, B, C, z, n, softplus, dev):
