@@ -80,9 +80,6 @@ struct Pack<__nv_bfloat16> {
     }
 };
 
-// silu(x) = x s, s = 1 / (1 + exp(-x)), and s; a few units in the last place of fp32.
-__device__ __forceinline__ float logistic(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
-
 // N consecutive fp32 parameters (16-byte aligned).
 template <int N>
 __device__ __forceinline__ void load_params(float (&v)[N], const float* p)

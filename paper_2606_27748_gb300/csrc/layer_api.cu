@@ -97,7 +97,7 @@ size_t ssm_ws_bytes(const flex::SsmArgs& a, bool backward)
 }
 size_t ssm_save_bytes(const flex::SsmArgs& a)
 {
-    return floats((size_t)flex::block_slots(a.T, a.n, flex::ssm::kTile) * a.D * a.N);
+    return floats((size_t)flex::block_slots(a.T, a.n, flex::ssm::kMark) * a.D * a.N);
 }
 
 int make_conv(const flex_conv* s, flex::ConvArgs* a)

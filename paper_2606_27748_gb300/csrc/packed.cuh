@@ -98,4 +98,21 @@ struct Quad<__nv_bfloat16> {
     }
 };
 
+// 2^x and 1 / x, one instruction each: two units in the last place and one, denormals as 0.
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float rcp(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
+// 1 / (1 + exp(-x)), a few units in the last place; 0 and 1 where exp(-x) leaves fp32.
+__device__ __forceinline__ float logistic(float x) { return rcp(1.f + ex2(-kLog2e * x)); }
+
 }  // namespace flex

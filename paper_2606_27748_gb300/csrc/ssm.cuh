@@ -21,7 +21,7 @@ struct SsmArgs {  // (declared in flex_internal.h)
     int rows;     // tokens of a block; T + 1: sequences are not cut
     float* ends;  // [slots][D][N]: what a block's tokens alone leave behind
     float* sums;  // [slots][D]: sum of its D_t
-    float* marks; // NULL, or the states ahead of every kTile tokens, [mark slots][D][N]
+    float* marks; // NULL, or the states ahead of every kMark tokens, [mark slots][D][N]
     // backward
     const void* dout;
     void *dx, *ddt, *dB, *dC, *dz;
@@ -33,18 +33,10 @@ struct SsmArgs {  // (declared in flex_internal.h)
 
 namespace ssm {
 
-constexpr int kTile = 16;  // tokens staged at a time, and between two marks
+constexpr int kTile = 16;  // tokens of the forward's tiles
+constexpr int kMark = 8;   // tokens between two marks, and of the backward's tiles
 constexpr int kSMs = 152;  // of a GB300: a workspace's size is to depend on the shape alone
 
-// A thread holds 4 states of one channel; L = N / 4 lanes hold a channel; a block takes CT channels.
-template <int L, int CT_>
-struct Cfg {
-    static constexpr int N = 4 * L, CT = CT_, THREADS = CT * L;
-    static constexpr int QUADS = kTile * CT / 4;  // groups of 4 channels of a token in a tile
-    static constexpr int PT = QUADS > THREADS ? QUADS / THREADS : 1;  // of them a thread stages
-    static constexpr int BC = kTile * N / 2;      // groups of 4 values of B and C in a tile
-    static constexpr int PBC = BC > THREADS ? BC / THREADS : 1;
-};
 inline int group_tiles(const SsmArgs& a, int channels)
 {
     return (a.D / a.G + channels - 1) / channels;
@@ -66,20 +58,6 @@ __device__ __forceinline__ float lane_sums(float (&x)[L], int p)
     }
     return x[0];
 }
-
-__device__ __forceinline__ float ex2(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ float rcp(float x)
-{
-    float y;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 
 __device__ __forceinline__ float max_nan(float x, float y)  // a NaN stays one
 {
@@ -125,42 +103,58 @@ __device__ __forceinline__ float sigmoid(float x)
     const float t = exp_neg(x), r = rcp(1.f + t);
     return x < 0.f ? t * r : r;
 }
-__device__ __forceinline__ float silu(float x) { return __fdividef(x, 1.f + __expf(-x)); }
+__device__ __forceinline__ float silu(float x) { return x * logistic(x); }
 
-struct alignas(16) F2x2 {  // a thread's 4 states as packed pairs
-    uint64_t x, y;
-    __device__ __forceinline__ void from(float4 v)
+// ex2.approx comes out 0 to 5e-8 low on average (by up to 2.7e-8 where a state lasts for tens of
+// tokens), which adds up over the tokens a state lasts; kUp in the exponent makes half of that good, at
+// no cost (dA of 8 x 1024 tokens: 1.3e-6 off without, 4.9e-7 with it and sums of sums).
+constexpr float kUp = 2e-8f;
+
+__device__ __forceinline__ void copy_quad(float* to, const float* from, bool in)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
+                 "l"(from), "r"(in ? 16 : 0));
+}
+__device__ __forceinline__ void copy_quad(__nv_bfloat16* to, const __nv_bfloat16* from, bool in)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
+                 "l"(from), "r"(in ? 8 : 0));
+}
+
+// SP states as packed pairs.
+template <int SP>
+struct States {
+    uint64_t v[SP / 2];
+    __device__ __forceinline__ void read(const float* p)
     {
-        x = tc::f2_pack(v.x, v.y);
-        y = tc::f2_pack(v.z, v.w);
+#pragma unroll
+        for (int i = 0; i < SP / 4; ++i) {
+            const ulonglong2 u = *(const ulonglong2*)(p + 4 * i);
+            v[2 * i] = u.x;
+            v[2 * i + 1] = u.y;
+        }
     }
-    __device__ __forceinline__ float4 get() const
+    __device__ __forceinline__ void write(float* p) const
     {
-        float4 v;
-        tc::f2_unpack(x, v.x, v.y);
-        tc::f2_unpack(y, v.z, v.w);
-        return v;
+#pragma unroll
+        for (int i = 0; i < SP / 4; ++i) *(ulonglong2*)(p + 4 * i) = make_ulonglong2(v[2 * i], v[2 * i + 1]);
     }
-    __device__ __forceinline__ float dot(const F2x2& o) const
+    __device__ __forceinline__ void zero()
     {
-        float lo, hi;
-        tc::f2_unpack(tc::f2_fma(y, o.y, tc::f2_mul(x, o.x)), lo, hi);
-        return lo + hi;
+#pragma unroll
+        for (int i = 0; i < SP / 2; ++i) v[i] = 0;
     }
 };
-// exp(d A) for A2 = A log2(e).  ex2.approx comes out 0 to 5e-8 low on average (by up to 2.7e-8 where
-// a state lasts for tens of tokens), which adds up over the tokens a state lasts; kUp in the
-// exponent makes half of that good, at no cost.
-constexpr float kUp = 2e-8f;
-__device__ __forceinline__ F2x2 decay(const F2x2& A2, uint64_t dd)
+// The second half's own barrier: each thread's copies are there for all of it.
+__device__ __forceinline__ void bring_barrier(int threads) { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); }
+
+__device__ __forceinline__ uint64_t ex2_pair(uint64_t x)
 {
-    F2x2 e;
-    e.x = tc::f2_fma(A2.x, dd, tc::f2_pack(kUp, kUp));
-    e.y = tc::f2_fma(A2.y, dd, tc::f2_pack(kUp, kUp));
-    const float4 v = e.get();
-    e.from(make_float4(ex2(v.x), ex2(v.y), ex2(v.z), ex2(v.w)));
-    return e;
+    float a, b;
+    tc::f2_unpack(x, a, b);
+    return tc::f2_pack(ex2(a), ex2(b));
 }
+__device__ __forceinline__ uint64_t twice(float x) { return tc::f2_pack(x, x); }
 
 // Where a block of threads stands: its channels and its rows of one sequence.
 struct Place {

@@ -4,11 +4,13 @@
 //   q_t = e_t exp(D_t A) h_{t-1};  dA += D_t q_t;  dD_t = s_t x_t + <q_t, A>;
 //   dx_t = s_t D_t + Ds dy_t;  dDs += dy_t x_t;  e_{t-1} = exp(D_t A) e_t.
 //
-// A thread holds 4 states of one channel, as in the forward.  The states themselves are found again
-// from the marks that the forward left every 16 tokens, and kept in registers for the 16 tokens on
-// the way back.  Sums over a channel's states go by shuffles; sums over channels (dB, dC) through
-// shared memory, first within a warp for two tokens at a time, then over its warps once a tile,
-// then over the blocks of a group in a kernel of its own: every order is fixed.
+// A thread holds 4 states of each of 2 channels, as in the forward, and walks tiles of 8 tokens from
+// the marks that the forward left: the tile's states again, kept in registers, then back.  The other
+// half of the threads brings tiles, finishes what the walk has summed over states (s_t, <q_t, A>,
+// <C_t, h_t>, by shuffles) and sums dB and dC over the block's channels, which the walk leaves in shared
+// memory for 4 tokens at a time.  Sums over blocks go through global memory to a kernel of their own.
+// Every order is fixed.  What bounds it is shared memory's bandwidth: B, C and steps twice, and dB and dC
+// out and in again, 6 of its 128-byte wavefronts for 32 elements (token, channel, state).
 #include "flex_internal.h"
 #include "ssm.cuh"
 
@@ -17,293 +19,361 @@ namespace {
 
 using namespace ssm;
 
+constexpr int kHalf = kMark / 2;
 // Channels of a block.
-constexpr int channels(int L) { return L <= 4 ? 64 : 32; }
+constexpr int channels(int N) { return N <= 16 ? 64 : 32; }
 
-template <int L>
-struct Smem {
-    using C = Cfg<L, channels(L)>;
-    static constexpr int WARPS = C::THREADS / 32, SPLIT = 8 / L, PARTS = WARPS * SPLIT;
-    struct Tile {
-        float2 td[kTile][C::CT];       // D_t, D_t x_t
-        float dy[kTile][C::CT];
-        float bc[kTile][2][C::N];
-    } tiles[2];
-    float sums[3][kTile][C::CT + 8];   // s_t, <q_t, A>, <C_t, h_t>
-    float pair[WARPS][2][2][128];      // a warp's two tokens, dB and dC: [channel][N]
-    float parts[PARTS][kTile][2][C::N];
+template <typename T, int N_>
+struct Layout {
+    static constexpr int N = N_, CT = channels(N), L = N / 4, CG = CT / 2;  // CG: pairs of channels
+    static constexpr int WALK = CG * L, BRING = 2 * CT;
+    static constexpr int RING = 4;
+    struct Raw {
+        T x[kMark][CT], dt[kMark][CT], z[kMark][CT], dout[kMark][CT], bc[kMark][2][N];
+        float mark[CT][N];
+    };
+    struct Smem {
+        Raw raw[RING];
+        float2 td[2][kMark][CT];            // D_t, D_t x_t
+        float dy[2][kMark][CT];
+        float bc[2][kMark][2][N];
+        float sums[2][3][kMark][CT + 8];    // s_t, <q_t, A>, <C_t, h_t>
+        float pair[2][kHalf][2][CG][N];     // dB and dC of a pair of channels
+    };
+    static_assert(kMark * CT / 4 == BRING, "a group of 4 channels of a token for each");
 };
 
-template <typename T, int L>
-__global__ void __launch_bounds__(channels(L) * L, 512 / (channels(L) * L))
-ssm_bwd_kernel(SsmArgs a)
+// Sums of 4 tokens' values over a channel's L lanes; lane sub returns those of tokens
+// sub, sub + L, ... (L = 8: sub % 4, twice).
+template <int L>
+__device__ __forceinline__ void token_sums(const float (&x)[4], int sub, float (&out)[L == 2 ? 2 : 1])
 {
-    using C = Cfg<L, channels(L)>;
-    using S = Smem<L>;
-    constexpr int N = C::N, CT = C::CT, NT = C::THREADS, PT = C::PT, PBC = C::PBC;
-    constexpr int YB = L < 4 ? 4 : L;
-    extern __shared__ __align__(16) unsigned char raw[];
-    S& sm = *(S*)raw;
-    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    if constexpr (L == 2) {
+        float a[2] = {x[0], x[1]}, b[2] = {x[2], x[3]};
+        out[0] = lane_sums<2>(a, sub);
+        out[1] = lane_sums<2>(b, sub);
+    } else {
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = L == 8 ? x[i] + __shfl_xor_sync(0xffffffffu, x[i], 4) : x[i];
+        out[0] = lane_sums<4>(v, sub % 4);
+    }
+}
+
+template <typename T, int N>
+__global__ void __launch_bounds__(Layout<T, N>::WALK + Layout<T, N>::BRING, 2) ssm_bwd_kernel(SsmArgs a)
+{
+    using Y = Layout<T, N>;
+    constexpr int CT = Y::CT, L = Y::L, CG = Y::CG, NT = Y::BRING, CQ = CT / 4;
+    extern __shared__ __align__(16) unsigned char smem[];
+    typename Y::Smem& sm = *(typename Y::Smem*)smem;
+    const bool walks = threadIdx.x < Y::WALK;
+    const int tid = walks ? threadIdx.x : threadIdx.x - Y::WALK;
     Place p;
-    const bool found = find_place<channels(L)>(a, blockIdx.x, p);
-    const int ch = tid / L, sub = tid % L;
-    const bool mine = ch < p.nc;
+    const bool found = find_place<CT>(a, blockIdx.x, p);
+    const int cg = tid / L, ch = 2 * cg, sub = tid % L;
+    const bool mine = walks && ch < p.nc;  // (channels come in fours)
     const size_t DN = (size_t)a.D * N, state = (size_t)(p.c0 + ch) * N + 4 * sub;
-    constexpr int CQ = CT / 4;
-    const int q4 = 4 * (tid % CQ), tq = tid / CQ;
-    const bool stages = tid < C::QUADS && q4 < p.nc;
+    const int q4 = 4 * (tid % CQ), tt = tid / CQ;  // a bringing thread's group of 4 channels of a token
+    const bool stages = !walks && q4 < p.nc;
     tc::grid_dep_wait();
     if (!found) {  // no rows, no gradients
         const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (mine) *(float4*)(a.part_a + p.slot * DN + state) = zero;
-        if (tid < CQ && q4 < p.nc)
-            for (int k = 0; k < 2; ++k)
-                *(float4*)(a.part_d + ((size_t)p.slot * 2 + k) * a.D + p.c0 + q4) = zero;
+        if (mine)
+            for (int c = 0; c < 2; ++c) *(float4*)(a.part_a + p.slot * DN + state + c * N) = zero;
+        if (stages && tt < 2) *(float4*)(a.part_d + ((size_t)p.slot * 2 + tt) * a.D + p.c0 + q4) = zero;
         return;
     }
     const int blocks = (p.hi - p.lo + a.rows - 1) / a.rows;
-    F2x2 A2, e, dA;
-    {
-        const float4 v = mine ? *(const float4*)(a.A + state) : make_float4(0.f, 0.f, 0.f, 0.f);
-        A2.from(make_float4(v.x * kLog2e, v.y * kLog2e, v.z * kLog2e, v.w * kLog2e));
-        e.x = e.y = dA.x = dA.y = 0;
-    }
-    // the gradient of the state behind the block, from the blocks after it
-    if (mine)
-        for (int j = p.slot - p.block + blocks - 1; j > p.slot; --j) {
-            const float sum = a.sums[(size_t)j * a.D + p.c0 + ch];
-            const F2x2 w = decay(A2, tc::f2_pack(sum, sum));
-            F2x2 v;
-            v.from(*(const float4*)(a.ends + j * DN + state));
-            e.x = tc::f2_fma(w.x, e.x, v.x);
-            e.y = tc::f2_fma(w.y, e.y, v.y);
-        }
+    const int nt = (p.last - p.first + kMark - 1) / kMark;
+    const bool gate = a.z != nullptr;
 
-    const T *x = (const T*)a.x, *dt = (const T*)a.dt, *z = (const T*)a.z, *dout = (const T*)a.dout;
-    float4 bias = make_float4(0.f, 0.f, 0.f, 0.f), Ds = bias, dDs = bias, dbias = bias;
-    if (stages) {
-        if (a.bias) bias = *(const float4*)(a.bias + p.c0 + q4);
-        if (a.Ds) Ds = *(const float4*)(a.Ds + p.c0 + q4);
-    }
-    const int nt = (p.last - p.first + kTile - 1) / kTile;
-
-    struct Raw { Quad<T> x[PT], d[PT], z[PT], o[PT], bc[PBC]; } r;
-    auto load = [&](int i) {
-        const int t0 = p.first + i * kTile;
-#pragma unroll
-        for (int k = 0; k < PT; ++k) {
-            const long long t = t0 + tq + k * (NT / CQ);
-            r.x[k].zero(); r.z[k].zero(); r.o[k].zero();
-            if (a.softplus) r.d[k].low(); else r.d[k].zero();  // a step of 0
-            if (stages && t < p.last) {
-                r.x[k].load(x + t * a.xs + p.c0 + q4);
-                r.d[k].load(dt + t * a.ds + p.c0 + q4);
-                r.o[k].load(dout + t * a.D + p.c0 + q4);
-                if (z) r.z[k].load(z + t * a.zs + p.c0 + q4);
-            }
+    if (!walks) {
+        const T *x = (const T*)a.x, *dt = (const T*)a.dt, *z = (const T*)a.z, *dout = (const T*)a.dout;
+        float4 bias = make_float4(0.f, 0.f, 0.f, 0.f), Ds = bias, dDs = bias, dbias = bias;
+        if (stages) {
+            if (a.bias) bias = *(const float4*)(a.bias + p.c0 + q4);
+            if (a.Ds) Ds = *(const float4*)(a.Ds + p.c0 + q4);
         }
-#pragma unroll
-        for (int k = 0; k < PBC; ++k) {
-            const int f = tid + k * NT, which = f / (C::BC / 2), i4 = f % (C::BC / 2);
-            const long long t = t0 + i4 / L;
-            r.bc[k].zero();
-            if (f < C::BC && t < p.last) {
-                const int at = p.g * N + 4 * (i4 % L);
-                if (which == 0) r.bc[k].load((const T*)a.B + t * a.bs + at);
-                else r.bc[k].load((const T*)a.C + t * a.cs + at);
+        const float* marks = a.marks + ((size_t)(p.lo / kMark + p.s) + (p.first - p.lo) / kMark) * DN
+                           + (size_t)p.c0 * N;
+        auto fetch = [&](int i) {
+            typename Y::Raw& r = sm.raw[i % Y::RING];
+            const int t0 = p.first + i * kMark;
+            {
+                const long long t = t0 + tt;
+                const bool in = stages && t < p.last;
+                const long long row = in ? t : p.first;
+                const int c = in ? p.c0 + q4 : p.c0;
+                copy_quad(&r.x[tt][q4], x + row * a.xs + c, in);
+                copy_quad(&r.dt[tt][q4], dt + row * a.ds + c, in);
+                copy_quad(&r.dout[tt][q4], dout + row * a.D + c, in);
+                if (gate) copy_quad(&r.z[tt][q4], z + row * a.zs + c, in);
             }
-        }
-    };
-    auto put = [&](typename S::Tile& s) {
 #pragma unroll
-        for (int k = 0; k < PT; ++k) {
-            const int tt = tq + k * (NT / CQ);
-            if (tid >= C::QUADS) break;
-            const float4 dv = r.d[k].get(), xv = r.x[k].get();
-            float4 o = r.o[k].get();
-            if (z) {
-                const float4 g = r.z[k].get();
-                o.x *= silu(g.x); o.y *= silu(g.y); o.z *= silu(g.z); o.w *= silu(g.w);
+            for (int f = tid; f < kMark * 2 * L; f += NT) {
+                const int which = f / (kMark * L), u = f / L % kMark, m = 4 * (f % L);
+                const bool in = t0 + u < p.last;
+                const long long row = in ? t0 + u : p.first;
+                if (which) copy_quad(&r.bc[u][1][m], (const T*)a.C + row * a.cs + p.g * N + m, in);
+                else copy_quad(&r.bc[u][0][m], (const T*)a.B + row * a.bs + p.g * N + m, in);
             }
-            float d[4] = {dv.x + bias.x, dv.y + bias.y, dv.z + bias.z, dv.w + bias.w};
+#pragma unroll
+            for (int f = tid; f < CT * L; f += NT) {
+                const bool in = f / L < p.nc;
+                copy_quad(&r.mark[f / L][4 * (f % L)], marks + i * DN + (in ? 4 * f : 0), in);
+            }
+        };
+        auto convert = [&](int i) {
+            const typename Y::Raw& r = sm.raw[i % Y::RING];
+            Quad<T> xr, dr, zr, gr;
+            xr.load(&r.x[tt][q4]);
+            dr.load(&r.dt[tt][q4]);
+            gr.load(&r.dout[tt][q4]);
+            const bool in = stages && p.first + i * kMark + tt < p.last;
+            if (a.softplus && !in) dr.low();  // a token that does not exist takes a step of 0
+            const float4 xv = xr.get(), w = dr.get();
+            float4 dy = gr.get();
+            if (gate) {
+                zr.load(&r.z[tt][q4]);
+                const float4 g = zr.get();
+                dy.x *= silu(g.x); dy.y *= silu(g.y); dy.z *= silu(g.z); dy.w *= silu(g.w);
+            }
+            float d[4] = {w.x + bias.x, w.y + bias.y, w.z + bias.z, w.w + bias.w};
             if (a.softplus) softplus4(d);
-            float4* to = (float4*)&s.td[tt][q4];
-            to[0] = make_float4(d[0], d[0] * xv.x, d[1], d[1] * xv.y);
-            to[1] = make_float4(d[2], d[2] * xv.z, d[3], d[3] * xv.w);
-            *(float4*)&s.dy[tt][q4] = o;
-        }
+            else if (!in) d[0] = d[1] = d[2] = d[3] = 0.f;
+            float4* to = (float4*)&sm.td[i & 1][tt][q4];
+            const float4 lo = make_float4(d[0], d[0] * xv.x, d[1], d[1] * xv.y);
+            const float4 hi = make_float4(d[2], d[2] * xv.z, d[3], d[3] * xv.w);
+            const bool odd = tid / 4 % 2;  // (halves in turn: 8 lanes' 128 bytes are in 32 banks)
+            to[odd] = odd ? hi : lo;
+            to[!odd] = odd ? lo : hi;
+            *(float4*)&sm.dy[i & 1][tt][q4] = dy;
 #pragma unroll
-        for (int k = 0; k < PBC; ++k) {
-            const int f = tid + k * NT, which = f / (C::BC / 2), i4 = f % (C::BC / 2);
-            if (f < C::BC) *(float4*)&s.bc[i4 / L][which][4 * (i4 % L)] = r.bc[k].get();
-        }
-    };
-
-    const float* marks = a.marks + ((size_t)(p.lo / kTile + p.s) + (p.first - p.lo) / kTile) * DN + state;
-    load(nt - 1);
-    F2x2 dAt;  // a tile's part, so that long sums are sums of sums
-    for (int i = nt - 1; i >= 0; --i) {
-        typename S::Tile& s = sm.tiles[i & 1];
-        put(s);
-        F2x2 h0;
-        h0.from(mine ? *(const float4*)(marks + i * DN) : make_float4(0.f, 0.f, 0.f, 0.f));
-        __syncthreads();
-        dAt.x = dAt.y = 0;
-        // the states again, and y
-        F2x2 hh[kTile];
-#pragma unroll
-        for (int b = 0; b < kTile; b += YB) {
-            float y[YB];
-#pragma unroll
-            for (int j = 0; j < YB; ++j) {
-                const float2 td = s.td[b + j][ch];
-                const F2x2 B = *(const F2x2*)&s.bc[b + j][0][4 * sub];
-                const F2x2 w = decay(A2, tc::f2_pack(td.x, td.x)), &h = b + j ? hh[b + j - 1] : h0;
-                const uint64_t dx = tc::f2_pack(td.y, td.y);
-                hh[b + j].x = tc::f2_fma(w.x, h.x, tc::f2_mul(dx, B.x));
-                hh[b + j].y = tc::f2_fma(w.y, h.y, tc::f2_mul(dx, B.y));
-                if (z) y[j] = hh[b + j].dot(*(const F2x2*)&s.bc[b + j][1][4 * sub]);
+            for (int f = tid; f < kMark * 2 * L; f += NT) {
+                const int which = f / (kMark * L), u = f / L % kMark, m = 4 * (f % L);
+                Quad<T> v;
+                v.load(&r.bc[u][which][m]);
+                *(float4*)&sm.bc[i & 1][u][which][m] = v.get();
             }
-            if (z) {
-#pragma unroll
-                for (int j = 0; j < YB; j += L) {
-                    float v[L];
-#pragma unroll
-                    for (int k = 0; k < L; ++k) v[k] = y[j + k];
-                    sm.sums[2][b + j + sub][ch] = lane_sums<L>(v, sub);
-                }
-            }
-        }
-        // and back
-#pragma unroll
-        for (int b = kTile - YB; b >= 0; b -= YB) {
-            float s1[YB], s2[YB];
-#pragma unroll
-            for (int j2 = YB - 2; j2 >= 0; j2 -= 2) {
-#pragma unroll
-                for (int j = j2 + 1; j >= j2; --j) {
-                    const int t = b + j;
-                    const float2 td = s.td[t][ch];
-                    const float dyv = s.dy[t][ch];
-                    const F2x2 B = *(const F2x2*)&s.bc[t][0][4 * sub];
-                    const F2x2 Cv = *(const F2x2*)&s.bc[t][1][4 * sub];
-                    const uint64_t dy = tc::f2_pack(dyv, dyv), dx = tc::f2_pack(td.y, td.y);
-                    const uint64_t dd = tc::f2_pack(td.x, td.x);
-                    F2x2 v;
-                    v.x = tc::f2_mul(dy, hh[t].x);
-                    v.y = tc::f2_mul(dy, hh[t].y);
-                    *(F2x2*)&sm.pair[warp][t & 1][1][4 * lane] = v;
-                    e.x = tc::f2_fma(dy, Cv.x, e.x);
-                    e.y = tc::f2_fma(dy, Cv.y, e.y);
-                    v.x = tc::f2_mul(dx, e.x);
-                    v.y = tc::f2_mul(dx, e.y);
-                    *(F2x2*)&sm.pair[warp][t & 1][0][4 * lane] = v;
-                    s1[j] = e.dot(B);
-                    const F2x2 w = decay(A2, dd);
-                    e.x = tc::f2_mul(w.x, e.x);
-                    e.y = tc::f2_mul(w.y, e.y);
-                    const F2x2& h = t ? hh[t - 1] : h0;
-                    v.x = tc::f2_mul(e.x, h.x);
-                    v.y = tc::f2_mul(e.y, h.y);
-                    s2[j] = v.dot(A2);
-                    dAt.x = tc::f2_fma(dd, v.x, dAt.x);
-                    dAt.y = tc::f2_fma(dd, v.y, dAt.y);
-                }
-                // Sums over the warp's channels for two tokens: 4 L groups of 4 values, of which a
-                // lane adds those of 4 channels.  They are read in turn, since two groups' rows
-                // start in the same bank.
-                __syncwarp();
-                {
-                    const int group = lane % (4 * L), part = lane / (4 * L), k = group / L, m = group % L;
-                    const float* from = &sm.pair[warp][k / 2][k % 2][4 * m];
-                    F2x2 v = *(const F2x2*)(from + (4 * part + (k & 3)) * N);
-#pragma unroll
-                    for (int c = 1; c < 4; ++c) {
-                        const F2x2 u = *(const F2x2*)(from + (4 * part + ((k + c) & 3)) * N);
-                        v.x = tc::f2_fma(u.x, tc::f2_pack(1.f, 1.f), v.x);
-                        v.y = tc::f2_fma(u.y, tc::f2_pack(1.f, 1.f), v.y);
-                    }
-                    *(F2x2*)&sm.parts[warp * S::SPLIT + part][b + j2 + k / 2][k % 2][4 * m] = v;
-                }
-                __syncwarp();
-            }
-#pragma unroll
-            for (int j = 0; j < YB; j += L) {
-                float v[L], u[L];
-#pragma unroll
-                for (int k = 0; k < L; ++k) { v[k] = s1[j + k]; u[k] = s2[j + k]; }
-                sm.sums[0][b + j + sub][ch] = lane_sums<L>(v, sub);
-                sm.sums[1][b + j + sub][ch] = lane_sums<L>(u, sub);
-            }
-        }
-        __syncthreads();
-        dA.x = tc::f2_fma(dAt.x, tc::f2_pack(1.f, 1.f), dA.x);
-        dA.y = tc::f2_fma(dAt.y, tc::f2_pack(1.f, 1.f), dA.y);
-        // the tile's gradients
-#pragma unroll
-        for (int k = 0; k < PT; ++k) {
-            const int tt = tq + k * (NT / CQ);
-            const long long t = p.first + i * kTile + tt;
-            if (!stages || t >= p.last) continue;
-            const float4 xq = r.x[k].get(), dq = r.d[k].get(), oq = r.o[k].get(), zq = r.z[k].get();
-            const float xv[4] = {xq.x, xq.y, xq.z, xq.w};
-            const float rv[4] = {dq.x + bias.x, dq.y + bias.y, dq.z + bias.z, dq.w + bias.w};
-            const float ov[4] = {oq.x, oq.y, oq.z, oq.w}, zv[4] = {zq.x, zq.y, zq.z, zq.w};
+        };
+        // dx, ddt, dz of a tile
+        auto finish = [&](int i) {
+            const long long t = p.first + i * kMark + tt;
+            if (!stages || t >= p.last) return;
+            const typename Y::Raw& r = sm.raw[i % Y::RING];
+            Quad<T> xr, dr, zr, gr;
+            xr.load(&r.x[tt][q4]);
+            dr.load(&r.dt[tt][q4]);
+            const float4 xq = xr.get(), dq = dr.get(), dyq = *(const float4*)&sm.dy[i & 1][tt][q4];
+            const float4 s1 = *(const float4*)&sm.sums[i & 1][0][tt][q4];
+            const float4 s2 = *(const float4*)&sm.sums[i & 1][1][tt][q4];
+            const float xv[4] = {xq.x, xq.y, xq.z, xq.w}, dy[4] = {dyq.x, dyq.y, dyq.z, dyq.w};
+            const float raw[4] = {dq.x + bias.x, dq.y + bias.y, dq.z + bias.z, dq.w + bias.w};
             const float Dv[4] = {Ds.x, Ds.y, Ds.z, Ds.w};
-            float gx[4], gd[4], gz[4], gD[4];
+            const float s[4] = {s1.x, s1.y, s1.z, s1.w}, q[4] = {s2.x, s2.y, s2.z, s2.w};
+            float gx[4], gd[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float s1 = sm.sums[0][tt][q4 + j], s2 = sm.sums[1][tt][q4 + j] * kLn2;
-                const float dy = s.dy[tt][q4 + j], d = s.td[tt][q4 + j].x;
-                gx[j] = fmaf(s1, d, Dv[j] * dy);
-                gd[j] = fmaf(s1, xv[j], s2);
-                if (a.softplus) gd[j] *= sigmoid(rv[j]);
-                gD[j] = dy * xv[j];
-                if (z) {
-                    const float y = fmaf(Dv[j], xv[j], sm.sums[2][tt][q4 + j]), g = sigmoid(zv[j]);
-                    gz[j] = ov[j] * y * g * fmaf(zv[j], 1.f - g, 1.f);
-                }
+                gx[j] = fmaf(s[j], sm.td[i & 1][tt][q4 + j].x, Dv[j] * dy[j]);
+                gd[j] = fmaf(s[j], xv[j], q[j] * kLn2);
+                if (a.softplus) gd[j] *= sigmoid(raw[j]);
             }
-            dDs.x += gD[0]; dDs.y += gD[1]; dDs.z += gD[2]; dDs.w += gD[3];
+            dDs.x = fmaf(dy[0], xv[0], dDs.x); dDs.y = fmaf(dy[1], xv[1], dDs.y);
+            dDs.z = fmaf(dy[2], xv[2], dDs.z); dDs.w = fmaf(dy[3], xv[3], dDs.w);
             dbias.x += gd[0]; dbias.y += gd[1]; dbias.z += gd[2]; dbias.w += gd[3];
             const size_t at = t * a.D + p.c0 + q4;
             store4((T*)a.dx + at, make_float4(gx[0], gx[1], gx[2], gx[3]));
             store4((T*)a.ddt + at, make_float4(gd[0], gd[1], gd[2], gd[3]));
-            if (z) store4((T*)a.dz + at, make_float4(gz[0], gz[1], gz[2], gz[3]));
-        }
-        for (int f = tid; f < kTile * 2 * L; f += NT) {  // groups of 4 values of dB and dC
-            const int tt = f / (2 * L);
-            const long long t = p.first + i * kTile + tt;
-            const float* from = &sm.parts[0][0][0][0] + 4 * f;
-            float4 v = *(const float4*)from;
+            if (gate) {
+                zr.load(&r.z[tt][q4]);
+                gr.load(&r.dout[tt][q4]);
+                const float4 zq = zr.get(), oq = gr.get(), yq = *(const float4*)&sm.sums[i & 1][2][tt][q4];
+                const float zv[4] = {zq.x, zq.y, zq.z, zq.w}, o[4] = {oq.x, oq.y, oq.z, oq.w};
+                const float y[4] = {yq.x, yq.y, yq.z, yq.w};
+                float gz[4];
 #pragma unroll
-            for (int k = 1; k < S::PARTS; ++k) {
-                const float4 u = *(const float4*)(from + (size_t)k * kTile * 2 * N);
+                for (int j = 0; j < 4; ++j) {
+                    const float g = logistic(zv[j]);
+                    gz[j] = o[j] * fmaf(Dv[j], xv[j], y[j]) * g * fmaf(zv[j], 1.f - g, 1.f);
+                }
+                store4((T*)a.dz + at, make_float4(gz[0], gz[1], gz[2], gz[3]));
+            }
+        };
+        // dB and dC of 4 tokens: 4 threads add up a quarter of the pairs of channels each, in turn
+        auto sum_pairs = [&](int i, int half) {
+#pragma unroll
+            for (int f = tid; f < 32 * L; f += NT) {
+                const int m = f % L, part = f / L % 4, which = f / (4 * L) % 2, u = f / (8 * L);
+                const float* from = &sm.pair[half][u][which][part][4 * m];
+                float4 v = *(const float4*)from;
+#pragma unroll
+                for (int k = 1; k < CG / 4; ++k) {
+                    const float4 w = *(const float4*)(from + 4 * k * N);
+                    v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+                }
+#pragma unroll
+                for (int k = L; k <= 2 * L; k *= 2) {
+                    v.x += __shfl_xor_sync(0xffffffffu, v.x, k);
+                    v.y += __shfl_xor_sync(0xffffffffu, v.y, k);
+                    v.z += __shfl_xor_sync(0xffffffffu, v.z, k);
+                    v.w += __shfl_xor_sync(0xffffffffu, v.w, k);
+                }
+                const long long t = p.first + i * kMark + half * kHalf + u;
+                if (part == 0 && t < p.last)
+                    *(float4*)(a.part_bc + (((size_t)p.tile * a.T + t) * a.G + p.g) * 2 * N + which * N + 4 * m) = v;
+            }
+        };
+        fetch(nt - 1);
+        asm volatile("cp.async.commit_group;");
+        if (nt > 1) fetch(nt - 2);
+        asm volatile("cp.async.commit_group;");
+        asm volatile("cp.async.wait_group 1;");
+        bring_barrier(NT);
+        convert(nt - 1);
+        for (int i = nt - 1; i >= 0; --i) {
+            asm volatile("cp.async.wait_group 0;");
+            __syncthreads();  // tile i is there, and i + 1 walked
+            if (i > 1) fetch(i - 2);
+            asm volatile("cp.async.commit_group;");
+            if (i + 1 < nt) {
+                sum_pairs(i + 1, 0);
+                finish(i + 1);
+            }
+            if (i > 0) convert(i - 1);
+            __syncthreads();  // the tile's later tokens are walked
+            sum_pairs(i, 1);
+        }
+        __syncthreads();
+        sum_pairs(0, 0);
+        finish(0);
+        // dDs and dbias over the tokens of a tile, which 8 threads hold; all of them are done with sums
+        bring_barrier(NT);
+        *(float4*)&sm.sums[0][0][tt][q4] = dDs;
+        *(float4*)&sm.sums[0][1][tt][q4] = dbias;
+        bring_barrier(NT);
+        if (stages && tt < 2) {
+            float4 v = *(const float4*)&sm.sums[0][tt][0][q4];
+#pragma unroll
+            for (int k = 1; k < kMark; ++k) {
+                const float4 u = *(const float4*)&sm.sums[0][tt][k][q4];
                 v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
             }
-            if (t < p.last)
-                *(float4*)(a.part_bc + (((size_t)p.tile * a.T + t) * a.G + p.g) * 2 * N + 4 * (f % (2 * L))) = v;
+            *(float4*)(a.part_d + ((size_t)p.slot * 2 + tt) * a.D + p.c0 + q4) = v;
         }
-        if (i > 0) load(i - 1);
-        __syncthreads();
+        return;
     }
-    if (mine) *(float4*)(a.part_a + p.slot * DN + state) = dA.get();
-    // dDs and dbias: over the tokens of a tile, which NT / CQ threads hold
-    constexpr int ROWS = C::QUADS / CQ / PT;
-    if (tid < C::QUADS) {
-        *(float4*)&sm.sums[0][tq][q4] = dDs;
-        *(float4*)&sm.sums[1][tq][q4] = dbias;
+
+    States<4> A2[2], e[2], dA[2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        A2[c].zero(); e[c].zero(); dA[c].zero();
+        if (!mine) continue;
+        A2[c].read(a.A + state + c * N);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) A2[c].v[k] = tc::f2_mul(A2[c].v[k], twice(kLog2e));
+        // the gradient of the state behind the block, from the blocks after it
+        for (int j = p.slot - p.block + blocks - 1; j > p.slot; --j) {
+            const uint64_t sum = twice(a.sums[(size_t)j * a.D + p.c0 + ch + c]);
+            States<4> v;
+            v.read(a.ends + j * DN + state + c * N);
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                e[c].v[k] = tc::f2_fma(ex2_pair(tc::f2_mul(A2[c].v[k], sum)), e[c].v[k], v.v[k]);
+        }
+    }
+    for (int i = nt - 1; i >= 0; --i) {
+        __syncthreads();
+        const float2(*td)[CT] = sm.td[i & 1];
+        const float(*dys)[CT] = sm.dy[i & 1];
+        const float(*bc)[2][N] = sm.bc[i & 1];
+        States<4> h0[2], hh[kMark][2], dAt[2];  // dAt: the tile's part, so that long sums are sums of sums
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            h0[c].read(&sm.raw[i % Y::RING].mark[ch + c][4 * sub]);
+            dAt[c].zero();
+        }
+#pragma unroll
+        for (int t = 0; t < kMark; ++t) {
+            const float4 v = *(const float4*)&td[t][ch];
+            States<4> B;
+            B.read(&bc[t][0][4 * sub]);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const uint64_t d = twice(c ? v.z : v.x), u = twice(c ? v.w : v.y);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const uint64_t w = ex2_pair(tc::f2_fma(A2[c].v[k], d, twice(kUp)));
+                    hh[t][c].v[k] = tc::f2_fma(w, t ? hh[t - 1][c].v[k] : h0[c].v[k], tc::f2_mul(u, B.v[k]));
+                }
+            }
+        }
+#pragma unroll
+        for (int half = 1; half >= 0; --half) {
+            float s1[2][kHalf], s2[2][kHalf], y[2][kHalf];
+#pragma unroll
+            for (int u = kHalf - 1; u >= 0; --u) {
+                const int t = half * kHalf + u;
+                const float4 v = *(const float4*)&td[t][ch];
+                const float2 g = *(const float2*)&dys[t][ch];
+                States<4> B, Cv, dB, dC;
+                B.read(&bc[t][0][4 * sub]);
+                Cv.read(&bc[t][1][4 * sub]);
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const uint64_t dy = twice(c ? g.y : g.x), d = twice(c ? v.z : v.x), dx = twice(c ? v.w : v.y);
+                    uint64_t ya = 0, sa = 0, qa = 0;
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const uint64_t h = hh[t][c].v[k], hp = t ? hh[t - 1][c].v[k] : h0[c].v[k];
+                        uint64_t& ek = e[c].v[k];
+                        ya = k ? tc::f2_fma(h, Cv.v[k], ya) : tc::f2_mul(h, Cv.v[k]);
+                        dC.v[k] = c ? tc::f2_fma(dy, h, dC.v[k]) : tc::f2_mul(dy, h);
+                        ek = tc::f2_fma(dy, Cv.v[k], ek);
+                        dB.v[k] = c ? tc::f2_fma(dx, ek, dB.v[k]) : tc::f2_mul(dx, ek);
+                        sa = k ? tc::f2_fma(ek, B.v[k], sa) : tc::f2_mul(ek, B.v[k]);
+                        ek = tc::f2_mul(ex2_pair(tc::f2_fma(A2[c].v[k], d, twice(kUp))), ek);
+                        const uint64_t q = tc::f2_mul(ek, hp);
+                        qa = k ? tc::f2_fma(q, A2[c].v[k], qa) : tc::f2_mul(q, A2[c].v[k]);
+                        dAt[c].v[k] = tc::f2_fma(d, q, dAt[c].v[k]);
+                    }
+                    float lo, hi;
+                    tc::f2_unpack(ya, lo, hi);
+                    y[c][u] = lo + hi;
+                    tc::f2_unpack(sa, lo, hi);
+                    s1[c][u] = lo + hi;
+                    tc::f2_unpack(qa, lo, hi);
+                    s2[c][u] = lo + hi;
+                }
+                dB.write(&sm.pair[half][u][0][cg][4 * sub]);
+                dC.write(&sm.pair[half][u][1][cg][4 * sub]);
+            }
+            constexpr int M = L == 2 ? 2 : 1;
+            float r[3][2][M];
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                token_sums<L>(s1[c], sub, r[0][c]);
+                token_sums<L>(s2[c], sub, r[1][c]);
+                if (gate) token_sums<L>(y[c], sub, r[2][c]);
+            }
+#pragma unroll
+            for (int k = 0; k < 3; ++k)
+#pragma unroll
+                for (int m = 0; m < M; ++m)
+                    if (k < 2 || gate)
+                        *(float2*)&sm.sums[i & 1][k][half * kHalf + sub % 4 + m * L][ch] =
+                            make_float2(r[k][0][m], r[k][1][m]);
+            if (half) __syncthreads();
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) dA[c].v[k] = tc::f2_fma(dAt[c].v[k], twice(1.f), dA[c].v[k]);
     }
     __syncthreads();
-    for (int f = tid; f < 2 * CT; f += NT) {
-        const int k = f / CT, c = f % CT;
-        if (c >= p.nc) continue;
-        float v = 0.f;
+    if (!mine) return;
 #pragma unroll
-        for (int j = 0; j < ROWS; ++j) v += sm.sums[k][j][c];
-        a.part_d[((size_t)p.slot * 2 + k) * a.D + p.c0 + c] = v;
-    }
+    for (int c = 0; c < 2; ++c) dA[c].write(a.part_a + p.slot * DN + state + c * N);
 }
 
 // Sums over blocks, in their order: dB and dC over the blocks of a group (4 values a thread), then dA,
@@ -349,16 +419,18 @@ __global__ void __launch_bounds__(256) ssm_bwd_sum_kernel(SsmArgs a, int tiles, 
     *(float4*)to = v;
 }
 
-template <typename T, int L>
+template <typename T, int N>
 cudaError_t bwd(const SsmArgs& a, bool after, cudaStream_t s)
 {
-    const int slots = block_slots(a.T, a.n, a.rows), tiles = group_tiles(a, channels(L));
-    auto kernel = ssm_bwd_kernel<T, L>;
-    static_assert(sizeof(Smem<L>) <= 113 * 1024, "two blocks an SM");
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Smem<L>));
+    using Y = Layout<T, N>;
+    const int slots = block_slots(a.T, a.n, a.rows), tiles = group_tiles(a, Y::CT);
+    auto kernel = ssm_bwd_kernel<T, N>;
+    constexpr int bytes = sizeof(typename Y::Smem);
+    static_assert(bytes <= 112 * 1024, "two blocks an SM");
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != cudaSuccess) return e;
-    e = tc::launch_after(kernel, dim3((unsigned)((long long)slots * tiles * a.G)), channels(L) * L,
-                         sizeof(Smem<L>), 0, after, s, a);
+    e = tc::launch_after(kernel, dim3((unsigned)((long long)slots * tiles * a.G)), Y::WALK + Y::BRING, bytes, 0,
+                         after, s, a);
     if (e != cudaSuccess) return e;
     const long long bc = ((long long)a.T * a.G * 2 * a.N / 4 + 255) / 256;
     const long long par = (((long long)a.D * (a.N + 2)) / 4 + 255) / 256;
@@ -368,16 +440,12 @@ cudaError_t bwd(const SsmArgs& a, bool after, cudaStream_t s)
 template <typename T>
 cudaError_t bwd_n(const SsmArgs& a, bool after, cudaStream_t s)
 {
-    switch (a.N) {
-    case 8: return bwd<T, 2>(a, after, s);
-    case 16: return bwd<T, 4>(a, after, s);
-    default: return bwd<T, 8>(a, after, s);
-    }
+    return a.N == 8 ? bwd<T, 8>(a, after, s) : a.N == 16 ? bwd<T, 16>(a, after, s) : bwd<T, 32>(a, after, s);
 }
 
 }  // namespace
 
-int ssm_bwd_tiles(const SsmArgs& a) { return group_tiles(a, channels(a.N / 4)); }
+int ssm_bwd_tiles(const SsmArgs& a) { return group_tiles(a, channels(a.N)); }
 
 cudaError_t launch_ssm_bwd(const SsmArgs& a, cudaStream_t s)
 {

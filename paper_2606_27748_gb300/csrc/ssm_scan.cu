@@ -22,9 +22,10 @@ enum Mode { kOut, kEnds, kBack };
 // How a block's threads divide a tile of tokens.  A thread holds SP states of each of CH channels.
 template <typename T, int N_, int CH, int SP, int CT_>
 struct Layout {
-    static constexpr int N = N_, CT = CT_, L = N / SP, NT = CT / CH * L;
-    static constexpr int QUADS = kTile * CT / 4, PT = QUADS / NT;  // groups of 4 channels of a token
-    static constexpr int BC = kTile * N / 2, PBC = (BC + NT - 1) / NT;  // of 4 values of B and C
+    static constexpr int N = N_, CT = CT_, L = N / SP;
+    static constexpr int WALK = CT / CH * L, BRING = 2 * CT;  // threads that walk, and that bring tiles
+    static constexpr int QUADS = kTile * CT / 4, PT = QUADS / BRING;  // groups of 4 channels of a token
+    static constexpr int BC = kTile * N / 2, PBC = (BC + BRING - 1) / BRING;  // of 4 values of B and C
     static constexpr int RING = 4;
     struct Raw {  // a tile as it lies in memory
         T x[kTile][CT], dt[kTile][CT], z[kTile][CT], bc[kTile][2][N];
@@ -37,68 +38,28 @@ struct Layout {
     };
 };
 
-__device__ __forceinline__ void copy_quad(float* to, const float* from, bool in)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
-                 "l"(from), "r"(in ? 16 : 0));
-}
-__device__ __forceinline__ void copy_quad(__nv_bfloat16* to, const __nv_bfloat16* from, bool in)
-{
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
-                 "l"(from), "r"(in ? 8 : 0));
-}
-
-// SP states as packed pairs.
-template <int SP>
-struct States {
-    uint64_t v[SP / 2];
-    __device__ __forceinline__ void read(const float* p)
-    {
-#pragma unroll
-        for (int i = 0; i < SP / 4; ++i) {
-            const ulonglong2 u = *(const ulonglong2*)(p + 4 * i);
-            v[2 * i] = u.x;
-            v[2 * i + 1] = u.y;
-        }
-    }
-    __device__ __forceinline__ void write(float* p) const
-    {
-#pragma unroll
-        for (int i = 0; i < SP / 4; ++i) *(ulonglong2*)(p + 4 * i) = make_ulonglong2(v[2 * i], v[2 * i + 1]);
-    }
-    __device__ __forceinline__ void zero()
-    {
-#pragma unroll
-        for (int i = 0; i < SP / 2; ++i) v[i] = 0;
-    }
-};
-__device__ __forceinline__ uint64_t ex2_pair(uint64_t x)
-{
-    float a, b;
-    tc::f2_unpack(x, a, b);
-    return tc::f2_pack(ex2(a), ex2(b));
-}
-__device__ __forceinline__ uint64_t twice(float x) { return tc::f2_pack(x, x); }
-
 // kOut: outputs, last states and marks.  kEnds: what a block leaves behind, without outputs.  kBack:
 // the same of the gradient of the state, from the block's last token to its first:
 // e_{t-1} = exp(D_t A) (e_t + dy_t C_t).
 //
 // Tiles of 16 tokens are copied to shared memory two ahead, their steps and inputs computed one
 // ahead, once for all states; a tile's outputs are finished after the next block barrier, of which
-// there is one a tile.
+// there is one a tile.  That is the second half of the threads' work: a walk's tokens follow one
+// another, and few sequences leave few warps to hide it behind.
 template <typename T, int N, int CH, int SP, int CT, int MODE>
-__global__ void __launch_bounds__(CT / CH * (N / SP)) ssm_scan_kernel(SsmArgs a)
+__global__ void __launch_bounds__(CT / CH * (N / SP) + 2 * CT, N <= 16 ? 3 : 1) ssm_scan_kernel(SsmArgs a)
 {
     using Y = Layout<T, N, CH, SP, CT>;
-    constexpr int L = Y::L, NT = Y::NT, PT = Y::PT, PBC = Y::PBC, CQ = CT / 4;
+    constexpr int L = Y::L, NT = Y::BRING, PT = Y::PT, PBC = Y::PBC, CQ = CT / 4;
     extern __shared__ __align__(16) unsigned char smem[];
     typename Y::Smem& sm = *(typename Y::Smem*)smem;
-    const int tid = threadIdx.x;
+    // some threads walk the tokens, the others bring them and take the outputs away
+    const bool walks = threadIdx.x < Y::WALK;
+    const int tid = walks ? threadIdx.x : threadIdx.x - Y::WALK;
     Place p;
     const bool found = find_place<CT>(a, blockIdx.x, p);
     const int ch = tid / L * CH, sub = tid % L;
-    const bool mine = ch < p.nc;  // (channels come in fours)
+    const bool mine = walks && ch < p.nc;  // (channels come in fours)
     const size_t state = (size_t)(p.c0 + ch) * N + SP * sub;  // within [D][N]; the next channel's + N
     const size_t DN = (size_t)a.D * N;
     // the kernel ahead left ends and sums; nothing is read of them before this
@@ -156,29 +117,34 @@ __global__ void __launch_bounds__(CT / CH * (N / SP)) ssm_scan_kernel(SsmArgs a)
     const bool gate = MODE != kEnds && a.z;
     const int nt = (p.last - p.first + kTile - 1) / kTile;
     auto start = [&](int i) { return MODE == kBack ? p.first + (nt - 1 - i) * kTile : p.first + i * kTile; };
+    // a thread's first groups in memory, and how far on the next ones and the next tile's are
+    const long long t0 = (MODE == kBack ? p.first + (nt - 1) * kTile : p.first) + tq;
+    const T* from[3] = {(const T*)a.dt + t0 * a.ds + p.c0 + q4,
+                        MODE == kBack ? (const T*)a.dout + t0 * a.D + p.c0 + q4
+                                      : (const T*)a.x + t0 * a.xs + p.c0 + q4,
+                        (const T*)a.z + (gate ? t0 * a.zs + p.c0 + q4 : 0)};
+    const long long per_row[3] = {a.ds, MODE == kBack ? (long long)a.D : a.xs, a.zs};
     auto fetch = [&](int i) {
         typename Y::Raw& r = sm.raw[i % Y::RING];
-        const int t0 = start(i);
-        const size_t c = p.c0 + q4;
+        const int t0 = start(i), left = p.last - t0;  // rows that exist, from the tile's first
+        const long long tiles = MODE == kBack ? -i : i;
 #pragma unroll
         for (int k = 0; k < PT; ++k) {
             const int tt = tq + k * (NT / CQ);
-            const long long t = t0 + tt;
-            const bool in = stages && t < p.last;
-            const size_t row = in ? t : p.first;  // (what is not read has a valid address too)
-            const size_t at = in ? c : p.c0;
-            copy_quad(&r.dt[tt][q4], (const T*)a.dt + row * a.ds + at, in);
-            if (MODE == kBack) copy_quad(&r.x[tt][q4], (const T*)a.dout + row * a.D + at, in);
-            else copy_quad(&r.x[tt][q4], (const T*)a.x + row * a.xs + at, in);
-            if (gate) copy_quad(&r.z[tt][q4], (const T*)a.z + row * a.zs + at, in);
+            const bool in = stages && tt < left;
+            const long long row = in ? tiles * kTile + k * (NT / CQ) : 0;
+            // (what is not read has a valid address too: the tensor's)
+            copy_quad(&r.dt[tt][q4], in ? from[0] + row * per_row[0] : (const T*)a.dt, in);
+            copy_quad(&r.x[tt][q4], in ? from[1] + row * per_row[1] : (const T*)a.dt, in);
+            if (gate) copy_quad(&r.z[tt][q4], in ? from[2] + row * per_row[2] : (const T*)a.dt, in);
         }
 #pragma unroll
         for (int k = 0; k < PBC; ++k) {
             const int e = tid + k * NT;
             if (Y::BC % NT && e >= Y::BC) break;
             const int which = e / (Y::BC / 2), i4 = e % (Y::BC / 2), tt = i4 / (N / 4), m = 4 * (i4 % (N / 4));
-            const bool in = t0 + tt < p.last;
-            const size_t row = in ? t0 + tt : p.first;
+            const bool in = tt < left;
+            const long long row = in ? t0 + tt : p.first;
             if (which == 0 && MODE != kBack) copy_quad(&r.bc[tt][0][m], (const T*)a.B + row * a.bs + p.g * N + m, in);
             if (which == 1 && MODE != kEnds) copy_quad(&r.bc[tt][1][m], (const T*)a.C + row * a.cs + p.g * N + m, in);
         }
@@ -206,8 +172,10 @@ __global__ void __launch_bounds__(CT / CH * (N / SP)) ssm_scan_kernel(SsmArgs a)
             else if (!(stages && t0 + tt < p.last)) d[0] = d[1] = d[2] = d[3] = 0.f;
             if (MODE != kBack) { v.x *= d[0]; v.y *= d[1]; v.z *= d[2]; v.w *= d[3]; }
             float4* to = (float4*)&sm.td[i & 1][tt][q4];
-            to[0] = make_float4(d[0], v.x, d[1], v.y);
-            to[1] = make_float4(d[2], v.z, d[3], v.w);
+            const float4 lo = make_float4(d[0], v.x, d[1], v.y), hi = make_float4(d[2], v.z, d[3], v.w);
+            const bool odd = tid / 4 % 2;  // (halves in turn: 8 lanes' 128 bytes are in 32 banks)
+            to[odd] = odd ? hi : lo;
+            to[!odd] = odd ? lo : hi;
         }
 #pragma unroll
         for (int k = 0; k < PBC; ++k) {
@@ -245,32 +213,43 @@ __global__ void __launch_bounds__(CT / CH * (N / SP)) ssm_scan_kernel(SsmArgs a)
 
     float sum[CH] = {};
     float* marks = MODE == kOut && a.marks && mine
-        ? a.marks + ((size_t)(p.lo / kTile + p.s) + (p.first - p.lo) / kTile) * DN + state : nullptr;
-    fetch(0);
-    asm volatile("cp.async.commit_group;");
-    if (nt > 1) fetch(1);
-    asm volatile("cp.async.commit_group;");
-    asm volatile("cp.async.wait_group 1;");
-    __syncthreads();
-    convert(0);
-    for (int i = 0; i < nt; ++i) {
-        asm volatile("cp.async.wait_group 0;");
-        __syncthreads();
-        if (i + 2 < nt) fetch(i + 2);
+        ? a.marks + ((size_t)(p.lo / kMark + p.s) + (p.first - p.lo) / kMark) * DN + state : nullptr;
+    if (!walks) {
+        fetch(0);
         asm volatile("cp.async.commit_group;");
-        if (MODE == kOut && i > 0) finish(i - 1);
-        if (i + 1 < nt) convert(i + 1);
-        if (marks) {
-#pragma unroll
-            for (int c = 0; c < CH; ++c) h[c].write(marks + c * N);
-            marks += DN;
+        if (nt > 1) fetch(1);
+        asm volatile("cp.async.commit_group;");
+        asm volatile("cp.async.wait_group 1;");
+        bring_barrier(NT);
+        convert(0);
+        for (int i = 0; i < nt; ++i) {
+            asm volatile("cp.async.wait_group 0;");
+            __syncthreads();  // tile i's steps are there, and i - 1's outputs
+            if (i + 2 < nt) fetch(i + 2);
+            asm volatile("cp.async.commit_group;");
+            if (MODE == kOut && i > 0) finish(i - 1);
+            if (i + 1 < nt) convert(i + 1);
         }
+        if (MODE == kOut) {
+            __syncthreads();
+            finish(nt - 1);
+        }
+        return;
+    }
+    for (int i = 0; i < nt; ++i) {
+        __syncthreads();
         const float2(*td)[CT] = sm.td[i & 1];
         const float(*bc)[2][N] = sm.bc[i & 1];
         constexpr int YB = MODE == kOut && L > 2 ? L : 2;
-#pragma unroll 2
+#pragma unroll
         for (int b = 0; b < kTile; b += YB) {
             float y[CH][YB];
+            // (a mark only where tokens are: the slot after a sequence's last is another's)
+            if (b % kMark == 0 && marks && start(i) + b < p.last) {
+#pragma unroll
+                for (int c = 0; c < CH; ++c) h[c].write(marks + c * N);
+                marks += DN;
+            }
 #pragma unroll
             for (int jj = 0; jj < YB; ++jj) {
                 const int j = MODE == kBack ? kTile - 1 - b - jj : b + jj;
@@ -323,10 +302,7 @@ __global__ void __launch_bounds__(CT / CH * (N / SP)) ssm_scan_kernel(SsmArgs a)
             }
         }
     }
-    if (MODE == kOut) {
-        __syncthreads();
-        finish(nt - 1);
-    }
+    if (MODE == kOut) __syncthreads();
     if (!mine) return;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -406,7 +382,7 @@ cudaError_t scan(const SsmArgs& a, int mode, bool after, cudaStream_t s)
     constexpr int bytes = sizeof(typename Y::Smem);
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != cudaSuccess) return e;
-    return tc::launch_after(kernel, dim3((unsigned)blocks), Y::NT, bytes, 0, after, s, a);
+    return tc::launch_after(kernel, dim3((unsigned)blocks), Y::WALK + Y::BRING, bytes, 0, after, s, a);
 }
 template <typename T>
 cudaError_t scan_n(const SsmArgs& a, int mode, bool after, cudaStream_t s)
@@ -423,7 +399,6 @@ cudaError_t decode(const SsmArgs& a, cudaStream_t s)
     const dim3 grid((unsigned)(((long long)a.D * L + 255) / 256), (unsigned)((a.n + kSeqs - 1) / kSeqs));
     return tc::launch_after(ssm_decode_kernel<T, L>, grid, 256, 0, 0, false, s, a);
 }
-
 template <typename T>
 cudaError_t decode_n(const SsmArgs& a, cudaStream_t s)
 {

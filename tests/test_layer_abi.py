@@ -103,7 +103,7 @@ def test_ssm_gate_stride_save_and_workspace(lib):
     assert 256 <= need[0] <= need[1]
     assert _fwd(lib, s, n=255) == FLEX_EWORKSPACE and _fwd(lib, s, n=need[0] - 1) == FLEX_EWORKSPACE
     assert _bwd(lib, s, n=need[1] - 1) == FLEX_EWORKSPACE
-    assert lib.flex_ssm_save_bytes(b) == (100 // 16 + 3) * 64 * 16 * 4
+    assert lib.flex_ssm_save_bytes(b) == (100 // 8 + 3) * 64 * 16 * 4
 
 
 def test_ssm_binding_refuses():
