@@ -24,21 +24,32 @@ __device__ __forceinline__ int rows_end(const int* cu, int n, int T) { return mi
 
 constexpr int kAhead = 8;  // rows whose loads are in flight together
 
+struct Four {  // 4 channels' values as packed pairs
+    uint64_t a, b;
+    __device__ __forceinline__ void set(float4 v) { a = tc::f2_pack(v.x, v.y); b = tc::f2_pack(v.z, v.w); }
+    __device__ __forceinline__ float4 get() const
+    {
+        float4 v;
+        tc::f2_unpack(a, v.x, v.y);
+        tc::f2_unpack(b, v.z, v.w);
+        return v;
+    }
+    __device__ __forceinline__ void add(const Four& x, const Four& y)  // += x y
+    {
+        a = tc::f2_fma(x.a, y.a, a);
+        b = tc::f2_fma(x.b, y.b, b);
+    }
+};
 // 4 channels' parameters: w [D][W], fp32.
 template <int W>
-__device__ __forceinline__ void load_taps(float (&w)[W][4], float (&b)[4], const ConvArgs& a, int c)
+__device__ __forceinline__ void load_taps(Four (&w)[W], Four& bias, const ConvArgs& a, int c)
 {
     float v[4 * W];
     load_params<4 * W>(v, a.w + (size_t)c * W);
-    if (a.bias) load_params<4>(b, a.bias + c);
+    bias.set(a.bias ? *(const float4*)(a.bias + c) : make_float4(0.f, 0.f, 0.f, 0.f));
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        if (!a.bias) b[q] = 0.f;
-#pragma unroll
-        for (int j = 0; j < W; ++j) w[j][q] = v[q * W + j];
-    }
+    for (int j = 0; j < W; ++j) w[j].set(make_float4(v[j], v[W + j], v[2 * W + j], v[3 * W + j]));
 }
-__device__ __forceinline__ void spread(float (&v)[4], float4 u) { v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w; }
 
 template <typename T, int W>
 __global__ void __launch_bounds__(128) conv_fwd_kernel(ConvArgs a, long long run_blocks)
@@ -68,7 +79,7 @@ __global__ void __launch_bounds__(128) conv_fwd_kernel(ConvArgs a, long long run
     const int t0 = (int)first, t1 = min(end, t0 + a.run);
     int s = find_row(a.cu, a.n, t0), lo, hi;
     seq_rows(a.cu, s, a.T, lo, hi);
-    float w[W][4], b[4], win[W - 1][4];
+    Four w[W], b, win[W - 1];
     load_taps<W>(w, b, a, c);
     // the rows ahead of row t of sequence s
     auto before = [&](int t) {
@@ -79,15 +90,39 @@ __global__ void __launch_bounds__(128) conv_fwd_kernel(ConvArgs a, long long run
             v.zero();
             if (u >= lo) v.load(x + (long long)u * a.xs + c);
             else if (a.S0) v.load((const T*)a.S0 + ((long long)s * (W - 1) + (u - lo + W - 1)) * a.D + c);
-            spread(win[j], v.get());
+            win[j].set(v.get());
         }
     };
     before(t0);
-    for (int t = t0; t < t1; t += kAhead) {
+    const T* from = x + (long long)t0 * a.xs + c;
+    T* to = (T*)a.out + (long long)t0 * a.D + c;
+    auto step = [&](const Quad<T>& row, T* at) {
+        Four v, p = b;
+        v.set(row.get());
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) p.add(w[j], win[j]);
+        p.add(w[W - 1], v);
+        float4 y = p.get();
+        if (a.silu) {
+            y.x *= logistic(y.x); y.y *= logistic(y.y); y.z *= logistic(y.z); y.w *= logistic(y.w);
+        }
+        store4(at, y);
+#pragma unroll
+        for (int j = 0; j + 1 < W - 1; ++j) win[j] = win[j + 1];
+        win[W - 2] = v;
+    };
+    for (int t = t0; t < t1; t += kAhead, from += kAhead * a.xs, to += (long long)kAhead * a.D) {
         Quad<T> rows[kAhead];
+        if (t + kAhead <= min(t1, hi)) {  // one sequence's rows, as most are: nothing to look at
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) rows[k].load(from + k * a.xs);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) step(rows[k], to + (long long)k * a.D);
+            continue;
+        }
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
-            if (t + k < t1) rows[k].load(x + (long long)(t + k) * a.xs + c);
+            if (t + k < t1) rows[k].load(from + k * a.xs);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             if (t + k >= t1) break;
@@ -98,20 +133,7 @@ __global__ void __launch_bounds__(128) conv_fwd_kernel(ConvArgs a, long long run
                 } while (t + k >= hi && s + 1 < a.n);
                 before(t + k);
             }
-            float v[4], y[4];
-            spread(v, rows[k].get());
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                float p = b[q];
-#pragma unroll
-                for (int j = 0; j < W - 1; ++j) p = fmaf(w[j][q], win[j][q], p);
-                p = fmaf(w[W - 1][q], v[q], p);
-                y[q] = a.silu ? p * logistic(p) : p;
-#pragma unroll
-                for (int j = 0; j + 1 < W - 1; ++j) win[j][q] = win[j + 1][q];
-                win[W - 2][q] = v[q];
-            }
-            store4((T*)a.out + (long long)(t + k) * a.D + c, make_float4(y[0], y[1], y[2], y[3]));
+            step(rows[k], to + (long long)k * a.D);
         }
     }
 }
@@ -129,30 +151,87 @@ __global__ void __launch_bounds__(256, 2) conv_bwd_kernel(ConvArgs a)
     const bool mine = c < a.D;
     const int end = rows_end(a.cu, a.n, a.T);
     const long long first = ((long long)blockIdx.y * 8 + threadIdx.y) * a.run;
-    const T *x = (const T*)a.x, *dout = (const T*)a.dout;
-    float dw[W][4] = {}, db[4] = {};
+    Four dw[W], db;
+    db.a = db.b = 0;
+#pragma unroll
+    for (int j = 0; j < W; ++j) dw[j].a = dw[j].b = 0;
     if (mine && first < end) {
         const int t0 = (int)first, t1 = min(end, t0 + a.run), t2 = min(end, t1 + W - 1);
         int s = find_row(a.cu, a.n, t0), lo, hi;
         seq_rows(a.cu, s, a.T, lo, hi);
-        float w[W][4], b[4], win[W - 1][4], acc[W][4];
+        Four w[W], b, win[W - 1], acc[W];
         load_taps<W>(w, b, a, c);
 #pragma unroll
-        for (int j = 0; j < W; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+        for (int j = 0; j < W; ++j) acc[j].a = acc[j].b = 0;
+        const T *x = (const T*)a.x + (long long)t0 * a.xs + c, *dout = (const T*)a.dout + (long long)t0 * a.D + c;
+        T* dx = (T*)a.dx + (long long)(t0 - (W - 1)) * a.D + c;  // (the row that row t0 completes)
 #pragma unroll
         for (int j = 0; j < W - 1; ++j) {
-            const int u = t0 - (W - 1) + j;
-            const float4 v = u >= lo ? load4(x + (long long)u * a.xs + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-            win[j][0] = v.x; win[j][1] = v.y; win[j][2] = v.z; win[j][3] = v.w;
+            Quad<T> v;
+            v.zero();
+            if (t0 - (W - 1) + j >= lo) v.load(x + (long long)(j - (W - 1)) * a.xs);
+            win[j].set(v.get());
         }
-        for (int t = t0; t < t1 + W - 1; t += kBack) {
+        // Row u's share in its own and the rows' ahead; `at` of these are of its sequence.
+        auto add = [&](const Quad<T>& px, const Quad<T>& pd, bool own, int at) {
+            Four v, p = b, dp;
+            v.set(px.get());
+#pragma unroll
+            for (int j = 0; j < W - 1; ++j) p.add(w[j], win[j]);
+            p.add(w[W - 1], v);
+            float4 g = pd.get();
+            if (a.silu) {
+                const float4 q = p.get();
+                const float4 l = make_float4(logistic(q.x), logistic(q.y), logistic(q.z), logistic(q.w));
+                g.x *= l.x * fmaf(q.x, 1.f - l.x, 1.f);
+                g.y *= l.y * fmaf(q.y, 1.f - l.y, 1.f);
+                g.z *= l.z * fmaf(q.z, 1.f - l.z, 1.f);
+                g.w *= l.w * fmaf(q.w, 1.f - l.w, 1.f);
+            }
+            dp.set(g);
+            if (own) {
+                Four one;
+                one.a = one.b = tc::f2_pack(1.f, 1.f);
+                db.add(dp, one);
+#pragma unroll
+                for (int j = 0; j < W - 1; ++j) dw[j].add(dp, win[j]);
+                dw[W - 1].add(dp, v);
+            }
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+                if (W - 1 - j <= at) acc[j].add(w[j], dp);
+#pragma unroll
+            for (int j = 0; j + 1 < W - 1; ++j) win[j] = win[j + 1];
+            win[W - 2] = v;
+        };
+        auto next = [&]() {
+#pragma unroll
+            for (int j = 0; j + 1 < W; ++j) acc[j] = acc[j + 1];
+            acc[W - 1].a = acc[W - 1].b = 0;
+        };
+        for (int t = t0; t < t1 + W - 1; t += kBack, x += kBack * a.xs, dout += (long long)kBack * a.D,
+                 dx += (long long)kBack * a.D) {
             Quad<T> px[kBack], pd[kBack];
+            if (t >= t0 + W - 1 && t >= lo + W - 1 && t + kBack <= min(t1, hi)) {  // nothing to look at
+#pragma unroll
+                for (int k = 0; k < kBack; ++k) {
+                    px[k].load(x + k * a.xs);
+                    pd[k].load(dout + (long long)k * a.D);
+                }
+#pragma unroll
+                for (int k = 0; k < kBack; ++k) {
+                    add(px[k], pd[k], true, W - 1);
+                    store4(dx + (long long)k * a.D, acc[0].get());
+                    next();
+                }
+                continue;
+            }
 #pragma unroll
             for (int k = 0; k < kBack; ++k) {
                 px[k].zero(); pd[k].zero();
                 if (t + k < t2) {
-                    px[k].load(x + (long long)(t + k) * a.xs + c);
-                    pd[k].load(dout + (long long)(t + k) * a.D + c);
+                    px[k].load(x + k * a.xs);
+                    pd[k].load(dout + (long long)k * a.D);
                 }
             }
 #pragma unroll
@@ -166,55 +245,19 @@ __global__ void __launch_bounds__(256, 2) conv_bwd_kernel(ConvArgs a)
                             seq_rows(a.cu, s, a.T, lo, hi);
                         } while (u >= hi && s + 1 < a.n);
 #pragma unroll
-                        for (int j = 0; j < W - 1; ++j) win[j][0] = win[j][1] = win[j][2] = win[j][3] = 0.f;
+                        for (int j = 0; j < W - 1; ++j) win[j].a = win[j].b = 0;
                     }
-                    float v[4], g[4];
-                    spread(v, px[k].get());
-                    spread(g, pd[k].get());
-                    const bool own = u < t1;
-                    const int at = u - lo;  // rows of the sequence ahead of this one
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        float p = b[q];
-#pragma unroll
-                        for (int j = 0; j < W - 1; ++j) p = fmaf(w[j][q], win[j][q], p);
-                        p = fmaf(w[W - 1][q], v[q], p);
-                        float dp = g[q];
-                        if (a.silu) {
-                            const float l = logistic(p);
-                            dp *= l * fmaf(p, 1.f - l, 1.f);
-                        }
-                        if (own) {
-                            db[q] += dp;
-#pragma unroll
-                            for (int j = 0; j < W - 1; ++j) dw[j][q] = fmaf(dp, win[j][q], dw[j][q]);
-                            dw[W - 1][q] = fmaf(dp, v[q], dw[W - 1][q]);
-                        }
-#pragma unroll
-                        for (int j = 0; j < W; ++j)
-                            if (W - 1 - j <= at) acc[j][q] = fmaf(w[j][q], dp, acc[j][q]);
-#pragma unroll
-                        for (int j = 0; j + 1 < W - 1; ++j) win[j][q] = win[j + 1][q];
-                        win[W - 2][q] = v[q];
-                    }
+                    add(px[k], pd[k], u < t1, u - lo);
                 }
-                const int done = u - (W - 1);  // nothing more is added to this row's dx
-                if (done >= t0)
-                    store4((T*)a.dx + (long long)done * a.D + c,
-                           make_float4(acc[0][0], acc[0][1], acc[0][2], acc[0][3]));
-#pragma unroll
-                for (int j = 0; j + 1 < W; ++j)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) acc[j][q] = acc[j + 1][q];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) acc[W - 1][q] = 0.f;
+                // nothing more is added to this row's dx
+                if (u - (W - 1) >= t0) store4(dx + (long long)k * a.D, acc[0].get());
+                next();
             }
         }
     }
 #pragma unroll
-    for (int j = 0; j < W; ++j)
-        sums[threadIdx.y][j][threadIdx.x] = make_float4(dw[j][0], dw[j][1], dw[j][2], dw[j][3]);
-    sums[threadIdx.y][W][threadIdx.x] = make_float4(db[0], db[1], db[2], db[3]);
+    for (int j = 0; j < W; ++j) sums[threadIdx.y][j][threadIdx.x] = dw[j].get();
+    sums[threadIdx.y][W][threadIdx.x] = db.get();
     __syncthreads();
     if (threadIdx.y <= W && mine) {
         float4 v = sums[0][threadIdx.y][threadIdx.x];
