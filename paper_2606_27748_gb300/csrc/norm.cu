@@ -28,7 +28,7 @@ __device__ __forceinline__ float group_sum(float v, int tpr, float* slots)
     return v;
 }
 
-__device__ __forceinline__ long long row_count(const NormArgs& a)
+__device__ __forceinline__ int row_count(const NormArgs& a)
 {
     return a.end ? min(max(__ldg(a.end), 0), a.T) : a.T;
 }
@@ -38,22 +38,23 @@ __global__ void __launch_bounds__(kThreads) norm_fwd_kernel(NormArgs a, int tpr)
 {
     constexpr int V = Pack<T>::N;
     __shared__ float slots[kThreads / 32];
-    const long long item = (long long)blockIdx.x * (kThreads / tpr) + threadIdx.x / tpr;
-    const int lane = threadIdx.x % tpr;
-    const long long t = item / a.H;
-    const int h = (int)(item % a.H);
-    const bool in = t < row_count(a);
+    // (tpr is a power of two, and rows times heads fit 31 bits)
+    const int lane = threadIdx.x & (tpr - 1), shift = 31 - __clz(tpr);
+    const unsigned item = blockIdx.x * (kThreads >> shift) + (threadIdx.x >> shift);
+    const unsigned t = item / (unsigned)a.H, h = item - t * a.H;
+    const bool in = t < (unsigned)row_count(a);
+    const size_t out = (size_t)item * a.d;
     Pack<T> xr[K], zr[K], rr[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const int e = (lane + k * tpr) * V;
         xr[k].zero(); zr[k].zero(); rr[k].zero();
         if (!in || e >= a.d) continue;
-        xr[k].load((const T*)a.x + t * a.xs + (long long)h * a.d + e);
-        if (a.res) rr[k].load((const T*)a.res + t * a.rs + (long long)h * a.d + e);
-        if (a.z) zr[k].load((const T*)a.z + t * a.zs + (long long)h * a.d + e);
+        xr[k].load((const T*)a.x + t * a.xs + h * a.d + e);
+        if (a.res) rr[k].load((const T*)a.res + t * a.rs + h * a.d + e);
+        if (a.z) zr[k].load((const T*)a.z + t * a.zs + h * a.d + e);
     }
-    const int p = a.heads > 1 ? h * a.d : 0;
+    const int p = a.heads > 1 ? (int)h * a.d : 0;
     float r[K][V], sum = 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -67,7 +68,7 @@ __global__ void __launch_bounds__(kThreads) norm_fwd_kernel(NormArgs a, int tpr)
             for (int q = 0; q < V; ++q) r[k][q] = a.scale ? fmaf(e < a.d ? s[q] : 0.f, r[k][q], y[q]) : r[k][q] + y[q];
             if (in && e < a.d) {
                 rr[k].set(r[k]);
-                rr[k].store((T*)a.total + item * a.d + e);
+                rr[k].store((T*)a.total + out + e);
             }
         }
 #pragma unroll
@@ -90,7 +91,7 @@ __global__ void __launch_bounds__(kThreads) norm_fwd_kernel(NormArgs a, int tpr)
             if (a.z) r[k][q] *= g[q] * logistic(g[q]);
         }
         xr[k].set(r[k]);
-        xr[k].store((T*)a.out + item * a.d + e);
+        xr[k].store((T*)a.out + out + e);
     }
 }
 
@@ -102,15 +103,32 @@ __global__ void __launch_bounds__(kThreads, K == 1 ? 2 : 1) norm_bwd_kernel(Norm
 {
     constexpr int V = Pack<T>::N;
     __shared__ float slots[2][kThreads / 32];
-    const int per = kThreads / tpr, lane = threadIdx.x % tpr;
-    const long long group = (long long)blockIdx.x * per + threadIdx.x / tpr, groups = (long long)gridDim.x * per;
-    const long long items = row_count(a) * a.H;
+    const int lane = threadIdx.x & (tpr - 1), shift = 31 - __clz(tpr), per = kThreads >> shift;
+    const int mine = threadIdx.x >> shift;
+    const unsigned group = blockIdx.x * per + mine, groups = gridDim.x * per;
+    const unsigned items = (unsigned)row_count(a) * a.H;
     // groups % H == 0 where the parameters are a head's own: a group's head is always the same
     const int p = a.heads > 1 ? (int)(group % a.H) * a.d : 0;
     float dw[K][V] = {}, ds[RES ? K : 1][V] = {};
+    // one unit a thread: its parameters stay
+    float w1[V], s1[V];
+    auto params = [&](int e, float (&w)[V], float (&s)[V]) {
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+            w[q] = 0.f;
+            s[q] = a.scale || e >= a.d ? 0.f : 1.f;
+        }
+        if (e >= a.d) return;
+        load_params<V>(w, a.w + p + e);
+        if (RES && a.scale) load_params<V>(s, a.scale + p + e);
+    };
+    if (K == 1) params(lane * V, w1, s1);
+    // the row and head that are loaded next
+    unsigned t = group / (unsigned)a.H, h = group - t * a.H;
+    const unsigned rows_on = groups / (unsigned)a.H, heads_on = groups - rows_on * a.H;
     Pack<T> xr[K], rr[K], zr[K], gr[K], tr[K];
-    auto load = [&](long long item) {
-        const long long t = item / a.H, at = item % a.H * a.d;
+    auto load = [&](unsigned item) {
+        const size_t at = h * a.d, out = (size_t)item * a.d;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int e = (lane + k * tpr) * V;
@@ -119,35 +137,38 @@ __global__ void __launch_bounds__(kThreads, K == 1 ? 2 : 1) norm_bwd_kernel(Norm
             if (GATE) zr[k].zero();
             if (item >= items || e >= a.d) continue;
             xr[k].load((const T*)a.x + t * a.xs + at + e);
-            gr[k].load((const T*)a.dout + item * a.d + e);
+            gr[k].load((const T*)a.dout + out + e);
             if (RES) rr[k].load((const T*)a.res + t * a.rs + at + e);
-            if (RES && a.dtotal) tr[k].load((const T*)a.dtotal + item * a.d + e);
+            if (RES && a.dtotal) tr[k].load((const T*)a.dtotal + out + e);
             if (GATE) zr[k].load((const T*)a.z + t * a.zs + at + e);
         }
+        t += rows_on;
+        h += heads_on;
+        if (h >= (unsigned)a.H) { h -= a.H; ++t; }
     };
     int turn = 0;
     load(group);
     // (every group of a block makes the same number of rounds: the sums may have block barriers)
-    for (long long base = group - threadIdx.x / tpr; base < items; base += groups, turn ^= 1) {
-        const long long item = base + threadIdx.x / tpr;
+    for (unsigned base = blockIdx.x * per; base < items; base += groups, turn ^= 1) {
+        const unsigned item = base + mine;
+        const size_t out = (size_t)item * a.d;
         const bool in = item < items;
         const float rstd = in ? a.rstd[item] : 0.f;
         float n[K][V], dn[K][V], sum = 0.f;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int e = (lane + k * tpr) * V;
-            float w[V], g[V], x[V];
+            float w[V], s[V], g[V], x[V];
+            if (K > 1) params(e, w, s);
 #pragma unroll
-            for (int q = 0; q < V; ++q) w[q] = 0.f;
-            if (e < a.d) load_params<V>(w, a.w + p + e);
+            for (int q = 0; q < V; ++q)
+                if (K == 1) { w[q] = w1[q]; s[q] = s1[q]; }
             xr[k].get(n[k]);
             if (RES) {
-                float y[V], s[V];
+                float y[V];
                 rr[k].get(y);
-                if (a.scale && e < a.d) load_params<V>(s, a.scale + p + e);
 #pragma unroll
-                for (int q = 0; q < V; ++q)
-                    n[k][q] = a.scale ? fmaf(e < a.d ? s[q] : 0.f, n[k][q], y[q]) : n[k][q] + y[q];
+                for (int q = 0; q < V; ++q) n[k][q] = fmaf(s[q], n[k][q], y[q]);
             }
             gr[k].get(g);
             if (GATE) zr[k].get(x);
@@ -166,7 +187,7 @@ __global__ void __launch_bounds__(kThreads, K == 1 ? 2 : 1) norm_bwd_kernel(Norm
             }
             if (GATE && in && e < a.d) {
                 zr[k].set(dz);
-                zr[k].store((T*)a.dz + item * a.d + e);
+                zr[k].store((T*)a.dz + out + e);
             }
         }
         sum = group_sum(sum, tpr, slots[turn]) / (float)a.d;
@@ -195,15 +216,15 @@ __global__ void __launch_bounds__(kThreads, K == 1 ? 2 : 1) norm_bwd_kernel(Norm
                     ds[k][q] = fmaf(dr[q], x[q], ds[k][q]);
                 }
                 o.set(dr);
-                o.store((T*)a.dres + item * a.d + e);
+                o.store((T*)a.dres + out + e);
                 if (!a.scale) continue;
-                float s[V];
-                load_params<V>(s, a.scale + p + e);
+                float w[V], s[V];
+                if (K > 1) params(e, w, s);
 #pragma unroll
-                for (int q = 0; q < V; ++q) dr[q] *= s[q];
+                for (int q = 0; q < V; ++q) dr[q] *= K > 1 ? s[q] : s1[q];
             }
             o.set(dr);
-            o.store((T*)a.dx + item * a.d + e);
+            o.store((T*)a.dx + out + e);
         }
     }
     const int cols = RES && a.scale ? 2 * a.d : a.d;
