@@ -74,6 +74,13 @@ __device__ __forceinline__ float exp_neg(float x)
 // softplus(x) = max(x, 0) + log1p(t), t = exp(-|x|) in [0, 1], of 4 values.  log1p(t) / t is a
 // polynomial of degree 8 (least relative error, 3e-8, found by exchange), so that small steps keep
 // their relative accuracy.  0 for -inf, exactly.
+__device__ constexpr float soft(int k)
+{
+    constexpr float c[9] = {9.9999996988e-01f, -4.9999493140e-01f, 3.3319096808e-01f,
+                            -2.4842982216e-01f, 1.9106006770e-01f, -1.3663245815e-01f,
+                            7.8225952120e-02f, -2.9505238928e-02f, 5.2326943023e-03f};
+    return c[k];
+}
 __device__ __forceinline__ void softplus4(float (&x)[4])
 {
 #pragma unroll
@@ -81,21 +88,20 @@ __device__ __forceinline__ void softplus4(float (&x)[4])
         float a = max_nan(-fabsf(x[i]), -111.f), b = max_nan(-fabsf(x[i + 1]), -111.f);
         tc::f2_unpack(tc::f2_mul(tc::f2_pack(a, b), tc::f2_pack(kLog2e, kLog2e)), a, b);
         const uint64_t t = tc::f2_pack(ex2(a), ex2(b));
-        constexpr float c[9] = {9.9999996988e-01f, -4.9999493140e-01f, 3.3319096808e-01f,
-                                -2.4842982216e-01f, 1.9106006770e-01f, -1.3663245815e-01f,
-                                7.8225952120e-02f, -2.9505238928e-02f, 5.2326943023e-03f};
-        uint64_t p = tc::f2_pack(c[8], c[8]);
+        uint64_t p = tc::f2_pack(soft(8), soft(8));
 #pragma unroll
-        for (int k = 7; k >= 0; --k) p = tc::f2_fma(p, t, tc::f2_pack(c[k], c[k]));
+        for (int k = 7; k >= 0; --k) p = tc::f2_fma(p, t, tc::f2_pack(soft(k), soft(k)));
         p = tc::f2_fma(p, t, tc::f2_pack(fmaxf(x[i], 0.f), fmaxf(x[i + 1], 0.f)));
         tc::f2_unpack(p, x[i], x[i + 1]);
     }
 }
 __device__ __forceinline__ float softplus(float x)
 {
-    float v[4] = {x, x, x, x};
-    softplus4(v);
-    return v[0];
+    const float t = exp_neg(x);
+    float p = soft(8);
+#pragma unroll
+    for (int k = 7; k >= 0; --k) p = fmaf(p, t, soft(k));
+    return fmaf(p, t, fmaxf(x, 0.f));
 }
 // its derivative
 __device__ __forceinline__ float sigmoid(float x)

@@ -320,7 +320,7 @@ __global__ void __launch_bounds__(CT / CH * (N / SP) + 2 * CT, N <= 16 ? 3 : 1) 
 // are in flight together.
 constexpr int kSeqs = 4;
 template <typename T, int L>
-__global__ void __launch_bounds__(256) ssm_decode_kernel(SsmArgs a)
+__global__ void __launch_bounds__(256, 4) ssm_decode_kernel(SsmArgs a)
 {
     constexpr int N = 4 * L;
     const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
@@ -343,7 +343,8 @@ __global__ void __launch_bounds__(256) ssm_decode_kernel(SsmArgs a)
         d[k] = ((const T*)a.dt)[t * a.ds + c];
         if (a.z) z[k] = ((const T*)a.z)[t * a.zs + c];
     }
-    const float4 A = *(const float4*)(a.A + state);
+    float4 A2 = *(const float4*)(a.A + state);
+    A2.x *= kLog2e; A2.y *= kLog2e; A2.z *= kLog2e; A2.w *= kLog2e;
     const float bias = a.bias ? a.bias[c] : 0.f, Ds = a.Ds ? a.Ds[c] : 0.f;
 #pragma unroll
     for (int k = 0; k < kSeqs; ++k) {
@@ -355,10 +356,10 @@ __global__ void __launch_bounds__(256) ssm_decode_kernel(SsmArgs a)
         const float4 Bv = B[k].get(), Cv = C[k].get();
         const float dx = dv * xv;
         float4 v = h[k];
-        v.x = fmaf(expf(dv * A.x), v.x, dx * Bv.x);
-        v.y = fmaf(expf(dv * A.y), v.y, dx * Bv.y);
-        v.z = fmaf(expf(dv * A.z), v.z, dx * Bv.z);
-        v.w = fmaf(expf(dv * A.w), v.w, dx * Bv.w);
+        v.x = fmaf(ex2(dv * A2.x), v.x, dx * Bv.x);
+        v.y = fmaf(ex2(dv * A2.y), v.y, dx * Bv.y);
+        v.z = fmaf(ex2(dv * A2.z), v.z, dx * Bv.z);
+        v.w = fmaf(ex2(dv * A2.w), v.w, dx * Bv.w);
         *(float4*)(a.h1 + t * DN + state) = v;
         float y = fmaf(v.x, Cv.x, v.y * Cv.y) + fmaf(v.z, Cv.z, v.w * Cv.w);
 #pragma unroll
