@@ -43,6 +43,13 @@ struct Layout {
     static_assert(kMark * CT / 4 == BRING, "a group of 4 channels of a token for each");
 };
 
+__device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
 // Sums of 4 tokens' values over a channel's L lanes; lane sub returns those of tokens
 // sub, sub + L, ... (L = 8: sub % 4, twice).
 template <int L>
@@ -97,31 +104,38 @@ __global__ void __launch_bounds__(Layout<T, N>::WALK + Layout<T, N>::BRING, 2) s
         }
         const float* marks = a.marks + ((size_t)(p.lo / kMark + p.s) + (p.first - p.lo) / kMark) * DN
                            + (size_t)p.c0 * N;
-        auto fetch = [&](int i) {
+        // a thread's groups in memory (the walk goes from the last tile to the first)
+        const long long t0 = p.first + (nt - 1) * kMark + tt;
+        const T* from[4] = {x + t0 * a.xs + p.c0 + q4, dt + t0 * a.ds + p.c0 + q4, dout + t0 * a.D + p.c0 + q4,
+                            gate ? z + t0 * a.zs + p.c0 + q4 : z};
+        const long long back[4] = {kMark * a.xs, kMark * a.ds, (long long)kMark * a.D, kMark * a.zs};
+        constexpr int ROWS_BC = kMark * 2 * L / NT > 0 ? kMark * 2 * L / NT : 1;  // groups of B and C
+        const int bw = tid / (kMark * L) % 2, bu = tid / L % kMark, bm = 4 * (tid % L);
+        auto fetch = [&](int i) {  // (called for one tile after the other)
             typename Y::Raw& r = sm.raw[i % Y::RING];
-            const int t0 = p.first + i * kMark;
-            {
-                const long long t = t0 + tt;
-                const bool in = stages && t < p.last;
-                const long long row = in ? t : p.first;
-                const int c = in ? p.c0 + q4 : p.c0;
-                copy_quad(&r.x[tt][q4], x + row * a.xs + c, in);
-                copy_quad(&r.dt[tt][q4], dt + row * a.ds + c, in);
-                copy_quad(&r.dout[tt][q4], dout + row * a.D + c, in);
-                if (gate) copy_quad(&r.z[tt][q4], z + row * a.zs + c, in);
+            const int left = p.last - (p.first + i * kMark);  // rows that exist, from the tile's first
+            const bool in = stages && tt < left;
+            // (what is not read has a valid address too: the tensor's)
+            copy_quad(&r.x[tt][q4], in ? from[0] : x, in);
+            copy_quad(&r.dt[tt][q4], in ? from[1] : x, in);
+            copy_quad(&r.dout[tt][q4], in ? from[2] : x, in);
+            if (gate) copy_quad(&r.z[tt][q4], in ? from[3] : x, in);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) from[k] -= back[k];
+#pragma unroll
+            for (int k = 0; k < ROWS_BC; ++k) {
+                const int f = tid + k * NT, which = ROWS_BC > 1 ? f / (kMark * L) : bw;
+                if (f >= kMark * 2 * L) break;
+                const bool row = bu < left;
+                const long long at = row ? p.first + i * kMark + bu : p.first;
+                if (which) copy_quad(&r.bc[bu][1][bm], (const T*)a.C + at * a.cs + p.g * N + bm, row);
+                else copy_quad(&r.bc[bu][0][bm], (const T*)a.B + at * a.bs + p.g * N + bm, row);
             }
 #pragma unroll
-            for (int f = tid; f < kMark * 2 * L; f += NT) {
-                const int which = f / (kMark * L), u = f / L % kMark, m = 4 * (f % L);
-                const bool in = t0 + u < p.last;
-                const long long row = in ? t0 + u : p.first;
-                if (which) copy_quad(&r.bc[u][1][m], (const T*)a.C + row * a.cs + p.g * N + m, in);
-                else copy_quad(&r.bc[u][0][m], (const T*)a.B + row * a.bs + p.g * N + m, in);
-            }
-#pragma unroll
-            for (int f = tid; f < CT * L; f += NT) {
-                const bool in = f / L < p.nc;
-                copy_quad(&r.mark[f / L][4 * (f % L)], marks + i * DN + (in ? 4 * f : 0), in);
+            for (int k = 0; k < CT * L / NT; ++k) {
+                const int f = tid + k * NT;
+                const bool row = f / L < p.nc;
+                copy_quad(&r.mark[0][0] + 4 * f, marks + i * DN + (row ? 4 * f : 0), row);
             }
         };
         auto convert = [&](int i) {
@@ -150,11 +164,12 @@ __global__ void __launch_bounds__(Layout<T, N>::WALK + Layout<T, N>::BRING, 2) s
             to[!odd] = odd ? lo : hi;
             *(float4*)&sm.dy[i & 1][tt][q4] = dy;
 #pragma unroll
-            for (int f = tid; f < kMark * 2 * L; f += NT) {
-                const int which = f / (kMark * L), u = f / L % kMark, m = 4 * (f % L);
+            for (int k = 0; k < ROWS_BC; ++k) {
+                const int f = tid + k * NT, which = ROWS_BC > 1 ? f / (kMark * L) : bw;
+                if (f >= kMark * 2 * L) break;
                 Quad<T> v;
-                v.load(&r.bc[u][which][m]);
-                *(float4*)&sm.bc[i & 1][u][which][m] = v.get();
+                v.load(&r.bc[bu][which][bm]);
+                *(float4*)&sm.bc[i & 1][bu][which][bm] = v.get();
             }
         };
         // dx, ddt, dz of a tile
@@ -203,25 +218,27 @@ __global__ void __launch_bounds__(Layout<T, N>::WALK + Layout<T, N>::BRING, 2) s
         // dB and dC of 4 tokens: 4 threads add up a quarter of the pairs of channels each, in turn
         auto sum_pairs = [&](int i, int half) {
 #pragma unroll
-            for (int f = tid; f < 32 * L; f += NT) {
+            for (int k4 = 0; k4 < (32 * L + NT - 1) / NT; ++k4) {
+                const int f = tid + k4 * NT;
+                if (32 * L < NT && f >= 32 * L) break;  // (whole warps)
                 const int m = f % L, part = f / L % 4, which = f / (4 * L) % 2, u = f / (8 * L);
                 const float* from = &sm.pair[half][u][which][part][4 * m];
-                float4 v = *(const float4*)from;
+                States<4> v, w;
+                v.read(from);
 #pragma unroll
                 for (int k = 1; k < CG / 4; ++k) {
-                    const float4 w = *(const float4*)(from + 4 * k * N);
-                    v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+                    w.read(from + 4 * k * N);
+                    v.v[0] = f2_add(v.v[0], w.v[0]);
+                    v.v[1] = f2_add(v.v[1], w.v[1]);
                 }
 #pragma unroll
-                for (int k = L; k <= 2 * L; k *= 2) {
-                    v.x += __shfl_xor_sync(0xffffffffu, v.x, k);
-                    v.y += __shfl_xor_sync(0xffffffffu, v.y, k);
-                    v.z += __shfl_xor_sync(0xffffffffu, v.z, k);
-                    v.w += __shfl_xor_sync(0xffffffffu, v.w, k);
-                }
-                const long long t = p.first + i * kMark + half * kHalf + u;
+                for (int k = L; k <= 2 * L; k *= 2)
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+                        v.v[q] = f2_add(v.v[q], __shfl_xor_sync(0xffffffffu, (unsigned long long)v.v[q], k));
+                const int t = i * kMark + half * kHalf + u + p.first;
                 if (part == 0 && t < p.last)
-                    *(float4*)(a.part_bc + (((size_t)p.tile * a.T + t) * a.G + p.g) * 2 * N + which * N + 4 * m) = v;
+                    v.write(a.part_bc + (((size_t)p.tile * a.T + t) * a.G + p.g) * 2 * N + which * N + 4 * m);
             }
         };
         fetch(nt - 1);
@@ -368,7 +385,7 @@ __global__ void __launch_bounds__(Layout<T, N>::WALK + Layout<T, N>::BRING, 2) s
 #pragma unroll
         for (int c = 0; c < 2; ++c)
 #pragma unroll
-            for (int k = 0; k < 2; ++k) dA[c].v[k] = tc::f2_fma(dAt[c].v[k], twice(1.f), dA[c].v[k]);
+            for (int k = 0; k < 2; ++k) dA[c].v[k] = f2_add(dA[c].v[k], dAt[c].v[k]);
     }
     __syncthreads();
     if (!mine) return;
@@ -390,6 +407,7 @@ __global__ void __launch_bounds__(256) ssm_bwd_sum_kernel(SsmArgs a, int tiles, 
         const int f = (int)(i % per) * 4, g = f / (2 * a.N), k = f / a.N % 2, m = f % a.N;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         const size_t row = (size_t)a.G * 2 * a.N;
+#pragma unroll 8
         for (int j = 0; j < tiles; ++j) {
             const float4 u = *(const float4*)(a.part_bc + ((size_t)j * a.T + t) * row + f);
             v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
@@ -412,6 +430,7 @@ __global__ void __launch_bounds__(256) ssm_bwd_sum_kernel(SsmArgs a, int tiles, 
         from = a.part_d + c; to = base + c % a.D; step = 2 * (size_t)a.D;
     }
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
     for (int j = 0; j < slots; ++j) {
         const float4 u = *(const float4*)(from + j * step);
         v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
