@@ -162,27 +162,4 @@ int tc_softattn_rows(const Packed& p);        // rows of a block: 32, 128 or 256
 cudaError_t launch_tc_softattn(const AttnArgs& x, cudaStream_t s);
 cudaError_t launch_softattn_join(const AttnArgs& x, cudaStream_t s);
 
-// ---- packed batches: selective state space scan ----------------------------------------
-struct SsmArgs;  // ssm.cuh
-// Tokens of a block (a multiple of 64), or T + 1 where sequences stay whole.
-int ssm_rows(const SsmArgs& a, bool backward);
-int ssm_bwd_tiles(const SsmArgs& a);  // blocks of a group's channels in the backward
-cudaError_t launch_ssm_fwd(const SsmArgs& a, cudaStream_t s);        // 1 kernel, cut: 2
-cudaError_t launch_ssm_back_ends(const SsmArgs& a, cudaStream_t s);  // 1
-cudaError_t launch_ssm_bwd(const SsmArgs& a, cudaStream_t s);        // 2 kernels, cut: 3
-cudaError_t launch_ssm_decode(const SsmArgs& a, cudaStream_t s);
-
-// ---- packed batches: short convolution and norms around the recurrence -------------------
-struct ConvArgs;  // layer.cuh
-struct NormArgs;
-int conv_run(const ConvArgs& a);                 // rows of a thread (ConvArgs::run)
-int conv_bwd_blocks(const ConvArgs& a);          // blocks of rows, of which each leaves sums
-cudaError_t launch_conv_fwd(const ConvArgs& a, cudaStream_t s);     // 1 kernel
-cudaError_t launch_conv_bwd(const ConvArgs& a, cudaStream_t s);     // 2
-cudaError_t launch_conv_decode(const ConvArgs& a, cudaStream_t s);  // 1
-int norm_bwd_blocks(const NormArgs& a);
-size_t norm_part_floats(const NormArgs& a);
-cudaError_t launch_norm_fwd(const NormArgs& a, cudaStream_t s);     // 1
-cudaError_t launch_norm_bwd(const NormArgs& a, cudaStream_t s);     // 2
-
 }  // namespace flex

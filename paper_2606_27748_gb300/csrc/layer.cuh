@@ -97,4 +97,14 @@ __device__ __forceinline__ void load_params(float (&v)[N], const float* p)
 cudaError_t launch_column_sums(const float* from, int cols, int split, int sums, int step, int count,
                                float* to0, float* to1, cudaStream_t s);
 
+int conv_run(const ConvArgs& a);         // rows of a thread (ConvArgs::run)
+int conv_bwd_blocks(const ConvArgs& a);  // blocks of rows, of which each leaves sums
+cudaError_t launch_conv_fwd(const ConvArgs& a, cudaStream_t s);     // 1 kernel
+cudaError_t launch_conv_bwd(const ConvArgs& a, cudaStream_t s);     // 2
+cudaError_t launch_conv_decode(const ConvArgs& a, cudaStream_t s);  // 1
+int norm_bwd_blocks(const NormArgs& a);
+size_t norm_part_floats(const NormArgs& a);
+cudaError_t launch_norm_fwd(const NormArgs& a, cudaStream_t s);     // 1
+cudaError_t launch_norm_bwd(const NormArgs& a, cudaStream_t s);     // 2
+
 }  // namespace flex

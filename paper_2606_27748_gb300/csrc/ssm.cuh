@@ -9,7 +9,7 @@
 
 namespace flex {
 
-struct SsmArgs {  // (declared in flex_internal.h)
+struct SsmArgs {
     int n, T, D, G, N, bf16, softplus;
     long long xs, ds, bs, cs, zs;  // row strides in elements
     const void *x, *dt, *B, *C, *z;
@@ -30,6 +30,14 @@ struct SsmArgs {  // (declared in flex_internal.h)
     float *part_a;   // [slots][D][N]
     float *part_d;   // [slots][2][D]: dDs, dbias
 };
+
+// Tokens of a block (a multiple of 64), or T + 1 where sequences stay whole.
+int ssm_rows(const SsmArgs& a, bool backward);
+int ssm_bwd_tiles(const SsmArgs& a);  // blocks of a group's channels in the backward
+cudaError_t launch_ssm_fwd(const SsmArgs& a, cudaStream_t s);        // 1 kernel, cut: 2
+cudaError_t launch_ssm_back_ends(const SsmArgs& a, cudaStream_t s);  // 1
+cudaError_t launch_ssm_bwd(const SsmArgs& a, cudaStream_t s);        // 2 kernels, cut: 3
+cudaError_t launch_ssm_decode(const SsmArgs& a, cudaStream_t s);     // 1
 
 namespace ssm {
 

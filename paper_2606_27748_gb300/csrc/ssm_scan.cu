@@ -46,8 +46,8 @@ struct Layout {
 // ahead, once for all states; a tile's outputs are finished after the next block barrier, of which
 // there is one a tile.  That is the second half of the threads' work: a walk's tokens follow one
 // another, and few sequences leave few warps to hide it behind.
-template <typename T, int N, int CH, int SP, int CT, int MODE>
-__global__ void __launch_bounds__(CT / CH * (N / SP) + 2 * CT, N <= 16 ? 3 : 1) ssm_scan_kernel(SsmArgs a)
+template <typename T, int N, int CH, int SP, int CT, int MODE, int MIN>
+__global__ void __launch_bounds__(CT / CH * (N / SP) + 2 * CT, MIN) ssm_scan_kernel(SsmArgs a)
 {
     using Y = Layout<T, N, CH, SP, CT>;
     constexpr int L = Y::L, NT = Y::BRING, PT = Y::PT, PBC = Y::PBC, CQ = CT / 4;
@@ -377,9 +377,13 @@ cudaError_t scan(const SsmArgs& a, int mode, bool after, cudaStream_t s)
 {
     using Y = Layout<T, N, CH, SP, CT>;
     const long long blocks = (long long)block_slots(a.T, a.n, a.rows) * group_tiles(a, CT) * a.G;
-    auto kernel = mode == kOut ? ssm_scan_kernel<T, N, CH, SP, CT, kOut>
-                : mode == kEnds ? ssm_scan_kernel<T, N, CH, SP, CT, kEnds>
-                                : ssm_scan_kernel<T, N, CH, SP, CT, kBack>;
+    // Whole sequences have fewer blocks than fit: registers for loads ahead (8 x 4096, D 2048: 386 us,
+    // 408 at 3 blocks an SM); blocks of them run 3 an SM (8192, D 1280: 107 us, 113 at 2).
+    constexpr int MIN = N <= 16 ? 3 : 1;
+    auto kernel = mode == kEnds ? ssm_scan_kernel<T, N, CH, SP, CT, kEnds, MIN>
+                : mode == kBack ? ssm_scan_kernel<T, N, CH, SP, CT, kBack, MIN>
+                : a.rows > a.T ? ssm_scan_kernel<T, N, CH, SP, CT, kOut, 1>
+                               : ssm_scan_kernel<T, N, CH, SP, CT, kOut, MIN>;
     constexpr int bytes = sizeof(typename Y::Smem);
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != cudaSuccess) return e;
