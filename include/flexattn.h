@@ -349,9 +349,10 @@ size_t flex_ssm_save_bytes(const flex_ssm* shape);
  * S0: NULL or [n][D][N] fp32; S1: NULL or the same, receives each sequence's last state (an empty
  * sequence's is its first); S1 may be S0.  save: NULL, or flex_ssm_save_bytes() bytes, 256-byte
  * aligned, filled for flex_ssm_bwd; S0 must then be NULL.
- * States and sums are fp32.  A NaN in a row goes on to later rows of its sequence (of x, dt or z: of
- * its channel; of B or C: of its group) and never to other sequences.  Results repeat bit for bit.
- * 1 kernel, or 2 where sequences are cut.  Errors: FLEX_EINVAL, FLEX_EUNSUPPORTED (N, D, or more than
+ * out may be x or z.  States and sums are fp32.  A NaN in a row of x, dt or B goes on to the later
+ * rows of its sequence (of its channel, or its group) and to its last state, one of C or z to its own
+ * row's out; other sequences never see it.  Results repeat bit for bit.
+ * 1 kernel, or 3 where sequences are cut.  Errors: FLEX_EINVAL, FLEX_EUNSUPPORTED (N, D, or more than
  * 65535 sequences, 65536 channels or 1024 groups), FLEX_EWORKSPACE. */
 int flex_ssm_fwd(const flex_ssm* shape, const void* x, const void* dt, const float* A, const void* B,
                  const void* C, const float* D, const void* z, const float* dt_bias, const int* cu,
@@ -360,8 +361,8 @@ int flex_ssm_fwd(const flex_ssm* shape, const void* x, const void* dt, const flo
 
 /* Gradients of L = sum(dout * out) of flex_ssm_fwd from the zero state, with respect to all its
  * inputs, each in its input's shape (contiguous); dD, dz and ddt_bias are given exactly when D, z and
- * dt_bias are.  save: what flex_ssm_fwd left for the same shape, inputs and offsets.  Every sum has a
- * fixed order: results repeat bit for bit.  2 kernels, or 3 where sequences are cut. */
+ * dt_bias are; dx may be dout.  save: what flex_ssm_fwd left for the same shape, inputs and offsets.
+ * Every sum has a fixed order: results repeat bit for bit.  2 kernels, or 4 where sequences are cut. */
 int flex_ssm_bwd(const flex_ssm* shape, const void* x, const void* dt, const float* A, const void* B,
                  const void* C, const float* D, const void* z, const float* dt_bias, const int* cu,
                  const void* dout, const void* save, void* dx, void* ddt, float* dA, void* dB,
@@ -389,14 +390,14 @@ typedef struct {
  * x, out: [T][D]; w: [D][W], bias: NULL or [D], fp32; cu: offsets.  The rows ahead of a sequence's
  * first are those of S0 (NULL: zeros), [n][W - 1][D] in shape->dtype, oldest first; S1: NULL or the
  * same, receives each sequence's last W - 1 rows (with what S0 holds where it has fewer), and is
- * another buffer than S0.  One kernel.  Errors: FLEX_EINVAL, FLEX_EUNSUPPORTED (W, D, or more than
+ * another buffer than S0, as out is than x.  One kernel.  Errors: FLEX_EINVAL, FLEX_EUNSUPPORTED (W, D, or more than
  * 65535 sequences or 65536 channels). */
 int flex_conv_fwd(const flex_conv* shape, const void* x, const float* w, const float* bias,
                   const int* cu, const void* S0, void* S1, void* out, void* stream);
 
 /* Gradients of L = sum(dout * out) of flex_conv_fwd without S0: dx [T][D], dw [D][W], dbias [D] (given
- * exactly when bias is).  ws: flex_conv_workspace_bytes() bytes (0 if the shape is invalid or
- * unsupported).  Sums have a fixed order: results repeat bit for bit.  2 kernels. */
+ * exactly when bias is); dx is another buffer than x and dout.  ws: flex_conv_workspace_bytes() bytes
+ * (0 if the shape is invalid or unsupported).  Sums have a fixed order: results repeat bit for bit.  2 kernels. */
 size_t flex_conv_workspace_bytes(const flex_conv* shape);
 int flex_conv_bwd(const flex_conv* shape, const void* x, const float* w, const float* bias,
                   const int* cu, const void* dout, void* dx, float* dw, float* dbias, void* ws,

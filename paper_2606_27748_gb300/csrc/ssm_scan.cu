@@ -1,14 +1,18 @@
 // Selective state space scan, forward: whole sequences, and the single-token step.
 //
 // Channels and states are independent of one another but for y's sum over a channel's states, so a
-// thread walks 4 states of one channel through the tokens with everything in registers; lanes of a
-// channel add their y's up four tokens at a time.  What bounds it is arithmetic: per token and
-// state one exponential and four multiplications or additions.
+// thread walks 4 states of each of 2 channels through the tokens with everything in registers; lanes
+// of a channel add their y's up four tokens at a time.  Per token, channel and state that is one
+// exponential (32 a clock and SM) and four multiplications or additions (128): 107 us for 8 x 4096
+// tokens of 2048 channels of 16 states, 81 for their bytes.  Measured 386: 8.1 instructions a warp for
+// 32 of them (steps, sums over lanes and what feeds them), 63% of the issue slots, and 2.1 wavefronts of
+// shared memory, 63% of what an SM has.  1 channel a thread reads B and C twice as often (582 us), 4
+// leave too few warps (531).
 //
 // Where sequences and channels leave SMs idle, sequences are cut into blocks of `rows` tokens.  A
 // first kernel finds what each block's tokens leave behind by themselves and the sum of their
-// steps, exp(A sum) being the decay over the whole block; the second starts every block from the
-// ends ahead of it, joined in order.
+// steps, exp(A sum) being the decay over the whole block; a second joins these ends in order to the
+// states that the blocks start from, and the third starts from them.
 #include "flex_internal.h"
 #include "ssm.cuh"
 
@@ -89,22 +93,8 @@ __global__ void __launch_bounds__(CT / CH * (N / SP) + 2 * CT, MIN) ssm_scan_ker
         A2[c].read(a.A + state + c * N);
 #pragma unroll
         for (int i = 0; i < SP / 2; ++i) A2[c].v[i] = tc::f2_mul(A2[c].v[i], twice(kLog2e));
-        if (MODE != kBack && p.block == 0 && a.h0) {
-            // h1 may be h0: of a sequence in several blocks the first kernel keeps a copy, in the
-            // place of the last block's end, which nothing else takes
-            float* copy = a.ends + (size_t)(p.slot + blocks - 1) * DN + state + c * N;
-            h[c].read(MODE == kOut && blocks > 1 ? copy : a.h0 + p.s * DN + state + c * N);
-            if (MODE == kEnds) h[c].write(copy);
-        }
-        if (MODE == kOut && p.block > 0)
-            for (int j = p.slot - p.block; j < p.slot; ++j) {
-                const uint64_t sum = twice(a.sums[(size_t)j * a.D + p.c0 + ch + c]);
-                States<SP> e;
-                e.read(a.ends + j * DN + state + c * N);
-#pragma unroll
-                for (int i = 0; i < SP / 2; ++i)
-                    h[c].v[i] = tc::f2_fma(ex2_pair(tc::f2_mul(A2[c].v[i], sum)), h[c].v[i], e.v[i]);
-            }
+        if (MODE == kOut && blocks > 1) h[c].read(a.ends + p.slot * DN + state + c * N);
+        else if (MODE == kOut && a.h0) h[c].read(a.h0 + p.s * DN + state + c * N);
     }
 
     const int q4 = 4 * (tid % CQ), tq = tid / CQ;  // a thread's groups of channels: tokens tq + k NT / CQ
@@ -315,6 +305,53 @@ __global__ void __launch_bounds__(CT / CH * (N / SP) + 2 * CT, MIN) ssm_scan_ker
     }
 }
 
+// Blocks' ends to what their walks start from, in their place: of every sequence in several blocks the
+// states ahead of each (from S0), or (back) the gradients of the states behind each.  A thread takes 4
+// states of a channel through a sequence's blocks, the loads of 8 of them in flight (16384 tokens, D 256,
+// 256 blocks: 77 us, 111 where every block joined the ends ahead of it by itself; D 1280, 43 blocks of
+// 8192 tokens: 107 either way).
+constexpr int kJoin = 8;
+template <bool BACK>
+__global__ void __launch_bounds__(128) ssm_join_kernel(SsmArgs a)
+{
+    tc::grid_dep_wait();
+    const long long i = ((long long)blockIdx.x * 128 + threadIdx.x) * 4;
+    const size_t DN = (size_t)a.D * a.N;
+    const int s = blockIdx.y, c = (int)(i / a.N);
+    int lo, hi;
+    seq_rows(a.cu, s, a.T, lo, hi);
+    const int blocks = (hi - lo + a.rows - 1) / a.rows, first = lo / a.rows + s;
+    if (blocks < 2 || c >= a.D) return;
+    States<4> A2, h;
+    A2.read(a.A + i);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) A2.v[k] = tc::f2_mul(A2.v[k], twice(kLog2e));
+    h.zero();
+    if (!BACK && a.h0) h.read(a.h0 + s * DN + i);
+    for (int j0 = 0; j0 < blocks; j0 += kJoin) {
+        States<4> e[kJoin];
+        float sum[kJoin];
+#pragma unroll
+        for (int k = 0; k < kJoin; ++k) {
+            const int j = BACK ? blocks - 1 - j0 - k : j0 + k;
+            e[k].zero();
+            sum[k] = 0.f;
+            if (j0 + k + 1 >= blocks) continue;  // (the last one's end is nobody's start)
+            e[k].read(a.ends + (size_t)(first + j) * DN + i);
+            sum[k] = a.sums[(size_t)(first + j) * a.D + c];
+        }
+#pragma unroll
+        for (int k = 0; k < kJoin; ++k) {
+            const int j = BACK ? blocks - 1 - j0 - k : j0 + k;
+            if (j0 + k >= blocks) break;
+            h.write(a.ends + (size_t)(first + j) * DN + i);
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+                h.v[q] = tc::f2_fma(ex2_pair(tc::f2_mul(A2.v[q], twice(sum[k]))), h.v[q], e[k].v[q]);
+        }
+    }
+}
+
 // One token of every sequence.  Bound by the state, read and written once; a thread takes 4 states
 // of a channel through several sequences, so that A is read once for them and their states' loads
 // are in flight together.
@@ -429,16 +466,26 @@ int ssm_rows(const SsmArgs& a, bool backward)
     return rows > a.T ? a.T + 1 : (int)rows;
 }
 
+static cudaError_t join(const SsmArgs& a, bool back, cudaStream_t s)
+{
+    const dim3 grid((unsigned)(((long long)a.D * a.N / 4 + 127) / 128), (unsigned)a.n);
+    return tc::launch_after(back ? ssm_join_kernel<true> : ssm_join_kernel<false>, grid, 128, 0, 0, true, s, a);
+}
+
 cudaError_t launch_ssm_fwd(const SsmArgs& a, cudaStream_t s)
 {
-    cudaError_t e = cudaSuccess;
-    if (a.rows <= a.T) e = a.bf16 ? scan_n<__nv_bfloat16>(a, kEnds, false, s) : scan_n<float>(a, kEnds, false, s);
-    if (e != cudaSuccess) return e;
-    return a.bf16 ? scan_n<__nv_bfloat16>(a, kOut, a.rows <= a.T, s) : scan_n<float>(a, kOut, a.rows <= a.T, s);
+    const bool cut = a.rows <= a.T;
+    if (cut) {
+        cudaError_t e = a.bf16 ? scan_n<__nv_bfloat16>(a, kEnds, false, s) : scan_n<float>(a, kEnds, false, s);
+        if (e == cudaSuccess) e = join(a, false, s);
+        if (e != cudaSuccess) return e;
+    }
+    return a.bf16 ? scan_n<__nv_bfloat16>(a, kOut, cut, s) : scan_n<float>(a, kOut, cut, s);
 }
 cudaError_t launch_ssm_back_ends(const SsmArgs& a, cudaStream_t s)
 {
-    return a.bf16 ? scan_n<__nv_bfloat16>(a, kBack, false, s) : scan_n<float>(a, kBack, false, s);
+    const cudaError_t e = a.bf16 ? scan_n<__nv_bfloat16>(a, kBack, false, s) : scan_n<float>(a, kBack, false, s);
+    return e != cudaSuccess ? e : join(a, true, s);
 }
 cudaError_t launch_ssm_decode(const SsmArgs& a, cudaStream_t s)
 {

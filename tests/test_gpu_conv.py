@@ -153,3 +153,25 @@ def test_gradients_against_differences():
         up, down = ({**x, name: x[name].double() + s * way} for s in (1e-5, -1e-5))
         slope = (loss(up) - loss(down)) / 2e-5
         assert abs(float((g.double() * way).sum()) - slope) <= 2e-5 * float(g.double().norm() * way.norm()), name
+
+
+def test_out_is_another_buffer():
+    lens = (9,)
+    x = conv_inputs(lens, 64, 4, BF16)
+    cu = offsets(lens)
+    with pytest.raises(flexattn.FlexError):
+        flexattn.conv_fwd(x["x"], x["w"], cu, out=x["x"])
+    with pytest.raises(flexattn.FlexError):
+        flexattn.conv_bwd(x["x"], x["w"], cu, x["dout"], dx=x["dout"])
+
+
+def test_sequences_without_rows():
+    cu = offsets((0, 0, 0))
+    x = conv_inputs((5,), 64, 4, F32)
+    state, out = torch.randn(3, 3, 64, device="cuda"), torch.full_like(x["x"], 7.0)
+    _, last = flexattn.conv_fwd(x["x"], x["w"], cu, bias=x["bias"], state=state, out=out, want_state=True)
+    assert torch.equal(last, state) and (out == 7).all()
+    _, last = flexattn.conv_fwd(x["x"], x["w"], cu, out=out, want_state=True)
+    assert (last == 0).all()
+    got = flexattn.conv_bwd(x["x"], x["w"], cu, x["dout"], bias=x["bias"], dx=out)
+    assert (out == 7).all() and (got[1] == 0).all() and (got[2] == 0).all()

@@ -245,3 +245,74 @@ def test_extreme_steps():
     close(last, rlast, "last state")
     _, got = _train(x, cu)
     _check_grads(got, x, lens)
+
+
+def test_sequences_without_rows():
+    """No rows at all: the states stay, the parameters' gradients are 0, rows are left alone."""
+    lens, cu = (0, 0), offsets((0, 0))
+    x = ssm_inputs((5,), 64, 16, 1, F32, seed=12)
+    state = torch.randn(2, 64, 16, device="cuda")
+    out = torch.full_like(x["x"], 7.0)
+    _, last = _fwd(x, cu, state=state, out=out)
+    assert (out == 7).all() and torch.equal(last, state)
+    _, last = _fwd(x, cu, out=out)
+    assert (last == 0).all() and (out == 7).all()
+    save = flexattn.ssm_save(x["x"], x["B"], cu)
+    got = flexattn.ssm_bwd(*_five(x), cu, x["dout"], save, **_opt(x), dx=out)
+    assert (out == 7).all()
+    for g in (got[2], got[5], got[7]):
+        assert (g == 0).all()
+    assert lens == (0, 0)
+
+
+def test_many_sequences_of_a_token_and_one_long():
+    """Sequences that share no block, between them one of many blocks."""
+    lens = (1,) * 130 + (500,) + (2,) * 70
+    x = ssm_inputs(lens, 72, 16, 1, BF16, seed=13, pad=8)
+    cu = offsets(lens)
+    state = torch.randn(len(lens), 72, 16, device="cuda")
+    out, last = _fwd(x, cu, state=state)
+    ref, rlast = ssm_ref(x, lens, state=state)
+    close(out, ref, "out")
+    close(last, rlast, "last states")
+    _, got = _train(x, cu)
+    sent = x["dout"]
+    ref = gradients(lambda v: ssm_ref(v, lens)[:1], x, SSM, [sent])
+    for name, g, r in zip(GRADS, got, ref):
+        close(g, r, name)
+
+
+def test_calls_with_their_own_workspaces_side_by_side():
+    """Two calls on two streams, each with a workspace and save buffer of its own."""
+    lens = (700, 90)
+    cu = offsets(lens)
+    x, y = (ssm_inputs(lens, 64, 16, 1, BF16, seed=s) for s in (14, 15))
+    want = [_train(v, cu) for v in (x, y)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = []
+        for v, s in zip((x, y), streams):
+            with torch.cuda.stream(s):
+                got.append(_train(v, cu))
+        torch.cuda.synchronize()
+        for w, g in zip(want, got):
+            assert torch.equal(w[0], g[0]) and all(torch.equal(a, b) for a, b in zip(w[1], g[1]))
+
+
+def test_outputs_over_their_inputs():
+    """out may be x or z, and dx the incoming gradient: every value is read before it is replaced."""
+    lens = (300, 40)
+    cu = offsets(lens)
+    x = ssm_inputs(lens, 64, 16, 1, BF16, seed=16)
+    want, last = _fwd(x, cu)
+    for n in ("x", "z"):
+        y = {m: t.clone() for m, t in x.items()}
+        out, l2 = _fwd(y, cu, out=y[n])
+        assert out is y[n] and torch.equal(out, want) and torch.equal(l2, last)
+    _, grads = _train(x, cu)
+    save = flexattn.ssm_save(x["x"], x["B"], cu)
+    _fwd(x, cu, save=save, want_state=False)
+    up = x["dout"].clone()
+    got = flexattn.ssm_bwd(*_five(x), cu, up, save, **_opt(x), dx=up)
+    assert all(torch.equal(a, b) for a, b in zip(got, grads))

@@ -141,7 +141,9 @@ def _conv(**kw):
 
 
 def _plain_call(f, names, s, *more, **kw):
-    return f(ctypes.byref(s) if s else None, *(kw.get(n, None if n == "S0" else P) for n in names), *more, None)
+    at = {n: ctypes.c_void_p((1 << 20) + 4096 * i) for i, n in enumerate(names)}
+    at["S0"] = None
+    return f(ctypes.byref(s) if s else None, *(kw.get(n, at[n]) for n in names), *more, None)
 
 
 def _conv_calls(lib, s, n=BIG, **kw):
@@ -174,6 +176,9 @@ def test_conv_pointers_and_workspace(lib):
                 assert _plain_call(f, names, shape, *more, **{name: None}) == FLEX_EINVAL, name
     assert _plain_call(lib.flex_conv_decode, CONV_TOKEN, s) == FLEX_EINVAL  # T != n
     assert _plain_call(lib.flex_conv_fwd, CONV_FWD, s, S0=P, S1=P) == FLEX_EINVAL  # one buffer
+    assert _plain_call(lib.flex_conv_fwd, CONV_FWD, s, x=P, out=P) == FLEX_EINVAL
+    assert _plain_call(lib.flex_conv_bwd, CONV_BWD, s, BIG, x=P, dx=P) == FLEX_EINVAL
+    assert _plain_call(lib.flex_conv_bwd, CONV_BWD, s, BIG, dout=P, dx=P) == FLEX_EINVAL
     need = lib.flex_conv_workspace_bytes(ctypes.byref(s))
     assert need > 256
     assert _plain_call(lib.flex_conv_bwd, CONV_BWD, s, need - 1) == FLEX_EWORKSPACE
