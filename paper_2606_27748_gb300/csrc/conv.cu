@@ -2,9 +2,10 @@
 //   pre_t = b + sum_j w_j x_{t - (W - 1) + j},  out_t = silu(pre_t) or pre_t,
 // rows ahead of a sequence's first being its state's (the last W - 1 rows of what came before) or 0.
 //
-// A thread walks a run of rows of 4 channels with the last rows in registers, so every row is read once but for the W - 1 ahead of each run; runs are cut from all
-// rows alike, whatever the sequences.  Bound by DRAM: x read once and out written once, 32768 rows of 4096
-// channels (bf16) in 94 us, 5.7 TB/s; 16 bytes of channels a thread took 127 registers and 177 us.
+// A thread walks a run of rows of 4 channels with the last rows in registers, so every row is read once
+// but for the W - 1 ahead of each run; runs are cut from all rows alike, whatever the sequences.  Bound
+// by DRAM: x read once and out written once, 32768 rows of 4096 channels (bf16) in 94 us, 5.7 TB/s; 16
+// bytes of channels a thread took 127 registers and 177 us.
 #include "flex_internal.h"
 #include "layer.cuh"
 

@@ -4,12 +4,14 @@
 //
 // A group of threads, a power of two of them, takes a (row, head), 16 bytes at a time, and holds all of
 // it in registers between the sum and what it is for.  Bound by DRAM: every tensor is read or written
-// once.  The backward's groups stay with their
-// head and walk rows, keeping sums for dw and dscale.  32768 x 16 heads of 128 with the gate: 71 us, 5.7 TB/s
+// once.  The backward's groups stay with their head and walk rows, keeping sums for dw and dscale, with
+// the rows ahead on their way to shared memory.  32768 x 16 heads of 128 with the gate: 71 us, 5.7 TB/s
 // (1 unit of 16 bytes a thread instead of 2: 80); 16384 rows of 2048 with the residual sum: 47 us, and
-// gradients 88 for 403 MB, two blocks of 113 registers an SM.
+// gradients 66 for 403 MB (88 with one row ahead in registers).
 #include "flex_internal.h"
 #include "layer.cuh"
+
+#include <type_traits>
 
 namespace flex {
 namespace {
@@ -101,6 +103,18 @@ __global__ void __launch_bounds__(kThreads) norm_fwd_kernel(NormArgs a, int tpr)
 // With n = r rstd and g = dout silu(z): dn = g w, dr = rstd (dn - n mean(dn n)) + dtotal;
 // dres = dr, dx = scale dr, dscale += dr x, dw += g n, dz = dout silu'(z) n w.  r is found again from
 // x and res, since a rounded sum would leave its rounding in the parameters' gradients.
+// Rows of a group on their way: x, dout, res and dtotal, z.
+template <int K, bool RES, bool GATE>
+struct Ring {
+    static constexpr int TENSORS = 2 + 2 * RES + GATE, STAGES = K == 1 ? 4 : K <= 4 ? 2 : 1;
+    static constexpr int BYTES = STAGES * TENSORS * K * kThreads * 16;
+};
+__device__ __forceinline__ void copy_unit(uint4* to, const void* from, bool in)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
+                 "l"(from), "r"(in ? 16 : 0));
+}
+
 template <typename T, int K, bool RES, bool GATE>
 __global__ void __launch_bounds__(kThreads, K == 1 ? 2 : 1) norm_bwd_kernel(NormArgs a, int tpr)
 {
@@ -129,34 +143,44 @@ __global__ void __launch_bounds__(kThreads, K == 1 ? 2 : 1) norm_bwd_kernel(Norm
     // the row and head that are loaded next
     unsigned t = group / (unsigned)a.H, h = group - t * a.H;
     const unsigned rows_on = groups / (unsigned)a.H, heads_on = groups - rows_on * a.H;
-    Pack<T> xr[K], rr[K], zr[K], gr[K], tr[K];
-    auto load = [&](unsigned item) {
+    // A thread's own units of the rows ahead, [stage][tensor][K][threads]: nobody else reads them, so
+    // their arrival is all that is waited for.
+    constexpr int TENSORS = Ring<K, RES, GATE>::TENSORS, STAGES = Ring<K, RES, GATE>::STAGES;
+    extern __shared__ __align__(16) uint4 ring[];
+    auto slot = [&](int stage, int tensor, int k) {
+        return ring + ((stage * TENSORS + tensor) * K + k) * kThreads + threadIdx.x;
+    };
+    auto load = [&](unsigned item, int stage) {
         const size_t at = h * a.d, out = (size_t)item * a.d;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int e = (lane + k * tpr) * V;
-            xr[k].zero(); gr[k].zero();
-            if (RES) { rr[k].zero(); tr[k].zero(); }
-            if (GATE) zr[k].zero();
-            if (item >= items || e >= a.d) continue;
-            xr[k].load((const T*)a.x + t * a.xs + at + e);
-            gr[k].load((const T*)a.dout + out + e);
-            if (RES) rr[k].load((const T*)a.res + t * a.rs + at + e);
-            if (RES && a.dtotal) tr[k].load((const T*)a.dtotal + out + e);
-            if (GATE) zr[k].load((const T*)a.z + t * a.zs + at + e);
+            const bool in = item < items && e < a.d;
+            const size_t xe = in ? at + e : 0, oe = in ? out + e : 0, r = in ? t : 0;
+            copy_unit(slot(stage, 0, k), (const T*)a.x + r * a.xs + xe, in);
+            copy_unit(slot(stage, 1, k), (const T*)a.dout + oe, in);
+            if (RES) copy_unit(slot(stage, 2, k), (const T*)a.res + r * a.rs + xe, in);
+            if (RES && a.dtotal) copy_unit(slot(stage, 3, k), (const T*)a.dtotal + oe, in);
+            if (GATE) copy_unit(slot(stage, TENSORS - 1, k), (const T*)a.z + r * a.zs + xe, in);
         }
+        asm volatile("cp.async.commit_group;");
         t += rows_on;
         h += heads_on;
         if (h >= (unsigned)a.H) { h -= a.H; ++t; }
     };
-    int turn = 0;
-    load(group);
+    int turn = 0, stage = 0;
+    float ahead = group < items ? a.rstd[group] : 0.f;
+    for (int k = 0; k < STAGES - 1; ++k) load(group + k * groups, k);
     // (every group of a block makes the same number of rounds: the sums may have block barriers)
     for (unsigned base = blockIdx.x * per; base < items; base += groups, turn ^= 1) {
         const unsigned item = base + mine;
+        load(item + (STAGES - 1) * groups, (stage + STAGES - 1) % STAGES);
+        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1));
+        Pack<T> xr[K], tr[RES ? K : 1];
         const size_t out = (size_t)item * a.d;
         const bool in = item < items;
-        const float rstd = in ? a.rstd[item] : 0.f;
+        const float rstd = ahead;
+        ahead = item + groups < items ? a.rstd[item + groups] : 0.f;
         float n[K][V], dn[K][V], sum = 0.f;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
@@ -166,15 +190,22 @@ __global__ void __launch_bounds__(kThreads, K == 1 ? 2 : 1) norm_bwd_kernel(Norm
 #pragma unroll
             for (int q = 0; q < V; ++q)
                 if (K == 1) { w[q] = w1[q]; s[q] = s1[q]; }
+            Pack<T> in_;
+            xr[k].load((const T*)slot(stage, 0, k));
             xr[k].get(n[k]);
             if (RES) {
                 float y[V];
-                rr[k].get(y);
+                in_.load((const T*)slot(stage, 2, k));
+                in_.get(y);
 #pragma unroll
                 for (int q = 0; q < V; ++q) n[k][q] = fmaf(s[q], n[k][q], y[q]);
             }
-            gr[k].get(g);
-            if (GATE) zr[k].get(x);
+            in_.load((const T*)slot(stage, 1, k));
+            in_.get(g);
+            if (GATE) {
+                in_.load((const T*)slot(stage, TENSORS - 1, k));
+                in_.get(x);
+            }
             float dz[V];
 #pragma unroll
             for (int q = 0; q < V; ++q) {
@@ -189,18 +220,11 @@ __global__ void __launch_bounds__(kThreads, K == 1 ? 2 : 1) norm_bwd_kernel(Norm
                 sum = fmaf(dn[k][q], n[k][q], sum);
             }
             if (GATE && in && e < a.d) {
-                zr[k].set(dz);
-                zr[k].store((T*)a.dz + out + e);
+                in_.set(dz);
+                in_.store((T*)a.dz + out + e);
             }
         }
         sum = group_sum(sum, tpr, slots[turn]) / (float)a.d;
-        Pack<T> xo[K], to[K];
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            xo[k] = xr[k];
-            if (RES) to[k] = tr[k];
-        }
-        load(item + groups);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int e = (lane + k * tpr) * V;
@@ -211,8 +235,9 @@ __global__ void __launch_bounds__(kThreads, K == 1 ? 2 : 1) norm_bwd_kernel(Norm
             Pack<T> o;
             if (RES) {
                 float y[V], x[V];
-                to[k].get(y);
-                xo[k].get(x);
+                if (a.dtotal) tr[k].load((const T*)slot(stage, 3, k)); else tr[k].zero();
+                tr[k].get(y);
+                xr[k].get(x);
 #pragma unroll
                 for (int q = 0; q < V; ++q) {
                     dr[q] += y[q];
@@ -229,6 +254,7 @@ __global__ void __launch_bounds__(kThreads, K == 1 ? 2 : 1) norm_bwd_kernel(Norm
             o.set(dr);
             o.store((T*)a.dx + out + e);
         }
+        stage = (stage + 1) % STAGES;
     }
     const int cols = RES && a.scale ? 2 * a.d : a.d;
 #pragma unroll
@@ -271,10 +297,17 @@ cudaError_t fwd(const NormArgs& a, cudaStream_t s)
 template <typename T, int K>
 cudaError_t bwd_k(const NormArgs& a, const Plan& p, cudaStream_t s)
 {
-    auto kernel = a.res ? (a.z ? norm_bwd_kernel<T, K, true, true> : norm_bwd_kernel<T, K, true, false>)
-                        : (a.z ? norm_bwd_kernel<T, K, false, true> : norm_bwd_kernel<T, K, false, false>);
     const int blocks = norm_bwd_blocks(a), groups = blocks * (kThreads / p.tpr);
-    const cudaError_t e = tc::launch_after(kernel, dim3((unsigned)blocks), kThreads, 0, 0, false, s, a, p.tpr);
+    auto launch = [&](auto res, auto gate) {
+        auto kernel = norm_bwd_kernel<T, K, res, gate>;
+        constexpr int bytes = Ring<K, res, gate>::BYTES;
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e != cudaSuccess) return e;
+        return tc::launch_after(kernel, dim3((unsigned)blocks), kThreads, bytes, 0, false, s, a, p.tpr);
+    };
+    const std::true_type yes;
+    const std::false_type no;
+    const cudaError_t e = a.res ? (a.z ? launch(yes, yes) : launch(yes, no)) : (a.z ? launch(no, yes) : launch(no, no));
     if (e != cudaSuccess) return e;
     const bool two = a.res && a.scale;
     return launch_column_sums(a.part, two ? 2 * a.d : a.d, a.d, a.heads, a.heads, groups / a.heads, a.dw,
