@@ -144,13 +144,19 @@ __global__ void __launch_bounds__(128) conv_fwd_kernel(ConvArgs a, long long run
 // Gradients: dpre_t = dout_t silu'(pre_t), dx_t = sum_j w_j dpre_{t + (W - 1) - j} within the
 // sequence, dw_j = sum_t dpre_t x_{t - (W - 1) + j}, db = sum_t dpre_t.  A thread walks its run and the
 // W - 1 rows behind it, whose dpre its last rows' dx wants; dw and db are summed over a block's 8 runs
-// in their order, and over blocks by a kernel of their own.  12817 rows of 2048 channels: 52 us for 157 MB;
-// two blocks of 128 registers an SM leave few loads in flight (three spill: 80 us; 8 rows at once: 58).
+// in their order, and over blocks by a kernel of their own.  12817 rows of 2048 channels: 48 us for 157 MB,
+// 57% of the issue slots, 816 blocks of which 304 run at a time (52 with rows in registers; three blocks an
+// SM spill: 80).
 constexpr int kBack = 4;
+// Batches of rows on their way, a thread's own: 64 KB a block.
+template <typename T>
+constexpr int kStages = 32 / (kBack * sizeof(T));
+
 template <typename T, int W>
 __global__ void __launch_bounds__(256, 2) conv_bwd_kernel(ConvArgs a)
 {
     __shared__ float4 sums[8][W + 1][32];
+    extern __shared__ __align__(16) unsigned char ring[];
     const int c = (blockIdx.y * 32 + threadIdx.x) * 4;
     const bool mine = c < a.D;
     const int end = rows_end(a.cu, a.n, a.T);
@@ -213,15 +219,35 @@ __global__ void __launch_bounds__(256, 2) conv_bwd_kernel(ConvArgs a)
             for (int j = 0; j + 1 < W; ++j) acc[j] = acc[j + 1];
             acc[W - 1].a = acc[W - 1].b = 0;
         };
-        for (int t = t0; t < t1 + W - 1; t += kBack, x += kBack * a.xs, dout += (long long)kBack * a.D,
-                 dx += (long long)kBack * a.D) {
-            Quad<T> px[kBack], pd[kBack];
-            if (t >= t0 + W - 1 && t >= lo + W - 1 && t + kBack <= min(t1, hi)) {  // nothing to look at
+        // row k of a stage's batch: x, and dout 256 quads on
+        auto slot = [&](int stage, int k) {
+            return (T*)ring + 4 * ((stage * kBack + k) * 512 + threadIdx.y * 32 + threadIdx.x);
+        };
+        auto fetch = [&](int t, int stage) {
 #pragma unroll
-                for (int k = 0; k < kBack; ++k) {
-                    px[k].load(x + k * a.xs);
-                    pd[k].load(dout + (long long)k * a.D);
-                }
+            for (int k = 0; k < kBack; ++k) {
+                const bool in = t + k < t2;
+                const long long row = in ? t + k - t0 : 0;
+                copy_quad(slot(stage, k), x + row * a.xs, in);
+                copy_quad(slot(stage, k) + 1024, dout + row * a.D, in);
+            }
+            asm volatile("cp.async.commit_group;");
+        };
+        int stage = 0;
+        constexpr int STAGES = kStages<T>;
+#pragma unroll
+        for (int k = 0; k < STAGES - 1; ++k) fetch(t0 + k * kBack, k);
+        for (int t = t0; t < t1 + W - 1; t += kBack, dx += (long long)kBack * a.D) {
+            fetch(t + (STAGES - 1) * kBack, (stage + STAGES - 1) % STAGES);
+            asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1));
+            Quad<T> px[kBack], pd[kBack];
+#pragma unroll
+            for (int k = 0; k < kBack; ++k) {
+                px[k].load(slot(stage, k));
+                pd[k].load(slot(stage, k) + 1024);
+            }
+            stage = (stage + 1) % STAGES;
+            if (t >= t0 + W - 1 && t >= lo + W - 1 && t + kBack <= min(t1, hi)) {  // nothing to look at
 #pragma unroll
                 for (int k = 0; k < kBack; ++k) {
                     add(px[k], pd[k], true, W - 1);
@@ -229,14 +255,6 @@ __global__ void __launch_bounds__(256, 2) conv_bwd_kernel(ConvArgs a)
                     next();
                 }
                 continue;
-            }
-#pragma unroll
-            for (int k = 0; k < kBack; ++k) {
-                px[k].zero(); pd[k].zero();
-                if (t + k < t2) {
-                    px[k].load(x + k * a.xs);
-                    pd[k].load(dout + (long long)k * a.D);
-                }
             }
 #pragma unroll
             for (int k = 0; k < kBack; ++k) {
@@ -358,8 +376,11 @@ template <typename T, int W>
 cudaError_t bwd(const ConvArgs& a, cudaStream_t s)
 {
     const int rows = conv_bwd_blocks(a);
-    conv_bwd_kernel<T, W><<<dim3(rows, (a.D + 127) / 128), dim3(32, 8), 0, s>>>(a);
-    const cudaError_t e = cudaGetLastError();
+    constexpr int bytes = kStages<T> * kBack * 512 * 4 * sizeof(T);
+    cudaError_t e = cudaFuncSetAttribute(conv_bwd_kernel<T, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != cudaSuccess) return e;
+    conv_bwd_kernel<T, W><<<dim3(rows, (a.D + 127) / 128), dim3(32, 8), bytes, s>>>(a);
+    e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     return launch_column_sums(a.part, (W + 1) * a.D, W * a.D, 1, 1, rows, a.dw, a.dbias, s);
 }

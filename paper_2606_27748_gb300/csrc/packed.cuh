@@ -98,6 +98,18 @@ struct Quad<__nv_bfloat16> {
     }
 };
 
+// Four elements to shared memory, not waited for; zeros where `in` is false.
+__device__ __forceinline__ void copy_quad(float* to, const float* from, bool in)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
+                 "l"(from), "r"(in ? 16 : 0));
+}
+__device__ __forceinline__ void copy_quad(__nv_bfloat16* to, const __nv_bfloat16* from, bool in)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
+                 "l"(from), "r"(in ? 8 : 0));
+}
+
 // 2^x and 1 / x, one instruction each: two units in the last place and one, denormals as 0.
 __device__ __forceinline__ float ex2(float x)
 {

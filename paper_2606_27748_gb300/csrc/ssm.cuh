@@ -124,17 +124,6 @@ __device__ __forceinline__ float silu(float x) { return x * logistic(x); }
 // no cost (dA of 8 x 1024 tokens: 1.3e-6 off without, 4.9e-7 with it and sums of sums).
 constexpr float kUp = 2e-8f;
 
-__device__ __forceinline__ void copy_quad(float* to, const float* from, bool in)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
-                 "l"(from), "r"(in ? 16 : 0));
-}
-__device__ __forceinline__ void copy_quad(__nv_bfloat16* to, const __nv_bfloat16* from, bool in)
-{
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
-                 "l"(from), "r"(in ? 8 : 0));
-}
-
 // SP states as packed pairs.
 template <int SP>
 struct States {
