@@ -315,8 +315,8 @@ int flex_softattn_fwd(const flex_packed* shape, const void* q, const void* k, co
 
 /* ---- around the recurrence ------------------------------------------------------------
  * What a recurrent layer on packed batches has besides the calls above.  Rows are [T][channels],
- * found by the same offsets; rows behind the last sequence are neither read into a result nor
- * written.  Activations may be slices of wider rows (`*_stride` elements from one to the next, at
+ * found by the same offsets, fewer than 2^30 of them; rows behind the last sequence are neither read
+ * into a result nor written.  Activations may be slices of wider rows (`*_stride` elements from one to the next, at
  * least a row, whole 16-byte units; 16-byte aligned); outputs, gradients and parameters are
  * contiguous.  Parameters and their gradients are fp32. */
 typedef struct {

@@ -231,7 +231,7 @@ __global__ void __launch_bounds__(256, 2) conv_bwd_kernel(ConvArgs a)
                 copy_quad(slot(stage, k), x + row * a.xs, in);
                 copy_quad(slot(stage, k) + 1024, dout + row * a.D, in);
             }
-            asm volatile("cp.async.commit_group;");
+            copies_commit();
         };
         int stage = 0;
         constexpr int STAGES = kStages<T>;
@@ -239,7 +239,7 @@ __global__ void __launch_bounds__(256, 2) conv_bwd_kernel(ConvArgs a)
         for (int k = 0; k < STAGES - 1; ++k) fetch(t0 + k * kBack, k);
         for (int t = t0; t < t1 + W - 1; t += kBack, dx += (long long)kBack * a.D) {
             fetch(t + (STAGES - 1) * kBack, (stage + STAGES - 1) % STAGES);
-            asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1));
+            copies_wait<STAGES - 1>();
             Quad<T> px[kBack], pd[kBack];
 #pragma unroll
             for (int k = 0; k < kBack; ++k) {

@@ -52,7 +52,7 @@ int make_ssm(const flex_ssm* s, bool z, flex::SsmArgs* a)
     if (s->D % s->G) return FLEX_EINVAL;
     if (s->N != 8 && s->N != 16 && s->N != 32) return FLEX_EUNSUPPORTED;
     if (s->D % unit(s->dtype) || s->D / s->G % 4) return FLEX_EUNSUPPORTED;
-    if (s->n > 65535 || s->T > (1 << 30) || s->D > 65536 || s->G > 1024) return FLEX_EUNSUPPORTED;
+    if (s->n > 65535 || s->T >= (1 << 30) || s->D > 65536 || s->G > 1024) return FLEX_EUNSUPPORTED;
     if (!strides(s->dtype, {s->x_stride, s->dt_stride}, s->D)) return FLEX_EINVAL;
     if (!strides(s->dtype, {s->b_stride, s->c_stride}, s->G * s->N)) return FLEX_EINVAL;
     if (z && !strides(s->dtype, {s->z_stride}, s->D)) return FLEX_EINVAL;
@@ -105,7 +105,7 @@ int make_conv(const flex_conv* s, flex::ConvArgs* a)
     if (!s || s->n < 1 || s->T < 1 || s->D < 1 || s->W < 1) return FLEX_EINVAL;
     if (s->dtype != FLEX_F32 && s->dtype != FLEX_BF16) return FLEX_EINVAL;
     if (s->W < 2 || s->W > 4 || s->D % unit(s->dtype)) return FLEX_EUNSUPPORTED;
-    if (s->n > 65535 || s->T > (1 << 30) || s->D > 65536) return FLEX_EUNSUPPORTED;
+    if (s->n > 65535 || s->T >= (1 << 30) || s->D > 65536) return FLEX_EUNSUPPORTED;
     if (!strides(s->dtype, {s->x_stride}, s->D)) return FLEX_EINVAL;
     *a = {};
     a->n = s->n; a->T = s->T; a->D = s->D; a->W = s->W;
@@ -124,7 +124,7 @@ int make_norm(const flex_norm* s, bool z, bool res, flex::NormArgs* a)
     if (s->dtype != FLEX_F32 && s->dtype != FLEX_BF16) return FLEX_EINVAL;
     if (s->heads != 1 && s->heads != s->H) return FLEX_EINVAL;
     if (s->d % unit(s->dtype) || s->d > 8192) return FLEX_EUNSUPPORTED;
-    if (s->T > (1 << 30) || s->H > 1024 || (long long)s->T * s->H >= 1LL << 31) return FLEX_EUNSUPPORTED;
+    if (s->T >= (1 << 30) || s->H > 1024 || (long long)s->T * s->H >= 1LL << 31) return FLEX_EUNSUPPORTED;
     const int row = s->H * s->d;
     if (!strides(s->dtype, {s->x_stride}, row)) return FLEX_EINVAL;
     if (z && !strides(s->dtype, {s->z_stride}, row)) return FLEX_EINVAL;

@@ -112,7 +112,7 @@ struct Ring {
 __device__ __forceinline__ void copy_unit(uint4* to, const void* from, bool in)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
-                 "l"(from), "r"(in ? 16 : 0));
+                 "l"(from), "r"(in ? 16 : 0) : "memory");
 }
 
 template <typename T, int K, bool RES, bool GATE>
@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(kThreads, K == 1 ? 2 : 1) norm_bwd_kernel(Norm
             if (RES && a.dtotal) copy_unit(slot(stage, 3, k), (const T*)a.dtotal + oe, in);
             if (GATE) copy_unit(slot(stage, TENSORS - 1, k), (const T*)a.z + r * a.zs + xe, in);
         }
-        asm volatile("cp.async.commit_group;");
+        copies_commit();
         t += rows_on;
         h += heads_on;
         if (h >= (unsigned)a.H) { h -= a.H; ++t; }
@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(kThreads, K == 1 ? 2 : 1) norm_bwd_kernel(Norm
     for (unsigned base = blockIdx.x * per; base < items; base += groups, turn ^= 1) {
         const unsigned item = base + mine;
         load(item + (STAGES - 1) * groups, (stage + STAGES - 1) % STAGES);
-        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1));
+        copies_wait<STAGES - 1>();
         Pack<T> xr[K], tr[RES ? K : 1];
         const size_t out = (size_t)item * a.d;
         const bool in = item < items;

@@ -102,12 +102,20 @@ struct Quad<__nv_bfloat16> {
 __device__ __forceinline__ void copy_quad(float* to, const float* from, bool in)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
-                 "l"(from), "r"(in ? 16 : 0));
+                 "l"(from), "r"(in ? 16 : 0) : "memory");
 }
 __device__ __forceinline__ void copy_quad(__nv_bfloat16* to, const __nv_bfloat16* from, bool in)
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
-                 "l"(from), "r"(in ? 8 : 0));
+                 "l"(from), "r"(in ? 8 : 0) : "memory");
+}
+
+// Copies since the last call are a group; all groups but the youngest N have arrived (for this thread).
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait()
+{
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
 // 2^x and 1 / x, one instruction each: two units in the last place and one, denormals as 0.

@@ -244,17 +244,17 @@ __global__ void __launch_bounds__(Layout<T, N>::WALK + Layout<T, N>::BRING, 2) s
             }
         };
         fetch(nt - 1);
-        asm volatile("cp.async.commit_group;");
+        copies_commit();
         if (nt > 1) fetch(nt - 2);
-        asm volatile("cp.async.commit_group;");
-        asm volatile("cp.async.wait_group 1;");
+        copies_commit();
+        copies_wait<1>();
         bring_barrier(NT);
         convert(nt - 1);
         for (int i = nt - 1; i >= 0; --i) {
-            asm volatile("cp.async.wait_group 0;");
+            copies_wait<0>();
             __syncthreads();  // tile i is there, and i + 1 walked
             if (i > 1) fetch(i - 2);
-            asm volatile("cp.async.commit_group;");
+            copies_commit();
             if (i + 1 < nt) {
                 sum_pairs(i + 1, 0);
                 finish(i + 1);

@@ -206,17 +206,17 @@ __global__ void __launch_bounds__(CT / CH * (N / SP) + 2 * CT, MIN) ssm_scan_ker
         ? a.marks + ((size_t)(p.lo / kMark + p.s) + (p.first - p.lo) / kMark) * DN + state : nullptr;
     if (!walks) {
         fetch(0);
-        asm volatile("cp.async.commit_group;");
+        copies_commit();
         if (nt > 1) fetch(1);
-        asm volatile("cp.async.commit_group;");
-        asm volatile("cp.async.wait_group 1;");
+        copies_commit();
+        copies_wait<1>();
         bring_barrier(NT);
         convert(0);
         for (int i = 0; i < nt; ++i) {
-            asm volatile("cp.async.wait_group 0;");
+            copies_wait<0>();
             __syncthreads();  // tile i's steps are there, and i - 1's outputs
             if (i + 2 < nt) fetch(i + 2);
-            asm volatile("cp.async.commit_group;");
+            copies_commit();
             if (MODE == kOut && i > 0) finish(i - 1);
             if (i + 1 < nt) convert(i + 1);
         }

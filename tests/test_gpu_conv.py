@@ -175,3 +175,16 @@ def test_sequences_without_rows():
     assert (last == 0).all()
     got = flexattn.conv_bwd(x["x"], x["w"], cu, x["dout"], bias=x["bias"], dx=out)
     assert (out == 7).all() and (got[1] == 0).all() and (got[2] == 0).all()
+
+
+@pytest.mark.parametrize("cu", [(3, 10, 4, 40), (-5, 7, 900, 40), (0, 50, 20, 33)], ids=str)
+def test_offsets_that_are_none(cu):
+    """Whatever the offsets hold, nothing outside the tensors is touched: the rows around stay."""
+    x = conv_inputs((40,), 64, 4, F32, seed=11)
+    cu = torch.tensor(cu, dtype=torch.int32, device="cuda")
+    out, dx = (torch.full((104, 64), 7.0, device="cuda") for _ in range(2))
+    state = torch.zeros(3, 3, 64, device="cuda")
+    flexattn.conv_fwd(x["x"], x["w"], cu, bias=x["bias"], state=state, out=out[32:72], want_state=True)
+    flexattn.conv_bwd(x["x"], x["w"], cu, x["dout"], bias=x["bias"], dx=dx[32:72])
+    for t in (out, dx):
+        assert (t[:32] == 7).all() and (t[72:] == 7).all()

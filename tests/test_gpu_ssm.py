@@ -316,3 +316,37 @@ def test_outputs_over_their_inputs():
     up = x["dout"].clone()
     got = flexattn.ssm_bwd(*_five(x), cu, up, save, **_opt(x), dx=up)
     assert all(torch.equal(a, b) for a, b in zip(got, grads))
+
+
+def test_steps_of_zero_change_nothing():
+    """Tokens of step 0 leave the state bit for bit, however many and wherever a tile ends; so does a
+    single one."""
+    lens = (37, 16, 1)
+    x = ssm_inputs(lens, 72, 16, 1, F32, seed=17)
+    x["dt"].fill_(float("-inf"))
+    state = torch.randn(3, 72, 16, device="cuda")
+    _, last = _fwd(x, offsets(lens), state=state)
+    assert torch.equal(last, state)
+    tok = {n: (t[:3].clone() if n in ("x", "dt", "B", "C", "z") else t) for n, t in x.items()}
+    S = state.clone()
+    flexattn.ssm_decode(*_five(tok), S, **_opt(tok))
+    assert torch.equal(S, state)
+
+
+@pytest.mark.parametrize("cu", [(3, 10, 4, 40), (-5, 7, 900, 40), (0, 50, 20, 33)], ids=str)
+def test_offsets_that_are_none(cu):
+    """Whatever the offsets hold, nothing outside the tensors is touched: the rows around stay."""
+    x = ssm_inputs((40,), 64, 16, 1, F32, seed=18)
+    cu = torch.tensor(cu, dtype=torch.int32, device="cuda")
+    wide = {n: torch.full((40 + 64, *s), 7.0, device="cuda") for n, s in (
+        ("out", (64,)), ("dx", (64,)), ("ddt", (64,)), ("dz", (64,)), ("dB", (1, 16)), ("dC", (1, 16)))}
+    mid = {n: t[32:72] for n, t in wide.items()}
+    state = torch.zeros(3, 64, 16, device="cuda")
+    save = flexattn.ssm_save(x["x"], x["B"], cu)
+    save.zero_()
+    _fwd(x, cu, out=mid["out"], state=state)
+    _fwd(x, cu, out=mid["out"], want_state=False, save=save)
+    mid.pop("out")
+    flexattn.ssm_bwd(*_five(x), cu, x["dout"], save, **_opt(x), **mid)
+    for n, t in wide.items():
+        assert (t[:32] == 7).all() and (t[72:] == 7).all(), n

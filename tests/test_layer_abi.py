@@ -65,7 +65,7 @@ def test_ssm_bad_shapes(lib, kw):
 
 
 @pytest.mark.parametrize("kw", [dict(N=4), dict(N=24), dict(N=64), dict(D=68, x_stride=72, dt_stride=72),
-                                dict(n=65536), dict(T=(1 << 30) + 1), dict(D=65544)], ids=str)
+                                dict(n=65536), dict(T=1 << 30), dict(D=65544)], ids=str)
 def test_ssm_unsupported_shapes(lib, kw):
     s = _ssm(**kw)
     assert _fwd(lib, s) == _bwd(lib, s) == _token(lib, s) == FLEX_EUNSUPPORTED
@@ -156,7 +156,8 @@ def _conv_calls(lib, s, n=BIG, **kw):
     (dict(n=0), FLEX_EINVAL), (dict(T=0), FLEX_EINVAL), (dict(D=0), FLEX_EINVAL), (dict(W=0), FLEX_EINVAL),
     (dict(dtype=3), FLEX_EINVAL), (dict(x_stride=56), FLEX_EINVAL), (dict(x_stride=66), FLEX_EINVAL),
     (dict(W=1), FLEX_EUNSUPPORTED), (dict(W=5), FLEX_EUNSUPPORTED), (dict(D=60), FLEX_EUNSUPPORTED),
-    (dict(n=65536), FLEX_EUNSUPPORTED), (dict(D=65544), FLEX_EUNSUPPORTED)], ids=str)
+    (dict(n=65536), FLEX_EUNSUPPORTED), (dict(T=1 << 30), FLEX_EUNSUPPORTED),
+    (dict(D=65544), FLEX_EUNSUPPORTED)], ids=str)
 def test_conv_shapes(lib, kw, status):
     s = _conv(**kw)
     assert _conv_calls(lib, s) == [status] * 3
@@ -202,7 +203,8 @@ def _norm(**kw):
     (dict(dtype=-1), FLEX_EINVAL), (dict(eps=-1.0), FLEX_EINVAL), (dict(eps=float("nan")), FLEX_EINVAL),
     (dict(x_stride=248), FLEX_EINVAL), (dict(z_stride=260), FLEX_EINVAL), (dict(res_stride=0), FLEX_EINVAL),
     (dict(d=60), FLEX_EUNSUPPORTED), (dict(H=1, d=8200, x_stride=8200), FLEX_EUNSUPPORTED),
-    (dict(H=1025), FLEX_EUNSUPPORTED), (dict(T=1 << 30, H=2), FLEX_EUNSUPPORTED)], ids=str)
+    (dict(H=1025), FLEX_EUNSUPPORTED), (dict(T=1 << 30), FLEX_EUNSUPPORTED),
+    (dict(T=(1 << 30) - 1, H=3), FLEX_EUNSUPPORTED)], ids=str)
 def test_norm_shapes(lib, kw, status):
     s = _norm(**kw)
     assert _plain_call(lib.flex_norm_fwd, NORM_FWD, s) == status
