@@ -31,7 +31,7 @@ struct SsmArgs {
     float *part_d;   // [slots][2][D]: dDs, dbias
 };
 
-// Tokens of a block (a multiple of 64), or T + 1 where sequences stay whole.
+// Tokens of a block (64 of them and more, or 32 backward), or T + 1 where sequences stay whole.
 int ssm_rows(const SsmArgs& a, bool backward);
 int ssm_bwd_tiles(const SsmArgs& a);  // blocks of a group's channels in the backward
 cudaError_t launch_ssm_fwd(const SsmArgs& a, cudaStream_t s);        // 1 kernel, cut: 3

@@ -456,13 +456,16 @@ cudaError_t decode_n(const SsmArgs& a, cudaStream_t s)
 // Sequences stay whole where their blocks fill the SMs (8 x 4096, D 2048: 390 us whole, 544 cut);
 // else they are cut, so that there are 8 blocks an SM (8192, D 1280: 4 115 us, 8 107, 12 117).  The
 // backward's are cut in any case: its walk is the longer one, and blocks of sequences of different
-// lengths fill the SMs evenly (8 x 1024, D 2048, training: 2 an SM 533 us, 4 530, 8 502, 12 506).
+// lengths fill the SMs evenly (8 x 1024, D 2048, training: 2 an SM 533 us, 4 530, 8 502, 12 506).  Small
+// batches: blocks of 64 tokens forward (2000, D 512: 23 us, of 32 29, more of them to join), of 32
+// backward (600 tokens of three sequences, D 256, training: 33 us, of 64 42).
 int ssm_rows(const SsmArgs& a, bool backward)
 {
     const long long tiles = (long long)group_tiles(a, 64) * a.G, want = 8LL * kSMs;
     if (!backward && a.n * tiles >= kSMs) return a.T + 1;
     long long rows = (a.T * tiles + want - 1) / want;
-    rows = (rows + 4 * kTile - 1) / (4 * kTile) * (4 * kTile);
+    const int unit = backward ? 32 : 64;
+    rows = (rows + unit - 1) / unit * unit;
     return rows > a.T ? a.T + 1 : (int)rows;
 }
 
