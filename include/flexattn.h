@@ -352,7 +352,7 @@ size_t flex_ssm_save_bytes(const flex_ssm* shape);
  * out may be x or z.  States and sums are fp32.  A NaN in a row of x, dt or B goes on to the later
  * rows of its sequence (of its channel, or its group) and to its last state, one of C or z to its own
  * row's out; other sequences never see it.  Results repeat bit for bit.
- * 1 kernel, or 3 where sequences are cut.  Errors: FLEX_EINVAL, FLEX_EUNSUPPORTED (N, D, or more than
+ * 1 kernel, or 2 or 3 where sequences are cut.  Errors: FLEX_EINVAL, FLEX_EUNSUPPORTED (N, D, or more than
  * 65535 sequences, 65536 channels or 1024 groups), FLEX_EWORKSPACE. */
 int flex_ssm_fwd(const flex_ssm* shape, const void* x, const void* dt, const float* A, const void* B,
                  const void* C, const float* D, const void* z, const float* dt_bias, const int* cu,

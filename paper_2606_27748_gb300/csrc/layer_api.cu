@@ -167,7 +167,8 @@ int flex_ssm_fwd(const flex_ssm* shape, const void* x, const void* dt, const flo
     ssm_layout(&a, false, (char*)ws);
     a.x = x; a.dt = dt; a.A = A; a.B = B; a.C = C; a.Ds = D; a.z = z; a.bias = dt_bias; a.cu = cu;
     a.h0 = S0; a.h1 = S1; a.out = out; a.marks = (float*)save;
-    return counted(a.rows <= a.T ? 3 : 1, flex::launch_ssm_fwd(a, (cudaStream_t)stream));
+    a.joined = flex::ssm_joined(a);
+    return counted(a.rows > a.T ? 1 : a.joined ? 3 : 2, flex::launch_ssm_fwd(a, (cudaStream_t)stream));
 }
 
 int flex_ssm_bwd(const flex_ssm* shape, const void* x, const void* dt, const float* A, const void* B,

@@ -21,6 +21,7 @@ struct SsmArgs {
     int rows;     // tokens of a block; T + 1: sequences are not cut
     float* ends;  // [slots][D][N]: what a block's tokens alone leave behind, then what it starts from
     float* sums;  // [slots][D]: sum of its D_t
+    bool joined;  // ends are joined before the walk
     float* marks; // NULL, or the states ahead of every kMark tokens, [mark slots][D][N]
     // backward
     const void* dout;
@@ -33,8 +34,9 @@ struct SsmArgs {
 
 // Tokens of a block (64 of them and more, or 32 backward), or T + 1 where sequences stay whole.
 int ssm_rows(const SsmArgs& a, bool backward);
+bool ssm_joined(const SsmArgs& a);    // forward
 int ssm_bwd_tiles(const SsmArgs& a);  // blocks of a group's channels in the backward
-cudaError_t launch_ssm_fwd(const SsmArgs& a, cudaStream_t s);        // 1 kernel, cut: 3
+cudaError_t launch_ssm_fwd(const SsmArgs& a, cudaStream_t s);        // 1 kernel, cut: 2, or 3 if joined
 cudaError_t launch_ssm_back_ends(const SsmArgs& a, cudaStream_t s);  // 2
 cudaError_t launch_ssm_bwd(const SsmArgs& a, cudaStream_t s);        // 2 kernels, cut: 4
 cudaError_t launch_ssm_decode(const SsmArgs& a, cudaStream_t s);     // 1

@@ -93,8 +93,28 @@ __global__ void __launch_bounds__(CT / CH * (N / SP) + 2 * CT, MIN) ssm_scan_ker
         A2[c].read(a.A + state + c * N);
 #pragma unroll
         for (int i = 0; i < SP / 2; ++i) A2[c].v[i] = tc::f2_mul(A2[c].v[i], twice(kLog2e));
-        if (MODE == kOut && blocks > 1) h[c].read(a.ends + p.slot * DN + state + c * N);
+        if (MODE == kOut && blocks > 1 && a.joined) h[c].read(a.ends + p.slot * DN + state + c * N);
         else if (MODE == kOut && a.h0) h[c].read(a.h0 + p.s * DN + state + c * N);
+        if (MODE == kOut && p.block > 0 && !a.joined) {  // few blocks: each joins the ends ahead of it
+            for (int j = p.slot - p.block; j < p.slot; j += 4) {
+                States<SP> e[4];
+                float sum[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    e[k].zero();
+                    sum[k] = 0.f;
+                    if (j + k >= p.slot) continue;
+                    e[k].read(a.ends + (size_t)(j + k) * DN + state + c * N);
+                    sum[k] = a.sums[(size_t)(j + k) * a.D + p.c0 + ch + c];
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int i = 0; i < SP / 2; ++i)
+                        if (j + k < p.slot)
+                            h[c].v[i] = tc::f2_fma(ex2_pair(tc::f2_mul(A2[c].v[i], twice(sum[k]))), h[c].v[i], e[k].v[i]);
+            }
+        }
     }
 
     const int q4 = 4 * (tid % CQ), tq = tid / CQ;  // a thread's groups of channels: tokens tq + k NT / CQ
@@ -469,6 +489,11 @@ int ssm_rows(const SsmArgs& a, bool backward)
     return rows > a.T ? a.T + 1 : (int)rows;
 }
 
+// Whether the ends are joined by a kernel of their own: not where no sequence can have more than 24 blocks
+// (5 short prompts, 530 tokens, D 1024: 32 us with it, 28 without), unless S1 is S0, which a sequence's last
+// block may write before the others have read it.
+bool ssm_joined(const SsmArgs& a) { return a.T / a.rows + 1 > 24 || (a.h0 && a.h0 == a.h1); }
+
 static cudaError_t join(const SsmArgs& a, bool back, cudaStream_t s)
 {
     const dim3 grid((unsigned)(((long long)a.D * a.N / 4 + 127) / 128), (unsigned)a.n);
@@ -480,7 +505,7 @@ cudaError_t launch_ssm_fwd(const SsmArgs& a, cudaStream_t s)
     const bool cut = a.rows <= a.T;
     if (cut) {
         cudaError_t e = a.bf16 ? scan_n<__nv_bfloat16>(a, kEnds, false, s) : scan_n<float>(a, kEnds, false, s);
-        if (e == cudaSuccess) e = join(a, false, s);
+        if (e == cudaSuccess && a.joined) e = join(a, false, s);
         if (e != cudaSuccess) return e;
     }
     return a.bf16 ? scan_n<__nv_bfloat16>(a, kOut, cut, s) : scan_n<float>(a, kOut, cut, s);
