@@ -318,7 +318,8 @@ int flex_softattn_fwd(const flex_packed* shape, const void* q, const void* k, co
  * found by the same offsets, fewer than 2^30 of them; rows behind the last sequence are neither read
  * into a result nor written.  Activations may be slices of wider rows (`*_stride` elements from one to the next, at
  * least a row, whole 16-byte units; 16-byte aligned); outputs, gradients and parameters are
- * contiguous.  Parameters and their gradients are fp32. */
+ * contiguous.  Parameters and their gradients are fp32.  A workspace serves one call at a time: calls
+ * that may run side by side, captured graphs among them, have one each. */
 typedef struct {
     int n;         /* sequences, >= 1 */
     int T;         /* rows, >= 1 */
