@@ -316,10 +316,12 @@ int flex_softattn_fwd(const flex_packed* shape, const void* q, const void* k, co
 /* ---- around the recurrence ------------------------------------------------------------
  * What a recurrent layer on packed batches has besides the calls above.  Rows are [T][channels],
  * found by the same offsets, fewer than 2^30 of them; rows behind the last sequence are neither read
- * into a result nor written.  Activations may be slices of wider rows (`*_stride` elements from one to the next, at
- * least a row, whole 16-byte units; 16-byte aligned); outputs, gradients and parameters are
- * contiguous.  Parameters and their gradients are fp32.  A workspace serves one call at a time: calls
- * that may run side by side, captured graphs among them, have one each. */
+ * into a result nor written.  Activations may be slices of wider rows (`*_stride` elements from one to
+ * the next, at least a row, whole 16-byte units; 16-byte aligned).  Outputs, gradients and parameters
+ * are contiguous; an output that starts where an input that is a slice starts is FLEX_EINVAL, since its
+ * rows would replace others that are still to be read.  Parameters and their gradients are fp32.  A
+ * workspace serves one call at a time: calls that may run side by side, captured graphs among them,
+ * have one each. */
 typedef struct {
     int n;         /* sequences, >= 1 */
     int T;         /* rows, >= 1 */
@@ -350,7 +352,7 @@ size_t flex_ssm_save_bytes(const flex_ssm* shape);
  * S0: NULL or [n][D][N] fp32; S1: NULL or the same, receives each sequence's last state (an empty
  * sequence's is its first); S1 may be S0.  save: NULL, or flex_ssm_save_bytes() bytes, 256-byte
  * aligned, filled for flex_ssm_bwd; S0 must then be NULL.
- * out may be x or z.  States and sums are fp32.  A NaN in a row of x, dt or B goes on to the later
+ * out may be x or z where that is no slice.  States and sums are fp32.  A NaN in a row of x, dt or B goes on to the later
  * rows of its sequence (of its channel, or its group) and to its last state, one of C or z to its own
  * row's out; other sequences never see it.  Results repeat bit for bit.
  * 1 kernel, or 2 or 3 where sequences are cut.  Errors: FLEX_EINVAL, FLEX_EUNSUPPORTED (N, D, or more than
@@ -425,7 +427,7 @@ typedef struct {
  * one with the residual sum:
  *   r = x, or res + scale * x;  out = r (mean(r^2) + eps)^(-1/2) w, times silu(z) where z is given.
  * x, z, res, out: [T][H][d]; w, scale: [heads][d] fp32; z, res and scale (only with res) may be NULL.
- * total: [T][H][d], receives r (given exactly when res is; may be res itself, not a slice of it), of
+ * total: [T][H][d], receives r (given exactly when res is; may be res itself where that is no slice), of
  * which out is computed before it is rounded.  rstd: NULL or [T][H] fp32, for flex_norm_bwd.
  * end: NULL, or a device int (cu + n, say): only rows ahead of it are read and written.  One kernel.
  * Errors: FLEX_EINVAL, FLEX_EUNSUPPORTED (d, more than 1024 heads, or 2^31 rows of heads). */

@@ -45,6 +45,20 @@ bool strides(int dtype, std::initializer_list<int> stride, int least)
     return true;
 }
 
+// Whether an output lies over an input that is a slice of wider rows: its rows then replace others that
+// are still to be read.  Over an input of contiguous rows every value is read before it is replaced.
+struct Rows {
+    const void* p;
+    int stride;
+};
+bool over_slice(std::initializer_list<const void*> outs, std::initializer_list<Rows> ins, int row, int rows)
+{
+    for (const void* o : outs)
+        for (const Rows& i : ins)
+            if (o && o == i.p && rows > 1 && i.stride != row) return true;
+    return false;
+}
+
 int make_ssm(const flex_ssm* s, bool z, flex::SsmArgs* a)
 {
     if (!s || s->n < 1 || s->T < 1 || s->D < 1 || s->G < 1 || s->N < 1) return FLEX_EINVAL;
@@ -162,6 +176,8 @@ int flex_ssm_fwd(const flex_ssm* shape, const void* x, const void* dt, const flo
     if (rc) return rc;
     if (!all16({x, dt, A, B, C, out}) || !opt16({D, z, dt_bias, S0, S1}) || !offsets(cu)) return FLEX_EINVAL;
     if (save && (S0 || !aligned(save, 256))) return FLEX_EINVAL;
+    if (over_slice({out}, {{x, shape->x_stride}, {dt, shape->dt_stride}, {z, shape->z_stride}}, a.D, a.T))
+        return FLEX_EINVAL;
     const size_t need = ssm_layout(&a, false, nullptr);
     if ((rc = check_ws(ws, ws_bytes, need))) return rc;
     ssm_layout(&a, false, (char*)ws);
@@ -184,6 +200,8 @@ int flex_ssm_bwd(const flex_ssm* shape, const void* x, const void* dt, const flo
         return FLEX_EINVAL;
     if (!offsets(cu) || !save || !aligned(save, 256)) return FLEX_EINVAL;
     if (!D != !dD || !z != !dz || !dt_bias != !ddt_bias) return FLEX_EINVAL;
+    if (over_slice({dx, ddt, dz}, {{x, shape->x_stride}, {dt, shape->dt_stride}, {z, shape->z_stride}}, a.D, a.T))
+        return FLEX_EINVAL;
     const size_t need = ssm_layout(&a, true, nullptr);
     if ((rc = check_ws(ws, ws_bytes, need))) return rc;
     ssm_layout(&a, true, (char*)ws);
@@ -202,6 +220,8 @@ int flex_ssm_decode(const flex_ssm* shape, const void* x, const void* dt, const 
     if (rc) return rc;
     if (a.T != a.n) return FLEX_EINVAL;
     if (!all16({x, dt, A, B, C, S, out}) || !opt16({D, z, dt_bias})) return FLEX_EINVAL;
+    if (over_slice({out}, {{x, shape->x_stride}, {dt, shape->dt_stride}, {z, shape->z_stride}}, a.D, a.T))
+        return FLEX_EINVAL;
     a.x = x; a.dt = dt; a.A = A; a.B = B; a.C = C; a.Ds = D; a.z = z; a.bias = dt_bias;
     a.h1 = S; a.out = out;
     return counted(1, flex::launch_ssm_decode(a, (cudaStream_t)stream));
@@ -250,6 +270,7 @@ int flex_conv_decode(const flex_conv* shape, const void* x, const float* w, cons
     if (rc) return rc;
     if (a.T != a.n) return FLEX_EINVAL;
     if (!all16({x, w, S, out}) || !opt16({bias})) return FLEX_EINVAL;
+    if (over_slice({out}, {{x, shape->x_stride}}, a.D, a.T)) return FLEX_EINVAL;
     a.x = x; a.w = w; a.bias = bias; a.S1 = S; a.out = out;
     return counted(1, flex::launch_conv_decode(a, (cudaStream_t)stream));
 }
@@ -270,6 +291,9 @@ int flex_norm_fwd(const flex_norm* shape, const void* x, const float* w, const v
     if (!all16({x, w, out}) || !opt16({z, res, scale, total}) || !aligned(end, 4) || !aligned(rstd, 4))
         return FLEX_EINVAL;
     if (!res != !total || (scale && !res)) return FLEX_EINVAL;
+    if (over_slice({out, total}, {{x, shape->x_stride}, {z, shape->z_stride}, {res, shape->res_stride}},
+                   a.H * a.d, a.T))
+        return FLEX_EINVAL;
     a.x = x; a.w = w; a.z = z; a.res = res; a.scale = scale; a.end = end;
     a.out = out; a.total = total; a.rstd = rstd;
     return counted(1, flex::launch_norm_fwd(a, (cudaStream_t)stream));
@@ -288,6 +312,9 @@ int flex_norm_bwd(const flex_norm* shape, const void* x, const float* w, const v
     if (!res != !dres || !z != !dz || !scale != !dscale || (scale && !res) || (dtotal && !res))
         return FLEX_EINVAL;
     if (!dx != (res && !scale)) return FLEX_EINVAL;  // (without a scale dres is dx too)
+    if (over_slice({dx, dres, dz}, {{x, shape->x_stride}, {z, shape->z_stride}, {res, shape->res_stride}},
+                   a.H * a.d, a.T))
+        return FLEX_EINVAL;
     if ((rc = check_ws(ws, ws_bytes, kHeader + floats(flex::norm_part_floats(a))))) return rc;
     a.x = x; a.w = w; a.z = z; a.res = res; a.scale = scale; a.end = end; a.rstd = const_cast<float*>(rstd);
     a.dout = dout; a.dtotal = dtotal; a.dx = dx; a.dres = dres; a.dz = dz; a.dw = dw; a.dscale = dscale;

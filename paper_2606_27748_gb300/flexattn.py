@@ -570,7 +570,8 @@ def softattn_fwd(q, k, v, cu_q, cu_k=None, causal=True, scale=None, out=None, ls
 
 # ---- around the recurrence: rows [T, channels] of packed sequences ----------------------
 #
-# Activations may be slices of wider rows; parameters are fp32 and contiguous.
+# Activations may be slices of wider rows, of which no output may then take the place; parameters are
+# fp32 and contiguous.
 
 def _row_stride(t, what, shape, dtype, dev):
     """The row stride of a tensor of this shape and type on device `dev` whose rows are contiguous

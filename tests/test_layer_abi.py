@@ -253,3 +253,67 @@ def test_conv_and_norm_bindings_refuse():
             flexattn._packed_norm(*args, 1e-6, cpu)
     with pytest.raises(ValueError):
         flexattn._plain(torch.zeros(65), "w", flexattn._params(p, s), torch.float32, cpu)
+
+
+# ---- outputs over their inputs ---------------------------------------------------------------
+
+def _apart(names):
+    return {n: ctypes.c_void_p((1 << 20) + 4096 * i) for i, n in enumerate(names)}
+
+
+def _over(call, names, pairs, strides, make, rows):
+    """Every output over an input: refused where the input is a slice of wider rows, by any of
+    several rows; `call` gets one byte of workspace too little, so no launch is reached."""
+    for out, inp in pairs:
+        at = _apart(names)
+        at[out] = at[inp]
+        wide = {strides[inp]: 2 * make()[strides[inp]]}
+        assert call(make(**wide), at) == FLEX_EINVAL, (out, inp)
+        if rows:  # a single row, and rows of no wider ones, are in place
+            assert call(make(), at) == FLEX_EWORKSPACE, (out, inp)
+            assert call(make(**wide, **rows), at) == FLEX_EWORKSPACE, (out, inp)
+
+
+def test_ssm_output_over_a_slice(lib):
+    def make(**kw):
+        return {**dict(n=3, T=100, D=64, G=1, N=16, dtype=1, softplus=1, x_stride=64, dt_stride=64,
+                       b_stride=16, c_stride=16, z_stride=64), **kw}
+
+    def fwd(kw, at):
+        s = FlexSsm(*kw.values())
+        need = lib.flex_ssm_workspace_bytes(ctypes.byref(s), 0)
+        return _fwd(lib, s, n=need - 1, **{**at, "S0": None})
+
+    def bwd(kw, at):
+        s = FlexSsm(*kw.values())
+        need = lib.flex_ssm_workspace_bytes(ctypes.byref(s), 1)
+        return _bwd(lib, s, n=need - 1, **at)
+
+    strides = {"x": "x_stride", "dt": "dt_stride", "z": "z_stride"}
+    one = dict(n=1, T=1)
+    _over(fwd, FWD, [("out", i) for i in strides], strides, make, one)
+    _over(bwd, BWD, [(o, i) for o in ("dx", "ddt", "dz") for i in strides], strides, make, one)
+    token = lambda kw, at: _token(lib, FlexSsm(*kw.values()), **at)  # noqa: E731
+    _over(token, TOKEN, [("out", i) for i in strides], strides, lambda **kw: make(T=3, **kw), None)
+
+
+def test_conv_token_over_a_slice(lib):
+    make = lambda **kw: {**dict(n=3, T=3, D=64, W=4, dtype=1, silu=1, x_stride=64), **kw}  # noqa: E731
+    token = lambda kw, at: _plain_call(lib.flex_conv_decode, CONV_TOKEN, FlexConv(*kw.values()), **at)  # noqa: E731
+    _over(token, CONV_TOKEN, [("out", "x")], {"x": "x_stride"}, make, None)
+
+
+def test_norm_output_over_a_slice(lib):
+    def make(**kw):
+        return {**dict(T=100, H=4, d=64, dtype=1, heads=1, x_stride=256, z_stride=256, res_stride=256,
+                       eps=1e-6), **kw}
+
+    def bwd(kw, at):
+        s = FlexNorm(*kw.values())
+        need = lib.flex_norm_workspace_bytes(ctypes.byref(s))
+        return _plain_call(lib.flex_norm_bwd, NORM_BWD, s, need - 1, **at)
+
+    strides = {"x": "x_stride", "z": "z_stride", "res": "res_stride"}
+    fwd = lambda kw, at: _plain_call(lib.flex_norm_fwd, NORM_FWD, FlexNorm(*kw.values()), **at)  # noqa: E731
+    _over(fwd, NORM_FWD, [(o, i) for o in ("out", "total") for i in strides], strides, make, None)
+    _over(bwd, NORM_BWD, [(o, i) for o in ("dx", "dres", "dz") for i in strides], strides, make, dict(T=1))
