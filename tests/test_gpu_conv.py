@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2606_27748_gb300 import flexattn
-from layer_ref import BF16, F32, CONV, close, close_each, conv_inputs, conv_ref, gradients
+from layer_ref import BF16, F32, CONV, close, close_each, conv_inputs, conv_ref, gradients, silu
 from packed_ref import offsets
 
 pytestmark = pytest.mark.gpu
@@ -188,3 +188,42 @@ def test_offsets_that_are_none(cu):
     flexattn.conv_bwd(x["x"], x["w"], cu, x["dout"], bias=x["bias"], dx=dx[32:72])
     for t in (out, dx):
         assert (t[:32] == 7).all() and (t[72:] == 7).all()
+
+
+def _packed_ref(x, lens):
+    """conv_ref's out without a loop over rows: tap W - 1 - k of all rows at once, masked where the row
+    k ahead lies in the sequence ahead."""
+    v, w = x["x"].double(), x["w"].double()
+    at = torch.cat([torch.arange(n) for n in lens]).to(v.device)[:, None]
+    W = w.shape[1]
+    p = sum(torch.where(at >= k, torch.roll(v, k, 0), 0.0) * w[:, W - 1 - k] for k in range(W))
+    return silu(p + x["bias"].double())
+
+
+# Rows of a thread's run, by rows x channels: 8, 16 and 32 (4 above).  Sequences end inside runs and
+# batches of rows, at their first and last rows among others.
+RUNS = [(8, 2048, (1203, 1, 2, 0, 3, 777, 515)), (8, 1032, (2403, 8, 1, 1, 2, 0, 1500, 1093)),
+        (16, 2048, (2403, 1, 1, 2, 0, 1500, 16, 1093)), (32, 2048, (4097, 5, 0, 1, 2903, 31, 670, 97, 1, 1, 2192))]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("W", [2, 3, 4])
+@pytest.mark.parametrize("run,D,lens", RUNS, ids=str)
+def test_long_runs(run, D, lens, W, dtype):
+    """All outputs of batches large enough for runs of 8 rows and more, where most rows are taken without
+    looking at the offsets.  Sums over 10000 rows are off by sqrt(10000) 2^-24 = 6e-6 of a typical sum if
+    they were one chain, a third of the bound."""
+    x = conv_inputs(lens, D, W, dtype, seed=12, pad=8)
+    cu = offsets(lens)
+    ws = flexattn.conv_workspace(x["x"], x["w"], cu)
+    assert (ws.numel() - 256) // (4 * (W + 1) * D) == -(-sum(lens) // (8 * run))
+    out, last = flexattn.conv_fwd(x["x"], x["w"], cu, bias=x["bias"], want_state=True)
+    close_each(out, _packed_ref(x, lens), lens, "out")
+    for i, end in enumerate(cu[1:].tolist()):
+        n = min(lens[i], W - 1)
+        assert torch.equal(last[i, W - 1 - n:], x["x"][end - n:end]) and (last[i, :W - 1 - n] == 0).all()
+    got = flexattn.conv_bwd(x["x"], x["w"], cu, x["dout"], bias=x["bias"], ws=ws)
+    ref = gradients(lambda v: [_packed_ref(v, lens)], x, CONV, [x["dout"]])
+    close_each(got[0], ref[0], lens, "dx")
+    close(got[1], ref[1], "dw")
+    close(got[2], ref[2], "dbias")
