@@ -149,3 +149,34 @@ def test_gradients_against_differences():
         up, down = ({**x, name: x[name].double() + s * way} for s in (1e-5, -1e-5))
         slope = (loss(up) - loss(down)) / 2e-5
         assert abs(float((g.double() * way).sum()) - slope) <= 2e-5 * float(g.double().norm() * way.norm()), name
+
+
+# More than two rounds of every group of threads, at each number of threads a group (past 32 with block
+# barriers between) and of 16-byte units a thread.
+ROUNDS = [(BF16, 2600, 1, 512), (BF16, 1300, 1, 1000), (BF16, 650, 2, 2048), (BF16, 700, 1, 4096),
+          (BF16, 620, 1, 8192), (F32, 650, 2, 1024), (F32, 700, 1, 2048), (F32, 620, 1, 4096),
+          (F32, 310, 2, 8192)]
+
+
+@pytest.mark.parametrize("form", FORMS, ids=lambda f: "-".join(f) or "plain")
+@pytest.mark.parametrize("own", [False, True], ids=["shared", "own"])
+@pytest.mark.parametrize("dtype,T,H,d", ROUNDS, ids=str)
+def test_many_rounds(dtype, T, H, d, own, form):
+    x = norm_inputs(T, H, d, dtype, heads=H if own else None, seed=7, pad=8, **form)
+    out, total, rstd = _fwd(x, want_rstd=True)
+    _check(x, out, total, _bwd(x, rstd))
+
+
+@pytest.mark.parametrize("dtype,T,H,d", ROUNDS, ids=str)
+def test_rounds_that_some_groups_sit_out(dtype, T, H, d):
+    """The last sequence ends where a part of a block's groups, or of the blocks, has a row left."""
+    x = norm_inputs(T, H, d, dtype, heads=H, gate=True, res=True, scale=True, seed=8)
+    for rows in (T - 7, T // 2 + 1, 1):
+        y = {n: t.clone() if n in ("x", "res", "z", "dout", "dtotal") else t for n, t in x.items()}
+        for n in ("x", "res", "z", "dout", "dtotal"):
+            y[n][rows:] = float("nan")
+        cu = offsets((rows,))
+        out, total, rstd = _fwd(y, cu=cu, want_rstd=True)
+        got = _bwd(y, rstd, cu=cu)
+        z = {n: t[:rows] if n in ("x", "res", "z", "dout", "dtotal") else t for n, t in x.items()}
+        _check(z, out[:rows], total[:rows], [g[:rows] if g.dim() == 3 else g for g in got])
