@@ -350,3 +350,32 @@ def test_offsets_that_are_none(cu):
     flexattn.ssm_bwd(*_five(x), cu, x["dout"], save, **_opt(x), **mid)
     for n, t in wide.items():
         assert (t[:32] == 7).all() and (t[72:] == 7).all(), n
+
+
+# Tokens x blocks of 64 channels large enough for blocks of more than 32 tokens backward (64, 64, 64, 96) and
+# forward of 128 (the last; the others stay whole), with sequences of one and of many blocks.
+LARGE = [(2048, 16, 2, (900, 1, 0, 333, 64, 202)), (2048, 8, 1, (1211, 1, 1, 1, 287)),
+         (2048, 32, 4, (65, 700, 3, 128, 604)), (4096, 16, 1, (1203, 97))]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("D,N,G,lens", LARGE, ids=str)
+def test_blocks_of_more_tokens(D, N, G, lens, dtype):
+    x = ssm_inputs(lens, D, N, G, dtype, seed=19, pad=8)
+    out, got = _train(x, offsets(lens))
+    _, last = _fwd(x, offsets(lens))
+    ref, rlast = ssm_ref(x, lens)
+    close_each(out, ref, lens, "out")
+    close(last, rlast, "last states")
+    _check_grads(got, x, lens)
+
+
+def test_nan_of_c_stays_in_its_row():
+    lens = (20, 30, 10)
+    x = ssm_inputs(lens, 64, 16, 1, BF16, seed=7)
+    cu = offsets(lens)
+    clean, last = _fwd(x, cu)
+    x["C"][25] = float("nan")
+    out, l2 = _fwd(x, cu)
+    assert torch.isnan(out[25]).all() and torch.equal(l2, last)
+    assert torch.equal(out[:25], clean[:25]) and torch.equal(out[26:], clean[26:])
