@@ -339,7 +339,9 @@ typedef struct {
 
 /* Workspace bytes of flex_ssm_fwd (backward = 0) or of both flex_ssm_fwd and flex_ssm_bwd
  * (backward = 1), and of the buffer that flex_ssm_fwd leaves for flex_ssm_bwd; 0 if the shape is
- * invalid or unsupported. */
+ * invalid or unsupported.  The buffer is (T / 8 + n) D N floats: 8 bytes a channel of a row at 16 states,
+ * and D N floats for a sequence however short.  A workspace is at most (T / 64 + n) D (N + 1) floats;
+ * backward at most 2 (T / 32 + n) D (N + 2), and 2 N floats a row for every 64 channels (32 at N = 32). */
 size_t flex_ssm_workspace_bytes(const flex_ssm* shape, int backward);
 size_t flex_ssm_save_bytes(const flex_ssm* shape);
 

@@ -7,7 +7,10 @@
 // once.  The backward's groups stay with their head and walk rows, keeping sums for dw and dscale, with
 // the rows ahead on their way to shared memory.  32768 x 16 heads of 128 with the gate: 71 us, 5.7 TB/s
 // (1 unit of 16 bytes a thread instead of 2: 80); 16384 rows of 2048 with the residual sum: 47 us, and
-// gradients 66 for 403 MB (88 with one row ahead in registers).
+// gradients 66 for 403 MB (88 with one row ahead in registers).  A backward row of more than 256 units (2048
+// elements in bf16, 1024 in fp32) is 2 to 8 units a thread, 8 warps an SM in bf16, whose parameters are
+// loaded again for every row: the same 403 MB as rows of 4096 take its two kernels 115 us, of 8192 107 (72 as
+// rows of 2048).
 #include "flex_internal.h"
 #include "layer.cuh"
 

@@ -434,8 +434,10 @@ cudaError_t scan(const SsmArgs& a, int mode, bool after, cudaStream_t s)
 {
     using Y = Layout<T, N, CH, SP, CT>;
     const long long blocks = (long long)block_slots(a.T, a.n, a.rows) * group_tiles(a, CT) * a.G;
-    // Whole sequences have fewer blocks than fit: registers for loads ahead (8 x 4096, D 2048: 386 us,
-    // 408 at 3 blocks an SM); blocks of them run 3 an SM (8192, D 1280: 107 us, 113 at 2).
+    // Whole sequences: registers for loads ahead, which at 16 states leaves 2 blocks an SM; a few long
+    // sequences do not fill those (8 x 4096, D 2048: 384 us, 406 at 3), and where more blocks wait it costs
+    // little (64 x 512: 338 us, 330 at 3).  Blocks of sequences run 3 an SM (8192, D 1280: 107 us, 113 at
+    // 2); in fp32 shared memory, 87 KB a block, holds 2 all the same, and 32 states' 384 threads 1.
     constexpr int MIN = N <= 16 ? 3 : 1;
     auto kernel = mode == kEnds ? ssm_scan_kernel<T, N, CH, SP, CT, kEnds, MIN>
                 : mode == kBack ? ssm_scan_kernel<T, N, CH, SP, CT, kBack, MIN>
@@ -479,6 +481,10 @@ cudaError_t decode_n(const SsmArgs& a, cudaStream_t s)
 // lengths fill the SMs evenly (8 x 1024, D 2048, training: 2 an SM 533 us, 4 530, 8 502, 12 506).  Small
 // batches: blocks of 64 tokens forward (2000, D 512: 23 us, of 32 29, more of them to join), of 32
 // backward (600 tokens of three sequences, D 256, training: 33 us, of 64 42).
+// The forward's rule sees how many sequences there are, empty ones among them, and not their lengths, which
+// the host does not know: one far longer than the others then keeps few blocks busy (8192 tokens and four of
+// 1, D 2048: 463 us, as 8196 tokens of one sequence, cut, 156; 25 documents of 1 to 5003 tokens 291 us, as
+// many tokens in 8 of one length 158).
 int ssm_rows(const SsmArgs& a, bool backward)
 {
     const long long tiles = (long long)group_tiles(a, 64) * a.G, want = 8LL * kSMs;
@@ -490,8 +496,8 @@ int ssm_rows(const SsmArgs& a, bool backward)
 }
 
 // Whether the ends are joined by a kernel of their own: not where no sequence can have more than 24 blocks
-// (5 short prompts, 530 tokens, D 1024: 32 us with it, 28 without), unless S1 is S0, which a sequence's last
-// block may write before the others have read it.
+// (5 short prompts, 530 tokens, D 1024, captured: 17 us with it, 15 without), unless S1 is S0, which a
+// sequence's last block may write before the others have read it.
 bool ssm_joined(const SsmArgs& a) { return a.T / a.rows + 1 > 24 || (a.h0 && a.h0 == a.h1); }
 
 static cudaError_t join(const SsmArgs& a, bool back, cudaStream_t s)
